@@ -20,6 +20,12 @@
  *                    visible to every row (Sec. 3.2, C_full in App. C): the
  *                    baseline the cache is measured against.
  *
+ * For training the students that the paper distils (Sec. 3.4), and for the block
+ * around the attention: the three calls' gradients (*_backward), the way from a
+ * projection's rows to the attention's q, k and v (refcache_qkv_rope), the gated
+ * residual with the norm behind it (refcache_gated_norm), both with their
+ * gradients, and the clipping of gradients (refcache_clip_gradients).
+ *
  * Conventions shared by every entry point
  *   - Tensors are THD: [tokens, num_heads, head_dim] bf16, head_dim
  *     contiguous, rows of consecutive requests packed back to back.  Base
@@ -310,6 +316,191 @@ REFCACHE_API int full_attention(int batch, int num_heads, int head_dim, const in
 REFCACHE_API int full_attention_noalloc(int batch, int num_heads, int head_dim, const int32_t* cu_seqlens,
                                         const void* q, const void* k, const void* v, void* o, float* lse,
                                         float softmax_scale, void* stream);
+
+/* ---- gradients of the attention calls -------------------------------------
+ *
+ * With P = exp(scale Q K^T - lse), recomputed from the log-sum-exp that the
+ * forward call wrote:
+ *   dV = P^T dO, dP = dO V^T, dS = P (dP - rowsum(dO O)), dQ = scale dS K,
+ *   dK = scale dS^T Q
+ * over exactly the pairs that the forward call attends.  Shared conventions:
+ *   - q, k, v, o, lse: inputs and outputs of the forward call; d_o: the gradient
+ *     of o.  dq, dk, dv are written (not added to).  All bf16, like the forward
+ *     call's tensors, except lse (fp32 [rows, H], not optional here).
+ *   - Scores, P, dP, dS and all sums are fp32; P and dS are rounded to bf16 as
+ *     operands of their products, gradients once when they are written.
+ *   - Every sum has one place and one order: the same inputs give the same bits,
+ *     and a request's gradients do not depend on the rest of the batch.
+ *   - work: refcache_backward_bytes(rows, H) bytes of device memory, 16-byte
+ *     aligned, overwritten; free again when the call's work on the stream is done.
+ *   - Every q, k, v, o, d_o row must hold finite values, as in the forward calls.
+ *   - They launch kernels only (two chains of three at most for every 32
+ *     requests), so they can be captured in a CUDA graph, after a first call on
+ *     the device outside the capture.
+ *   - Outputs must not overlap inputs.
+ */
+REFCACHE_API size_t refcache_backward_bytes(int64_t rows, int num_heads);
+
+/*
+ * Gradient of step_attention: rows = cu_live[batch].  dk_live, dv_live are the
+ * gradients of the live rows' own keys; dk_ref, dv_ref [cached rows, H, d] bf16
+ * (the slots' row order, refcache_kv_ptr) those of the cached rows, or both NULL
+ * when the cache takes no gradient (their work is then left out).  With
+ * accumulate != 0 the call adds to what dk_ref and dv_ref hold (several denoising
+ * steps of one rollout share a cache; the sum is rounded to bf16 at each call).
+ * A bf16 cache; REFCACHE_ERR_UNSUPPORTED for an E4M3 cache, whose quantisation has
+ * no gradient, REFCACHE_ERR_NOT_BUILT for a layer that was never built.
+ */
+REFCACHE_API int step_attention_backward(refcache_t* cache, int layer, const void* q_live, const void* k_live,
+                                         const void* v_live, const void* o_live, const float* lse_live,
+                                         const void* do_live, void* dq_live, void* dk_live, void* dv_live, void* dk_ref,
+                                         void* dv_ref, int accumulate, void* work, float softmax_scale, void* stream);
+
+/*
+ * Gradient of refcache_build: rows = cu_static[batch], under the cache's mask
+ * mode.  dk_ref, dv_ref (NULL, or [cached rows, H, d] bf16 from
+ * step_attention_backward) are added to the cached rows' gradients before they
+ * are rounded: the cached K and V are the static rows' own.  Reads no slot of the
+ * cache (`layer` is only checked), so the layer may have been rebuilt since.
+ */
+REFCACHE_API int refcache_build_backward(refcache_t* cache, int layer, const void* q_static, const void* k_static,
+                                         const void* v_static, const void* o_static, const float* lse_static,
+                                         const void* do_static, void* dq_static, void* dk_static, void* dv_static,
+                                         const void* dk_ref, const void* dv_ref, void* work, float softmax_scale,
+                                         void* stream);
+
+/* Gradient of full_attention (and full_attention_noalloc); capturable, allocates nothing. */
+REFCACHE_API int full_attention_backward(int batch, int num_heads, int head_dim, const int32_t* cu_seqlens,
+                                         const void* q, const void* k, const void* v, const void* o, const float* lse,
+                                         const void* d_o, void* dq, void* dk, void* dv, void* work, float softmax_scale,
+                                         void* stream);
+
+/* ---- from a projection to the attention's q, k and v ----------------------
+ *
+ * Per head RMS norm of query and key and rotary positions with several axes
+ * (frame, height and width of image tokens, for instance):
+ *   n = x / sqrt(mean(x^2) + eps) * weight        (weight NULL: n = x)
+ *   (a, b) -> (a cos t - b sin t, a sin t + b cos t) for each pair of n,
+ *   t = position[axis of the pair] * theta^(-2 j / axis_dim), j = its number on the axis
+ * Axis i takes the next axis_dims[i] / 2 pairs; pairs past the axes' dims (their
+ * sum may be below head_dim) are not turned.  Pair j is elements (2 j, 2 j + 1)
+ * when interleaved, else (j, j + head_dim / 2).  Arithmetic in fp32, angles exact
+ * for positions up to 2^24 in magnitude, one rounding to bf16 at the end.
+ */
+#define REFCACHE_ROPE_MAX_AXES 4
+typedef struct {
+  int32_t head_dim, num_axes, interleaved;
+  float turn_hi[64], turn_lo[64]; /* frequency / (2 pi) of each pair, as a sum of two */
+  uint8_t axis[64];               /* axis of each pair */
+} refcache_rope_t;
+
+/* Fill *rope (host memory, the caller's; needs no device). */
+REFCACHE_API int refcache_rope_init(refcache_rope_t* rope, int head_dim, int num_axes, const int32_t* axis_dims,
+                                    double theta, int interleaved);
+
+/* The rows of one call.  positions, row_map and the weights are device memory. */
+typedef struct {
+  int64_t rows;              /* token rows of q, k and v */
+  int64_t out_rows;          /* rows of q_out, k_out and v_out */
+  int32_t num_heads;
+  int32_t weight_f32;        /* weights fp32 (else bf16) */
+  const int32_t* positions;  /* [rows, num_axes] */
+  const int32_t* row_map;    /* row i goes to row row_map[i] of the outputs (distinct; outside
+                                [0, out_rows): dropped, its gradient is 0); NULL: to row i */
+  const void* weight_q;      /* [head_dim], or NULL: not normalised */
+  const void* weight_k;
+  float eps;
+} refcache_rope_rows_t;
+
+/*
+ * q, k, v: rows of num_heads x head_dim bf16, contiguous within a row, ld elements
+ * between rows (a multiple of 8: a fused projection's [rows, 3, H, d] may be passed
+ * as three tensors).  Outputs: [out_rows, H, d] bf16, packed, as the attention calls
+ * take them; k_out and v_out may be a cache's slots (refcache_kv_ptr), before
+ * refcache_build_in_slot.  v is moved only.  Each of the three may be NULL together
+ * with its output.  Output rows that no row goes to are left as they are.
+ */
+REFCACHE_API int refcache_qkv_rope(const refcache_rope_t* rope, const refcache_rope_rows_t* rows, const void* q,
+                                   int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v, void* q_out,
+                                   void* k_out, void* v_out, void* stream);
+
+/*
+ * Its gradient: from those of the outputs ([out_rows, H, d] packed) to dq, dk, dv
+ * (rows with ld elements between them) and the weights' (fp32 [head_dim], may be
+ * NULL).  q and k are the forward call's inputs, read where they were normalised.
+ * work: refcache_qkv_rope_backward_bytes bytes of device memory, needed with a
+ * weight.  The weights' sums are taken in a fixed order.
+ */
+REFCACHE_API size_t refcache_qkv_rope_backward_bytes(const refcache_rope_t* rope);
+REFCACHE_API int refcache_qkv_rope_backward(const refcache_rope_t* rope, const refcache_rope_rows_t* rows, const void* q,
+                                            int64_t ld_q, const void* k, int64_t ld_k, const void* dq_out,
+                                            const void* dk_out, const void* dv_out, void* dq, int64_t ld_dq, void* dk,
+                                            int64_t ld_dk, void* dv, int64_t ld_dv, float* dweight_q, float* dweight_k,
+                                            void* work, void* stream);
+
+/* ---- gated residual and norm ----------------------------------------------
+ *
+ * The end of one half of a transformer block and the start of the next, for rows
+ * of `width` bf16 (a multiple of 8, at most 8192), packed, requests back to back:
+ *   h = branch, or post_norm(branch) * post_weight
+ *   x_out = x + gate * h                            (no branch: x)
+ *   y = norm(x_out) * weight * (1 + scale) + shift  (before x_out is rounded)
+ * gate, scale and shift are rows of the request (ld elements between requests'
+ * rows, a multiple of 8); gate NULL is 1, scale and shift NULL are 0, weights NULL
+ * are 1.  Layer norm: (x - mean) / sqrt(var + eps); RMS norm: x / sqrt(mean(x^2) +
+ * eps).  Statistics and arithmetic in fp32.
+ */
+#define REFCACHE_NORM_NONE 0
+#define REFCACHE_NORM_LAYER 1
+#define REFCACHE_NORM_RMS 2
+typedef struct {
+  int32_t batch;
+  int32_t width;
+  const int32_t* cu_rows;   /* HOST [batch + 1]: first row of each request, cu_rows[0] = 0 */
+  int32_t norm, post_norm;  /* REFCACHE_NORM_* */
+  int32_t mod_f32;          /* gate, scale, shift and the weights are fp32 (else bf16) */
+  float eps;
+  const void *gate, *scale, *shift; /* device, [batch, width] with ld_* */
+  int64_t ld_gate, ld_scale, ld_shift;
+  const void *weight, *post_weight; /* device, [width] */
+} refcache_gated_norm_t;
+
+/* x, branch (may be NULL): [rows, width] bf16.  x_out (may be NULL, or x itself) and y (may be NULL) are written. */
+REFCACHE_API int refcache_gated_norm(const refcache_gated_norm_t* p, const void* x, const void* branch, void* x_out,
+                                     void* y, void* stream);
+
+/*
+ * Its gradient.  x_out: the forward call's output (its x where there is no
+ * branch), needed with dy; dy, dx_out: gradients of y and x_out, either may be
+ * NULL for zero, not both.  Written, each unless NULL: dx, d_branch [rows, width] bf16;
+ * d_gate, d_scale, d_shift fp32 [batch, width]; d_weight, d_post_weight fp32 [width].
+ * The statistics are found again from x_out and branch.  Column sums are fp32, in a
+ * fixed order for a given device.  work: refcache_gated_norm_backward_bytes(p)
+ * bytes of device memory, 16-byte aligned.
+ */
+REFCACHE_API size_t refcache_gated_norm_backward_bytes(const refcache_gated_norm_t* p);
+REFCACHE_API int refcache_gated_norm_backward(const refcache_gated_norm_t* p, const void* x_out, const void* branch,
+                                              const void* dy, const void* dx_out, void* dx, void* d_branch, float* d_gate,
+                                              float* d_scale, float* d_shift, float* d_weight, float* d_post_weight,
+                                              void* work, void* stream);
+
+/* ---- clipping of gradients --------------------------------------------------
+ *
+ * norm = sqrt(sum of squares of all n tensors), out_i = grads_i * min(1, max_norm /
+ * (norm + 1e-6)).  The lists are HOST arrays: device pointers, element counts, and
+ * types[i] = REFCACHE_CLIP_* flags.  Tensors need the alignment of their elements
+ * only.  out NULL: in place (nothing is written where the factor is 1).  norm: device
+ * fp32, may be NULL.  max_norm may be +inf (the norm alone).  A norm that is NaN
+ * makes the outputs NaN; an infinite one makes finite elements 0.  (Squares are summed
+ * in fp32 per thread and in fp64 from there on: the norm is infinite where a
+ * thread's squares overflow fp32.)  work: refcache_clip_gradients_bytes(n) bytes of
+ * device memory, 16-byte aligned.
+ */
+#define REFCACHE_CLIP_GRAD_F32 1 /* gradient fp32 (else bf16) */
+#define REFCACHE_CLIP_OUT_F32 2  /* output fp32 (else bf16) */
+REFCACHE_API size_t refcache_clip_gradients_bytes(int n);
+REFCACHE_API int refcache_clip_gradients(int n, const void* const* grads, void* const* out, const int64_t* counts,
+                                         const int32_t* types, float max_norm, float* norm, void* work, void* stream);
 
 /*
  * Synchronise `stream`, then read and clear the current device's error word

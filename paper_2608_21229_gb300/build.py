@@ -1,7 +1,8 @@
 """Build the CUDA library (librefcache.so) for sm_103a with nvcc, in-tree.
 
-The library is one translation unit (csrc/refcache.cu, which includes the
-kernels) compiled with ``-gencode arch=compute_103a,code=sm_103a`` and linked
+The library is two translation units, compiled in parallel (csrc/refcache.cu
+with the attention kernels, csrc/block_ops.cu with those of the block around it),
+compiled with ``-gencode arch=compute_103a,code=sm_103a`` and linked
 against the shared CUDA runtime, so that it shares the runtime (and the
 streams) of the host process.
 """
@@ -18,6 +19,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(BUILD_DIR, "librefcache.so")
+UNITS = ("refcache.cu", "block_ops.cu")
 ARCH_FLAGS = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -48,7 +50,7 @@ def nvcc_cmd(out: str, extra=()) -> list:
     return [
         os.path.join(home, "bin", "nvcc"), *ARCH_FLAGS, "-O3", "-lineinfo", "-std=c++17", "-shared",
         "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "--expt-relaxed-constexpr",
-        "-cudart", "shared", f"-I{INCLUDE}", f"-I{CSRC}", os.path.join(CSRC, "refcache.cu"),
+        "-cudart", "shared", f"-I{INCLUDE}", f"-I{CSRC}", "-t", "0", *(os.path.join(CSRC, f) for f in UNITS),
         "-o", out, f"-L{os.path.join(home, 'lib64')}", f"-Xlinker", f"-rpath={os.path.join(home, 'lib64')}",
         *extra,
     ]

@@ -1,0 +1,266 @@
+// qkv_rope.cuh -- from a projection's rows to the attention's q, k and v: per
+// head RMS norm of query and key, rotary positions with several axes, rows moved
+// to where the packed tensors (or the cache's slots) keep them; and its gradient.
+//
+//   n = x / sqrt(mean(x^2) + eps) * w          (w absent: n = x)
+//   (a, b) -> (a cos t - b sin t, a sin t + b cos t)   for each pair of n, with
+//   t = position[axis of the pair] * frequency of the pair
+// Gradient, with g the output's gradient turned back by -t and u = g w:
+//   dx = r u - x r^3 mean(x u),   r = 1 / sqrt(mean(x^2) + eps);   dw = sum over rows and heads of g x r
+//
+// The angle is taken in turns: frequency / 2 pi is held as a sum of two fp32
+// numbers and the product's whole turns are removed before it is rounded, so
+// that the angle is as exact at position 10^6 as at 1 (an fp32 product of
+// position and frequency is off by 2^-24 of the whole angle).  sincospif then
+// needs no range reduction of its own.
+//
+// All of it is bound by memory: every head row is read once and written once.
+// A row of one head is 16 bytes for each of D / 8 lanes, so that a warp holds
+// 32 / (D / 8) heads of one token at a time, the mean takes log2(D / 8)
+// shuffles, and the angles of a token (4 or 8 for each lane) are found once for
+// all its heads.
+#pragma once
+#include "vec8.cuh"
+
+namespace rc {
+
+constexpr int kRopeMaxPairs = 64;
+constexpr int kRopeThreads = 256;
+constexpr int kRopeTokens = kRopeThreads / 32;  // tokens of a block at a time, one per warp
+
+struct RopeTable {
+  float turn_hi[kRopeMaxPairs], turn_lo[kRopeMaxPairs];  // frequency / 2 pi
+  uint8_t axis[kRopeMaxPairs];
+  int32_t num_axes;
+};
+
+struct RopeArgs {
+  const uint16_t* src[3];  // forward: q, k, v; backward: q, k and (unused) v
+  int64_t ld[3];           // elements between their rows
+  uint16_t* dst[3];        // forward: q, k, v out; backward: the gradients of q, k, v
+  int64_t ld_dst[3];
+  const uint16_t* grad[3];  // backward: gradients of the outputs
+  const void* weight[2];    // of q and k, null: not normalised
+  const int32_t* positions;
+  const int32_t* row_map;  // null: row i is row i of the outputs
+  float* dw_part;          // backward: [block][2][D] partial sums of the weights' gradients
+  int64_t rows, out_rows;
+  int32_t num_heads;
+  int32_t weight_f32;
+  int32_t head_step;  // heads of a warp's slice (grid.y slices)
+  float eps;
+};
+
+// cos and sin of this lane's pairs for one token.  kHalves: lane l of a row
+// holds elements [8 l, 8 l + 8), which are the first (l < D / 16) or second
+// members of pairs (8 l + e) mod D / 2; else pairs 4 l .. 4 l + 3 whole.
+template <int D, bool kHalves>
+struct Turn {
+  static constexpr int kN = kHalves ? 8 : 4;
+  float c[kN], s[kN];
+  __device__ __forceinline__ void set(const RopeTable& t, const int32_t* pos, int l) {
+#pragma unroll
+    for (int e = 0; e < kN; ++e) {
+      const int j = kHalves ? (8 * l + e) % (D / 2) : 4 * l + e;
+      const float p = static_cast<float>(pos[t.axis[j]]);
+      const float whole = p * t.turn_hi[j];
+      const float rest = fmaf(p, t.turn_hi[j], -whole) + p * t.turn_lo[j];
+      sincospif(2.f * ((whole - rintf(whole)) + rest), &s[e], &c[e]);
+    }
+  }
+  // x turned by the angles (back: by their negatives).
+  template <bool kBack>
+  __device__ __forceinline__ Vec8 apply(const Vec8& x, int l) const {
+    Vec8 o;
+    if constexpr (kHalves) {
+      const float sign = (l < D / 16) != kBack ? -1.f : 1.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float y = __shfl_xor_sync(0xffffffffu, x.v[e], D / 16);
+        o.v[e] = fmaf(x.v[e], c[e], sign * y * s[e]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float sn = kBack ? -s[e] : s[e];
+        o.v[2 * e] = x.v[2 * e] * c[e] - x.v[2 * e + 1] * sn;
+        o.v[2 * e + 1] = x.v[2 * e] * sn + x.v[2 * e + 1] * c[e];
+      }
+    }
+    return o;
+  }
+};
+
+template <int D>
+__device__ __forceinline__ float row_sum(float x) {
+#pragma unroll
+  for (int o = D / 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+
+// Heads in flight for each tensor: four 16-byte loads a lane.
+template <int D, bool kHalves>
+__global__ void __launch_bounds__(kRopeThreads) qkv_rope_kernel(const __grid_constant__ RopeTable table,
+                                                                const __grid_constant__ RopeArgs a) {
+  constexpr int kLanes = D / 8, kPer = 32 / kLanes, kUnroll = 4;
+  const int lane = threadIdx.x & 31, l = lane % kLanes, sub = lane / kLanes;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kRopeTokens + (threadIdx.x >> 5);
+  grid_dependency_wait();
+  if (threadIdx.x == 0) grid_launch_dependents();
+  if (row >= a.rows) return;
+  const int64_t to = a.row_map ? a.row_map[row] : row;
+  if (to < 0 || to >= a.out_rows) return;
+  const int h0 = blockIdx.y * a.head_step, h1 = min(a.num_heads, h0 + a.head_step);
+  Turn<D, kHalves> turn;
+  if (a.src[0] || a.src[1]) turn.set(table, a.positions + row * table.num_axes, l);
+#pragma unroll 1
+  for (int t = 0; t < 3; ++t) {
+    if (!a.src[t]) continue;
+    const uint16_t* src = a.src[t] + row * a.ld[t] + 8 * l;
+    uint16_t* dst = a.dst[t] + to * a.ld_dst[t] + 8 * l;
+    const void* wp = t < 2 ? a.weight[t] : nullptr;
+    const Vec8 w = wp ? load_param8(wp, 8 * l, a.weight_f32 != 0) : fill8(1.f);
+#pragma unroll 1
+    for (int h = h0; h < h1; h += kUnroll * kPer) {
+      uint4 raw[kUnroll];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const int hh = h + u * kPer + sub;
+        raw[u] = hh < h1 ? ld_stream(src + hh * D) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const int hh = h + u * kPer + sub;
+        uint4 out = raw[u];
+        if (t < 2) {
+          Vec8 x = unpack8(raw[u]);
+          if (wp) {
+            float ss = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ss = fmaf(x.v[e], x.v[e], ss);
+            const float r = rsqrtf(row_sum<D>(ss) * (1.f / D) + a.eps);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x.v[e] *= r * w.v[e];
+          }
+          out = pack8(turn.template apply<false>(x, l));
+        }
+        if (hh < h1) *reinterpret_cast<uint4*>(dst + hh * D) = out;
+      }
+    }
+  }
+}
+
+// The gradient: a warp walks over tokens row, row + stride, ... so that the sums
+// of dw stay in registers; the block's sum goes to dw_part.
+template <int D, bool kHalves>
+__global__ void __launch_bounds__(kRopeThreads) qkv_rope_backward_kernel(const __grid_constant__ RopeTable table,
+                                                                         const __grid_constant__ RopeArgs a) {
+  constexpr int kLanes = D / 8, kPer = 32 / kLanes, kUnroll = 2;
+  __shared__ float sums[kRopeTokens][D];
+  const int lane = threadIdx.x & 31, l = lane % kLanes, sub = lane / kLanes, warp = threadIdx.x >> 5;
+  grid_dependency_wait();
+  if (threadIdx.x == 0) grid_launch_dependents();
+  const int h0 = blockIdx.y * a.head_step, h1 = min(a.num_heads, h0 + a.head_step);
+  Vec8 w[2], dw[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    w[t] = a.weight[t] ? load_param8(a.weight[t], 8 * l, a.weight_f32 != 0) : fill8(1.f);
+    dw[t] = fill8(0.f);
+  }
+#pragma unroll 1
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * kRopeTokens + warp; row < a.rows;
+       row += static_cast<int64_t>(gridDim.x) * kRopeTokens) {
+    const int64_t to = a.row_map ? a.row_map[row] : row;
+    const bool kept = to >= 0 && to < a.out_rows;  // a row that was not kept has no gradient
+    Turn<D, kHalves> turn;
+    if (a.grad[0] || a.grad[1]) turn.set(table, a.positions + row * table.num_axes, l);
+#pragma unroll
+    for (int t = 0; t < 3; ++t) {
+      if (!a.grad[t]) continue;
+      const bool normed = t < 2 && a.weight[t];
+      const uint16_t* src = normed ? a.src[t] + row * a.ld[t] + 8 * l : nullptr;
+      const uint16_t* grad = a.grad[t] + (kept ? to : 0) * static_cast<int64_t>(a.num_heads) * D + 8 * l;
+      uint16_t* dst = a.dst[t] + row * a.ld_dst[t] + 8 * l;
+#pragma unroll 1
+      for (int h = h0; h < h1; h += kUnroll * kPer) {
+        uint4 graw[kUnroll], xraw[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          const int hh = h + u * kPer + sub;
+          graw[u] = kept && hh < h1 ? ld_stream(grad + hh * D) : make_uint4(0, 0, 0, 0);
+          xraw[u] = normed && hh < h1 ? ld_stream(src + hh * D) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          const int hh = h + u * kPer + sub;
+          uint4 out = graw[u];
+          if (t < 2) {
+            Vec8 g = turn.template apply<true>(unpack8(graw[u]), l);
+            if (normed) {
+              const Vec8 x = unpack8(xraw[u]);
+              float ss = 0.f, xu = 0.f;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                ss = fmaf(x.v[e], x.v[e], ss);
+                xu = fmaf(x.v[e], g.v[e] * w[t < 2 ? t : 0].v[e], xu);
+              }
+              const float r = rsqrtf(row_sum<D>(ss) * (1.f / D) + a.eps);
+              const float k = r * r * r * row_sum<D>(xu) * (1.f / D);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const float y = x.v[e];
+                if (hh < h1) dw[t < 2 ? t : 0].v[e] = fmaf(g.v[e], y * r, dw[t < 2 ? t : 0].v[e]);
+                g.v[e] = fmaf(r, g.v[e] * w[t < 2 ? t : 0].v[e], -y * k);
+              }
+            }
+            out = pack8(g);
+          }
+          if (hh < h1) *reinterpret_cast<uint4*>(dst + hh * D) = out;
+        }
+      }
+    }
+  }
+  // the block's sums, lanes of one column first, then warps, in a fixed order
+  const int64_t block = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    if (!a.weight[t]) continue;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float s = dw[t].v[e];
+#pragma unroll
+      for (int o = kLanes; o < 32; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      if (sub == 0) sums[warp][8 * l + e] = s;
+    }
+    __syncthreads();
+    if (threadIdx.x < D) {
+      float s = 0.f;
+#pragma unroll
+      for (int k = 0; k < kRopeTokens; ++k) s += sums[k][threadIdx.x];
+      a.dw_part[(block * 2 + t) * D + threadIdx.x] = s;
+    }
+    __syncthreads();
+  }
+}
+
+// dw = the sum of the blocks' parts; one block per weight, D threads in each of
+// 1024 / D groups that take every n-th part.
+__global__ void __launch_bounds__(1024) rope_weight_grad_kernel(const float* __restrict__ part, int n_parts, int D, float* dwq,
+                                                                float* dwk) {
+  __shared__ float sums[1024];
+  grid_dependency_wait();
+  if (threadIdx.x == 0) grid_launch_dependents();
+  const int t = blockIdx.x, c = threadIdx.x % D, g = threadIdx.x / D, groups = 1024 / D;
+  float* dw = t == 0 ? dwq : dwk;
+  if (!dw) return;
+  float s = 0.f;
+  for (int i = g; i < n_parts; i += groups) s += part[(static_cast<int64_t>(i) * 2 + t) * D + c];
+  sums[threadIdx.x] = s;
+  __syncthreads();
+  if (g == 0) {
+    for (int k = 1; k < groups; ++k) s += sums[k * D + c];
+    dw[c] = s;
+  }
+}
+
+}  // namespace rc

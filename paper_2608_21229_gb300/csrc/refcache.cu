@@ -21,11 +21,13 @@
 #include <vector>
 
 #include "refcache.h"
+#include "attn_bwd.cuh"
 #include "attn_mma.cuh"
 #include "attn_tc.cuh"
 #include "attn_tc2.cuh"
 #include "attn_combine.cuh"
 #include "cache_fp8.cuh"
+#include "host_common.h"
 #include "mufu_rate.cuh"
 
 using rc::AttnArgs;
@@ -43,6 +45,10 @@ std::atomic<int> g_kernel{REFCACHE_KERNEL_TCGEN05};
 std::atomic<uint64_t> g_timeout_ns{1000000000ull};
 std::atomic<int> g_dbg_skip{0};
 
+}  // namespace
+
+namespace rc_host {
+
 int fail(int code, const char* fmt, ...) {
   char buf[512];
   va_list ap;
@@ -57,7 +63,13 @@ int cuda_fail(cudaError_t e, const char* what) {
   return fail(REFCACHE_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
-constexpr int kMaxDevices = 64;
+}  // namespace rc_host
+
+namespace {
+
+using rc_host::cuda_fail;
+using rc_host::fail;
+using rc_host::kMaxDevices;
 constexpr int kWorkOffset = 32;  // ints from a cache's error word to its work counter (a line of its own)
 
 struct DeviceInfo {
@@ -65,6 +77,7 @@ struct DeviceInfo {
   bool ok = false;
   int num_sms = 0;
   bool attr_set[9] = {false, false, false, false, false, false, false, false, false};
+  bool bwd_attr_set[2] = {false, false};
   int max_clusters[5] = {0, 0, 0, 0, 0};  // CTA pairs of each attn_tc2_kernel variant that fit at once
 };
 DeviceInfo g_dev[kMaxDevices];
@@ -97,6 +110,18 @@ int current_device(int* dev_out, DeviceInfo** info) {
   *info = &d;
   return REFCACHE_OK;
 }
+
+}  // namespace
+
+int rc_host::device_sms(int* sms) {
+  int dev = 0;
+  DeviceInfo* info = nullptr;
+  const int rc = current_device(&dev, &info);
+  if (rc == REFCACHE_OK) *sms = info->num_sms;
+  return rc;
+}
+
+namespace {
 
 // ---------------------------------------------------------------- tensor maps
 using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
@@ -864,6 +889,94 @@ int enter_device(refcache* h, DeviceInfo** info) {
   return REFCACHE_OK;
 }
 
+// ---------------------------------------------------------------- gradients
+constexpr int kBwdRequests = rc::kBwdMaxSegs / 2;  // requests of one launch (two runs of rows each)
+
+// What a request's rows see, for the two kernels of attn_bwd.cuh.
+struct BwdRequest {
+  rc::BwdQuerySeg q[2];
+  rc::BwdKeySeg k[2];
+  int nq = 0, nk = 0;
+  void queries(int row0, int n, int a0, int na, int b0, int nb) {
+    if (n > 0) q[nq++] = rc::BwdQuerySeg{row0, n, a0, na, b0, nb, 0, 0};
+  }
+  void keys(int row0, int n, int q0, int n_q, bool in_b, int add_from, int add_row0) {
+    if (n > 0) k[nk++] = rc::BwdKeySeg{row0, n, q0, n_q, in_b ? 1 : 0, add_from, add_row0, 0};
+  }
+};
+constexpr int kNoAdd = 0x7fffffff;
+
+template <int D>
+int launch_bwd_mma(const rc::BwdKeys& keys, const rc::BwdQueries& queries, const rc::BwdArgs& a, DeviceInfo* info, cudaStream_t s) {
+  constexpr int smem = rc::mm::bwd_smem<D>();
+  const int key = D == 64 ? 0 : 1;
+  if (!info->bwd_attr_set[key]) {
+    cudaError_t e = cudaFuncSetAttribute(rc::attn_bwd_mma_keys_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(rc::attn_bwd_mma_queries_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(attn_bwd_mma)");
+    info->bwd_attr_set[key] = true;
+  }
+  if (keys.n_tiles > 0) rc::attn_bwd_mma_keys_kernel<D><<<static_cast<unsigned>(keys.n_tiles) * a.num_heads, 128, smem, s>>>(keys, a);
+  if (queries.n_tiles > 0)
+    rc::attn_bwd_mma_queries_kernel<D><<<static_cast<unsigned>(queries.n_tiles) * a.num_heads, 128, smem, s>>>(queries, a);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "attn_bwd_mma kernel launch");
+}
+
+// The gradients of `batch` requests, request(b, &out) naming what request b's rows see.
+template <typename Request>
+int run_backward(int batch, int H, int D, rc::BwdArgs a, const float* lse, const void* o, void* work, float scale, int* status,
+                 DeviceInfo* info, cudaStream_t s, const Request& request) {
+  a.row_stride = static_cast<int64_t>(H) * D;
+  a.num_heads = H;
+  a.scale = scale;
+  a.scale_log2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634074);
+  a.stats = static_cast<const float2*>(work);
+  a.timeout_ns = g_timeout_ns.load();
+  a.status = status;
+  if (a.rows > 0) {
+    const int per = 256 / (D / 8);
+    const dim3 grid(static_cast<unsigned>((a.rows + per - 1) / per), static_cast<unsigned>((H + rc::kBwdPrepHeads - 1) / rc::kBwdPrepHeads));
+    auto go = [&](auto kernel) {
+      return rc_host::launch_dependent(kernel, grid, dim3(256), 0, s, static_cast<const __nv_bfloat16*>(o), a.d_o, lse,
+                                       static_cast<float2*>(work), a.rows, H);
+    };
+    const cudaError_t e = D == 128 ? go(rc::attn_bwd_prep_kernel<128>) : go(rc::attn_bwd_prep_kernel<64>);
+    if (e != cudaSuccess) return cuda_fail(e, "attn_bwd_prep_kernel launch");
+  }
+  for (int b0 = 0; b0 < batch; b0 += kBwdRequests) {
+    rc::BwdQueries queries{};
+    rc::BwdKeys keys{};
+    const int tile_q = rc::mm::kBwdRows, tile_k = rc::mm::kBwdRows;
+    for (int b = b0; b < std::min(batch, b0 + kBwdRequests); ++b) {
+      BwdRequest r;
+      request(b, &r);
+      for (int i = 0; i < r.nq; ++i) {
+        r.q[i].tile0 = queries.n_tiles;
+        queries.n_tiles += (r.q[i].q_rows + tile_q - 1) / tile_q;
+        queries.seg[queries.n++] = r.q[i];
+      }
+      for (int i = 0; i < r.nk; ++i) {
+        r.k[i].tile0 = keys.n_tiles;
+        keys.n_tiles += (r.k[i].k_rows + tile_k - 1) / tile_k;
+        keys.seg[keys.n++] = r.k[i];
+      }
+    }
+    const int rc = D == 64 ? launch_bwd_mma<64>(keys, queries, a, info, s) : launch_bwd_mma<128>(keys, queries, a, info, s);
+    if (rc) return rc;
+  }
+  return REFCACHE_OK;
+}
+
+int check_backward(std::initializer_list<const void*> tensors, const float* lse, const void* work, int64_t rows, int H, const char* what) {
+  int rc = check_ptrs(tensors, rows, what);
+  if (rc || rows == 0) return rc;
+  if (!lse || (reinterpret_cast<uintptr_t>(lse) & 3u)) return fail(REFCACHE_ERR_INVALID_ARG, "%s: lse is NULL or not 4-byte aligned", what);
+  if (!work || !aligned16(work)) return fail(REFCACHE_ERR_INVALID_ARG, "%s: work is NULL or not 16-byte aligned", what);
+  if ((rows + 63) / 64 > (1ll << 30) / H) return fail(REFCACHE_ERR_INVALID_ARG, "%s: too many work items", what);
+  return REFCACHE_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1261,6 +1374,122 @@ int full_attention_noalloc(int batch, int num_heads, int head_dim, const int32_t
   if (e != cudaSuccess) return cuda_fail(e, "cudaMemcpyAsync(work list)");
   Operands op{q, rows, k, v, rows, nullptr, nullptr, 0, o, lse};
   return run_attention(g_noalloc_dev_ptr[dev], n, num_heads, head_dim, op, softmax_scale, info, s);
+}
+
+size_t refcache_backward_bytes(int64_t rows, int num_heads) {
+  return rows < 0 || num_heads < 0 ? 0 : static_cast<size_t>(rows) * num_heads * sizeof(float2);
+}
+
+int step_attention_backward(refcache_t* h, int layer, const void* q_live, const void* k_live, const void* v_live, const void* o_live,
+                            const float* lse_live, const void* do_live, void* dq_live, void* dk_live, void* dv_live, void* dk_ref,
+                            void* dv_ref, int accumulate, void* work, float softmax_scale, void* stream) {
+  int rc = check_handle_layer(h, layer);
+  if (rc) return rc;
+  if (h->f8) return fail(REFCACHE_ERR_UNSUPPORTED, "step_attention_backward needs a bf16 cache");
+  if (!h->built[layer]) return fail(REFCACHE_ERR_NOT_BUILT, "layer %d has not been built", layer);
+  if ((rc = check_scale(softmax_scale)) != 0) return rc;
+  if ((rc = check_backward({q_live, k_live, v_live, o_live, do_live, dq_live, dk_live, dv_live}, lse_live, work, h->live_rows, h->H,
+                           "step_attention_backward")) != 0)
+    return rc;
+  if ((dk_ref == nullptr) != (dv_ref == nullptr)) return fail(REFCACHE_ERR_INVALID_ARG, "dk_ref without dv_ref, or the reverse");
+  if (dk_ref && (rc = check_ptrs({dk_ref, dv_ref}, h->cache_rows, "step_attention_backward")) != 0) return rc;
+  DeviceInfo* info = nullptr;
+  if ((rc = enter_device(h, &info)) != 0) return rc;
+  void *kslot = nullptr, *vslot = nullptr;
+  refcache_kv_ptr(h, layer, &kslot, &vslot, nullptr);
+  rc::BwdArgs a{};
+  a.q = static_cast<const __nv_bfloat16*>(q_live);
+  a.ka = static_cast<const __nv_bfloat16*>(k_live);
+  a.va = static_cast<const __nv_bfloat16*>(v_live);
+  a.kb = static_cast<const __nv_bfloat16*>(kslot);
+  a.vb = static_cast<const __nv_bfloat16*>(vslot);
+  a.d_o = static_cast<const __nv_bfloat16*>(do_live);
+  a.dq = static_cast<__nv_bfloat16*>(dq_live);
+  a.dka = static_cast<__nv_bfloat16*>(dk_live);
+  a.dva = static_cast<__nv_bfloat16*>(dv_live);
+  a.add_k = a.dkb = static_cast<__nv_bfloat16*>(dk_ref);
+  a.add_v = a.dvb = static_cast<__nv_bfloat16*>(dv_ref);
+  a.rows = h->live_rows;
+  a.a_rows = h->live_rows;
+  a.b_rows = h->cache_rows;
+  return run_backward(h->batch, h->H, h->D, a, lse_live, o_live, work, softmax_scale, h->d_status, info,
+                      static_cast<cudaStream_t>(stream), [&](int b, BwdRequest* r) {
+                        const int l0 = h->cu_live[b], nl = h->cu_live[b + 1] - l0;
+                        const int c0 = static_cast<int>(h->cache_off[b]), nc = static_cast<int>(h->cache_off[b + 1]) - c0;
+                        r->queries(l0, nl, l0, nl, c0, nc);
+                        r->keys(l0, nl, l0, nl, false, kNoAdd, 0);
+                        if (dk_ref) r->keys(c0, nc, l0, nl, true, accumulate ? 0 : kNoAdd, c0);
+                      });
+}
+
+int refcache_build_backward(refcache_t* h, int layer, const void* q_static, const void* k_static, const void* v_static,
+                            const void* o_static, const float* lse_static, const void* do_static, void* dq_static, void* dk_static,
+                            void* dv_static, const void* dk_ref, const void* dv_ref, void* work, float softmax_scale, void* stream) {
+  int rc = check_handle_layer(h, layer);
+  if (rc) return rc;
+  if ((rc = check_scale(softmax_scale)) != 0) return rc;
+  if ((rc = check_backward({q_static, k_static, v_static, o_static, do_static, dq_static, dk_static, dv_static}, lse_static, work,
+                           h->static_rows, h->H, "refcache_build_backward")) != 0)
+    return rc;
+  if ((dk_ref == nullptr) != (dv_ref == nullptr)) return fail(REFCACHE_ERR_INVALID_ARG, "dk_ref without dv_ref, or the reverse");
+  if (dk_ref && (rc = check_ptrs({dk_ref, dv_ref}, h->cache_rows, "refcache_build_backward")) != 0) return rc;
+  DeviceInfo* info = nullptr;
+  if ((rc = enter_device(h, &info)) != 0) return rc;
+  rc::BwdArgs a{};
+  a.q = static_cast<const __nv_bfloat16*>(q_static);
+  a.ka = static_cast<const __nv_bfloat16*>(k_static);
+  a.va = static_cast<const __nv_bfloat16*>(v_static);
+  a.d_o = static_cast<const __nv_bfloat16*>(do_static);
+  a.dq = static_cast<__nv_bfloat16*>(dq_static);
+  a.dka = static_cast<__nv_bfloat16*>(dk_static);
+  a.dva = static_cast<__nv_bfloat16*>(dv_static);
+  a.add_k = static_cast<const __nv_bfloat16*>(dk_ref);
+  a.add_v = static_cast<const __nv_bfloat16*>(dv_ref);
+  a.rows = h->static_rows;
+  a.a_rows = h->static_rows;
+  return run_backward(h->batch, h->H, h->D, a, lse_static, o_static, work, softmax_scale, h->d_status, info,
+                      static_cast<cudaStream_t>(stream), [&](int b, BwdRequest* r) {
+                        const int s0 = h->cu_static[b], ns = h->cu_static[b + 1] - s0, na = h->n_anchor[b];
+                        const int c0 = static_cast<int>(h->cache_off[b]);
+                        if (h->mode == REFCACHE_MASK_BEYOND_ALT) {  // ST sees ST, R sees [ST; R]; all of it is cached
+                          r->queries(s0, na, s0, na, 0, 0);
+                          r->queries(s0 + na, ns - na, s0, ns, 0, 0);
+                          r->keys(s0, na, s0, ns, false, dk_ref ? 0 : kNoAdd, c0);
+                          r->keys(s0 + na, ns - na, s0 + na, ns - na, false, dk_ref ? 0 : kNoAdd, c0 + na);
+                        } else {
+                          r->queries(s0, ns, s0, ns, 0, 0);
+                          r->keys(s0, ns, s0, ns, false, dk_ref ? na : kNoAdd, c0 - na);
+                        }
+                      });
+}
+
+int full_attention_backward(int batch, int num_heads, int head_dim, const int32_t* cu_seqlens, const void* q, const void* k,
+                            const void* v, const void* o, const float* lse, const void* d_o, void* dq, void* dk, void* dv, void* work,
+                            float softmax_scale, void* stream) {
+  int rc = check_dims(batch, num_heads, head_dim);
+  if (rc) return rc;
+  if ((rc = check_cu(cu_seqlens, batch, "cu_seqlens", (1ll << 31) - 1 - 512)) != 0) return rc;
+  if ((rc = check_scale(softmax_scale)) != 0) return rc;
+  const int64_t rows = cu_seqlens[batch];
+  if ((rc = check_backward({q, k, v, o, d_o, dq, dk, dv}, lse, work, rows, num_heads, "full_attention_backward")) != 0) return rc;
+  DeviceInfo* info = nullptr;
+  if ((rc = enter_device(nullptr, &info)) != 0) return rc;
+  rc::BwdArgs a{};
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.ka = static_cast<const __nv_bfloat16*>(k);
+  a.va = static_cast<const __nv_bfloat16*>(v);
+  a.d_o = static_cast<const __nv_bfloat16*>(d_o);
+  a.dq = static_cast<__nv_bfloat16*>(dq);
+  a.dka = static_cast<__nv_bfloat16*>(dk);
+  a.dva = static_cast<__nv_bfloat16*>(dv);
+  a.rows = rows;
+  a.a_rows = rows;
+  return run_backward(batch, num_heads, head_dim, a, lse, o, work, softmax_scale, nullptr, info, static_cast<cudaStream_t>(stream),
+                      [&](int b, BwdRequest* r) {
+                        const int s0 = cu_seqlens[b], n = cu_seqlens[b + 1] - s0;
+                        r->queries(s0, n, s0, n, 0, 0);
+                        r->keys(s0, n, s0, n, false, kNoAdd, 0);
+                      });
 }
 
 int refcache_status(void* stream) {

@@ -1,0 +1,52 @@
+// vec8.cuh -- eight consecutive values of a row as one 16-byte access (bf16) or
+// two (fp32), in registers as fp32.
+#pragma once
+#include <cstdint>
+
+#include "ptx.cuh"
+
+namespace rc {
+
+struct Vec8 {
+  float v[8];
+};
+
+__device__ __forceinline__ Vec8 unpack8(uint4 r) {
+  Vec8 o;
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    o.v[2 * i] = __uint_as_float(w[i] << 16);
+    o.v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+  return o;
+}
+__device__ __forceinline__ uint4 pack8(const Vec8& a) {
+  return make_uint4(pack_bf16x2(a.v[0], a.v[1]), pack_bf16x2(a.v[2], a.v[3]), pack_bf16x2(a.v[4], a.v[5]),
+                    pack_bf16x2(a.v[6], a.v[7]));
+}
+__device__ __forceinline__ Vec8 fill8(float x) {
+  Vec8 o;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o.v[i] = x;
+  return o;
+}
+// Elements [i, i + 8) of a parameter row held in bf16 or fp32.
+__device__ __forceinline__ Vec8 load_param8(const void* p, int64_t i, bool f32) {
+  if (f32) {
+    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
+    const float4 a = __ldg(q), b = __ldg(q + 1);
+    return Vec8{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+  }
+  return unpack8(__ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i)));
+}
+// Loads and stores of data that is used once.
+__device__ __forceinline__ uint4 ld_stream(const void* p) { return __ldcs(static_cast<const uint4*>(p)); }
+
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+
+}  // namespace rc

@@ -24,6 +24,8 @@ ERR_TIMEOUT = -6
 
 MASK_MODES = {"beyond": 0, "beyond_alt": 1, "isolated": 2}
 KERNELS = {"tcgen05": 0, "mma_sync": 1, "tcgen05_k128": 2}
+NORMS = {None: 0, "layer": 1, "rms": 2}
+ROPE_PAIRS = {"halves": 0, "interleaved": 1}
 CACHE_DTYPES = {"bf16": 0, "fp8": 0x100}  # REFCACHE_CACHE_FP8: E4M3 codes with per-tile scales
 
 EXPORTED = (
@@ -32,6 +34,10 @@ EXPORTED = (
     "refcache_set_kernel", "refcache_debug_skip_first_load", "refcache_last_error", "refcache_version",
     "full_attention_noalloc", "refcache_call_launches", "refcache_fp8_ptr", "refcache_build_in_slot",
     "refcache_cache_status", "refcache_ex2_rate",
+    "refcache_backward_bytes", "step_attention_backward", "refcache_build_backward", "full_attention_backward",
+    "refcache_rope_init", "refcache_qkv_rope", "refcache_qkv_rope_backward_bytes", "refcache_qkv_rope_backward",
+    "refcache_gated_norm", "refcache_gated_norm_backward_bytes", "refcache_gated_norm_backward",
+    "refcache_clip_gradients_bytes", "refcache_clip_gradients",
 )
 NOALLOC_MAX_TASKS = 16384
 
@@ -48,6 +54,25 @@ class _Segments(ctypes.Structure):
         ("cu_live", ctypes.POINTER(ctypes.c_int32)), ("cu_static", ctypes.POINTER(ctypes.c_int32)),
         ("n_anchor", ctypes.POINTER(ctypes.c_int32)), ("n_instr", ctypes.POINTER(ctypes.c_int32)),
     ]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("num_axes", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("turn_hi", ctypes.c_float * 64), ("turn_lo", ctypes.c_float * 64), ("axis", ctypes.c_uint8 * 64)]
+
+
+class _RopeRows(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("out_rows", ctypes.c_int64), ("num_heads", ctypes.c_int32),
+                ("weight_f32", ctypes.c_int32), ("positions", ctypes.c_void_p), ("row_map", ctypes.c_void_p),
+                ("weight_q", ctypes.c_void_p), ("weight_k", ctypes.c_void_p), ("eps", ctypes.c_float)]
+
+
+class _GatedNorm(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("width", ctypes.c_int32), ("cu_rows", ctypes.POINTER(ctypes.c_int32)),
+                ("norm", ctypes.c_int32), ("post_norm", ctypes.c_int32), ("mod_f32", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("gate", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("shift", ctypes.c_void_p),
+                ("ld_gate", ctypes.c_int64), ("ld_scale", ctypes.c_int64), ("ld_shift", ctypes.c_int64),
+                ("weight", ctypes.c_void_p), ("post_weight", ctypes.c_void_p)]
 
 
 _lib = None
@@ -85,6 +110,24 @@ def load(path: Optional[str] = None):
     L.full_attention.argtypes = [i32, i32, i32, ctypes.POINTER(ctypes.c_int32), vp, vp, vp, vp, vp, f32, vp]
     L.full_attention_noalloc.argtypes = [i32, i32, i32, ctypes.POINTER(ctypes.c_int32), vp, vp, vp, vp, vp, f32,
                                          vp]
+    L.refcache_backward_bytes.argtypes = [i64, i32]
+    L.refcache_backward_bytes.restype = ctypes.c_size_t
+    L.step_attention_backward.argtypes = [vp, i32] + [vp] * 11 + [i32, vp, f32, vp]
+    L.refcache_build_backward.argtypes = [vp, i32] + [vp] * 12 + [f32, vp]
+    L.full_attention_backward.argtypes = [i32, i32, i32, ctypes.POINTER(ctypes.c_int32)] + [vp] * 10 + [f32, vp]
+    ropep, rowsp, normp = ctypes.POINTER(_Rope), ctypes.POINTER(_RopeRows), ctypes.POINTER(_GatedNorm)
+    L.refcache_rope_init.argtypes = [ropep, i32, i32, ctypes.POINTER(ctypes.c_int32), ctypes.c_double, i32]
+    L.refcache_qkv_rope.argtypes = [ropep, rowsp] + [vp, i64] * 3 + [vp] * 4
+    L.refcache_qkv_rope_backward_bytes.argtypes = [ropep]
+    L.refcache_qkv_rope_backward_bytes.restype = ctypes.c_size_t
+    L.refcache_qkv_rope_backward.argtypes = [ropep, rowsp, vp, i64, vp, i64, vp, vp, vp] + [vp, i64] * 3 + [vp] * 4
+    L.refcache_gated_norm.argtypes = [normp] + [vp] * 5
+    L.refcache_gated_norm_backward_bytes.argtypes = [normp]
+    L.refcache_gated_norm_backward_bytes.restype = ctypes.c_size_t
+    L.refcache_gated_norm_backward.argtypes = [normp] + [vp] * 13
+    L.refcache_clip_gradients_bytes.argtypes = [i32]
+    L.refcache_clip_gradients_bytes.restype = ctypes.c_size_t
+    L.refcache_clip_gradients.argtypes = [i32, vp, vp, vp, vp, f32, vp, vp, vp]
     L.refcache_status.argtypes = [vp]
     L.refcache_cache_status.argtypes = [vp, vp]
     L.refcache_set_wait_timeout_ns.argtypes = [ctypes.c_uint64]
@@ -364,6 +407,34 @@ class RefCache:
         scale = default_scale(D) if scale is None else scale
         _check(load().step_attention(self.h, layer, *ptrs, _ptr(lse), scale, _stream(stream)))
 
+    def step_backward(self, layer, q, k, v, o, lse, d_o, dq, dk, dv, dk_ref=None, dv_ref=None, accumulate=False, scale=None,
+                      stream=None):
+        """Gradient of ``step``: from ``d_o``, the gradient of its ``o``, to dq, dk, dv [live rows, H, D] and, unless
+        they are None, dk_ref and dv_ref [cached rows, H, D] (``accumulate``: added to what these hold).  ``lse`` is
+        the fp32 [live rows, H] that the step wrote."""
+        H, D, n = self.seg.num_heads, self.seg.head_dim, self.seg.live_rows
+        ptrs, work = _backward_ptrs(q, k, v, o, lse, d_o, dq, dk, dv, n, H, D, stream)
+        ref = self._ref_ptrs(dk_ref, dv_ref)
+        scale = default_scale(D) if scale is None else scale
+        _check(load().step_attention_backward(self.h, layer, *ptrs, *ref, 1 if accumulate else 0, _ptr(work), scale,
+                                              _stream(stream)))
+
+    def build_backward(self, layer, q, k, v, o, lse, d_o, dq, dk, dv, dk_ref=None, dv_ref=None, scale=None, stream=None):
+        """Gradient of ``build``; dk_ref and dv_ref, the cached rows' gradients from ``step_backward``, are added to
+        the cached rows' part of dk and dv unless they are None."""
+        H, D, n = self.seg.num_heads, self.seg.head_dim, self.seg.static_rows
+        ptrs, work = _backward_ptrs(q, k, v, o, lse, d_o, dq, dk, dv, n, H, D, stream)
+        ref = self._ref_ptrs(dk_ref, dv_ref)
+        scale = default_scale(D) if scale is None else scale
+        _check(load().refcache_build_backward(self.h, layer, *ptrs, *ref, _ptr(work), scale, _stream(stream)))
+
+    def _ref_ptrs(self, dk_ref, dv_ref):
+        if dk_ref is None and dv_ref is None:
+            return None, None
+        n = sum(s1 - s0 - (0 if self.mask_mode == "beyond_alt" else a)
+                for s0, s1, a in zip(self.seg.cu_static, self.seg.cu_static[1:], self.seg.n_anchor))
+        return _thd_ptrs((("dk_ref", dk_ref), ("dv_ref", dv_ref)), n, self.seg.num_heads, self.seg.head_dim)
+
 
 def full_attention(cu_seqlens, q, k, v, o, lse=None, scale=None, stream=None):
     rows, H, D = q.shape
@@ -381,3 +452,252 @@ def full_attention_noalloc(cu_seqlens, q, k, v, o, lse=None, scale=None, stream=
     ptrs = _thd_ptrs((("q", q), ("k", k), ("v", v), ("o", o)), cu[-1], H, D)
     scale = default_scale(D) if scale is None else scale
     _check(load().full_attention_noalloc(len(cu) - 1, H, D, _arr(cu), *ptrs, _ptr(lse), scale, _stream(stream)))
+
+
+def _work(nbytes, like, stream):
+    """A call's workspace from torch's allocator, which hands it on only to work behind this call on its stream."""
+    import torch
+
+    work = torch.empty(max(16, nbytes), dtype=torch.uint8, device=like.device)
+    if stream is not None:  # allocated for the current stream, used on another
+        s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=like.device)
+        work.record_stream(s)
+    return work
+
+
+def _backward_ptrs(q, k, v, o, lse, d_o, dq, dk, dv, rows, H, D, stream):
+    import torch
+
+    first = _thd_ptrs((("q", q), ("k", k), ("v", v), ("o", o)), rows, H, D)
+    if lse is None:
+        raise ValueError("lse is required")
+    if lse.dtype != torch.float32 or tuple(lse.shape) != (rows, H):
+        raise ValueError(f"lse: expected float32 [{rows}, {H}], got {lse.dtype} {tuple(lse.shape)}")
+    rest = _thd_ptrs((("d_o", d_o), ("dq", dq), ("dk", dk), ("dv", dv)), rows, H, D)
+    return [*first, _ptr(lse), *rest], _work(load().refcache_backward_bytes(rows, H), q, stream)
+
+
+def full_attention_backward(cu_seqlens, q, k, v, o, lse, d_o, dq, dk, dv, scale=None, stream=None):
+    """Gradient of ``full_attention`` (of either allocation variant)."""
+    _, H, D = q.shape
+    cu = list(cu_seqlens)
+    ptrs, work = _backward_ptrs(q, k, v, o, lse, d_o, dq, dk, dv, cu[-1], H, D, stream)
+    scale = default_scale(D) if scale is None else scale
+    _check(load().full_attention_backward(len(cu) - 1, H, D, _arr(cu), *ptrs, _ptr(work), scale, _stream(stream)))
+
+
+class Rope:
+    """Rotary positions with several axes (refcache_rope_t): ``axes`` are the dims of a head that each axis turns."""
+
+    def __init__(self, head_dim, axes, theta=10000.0, pairs="interleaved"):
+        if pairs not in ROPE_PAIRS:
+            raise ValueError(f"pairs: expected one of {sorted(ROPE_PAIRS)}, got {pairs!r}")
+        self.head_dim, self.axes, self.theta, self.pairs = int(head_dim), tuple(int(a) for a in axes), float(theta), pairs
+        self.c = _Rope()
+        _check(load().refcache_rope_init(ctypes.byref(self.c), self.head_dim, len(self.axes), _arr(self.axes), self.theta,
+                                         ROPE_PAIRS[pairs]))
+
+
+_NOTHING = 16  # the address of a tensor without elements, which torch gives as NULL; nothing is read or written there
+
+
+def _head_rows(name, t, rows, H, D):
+    """(pointer, elements between rows) of [rows, H, D] bf16 whose rows are contiguous."""
+    import torch
+
+    if t is None:
+        return None, H * D
+    if t.dtype is not torch.bfloat16 or t.shape != (rows, H, D):
+        raise ValueError(f"{name}: expected bf16 [{rows}, {H}, {D}], got {t.dtype} {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: tensor must live on the GPU")
+    s = t.stride()
+    if s[2] != 1 or (H > 1 and s[1] != D):
+        raise ValueError(f"{name}: the heads of a row must be contiguous, got strides {s}")
+    return t.data_ptr() or _NOTHING, s[0] if rows > 1 else H * D
+
+
+def _param(name, t, n, f32):
+    """The pointer of a contiguous [n] parameter in bf16 or fp32, and whether it is fp32 (``f32``: that of one before)."""
+    import torch
+
+    if t is None:
+        return None, f32
+    if t.dtype not in (torch.bfloat16, torch.float32) or t.shape != (n,):
+        raise ValueError(f"{name}: expected bf16 or float32 [{n}], got {t.dtype} {tuple(t.shape)}")
+    if f32 is not None and f32 != (t.dtype is torch.float32):
+        raise ValueError(f"{name}: the parameters of one call have one type")
+    return _ptr(t), t.dtype is torch.float32
+
+
+def _rope_rows(rope, positions, like, H, out_rows, wq, wk, rows, eps):
+    import torch
+
+    n = like.shape[0]
+    if positions.dtype is not torch.int32 or positions.shape != (n, len(rope.axes)):
+        raise ValueError(f"positions: expected int32 [{n}, {len(rope.axes)}], got {positions.dtype} {tuple(positions.shape)}")
+    if rows is not None and (rows.dtype is not torch.int32 or rows.shape != (n,)):
+        raise ValueError(f"rows: expected int32 [{n}], got {rows.dtype} {tuple(rows.shape)}")
+    pq, f32 = _param("weight_q", wq, rope.head_dim, None)
+    pk, f32 = _param("weight_k", wk, rope.head_dim, f32)
+    return _RopeRows(n, out_rows, H, 1 if f32 else 0, _ptr(positions), _ptr(rows), pq, pk, eps)
+
+
+def _same_rows(named):
+    """The [rows, H, D] of the tensors that are there."""
+    for _, t in named:
+        if t is not None:
+            if t.dim() != 3:
+                raise ValueError(f"expected [rows, heads, dim], got {tuple(t.shape)}")
+            return tuple(t.shape)
+    return None
+
+
+def qkv_rope(rope, positions, q, k, v, q_out, k_out, v_out, weight_q=None, weight_k=None, rows=None, eps=1e-6, stream=None):
+    """From a projection's q, k and v ([rows, H, D] bf16, rows may lie apart, as those of a fused projection do) to the
+    attention's ([out rows, H, D], packed): RMS norm of each head of q and k (with a weight), rotary positions, row i
+    moved to row ``rows[i]``.  q, k or v may be None together with its output."""
+    shape, out = _same_rows((("q", q), ("k", k), ("v", v))), _same_rows((("q_out", q_out), ("k_out", k_out), ("v_out", v_out)))
+    if shape is None or out is None:
+        raise ValueError("qkv_rope needs one of q, k and v with its output")
+    n, H, D = shape
+    r = _rope_rows(rope, positions, next(t for t in (q, k, v) if t is not None), H, out[0], weight_q, weight_k, rows, eps)
+    src = [x for name, t in (("q", q), ("k", k), ("v", v)) for x in _head_rows(name, t, n, H, rope.head_dim)]
+    dst = [None if t is None else _thd_ptrs(((name, t),), out[0], H, rope.head_dim)[0] or _NOTHING
+           for name, t in (("q_out", q_out), ("k_out", k_out), ("v_out", v_out))]
+    _check(load().refcache_qkv_rope(ctypes.byref(rope.c), ctypes.byref(r), *src, *dst, _stream(stream)))
+
+
+def qkv_rope_backward(rope, positions, q, k, dq_out, dk_out, dv_out, dq, dk, dv, weight_q=None, weight_k=None, dweight_q=None,
+                      dweight_k=None, rows=None, eps=1e-6, stream=None):
+    """Gradient of ``qkv_rope``: from those of its outputs to dq, dk and dv (rows may lie apart) and the weights' (fp32
+    [D]).  q and k are its inputs, needed where they were normalised."""
+    import torch
+
+    shape = _same_rows((("dq", dq), ("dk", dk), ("dv", dv)))
+    out = _same_rows((("dq_out", dq_out), ("dk_out", dk_out), ("dv_out", dv_out)))
+    if shape is None or out is None:
+        raise ValueError("qkv_rope_backward needs one of dq, dk and dv with the gradient of its output")
+    n, H, D = shape
+    like = next(t for t in (dq, dk, dv) if t is not None)
+    r = _rope_rows(rope, positions, like, H, out[0], weight_q, weight_k, rows, eps)
+    src = [x for name, t in (("q", q), ("k", k)) for x in _head_rows(name, t, n, H, rope.head_dim)]
+    grad = [None if t is None else _thd_ptrs(((name, t),), out[0], H, rope.head_dim)[0] or _NOTHING
+            for name, t in (("dq_out", dq_out), ("dk_out", dk_out), ("dv_out", dv_out))]
+    dst = [x for name, t in (("dq", dq), ("dk", dk), ("dv", dv)) for x in _head_rows(name, t, n, H, rope.head_dim)]
+    for name, t in (("dweight_q", dweight_q), ("dweight_k", dweight_k)):
+        if t is not None and (t.dtype is not torch.float32 or t.shape != (rope.head_dim,)):
+            raise ValueError(f"{name}: expected float32 [{rope.head_dim}], got {t.dtype} {tuple(t.shape)}")
+    L = load()
+    work = None
+    if weight_q is not None or weight_k is not None:
+        work = _work(L.refcache_qkv_rope_backward_bytes(ctypes.byref(rope.c)), like, stream)
+    _check(L.refcache_qkv_rope_backward(ctypes.byref(rope.c), ctypes.byref(r), *src, *grad, *dst, _ptr(dweight_q), _ptr(dweight_k),
+                                        _ptr(work), _stream(stream)))
+
+
+def _norm_params(cu_rows, width, gate, scale, shift, weight, post_weight, norm, post_norm, eps):
+    import torch
+
+    cu = list(cu_rows)
+    batch = len(cu) - 1
+    c = _GatedNorm(batch=batch, width=width, cu_rows=_arr(cu), norm=NORMS[norm], post_norm=NORMS[post_norm], eps=eps)
+    f32 = None
+    for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
+        if t is None:
+            continue
+        if t.dtype not in (torch.bfloat16, torch.float32) or t.shape != (batch, width):
+            raise ValueError(f"{name}: expected bf16 or float32 [{batch}, {width}], got {t.dtype} {tuple(t.shape)}")
+        if f32 is not None and f32 != (t.dtype is torch.float32):
+            raise ValueError(f"{name}: the parameters of one call have one type")
+        if not t.is_cuda or t.stride(1) != 1:
+            raise ValueError(f"{name}: must live on the GPU, its rows contiguous")
+        f32 = t.dtype is torch.float32
+        setattr(c, name, t.data_ptr())
+        setattr(c, "ld_" + name, t.stride(0) if batch > 1 else width)
+    c.weight, f32 = _param("weight", weight, width, f32)
+    c.post_weight, f32 = _param("post_weight", post_weight, width, f32)
+    c.mod_f32 = 1 if f32 else 0
+    return c
+
+
+def _rows_ptr(name, t, rows, width):
+    import torch
+
+    if t is None:
+        return None
+    if t.dtype is not torch.bfloat16 or t.shape != (rows, width):
+        raise ValueError(f"{name}: expected bf16 [{rows}, {width}], got {t.dtype} {tuple(t.shape)}")
+    return _ptr(t)
+
+
+def gated_norm(cu_rows, x, y=None, branch=None, x_out=None, gate=None, scale=None, shift=None, weight=None, post_weight=None,
+               norm="layer", post_norm=None, eps=1e-6, stream=None):
+    """x_out = x + gate * h with h = branch, or its ``post_norm`` times post_weight; y = norm(x_out) * weight *
+    (1 + scale) + shift.  x, branch, x_out (may be x) and y: [rows, width] bf16, packed; gate, scale and shift: a row for
+    each request of ``cu_rows``, rows may lie apart; norms "layer", "rms" or None."""
+    n, width = x.shape
+    c = _norm_params(cu_rows, width, gate, scale, shift, weight, post_weight, norm, post_norm, eps)
+    n = cu_rows[-1]
+    _check(load().refcache_gated_norm(ctypes.byref(c), _rows_ptr("x", x, n, width), _rows_ptr("branch", branch, n, width),
+                                      _rows_ptr("x_out", x_out, n, width), _rows_ptr("y", y, n, width), _stream(stream)))
+
+
+def gated_norm_backward(cu_rows, x_out, dy, dx, branch=None, dx_out=None, d_branch=None, gate=None, scale=None, weight=None,
+                        post_weight=None, d_gate=None, d_scale=None, d_shift=None, d_weight=None, d_post_weight=None,
+                        norm="layer", post_norm=None, eps=1e-6, stream=None):
+    """Gradient of ``gated_norm``: from dy and dx_out, the gradients of its outputs (either may be None), to dx, d_branch,
+    the modulation's (fp32 [requests, width]) and the weights' (fp32 [width]), each unless it is None.  ``x_out`` is the
+    call's output (its x where there was no branch)."""
+    import torch
+
+    like = next((t for t in (dy, dx_out, x_out) if t is not None), None)
+    if like is None:
+        raise ValueError("gated_norm_backward needs dy or dx_out")
+    width, n = like.shape[1], cu_rows[-1]
+    c = _norm_params(cu_rows, width, gate, scale, None, weight, post_weight, norm, post_norm, eps)
+    for name, t, shape in (("d_gate", d_gate, (c.batch, width)), ("d_scale", d_scale, (c.batch, width)),
+                           ("d_shift", d_shift, (c.batch, width)), ("d_weight", d_weight, (width,)),
+                           ("d_post_weight", d_post_weight, (width,))):
+        if t is not None and (t.dtype is not torch.float32 or t.shape != shape):
+            raise ValueError(f"{name}: expected float32 {list(shape)}, got {t.dtype} {tuple(t.shape)}")
+    L = load()
+    work = _work(L.refcache_gated_norm_backward_bytes(ctypes.byref(c)), like, stream)
+    _check(L.refcache_gated_norm_backward(
+        ctypes.byref(c), _rows_ptr("x_out", x_out, n, width), _rows_ptr("branch", branch, n, width), _rows_ptr("dy", dy, n, width),
+        _rows_ptr("dx_out", dx_out, n, width), _rows_ptr("dx", dx, n, width), _rows_ptr("d_branch", d_branch, n, width), _ptr(d_gate),
+        _ptr(d_scale), _ptr(d_shift), _ptr(d_weight), _ptr(d_post_weight), _ptr(work), _stream(stream)))
+
+
+def clip_gradients(grads, max_norm, out=None, norm=None, stream=None):
+    """Scales gradients (bf16 or float32 tensors of any shapes) so that their global norm is at most ``max_norm``, in
+    place or into the tensors ``out``; returns the norm before (float32, on the GPU; ``norm`` if given).  max_norm
+    may be infinite: the norm alone."""
+    import torch
+
+    grads = list(grads)
+    outs = grads if out is None else list(out)
+    if len(outs) != len(grads):
+        raise ValueError(f"{len(grads)} gradients and {len(outs)} outputs")
+    bf16, f32 = torch.bfloat16, torch.float32
+    n = len(grads)
+    ptrs, outp, counts, types = (ctypes.c_void_p * n)(), (ctypes.c_void_p * n)(), (ctypes.c_int64 * n)(), (ctypes.c_int32 * n)()
+    for i, (g, o) in enumerate(zip(grads, outs)):
+        gt, ot = g.dtype, o.dtype
+        if (gt is not bf16 and gt is not f32) or (ot is not bf16 and ot is not f32):
+            raise ValueError(f"gradient {i}: expected bf16 or float32, got {gt} to {ot}")
+        if not (g.is_cuda and g.is_contiguous() and o.is_cuda and o.is_contiguous()):
+            raise ValueError(f"gradient {i}: tensors must live on the GPU and be contiguous")
+        m = g.numel()
+        if o is not g and o.numel() != m:
+            raise ValueError(f"gradient {i}: {m} elements and an output of {o.numel()}")
+        ptrs[i], outp[i], counts[i], types[i] = g.data_ptr(), o.data_ptr(), m, (gt is f32) + 2 * (ot is f32)
+    if norm is None:
+        norm = torch.empty((), dtype=f32, device=grads[0].device if grads else "cuda")
+    elif norm.dtype is not f32 or norm.numel() != 1:
+        raise ValueError(f"norm: expected one float32, got {norm.dtype} {tuple(norm.shape)}")
+    L = load()
+    work = _work(L.refcache_clip_gradients_bytes(n), norm, stream)
+    _check(L.refcache_clip_gradients(n, ptrs, None if out is None else outp, counts, types, max_norm, _ptr(norm), _ptr(work),
+                                     _stream(stream)))
+    return norm
