@@ -25,6 +25,7 @@
 #include "attn_mma.cuh"
 #include "attn_tc.cuh"
 #include "attn_tc2.cuh"
+#include "attn_bwd_tc.cuh"
 #include "attn_combine.cuh"
 #include "cache_fp8.cuh"
 #include "host_common.h"
@@ -78,6 +79,7 @@ struct DeviceInfo {
   int num_sms = 0;
   bool attr_set[9] = {false, false, false, false, false, false, false, false, false};
   bool bwd_attr_set[2] = {false, false};
+  int bwd_clusters[4] = {0, 0, 0, 0};  // CTA pairs of each tcgen05 gradient kernel that fit at once (0: not asked yet)
   int max_clusters[5] = {0, 0, 0, 0, 0};  // CTA pairs of each attn_tc2_kernel variant that fit at once
 };
 DeviceInfo g_dev[kMaxDevices];
@@ -923,6 +925,53 @@ int launch_bwd_mma(const rc::BwdKeys& keys, const rc::BwdQueries& queries, const
   return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "attn_bwd_mma kernel launch");
 }
 
+// The boxes that the tcgen05 kernels load: 64 rows x 64 columns, and 128 rows x D / 2 columns.
+int bwd_maps(const rc::BwdArgs& a, int H, int D, rc::BwdMaps* for_keys, rc::BwdMaps* for_queries) {
+  rc::BwdMaps m{};
+  int rc = 0;
+  auto rows_box = [&](CUtensorMap* t, const void* p, int64_t rows) { return rc = make_tmap(t, p, rows, H, D, 64, 64); };
+  auto cols_box = [&](CUtensorMap* t, const void* p, int64_t rows) { return rc = make_tmap(t, p, rows, H, D, 128, static_cast<uint32_t>(D / 2)); };
+  if (rows_box(&m.q, a.q, a.rows) || rows_box(&m.d_o, a.d_o, a.rows) || rows_box(&m.ka, a.ka, a.a_rows) || rows_box(&m.va, a.va, a.a_rows))
+    return rc;
+  m.kb = m.ka, m.vb = m.va;
+  if (a.b_rows > 0 && (rows_box(&m.kb, a.kb, a.b_rows) || rows_box(&m.vb, a.vb, a.b_rows))) return rc;
+  *for_keys = *for_queries = m;
+  if (cols_box(&for_keys->cols0, a.d_o, a.rows) || cols_box(&for_keys->cols1, a.q, a.rows) || cols_box(&for_queries->cols0, a.ka, a.a_rows))
+    return rc;
+  for_queries->cols1 = for_queries->cols0;
+  return a.b_rows > 0 ? cols_box(&for_queries->cols1, a.kb, a.b_rows) : REFCACHE_OK;
+}
+
+// One of the tcgen05 kernels: a programmatic dependent on as many CTA pairs as fit at once.
+template <typename Kernel, typename List>
+int launch_bwd_tc(Kernel kernel, uint32_t smem, int which, const rc::BwdMaps& maps, const List& list, const rc::BwdArgs& a, DeviceInfo* info,
+                  cudaStream_t s) {
+  if (list.n_tiles == 0) return REFCACHE_OK;
+  if (info->bwd_clusters[which] == 0) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(attn_bwd)");
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(2 * static_cast<unsigned>(info->num_sms / 2), 1, 1);
+    cfg.blockDim = dim3(rc::bwd::kThreads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    int clusters = 0;
+    e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg);
+    info->bwd_clusters[which] = e == cudaSuccess && clusters > 0 ? clusters : info->num_sms / 2;
+  }
+  const int64_t items = static_cast<int64_t>(list.n_tiles) * a.num_heads;
+  const unsigned clusters = static_cast<unsigned>(std::min<int64_t>(items, info->bwd_clusters[which]));
+  const cudaError_t e = rc_host::launch_dependent(kernel, dim3(2 * clusters), dim3(rc::bwd::kThreads), smem, s, maps, list, a);
+  return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "attn_bwd kernel launch");
+}
+
+template <int D>
+int launch_bwd(const rc::BwdKeys& keys, const rc::BwdQueries& queries, const rc::BwdMaps& for_keys, const rc::BwdMaps& for_queries,
+               const rc::BwdArgs& a, DeviceInfo* info, cudaStream_t s) {
+  const int v = D == 64 ? 0 : 2;
+  const int rc = launch_bwd_tc(rc::attn_bwd_keys_kernel<D>, rc::bwd::Smem<D, true>::kDynamic, v, for_keys, keys, a, info, s);
+  return rc ? rc : launch_bwd_tc(rc::attn_bwd_queries_kernel<D>, rc::bwd::Smem<D, false>::kDynamic, v + 1, for_queries, queries, a, info, s);
+}
+
 // The gradients of `batch` requests, request(b, &out) naming what request b's rows see.
 template <typename Request>
 int run_backward(int batch, int H, int D, rc::BwdArgs a, const float* lse, const void* o, void* work, float scale, int* status,
@@ -944,25 +993,33 @@ int run_backward(int batch, int H, int D, rc::BwdArgs a, const float* lse, const
     const cudaError_t e = D == 128 ? go(rc::attn_bwd_prep_kernel<128>) : go(rc::attn_bwd_prep_kernel<64>);
     if (e != cudaSuccess) return cuda_fail(e, "attn_bwd_prep_kernel launch");
   }
+  const bool mma = g_kernel.load() == REFCACHE_KERNEL_MMA_SYNC;
+  const int tile = mma ? rc::mm::kBwdRows : rc::bwd::kBlock;
+  rc::BwdMaps for_keys{}, for_queries{};
+  if (!mma && a.rows > 0) {
+    const int rc = bwd_maps(a, H, D, &for_keys, &for_queries);
+    if (rc) return rc;
+  }
   for (int b0 = 0; b0 < batch; b0 += kBwdRequests) {
     rc::BwdQueries queries{};
     rc::BwdKeys keys{};
-    const int tile_q = rc::mm::kBwdRows, tile_k = rc::mm::kBwdRows;
     for (int b = b0; b < std::min(batch, b0 + kBwdRequests); ++b) {
       BwdRequest r;
       request(b, &r);
       for (int i = 0; i < r.nq; ++i) {
         r.q[i].tile0 = queries.n_tiles;
-        queries.n_tiles += (r.q[i].q_rows + tile_q - 1) / tile_q;
+        queries.n_tiles += (r.q[i].q_rows + tile - 1) / tile;
         queries.seg[queries.n++] = r.q[i];
       }
       for (int i = 0; i < r.nk; ++i) {
         r.k[i].tile0 = keys.n_tiles;
-        keys.n_tiles += (r.k[i].k_rows + tile_k - 1) / tile_k;
+        keys.n_tiles += (r.k[i].k_rows + tile - 1) / tile;
         keys.seg[keys.n++] = r.k[i];
       }
     }
-    const int rc = D == 64 ? launch_bwd_mma<64>(keys, queries, a, info, s) : launch_bwd_mma<128>(keys, queries, a, info, s);
+    const int rc = mma ? (D == 64 ? launch_bwd_mma<64>(keys, queries, a, info, s) : launch_bwd_mma<128>(keys, queries, a, info, s))
+                   : D == 64 ? launch_bwd<64>(keys, queries, for_keys, for_queries, a, info, s)
+                             : launch_bwd<128>(keys, queries, for_keys, for_queries, a, info, s);
     if (rc) return rc;
   }
   return REFCACHE_OK;
