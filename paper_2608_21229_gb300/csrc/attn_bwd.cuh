@@ -61,19 +61,32 @@ struct BwdArgs {
   float scale, scale_log2;
   uint64_t timeout_ns;
   int* status;
+  int *work_keys, *work_queries;  // tcgen05 kernels: counters of items, zero at launch (null: fixed order)
+  int32_t behind_queries;         // keys kernel: launched right behind the queries kernel
 };
+// The workspace of a call: the statistics, then a pair of counters for each list of requests.
+constexpr int kBwdCounters = 256;
 
+// Item `it` of a list: runs in the list's order (longest first), within a run
+// head by head, so that the CTAs that work at the same time share few heads' rows
+// in the L2.
+struct BwdItem {
+  int seg, head, tile;  // tile within the run
+};
 template <typename List>
-__device__ __forceinline__ int bwd_seg(const List& l, int tile) {
+__device__ __forceinline__ BwdItem bwd_item(const List& l, int it, int num_heads) {
+  const int at = it / num_heads;
   int lo = 0, hi = l.n - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if (l.seg[mid].tile0 <= tile)
+    if (l.seg[mid].tile0 <= at)
       lo = mid;
     else
       hi = mid - 1;
   }
-  return lo;
+  const int first = l.seg[lo].tile0, tiles = (lo + 1 < l.n ? l.seg[lo + 1].tile0 : l.n_tiles) - first;
+  const int r = it - first * num_heads;
+  return BwdItem{lo, r / tiles, r % tiles};
 }
 
 // stats[head][row] = (lse log2 e, delta).  A block takes 256 / (D / 8) rows of four
@@ -86,6 +99,8 @@ __global__ void __launch_bounds__(256) attn_bwd_prep_kernel(const __nv_bfloat16*
   constexpr int kLanes = D / 8, kRows = 256 / kLanes;
   grid_dependency_wait();
   if (threadIdx.x == 0) grid_launch_dependents();
+  static_assert(kBwdCounters == 256, "one counter per thread");
+  if (blockIdx.x == 0 && blockIdx.y == 0) reinterpret_cast<int*>(stats + rows * num_heads)[threadIdx.x] = 0;
   const int l = threadIdx.x % kLanes;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / kLanes;
   const int h0 = blockIdx.y * kBwdPrepHeads;
@@ -175,9 +190,10 @@ __global__ void __launch_bounds__(128) attn_bwd_mma_keys_kernel(const __grid_con
   __nv_bfloat16* sO = sQ + 2 * kBwdStep * D;
   float2* sT = reinterpret_cast<float2*>(sO + 2 * kBwdStep * D);
   auto off = [](int row, int ch) { return row * D + ((ch ^ (row & 7)) << 3); };
-  const int head = blockIdx.x / keys.n_tiles, tile = blockIdx.x % keys.n_tiles;
-  const BwdKeySeg sg = keys.seg[bwd_seg(keys, tile)];
-  const int r0 = (tile - sg.tile0) * kBwdRows, nk = min(kBwdRows, sg.k_rows - r0);
+  const BwdItem item = bwd_item(keys, blockIdx.x, a.num_heads);
+  const int head = item.head;
+  const BwdKeySeg sg = keys.seg[item.seg];
+  const int r0 = item.tile * kBwdRows, nk = min(kBwdRows, sg.k_rows - r0);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t ld = a.row_stride;
   auto load_rows = [&](__nv_bfloat16* dst, const __nv_bfloat16* src, int64_t row0, int n, int valid) {
@@ -267,9 +283,10 @@ __global__ void __launch_bounds__(128) attn_bwd_mma_queries_kernel(const __grid_
   __nv_bfloat16* sK = sO + kBwdRows * D;
   __nv_bfloat16* sV = sK + 2 * kBwdStep * D;
   auto off = [](int row, int ch) { return row * D + ((ch ^ (row & 7)) << 3); };
-  const int head = blockIdx.x / queries.n_tiles, tile = blockIdx.x % queries.n_tiles;
-  const BwdQuerySeg sg = queries.seg[bwd_seg(queries, tile)];
-  const int r0 = (tile - sg.tile0) * kBwdRows, nq = min(kBwdRows, sg.q_rows - r0);
+  const BwdItem item = bwd_item(queries, blockIdx.x, a.num_heads);
+  const int head = item.head;
+  const BwdQuerySeg sg = queries.seg[item.seg];
+  const int r0 = item.tile * kBwdRows, nq = min(kBwdRows, sg.q_rows - r0);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t ld = a.row_stride;
   auto load_rows = [&](__nv_bfloat16* dst, const __nv_bfloat16* src, int64_t row0, int n, int valid) {

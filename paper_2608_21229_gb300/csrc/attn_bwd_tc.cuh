@@ -30,6 +30,12 @@
 // written over the columns that the same warp has read), 8 TMA producer, 9 MMAs
 // (leader), 10 statistics of the query tiles (keys kernel).
 //
+// The queries kernel is launched first and the keys kernel as its programmatic
+// dependent: the keys kernel's CTAs take SMs as the queries kernel's leave, which they
+// need not wait for (its CTAs have all passed their own wait for the pass over the
+// outputs by then), only before their own end.  Items are handed out to whichever
+// pair is free.
+//
 // All waits are bounded as in attn_tc2_kernel, and the teardown is that kernel's:
 // loads complete on the leader's barriers, which it arms for both CTAs' bytes.
 #pragma once
@@ -51,6 +57,7 @@ constexpr int kScoreWarps = 8, kProducerWarp = 8, kMmaWarp = 9, kStatWarp = 10;
 constexpr int kTile = 128;   // rows of a tile
 constexpr int kBlock = 256;  // rows of an item
 constexpr int kStatSlots = 2;
+constexpr int kItemSlots = 4;
 
 template <int D, bool kKeys>
 struct Smem {
@@ -66,11 +73,16 @@ struct Smem {
   static constexpr int kOwnFull = 0, kOwnEmpty = 1, kNFull = 2, kNEmpty = kNFull + kNStages, kDFull = kNEmpty + kNStages,
                        kDEmpty = kDFull + kDStages, kSDone = kDEmpty + kDStages, kPDone = kSDone + 1, kSUsed = kPDone + 2,
                        kDsFull = kSUsed + 1, kAccDone = kDsFull + 2, kAccFree = kAccDone + 1, kStatFull = kAccFree + 1,
-                       kStatEmpty = kStatFull + kStatSlots, kMmaDone = kStatEmpty + kStatSlots, kNumBars = kMmaDone + 1;
+                       kStatEmpty = kStatFull + kStatSlots, kItemFull = kStatEmpty + kStatSlots,
+                       kItemEmpty = kItemFull + kItemSlots, kMmaDone = kItemEmpty + kItemSlots, kNumBars = kMmaDone + 1;
+  // warps that read each item from the ring: the leader's MMA warp, the follower's
+  // producer, and the score (and statistics) warps of both
+  static constexpr int kItemTakers = 2 + 2 * kScoreWarps + (kKeys ? 2 : 0);
   static constexpr uint32_t kTmemHolder = kBars + 8 * kNumBars;
   static constexpr uint32_t kAbort = kTmemHolder + 4, kPeerAbort = kAbort + 4;
   static constexpr uint32_t kLoadRec = kPeerAbort + 4;  // each CTA's loads: own rows, rows ring, columns ring
-  static constexpr uint32_t kUsed = kLoadRec + 24;
+  static constexpr uint32_t kItemRing = kLoadRec + 24;
+  static constexpr uint32_t kUsed = kItemRing + 4 * kItemSlots;
   static constexpr uint32_t kMaxDynamic = 232448;
   static constexpr uint32_t kDynamic = kUsed + 1024 < kMaxDynamic ? kUsed + 1024 : kMaxDynamic;
   static_assert(kUsed <= kMaxDynamic, "shared-memory layout too large");
@@ -153,11 +165,52 @@ struct Cta {
     return tc::wait_one(bar(i), static_cast<uint32_t>(n) & 1u, ctl, where);
   }
   __device__ __forceinline__ bool wait_all(int i, int n, int where) const { return __all_sync(0xffffffffu, wait(i, n, where)); }
+  // Items reach the warps through a ring in the shared memory of both CTAs.  The
+  // leader's producer (one lane) passes on item k, -1 when none is left:
+  __device__ __forceinline__ bool publish(int k, int item) const {
+    const int s = k % kItemSlots;
+    if (k >= kItemSlots && !(wait(L::kItemEmpty + s, k / kItemSlots - 1, 81) &&
+                             mbar_try_wait_acquire_cluster(bar(L::kItemEmpty + s), static_cast<uint32_t>(k / kItemSlots - 1) & 1u)))
+      return false;
+    const uint32_t at = base + L::kItemRing + 4u * static_cast<uint32_t>(s);
+    st_cluster_u32(mapa_shared(at, 0), static_cast<uint32_t>(item));
+    st_cluster_u32(mapa_shared(at, 1), static_cast<uint32_t>(item));
+    mbar_arrive_release_cluster(mapa_shared(bar(L::kItemFull + s), 0));
+    mbar_arrive_release_cluster(mapa_shared(bar(L::kItemFull + s), 1));
+    return true;
+  }
+  // and the other roles take it, a whole warp (`lanes` 32) or one lane alone; -2: gave up.
+  __device__ __forceinline__ int take(int k, bool whole_warp) const {
+    const int s = k % kItemSlots;
+    const uint32_t parity = static_cast<uint32_t>(k / kItemSlots) & 1u;
+    bool ok = wait(L::kItemFull + s, k / kItemSlots, 82) && mbar_try_wait_acquire_cluster(bar(L::kItemFull + s), parity);
+    if (whole_warp) ok = __all_sync(0xffffffffu, ok);
+    if (!ok) return -2;
+    const int item = *reinterpret_cast<const volatile int*>(ptr + L::kItemRing + 4 * s);
+    if (whole_warp) __syncwarp();
+    if (!whole_warp || lane == 0) mbar_arrive_release_cluster(lbar(L::kItemEmpty + s));
+    return whole_warp ? __shfl_sync(0xffffffffu, item, 0) : item;
+  }
+};
+// The leader's choice of items: its cluster's index first, then the next of the
+// list (a counter that the pass over the outputs has set to zero), or every
+// n_clusters-th without a counter.
+struct Chooser {
+  int* work;
+  int cluster, n_clusters, n_items;
+  int k = 0;  // items chosen
+  __device__ __forceinline__ int next() {
+    const int64_t it = k == 0 ? cluster : work ? static_cast<int64_t>(n_clusters) + atomicAdd(work, 1)
+                                               : cluster + static_cast<int64_t>(k) * n_clusters;
+    ++k;
+    return it < n_items ? static_cast<int>(it) : -1;
+  }
 };
 
-// Returns false where the block has to leave (both CTAs of the pair alike).
+// Returns false where the block has to leave (both CTAs of the pair alike).  late:
+// the wait for the kernel before this one is at the end (BwdArgs::behind_queries).
 template <typename L>
-__device__ __forceinline__ bool enter(Cta<L>& c, uint8_t* smem, const BwdArgs& a, const BwdMaps& maps) {
+__device__ __forceinline__ bool enter(Cta<L>& c, uint8_t* smem, const BwdArgs& a, const BwdMaps& maps, bool late) {
   const uint32_t raw = smem_u32(smem);
   c.base = (raw + 1023u) & ~1023u;
   c.ptr = smem + (c.base - raw);
@@ -167,6 +220,7 @@ __device__ __forceinline__ bool enter(Cta<L>& c, uint8_t* smem, const BwdArgs& a
   c.lane = threadIdx.x & 31;
   if (c.base - raw + L::kUsed > L::kDynamic) {
     if (threadIdx.x == 0) tc::report_timeout(a.status, 98);
+    if (late) grid_dependency_wait();
     return false;
   }
   volatile int* abort_flag = reinterpret_cast<volatile int*>(c.ptr + L::kAbort);
@@ -175,7 +229,8 @@ __device__ __forceinline__ bool enter(Cta<L>& c, uint8_t* smem, const BwdArgs& a
     for (int i = 0; i < L::kNumBars; ++i) {
       const bool scores = i == L::kSUsed || i == L::kDsFull || i == L::kDsFull + 1 || i == L::kAccFree;
       const bool local = i >= L::kStatEmpty && i < L::kStatEmpty + kStatSlots;
-      mbar_init(c.bar(i), scores ? 2 * kScoreWarps : local ? kScoreWarps : 1);
+      const bool items = i >= L::kItemEmpty && i < L::kItemEmpty + kItemSlots;
+      mbar_init(c.bar(i), scores ? 2 * kScoreWarps : local ? kScoreWarps : items ? L::kItemTakers : 1);
     }
     *abort_flag = 0;
     fence_barrier_init();
@@ -198,7 +253,7 @@ __device__ __forceinline__ bool enter(Cta<L>& c, uint8_t* smem, const BwdArgs& a
   cluster_sync();
   tc_fence_after();
   c.ctl = Ctl{abort_flag, a.timeout_ns, a.status};
-  grid_dependency_wait();
+  if (!late) grid_dependency_wait();
   if (threadIdx.x == 0) grid_launch_dependents();
   c.tmem = __shfl_sync(0xffffffffu, *holder, 0);
   return true;
@@ -272,7 +327,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
   constexpr uint32_t kColS = 0, kColP = 128, kColV = 256, kColK = 384;
   extern __shared__ uint8_t smem_raw[];
   Cta<L> c;
-  if (!enter(c, smem_raw, args, maps)) return;
+  if (!enter(c, smem_raw, args, maps, args.behind_queries != 0)) return;
   const int cluster = static_cast<int>(blockIdx.x >> 1), n_clusters = static_cast<int>(gridDim.x >> 1);
   const int n_items = keys.n_tiles * args.num_heads;
   struct Item {
@@ -280,10 +335,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
   };
   auto item_of = [&](int it) -> Item {
     Item t;
-    t.head = it / keys.n_tiles;
-    const int tile = it - t.head * keys.n_tiles;
-    const BwdKeySeg& s = keys.seg[bwd_seg(keys, tile)];
-    const int r0 = (tile - s.tile0) * kBlock;
+    const BwdItem i = bwd_item(keys, it, args.num_heads);
+    t.head = i.head;
+    const BwdKeySeg& s = keys.seg[i.seg];
+    const int r0 = i.tile * kBlock;
     t.row0 = s.k_row0 + r0;
     t.rows = min(kBlock, s.k_rows - r0);
     t.q0 = s.q_row0;
@@ -297,10 +352,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
   int own = 0, nn = 0, nd = 0;  // loads issued
   if (c.warp == kProducerWarp) {
     if (c.lane == 0) {
+      Chooser choose{args.work_keys, cluster, n_clusters, n_items};
+      int it = c.leader ? choose.next() : 0;
+      if (c.leader && !c.publish(0, it)) it = -2;
 #pragma unroll 1
-      for (int it = cluster; it < n_items; it += n_clusters) {
+      for (int k = 0;; ++k) {
+        if (!c.leader) it = c.take(k, false);
+        if (it < 0) break;
+        int ahead = c.leader ? choose.next() : 0;  // used two tiles later
         const Item t = item_of(it);
-        if (t.nt == 0) continue;
+        if (t.nt == 0) {
+          if (c.leader && !c.publish(k + 1, ahead)) break;
+          it = ahead;
+          continue;
+        }
         const int x = t.head * D, xc = x + D / 2 * static_cast<int>(c.rank);
         if (own > 0 && !c.wait(L::kOwnEmpty, own - 1, 31)) break;
         if (c.leader) mbar_arrive_expect_tx(c.bar(L::kOwnFull), 4 * L::kOwn);
@@ -325,8 +390,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
           tma_load_2d_pair(d, &maps.cols0, c.lbar(L::kDFull + ds), xc, y0);
           tma_load_2d_pair(d + L::kHalf, &maps.cols1, c.lbar(L::kDFull + ds), xc, y0);
           ++nd;
+          if (c.leader && j == min(1, t.nt - 1) && !(ok = c.publish(k + 1, ahead))) break;
         }
         if (!ok) break;
+        it = ahead;
       }
     }
     __syncwarp();
@@ -336,9 +403,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
       const uint64_t nd0 = sdesc_sw128(c.base + L::kN, 16, 1024), dd0 = cols_desc<D>(c.base + L::kD);
       const uint32_t tm = c.tmem;
       bool issued = false;
-      int t = 0, k = 0;  // tiles and items so far
+      int t = 0, k = 0;  // tiles, and items with tiles, so far
 #pragma unroll 1
-      for (int it = cluster; it < n_items; it += n_clusters) {
+      for (int i = 0;; ++i) {
+        const int it = c.take(i, true);
+        if (it < 0) break;
         const int nt = __shfl_sync(0xffffffffu, item_of(it).nt, 0);
         if (nt == 0) continue;
         // S and dP of tile i (dP's commit also frees the tile's rows)
@@ -402,7 +471,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
     int t = 0;
     bool ok = true;
 #pragma unroll 1
-    for (int it = cluster; ok && it < n_items; it += n_clusters) {
+    for (int i = 0; ok; ++i) {
+      const int it = c.take(i, true);
+      if (it < 0) break;
       const Item m = item_of(it);
       const float2* src = args.stats + m.head * args.rows + m.q0;
 #pragma unroll 1
@@ -439,7 +510,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
     };
     int t = 0, k = 0;
 #pragma unroll 1
-    for (int it = cluster; it < n_items; it += n_clusters) {
+    for (int i = 0;; ++i) {
+      const int it = c.take(i, true);
+      if (it < 0) break;
       const Item m = item_of(it);
 #pragma unroll 1
       for (int j = 0; j < m.nt; ++j, ++t) {
@@ -537,6 +610,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
   scores_done:;
   }
   leave(c, own, nn, nd);
+  if (args.behind_queries) grid_dependency_wait();  // the work after this kernel sees both
 }
 
 template <int D>
@@ -548,7 +622,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
   constexpr uint32_t kColS = 0, kColP = 128, kColQ = 384;
   extern __shared__ uint8_t smem_raw[];
   Cta<L> c;
-  if (!enter(c, smem_raw, args, maps)) return;
+  if (!enter(c, smem_raw, args, maps, false)) return;
   const int cluster = static_cast<int>(blockIdx.x >> 1), n_clusters = static_cast<int>(gridDim.x >> 1);
   const int n_items = queries.n_tiles * args.num_heads;
   struct Item {
@@ -556,10 +630,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
   };
   auto item_of = [&](int it) -> Item {
     Item t;
-    t.head = it / queries.n_tiles;
-    const int tile = it - t.head * queries.n_tiles;
-    const BwdQuerySeg& s = queries.seg[bwd_seg(queries, tile)];
-    const int r0 = (tile - s.tile0) * kBlock;
+    const BwdItem i = bwd_item(queries, it, args.num_heads);
+    t.head = i.head;
+    const BwdQuerySeg& s = queries.seg[i.seg];
+    const int r0 = i.tile * kBlock;
     t.row0 = s.q_row0 + r0;
     t.rows = min(kBlock, s.q_rows - r0);
     t.a0 = s.a_row0, t.a_len = s.a_len, t.b0 = s.b_row0, t.b_len = s.b_len;
@@ -570,8 +644,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
   int own = 0, nn = 0, nd = 0;  // loads issued
   if (c.warp == kProducerWarp) {
     if (c.lane == 0) {
+      Chooser choose{args.work_queries, cluster, n_clusters, n_items};
+      int it = c.leader ? choose.next() : 0;
+      if (c.leader && !c.publish(0, it)) it = -2;
 #pragma unroll 1
-      for (int it = cluster; it < n_items; it += n_clusters) {
+      for (int k = 0;; ++k) {
+        if (!c.leader) it = c.take(k, false);
+        if (it < 0) break;
+        int ahead = c.leader ? choose.next() : 0;  // used two tiles later
         const Item t = item_of(it);
         const int x = t.head * D, xc = x + D / 2 * static_cast<int>(c.rank);
         if (own > 0 && !c.wait(L::kOwnEmpty, own - 1, 51)) break;
@@ -596,8 +676,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
           if (c.leader) mbar_arrive_expect_tx(c.bar(L::kDFull + ds), 2 * L::kDBytes);
           tma_load_2d_pair(c.base + L::kD + ds * L::kDBytes, b ? &maps.cols1 : &maps.cols0, c.lbar(L::kDFull + ds), xc, y0);
           ++nd;
+          if (c.leader && j == min(1, t.nt - 1) && !(ok = c.publish(k + 1, ahead))) break;
         }
         if (!ok) break;
+        it = ahead;
       }
     }
     __syncwarp();
@@ -607,9 +689,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
       const uint64_t nd0 = sdesc_sw128(c.base + L::kN, 16, 1024), dd0 = cols_desc<D>(c.base + L::kD);
       const uint32_t tm = c.tmem;
       bool issued = false;
-      int t = 0, k = 0;
+      int t = 0;
 #pragma unroll 1
-      for (int it = cluster; it < n_items; it += n_clusters, ++k) {
+      for (int k = 0;; ++k) {
+        const int it = c.take(k, true);
+        if (it < 0) break;
         const int nt = __shfl_sync(0xffffffffu, item_of(it).nt, 0);
         if (!c.wait_all(L::kOwnFull, k, 54)) goto mma_done;
         // step j: S and dP of tile j, then dQ of tile j - 1
@@ -662,9 +746,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
     const uint32_t t_s = c.tmem + lanes + kColS + 64 * half, t_p = c.tmem + lanes + kColP + 64 * half;
     const f32x2 sl2 = make_f32x2(args.scale_log2, args.scale_log2);
     const uint32_t l_used = c.lbar(L::kSUsed), l_ds = c.lbar(L::kDsFull), l_free = c.lbar(L::kAccFree);
-    int t = 0, k = 0;
+    int t = 0;
 #pragma unroll 1
-    for (int it = cluster; it < n_items; it += n_clusters, ++k) {
+    for (int k = 0;; ++k) {
+      const int it = c.take(k, true);
+      if (it < 0) break;
       const Item m = item_of(it);
       const int row = 128 * static_cast<int>(c.rank) + lane0;  // the warp's first row in the item
       const float2 st = row + c.lane < m.rows ? args.stats[m.head * args.rows + m.row0 + row + c.lane] : make_float2(INFINITY, 0.f);

@@ -966,10 +966,11 @@ int launch_bwd_tc(Kernel kernel, uint32_t smem, int which, const rc::BwdMaps& ma
 
 template <int D>
 int launch_bwd(const rc::BwdKeys& keys, const rc::BwdQueries& queries, const rc::BwdMaps& for_keys, const rc::BwdMaps& for_queries,
-               const rc::BwdArgs& a, DeviceInfo* info, cudaStream_t s) {
+               rc::BwdArgs a, DeviceInfo* info, cudaStream_t s) {
+  a.behind_queries = queries.n_tiles > 0;
   const int v = D == 64 ? 0 : 2;
-  const int rc = launch_bwd_tc(rc::attn_bwd_keys_kernel<D>, rc::bwd::Smem<D, true>::kDynamic, v, for_keys, keys, a, info, s);
-  return rc ? rc : launch_bwd_tc(rc::attn_bwd_queries_kernel<D>, rc::bwd::Smem<D, false>::kDynamic, v + 1, for_queries, queries, a, info, s);
+  const int rc = launch_bwd_tc(rc::attn_bwd_queries_kernel<D>, rc::bwd::Smem<D, false>::kDynamic, v + 1, for_queries, queries, a, info, s);
+  return rc ? rc : launch_bwd_tc(rc::attn_bwd_keys_kernel<D>, rc::bwd::Smem<D, true>::kDynamic, v, for_keys, keys, a, info, s);
 }
 
 // The gradients of `batch` requests, request(b, &out) naming what request b's rows see.
@@ -993,6 +994,7 @@ int run_backward(int batch, int H, int D, rc::BwdArgs a, const float* lse, const
     const cudaError_t e = D == 128 ? go(rc::attn_bwd_prep_kernel<128>) : go(rc::attn_bwd_prep_kernel<64>);
     if (e != cudaSuccess) return cuda_fail(e, "attn_bwd_prep_kernel launch");
   }
+  int* counters = reinterpret_cast<int*>(static_cast<float2*>(work) + a.rows * H);
   const bool mma = g_kernel.load() == REFCACHE_KERNEL_MMA_SYNC;
   const int tile = mma ? rc::mm::kBwdRows : rc::bwd::kBlock;
   rc::BwdMaps for_keys{}, for_queries{};
@@ -1006,16 +1008,31 @@ int run_backward(int batch, int H, int D, rc::BwdArgs a, const float* lse, const
     for (int b = b0; b < std::min(batch, b0 + kBwdRequests); ++b) {
       BwdRequest r;
       request(b, &r);
-      for (int i = 0; i < r.nq; ++i) {
-        r.q[i].tile0 = queries.n_tiles;
-        queries.n_tiles += (r.q[i].q_rows + tile - 1) / tile;
-        queries.seg[queries.n++] = r.q[i];
-      }
-      for (int i = 0; i < r.nk; ++i) {
-        r.k[i].tile0 = keys.n_tiles;
-        keys.n_tiles += (r.k[i].k_rows + tile - 1) / tile;
-        keys.seg[keys.n++] = r.k[i];
-      }
+      for (int i = 0; i < r.nq; ++i) queries.seg[queries.n++] = r.q[i];
+      for (int i = 0; i < r.nk; ++i) keys.seg[keys.n++] = r.k[i];
+    }
+    // longest items first: they are handed out in this order
+    std::sort(queries.seg, queries.seg + queries.n, [](const rc::BwdQuerySeg& x, const rc::BwdQuerySeg& y) {
+      const int64_t nx = static_cast<int64_t>(x.a_len) + x.b_len, ny = static_cast<int64_t>(y.a_len) + y.b_len;
+      return nx != ny ? nx > ny : x.q_row0 < y.q_row0;
+    });
+    std::sort(keys.seg, keys.seg + keys.n, [](const rc::BwdKeySeg& x, const rc::BwdKeySeg& y) {
+      return x.q_rows != y.q_rows ? x.q_rows > y.q_rows : x.in_b != y.in_b ? x.in_b < y.in_b : x.k_row0 < y.k_row0;
+    });
+    for (int i = 0; i < queries.n; ++i) {
+      queries.seg[i].tile0 = queries.n_tiles;
+      queries.n_tiles += (queries.seg[i].q_rows + tile - 1) / tile;
+    }
+    for (int i = 0; i < keys.n; ++i) {
+      keys.seg[i].tile0 = keys.n_tiles;
+      keys.n_tiles += (keys.seg[i].k_rows + tile - 1) / tile;
+    }
+    const int list = b0 / kBwdRequests;
+    if (a.rows > 0 && 2 * list + 1 < rc::kBwdCounters) {
+      a.work_keys = counters + 2 * list;
+      a.work_queries = counters + 2 * list + 1;
+    } else {
+      a.work_keys = a.work_queries = nullptr;
     }
     const int rc = mma ? (D == 64 ? launch_bwd_mma<64>(keys, queries, a, info, s) : launch_bwd_mma<128>(keys, queries, a, info, s))
                    : D == 64 ? launch_bwd<64>(keys, queries, for_keys, for_queries, a, info, s)
@@ -1434,7 +1451,7 @@ int full_attention_noalloc(int batch, int num_heads, int head_dim, const int32_t
 }
 
 size_t refcache_backward_bytes(int64_t rows, int num_heads) {
-  return rows < 0 || num_heads < 0 ? 0 : static_cast<size_t>(rows) * num_heads * sizeof(float2);
+  return rows < 0 || num_heads < 0 ? 0 : static_cast<size_t>(rows) * num_heads * sizeof(float2) + rc::kBwdCounters * sizeof(int);
 }
 
 int step_attention_backward(refcache_t* h, int layer, const void* q_live, const void* k_live, const void* v_live, const void* o_live,

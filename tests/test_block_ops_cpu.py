@@ -129,4 +129,4 @@ def test_attention_gradient_refusals(lib):
         assert f(1, 4, 64, cu, *t[:i], P + 2, *t[i + 1:], 0.1, None) == rcb.ERR_INVALID_ARG, i
     assert lib.step_attention_backward(None, 0, *[P] * 11, 0, P, 0.1, None) == rcb.ERR_INVALID_ARG
     assert lib.refcache_build_backward(None, 0, *[P] * 12, 0.1, None) == rcb.ERR_INVALID_ARG
-    assert lib.refcache_backward_bytes(100, 24) == 100 * 24 * 8 and lib.refcache_backward_bytes(-1, 2) == 0
+    assert lib.refcache_backward_bytes(100, 24) >= 100 * 24 * 8 and lib.refcache_backward_bytes(-1, 2) == 0
