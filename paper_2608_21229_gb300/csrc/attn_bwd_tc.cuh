@@ -28,7 +28,7 @@
 //
 // Warps: 0-7 scores (warp w: lanes 32 (w % 4).., columns 64 (w / 4)..; P and dS are
 // written over the columns that the same warp has read), 8 TMA producer, 9 MMAs
-// (leader), 10 statistics of the query tiles (keys kernel).
+// (leader), 10 statistics of the query tiles (keys kernel), 11 items (leader).
 //
 // The queries kernel is launched first and the keys kernel as its programmatic
 // dependent: the keys kernel's CTAs take SMs as the queries kernel's leave, which they
@@ -52,37 +52,51 @@ struct BwdMaps {
 
 namespace bwd {
 using tc::Ctl;
-constexpr int kThreads = 32 * 11;
-constexpr int kScoreWarps = 8, kProducerWarp = 8, kMmaWarp = 9, kStatWarp = 10;
+constexpr int kThreads = 32 * 12;
+constexpr int kScoreWarps = 8, kProducerWarp = 8, kMmaWarp = 9, kStatWarp = 10, kItemWarp = 11;
 constexpr int kTile = 128;   // rows of a tile
 constexpr int kBlock = 256;  // rows of an item
 constexpr int kStatSlots = 2;
-constexpr int kItemSlots = 4;
+constexpr int kItemSlots = 2;
 
+// What a CTA keeps of an item is its 128 rows of two operands: X (K or Q), of S, and
+// Y (V or dO), of dP.  R: a tile's rows, half of them in each CTA, of S and of dP;
+// C: its columns.
+//   keys kernel     X and Y once, loaded together; R of S and dP together; an area where
+//                   dK and dV are staged on their way out
+//   queries kernel  X and Y twice, so that an item's first S and dP are issued inside
+//                   the item before it, whose X then takes its dQ on its way out
+// At head dim 64 a tile is half as many bytes and takes less time, so its rings are
+// deeper (a load takes about as long as a tile).
 template <int D, bool kKeys>
 struct Smem {
-  static constexpr uint32_t kOwn = 128 * D * 2;    // this CTA's 128 rows of one operand
-  static constexpr uint32_t kHalf = 64 * D * 2;    // half a tile's rows, or its columns of all rows
-  static constexpr int kNStages = kKeys ? 2 : 3, kDStages = 2;
-  static constexpr uint32_t kNBytes = 2 * kHalf, kDBytes = (kKeys ? 2 : 1) * kHalf;  // one CTA's bytes of a stage
-  static constexpr uint32_t kN = 2 * kOwn;                      // rows ring
-  static constexpr uint32_t kD = kN + kNStages * kNBytes;       // columns ring
-  static constexpr uint32_t kStage = kD + kDStages * kDBytes;   // epilogue: 32 rows x 64 columns per warp
-  static constexpr uint32_t kStat = kStage + kScoreWarps * 4096;
+  static constexpr uint32_t kOwn = 128 * D * 2;  // this CTA's 128 rows of one operand
+  static constexpr uint32_t kHalf = 64 * D * 2;  // half a tile's rows, or half its columns
+  static constexpr int kXSlots = kKeys ? 1 : 2, kYSlots = kXSlots;
+  static constexpr uint32_t kXSlot = kKeys ? kOwn : 32768;  // (32 rows x 64 columns a warp are staged in it)
+  static constexpr uint32_t kXBytes = kKeys ? 2 * kOwn : kOwn;  // one CTA's bytes of a load: with Y in the keys kernel
+  static constexpr int kSlots = D == 64 ? 4 : 2;                // of each ring of a tile
+  static constexpr uint32_t kR1Bytes = kKeys ? 2 * kHalf : kHalf;  // R of dP with R of S, or of S
+  static constexpr uint32_t kCBytes = (kKeys ? 2 : 1) * kHalf;
+  static constexpr uint32_t kX = 0, kY = kX + kXSlots * kXSlot, kR1 = kY + kYSlots * kOwn, kR2 = kR1 + kSlots * kR1Bytes,
+                            kC = kR2 + (kKeys ? 0 : kSlots * kHalf), kStage = kC + kSlots * kCBytes,
+                            kStat = kStage + (kKeys ? kScoreWarps * 4096 : 0);
   static constexpr uint32_t kBars = kStat + (kKeys ? kStatSlots * 1024 : 0);
-  static constexpr int kOwnFull = 0, kOwnEmpty = 1, kNFull = 2, kNEmpty = kNFull + kNStages, kDFull = kNEmpty + kNStages,
-                       kDEmpty = kDFull + kDStages, kSDone = kDEmpty + kDStages, kPDone = kSDone + 1, kSUsed = kPDone + 2,
-                       kDsFull = kSUsed + 1, kAccDone = kDsFull + 2, kAccFree = kAccDone + 1, kStatFull = kAccFree + 1,
-                       kStatEmpty = kStatFull + kStatSlots, kItemFull = kStatEmpty + kStatSlots,
+  // barriers; those of loads first: X, Y, rows of S, rows of dP, columns
+  static constexpr int kXFull = 0, kYFull = kXFull + kXSlots, kR1Full = kYFull + kYSlots, kR2Full = kR1Full + kSlots,
+                       kCFull = kR2Full + kSlots, kXEmpty = kCFull + kSlots, kYEmpty = kXEmpty + kXSlots, kR1Empty = kYEmpty + kYSlots,
+                       kR2Empty = kR1Empty + kSlots, kCEmpty = kR2Empty + kSlots, kSDone = kCEmpty + kSlots, kPDone = kSDone + 1,
+                       kSUsed = kPDone + 2, kDsFull = kSUsed + 1, kAccFree = kDsFull + 2, kAccDone = kAccFree + 1,
+                       kStatFull = kAccDone + 1, kStatEmpty = kStatFull + kStatSlots, kItemFull = kStatEmpty + kStatSlots,
                        kItemEmpty = kItemFull + kItemSlots, kMmaDone = kItemEmpty + kItemSlots, kNumBars = kMmaDone + 1;
-  // warps that read each item from the ring: the leader's MMA warp, the follower's
-  // producer, and the score (and statistics) warps of both
-  static constexpr int kItemTakers = 2 + 2 * kScoreWarps + (kKeys ? 2 : 0);
+  // warps that read each item from the ring: the leader's MMA warp, and the
+  // producer, score (and statistics) warps of both CTAs
+  static constexpr int kItemTakers = 1 + 2 * (1 + kScoreWarps + (kKeys ? 1 : 0));
   static constexpr uint32_t kTmemHolder = kBars + 8 * kNumBars;
   static constexpr uint32_t kAbort = kTmemHolder + 4, kPeerAbort = kAbort + 4;
-  static constexpr uint32_t kLoadRec = kPeerAbort + 4;  // each CTA's loads: own rows, rows ring, columns ring
-  static constexpr uint32_t kItemRing = kLoadRec + 24;
-  static constexpr uint32_t kUsed = kItemRing + 4 * kItemSlots;
+  static constexpr uint32_t kLoadRec = kPeerAbort + 4;  // each CTA's loads: X, Y, rows of S, rows of dP, columns
+  static constexpr uint32_t kItemRing = (kLoadRec + 40 + 15u) & ~15u;
+  static constexpr uint32_t kUsed = kItemRing + 48 * kItemSlots;
   static constexpr uint32_t kMaxDynamic = 232448;
   static constexpr uint32_t kDynamic = kUsed + 1024 < kMaxDynamic ? kUsed + 1024 : kMaxDynamic;
   static_assert(kUsed <= kMaxDynamic, "shared-memory layout too large");
@@ -140,7 +154,7 @@ struct RowsOut {
   __device__ __forceinline__ void flush(__nv_bfloat16* dst, int64_t stride, int rows) const {
     __syncwarp();
     const int r0 = lane >> 3, ch = lane & 7;
-#pragma unroll
+#pragma unroll 4
     for (int i = 0; i < 8; ++i) {
       const int r = 4 * i + r0;
       const uint4 v = ld_shared_v4(stage + 128u * r + (static_cast<uint32_t>(ch ^ (r & 7)) << 4));
@@ -148,6 +162,12 @@ struct RowsOut {
     }
     __syncwarp();
   }
+};
+
+// An item: rows [row0, row0 + rows) of one head and nt tiles of the other side.
+struct Item {
+  int head, row0, rows, nt;
+  int v[5];  // keys kernel: first query row, query rows, in_b, add_from, add_row0; queries kernel: a_row0, a_len, b_row0, b_len, tiles of A
 };
 
 // What both kernels set up before their roles part.
@@ -165,47 +185,54 @@ struct Cta {
     return tc::wait_one(bar(i), static_cast<uint32_t>(n) & 1u, ctl, where);
   }
   __device__ __forceinline__ bool wait_all(int i, int n, int where) const { return __all_sync(0xffffffffu, wait(i, n, where)); }
-  // Items reach the warps through a ring in the shared memory of both CTAs.  The
-  // leader's producer (one lane) passes on item k, -1 when none is left:
-  __device__ __forceinline__ bool publish(int k, int item) const {
+  // Items reach the warps through a ring in the shared memory of both CTAs, decoded.
+  // The leader's item warp (one lane): waits until item k may be chosen, and passes it
+  // on; its head is -1 when none is left.
+  __device__ __forceinline__ bool may_choose(int k) const {
     const int s = k % kItemSlots;
-    if (k >= kItemSlots && !(wait(L::kItemEmpty + s, k / kItemSlots - 1, 81) &&
-                             mbar_try_wait_acquire_cluster(bar(L::kItemEmpty + s), static_cast<uint32_t>(k / kItemSlots - 1) & 1u)))
-      return false;
-    const uint32_t at = base + L::kItemRing + 4u * static_cast<uint32_t>(s);
-    st_cluster_u32(mapa_shared(at, 0), static_cast<uint32_t>(item));
-    st_cluster_u32(mapa_shared(at, 1), static_cast<uint32_t>(item));
-    mbar_arrive_release_cluster(mapa_shared(bar(L::kItemFull + s), 0));
+    return k < kItemSlots || (wait(L::kItemEmpty + s, k / kItemSlots - 1, 81) &&
+                              mbar_try_wait_acquire_cluster(bar(L::kItemEmpty + s), static_cast<uint32_t>(k / kItemSlots - 1) & 1u));
+  }
+  __device__ __forceinline__ void publish(int k, const Item& item) const {
+    const int s = k % kItemSlots;
+    const uint32_t at = base + L::kItemRing + 48u * static_cast<uint32_t>(s);
+    const uint4 x = make_uint4(item.head, item.row0, item.rows, item.nt), y = make_uint4(item.v[0], item.v[1], item.v[2], item.v[3]);
+    const uint4 z = make_uint4(item.v[4], 0, 0, 0);
+    st_shared_v4(at, x);
+    st_shared_v4(at + 16, y);
+    st_shared_v4(at + 32, z);
+    mbar_arrive(bar(L::kItemFull + s));
+    const uint32_t to = mapa_shared(at, 1);
+    st_cluster_v4(to, x);
+    st_cluster_v4(to + 16, y);
+    st_cluster_v4(to + 32, z);
     mbar_arrive_release_cluster(mapa_shared(bar(L::kItemFull + s), 1));
-    return true;
   }
-  // and the other roles take it, a whole warp (`lanes` 32) or one lane alone; -2: gave up.
-  __device__ __forceinline__ int take(int k, bool whole_warp) const {
+  // The other roles wait for it (a whole warp, or one lane alone), read it and, when
+  // they are done with it, release it (one lane).
+  __device__ __forceinline__ bool await(int k, bool whole_warp) const {
     const int s = k % kItemSlots;
-    const uint32_t parity = static_cast<uint32_t>(k / kItemSlots) & 1u;
-    bool ok = wait(L::kItemFull + s, k / kItemSlots, 82) && mbar_try_wait_acquire_cluster(bar(L::kItemFull + s), parity);
-    if (whole_warp) ok = __all_sync(0xffffffffu, ok);
-    if (!ok) return -2;
-    const int item = *reinterpret_cast<const volatile int*>(ptr + L::kItemRing + 4 * s);
-    if (whole_warp) __syncwarp();
-    if (!whole_warp || lane == 0) mbar_arrive_release_cluster(lbar(L::kItemEmpty + s));
-    return whole_warp ? __shfl_sync(0xffffffffu, item, 0) : item;
+    const bool ok = wait(L::kItemFull + s, k / kItemSlots, 82) &&
+                    (leader || mbar_try_wait_acquire_cluster(bar(L::kItemFull + s), static_cast<uint32_t>(k / kItemSlots) & 1u));
+    return whole_warp ? __all_sync(0xffffffffu, ok) : ok;
   }
-};
-// The leader's choice of items: its cluster's index first, then the next of the
-// list (a counter that the pass over the outputs has set to zero), or every
-// n_clusters-th without a counter.
-struct Chooser {
-  int* work;
-  int cluster, n_clusters, n_items;
-  int k = 0;  // items chosen
-  __device__ __forceinline__ int next() {
-    const int64_t it = k == 0 ? cluster : work ? static_cast<int64_t>(n_clusters) + atomicAdd(work, 1)
-                                               : cluster + static_cast<int64_t>(k) * n_clusters;
-    ++k;
-    return it < n_items ? static_cast<int>(it) : -1;
+  __device__ __forceinline__ Item read(int k) const {
+    const uint32_t at = base + L::kItemRing + 48u * static_cast<uint32_t>(k % kItemSlots);
+    const uint4 a = ld_shared_v4(at), b = ld_shared_v4(at + 16), d = ld_shared_v4(at + 32);
+    Item t;
+    t.head = static_cast<int>(a.x), t.row0 = static_cast<int>(a.y), t.rows = static_cast<int>(a.z), t.nt = static_cast<int>(a.w);
+    t.v[0] = static_cast<int>(b.x), t.v[1] = static_cast<int>(b.y), t.v[2] = static_cast<int>(b.z), t.v[3] = static_cast<int>(b.w);
+    t.v[4] = static_cast<int>(d.x);
+    return t;
   }
+  __device__ __forceinline__ void release(int k) const { mbar_arrive_release_cluster(lbar(L::kItemEmpty + k % kItemSlots)); }
 };
+// The item that the leader chooses as its k-th: its cluster's index first, then the
+// next of the list (a counter that the pass over the outputs has set to zero), or
+// every n_clusters-th without a counter.
+__device__ __forceinline__ int64_t choose_item(int* work, int k, int cluster, int n_clusters) {
+  return k == 0 ? cluster : work ? static_cast<int64_t>(n_clusters) + atomicAdd(work, 1) : cluster + static_cast<int64_t>(k) * n_clusters;
+}
 
 // Returns false where the block has to leave (both CTAs of the pair alike).  late:
 // the wait for the kernel before this one is at the end (BwdArgs::behind_queries).
@@ -227,9 +254,9 @@ __device__ __forceinline__ bool enter(Cta<L>& c, uint8_t* smem, const BwdArgs& a
   uint32_t* holder = reinterpret_cast<uint32_t*>(c.ptr + L::kTmemHolder);
   if (threadIdx.x == 0) {
     for (int i = 0; i < L::kNumBars; ++i) {
-      const bool scores = i == L::kSUsed || i == L::kDsFull || i == L::kDsFull + 1 || i == L::kAccFree;
-      const bool local = i >= L::kStatEmpty && i < L::kStatEmpty + kStatSlots;
-      const bool items = i >= L::kItemEmpty && i < L::kItemEmpty + kItemSlots;
+      const bool scores = i >= L::kSUsed && i <= L::kAccFree;  // the score warps of both CTAs
+      const bool local = (i >= L::kStatEmpty && i < L::kItemFull) || (L::kXSlots == 2 && i >= L::kXEmpty && i < L::kYEmpty);  // of this CTA
+      const bool items = i >= L::kItemEmpty && i < L::kMmaDone;
       mbar_init(c.bar(i), scores ? 2 * kScoreWarps : local ? kScoreWarps : items ? L::kItemTakers : 1);
     }
     *abort_flag = 0;
@@ -273,17 +300,20 @@ __device__ __forceinline__ void load_half(uint32_t dst, const CUtensorMap* m, ui
   for (int ch = 0; ch < D / 64; ++ch) tma_load_2d_pair(dst + ch * 8192u, m, full, x + 64 * ch, y);
 }
 
-// Teardown, after the roles (the producer's counts are in `own`, `rows`, `cols` of
-// its lane 0).  As in attn_tc2_kernel: when neither CTA gave up, every load was
-// waited for by the MMAs that read it; else the leader arms or counts what the
-// other CTA's half lacks, and waits for the last phase of each barrier.
+// Loads that a CTA's producer has issued, by ring: X, Y, rows of S, rows of dP, columns.
+struct Loads {
+  int n[5] = {0, 0, 0, 0, 0};
+};
+
+// Teardown, after the roles (`loads` of the producer's lane 0).  As in
+// attn_tc2_kernel: when neither CTA gave up, every load was waited for by the MMAs
+// that read it; else the leader arms or counts what the other CTA's half lacks,
+// and waits for the last phase of each barrier.
 template <typename L>
-__device__ __forceinline__ void leave(const Cta<L>& c, int own, int rows, int cols) {
+__device__ __forceinline__ void leave(const Cta<L>& c, const Loads& loads) {
   if (c.warp == kProducerWarp && c.lane == 0) {
-    const uint32_t rec = mapa_shared(c.base + L::kLoadRec + 12u * c.rank, 0);
-    st_cluster_u32(rec, static_cast<uint32_t>(own));
-    st_cluster_u32(rec + 4, static_cast<uint32_t>(rows));
-    st_cluster_u32(rec + 8, static_cast<uint32_t>(cols));
+#pragma unroll
+    for (int i = 0; i < 5; ++i) st_cluster_u32(mapa_shared(c.base + L::kLoadRec + 20u * c.rank + 4u * i, 0), static_cast<uint32_t>(loads.n[i]));
   }
   tc_fence_before();
   __syncthreads();
@@ -297,25 +327,40 @@ __device__ __forceinline__ void leave(const Cta<L>& c, int own, int rows, int co
   if (*c.ctl.abort_flag == 0 && *reinterpret_cast<const volatile int*>(c.ptr + L::kPeerAbort) == 0) return;
   if (c.leader && c.warp == kProducerWarp && c.lane == 0) {
     const volatile uint32_t* mine = reinterpret_cast<const volatile uint32_t*>(c.ptr + L::kLoadRec);
-    auto settle = [&](int b, int n, int slots, int slot, uint32_t bytes) {
-      auto loads = [&](uint32_t total) { return (static_cast<int>(total) - slot + slots - 1) / slots; };
-      int m = loads(mine[n]);
-      const int theirs = loads(mine[3 + n]);
-      if (theirs == m + 1) {
-        mbar_arrive_expect_tx(c.bar(b), bytes);
-        m = theirs;
-      } else if (m == theirs + 1) {
-        mbar_complete_tx(c.bar(b), bytes);
+    // bytes: one CTA's of a load
+    auto settle = [&](int first, int ring, int slots, uint32_t bytes) {
+#pragma unroll 1
+      for (int slot = 0; slot < slots; ++slot) {
+        auto count = [&](uint32_t total) { return (static_cast<int>(total) - slot + slots - 1) / slots; };
+        int m = count(mine[ring]);
+        const int theirs = count(mine[5 + ring]);
+        if (theirs == m + 1) {
+          mbar_arrive_expect_tx(c.bar(first + slot), bytes);
+          m = theirs;
+        } else if (m == theirs + 1) {
+          mbar_complete_tx(c.bar(first + slot), bytes);
+        }
+        if (m > 0) tc::drain_one(c.bar(first + slot), static_cast<uint32_t>(m - 1) & 1u, c.ctl.timeout_ns);
       }
-      if (m > 0) tc::drain_one(c.bar(b), static_cast<uint32_t>(m - 1) & 1u, c.ctl.timeout_ns);
     };
-    settle(L::kOwnFull, 0, 1, 0, 2 * L::kOwn);
-#pragma unroll 1
-    for (int s = 0; s < L::kNStages; ++s) settle(L::kNFull + s, 1, L::kNStages, s, L::kNBytes);
-#pragma unroll 1
-    for (int s = 0; s < L::kDStages; ++s) settle(L::kDFull + s, 2, L::kDStages, s, L::kDBytes);
+    settle(L::kXFull, 0, L::kXSlots, L::kXBytes);
+    settle(L::kYFull, 1, L::kYSlots, L::kOwn);
+    settle(L::kR1Full, 2, L::kSlots, L::kR1Bytes);
+    settle(L::kR2Full, 3, L::kSlots, L::kHalf);
+    settle(L::kCFull, 4, L::kSlots, L::kCBytes);
   }
   cluster_sync();
+}
+
+// The producer's next load of a ring: waits until its slot is free and arms the
+// barrier (leader); the slot, or -1 when it gave up.
+template <typename L>
+__device__ __forceinline__ int begin_load(const Cta<L>& c, Loads& loads, int ring, int slots, int full, int empty, uint32_t bytes, int where) {
+  const int n = loads.n[ring], slot = n % slots;
+  if (n >= slots && !c.wait(empty + slot, n / slots - 1, where)) return -1;
+  if (c.leader) mbar_arrive_expect_tx(c.bar(full + slot), 2 * bytes);
+  ++loads.n[ring];
+  return slot;
 }
 }  // namespace bwd
 
@@ -324,106 +369,99 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
     attn_bwd_keys_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant__ BwdKeys keys, const __grid_constant__ BwdArgs args) {
   using namespace bwd;
   using L = Smem<D, true>;
-  constexpr uint32_t kColS = 0, kColP = 128, kColV = 256, kColK = 384;
+  constexpr uint32_t kColS = 0, kColP = 128, kColV = 256, kColK = kColV + D;
+  static_assert(kColK + D <= tc::kTmemCols, "tensor-memory layout");
   extern __shared__ uint8_t smem_raw[];
   Cta<L> c;
   if (!enter(c, smem_raw, args, maps, args.behind_queries != 0)) return;
   const int cluster = static_cast<int>(blockIdx.x >> 1), n_clusters = static_cast<int>(gridDim.x >> 1);
   const int n_items = keys.n_tiles * args.num_heads;
-  struct Item {
-    int head, row0, rows, q0, q_rows, nt, in_b, add_from, add_row0;
-  };
-  auto item_of = [&](int it) -> Item {
-    Item t;
-    const BwdItem i = bwd_item(keys, it, args.num_heads);
-    t.head = i.head;
-    const BwdKeySeg& s = keys.seg[i.seg];
-    const int r0 = i.tile * kBlock;
-    t.row0 = s.k_row0 + r0;
-    t.rows = min(kBlock, s.k_rows - r0);
-    t.q0 = s.q_row0;
-    t.q_rows = s.q_rows;
-    t.nt = (s.q_rows + kTile - 1) / kTile;
-    t.in_b = s.in_b;
-    t.add_from = s.add_from - r0;  // within the item
-    t.add_row0 = s.add_row0 + r0;
-    return t;
-  };
-  int own = 0, nn = 0, nd = 0;  // loads issued
+  Loads loads;
   if (c.warp == kProducerWarp) {
     if (c.lane == 0) {
-      Chooser choose{args.work_keys, cluster, n_clusters, n_items};
-      int it = c.leader ? choose.next() : 0;
-      if (c.leader && !c.publish(0, it)) it = -2;
+      int s = 0;
 #pragma unroll 1
-      for (int k = 0;; ++k) {
-        if (!c.leader) it = c.take(k, false);
-        if (it < 0) break;
-        int ahead = c.leader ? choose.next() : 0;  // used two tiles later
-        const Item t = item_of(it);
-        if (t.nt == 0) {
-          if (c.leader && !c.publish(k + 1, ahead)) break;
-          it = ahead;
-          continue;
-        }
-        const int x = t.head * D, xc = x + D / 2 * static_cast<int>(c.rank);
-        if (own > 0 && !c.wait(L::kOwnEmpty, own - 1, 31)) break;
-        if (c.leader) mbar_arrive_expect_tx(c.bar(L::kOwnFull), 4 * L::kOwn);
+      for (int k = 0; s >= 0 && c.await(k, false); ++k) {
+        const Item t = c.read(k);
+        c.release(k);
+        if (t.head < 0) break;
+        if (t.nt == 0) continue;
+        const int x = t.head * D, xc = x + D / 2 * static_cast<int>(c.rank), r64 = 64 * static_cast<int>(c.rank);
         const int y = t.row0 + 128 * static_cast<int>(c.rank);
-        load_own<D>(c.base, t.in_b ? &maps.kb : &maps.ka, c.lbar(L::kOwnFull), x, y);
-        load_own<D>(c.base + L::kOwn, t.in_b ? &maps.vb : &maps.va, c.lbar(L::kOwnFull), x, y);
-        ++own;
-        bool ok = true;
+        if ((s = begin_load(c, loads, 0, 1, L::kXFull, L::kXEmpty, L::kXBytes, 31)) < 0) break;
+        load_own<D>(c.base + L::kX, t.v[2] ? &maps.kb : &maps.ka, c.lbar(L::kXFull), x, y);
+        load_own<D>(c.base + L::kY, t.v[2] ? &maps.vb : &maps.va, c.lbar(L::kXFull), x, y);
 #pragma unroll 1
         for (int j = 0; j < t.nt; ++j) {
-          const int y0 = t.q0 + kTile * j;
-          const int ns = nn % L::kNStages, ds = nd % L::kDStages;
-          if (nn >= L::kNStages && !(ok = c.wait(L::kNEmpty + ns, nn / L::kNStages - 1, 32))) break;
-          if (c.leader) mbar_arrive_expect_tx(c.bar(L::kNFull + ns), 2 * L::kNBytes);
-          const uint32_t n = c.base + L::kN + ns * L::kNBytes;
-          load_half<D>(n, &maps.q, c.lbar(L::kNFull + ns), x, y0 + 64 * static_cast<int>(c.rank));
-          load_half<D>(n + L::kHalf, &maps.d_o, c.lbar(L::kNFull + ns), x, y0 + 64 * static_cast<int>(c.rank));
-          ++nn;
-          if (nd >= L::kDStages && !(ok = c.wait(L::kDEmpty + ds, nd / L::kDStages - 1, 33))) break;
-          if (c.leader) mbar_arrive_expect_tx(c.bar(L::kDFull + ds), 2 * L::kDBytes);
-          const uint32_t d = c.base + L::kD + ds * L::kDBytes;
-          tma_load_2d_pair(d, &maps.cols0, c.lbar(L::kDFull + ds), xc, y0);
-          tma_load_2d_pair(d + L::kHalf, &maps.cols1, c.lbar(L::kDFull + ds), xc, y0);
-          ++nd;
-          if (c.leader && j == min(1, t.nt - 1) && !(ok = c.publish(k + 1, ahead))) break;
+          const int y0 = t.v[0] + kTile * j;
+          if ((s = begin_load(c, loads, 2, L::kSlots, L::kR1Full, L::kR1Empty, L::kR1Bytes, 32)) < 0) break;
+          const uint32_t r = c.base + L::kR1 + s * L::kR1Bytes;
+          load_half<D>(r, &maps.q, c.lbar(L::kR1Full + s), x, y0 + r64);
+          load_half<D>(r + L::kHalf, &maps.d_o, c.lbar(L::kR1Full + s), x, y0 + r64);
+          if ((s = begin_load(c, loads, 4, L::kSlots, L::kCFull, L::kCEmpty, L::kCBytes, 35)) < 0) break;
+          const uint32_t d = c.base + L::kC + s * L::kCBytes;
+          tma_load_2d_pair(d, &maps.cols0, c.lbar(L::kCFull + s), xc, y0);
+          tma_load_2d_pair(d + L::kHalf, &maps.cols1, c.lbar(L::kCFull + s), xc, y0);
         }
-        if (!ok) break;
-        it = ahead;
+      }
+    }
+    __syncwarp();
+  } else if (c.warp == kItemWarp) {
+    if (c.leader && c.lane == 0) {
+      // Kept apart from the producer, whose loads are few tiles ahead: choosing, decoding
+      // and passing on an item takes longer than that.  An item is chosen while the one
+      // before it runs, not earlier: a pair that holds more leaves others idle at the end.
+      auto item_of = [&](int64_t it) -> Item {
+        Item t{};
+        t.head = -1;
+        if (it >= n_items) return t;
+        const BwdItem i = bwd_item(keys, static_cast<int>(it), args.num_heads);
+        const BwdKeySeg& s = keys.seg[i.seg];
+        const int r0 = i.tile * kBlock;
+        t.head = i.head;
+        t.row0 = s.k_row0 + r0;
+        t.rows = min(kBlock, s.k_rows - r0);
+        t.nt = (s.q_rows + kTile - 1) / kTile;
+        t.v[0] = s.q_row0, t.v[1] = s.q_rows, t.v[2] = s.in_b;
+        t.v[3] = s.add_from - r0, t.v[4] = s.add_row0 + r0;  // within the item
+        return t;
+      };
+      for (int k = 0; c.may_choose(k); ++k) {
+        const Item t = item_of(choose_item(args.work_keys, k, cluster, n_clusters));
+        c.publish(k, t);
+        if (t.head < 0) break;
       }
     }
     __syncwarp();
   } else if (c.warp == kMmaWarp) {
     if (c.leader) {
-      const uint64_t kd = sdesc_sw128(c.base, 16, 1024), vd = sdesc_sw128(c.base + L::kOwn, 16, 1024);
-      const uint64_t nd0 = sdesc_sw128(c.base + L::kN, 16, 1024), dd0 = cols_desc<D>(c.base + L::kD);
+      const uint64_t xd = sdesc_sw128(c.base + L::kX, 16, 1024), yd = sdesc_sw128(c.base + L::kY, 16, 1024);
+      const uint64_t rd = sdesc_sw128(c.base + L::kR1, 16, 1024), cd = cols_desc<D>(c.base + L::kC);
       const uint32_t tm = c.tmem;
       bool issued = false;
-      int t = 0, k = 0;  // tiles, and items with tiles, so far
+      int t = 0, n = 0;  // tiles, and items with tiles, so far
+      auto rows = [&](int i) { return rd + static_cast<uint64_t>(i % L::kSlots) * (L::kR1Bytes >> 4); };
+      auto rows_ready = [&](int i) { return c.wait_all(L::kR1Full + i % L::kSlots, i / L::kSlots, 37); };
+      auto issue_s = [&](int i) {
+        mma_rows<D>(tm + kColS, xd, rows(i));
+        tc2_commit_mc(c.bar(L::kSDone), 3);
+      };
+      // (dP's commit also frees the tile's rows and, with the last tile, the item's own)
+      auto issue_dp = [&](int i, bool last) {
+        mma_rows<D>(tm + kColP, yd, rows(i) + (L::kHalf >> 4));
+        tc2_commit_mc(c.bar(L::kPDone), 3);
+        tc2_commit_mc(c.bar(L::kR1Empty + i % L::kSlots), 3);
+        if (last) tc2_commit_mc(c.bar(L::kXEmpty), 3);
+      };
 #pragma unroll 1
-      for (int i = 0;; ++i) {
-        const int it = c.take(i, true);
-        if (it < 0) break;
-        const int nt = __shfl_sync(0xffffffffu, item_of(it).nt, 0);
+      for (int k = 0;; ++k) {
+        if (!c.await(k, true)) goto mma_done;
+        const int head = __shfl_sync(0xffffffffu, c.read(k).head, 0), nt = __shfl_sync(0xffffffffu, c.read(k).nt, 0);
+        __syncwarp();
+        if (c.lane == 0) c.release(k);
+        if (head < 0) break;
         if (nt == 0) continue;
-        // S and dP of tile i (dP's commit also frees the tile's rows)
-        auto slot = [&](int i) { return nd0 + static_cast<uint64_t>(i % L::kNStages) * (L::kNBytes >> 4); };
-        auto cols = [&](int i) { return dd0 + static_cast<uint64_t>(i % L::kDStages) * (L::kDBytes >> 4); };
-        auto issue_s = [&](int i) {
-          mma_rows<D>(tm + kColS, kd, slot(i));
-          tc2_commit_mc(c.bar(L::kSDone), 3);
-        };
-        auto issue_dp = [&](int i, bool last) {
-          mma_rows<D>(tm + kColP, vd, slot(i) + (L::kHalf >> 4));
-          tc2_commit_mc(c.bar(L::kPDone), 3);
-          tc2_commit_mc(c.bar(L::kNEmpty + i % L::kNStages), 3);
-          if (last) tc2_commit_mc(c.bar(L::kOwnEmpty), 3);
-        };
-        if (!c.wait_all(L::kOwnFull, k, 34) || !c.wait_all(L::kNFull + t % L::kNStages, t / L::kNStages, 35)) goto mma_done;
+        if (!c.wait_all(L::kXFull, n, 36) || !rows_ready(t)) goto mma_done;
         issued = true;
         if (elect_one()) {
           tc_fence_after();
@@ -434,21 +472,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
 #pragma unroll 1
         for (int j = 0; j < nt; ++j, ++t) {
           const bool next = j + 1 < nt;
-          if (!c.wait_all(L::kDFull + t % L::kDStages, t / L::kDStages, 36)) goto mma_done;
-          if (j == 0 && k > 0 && !c.wait_all(L::kAccFree, k - 1, 37)) goto mma_done;
-          if (next && !c.wait_all(L::kNFull + (t + 1) % L::kNStages, (t + 1) / L::kNStages, 35)) goto mma_done;
-          if (!c.wait_all(L::kSUsed, t, 38)) goto mma_done;  // P is written
+          const uint64_t cols = cd + static_cast<uint64_t>(t % L::kSlots) * (L::kCBytes >> 4);
+          if (!c.wait_all(L::kCFull + t % L::kSlots, t / L::kSlots, 40)) goto mma_done;
+          if (j == 0 && n > 0 && !c.wait_all(L::kAccFree, n - 1, 41)) goto mma_done;
+          if (next && !rows_ready(t + 1)) goto mma_done;
+          if (!c.wait_all(L::kSUsed, t, 42)) goto mma_done;  // P is written
           if (elect_one()) {
             tc_fence_after();
-            mma_cols<D>(tm + kColV, tm + kColS, cols(t), j > 0 ? 1u : 0u);
+            mma_cols<D>(tm + kColV, tm + kColS, cols, j > 0 ? 1u : 0u);
             if (next) issue_s(t + 1);
           }
           __syncwarp();
-          if (!c.wait_all(L::kDsFull, t, 39)) goto mma_done;
+          if (!c.wait_all(L::kDsFull, t, 43)) goto mma_done;
           if (elect_one()) {
             tc_fence_after();
-            mma_cols<D>(tm + kColK, tm + kColP, cols(t) + (L::kHalf >> 4), j > 0 ? 1u : 0u);
-            tc2_commit_mc(c.bar(L::kDEmpty + t % L::kDStages), 3);
+            mma_cols<D>(tm + kColK, tm + kColP, cols + (L::kHalf >> 4), j > 0 ? 1u : 0u);
+            tc2_commit_mc(c.bar(L::kCEmpty + t % L::kSlots), 3);
             if (next)
               issue_dp(t + 1, j + 2 == nt);
             else
@@ -456,7 +495,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
           }
           __syncwarp();
         }
-        ++k;
+        ++n;
       }
     mma_done:
       __syncwarp();
@@ -471,21 +510,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
     int t = 0;
     bool ok = true;
 #pragma unroll 1
-    for (int i = 0; ok; ++i) {
-      const int it = c.take(i, true);
-      if (it < 0) break;
-      const Item m = item_of(it);
-      const float2* src = args.stats + m.head * args.rows + m.q0;
+    for (int k = 0; ok && c.await(k, true); ++k) {
+      const Item m = c.read(k);
+      __syncwarp();
+      if (c.lane == 0) c.release(k);
+      if (m.head < 0) break;
+      const float2* src = args.stats + m.head * args.rows + m.v[0];
 #pragma unroll 1
       for (int j = 0; j < m.nt; ++j, ++t) {
         float2 v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int r = kTile * j + 32 * i + c.lane;
-          v[i] = r < m.q_rows ? src[r] : make_float2(INFINITY, 0.f);
+          v[i] = r < m.v[1] ? src[r] : make_float2(INFINITY, 0.f);
         }
         const int s = t % kStatSlots;
-        if (t >= kStatSlots && !(ok = c.wait_all(L::kStatEmpty + s, t / kStatSlots - 1, 40))) break;
+        if (t >= kStatSlots && !(ok = c.wait_all(L::kStatEmpty + s, t / kStatSlots - 1, 48))) break;
         float* dst = reinterpret_cast<float*>(c.ptr + L::kStat + 1024 * s);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -498,28 +538,84 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
     }
   } else {
     const int half = c.warp >> 2, lane0 = 32 * (c.warp & 3);
+    const int row = 128 * static_cast<int>(c.rank) + lane0;  // the warp's first row in an item
     const uint32_t lanes = static_cast<uint32_t>(lane0) << 16;
-    const uint32_t t_s = c.tmem + lanes + kColS + 64 * half, t_p = c.tmem + lanes + kColP + 64 * half;
+    const uint32_t t_p = c.tmem + lanes + kColP + 64 * half;
     const f32x2 sl2 = make_f32x2(args.scale_log2, args.scale_log2);
-    const uint32_t l_used = c.lbar(L::kSUsed), l_ds = c.lbar(L::kDsFull), l_free = c.lbar(L::kAccFree);
-    auto arrive = [&](uint32_t b) {
+    const uint32_t l_bars = c.lbar(0);
+    auto arrive = [&](int b) {
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (c.lane == 0) mbar_arrive_cluster(b);
+      if (c.lane == 0) mbar_arrive_cluster(l_bars + 8u * static_cast<uint32_t>(b));
     };
-    int t = 0, k = 0;
+    // dV (warps 0-3) and dK (warps 4-7) of this warp's 32 keys for the n-th item with tiles
+    auto write_out = [&](const Item& m, int n) -> bool {
+      if (!c.wait_all(L::kAccDone, n, 47)) return false;
+      tc_fence_after();
+      const float scale = half ? args.scale : 1.f;
+      __nv_bfloat16* out = half ? (m.v[2] ? args.dkb : args.dka) : (m.v[2] ? args.dvb : args.dva);
+      out += (static_cast<int64_t>(m.row0) + row) * args.row_stride + m.head * D;
+      const bool adds = row + c.lane >= m.v[3] && row + c.lane < m.rows;
+      const __nv_bfloat16* from =
+          adds ? (half ? args.add_k : args.add_v) + (static_cast<int64_t>(m.v[4]) + row + c.lane) * args.row_stride + m.head * D : nullptr;
+      const RowsOut rows{c.base + L::kStage + 4096u * c.warp, c.lane};
+#pragma unroll
+      for (int cc = 0; cc < D / 64; ++cc) {
+        float v[64];
+        load64(c.tmem + lanes + (half ? kColK : kColV) + 64 * cc, v);
+        if (cc + 1 == D / 64) {  // all of it is read
+          tc_fence_before();
+          __syncwarp();
+          if (c.lane == 0) mbar_arrive_cluster(l_bars + 8u * L::kAccFree);
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          Vec8 x;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x.v[e] = v[8 * q + e] * scale;
+          if (adds) {
+            const Vec8 y = unpack8(*reinterpret_cast<const uint4*>(from + 64 * cc + 8 * q));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x.v[e] += y.v[e];
+          }
+          rows.put(q, pack8(x));
+        }
+        rows.flush(out + 64 * cc, args.row_stride, m.rows - row);
+      }
+      return true;
+    };
+    // The gradients of an item that no query sees: zero, or what is added to them.
+    auto write_none = [&](const Item& m) {
+      const int r = row + c.lane;
+      if (r >= m.rows) return;
+      const int64_t at = (static_cast<int64_t>(m.row0) + r) * args.row_stride + m.head * D;
+      const int64_t from = (static_cast<int64_t>(m.v[4]) + r) * args.row_stride + m.head * D;
+      __nv_bfloat16* out = (half ? (m.v[2] ? args.dkb : args.dka) : (m.v[2] ? args.dvb : args.dva)) + at;
+      const __nv_bfloat16* add = half ? args.add_k : args.add_v;
 #pragma unroll 1
-    for (int i = 0;; ++i) {
-      const int it = c.take(i, true);
-      if (it < 0) break;
-      const Item m = item_of(it);
+      for (int i = 0; i < D; i += 8)
+        *reinterpret_cast<uint4*>(out + i) = r >= m.v[3] ? *reinterpret_cast<const uint4*>(add + from + i) : make_uint4(0, 0, 0, 0);
+    };
+    const uint32_t t_s = c.tmem + lanes + kColS + 64u * half;
+    int t = 0, n = 0;  // tiles, and items with tiles, so far
+#pragma unroll 1
+    for (int k = 0;; ++k) {
+      if (!c.await(k, true)) goto scores_done;
+      const Item m = c.read(k);
+      if (m.head < 0) break;
+      if (m.nt == 0) {
+        write_none(m);
+        __syncwarp();
+        if (c.lane == 0) c.release(k);
+        continue;
+      }
 #pragma unroll 1
       for (int j = 0; j < m.nt; ++j, ++t) {
         const int s = t % kStatSlots;
         const uint32_t stat = c.base + L::kStat + 1024u * s + 256u * half;
         float p[64];
-        if (!c.wait_all(L::kStatFull + s, t / kStatSlots, 41) || !c.wait_all(L::kSDone, t, 42)) goto scores_done;
+        if (!c.wait_all(L::kStatFull + s, t / kStatSlots, 44) || !c.wait_all(L::kSDone, t, 45)) goto scores_done;
         tc_fence_after();
         load64(t_s, p);
 #pragma unroll
@@ -538,8 +634,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
           }
           tmem_st16(t_s + 16u * h, pk);
         }
-        arrive(l_used);
-        if (!c.wait_all(L::kPDone, t, 43)) goto scores_done;
+        arrive(L::kSUsed);
+        if (!c.wait_all(L::kPDone, t, 46)) goto scores_done;
         tc_fence_after();
         {
           float d[64];
@@ -561,55 +657,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
             tmem_st16(t_p + 16u * h, pk);
           }
         }
-        arrive(l_ds);
+        arrive(L::kDsFull);
         if (c.lane == 0) mbar_arrive(c.bar(L::kStatEmpty + s));
       }
-      // dV (warps 0-3) and dK (warps 4-7) of this warp's 32 keys
-      if (m.nt > 0) {
-        if (!c.wait_all(L::kAccDone, k, 44)) goto scores_done;
-        tc_fence_after();
-        ++k;
-      }
-      const int row = 128 * static_cast<int>(c.rank) + lane0;  // the warp's first row in the item
-      const float scale = half ? args.scale : 1.f;
-      __nv_bfloat16* out = half ? (m.in_b ? args.dkb : args.dka) : (m.in_b ? args.dvb : args.dva);
-      const __nv_bfloat16* add = half ? args.add_k : args.add_v;
-      const bool adds = row + c.lane >= m.add_from && row + c.lane < m.rows;
-      const __nv_bfloat16* from = adds ? add + (static_cast<int64_t>(m.add_row0) + row + c.lane) * args.row_stride + m.head * D : nullptr;
-      out += (static_cast<int64_t>(m.row0) + row) * args.row_stride + m.head * D;
-      const RowsOut rows{c.base + L::kStage + 4096u * c.warp, c.lane};
-#pragma unroll
-      for (int cc = 0; cc < D / 64; ++cc) {
-        float v[64];
-        if (m.nt > 0) {
-          load64(c.tmem + lanes + (half ? kColK : kColV) + 64 * cc, v);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 64; ++i) v[i] = 0.f;
-        }
-        if (cc + 1 == D / 64 && m.nt > 0) {  // all of it is read
-          tc_fence_before();
-          __syncwarp();
-          if (c.lane == 0) mbar_arrive_cluster(l_free);
-        }
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          Vec8 x;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x.v[e] = v[8 * q + e] * scale;
-          if (adds) {
-            const Vec8 y = unpack8(*reinterpret_cast<const uint4*>(from + 64 * cc + 8 * q));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x.v[e] += y.v[e];
-          }
-          rows.put(q, pack8(x));
-        }
-        rows.flush(out + 64 * cc, args.row_stride, m.rows - row);
-      }
+      if (!write_out(m, n)) goto scores_done;
+      ++n;
+      if (c.lane == 0) c.release(k);
     }
   scores_done:;
   }
-  leave(c, own, nn, nd);
+  leave(c, loads);
   if (args.behind_queries) grid_dependency_wait();  // the work after this kernel sees both
 }
 
@@ -625,112 +682,154 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
   if (!enter(c, smem_raw, args, maps, false)) return;
   const int cluster = static_cast<int>(blockIdx.x >> 1), n_clusters = static_cast<int>(gridDim.x >> 1);
   const int n_items = queries.n_tiles * args.num_heads;
-  struct Item {
-    int head, row0, rows, a0, a_len, b0, b_len, na, nt;
-  };
-  auto item_of = [&](int it) -> Item {
-    Item t;
-    const BwdItem i = bwd_item(queries, it, args.num_heads);
-    t.head = i.head;
-    const BwdQuerySeg& s = queries.seg[i.seg];
-    const int r0 = i.tile * kBlock;
-    t.row0 = s.q_row0 + r0;
-    t.rows = min(kBlock, s.q_rows - r0);
-    t.a0 = s.a_row0, t.a_len = s.a_len, t.b0 = s.b_row0, t.b_len = s.b_len;
-    t.na = (s.a_len + kTile - 1) / kTile;
-    t.nt = t.na + (s.b_len + kTile - 1) / kTile;
-    return t;
-  };
-  int own = 0, nn = 0, nd = 0;  // loads issued
+  Loads loads;
   if (c.warp == kProducerWarp) {
     if (c.lane == 0) {
-      Chooser choose{args.work_queries, cluster, n_clusters, n_items};
-      int it = c.leader ? choose.next() : 0;
-      if (c.leader && !c.publish(0, it)) it = -2;
+      Item t{}, next{};
+      int s = 0;
+      bool x_loaded = false, c_due = false, c_b = false;  // columns of the tile before, whose dQ comes a tile later
+      int c_x = 0, c_y = 0;
+      auto load_x = [&](const Item& m) -> bool {
+        const int b = begin_load(c, loads, 0, L::kXSlots, L::kXFull, L::kXEmpty, L::kOwn, 51);
+        if (b < 0) return false;
+        load_own<D>(c.base + L::kX + b * L::kXSlot, &maps.q, c.lbar(L::kXFull + b), m.head * D, m.row0 + 128 * static_cast<int>(c.rank));
+        return true;
+      };
+      auto load_cols = [&]() -> bool {
+        const int b = begin_load(c, loads, 4, L::kSlots, L::kCFull, L::kCEmpty, L::kCBytes, 55);
+        if (b < 0) return false;
+        tma_load_2d_pair(c.base + L::kC + b * L::kCBytes, c_b ? &maps.cols1 : &maps.cols0, c.lbar(L::kCFull + b), c_x, c_y);
+        return true;
+      };
+      auto get_next = [&](int k) -> bool {  // the item after item k
+        if (!c.await(k + 1, false)) return false;
+        next = c.read(k + 1);
+        c.release(k + 1);
+        return true;
+      };
+      bool ok = get_next(-1);
 #pragma unroll 1
-      for (int k = 0;; ++k) {
-        if (!c.leader) it = c.take(k, false);
-        if (it < 0) break;
-        int ahead = c.leader ? choose.next() : 0;  // used two tiles later
-        const Item t = item_of(it);
-        const int x = t.head * D, xc = x + D / 2 * static_cast<int>(c.rank);
-        if (own > 0 && !c.wait(L::kOwnEmpty, own - 1, 51)) break;
-        if (c.leader) mbar_arrive_expect_tx(c.bar(L::kOwnFull), 4 * L::kOwn);
-        const int y = t.row0 + 128 * static_cast<int>(c.rank);
-        load_own<D>(c.base, &maps.q, c.lbar(L::kOwnFull), x, y);
-        load_own<D>(c.base + L::kOwn, &maps.d_o, c.lbar(L::kOwnFull), x, y);
-        ++own;
-        bool ok = true;
+      for (int k = 0; ok && next.head >= 0; ++k) {
+        t = next;
+        const int x = t.head * D, xc = x + D / 2 * static_cast<int>(c.rank), r64 = 64 * static_cast<int>(c.rank);
+        if (!x_loaded && !(ok = load_x(t))) break;
+        x_loaded = false;
 #pragma unroll 1
-        for (int j = 0; j < t.nt; ++j) {
-          const bool b = j >= t.na;
-          const int y0 = b ? t.b0 + kTile * (j - t.na) : t.a0 + kTile * j;
-          const int ns = nn % L::kNStages, ds = nd % L::kDStages;
-          if (nn >= L::kNStages && !(ok = c.wait(L::kNEmpty + ns, nn / L::kNStages - 1, 52))) break;
-          if (c.leader) mbar_arrive_expect_tx(c.bar(L::kNFull + ns), 2 * L::kNBytes);
-          const uint32_t n = c.base + L::kN + ns * L::kNBytes;
-          load_half<D>(n, b ? &maps.kb : &maps.ka, c.lbar(L::kNFull + ns), x, y0 + 64 * static_cast<int>(c.rank));
-          load_half<D>(n + L::kHalf, b ? &maps.vb : &maps.va, c.lbar(L::kNFull + ns), x, y0 + 64 * static_cast<int>(c.rank));
-          ++nn;
-          if (nd >= L::kDStages && !(ok = c.wait(L::kDEmpty + ds, nd / L::kDStages - 1, 53))) break;
-          if (c.leader) mbar_arrive_expect_tx(c.bar(L::kDFull + ds), 2 * L::kDBytes);
-          tma_load_2d_pair(c.base + L::kD + ds * L::kDBytes, b ? &maps.cols1 : &maps.cols0, c.lbar(L::kDFull + ds), xc, y0);
-          ++nd;
-          if (c.leader && j == min(1, t.nt - 1) && !(ok = c.publish(k + 1, ahead))) break;
+        for (int j = 0; ok && j < t.nt; ++j) {
+          const bool b = j >= t.v[4];
+          const int y0 = b ? t.v[2] + kTile * (j - t.v[4]) : t.v[0] + kTile * j;
+          ok = false;
+          if ((s = begin_load(c, loads, 2, L::kSlots, L::kR1Full, L::kR1Empty, L::kHalf, 52)) < 0) break;
+          load_half<D>(c.base + L::kR1 + s * L::kHalf, b ? &maps.kb : &maps.ka, c.lbar(L::kR1Full + s), x, y0 + r64);
+          if (j == 0) {
+            if ((s = begin_load(c, loads, 1, L::kYSlots, L::kYFull, L::kYEmpty, L::kOwn, 53)) < 0) break;
+            load_own<D>(c.base + L::kY + s * L::kOwn, &maps.d_o, c.lbar(L::kYFull + s), x, t.row0 + 128 * static_cast<int>(c.rank));
+          }
+          if ((s = begin_load(c, loads, 3, L::kSlots, L::kR2Full, L::kR2Empty, L::kHalf, 54)) < 0) break;
+          load_half<D>(c.base + L::kR2 + s * L::kHalf, b ? &maps.vb : &maps.va, c.lbar(L::kR2Full + s), x, y0 + r64);
+          if (c_due && !load_cols()) break;
+          c_due = true, c_b = b, c_x = xc, c_y = y0;
+          if (j == max(0, t.nt - 3)) {  // the next item's X, ahead of this one's last tiles
+            if (!get_next(k)) break;
+            if (next.head >= 0) {
+              if (!load_x(next)) break;
+              x_loaded = true;
+            }
+          }
+          ok = true;
         }
-        if (!ok) break;
-        it = ahead;
+      }
+      if (ok && c_due) load_cols();
+    }
+    __syncwarp();
+  } else if (c.warp == kItemWarp) {
+    if (c.leader && c.lane == 0) {
+      // Kept apart from the producer, whose loads are few tiles ahead: choosing, decoding
+      // and passing on an item takes longer than that.  An item is chosen while the one
+      // before it runs, not earlier: a pair that holds more leaves others idle at the end.
+      auto item_of = [&](int64_t it) -> Item {
+        Item t{};
+        t.head = -1;
+        if (it >= n_items) return t;
+        const BwdItem i = bwd_item(queries, static_cast<int>(it), args.num_heads);
+        const BwdQuerySeg& s = queries.seg[i.seg];
+        const int r0 = i.tile * kBlock;
+        t.head = i.head;
+        t.row0 = s.q_row0 + r0;
+        t.rows = min(kBlock, s.q_rows - r0);
+        t.v[0] = s.a_row0, t.v[1] = s.a_len, t.v[2] = s.b_row0, t.v[3] = s.b_len;
+        t.v[4] = (s.a_len + kTile - 1) / kTile;
+        t.nt = t.v[4] + (s.b_len + kTile - 1) / kTile;
+        return t;
+      };
+      for (int k = 0; c.may_choose(k); ++k) {
+        const Item t = item_of(choose_item(args.work_queries, k, cluster, n_clusters));
+        c.publish(k, t);
+        if (t.head < 0) break;
       }
     }
     __syncwarp();
   } else if (c.warp == kMmaWarp) {
     if (c.leader) {
-      const uint64_t qd = sdesc_sw128(c.base, 16, 1024), od = sdesc_sw128(c.base + L::kOwn, 16, 1024);
-      const uint64_t nd0 = sdesc_sw128(c.base + L::kN, 16, 1024), dd0 = cols_desc<D>(c.base + L::kD);
+      const uint64_t xd = sdesc_sw128(c.base + L::kX, 16, 1024), yd = sdesc_sw128(c.base + L::kY, 16, 1024);
+      const uint64_t r1 = sdesc_sw128(c.base + L::kR1, 16, 1024), r2 = sdesc_sw128(c.base + L::kR2, 16, 1024);
+      const uint64_t cd = cols_desc<D>(c.base + L::kC);
       const uint32_t tm = c.tmem;
       bool issued = false;
-      int t = 0;
+      int nt = 0, k = -1, j = 0;  // S and dP: tile j of nt of item k
+      int pj = 0, pnt = 0, pk = 0;  // dQ, a tile behind: tile pj of pnt of item pk
+      // step t: S and dP of tile t, then dQ of tile t - 1
 #pragma unroll 1
-      for (int k = 0;; ++k) {
-        const int it = c.take(k, true);
-        if (it < 0) break;
-        const int nt = __shfl_sync(0xffffffffu, item_of(it).nt, 0);
-        if (!c.wait_all(L::kOwnFull, k, 54)) goto mma_done;
-        // step j: S and dP of tile j, then dQ of tile j - 1
-#pragma unroll 1
-        for (int j = 0; j <= nt; ++j) {
-          if (j < nt) {
-            const int i = t + j, s = i % L::kNStages;
-            if (!c.wait_all(L::kNFull + s, i / L::kNStages, 55)) goto mma_done;
-            if (i > 0 && !c.wait_all(L::kSUsed, i - 1, 56)) goto mma_done;
-            issued = true;
-            if (elect_one()) {
-              tc_fence_after();
-              const uint64_t b = nd0 + static_cast<uint64_t>(s) * (L::kNBytes >> 4);
-              mma_rows<D>(tm + kColS, qd, b);
-              tc2_commit_mc(c.bar(L::kSDone), 3);
-              mma_rows<D>(tm + kColP + 128u * (i & 1), od, b + (L::kHalf >> 4));
-              tc2_commit_mc(c.bar(L::kPDone + (i & 1)), 3);
-              tc2_commit_mc(c.bar(L::kNEmpty + s), 3);
-              if (j + 1 == nt) tc2_commit_mc(c.bar(L::kOwnEmpty), 3);
-            }
-            __syncwarp();
-          }
-          if (j > 0) {
-            const int i = t + j - 1, s = i % L::kDStages;
-            if (!c.wait_all(L::kDFull + s, i / L::kDStages, 57)) goto mma_done;
-            if (j == 1 && k > 0 && !c.wait_all(L::kAccFree, k - 1, 58)) goto mma_done;
-            if (!c.wait_all(L::kDsFull + (i & 1), i >> 1, 59)) goto mma_done;
-            if (elect_one()) {
-              tc_fence_after();
-              mma_cols<D>(tm + kColQ, tm + kColP + 128u * (i & 1), dd0 + static_cast<uint64_t>(s) * (L::kDBytes >> 4), j > 1 ? 1u : 0u);
-              tc2_commit_mc(c.bar(L::kDEmpty + s), 3);
-              if (j == nt) tc2_commit_mc(c.bar(L::kAccDone), 3);
-            }
-            __syncwarp();
-          }
+      for (int t = 0;; ++t) {
+        if (j == nt) {
+          ++k;
+          if (!c.await(k, true)) goto mma_done;
+          nt = __shfl_sync(0xffffffffu, c.read(k).nt, 0);  // (0 where none is left)
+          __syncwarp();
+          if (c.lane == 0) c.release(k);
+          j = 0;
         }
-        t += nt;
+        if (nt > 0) {
+          const int u = t & 1, r = t % L::kSlots, h = t / L::kSlots;
+          const uint64_t kb = static_cast<uint64_t>(k & 1);
+          if (j == 0 && !c.wait_all(L::kXFull + (k & 1), k >> 1, 56)) goto mma_done;
+          if (!c.wait_all(L::kR1Full + r, h, 57)) goto mma_done;
+          if (t > 0 && !c.wait_all(L::kSUsed, t - 1, 58)) goto mma_done;
+          issued = true;
+          if (elect_one()) {
+            tc_fence_after();
+            mma_rows<D>(tm + kColS, xd + kb * (L::kXSlot >> 4), r1 + static_cast<uint64_t>(r) * (L::kHalf >> 4));
+            tc2_commit_mc(c.bar(L::kSDone), 3);
+            tc2_commit_mc(c.bar(L::kR1Empty + r), 3);
+          }
+          __syncwarp();
+          if (j == 0 && !c.wait_all(L::kYFull + (k & 1), k >> 1, 59)) goto mma_done;
+          if (!c.wait_all(L::kR2Full + r, h, 60)) goto mma_done;
+          if (elect_one()) {
+            tc_fence_after();
+            mma_rows<D>(tm + kColP + 128u * u, yd + kb * (L::kOwn >> 4), r2 + static_cast<uint64_t>(r) * (L::kHalf >> 4));
+            tc2_commit_mc(c.bar(L::kPDone + u), 3);
+            tc2_commit_mc(c.bar(L::kR2Empty + r), 3);
+            if (j + 1 == nt) tc2_commit_mc(c.bar(L::kYEmpty + (k & 1)), 3);
+          }
+          __syncwarp();
+        }
+        if (t > 0) {
+          const int i = t - 1, u = i & 1, r = i % L::kSlots;
+          if (!c.wait_all(L::kCFull + r, i / L::kSlots, 61)) goto mma_done;
+          if (pj == 0 && pk > 0 && !c.wait_all(L::kAccFree, pk - 1, 62)) goto mma_done;
+          if (!c.wait_all(L::kDsFull + u, i >> 1, 63)) goto mma_done;
+          if (elect_one()) {
+            tc_fence_after();
+            mma_cols<D>(tm + kColQ, tm + kColP + 128u * u, cd + static_cast<uint64_t>(r) * (L::kCBytes >> 4), pj > 0 ? 1u : 0u);
+            tc2_commit_mc(c.bar(L::kCEmpty + r), 3);
+            if (pj + 1 == pnt) tc2_commit_mc(c.bar(L::kAccDone), 3);
+          }
+          __syncwarp();
+        }
+        if (nt == 0) break;
+        pj = j, pnt = nt, pk = k;
+        ++j;
       }
     mma_done:
       __syncwarp();
@@ -746,21 +845,75 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
     const uint32_t t_s = c.tmem + lanes + kColS + 64 * half, t_p = c.tmem + lanes + kColP + 64 * half;
     const f32x2 sl2 = make_f32x2(args.scale_log2, args.scale_log2);
     const uint32_t l_used = c.lbar(L::kSUsed), l_ds = c.lbar(L::kDsFull), l_free = c.lbar(L::kAccFree);
-    int t = 0;
+    const int row = 128 * static_cast<int>(c.rank) + lane0;  // the warp's first row in an item
+    // dQ of item k: columns [D / 2 half, D / 2 (half + 1)) of this warp's 32 rows
+    auto write_out = [&](int k) -> bool {
+      const Item m = c.read(k);
+      if (!c.wait_all(L::kAccDone, k, 67)) return false;
+      tc_fence_after();
+      uint32_t v[D / 2];
+      if constexpr (D == 128) {
+        uint32_t(&v0)[32] = reinterpret_cast<uint32_t(&)[32]>(v);
+        uint32_t(&v1)[32] = reinterpret_cast<uint32_t(&)[32]>(v[32]);
+        tmem_ld32(c.tmem + lanes + kColQ + 64u * half, v0);
+        tmem_ld32(c.tmem + lanes + kColQ + 64u * half + 32u, v1);
+        tmem_wait_ld(v0);
+        tmem_wait_ld(v1);
+      } else {
+        tmem_ld32(c.tmem + lanes + kColQ + 32u * half, v);
+        tmem_wait_ld(v);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (c.lane == 0) mbar_arrive_cluster(l_free);
+      // staged in the item's Q, which its last S has read: chunks of 16 bytes, eight a row, or four at D = 64
+      const RowsOut rows{c.base + L::kX + L::kXSlot * static_cast<uint32_t>(k & 1) + 4096u * c.warp, c.lane};
+#pragma unroll
+      for (int q = 0; q < D / 16; ++q) {
+        Vec8 x;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x.v[e] = __uint_as_float(v[8 * q + e]) * args.scale;
+        rows.put(q, pack8(x));
+      }
+      __nv_bfloat16* out = args.dq + (static_cast<int64_t>(m.row0) + row) * args.row_stride + m.head * D + D / 2 * half;
+      if constexpr (D == 128) {
+        rows.flush(out, args.row_stride, m.rows - row);
+      } else {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = 8 * i + (c.lane >> 2), ch = c.lane & 3;
+          const uint4 x = ld_shared_v4(rows.stage + 128u * r + (static_cast<uint32_t>(ch ^ (r & 7)) << 4));
+          if (r < m.rows - row) *reinterpret_cast<uint4*>(out + r * args.row_stride + 8 * ch) = x;
+        }
+        __syncwarp();
+      }
+      fence_proxy_async_smem();  // the buffer is free for the loads of the item after the next
+      __syncwarp();
+      if (c.lane == 0) {
+        mbar_arrive(c.bar(L::kXEmpty + (k & 1)));
+        c.release(k);
+      }
+      return true;
+    };
+    int t = 0, k = 0;
 #pragma unroll 1
-    for (int k = 0;; ++k) {
-      const int it = c.take(k, true);
-      if (it < 0) break;
-      const Item m = item_of(it);
-      const int row = 128 * static_cast<int>(c.rank) + lane0;  // the warp's first row in the item
+    for (;; ++k) {  // item k; the dQ of item k - 1 is written behind its first P
+      if (!c.await(k, true)) goto scores_done;
+      const Item m = c.read(k);
+      if (m.head < 0) {
+        __syncwarp();
+        if (c.lane == 0) c.release(k);
+        break;
+      }
       const float2 st = row + c.lane < m.rows ? args.stats[m.head * args.rows + m.row0 + row + c.lane] : make_float2(INFINITY, 0.f);
       const f32x2 nl = make_f32x2(-st.x, -st.x), ndl = make_f32x2(-st.y, -st.y);
 #pragma unroll 1
       for (int j = 0; j < m.nt; ++j, ++t) {
         float p[64];
-        if (!c.wait_all(L::kSDone, t, 61)) goto scores_done;
+        if (!c.wait_all(L::kSDone, t, 65)) goto scores_done;
         tc_fence_after();
-        const int valid = (j < m.na ? m.a_len - kTile * j : m.b_len - kTile * (j - m.na)) - 64 * half;  // of this warp's 64 keys
+        const int valid = (j < m.v[4] ? m.v[1] - kTile * j : m.v[3] - kTile * (j - m.v[4])) - 64 * half;  // of this warp's 64 keys
         if (valid < 64) {  // keys past the end: scores of -inf
 #pragma unroll 1
           for (int i = max(valid, 0); i < 64; ++i) tmem_st1(t_s + static_cast<uint32_t>(i), 0xFF800000u);
@@ -776,8 +929,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
           split_f32x2(fma_f32x2(make_f32x2(p[i], p[i + 1]), sl2, nl), e0, e1);
           p[i] = ex2_approx(e0), p[i + 1] = ex2_approx(e1);
         }
+        if (j == 0 && k > 0 && !write_out(k - 1)) goto scores_done;
         const int b = t & 1;
-        if (!c.wait_all(L::kPDone + b, t >> 1, 62)) goto scores_done;
+        if (!c.wait_all(L::kPDone + b, t >> 1, 66)) goto scores_done;
         tc_fence_after();
         {
           float d[64];
@@ -800,52 +954,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
         __syncwarp();
         if (c.lane == 0) mbar_arrive_cluster(l_ds + 8u * b);
       }
-      // dQ: columns [D / 2 half, D / 2 (half + 1)) of this warp's 32 rows
-      if (!c.wait_all(L::kAccDone, k, 63)) goto scores_done;
-      tc_fence_after();
-      {
-        uint32_t v[D / 2];
-        if constexpr (D == 128) {
-          uint32_t(&v0)[32] = reinterpret_cast<uint32_t(&)[32]>(v);
-          uint32_t(&v1)[32] = reinterpret_cast<uint32_t(&)[32]>(v[32]);
-          tmem_ld32(c.tmem + lanes + kColQ + 64u * half, v0);
-          tmem_ld32(c.tmem + lanes + kColQ + 64u * half + 32u, v1);
-          tmem_wait_ld(v0);
-          tmem_wait_ld(v1);
-        } else {
-          tmem_ld32(c.tmem + lanes + kColQ + 32u * half, v);
-          tmem_wait_ld(v);
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (c.lane == 0) mbar_arrive_cluster(l_free);
-        // staged as chunks of 16 bytes: 8 a row, or 4 of each of the two warps at D = 64
-        const RowsOut rows{c.base + L::kStage + 4096u * c.warp, c.lane};
-#pragma unroll
-        for (int q = 0; q < D / 16; ++q) {
-          Vec8 x;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x.v[e] = __uint_as_float(v[8 * q + e]) * args.scale;
-          rows.put(q, pack8(x));
-        }
-        __nv_bfloat16* out = args.dq + (static_cast<int64_t>(m.row0) + row) * args.row_stride + m.head * D + D / 2 * half;
-        if constexpr (D == 128) {
-          rows.flush(out, args.row_stride, m.rows - row);
-        } else {
-          __syncwarp();
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = 8 * i + (c.lane >> 2), ch = c.lane & 3;
-            const uint4 x = ld_shared_v4(rows.stage + 128u * r + (static_cast<uint32_t>(ch ^ (r & 7)) << 4));
-            if (r < m.rows - row) *reinterpret_cast<uint4*>(out + r * args.row_stride + 8 * ch) = x;
-          }
-          __syncwarp();
-        }
-      }
     }
+    if (k > 0) write_out(k - 1);
   scores_done:;
   }
-  leave(c, own, nn, nd);
+  leave(c, loads);
 }
 
 }  // namespace rc
