@@ -67,7 +67,9 @@ constexpr int kItemSlots = 2;
 //   queries kernel  X and Y twice, so that an item's first S and dP are issued inside
 //                   the item before it, whose X then takes its dQ on its way out
 // At head dim 64 a tile is half as many bytes and takes less time, so its rings are
-// deeper (a load takes about as long as a tile).
+// deeper (a load takes about as long as a tile).  At 128 the queries kernel's R are loads
+// of their own, so that each has all the time between its uses; at 64 they are one, for
+// the MMA warp, whose waits and commits take the longer the shorter a tile is.
 template <int D, bool kKeys>
 struct Smem {
   static constexpr uint32_t kOwn = 128 * D * 2;  // this CTA's 128 rows of one operand
@@ -76,10 +78,11 @@ struct Smem {
   static constexpr uint32_t kXSlot = kKeys ? kOwn : 32768;  // (32 rows x 64 columns a warp are staged in it)
   static constexpr uint32_t kXBytes = kKeys ? 2 * kOwn : kOwn;  // one CTA's bytes of a load: with Y in the keys kernel
   static constexpr int kSlots = D == 64 ? 4 : 2;                // of each ring of a tile
-  static constexpr uint32_t kR1Bytes = kKeys ? 2 * kHalf : kHalf;  // R of dP with R of S, or of S
+  static constexpr bool kRApart = !kKeys && D == 128;           // R of S and of dP are loads of their own
+  static constexpr uint32_t kR1Bytes = kRApart ? kHalf : 2 * kHalf;
   static constexpr uint32_t kCBytes = (kKeys ? 2 : 1) * kHalf;
   static constexpr uint32_t kX = 0, kY = kX + kXSlots * kXSlot, kR1 = kY + kYSlots * kOwn, kR2 = kR1 + kSlots * kR1Bytes,
-                            kC = kR2 + (kKeys ? 0 : kSlots * kHalf), kStage = kC + kSlots * kCBytes,
+                            kC = kR2 + (kRApart ? kSlots * kHalf : 0), kStage = kC + kSlots * kCBytes,
                             kStat = kStage + (kKeys ? kScoreWarps * 4096 : 0);
   static constexpr uint32_t kBars = kStat + (kKeys ? kStatSlots * 1024 : 0);
   // barriers; those of loads first: X, Y, rows of S, rows of dP, columns
@@ -719,14 +722,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
           const bool b = j >= t.v[4];
           const int y0 = b ? t.v[2] + kTile * (j - t.v[4]) : t.v[0] + kTile * j;
           ok = false;
-          if ((s = begin_load(c, loads, 2, L::kSlots, L::kR1Full, L::kR1Empty, L::kHalf, 52)) < 0) break;
-          load_half<D>(c.base + L::kR1 + s * L::kHalf, b ? &maps.kb : &maps.ka, c.lbar(L::kR1Full + s), x, y0 + r64);
+          if ((s = begin_load(c, loads, 2, L::kSlots, L::kR1Full, L::kR1Empty, L::kR1Bytes, 52)) < 0) break;
+          load_half<D>(c.base + L::kR1 + s * L::kR1Bytes, b ? &maps.kb : &maps.ka, c.lbar(L::kR1Full + s), x, y0 + r64);
+          if (!L::kRApart) load_half<D>(c.base + L::kR1 + s * L::kR1Bytes + L::kHalf, b ? &maps.vb : &maps.va, c.lbar(L::kR1Full + s), x, y0 + r64);
           if (j == 0) {
             if ((s = begin_load(c, loads, 1, L::kYSlots, L::kYFull, L::kYEmpty, L::kOwn, 53)) < 0) break;
             load_own<D>(c.base + L::kY + s * L::kOwn, &maps.d_o, c.lbar(L::kYFull + s), x, t.row0 + 128 * static_cast<int>(c.rank));
           }
-          if ((s = begin_load(c, loads, 3, L::kSlots, L::kR2Full, L::kR2Empty, L::kHalf, 54)) < 0) break;
-          load_half<D>(c.base + L::kR2 + s * L::kHalf, b ? &maps.vb : &maps.va, c.lbar(L::kR2Full + s), x, y0 + r64);
+          if (L::kRApart) {
+            if ((s = begin_load(c, loads, 3, L::kSlots, L::kR2Full, L::kR2Empty, L::kHalf, 54)) < 0) break;
+            load_half<D>(c.base + L::kR2 + s * L::kHalf, b ? &maps.vb : &maps.va, c.lbar(L::kR2Full + s), x, y0 + r64);
+          }
           if (c_due && !load_cols()) break;
           c_due = true, c_b = b, c_x = xc, c_y = y0;
           if (j == max(0, t.nt - 3)) {  // the next item's X, ahead of this one's last tiles
@@ -795,24 +801,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
           if (j == 0 && !c.wait_all(L::kXFull + (k & 1), k >> 1, 56)) goto mma_done;
           if (!c.wait_all(L::kR1Full + r, h, 57)) goto mma_done;
           if (t > 0 && !c.wait_all(L::kSUsed, t - 1, 58)) goto mma_done;
+          if (!L::kRApart && j == 0 && !c.wait_all(L::kYFull + (k & 1), k >> 1, 59)) goto mma_done;
           issued = true;
           if (elect_one()) {
             tc_fence_after();
-            mma_rows<D>(tm + kColS, xd + kb * (L::kXSlot >> 4), r1 + static_cast<uint64_t>(r) * (L::kHalf >> 4));
+            mma_rows<D>(tm + kColS, xd + kb * (L::kXSlot >> 4), r1 + static_cast<uint64_t>(r) * (L::kR1Bytes >> 4));
             tc2_commit_mc(c.bar(L::kSDone), 3);
-            tc2_commit_mc(c.bar(L::kR1Empty + r), 3);
+            if (L::kRApart) tc2_commit_mc(c.bar(L::kR1Empty + r), 3);
+            else {
+              mma_rows<D>(tm + kColP + 128u * u, yd + kb * (L::kOwn >> 4), r1 + static_cast<uint64_t>(r) * (L::kR1Bytes >> 4) + (L::kHalf >> 4));
+              tc2_commit_mc(c.bar(L::kPDone + u), 3);
+              tc2_commit_mc(c.bar(L::kR1Empty + r), 3);
+              if (j + 1 == nt) tc2_commit_mc(c.bar(L::kYEmpty + (k & 1)), 3);
+            }
           }
           __syncwarp();
-          if (j == 0 && !c.wait_all(L::kYFull + (k & 1), k >> 1, 59)) goto mma_done;
-          if (!c.wait_all(L::kR2Full + r, h, 60)) goto mma_done;
-          if (elect_one()) {
-            tc_fence_after();
-            mma_rows<D>(tm + kColP + 128u * u, yd + kb * (L::kOwn >> 4), r2 + static_cast<uint64_t>(r) * (L::kHalf >> 4));
-            tc2_commit_mc(c.bar(L::kPDone + u), 3);
-            tc2_commit_mc(c.bar(L::kR2Empty + r), 3);
-            if (j + 1 == nt) tc2_commit_mc(c.bar(L::kYEmpty + (k & 1)), 3);
+          if (L::kRApart) {
+            if (j == 0 && !c.wait_all(L::kYFull + (k & 1), k >> 1, 59)) goto mma_done;
+            if (!c.wait_all(L::kR2Full + r, h, 60)) goto mma_done;
+            if (elect_one()) {
+              tc_fence_after();
+              mma_rows<D>(tm + kColP + 128u * u, yd + kb * (L::kOwn >> 4), r2 + static_cast<uint64_t>(r) * (L::kHalf >> 4));
+              tc2_commit_mc(c.bar(L::kPDone + u), 3);
+              tc2_commit_mc(c.bar(L::kR2Empty + r), 3);
+              if (j + 1 == nt) tc2_commit_mc(c.bar(L::kYEmpty + (k & 1)), 3);
+            }
+            __syncwarp();
           }
-          __syncwarp();
         }
         if (t > 0) {
           const int i = t - 1, u = i & 1, r = i % L::kSlots;
