@@ -24,7 +24,7 @@ namespace {
 
 constexpr int64_t kMaxRows = (1ll << 31) - 1 - 512;
 constexpr int kRopeMaxParts = 1024;   // blocks of the rotary gradient's launch
-constexpr int kNormMaxBlocks = 512;   // blocks of a gated norm's gradient launch
+constexpr int kNormMaxBlocks = 1280;  // blocks of a gated norm's gradient launch
 constexpr int kClipMaxBlocks = 1024;  // blocks of a clipping launch
 
 int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
@@ -155,7 +155,32 @@ rc::NormArgs norm_args(const refcache_gated_norm_t* p, int b, int rows) {
   return a;
 }
 
-int norm_blocks(int rows, int sms) { return std::min({rows, 2 * sms, kNormMaxBlocks}); }
+// A block's threads for a row of `width`, its vectors per thread and its shared memory.
+struct NormShape {
+  int nv, threads, smem;
+};
+NormShape norm_shape(int width, bool backward) {
+  const int nvec = width / 8;
+  NormShape n{};
+  n.nv = nvec <= 256 ? 1 : 2;
+  n.threads = 32 * ceil_div(nvec, 32 * n.nv);
+  n.smem = n.nv * n.threads * 16 * (backward ? rc::norm_bwd_slots(n.threads) * 4 + 4 : rc::kNormFwdSlots * 2);
+  return n;
+}
+// Blocks: as many as an SM holds (of 65536 registers, 128 a thread, and 227 KB), and at
+// most a row each.
+int norm_blocks(int rows, int sms, const NormShape& n) {
+  const int per_sm = std::max(1, std::min({512 / n.threads, (227 << 10) / (n.smem + 2048), 16}));
+  return std::min(rows, per_sm * sms);
+}
+template <typename Kernel>
+cudaError_t launch_norm(Kernel kernel, const NormShape& n, int blocks, cudaStream_t s, const rc::NormSegs& segs, const rc::NormArgs& a) {
+  if (n.smem > 40 << 10) {  // (with the static part, above what a launch may have by default)
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, n.smem);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_dependent(kernel, dim3(static_cast<unsigned>(blocks)), dim3(static_cast<unsigned>(n.threads)), n.smem, s, segs, a);
+}
 
 }  // namespace
 
@@ -272,8 +297,8 @@ int refcache_qkv_rope_backward(const refcache_rope_t* r, const refcache_rope_row
   cudaError_t e = cudaSuccess;
   int parts = 0;
   if (w->rows > 0 && (dq_out || dk_out || dv_out)) {
-    const int slices = rope_slices(r, w, sms, 2, &a.head_step);
-    const int blocks = std::max(1, std::min({ceil_div(w->rows, rc::kRopeTokens), 3 * sms, kRopeMaxParts / slices}));
+    const int slices = rope_slices(r, w, sms, 4, &a.head_step);
+    const int blocks = std::max(1, std::min({ceil_div(w->rows, rc::kRopeTokens), 2 * sms, kRopeMaxParts / slices}));
     parts = blocks * slices;
     const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(slices), 1);
     auto go = [&](auto kernel) { return launch_dependent(kernel, grid, dim3(rc::kRopeThreads), 0, s, t, a); };
@@ -301,11 +326,7 @@ int refcache_gated_norm(const refcache_gated_norm_t* p, const void* x, const voi
   int sms = 0;
   if ((rc = device_sms(&sms)) != 0) return rc;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  // a lane holds up to four vectors of a row
-  const int nvec = p->width / 8, nv = nvec <= 32 ? 1 : nvec <= 64 ? 2 : 4;
-  int warps = 1;
-  while (warps * 32 * nv < nvec) warps *= 2;
-  const int per_block = std::max(1, 4 / warps);
+  const NormShape shape = norm_shape(p->width, false);
   for (int b = 0; b < p->batch; b += rc::kNormMaxSegs) {
     const int n = std::min(rc::kNormMaxSegs, p->batch - b);
     const rc::NormSegs segs = norm_segs(p, b, n);
@@ -316,12 +337,11 @@ int refcache_gated_norm(const refcache_gated_norm_t* p, const void* x, const voi
     a.branch = branch ? static_cast<const uint16_t*>(branch) + off : nullptr;
     a.x_out = x_out ? static_cast<uint16_t*>(x_out) + off : nullptr;
     a.y = y ? static_cast<uint16_t*>(y) + off : nullptr;
-    a.warps_per_row = warps;
-    a.rows_per_block = per_block;
-    const dim3 grid(static_cast<unsigned>(ceil_div(a.rows, per_block))), block(static_cast<unsigned>(32 * warps * per_block));
-    const cudaError_t e = nv == 1   ? launch_dependent(rc::gated_norm_kernel<1>, grid, block, 0, s, segs, a)
-                          : nv == 2 ? launch_dependent(rc::gated_norm_kernel<2>, grid, block, 0, s, segs, a)
-                                    : launch_dependent(rc::gated_norm_kernel<4>, grid, block, 0, s, segs, a);
+    a.rows_per_block = ceil_div(a.rows, norm_blocks(a.rows, sms, shape));
+    const int blocks = ceil_div(a.rows, a.rows_per_block);
+    const cudaError_t e = shape.nv == 1          ? launch_norm(rc::gated_norm_kernel<1, 256>, shape, blocks, s, segs, a)
+                          : shape.threads <= 256 ? launch_norm(rc::gated_norm_kernel<2, 256>, shape, blocks, s, segs, a)
+                                                 : launch_norm(rc::gated_norm_kernel<2, 512>, shape, blocks, s, segs, a);
     if (e != cudaSuccess) return cuda_fail(e, "gated_norm_kernel launch");
   }
   return REFCACHE_OK;
@@ -352,8 +372,7 @@ int refcache_gated_norm_backward(const refcache_gated_norm_t* p, const void* x_o
   int sms = 0;
   if ((rc = device_sms(&sms)) != 0) return rc;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const int nvec = p->width / 8, nv = nvec <= 256 ? 1 : 2;
-  const int warps = ceil_div(nvec, 32 * nv);
+  const NormShape shape = norm_shape(p->width, true);
   for (int b = 0; b < p->batch; b += rc::kNormMaxSegs) {
     const int n = std::min(rc::kNormMaxSegs, p->batch - b);
     const rc::NormSegs segs = norm_segs(p, b, n);
@@ -371,11 +390,11 @@ int refcache_gated_norm_backward(const refcache_gated_norm_t* p, const void* x_o
     a.rows_per_block = 1;
     cudaError_t e = cudaSuccess;
     if (a.rows > 0) {
-      a.rows_per_block = ceil_div(a.rows, norm_blocks(a.rows, sms));
-      const dim3 grid(static_cast<unsigned>(ceil_div(a.rows, a.rows_per_block))), block(static_cast<unsigned>(32 * warps));
-      e = nv == 1      ? launch_dependent(rc::gated_norm_backward_kernel<1, 256>, grid, block, 0, s, segs, a)
-          : warps <= 8 ? launch_dependent(rc::gated_norm_backward_kernel<2, 256>, grid, block, 0, s, segs, a)
-                       : launch_dependent(rc::gated_norm_backward_kernel<2, 512>, grid, block, 0, s, segs, a);
+      a.rows_per_block = ceil_div(a.rows, std::min(kNormMaxBlocks, norm_blocks(a.rows, sms, shape)));
+      const int blocks = ceil_div(a.rows, a.rows_per_block);
+      e = shape.nv == 1          ? launch_norm(rc::gated_norm_backward_kernel<1, 256>, shape, blocks, s, segs, a)
+          : shape.threads <= 256 ? launch_norm(rc::gated_norm_backward_kernel<2, 256>, shape, blocks, s, segs, a)
+                                 : launch_norm(rc::gated_norm_backward_kernel<2, 512>, shape, blocks, s, segs, a);
       if (e != cudaSuccess) return cuda_fail(e, "gated_norm_backward_kernel launch");
     }
     if (!d_gate && !d_scale && !d_shift && !d_weight && !d_post_weight) continue;

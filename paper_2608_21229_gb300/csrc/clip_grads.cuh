@@ -138,30 +138,43 @@ __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const __grid_c
       else
         reinterpret_cast<__nv_bfloat16*>(to)[i] = __float2bfloat16_rn(x);
     };
-#pragma unroll 4
-    for (int i = threadIdx.x; i < nv; i += kClipThreads) {
-      const uint4 r = __ldcs(v + i);
-      if (p.src32) {
-        const float x[4] = {__uint_as_float(r.x) * coef, __uint_as_float(r.y) * coef, __uint_as_float(r.z) * coef,
-                            __uint_as_float(r.w) * coef};
-        if (p.dst32 && aligned) {
-          reinterpret_cast<float4*>(dst)[i] = make_float4(x[0], x[1], x[2], x[3]);
+    // eight loads ahead of their stores (which the compiler may not move them over)
+    constexpr int kDepth = 8;
+#pragma unroll 1
+    for (int i0 = threadIdx.x; i0 < nv; i0 += kDepth * kClipThreads) {
+      uint4 raw[kDepth];
+#pragma unroll
+      for (int u = 0; u < kDepth; ++u) {
+        const int i = i0 + u * kClipThreads;
+        raw[u] = i < nv ? __ldcs(v + i) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int u = 0; u < kDepth; ++u) {
+        const int i = i0 + u * kClipThreads;
+        if (i >= nv) break;
+        const uint4 r = raw[u];
+        if (p.src32) {
+          const float x[4] = {__uint_as_float(r.x) * coef, __uint_as_float(r.y) * coef, __uint_as_float(r.z) * coef,
+                              __uint_as_float(r.w) * coef};
+          if (p.dst32 && aligned) {
+            __stcs(reinterpret_cast<float4*>(dst) + i, make_float4(x[0], x[1], x[2], x[3]));
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) put(dst, 4 * i + e, x[e]);
+          }
         } else {
+          Vec8 x = unpack8(r);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) put(dst, 4 * i + e, x[e]);
-        }
-      } else {
-        Vec8 x = unpack8(r);
+          for (int e = 0; e < 8; ++e) x.v[e] *= coef;
+          if (!aligned) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x.v[e] *= coef;
-        if (!aligned) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) put(dst, 8 * i + e, x.v[e]);
-        } else if (p.dst32) {
-          reinterpret_cast<float4*>(dst)[2 * i] = make_float4(x.v[0], x.v[1], x.v[2], x.v[3]);
-          reinterpret_cast<float4*>(dst)[2 * i + 1] = make_float4(x.v[4], x.v[5], x.v[6], x.v[7]);
-        } else {
-          reinterpret_cast<uint4*>(dst)[i] = pack8(x);
+            for (int e = 0; e < 8; ++e) put(dst, 8 * i + e, x.v[e]);
+          } else if (p.dst32) {
+            __stcs(reinterpret_cast<float4*>(dst) + 2 * i, make_float4(x.v[0], x.v[1], x.v[2], x.v[3]));
+            __stcs(reinterpret_cast<float4*>(dst) + 2 * i + 1, make_float4(x.v[4], x.v[5], x.v[6], x.v[7]));
+          } else {
+            __stcs(reinterpret_cast<uint4*>(dst) + i, pack8(x));
+          }
         }
       }
     }

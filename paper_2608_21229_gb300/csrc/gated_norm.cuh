@@ -9,12 +9,18 @@
 //
 // Bound by memory: forward reads x and the branch and writes x_out and y,
 // backward reads x_out, the branch and two gradients and writes two, each once.
-// A row is spread over W warps of its block with at most kNV eight-column
-// vectors per lane, so that it stays in registers between its statistics and its
-// use.  The variance is merged from the threads' own means and sums of squared
-// deviations (Chan, Golub and LeVeque's pairwise formula): one exchange instead
-// of one for the mean and one for the deviations, and no cancellation where the
-// mean is large.
+//
+// A block walks over a run of consecutive rows, a row spread over all its threads, at
+// most kNV eight-column vectors each, which stay in registers between the row's
+// statistics and their use.  What the rows of a request share (gate, scale, shift,
+// weights) is made into two or three vectors at the request's first row.  The rows
+// ahead are on their way into shared memory meanwhile (cp.async; every thread copies
+// and reads its own columns, so that no barrier is needed for them): loaded a row at a
+// time into registers, a row of 4096 columns took 5 us from its loads to its last
+// store, five times its share of the memory's bandwidth.
+//
+// The mean is found before the squares, from values in registers: two exchanges of the
+// block's warps for a layer norm, and no cancellation where the mean is large.
 #pragma once
 #include "vec8.cuh"
 
@@ -38,7 +44,7 @@ struct NormArgs {
   int64_t ld_gate, ld_scale, ld_shift;  // elements between requests' rows
   float* part;                          // backward: [slot][3][width]
   int32_t rows, width, norm, post_norm, mod_f32;
-  int32_t warps_per_row, rows_per_block;
+  int32_t rows_per_block;
   float eps;
 };
 
@@ -54,152 +60,181 @@ __device__ __forceinline__ int segment_of(const NormSegs& s, int row) {
   return lo;
 }
 
-// n values with their mean and the sum of their squared deviations.
-struct Moments {
-  float n, mean, m2;
-  __device__ __forceinline__ void merge(float n2, float mean2, float m22) {
-    const float total = n + n2;
-    const float f = total > 0.f ? __fdividef(n2, total) : 0.f;
-    const float d = mean2 - mean;
-    mean = fmaf(d, f, mean);
-    m2 += m22 + d * d * (n * f);
-    n = total;
+// Sums of up to four values over the block's threads; every thread gets them.  Slots
+// alternate: two exchanges apart they are free again.
+struct BlockSum {
+  float4* slots;  // [2][warps]
+  int warps, turn = 0;
+  template <int N>
+  __device__ __forceinline__ void operator()(float (&v)[N]) {
+    static_assert(N <= 4, "one float4 per warp");
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    if (warps == 1) return;
+    float4* s = slots + turn * warps;
+    turn ^= 1;
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = make_float4(v[0], N > 1 ? v[N > 1 ? 1 : 0] : 0.f, N > 2 ? v[N > 2 ? 2 : 0] : 0.f, N > 3 ? v[N > 3 ? 3 : 0] : 0.f);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = 0.f;
+    for (int w = 0; w < warps; ++w) {
+      const float4 g = s[w];
+      v[0] += g.x;
+      if (N > 1) v[N > 1 ? 1 : 0] += g.y;
+      if (N > 2) v[N > 2 ? 2 : 0] += g.z;
+      if (N > 3) v[N > 3 ? 3 : 0] += g.w;
+    }
   }
 };
 
-// Statistics of one row (mean, 1 / deviation) over the row's warps.  `slot`: the
-// block's shared memory of this exchange, one entry per warp.
-template <int kNV>
-__device__ __forceinline__ float2 row_stats(const Vec8 (&t)[kNV], int have, int kind, float eps, int width, float4* slot,
-                                            int warps, int first_warp) {
-  Moments m{8.f * have, 0.f, 0.f};
-  float sum = 0.f;
-  if (kind == kNormLayer) {
-#pragma unroll
-    for (int i = 0; i < kNV; ++i)
-      if (i < have) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum += t[i].v[e];
-      }
-    m.mean = have ? sum / m.n : 0.f;
+// The rows ahead of the one that is worked on, kTensors of each, in shared memory:
+// [slot][tensor][vector][thread], 16 bytes each.
+template <int kNV, int kTensors, int kSlots>
+struct RowsAhead {
+  uint8_t* smem;
+  const uint16_t* src[kTensors];  // null: zeros
+  int64_t width;
+  int have, issued = 0;
+  __device__ __forceinline__ uint8_t* at(int slot, int tensor, int i) const {
+    return smem + ((static_cast<int64_t>(slot * kTensors + tensor) * kNV + i) * blockDim.x + threadIdx.x) * 16;
   }
+  __device__ __forceinline__ void load(int row, bool on) {
+    const int slot = issued % kSlots;
+    if (on) {
+#pragma unroll
+      for (int t = 0; t < kTensors; ++t)
+        if (src[t]) {
+#pragma unroll
+          for (int i = 0; i < kNV; ++i)
+            if (i < have)
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(at(slot, t, i))),
+                           "l"(src[t] + row * width + 8 * static_cast<int64_t>(threadIdx.x + i * blockDim.x))
+                           : "memory");
+        }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    ++issued;
+  }
+  // the oldest row that is not read yet: `row`-th of the block
+  __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 2) : "memory"); }
+  __device__ __forceinline__ Vec8 get(int n, int tensor, int i) const {
+    if (i >= have || !src[tensor]) return fill8(0.f);
+    return unpack8(*reinterpret_cast<const uint4*>(at(n % kSlots, tensor, i)));
+  }
+};
+
+// (mean, 1 / deviation) of a layer norm, (0, 1 / rms) of an RMS norm.
+template <int kNV>
+__device__ __forceinline__ float centered_squares(const Vec8 (&t)[kNV], int have, float mean) {
+  float s = 0.f;
 #pragma unroll
   for (int i = 0; i < kNV; ++i)
     if (i < have) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float d = t[i].v[e] - m.mean;
-        m.m2 = fmaf(d, d, m.m2);
+        const float d = t[i].v[e] - mean;
+        s = fmaf(d, d, s);
       }
     }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float n2 = __shfl_xor_sync(0xffffffffu, m.n, o), mean2 = __shfl_xor_sync(0xffffffffu, m.mean, o),
-                m22 = __shfl_xor_sync(0xffffffffu, m.m2, o);
-    // both lanes of a pair merge the lower one's values first, so that they get the same bits
-    const bool upper = (threadIdx.x & o) != 0;
-    Moments lo{upper ? n2 : m.n, upper ? mean2 : m.mean, upper ? m22 : m.m2};
-    lo.merge(upper ? m.n : n2, upper ? m.mean : mean2, upper ? m.m2 : m22);
-    m = lo;
-  }
-  if (warps > 1) {
-    if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = make_float4(m.n, m.mean, m.m2, 0.f);
-    __syncthreads();
-    const float4 f = slot[first_warp];
-    m = Moments{f.x, f.y, f.z};
-    for (int w = 1; w < warps; ++w) {
-      const float4 g = slot[first_warp + w];
-      m.merge(g.x, g.y, g.z);
-    }
-  }
-  return make_float2(m.mean, rsqrtf(m.m2 / static_cast<float>(width) + eps));
+  return s;
 }
-
-// Sums of two values over the row's warps.
-__device__ __forceinline__ float2 row_sum2(float a, float b, float4* slot, int warps, int first_warp) {
-  a = warp_sum(a);
-  b = warp_sum(b);
-  if (warps > 1) {
-    if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = make_float4(a, b, 0.f, 0.f);
-    __syncthreads();
-    a = b = 0.f;
-    for (int w = 0; w < warps; ++w) {
-      const float4 g = slot[first_warp + w];
-      a += g.x;
-      b += g.y;
-    }
-  }
-  return make_float2(a, b);
-}
-
 template <int kNV>
-__global__ void __launch_bounds__(256) gated_norm_kernel(const __grid_constant__ NormSegs segs, const __grid_constant__ NormArgs a) {
-  __shared__ float4 slots[2][8];
-  const int warps = a.warps_per_row, warp = threadIdx.x >> 5;
-  const int group = warp / warps, first_warp = group * warps;
-  const int tid = threadIdx.x - 32 * first_warp;
-  const int row = blockIdx.x * a.rows_per_block + group;
-  const bool on = row < a.rows;
-  const int nvec = a.width / 8, stride = 32 * warps;
-  const int have = on && tid < nvec ? min(kNV, (nvec - tid + stride - 1) / stride) : 0;
+__device__ __forceinline__ float sum_of(const Vec8 (&t)[kNV]) {  // (columns past the row are zero)
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < kNV; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += t[i].v[e];
+  return s;
+}
+template <int kNV>
+__device__ __forceinline__ float2 row_stats(const Vec8 (&t)[kNV], int have, int kind, float eps, float inv_w, BlockSum& sum) {
+  float mean = 0.f;
+  if (kind == kNormLayer) {
+    float s[1] = {sum_of<kNV>(t)};
+    sum(s);
+    mean = s[0] * inv_w;
+  }
+  float q[1] = {centered_squares<kNV>(t, have, mean)};
+  sum(q);
+  return make_float2(mean, rsqrtf(q[0] * inv_w + eps));
+}
+
+constexpr int kNormFwdSlots = 4;
+// rows of the backward pass in shared memory (four tensors: 64 KB a row at the largest width)
+__host__ __device__ constexpr int norm_bwd_slots(int threads) { return threads > 256 ? 2 : 3; }
+
+template <int kNV, int kThreads>
+__global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_kernel(const __grid_constant__ NormSegs segs,
+                                                                             const __grid_constant__ NormArgs a) {
+  extern __shared__ __align__(16) uint8_t smem_norm[];
+  __shared__ float4 slots[2 * kThreads / 32];
+  const int tid = threadIdx.x, nvec = a.width / 8;
+  const int have = tid < nvec ? min(kNV, (nvec - tid + static_cast<int>(blockDim.x) - 1) / static_cast<int>(blockDim.x)) : 0;
   const bool f32 = a.mod_f32 != 0;
+  const int r0 = blockIdx.x * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
+  const float inv_w = 1.f / static_cast<float>(a.width);
+  BlockSum sum{slots, static_cast<int>(blockDim.x >> 5)};
   grid_dependency_wait();
   if (threadIdx.x == 0) grid_launch_dependents();
-  const int seg = on ? segment_of(segs, row) : 0;
-  const int64_t base = static_cast<int64_t>(on ? row : 0) * a.width;
-  Vec8 t[kNV];
-  {
-    uint4 xr[kNV], br[kNV];
+  RowsAhead<kNV, 2, kNormFwdSlots> in{smem_norm, {a.x, a.branch}, a.width, have};
 #pragma unroll
-    for (int i = 0; i < kNV; ++i) {
-      xr[i] = br[i] = make_uint4(0, 0, 0, 0);
-      if (i < have) {
-        xr[i] = ld_stream(a.x + base + 8 * (tid + i * stride));
-        if (a.branch) br[i] = ld_stream(a.branch + base + 8 * (tid + i * stride));
+  for (int i = 0; i < kNormFwdSlots - 1; ++i) in.load(r0 + i, r0 + i < r1);
+  Vec8 gate[kNV], scale[kNV], shift[kNV];  // gate (times the branch's weight), weight (1 + scale), shift
+  int seg = segment_of(segs, r0) - 1;
+#pragma unroll 1
+  for (int row = r0; row < r1; ++row) {
+    if (row == r0 || row >= segs.cu[seg + 1]) {
+      do ++seg;
+      while (row >= segs.cu[seg + 1]);  // (skips requests without rows)
+#pragma unroll
+      for (int i = 0; i < kNV; ++i) {
+        if (i >= have) continue;
+        const int col = 8 * (tid + i * blockDim.x);
+        gate[i] = a.gate ? load_param8(a.gate, seg * a.ld_gate + col, f32) : fill8(1.f);
+        const Vec8 pw = a.post_weight ? load_param8(a.post_weight, col, f32) : fill8(1.f);
+        const Vec8 w = a.weight ? load_param8(a.weight, col, f32) : fill8(1.f);
+        scale[i] = a.scale ? load_param8(a.scale, seg * a.ld_scale + col, f32) : fill8(0.f);
+        shift[i] = a.shift ? load_param8(a.shift, seg * a.ld_shift + col, f32) : fill8(0.f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          gate[i].v[e] *= pw.v[e];
+          scale[i].v[e] = fmaf(w.v[e], scale[i].v[e], w.v[e]);
+        }
       }
     }
+    in.wait();
+    const int n = row - r0;
+    const int64_t base = static_cast<int64_t>(row) * a.width;
+    Vec8 t[kNV];
+#pragma unroll
+    for (int i = 0; i < kNV; ++i) t[i] = in.get(n, 0, i);
     if (a.branch) {
       Vec8 h[kNV];
 #pragma unroll
-      for (int i = 0; i < kNV; ++i) h[i] = unpack8(br[i]);
-      if (a.post_norm) {
-        const float2 st = row_stats<kNV>(h, have, a.post_norm, a.eps, a.width, slots[0], warps, first_warp);
-#pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-          if (i >= have) continue;
-          const Vec8 w = a.post_weight ? load_param8(a.post_weight, 8 * (tid + i * stride), f32) : fill8(1.f);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) h[i].v[e] = (h[i].v[e] - st.x) * st.y * w.v[e];
-        }
-      }
+      for (int i = 0; i < kNV; ++i) h[i] = in.get(n, 1, i);
+      const float2 st = a.post_norm ? row_stats<kNV>(h, have, a.post_norm, a.eps, inv_w, sum) : make_float2(0.f, 1.f);
 #pragma unroll
       for (int i = 0; i < kNV; ++i) {
-        t[i] = unpack8(xr[i]);
         if (i >= have) continue;
-        const int col = 8 * (tid + i * stride);
-        const Vec8 g = a.gate ? load_param8(a.gate, seg * a.ld_gate + col, f32) : fill8(1.f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[i].v[e] = fmaf(g.v[e], h[i].v[e], t[i].v[e]);
-        if (a.x_out) *reinterpret_cast<uint4*>(a.x_out + base + col) = pack8(t[i]);
+        for (int e = 0; e < 8; ++e) t[i].v[e] = fmaf(gate[i].v[e], (h[i].v[e] - st.x) * st.y, t[i].v[e]);
+        if (a.x_out) *reinterpret_cast<uint4*>(a.x_out + base + 8 * (tid + i * blockDim.x)) = pack8(t[i]);
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kNV; ++i) t[i] = unpack8(xr[i]);
     }
-  }
-  if (!a.y) return;
-  const float2 st = a.norm ? row_stats<kNV>(t, have, a.norm, a.eps, a.width, slots[1], warps, first_warp) : make_float2(0.f, 1.f);
+    in.load(row + kNormFwdSlots - 1, row + kNormFwdSlots - 1 < r1);
+    if (!a.y) continue;
+    const float2 st = a.norm ? row_stats<kNV>(t, have, a.norm, a.eps, inv_w, sum) : make_float2(0.f, 1.f);
 #pragma unroll
-  for (int i = 0; i < kNV; ++i) {
-    if (i >= have) continue;
-    const int col = 8 * (tid + i * stride);
-    const Vec8 w = a.weight ? load_param8(a.weight, col, f32) : fill8(1.f);
-    const Vec8 sc = a.scale ? load_param8(a.scale, seg * a.ld_scale + col, f32) : fill8(0.f);
-    const Vec8 sh = a.shift ? load_param8(a.shift, seg * a.ld_shift + col, f32) : fill8(0.f);
-    Vec8 y;
+    for (int i = 0; i < kNV; ++i) {
+      if (i >= have) continue;
+      Vec8 y;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y.v[e] = fmaf((t[i].v[e] - st.x) * st.y * w.v[e], 1.f + sc.v[e], sh.v[e]);
-    *reinterpret_cast<uint4*>(a.y + base + col) = pack8(y);
+      for (int e = 0; e < 8; ++e) y.v[e] = fmaf((t[i].v[e] - st.x) * st.y, scale[i].v[e], shift[i].v[e]);
+      *reinterpret_cast<uint4*>(a.y + base + 8 * (tid + i * blockDim.x)) = pack8(y);
+    }
   }
 }
 
@@ -212,106 +247,142 @@ __global__ void __launch_bounds__(256) gated_norm_kernel(const __grid_constant__
 //   d_shift = A, d_scale = weight B, d_gate = post_weight G,
 //   d_weight = sum over requests (1 + scale) B,  d_post_weight = sum over requests gate G
 //
-// A block walks over rows_per_block consecutive rows and keeps the three sums of
-// its columns in registers; at a request's end they go to slot block + request
-// of `part`, which no other (block, request) has.
+// A block keeps the three sums of its columns in registers over its rows; at a
+// request's end they go to slot block + request of `part`, which no other (block,
+// request) has.  The request's two vectors lie in shared memory beside the rows ahead,
+// for the registers' sake.
 template <int kNV, int kThreads>
-__global__ void __launch_bounds__(kThreads) gated_norm_backward_kernel(const __grid_constant__ NormSegs segs,
-                                                                   const __grid_constant__ NormArgs a) {
-  __shared__ float4 slots[4][kThreads / 32];
-  const int warps = blockDim.x >> 5, tid = threadIdx.x;
-  const int nvec = a.width / 8, stride = blockDim.x;
-  const int have = tid < nvec ? min(kNV, (nvec - tid + stride - 1) / stride) : 0;
+__global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_backward_kernel(const __grid_constant__ NormSegs segs,
+                                                                                      const __grid_constant__ NormArgs a) {
+  constexpr int kSlots = norm_bwd_slots(kThreads);
+  extern __shared__ __align__(16) uint8_t smem_norm[];
+  __shared__ float4 slots[2 * kThreads / 32];
+  const int tid = threadIdx.x, nvec = a.width / 8;
+  const int have = tid < nvec ? min(kNV, (nvec - tid + static_cast<int>(blockDim.x) - 1) / static_cast<int>(blockDim.x)) : 0;
   const bool f32 = a.mod_f32 != 0;
   const int r0 = blockIdx.x * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
+  const float inv_w = 1.f / static_cast<float>(a.width);
+  BlockSum sum{slots, static_cast<int>(blockDim.x >> 5)};
   grid_dependency_wait();
   if (threadIdx.x == 0) grid_launch_dependents();
+  RowsAhead<kNV, 4, kSlots> in{smem_norm, {a.dy ? a.x : nullptr, a.branch, a.dy, a.dx_out}, a.width, have};
+#pragma unroll
+  for (int i = 0; i < kSlots - 1; ++i) in.load(r0 + i, r0 + i < r1);
+  // [scale or gate][vector][half][thread] float4
+  float4* vecs = reinterpret_cast<float4*>(smem_norm + static_cast<int64_t>(kSlots) * 4 * kNV * blockDim.x * 16) + tid;
+  auto vec = [&](int k, int i, int h) -> float4& { return vecs[((k * kNV + i) * 2 + h) * blockDim.x]; };
+  auto get_vec = [&](int k, int i) -> Vec8 {
+    const float4 p = vec(k, i, 0), q = vec(k, i, 1);
+    return Vec8{{p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w}};
+  };
   Vec8 sa[kNV], sb[kNV], sg[kNV];
 #pragma unroll
   for (int i = 0; i < kNV; ++i) sa[i] = sb[i] = sg[i] = fill8(0.f);
-  const float inv_w = 1.f / static_cast<float>(a.width);
-  int seg = segment_of(segs, r0);
+  int seg = segment_of(segs, r0) - 1;
 #pragma unroll 1
   for (int row = r0; row < r1; ++row) {
-    while (row >= segs.cu[seg + 1]) ++seg;  // (skips requests without rows)
-    const int64_t base = static_cast<int64_t>(row) * a.width;
-    Vec8 x[kNV], f[kNV];
-    uint4 dyr[kNV], dor[kNV];
-#pragma unroll
-    for (int i = 0; i < kNV; ++i) {
-      const int col = 8 * (tid + i * stride);
-      const bool on = i < have;
-      const uint4 z = make_uint4(0, 0, 0, 0);
-      x[i] = unpack8(on && a.dy ? ld_stream(a.x + base + col) : z);
-      f[i] = unpack8(on && a.branch ? ld_stream(a.branch + base + col) : z);
-      dyr[i] = on && a.dy ? ld_stream(a.dy + base + col) : z;
-      dor[i] = on && a.dx_out ? ld_stream(a.dx_out + base + col) : z;
-    }
-    float2 fs = make_float2(0.f, 1.f);
-    if (a.branch && a.post_norm) fs = row_stats<kNV>(f, have, a.post_norm, a.eps, a.width, slots[0], warps, 0);
-    Vec8 d[kNV];
-#pragma unroll
-    for (int i = 0; i < kNV; ++i) d[i] = unpack8(dor[i]);
-    if (a.dy) {
-      const float2 st = a.norm ? row_stats<kNV>(x, have, a.norm, a.eps, a.width, slots[1], warps, 0) : make_float2(0.f, 1.f);
-      Vec8 u[kNV];
-      float su = 0.f, sux = 0.f;
+    if (row == r0 || row >= segs.cu[seg + 1]) {
+      do ++seg;
+      while (row >= segs.cu[seg + 1]);  // (skips requests without rows)
 #pragma unroll
       for (int i = 0; i < kNV; ++i) {
-        u[i] = unpack8(dyr[i]);
         if (i >= have) continue;
-        const int col = 8 * (tid + i * stride);
+        const int col = 8 * (tid + i * blockDim.x);
         const Vec8 w = a.weight ? load_param8(a.weight, col, f32) : fill8(1.f);
         const Vec8 sc = a.scale ? load_param8(a.scale, seg * a.ld_scale + col, f32) : fill8(0.f);
+        const Vec8 g = a.gate ? load_param8(a.gate, seg * a.ld_gate + col, f32) : fill8(1.f);
+        const Vec8 pw = a.post_weight ? load_param8(a.post_weight, col, f32) : fill8(1.f);
+        float p[8], q[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          x[i].v[e] = (x[i].v[e] - st.x) * st.y;
-          sa[i].v[e] += u[i].v[e];
-          sb[i].v[e] = fmaf(u[i].v[e], x[i].v[e], sb[i].v[e]);
-          u[i].v[e] *= (1.f + sc.v[e]) * w.v[e];
-          su += u[i].v[e];
-          sux = fmaf(u[i].v[e], x[i].v[e], sux);
+          p[e] = fmaf(w.v[e], sc.v[e], w.v[e]);
+          q[e] = g.v[e] * pw.v[e];
+        }
+        vec(0, i, 0) = make_float4(p[0], p[1], p[2], p[3]);
+        vec(0, i, 1) = make_float4(p[4], p[5], p[6], p[7]);
+        vec(1, i, 0) = make_float4(q[0], q[1], q[2], q[3]);
+        vec(1, i, 1) = make_float4(q[4], q[5], q[6], q[7]);
+      }
+    }
+    in.wait();
+    const int n = row - r0;
+    const int64_t base = static_cast<int64_t>(row) * a.width;
+    Vec8 x[kNV], f[kNV];
+#pragma unroll
+    for (int i = 0; i < kNV; ++i) {
+      x[i] = in.get(n, 0, i);
+      f[i] = in.get(n, 1, i);
+    }
+    // statistics of both norms in the same exchanges
+    const int kind = a.dy ? a.norm : kNormNone, post = a.branch ? a.post_norm : kNormNone;
+    float2 xs = make_float2(0.f, 1.f), fs = make_float2(0.f, 1.f);
+    if (kind == kNormLayer || post == kNormLayer) {
+      float m[2] = {sum_of<kNV>(x), sum_of<kNV>(f)};
+      sum(m);
+      if (kind == kNormLayer) xs.x = m[0] * inv_w;
+      if (post == kNormLayer) fs.x = m[1] * inv_w;
+    }
+    if (kind || post) {
+      float q[2] = {centered_squares<kNV>(x, have, xs.x), centered_squares<kNV>(f, have, fs.x)};
+      sum(q);
+      if (kind) xs.y = rsqrtf(q[0] * inv_w + a.eps);
+      if (post) fs.y = rsqrtf(q[1] * inv_w + a.eps);
+    }
+    float u2[2] = {0.f, 0.f};
+    if (a.dy) {
+#pragma unroll
+      for (int i = 0; i < kNV; ++i) {
+        if (i >= have) continue;
+        const Vec8 dy = in.get(n, 2, i), w = get_vec(0, i);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x[i].v[e] = (x[i].v[e] - xs.x) * xs.y;
+          sa[i].v[e] += dy.v[e];
+          sb[i].v[e] = fmaf(dy.v[e], x[i].v[e], sb[i].v[e]);
+          const float u = dy.v[e] * w.v[e];
+          u2[0] += u;
+          u2[1] = fmaf(u, x[i].v[e], u2[1]);
         }
       }
-      float2 s = make_float2(0.f, 0.f);
-      if (a.norm) s = row_sum2(su, sux, slots[2], warps, 0);
-      const float mu = a.norm == kNormLayer ? s.x * inv_w : 0.f, mux = s.y * inv_w;
-#pragma unroll
-      for (int i = 0; i < kNV; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[i].v[e] = fmaf(st.y, u[i].v[e] - mu - x[i].v[e] * mux, d[i].v[e]);
+      if (kind) sum(u2);
     }
-    float sd = 0.f, sdf = 0.f;
+    const float mu = kind == kNormLayer ? u2[0] * inv_w : 0.f, mux = kind ? u2[1] * inv_w : 0.f;
+    float d2[2] = {0.f, 0.f};
+    Vec8 d[kNV];  // dh times post_weight, in the end
 #pragma unroll
     for (int i = 0; i < kNV; ++i) {
       if (i >= have) continue;
-      const int col = 8 * (tid + i * stride);
+      const int col = 8 * (tid + i * blockDim.x);
+      d[i] = in.get(n, 3, i);
+      if (a.dy) {
+        const Vec8 dy = in.get(n, 2, i), w = get_vec(0, i);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[i].v[e] = fmaf(xs.y, fmaf(dy.v[e], w.v[e], -fmaf(x[i].v[e], mux, mu)), d[i].v[e]);
+      }
       if (a.dx) *reinterpret_cast<uint4*>(a.dx + base + col) = pack8(d[i]);
       if (!a.branch) continue;
-      const Vec8 g = a.gate ? load_param8(a.gate, seg * a.ld_gate + col, f32) : fill8(1.f);
-      const Vec8 w = a.post_norm && a.post_weight ? load_param8(a.post_weight, col, f32) : fill8(1.f);
+      const Vec8 g = get_vec(1, i);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         f[i].v[e] = (f[i].v[e] - fs.x) * fs.y;
         sg[i].v[e] = fmaf(d[i].v[e], f[i].v[e], sg[i].v[e]);
-        d[i].v[e] *= g.v[e] * w.v[e];
-        sd += d[i].v[e];
-        sdf = fmaf(d[i].v[e], f[i].v[e], sdf);
+        d[i].v[e] *= g.v[e];
+        d2[0] += d[i].v[e];
+        d2[1] = fmaf(d[i].v[e], f[i].v[e], d2[1]);
       }
     }
+    in.load(row + kSlots - 1, row + kSlots - 1 < r1);
     if (a.branch) {
-      float mu = 0.f, muf = 0.f;
-      if (a.post_norm) {
-        const float2 s = row_sum2(sd, sdf, slots[3], warps, 0);
-        mu = a.post_norm == kNormLayer ? s.x * inv_w : 0.f;
-        muf = s.y * inv_w;
-      }
+      if (post) sum(d2);
+      const float md = post == kNormLayer ? d2[0] * inv_w : 0.f, mdf = post ? d2[1] * inv_w : 0.f;
+      if (a.d_branch) {
 #pragma unroll
-      for (int i = 0; i < kNV; ++i) {
-        if (i >= have) continue;
+        for (int i = 0; i < kNV; ++i) {
+          if (i >= have) continue;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[i].v[e] = fs.y * (d[i].v[e] - mu - f[i].v[e] * muf);
-        if (a.d_branch) *reinterpret_cast<uint4*>(a.d_branch + base + 8 * (tid + i * stride)) = pack8(d[i]);
+          for (int e = 0; e < 8; ++e) d[i].v[e] = fs.y * (d[i].v[e] - fmaf(f[i].v[e], mdf, md));
+          *reinterpret_cast<uint4*>(a.d_branch + base + 8 * (tid + i * blockDim.x)) = pack8(d[i]);
+        }
       }
     }
     if (row + 1 == r1 || row + 1 == segs.cu[seg + 1]) {
@@ -319,7 +390,7 @@ __global__ void __launch_bounds__(kThreads) gated_norm_backward_kernel(const __g
 #pragma unroll
       for (int i = 0; i < kNV; ++i) {
         if (i >= have) continue;
-        const int col = 8 * (tid + i * stride);
+        const int col = 8 * (tid + i * blockDim.x);
         auto put = [&](int k, Vec8& s) {
           float4* q = reinterpret_cast<float4*>(p + static_cast<int64_t>(k) * a.width + col);
           q[0] = make_float4(s.v[0], s.v[1], s.v[2], s.v[3]);
@@ -331,7 +402,6 @@ __global__ void __launch_bounds__(kThreads) gated_norm_backward_kernel(const __g
         put(2, sg[i]);
       }
     }
-    __syncthreads();  // the exchange's shared memory is free for the next row
   }
 }
 

@@ -153,9 +153,9 @@ __global__ void __launch_bounds__(kRopeThreads) qkv_rope_kernel(const __grid_con
 // The gradient: a warp walks over tokens row, row + stride, ... so that the sums
 // of dw stay in registers; the block's sum goes to dw_part.
 template <int D, bool kHalves>
-__global__ void __launch_bounds__(kRopeThreads) qkv_rope_backward_kernel(const __grid_constant__ RopeTable table,
+__global__ void __launch_bounds__(kRopeThreads, 2) qkv_rope_backward_kernel(const __grid_constant__ RopeTable table,
                                                                          const __grid_constant__ RopeArgs a) {
-  constexpr int kLanes = D / 8, kPer = 32 / kLanes, kUnroll = 2;
+  constexpr int kLanes = D / 8, kPer = 32 / kLanes, kUnroll = 4;
   __shared__ float sums[kRopeTokens][D];
   const int lane = threadIdx.x & 31, l = lane % kLanes, sub = lane / kLanes, warp = threadIdx.x >> 5;
   grid_dependency_wait();
