@@ -91,7 +91,7 @@ void rope_tables(const refcache_rope_t* r, const refcache_rope_rows_t* w, rc::Ro
 // divided among up to as many warps as have a full set of loads each.
 int rope_slices(const refcache_rope_t* r, const refcache_rope_rows_t* w, int sms, int unroll, int* step) {
   const int per = 32 / (r->head_dim / 8), most = std::min(64, ceil_div(w->num_heads, unroll * per));
-  const int64_t want = (32ll * sms + w->rows - 1) / w->rows;
+  const int64_t want = 32ll * sms / w->rows;
   int slices = static_cast<int>(std::min<int64_t>(most, std::max<int64_t>(1, want)));
   *step = ceil_div(ceil_div(w->num_heads, slices), per) * per;
   return ceil_div(w->num_heads, *step);
@@ -164,7 +164,7 @@ NormShape norm_shape(int width, bool backward) {
   NormShape n{};
   n.nv = nvec <= 256 ? 1 : 2;
   n.threads = 32 * ceil_div(nvec, 32 * n.nv);
-  n.smem = n.nv * n.threads * 16 * (backward ? rc::norm_bwd_slots(n.threads) * 4 + 4 : rc::kNormFwdSlots * 2);
+  n.smem = n.nv * n.threads * 16 * (backward ? rc::kNormBwdSlots * 4 + 4 : rc::kNormFwdSlots * 2);
   return n;
 }
 // Blocks: as many as an SM holds (of 65536 registers, 128 a thread, and 227 KB), and at
@@ -308,7 +308,7 @@ int refcache_qkv_rope_backward(const refcache_rope_t* r, const refcache_rope_row
     if (e != cudaSuccess) return cuda_fail(e, "qkv_rope_backward_kernel launch");
   }
   if (dweight_q || dweight_k) {
-    e = launch_dependent(rc::rope_weight_grad_kernel, dim3(2), dim3(1024), 0, s, static_cast<const float*>(work), parts, r->head_dim,
+    e = launch_dependent(rc::rope_weight_grad_kernel, dim3(static_cast<unsigned>(r->head_dim / rc::kRopeSumCols), 2), dim3(1024), 0, s, static_cast<const float*>(work), parts, r->head_dim,
                          dweight_q, dweight_k);
     if (e != cudaSuccess) return cuda_fail(e, "rope_weight_grad_kernel launch");
   }
@@ -416,7 +416,7 @@ int refcache_gated_norm_backward(const refcache_gated_norm_t* p, const void* x_o
     g.rows_per_block = a.rows_per_block;
     g.mod_f32 = a.mod_f32;
     g.add = b > 0;
-    e = launch_dependent(rc::norm_param_grad_kernel, dim3(static_cast<unsigned>(ceil_div(p->width, 32)), 3), dim3(256), 0, s, segs, g);
+    e = launch_dependent(rc::norm_param_grad_kernel, dim3(static_cast<unsigned>(ceil_div(p->width, 64)), 3), dim3(32 * rc::kSumWarps), 0, s, segs, g);
     if (e != cudaSuccess) return cuda_fail(e, "norm_param_grad_kernel launch");
   }
   return REFCACHE_OK;

@@ -90,151 +90,183 @@ struct BlockSum {
 };
 
 // The rows ahead of the one that is worked on, kTensors of each, in shared memory:
-// [slot][tensor][vector][thread], 16 bytes each.
+// [slot][tensor][vector][thread], 16 bytes each.  A tensor that is not there (null) and
+// a vector past the row's end read as zeros.
 template <int kNV, int kTensors, int kSlots>
 struct RowsAhead {
-  uint8_t* smem;
-  const uint16_t* src[kTensors];  // null: zeros
-  int64_t width;
-  int have, issued = 0;
+  uint8_t* mine;               // this thread's first 16 bytes
+  const uint8_t* src[kTensors];  // this thread's first vector of the next row to load
+  uint32_t vec, row_bytes;     // bytes between vectors (of the row and in shared memory), between rows
+  bool last;                   // the kNV-th vector is inside the row
+  int write = 0, read = 0;     // slots
   __device__ __forceinline__ uint8_t* at(int slot, int tensor, int i) const {
-    return smem + ((static_cast<int64_t>(slot * kTensors + tensor) * kNV + i) * blockDim.x + threadIdx.x) * 16;
+    return mine + (static_cast<uint32_t>(slot * kTensors + tensor) * kNV + i) * vec;
   }
-  __device__ __forceinline__ void load(int row, bool on) {
-    const int slot = issued % kSlots;
-    if (on) {
+  __device__ __forceinline__ void init(uint8_t* smem, const uint16_t* const (&tensors)[kTensors], int width, int row0, bool last_vector) {
+    vec = 16u * blockDim.x;
+    row_bytes = 2u * static_cast<uint32_t>(width);
+    last = last_vector;
+    mine = smem + 16u * threadIdx.x;
 #pragma unroll
-      for (int t = 0; t < kTensors; ++t)
-        if (src[t]) {
+    for (int t = 0; t < kTensors; ++t) {
+      src[t] = tensors[t] ? reinterpret_cast<const uint8_t*>(tensors[t] + static_cast<int64_t>(row0) * width) + 16u * threadIdx.x : nullptr;
 #pragma unroll
-          for (int i = 0; i < kNV; ++i)
-            if (i < have)
-              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(at(slot, t, i))),
-                           "l"(src[t] + row * width + 8 * static_cast<int64_t>(threadIdx.x + i * blockDim.x))
-                           : "memory");
+      for (int i = 0; i < kNV; ++i)
+        if (!tensors[t] || (i == kNV - 1 && !last)) {
+#pragma unroll
+          for (int s = 0; s < kSlots; ++s) *reinterpret_cast<uint4*>(at(s, t, i)) = make_uint4(0, 0, 0, 0);
         }
     }
+  }
+  __device__ __forceinline__ void load(bool on) {
+#pragma unroll
+    for (int t = 0; t < kTensors; ++t) {
+      if (!src[t]) continue;
+      if (on) {
+#pragma unroll
+        for (int i = 0; i < kNV; ++i)
+          if (i < kNV - 1 || last)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(at(write, t, i))), "l"(src[t] + i * vec) : "memory");
+      }
+      src[t] += row_bytes;
+    }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    ++issued;
+    write = write + 1 == kSlots ? 0 : write + 1;
   }
-  // the oldest row that is not read yet: `row`-th of the block
+  // the oldest row that was not read yet
   __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 2) : "memory"); }
-  __device__ __forceinline__ Vec8 get(int n, int tensor, int i) const {
-    if (i >= have || !src[tensor]) return fill8(0.f);
-    return unpack8(*reinterpret_cast<const uint4*>(at(n % kSlots, tensor, i)));
-  }
+  __device__ __forceinline__ Pair8 get(int tensor, int i) const { return unpack_pairs(*reinterpret_cast<const uint4*>(at(read, tensor, i))); }
+  __device__ __forceinline__ void next() { read = read + 1 == kSlots ? 0 : read + 1; }
 };
 
+// Sums over this thread's columns: of the values, and of the squares of their
+// distances from the mean (columns past the row are zero, and left out there).
+template <int kNV>
+__device__ __forceinline__ float sum_of(const Pair8 (&t)[kNV]) {
+  f32x2 s = splat2(0.f);
+#pragma unroll
+  for (int i = 0; i < kNV; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s = add_f32x2(s, t[i].p[e]);
+  return sum2(s);
+}
+template <int kNV>
+__device__ __forceinline__ float centered_squares(const Pair8 (&t)[kNV], float mean, bool last) {
+  const f32x2 m = splat2(-mean);
+  float total = 0.f;
+#pragma unroll
+  for (int i = 0; i < kNV; ++i) {
+    f32x2 s = splat2(0.f);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const f32x2 d = add_f32x2(t[i].p[e], m);
+      s = fma_f32x2(d, d, s);
+    }
+    total += i < kNV - 1 || last ? sum2(s) : 0.f;
+  }
+  return total;
+}
 // (mean, 1 / deviation) of a layer norm, (0, 1 / rms) of an RMS norm.
 template <int kNV>
-__device__ __forceinline__ float centered_squares(const Vec8 (&t)[kNV], int have, float mean) {
-  float s = 0.f;
-#pragma unroll
-  for (int i = 0; i < kNV; ++i)
-    if (i < have) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float d = t[i].v[e] - mean;
-        s = fmaf(d, d, s);
-      }
-    }
-  return s;
-}
-template <int kNV>
-__device__ __forceinline__ float sum_of(const Vec8 (&t)[kNV]) {  // (columns past the row are zero)
-  float s = 0.f;
-#pragma unroll
-  for (int i = 0; i < kNV; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s += t[i].v[e];
-  return s;
-}
-template <int kNV>
-__device__ __forceinline__ float2 row_stats(const Vec8 (&t)[kNV], int have, int kind, float eps, float inv_w, BlockSum& sum) {
+__device__ __forceinline__ float2 row_stats(const Pair8 (&t)[kNV], bool last, int kind, float eps, float inv_w, BlockSum& sum) {
   float mean = 0.f;
   if (kind == kNormLayer) {
     float s[1] = {sum_of<kNV>(t)};
     sum(s);
     mean = s[0] * inv_w;
   }
-  float q[1] = {centered_squares<kNV>(t, have, mean)};
+  float q[1] = {centered_squares<kNV>(t, mean, last)};
   sum(q);
   return make_float2(mean, rsqrtf(q[0] * inv_w + eps));
 }
 
 constexpr int kNormFwdSlots = 4;
-// rows of the backward pass in shared memory (four tensors: 64 KB a row at the largest width)
-__host__ __device__ constexpr int norm_bwd_slots(int threads) { return threads > 256 ? 2 : 3; }
+// Rows of the backward pass in shared memory (four tensors: 32 KB a row at a width of 4096).
+constexpr int kNormBwdSlots = 2;
 
 template <int kNV, int kThreads>
 __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_kernel(const __grid_constant__ NormSegs segs,
                                                                              const __grid_constant__ NormArgs a) {
   extern __shared__ __align__(16) uint8_t smem_norm[];
   __shared__ float4 slots[2 * kThreads / 32];
-  const int tid = threadIdx.x, nvec = a.width / 8;
-  const int have = tid < nvec ? min(kNV, (nvec - tid + static_cast<int>(blockDim.x) - 1) / static_cast<int>(blockDim.x)) : 0;
+  const int tid = threadIdx.x;
+  const bool last = (tid + (kNV - 1) * static_cast<int>(blockDim.x)) * 8 < a.width;
   const bool f32 = a.mod_f32 != 0;
   const int r0 = blockIdx.x * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
   const float inv_w = 1.f / static_cast<float>(a.width);
   BlockSum sum{slots, static_cast<int>(blockDim.x >> 5)};
   grid_dependency_wait();
   if (threadIdx.x == 0) grid_launch_dependents();
-  RowsAhead<kNV, 2, kNormFwdSlots> in{smem_norm, {a.x, a.branch}, a.width, have};
+  RowsAhead<kNV, 2, kNormFwdSlots> in;
+  in.init(smem_norm, {a.x, a.branch}, a.width, r0, last);
 #pragma unroll
-  for (int i = 0; i < kNormFwdSlots - 1; ++i) in.load(r0 + i, r0 + i < r1);
-  Vec8 gate[kNV], scale[kNV], shift[kNV];  // gate (times the branch's weight), weight (1 + scale), shift
-  int seg = segment_of(segs, r0) - 1;
+  for (int i = 0; i < kNormFwdSlots - 1; ++i) in.load(r0 + i < r1);
+  Pair8 gate[kNV], scale[kNV], shift[kNV];  // gate (times the branch's weight), weight (1 + scale), shift
+  int seg = segment_of(segs, r0) - 1, end = r0;
+  const int64_t off0 = 2 * (static_cast<int64_t>(r0) * a.width + 8 * tid);
+  uint8_t* x_out = a.x_out ? reinterpret_cast<uint8_t*>(a.x_out) + off0 : nullptr;
+  uint8_t* y_out = a.y ? reinterpret_cast<uint8_t*>(a.y) + off0 : nullptr;
 #pragma unroll 1
   for (int row = r0; row < r1; ++row) {
-    if (row == r0 || row >= segs.cu[seg + 1]) {
-      do ++seg;
-      while (row >= segs.cu[seg + 1]);  // (skips requests without rows)
+    if (row >= end) {
+      do end = segs.cu[++seg + 1];
+      while (row >= end);  // (skips requests without rows)
 #pragma unroll
       for (int i = 0; i < kNV; ++i) {
-        if (i >= have) continue;
+        gate[i] = scale[i] = shift[i] = pairs_of(fill8(0.f));
+        if (i == kNV - 1 && !last) continue;
         const int col = 8 * (tid + i * blockDim.x);
-        gate[i] = a.gate ? load_param8(a.gate, seg * a.ld_gate + col, f32) : fill8(1.f);
+        Vec8 g = a.gate ? load_param8(a.gate, seg * a.ld_gate + col, f32) : fill8(1.f);
         const Vec8 pw = a.post_weight ? load_param8(a.post_weight, col, f32) : fill8(1.f);
         const Vec8 w = a.weight ? load_param8(a.weight, col, f32) : fill8(1.f);
-        scale[i] = a.scale ? load_param8(a.scale, seg * a.ld_scale + col, f32) : fill8(0.f);
-        shift[i] = a.shift ? load_param8(a.shift, seg * a.ld_shift + col, f32) : fill8(0.f);
+        Vec8 sc = a.scale ? load_param8(a.scale, seg * a.ld_scale + col, f32) : fill8(0.f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          gate[i].v[e] *= pw.v[e];
-          scale[i].v[e] = fmaf(w.v[e], scale[i].v[e], w.v[e]);
+          g.v[e] *= pw.v[e];
+          sc.v[e] = fmaf(w.v[e], sc.v[e], w.v[e]);
         }
+        gate[i] = pairs_of(g);
+        scale[i] = pairs_of(sc);
+        if (a.shift) shift[i] = pairs_of(load_param8(a.shift, seg * a.ld_shift + col, f32));
       }
     }
     in.wait();
-    const int n = row - r0;
-    const int64_t base = static_cast<int64_t>(row) * a.width;
-    Vec8 t[kNV];
+    Pair8 t[kNV];
 #pragma unroll
-    for (int i = 0; i < kNV; ++i) t[i] = in.get(n, 0, i);
+    for (int i = 0; i < kNV; ++i) t[i] = in.get(0, i);
     if (a.branch) {
-      Vec8 h[kNV];
+      Pair8 h[kNV];
 #pragma unroll
-      for (int i = 0; i < kNV; ++i) h[i] = in.get(n, 1, i);
-      const float2 st = a.post_norm ? row_stats<kNV>(h, have, a.post_norm, a.eps, inv_w, sum) : make_float2(0.f, 1.f);
+      for (int i = 0; i < kNV; ++i) h[i] = in.get(1, i);
+      if (a.post_norm) {
+        const float2 st = row_stats<kNV>(h, last, a.post_norm, a.eps, inv_w, sum);
+        const f32x2 r = splat2(st.y), m = splat2(-st.x * st.y);
+#pragma unroll
+        for (int i = 0; i < kNV; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) h[i].p[e] = fma_f32x2(h[i].p[e], r, m);
+      }
 #pragma unroll
       for (int i = 0; i < kNV; ++i) {
-        if (i >= have) continue;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[i].v[e] = fmaf(gate[i].v[e], (h[i].v[e] - st.x) * st.y, t[i].v[e]);
-        if (a.x_out) *reinterpret_cast<uint4*>(a.x_out + base + 8 * (tid + i * blockDim.x)) = pack8(t[i]);
+        for (int e = 0; e < 4; ++e) t[i].p[e] = fma_f32x2(gate[i].p[e], h[i].p[e], t[i].p[e]);
+        if (x_out && (i < kNV - 1 || last)) *reinterpret_cast<uint4*>(x_out + i * in.vec) = pack_pairs(t[i]);
       }
+      if (x_out) x_out += in.row_bytes;
     }
-    in.load(row + kNormFwdSlots - 1, row + kNormFwdSlots - 1 < r1);
-    if (!a.y) continue;
-    const float2 st = a.norm ? row_stats<kNV>(t, have, a.norm, a.eps, inv_w, sum) : make_float2(0.f, 1.f);
+    in.next();
+    in.load(row + kNormFwdSlots - 1 < r1);
+    if (!y_out) continue;
+    const float2 st = a.norm ? row_stats<kNV>(t, last, a.norm, a.eps, inv_w, sum) : make_float2(0.f, 1.f);
+    const f32x2 r = splat2(st.y), m = splat2(-st.x);
 #pragma unroll
     for (int i = 0; i < kNV; ++i) {
-      if (i >= have) continue;
-      Vec8 y;
+      Pair8 y;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y.v[e] = fmaf((t[i].v[e] - st.x) * st.y, scale[i].v[e], shift[i].v[e]);
-      *reinterpret_cast<uint4*>(a.y + base + 8 * (tid + i * blockDim.x)) = pack8(y);
+      for (int e = 0; e < 4; ++e) y.p[e] = fma_f32x2(mul_f32x2(add_f32x2(t[i].p[e], m), r), scale[i].p[e], shift[i].p[e]);
+      if (i < kNV - 1 || last) *reinterpret_cast<uint4*>(y_out + i * in.vec) = pack_pairs(y);
     }
+    y_out += in.row_bytes;
   }
 }
 
@@ -250,53 +282,57 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_kernel(co
 // A block keeps the three sums of its columns in registers over its rows; at a
 // request's end they go to slot block + request of `part`, which no other (block,
 // request) has.  The request's two vectors lie in shared memory beside the rows ahead,
-// for the registers' sake.
+// for the registers' sake; two blocks of 256 threads then share an SM.
 template <int kNV, int kThreads>
 __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_backward_kernel(const __grid_constant__ NormSegs segs,
                                                                                       const __grid_constant__ NormArgs a) {
-  constexpr int kSlots = norm_bwd_slots(kThreads);
   extern __shared__ __align__(16) uint8_t smem_norm[];
   __shared__ float4 slots[2 * kThreads / 32];
-  const int tid = threadIdx.x, nvec = a.width / 8;
-  const int have = tid < nvec ? min(kNV, (nvec - tid + static_cast<int>(blockDim.x) - 1) / static_cast<int>(blockDim.x)) : 0;
+  const int tid = threadIdx.x;
+  const bool last = (tid + (kNV - 1) * static_cast<int>(blockDim.x)) * 8 < a.width;
   const bool f32 = a.mod_f32 != 0;
   const int r0 = blockIdx.x * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
   const float inv_w = 1.f / static_cast<float>(a.width);
   BlockSum sum{slots, static_cast<int>(blockDim.x >> 5)};
   grid_dependency_wait();
   if (threadIdx.x == 0) grid_launch_dependents();
-  RowsAhead<kNV, 4, kSlots> in{smem_norm, {a.dy ? a.x : nullptr, a.branch, a.dy, a.dx_out}, a.width, have};
+  RowsAhead<kNV, 4, kNormBwdSlots> in;
+  in.init(smem_norm, {a.dy ? a.x : nullptr, a.branch, a.dy, a.dx_out}, a.width, r0, last);
 #pragma unroll
-  for (int i = 0; i < kSlots - 1; ++i) in.load(r0 + i, r0 + i < r1);
+  for (int i = 0; i < kNormBwdSlots - 1; ++i) in.load(r0 + i < r1);
   // [scale or gate][vector][half][thread] float4
-  float4* vecs = reinterpret_cast<float4*>(smem_norm + static_cast<int64_t>(kSlots) * 4 * kNV * blockDim.x * 16) + tid;
+  float4* vecs = reinterpret_cast<float4*>(smem_norm + static_cast<uint32_t>(kNormBwdSlots * 4 * kNV) * 16u * blockDim.x) + tid;
   auto vec = [&](int k, int i, int h) -> float4& { return vecs[((k * kNV + i) * 2 + h) * blockDim.x]; };
-  auto get_vec = [&](int k, int i) -> Vec8 {
+  auto get_vec = [&](int k, int i) -> Pair8 {
     const float4 p = vec(k, i, 0), q = vec(k, i, 1);
-    return Vec8{{p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w}};
+    return Pair8{{make_f32x2(p.x, p.y), make_f32x2(p.z, p.w), make_f32x2(q.x, q.y), make_f32x2(q.z, q.w)}};
   };
-  Vec8 sa[kNV], sb[kNV], sg[kNV];
+  Pair8 sa[kNV], sb[kNV], sg[kNV];
 #pragma unroll
-  for (int i = 0; i < kNV; ++i) sa[i] = sb[i] = sg[i] = fill8(0.f);
-  int seg = segment_of(segs, r0) - 1;
+  for (int i = 0; i < kNV; ++i) sa[i] = sb[i] = sg[i] = pairs_of(fill8(0.f));
+  int seg = segment_of(segs, r0) - 1, end = r0;
+  const int64_t off0 = 2 * (static_cast<int64_t>(r0) * a.width + 8 * tid);
+  uint8_t* dx_out = a.dx ? reinterpret_cast<uint8_t*>(a.dx) + off0 : nullptr;
+  uint8_t* db_out = a.d_branch ? reinterpret_cast<uint8_t*>(a.d_branch) + off0 : nullptr;
+  const int kind = a.dy ? a.norm : kNormNone, post = a.branch ? a.post_norm : kNormNone;
 #pragma unroll 1
   for (int row = r0; row < r1; ++row) {
-    if (row == r0 || row >= segs.cu[seg + 1]) {
-      do ++seg;
-      while (row >= segs.cu[seg + 1]);  // (skips requests without rows)
+    if (row >= end) {
+      do end = segs.cu[++seg + 1];
+      while (row >= end);  // (skips requests without rows)
 #pragma unroll
       for (int i = 0; i < kNV; ++i) {
-        if (i >= have) continue;
-        const int col = 8 * (tid + i * blockDim.x);
-        const Vec8 w = a.weight ? load_param8(a.weight, col, f32) : fill8(1.f);
-        const Vec8 sc = a.scale ? load_param8(a.scale, seg * a.ld_scale + col, f32) : fill8(0.f);
-        const Vec8 g = a.gate ? load_param8(a.gate, seg * a.ld_gate + col, f32) : fill8(1.f);
-        const Vec8 pw = a.post_weight ? load_param8(a.post_weight, col, f32) : fill8(1.f);
         float p[8], q[8];
+        const bool on = i < kNV - 1 || last;
+        const int col = 8 * (tid + i * blockDim.x);
+        const Vec8 w = on && a.weight ? load_param8(a.weight, col, f32) : fill8(1.f);
+        const Vec8 sc = on && a.scale ? load_param8(a.scale, seg * a.ld_scale + col, f32) : fill8(0.f);
+        const Vec8 g = on && a.gate ? load_param8(a.gate, seg * a.ld_gate + col, f32) : fill8(1.f);
+        const Vec8 pw = on && a.post_weight ? load_param8(a.post_weight, col, f32) : fill8(1.f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          p[e] = fmaf(w.v[e], sc.v[e], w.v[e]);
-          q[e] = g.v[e] * pw.v[e];
+          p[e] = on ? fmaf(w.v[e], sc.v[e], w.v[e]) : 0.f;
+          q[e] = on ? g.v[e] * pw.v[e] : 0.f;
         }
         vec(0, i, 0) = make_float4(p[0], p[1], p[2], p[3]);
         vec(0, i, 1) = make_float4(p[4], p[5], p[6], p[7]);
@@ -304,98 +340,101 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_backward_
         vec(1, i, 1) = make_float4(q[4], q[5], q[6], q[7]);
       }
     }
-    in.wait();
-    const int n = row - r0;
-    const int64_t base = static_cast<int64_t>(row) * a.width;
-    Vec8 x[kNV], f[kNV];
+    in.load(row + kNormBwdSlots - 1 < r1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kNormBwdSlots - 1) : "memory");
+    Pair8 x[kNV];
 #pragma unroll
-    for (int i = 0; i < kNV; ++i) {
-      x[i] = in.get(n, 0, i);
-      f[i] = in.get(n, 1, i);
-    }
+    for (int i = 0; i < kNV; ++i) x[i] = in.get(0, i);
     // statistics of both norms in the same exchanges
-    const int kind = a.dy ? a.norm : kNormNone, post = a.branch ? a.post_norm : kNormNone;
     float2 xs = make_float2(0.f, 1.f), fs = make_float2(0.f, 1.f);
-    if (kind == kNormLayer || post == kNormLayer) {
-      float m[2] = {sum_of<kNV>(x), sum_of<kNV>(f)};
-      sum(m);
-      if (kind == kNormLayer) xs.x = m[0] * inv_w;
-      if (post == kNormLayer) fs.x = m[1] * inv_w;
-    }
     if (kind || post) {
-      float q[2] = {centered_squares<kNV>(x, have, xs.x), centered_squares<kNV>(f, have, fs.x)};
+      Pair8 f[kNV];  // (read again where it is used: for the registers' sake)
+#pragma unroll
+      for (int i = 0; i < kNV; ++i) f[i] = in.get(1, i);
+      if (kind == kNormLayer || post == kNormLayer) {
+        float m[2] = {sum_of<kNV>(x), sum_of<kNV>(f)};
+        sum(m);
+        if (kind == kNormLayer) xs.x = m[0] * inv_w;
+        if (post == kNormLayer) fs.x = m[1] * inv_w;
+      }
+      float q[2] = {centered_squares<kNV>(x, xs.x, last), centered_squares<kNV>(f, fs.x, last)};
       sum(q);
       if (kind) xs.y = rsqrtf(q[0] * inv_w + a.eps);
       if (post) fs.y = rsqrtf(q[1] * inv_w + a.eps);
     }
-    float u2[2] = {0.f, 0.f};
+    f32x2 u0 = splat2(0.f), u1 = splat2(0.f);
+    const f32x2 xm = splat2(-xs.x), xr = splat2(xs.y), fm = splat2(-fs.x), fr = splat2(fs.y);
     if (a.dy) {
 #pragma unroll
       for (int i = 0; i < kNV; ++i) {
-        if (i >= have) continue;
-        const Vec8 dy = in.get(n, 2, i), w = get_vec(0, i);
+        const Pair8 dy = in.get(2, i), w = get_vec(0, i);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[i].v[e] = (x[i].v[e] - xs.x) * xs.y;
-          sa[i].v[e] += dy.v[e];
-          sb[i].v[e] = fmaf(dy.v[e], x[i].v[e], sb[i].v[e]);
-          const float u = dy.v[e] * w.v[e];
-          u2[0] += u;
-          u2[1] = fmaf(u, x[i].v[e], u2[1]);
+        for (int e = 0; e < 4; ++e) {
+          x[i].p[e] = mul_f32x2(add_f32x2(x[i].p[e], xm), xr);
+          sa[i].p[e] = add_f32x2(sa[i].p[e], dy.p[e]);
+          sb[i].p[e] = fma_f32x2(dy.p[e], x[i].p[e], sb[i].p[e]);
+          const f32x2 u = mul_f32x2(dy.p[e], w.p[e]);
+          u0 = add_f32x2(u0, u);
+          u1 = fma_f32x2(u, x[i].p[e], u1);
         }
       }
-      if (kind) sum(u2);
     }
-    const float mu = kind == kNormLayer ? u2[0] * inv_w : 0.f, mux = kind ? u2[1] * inv_w : 0.f;
-    float d2[2] = {0.f, 0.f};
-    Vec8 d[kNV];  // dh times post_weight, in the end
+    float u2[2] = {sum2(u0), sum2(u1)};
+    if (kind) sum(u2);
+    const f32x2 mu = splat2(kind == kNormLayer ? -u2[0] * inv_w : 0.f), mux = splat2(kind ? -u2[1] * inv_w : 0.f);
+    f32x2 d0 = splat2(0.f), d1 = splat2(0.f);
+    Pair8 d[kNV];  // dh times post_weight, in the end
 #pragma unroll
     for (int i = 0; i < kNV; ++i) {
-      if (i >= have) continue;
-      const int col = 8 * (tid + i * blockDim.x);
-      d[i] = in.get(n, 3, i);
+      d[i] = in.get(3, i);
       if (a.dy) {
-        const Vec8 dy = in.get(n, 2, i), w = get_vec(0, i);
+        const Pair8 dy = in.get(2, i), w = get_vec(0, i);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[i].v[e] = fmaf(xs.y, fmaf(dy.v[e], w.v[e], -fmaf(x[i].v[e], mux, mu)), d[i].v[e]);
+        for (int e = 0; e < 4; ++e)
+          d[i].p[e] = fma_f32x2(xr, fma_f32x2(dy.p[e], w.p[e], fma_f32x2(x[i].p[e], mux, mu)), d[i].p[e]);
       }
-      if (a.dx) *reinterpret_cast<uint4*>(a.dx + base + col) = pack8(d[i]);
+      if (dx_out && (i < kNV - 1 || last)) *reinterpret_cast<uint4*>(dx_out + i * in.vec) = pack_pairs(d[i]);
       if (!a.branch) continue;
-      const Vec8 g = get_vec(1, i);
+      const Pair8 g = get_vec(1, i), f = in.get(1, i);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        f[i].v[e] = (f[i].v[e] - fs.x) * fs.y;
-        sg[i].v[e] = fmaf(d[i].v[e], f[i].v[e], sg[i].v[e]);
-        d[i].v[e] *= g.v[e];
-        d2[0] += d[i].v[e];
-        d2[1] = fmaf(d[i].v[e], f[i].v[e], d2[1]);
+      for (int e = 0; e < 4; ++e) {
+        const f32x2 fhat = mul_f32x2(add_f32x2(f.p[e], fm), fr);
+        sg[i].p[e] = fma_f32x2(d[i].p[e], fhat, sg[i].p[e]);
+        d[i].p[e] = mul_f32x2(d[i].p[e], g.p[e]);
+        d0 = add_f32x2(d0, d[i].p[e]);
+        d1 = fma_f32x2(d[i].p[e], fhat, d1);
       }
     }
-    in.load(row + kSlots - 1, row + kSlots - 1 < r1);
-    if (a.branch) {
+    if (dx_out) dx_out += in.row_bytes;
+    if (db_out) {
+      float d2[2] = {sum2(d0), sum2(d1)};
       if (post) sum(d2);
-      const float md = post == kNormLayer ? d2[0] * inv_w : 0.f, mdf = post ? d2[1] * inv_w : 0.f;
-      if (a.d_branch) {
-#pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-          if (i >= have) continue;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) d[i].v[e] = fs.y * (d[i].v[e] - fmaf(f[i].v[e], mdf, md));
-          *reinterpret_cast<uint4*>(a.d_branch + base + 8 * (tid + i * blockDim.x)) = pack8(d[i]);
-        }
-      }
-    }
-    if (row + 1 == r1 || row + 1 == segs.cu[seg + 1]) {
-      float* p = a.part + static_cast<int64_t>(blockIdx.x + seg) * 3 * a.width;
+      const f32x2 md = splat2(post == kNormLayer ? -d2[0] * inv_w : 0.f), mdf = splat2(post ? -d2[1] * inv_w : 0.f);
 #pragma unroll
       for (int i = 0; i < kNV; ++i) {
-        if (i >= have) continue;
-        const int col = 8 * (tid + i * blockDim.x);
-        auto put = [&](int k, Vec8& s) {
-          float4* q = reinterpret_cast<float4*>(p + static_cast<int64_t>(k) * a.width + col);
-          q[0] = make_float4(s.v[0], s.v[1], s.v[2], s.v[3]);
-          q[1] = make_float4(s.v[4], s.v[5], s.v[6], s.v[7]);
-          s = fill8(0.f);
+        const Pair8 f = in.get(1, i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          d[i].p[e] = mul_f32x2(fr, add_f32x2(d[i].p[e], fma_f32x2(mul_f32x2(add_f32x2(f.p[e], fm), fr), mdf, md)));
+        if (i < kNV - 1 || last) *reinterpret_cast<uint4*>(db_out + i * in.vec) = pack_pairs(d[i]);
+      }
+      db_out += in.row_bytes;
+    }
+    in.next();
+    if (row + 1 == r1 || row + 1 == end) {
+      float* p = a.part + static_cast<int64_t>(blockIdx.x + seg) * 3 * a.width + 8 * tid;
+#pragma unroll
+      for (int i = 0; i < kNV; ++i) {
+        auto put = [&](int k, Pair8& s) {
+          if (i < kNV - 1 || last) {
+            float4 q[2];
+            split_f32x2(s.p[0], q[0].x, q[0].y), split_f32x2(s.p[1], q[0].z, q[0].w);
+            split_f32x2(s.p[2], q[1].x, q[1].y), split_f32x2(s.p[3], q[1].z, q[1].w);
+            float4* to = reinterpret_cast<float4*>(p + static_cast<int64_t>(k) * a.width + 8 * i * static_cast<int>(blockDim.x));
+            to[0] = q[0];
+            to[1] = q[1];
+          }
+          s = pairs_of(fill8(0.f));
         };
         put(0, sa[i]);
         put(1, sb[i]);
@@ -419,42 +458,64 @@ __device__ __forceinline__ float load_param(const void* p, int64_t i, bool f32) 
 }
 
 // The parameters' gradients from the blocks' sums: blockIdx.y = which sum (A, B,
-// G); 32 columns by 8 groups that take every eighth slot, joined in a fixed order.
-__global__ void __launch_bounds__(256) norm_param_grad_kernel(const __grid_constant__ NormSegs segs, const __grid_constant__ NormSumArgs a) {
-  __shared__ float sums[8][33];
+// G); a lane has two columns, a warp takes every kSumWarps-th slot of a request, and the
+// warps' sums are joined in their order.
+constexpr int kSumWarps = 16;
+__global__ void __launch_bounds__(32 * kSumWarps) norm_param_grad_kernel(const __grid_constant__ NormSegs segs,
+                                                                         const __grid_constant__ NormSumArgs a) {
+  __shared__ float2 sums[kSumWarps][32];
   grid_dependency_wait();
   if (threadIdx.x == 0) grid_launch_dependents();
-  const int lane = threadIdx.x & 31, g = threadIdx.x >> 5, k = blockIdx.y, col = blockIdx.x * 32 + lane;
+  const int lane = threadIdx.x & 31, g = threadIdx.x >> 5, k = blockIdx.y, col = 64 * blockIdx.x + 2 * lane;
   const bool on = col < a.width;
   const bool f32 = a.mod_f32 != 0;
-  float total = 0.f;
+  float2 total = make_float2(0.f, 0.f);
   for (int s = 0; s < segs.n; ++s) {
-    float sum = 0.f;
+    float2 sum = make_float2(0.f, 0.f);
     if (on && segs.cu[s + 1] > segs.cu[s]) {
       const int b0 = segs.cu[s] / a.rows_per_block, b1 = (segs.cu[s + 1] - 1) / a.rows_per_block;
       const float* p = a.part + (static_cast<int64_t>(s) * 3 + k) * a.width + col;
-#pragma unroll 4
-      for (int b = b0 + g; b <= b1; b += 8) sum += p[static_cast<int64_t>(b) * 3 * a.width];
+      int b = b0 + g;
+      for (; b + 3 * kSumWarps <= b1; b += 4 * kSumWarps) {
+        float2 v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float2*>(p + static_cast<int64_t>(b + i * kSumWarps) * 3 * a.width);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum.x += v[i].x, sum.y += v[i].y;
+      }
+      for (; b <= b1; b += kSumWarps) {
+        const float2 v = *reinterpret_cast<const float2*>(p + static_cast<int64_t>(b) * 3 * a.width);
+        sum.x += v.x, sum.y += v.y;
+      }
     }
     sums[g][lane] = sum;
     __syncthreads();
     if (g == 0 && on) {
-      for (int i = 1; i < 8; ++i) sum += sums[i][lane];
-      const int64_t at = static_cast<int64_t>(s) * a.width + col;
-      if (k == 0) {
-        if (a.d_shift) a.d_shift[at] = sum;
-      } else if (k == 1) {
-        if (a.d_scale) a.d_scale[at] = a.weight ? sum * load_param(a.weight, col, f32) : sum;
-        total += (a.scale ? 1.f + load_param(a.scale, s * a.ld_scale + col, f32) : 1.f) * sum;
-      } else {
-        if (a.d_gate) a.d_gate[at] = a.post_weight ? sum * load_param(a.post_weight, col, f32) : sum;
-        total += (a.gate ? load_param(a.gate, s * a.ld_gate + col, f32) : 1.f) * sum;
+      for (int i = 1; i < kSumWarps; ++i) sum.x += sums[i][lane].x, sum.y += sums[i][lane].y;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int c = col + h;
+        const float v = h ? sum.y : sum.x;
+        float& t = h ? total.y : total.x;
+        const int64_t at = static_cast<int64_t>(s) * a.width + c;
+        if (k == 0) {
+          if (a.d_shift) a.d_shift[at] = v;
+        } else if (k == 1) {
+          if (a.d_scale) a.d_scale[at] = a.weight ? v * load_param(a.weight, c, f32) : v;
+          t += (a.scale ? 1.f + load_param(a.scale, s * a.ld_scale + c, f32) : 1.f) * v;
+        } else {
+          if (a.d_gate) a.d_gate[at] = a.post_weight ? v * load_param(a.post_weight, c, f32) : v;
+          t += (a.gate ? load_param(a.gate, s * a.ld_gate + c, f32) : 1.f) * v;
+        }
       }
     }
     __syncthreads();
   }
   float* w = k == 1 ? a.d_weight : k == 2 ? a.d_post_weight : nullptr;
-  if (g == 0 && on && w) w[col] = a.add ? w[col] + total : total;
+  if (g == 0 && on && w) {
+    w[col] = a.add ? w[col] + total.x : total.x;
+    w[col + 1] = a.add ? w[col + 1] + total.y : total.y;
+  }
 }
 
 }  // namespace rc

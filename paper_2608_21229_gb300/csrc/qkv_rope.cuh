@@ -243,23 +243,30 @@ __global__ void __launch_bounds__(kRopeThreads, 2) qkv_rope_backward_kernel(cons
   }
 }
 
-// dw = the sum of the blocks' parts; one block per weight, D threads in each of
-// 1024 / D groups that take every n-th part.
+// dw = the sum of the blocks' parts, kRopeSumCols columns of one weight a block: 1024 /
+// kRopeSumCols groups take every n-th part and are joined in a fixed order.
+constexpr int kRopeSumCols = 8;
 __global__ void __launch_bounds__(1024) rope_weight_grad_kernel(const float* __restrict__ part, int n_parts, int D, float* dwq,
                                                                 float* dwk) {
-  __shared__ float sums[1024];
+  __shared__ float sums[32][kRopeSumCols];
   grid_dependency_wait();
   if (threadIdx.x == 0) grid_launch_dependents();
-  const int t = blockIdx.x, c = threadIdx.x % D, g = threadIdx.x / D, groups = 1024 / D;
+  constexpr int kGroups = 1024 / kRopeSumCols;
+  const int t = blockIdx.y, c = threadIdx.x % kRopeSumCols, g = threadIdx.x / kRopeSumCols, col = blockIdx.x * kRopeSumCols + c;
   float* dw = t == 0 ? dwq : dwk;
   if (!dw) return;
   float s = 0.f;
-  for (int i = g; i < n_parts; i += groups) s += part[(static_cast<int64_t>(i) * 2 + t) * D + c];
-  sums[threadIdx.x] = s;
+#pragma unroll 4
+  for (int i = g; i < n_parts; i += kGroups) s += part[(static_cast<int64_t>(i) * 2 + t) * D + col];
+#pragma unroll
+  for (int o = kRopeSumCols; o < 32; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if ((threadIdx.x & 31) < kRopeSumCols) sums[threadIdx.x >> 5][c] = s;
   __syncthreads();
-  if (g == 0) {
-    for (int k = 1; k < groups; ++k) s += sums[k * D + c];
-    dw[c] = s;
+  if (threadIdx.x < kRopeSumCols) {
+    s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) s += sums[k][c];
+    dw[col] = s;
   }
 }
 

@@ -43,6 +43,40 @@ __device__ __forceinline__ Vec8 load_param8(const void* p, int64_t i, bool f32) 
 // Loads and stores of data that is used once.
 __device__ __forceinline__ uint4 ld_stream(const void* p) { return __ldcs(static_cast<const uint4*>(p)); }
 
+// The same as four pairs, for the two-lane fp32 operations.
+struct Pair8 {
+  f32x2 p[4];
+};
+__device__ __forceinline__ f32x2 splat2(float x) { return make_f32x2(x, x); }
+__device__ __forceinline__ Pair8 unpack_pairs(uint4 r) {
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+  Pair8 o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o.p[i] = make_f32x2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+  return o;
+}
+__device__ __forceinline__ uint4 pack_pairs(const Pair8& a) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float lo, hi;
+    split_f32x2(a.p[i], lo, hi);
+    w[i] = pack_bf16x2(lo, hi);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ Pair8 pairs_of(const Vec8& a) {
+  Pair8 o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o.p[i] = make_f32x2(a.v[2 * i], a.v[2 * i + 1]);
+  return o;
+}
+__device__ __forceinline__ float sum2(f32x2 a) {
+  float lo, hi;
+  split_f32x2(a, lo, hi);
+  return lo + hi;
+}
+
 __device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
