@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "refcache.h"
 #include "clip_grads.cuh"
@@ -155,7 +156,8 @@ rc::NormArgs norm_args(const refcache_gated_norm_t* p, int b, int rows) {
   return a;
 }
 
-// A block's threads for a row of `width`, its vectors per thread and its shared memory.
+// A block's threads for a row of `width` (a power of two, with one vector of the row each
+// up to 2048 columns, two above) and its shared memory.
 struct NormShape {
   int nv, threads, smem;
 };
@@ -163,7 +165,8 @@ NormShape norm_shape(int width, bool backward) {
   const int nvec = width / 8;
   NormShape n{};
   n.nv = nvec <= 256 ? 1 : 2;
-  n.threads = 32 * ceil_div(nvec, 32 * n.nv);
+  n.threads = 32;
+  while (n.threads * n.nv < nvec) n.threads *= 2;
   n.smem = n.nv * n.threads * 16 * (backward ? rc::kNormBwdSlots * 4 + 4 : rc::kNormFwdSlots * 2);
   return n;
 }
@@ -172,6 +175,20 @@ NormShape norm_shape(int width, bool backward) {
 int norm_blocks(int rows, int sms, const NormShape& n) {
   const int per_sm = std::max(1, std::min({512 / n.threads, (227 << 10) / (n.smem + 2048), 16}));
   return std::min(rows, per_sm * sms);
+}
+// f(kNV, kThreads) of the shape, as constants.
+template <typename F>
+cudaError_t with_norm_shape(const NormShape& n, const F& f) {
+  using std::integral_constant;
+  if (n.nv == 2)
+    return n.threads == 256 ? f(integral_constant<int, 2>{}, integral_constant<int, 256>{})
+                            : f(integral_constant<int, 2>{}, integral_constant<int, 512>{});
+  switch (n.threads) {
+    case 32: return f(integral_constant<int, 1>{}, integral_constant<int, 32>{});
+    case 64: return f(integral_constant<int, 1>{}, integral_constant<int, 64>{});
+    case 128: return f(integral_constant<int, 1>{}, integral_constant<int, 128>{});
+    default: return f(integral_constant<int, 1>{}, integral_constant<int, 256>{});
+  }
 }
 template <typename Kernel>
 cudaError_t launch_norm(Kernel kernel, const NormShape& n, int blocks, cudaStream_t s, const rc::NormSegs& segs, const rc::NormArgs& a) {
@@ -339,9 +356,9 @@ int refcache_gated_norm(const refcache_gated_norm_t* p, const void* x, const voi
     a.y = y ? static_cast<uint16_t*>(y) + off : nullptr;
     a.rows_per_block = ceil_div(a.rows, norm_blocks(a.rows, sms, shape));
     const int blocks = ceil_div(a.rows, a.rows_per_block);
-    const cudaError_t e = shape.nv == 1          ? launch_norm(rc::gated_norm_kernel<1, 256>, shape, blocks, s, segs, a)
-                          : shape.threads <= 256 ? launch_norm(rc::gated_norm_kernel<2, 256>, shape, blocks, s, segs, a)
-                                                 : launch_norm(rc::gated_norm_kernel<2, 512>, shape, blocks, s, segs, a);
+    const cudaError_t e = with_norm_shape(shape, [&](auto nv, auto threads) {
+      return launch_norm(rc::gated_norm_kernel<decltype(nv)::value, decltype(threads)::value>, shape, blocks, s, segs, a);
+    });
     if (e != cudaSuccess) return cuda_fail(e, "gated_norm_kernel launch");
   }
   return REFCACHE_OK;
@@ -392,9 +409,9 @@ int refcache_gated_norm_backward(const refcache_gated_norm_t* p, const void* x_o
     if (a.rows > 0) {
       a.rows_per_block = ceil_div(a.rows, std::min(kNormMaxBlocks, norm_blocks(a.rows, sms, shape)));
       const int blocks = ceil_div(a.rows, a.rows_per_block);
-      e = shape.nv == 1          ? launch_norm(rc::gated_norm_backward_kernel<1, 256>, shape, blocks, s, segs, a)
-          : shape.threads <= 256 ? launch_norm(rc::gated_norm_backward_kernel<2, 256>, shape, blocks, s, segs, a)
-                                 : launch_norm(rc::gated_norm_backward_kernel<2, 512>, shape, blocks, s, segs, a);
+      e = with_norm_shape(shape, [&](auto nv, auto threads) {
+        return launch_norm(rc::gated_norm_backward_kernel<decltype(nv)::value, decltype(threads)::value>, shape, blocks, s, segs, a);
+      });
       if (e != cudaSuccess) return cuda_fail(e, "gated_norm_backward_kernel launch");
     }
     if (!d_gate && !d_scale && !d_shift && !d_weight && !d_post_weight) continue;

@@ -60,83 +60,79 @@ __device__ __forceinline__ int segment_of(const NormSegs& s, int row) {
   return lo;
 }
 
-// Sums of up to four values over the block's threads; every thread gets them.  Slots
+// Sums of a few values over the block's threads; every thread gets them.  Slots
 // alternate: two exchanges apart they are free again.
+template <int kWarps>
 struct BlockSum {
-  float4* slots;  // [2][warps]
-  int warps, turn = 0;
+  float4* slots;  // [2][kWarps]
+  int turn = 0;
   template <int N>
   __device__ __forceinline__ void operator()(float (&v)[N]) {
-    static_assert(N <= 4, "one float4 per warp");
+    static_assert(N <= 2, "two of a float4's values");
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-    if (warps == 1) return;
-    float4* s = slots + turn * warps;
-    turn ^= 1;
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = make_float4(v[0], N > 1 ? v[N > 1 ? 1 : 0] : 0.f, N > 2 ? v[N > 2 ? 2 : 0] : 0.f, N > 3 ? v[N > 3 ? 3 : 0] : 0.f);
-    __syncthreads();
+    if constexpr (kWarps > 1) {
+      float4* s = slots + turn;
+      turn ^= kWarps;
+      if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = make_float4(v[0], N > 1 ? v[N - 1] : 0.f, 0.f, 0.f);
+      __syncthreads();
+      // every warp adds up the warps' sums, a lane each
+      const float4 g = s[threadIdx.x & (kWarps - 1)];
+      v[0] = g.x;
+      if (N > 1) v[N - 1] = g.y;
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = 0.f;
-    for (int w = 0; w < warps; ++w) {
-      const float4 g = s[w];
-      v[0] += g.x;
-      if (N > 1) v[N > 1 ? 1 : 0] += g.y;
-      if (N > 2) v[N > 2 ? 2 : 0] += g.z;
-      if (N > 3) v[N > 3 ? 3 : 0] += g.w;
+      for (int o = 1; o < kWarps; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
     }
   }
 };
 
 // The rows ahead of the one that is worked on, kTensors of each, in shared memory:
 // [slot][tensor][vector][thread], 16 bytes each.  A tensor that is not there (null) and
-// a vector past the row's end read as zeros.
-template <int kNV, int kTensors, int kSlots>
+// a vector past the row's end read as zeros.  Thread t has vectors t and t + kThreads of
+// a row; all tensors share one offset into them.
+template <int kNV, int kThreads, int kTensors, int kSlots>
 struct RowsAhead {
+  static constexpr uint32_t kVec = 16u * kThreads, kTensor = kNV * kVec, kSlot = kTensors * kTensor;
   uint8_t* mine;               // this thread's first 16 bytes
-  const uint8_t* src[kTensors];  // this thread's first vector of the next row to load
-  uint32_t vec, row_bytes;     // bytes between vectors (of the row and in shared memory), between rows
   bool last;                   // the kNV-th vector is inside the row
-  int write = 0, read = 0;     // slots
-  __device__ __forceinline__ uint8_t* at(int slot, int tensor, int i) const {
-    return mine + (static_cast<uint32_t>(slot * kTensors + tensor) * kNV + i) * vec;
-  }
-  __device__ __forceinline__ void init(uint8_t* smem, const uint16_t* const (&tensors)[kTensors], int width, int row0, bool last_vector) {
-    vec = 16u * blockDim.x;
-    row_bytes = 2u * static_cast<uint32_t>(width);
+  uint32_t write = 0, read = 0;  // bytes of the slots
+  __device__ __forceinline__ void init(uint8_t* smem, const uint16_t* const (&src)[kTensors], bool last_vector) {
     last = last_vector;
     mine = smem + 16u * threadIdx.x;
 #pragma unroll
-    for (int t = 0; t < kTensors; ++t) {
-      src[t] = tensors[t] ? reinterpret_cast<const uint8_t*>(tensors[t] + static_cast<int64_t>(row0) * width) + 16u * threadIdx.x : nullptr;
+    for (int t = 0; t < kTensors; ++t)
 #pragma unroll
       for (int i = 0; i < kNV; ++i)
-        if (!tensors[t] || (i == kNV - 1 && !last)) {
+        if (!src[t] || (i == kNV - 1 && !last)) {
 #pragma unroll
-          for (int s = 0; s < kSlots; ++s) *reinterpret_cast<uint4*>(at(s, t, i)) = make_uint4(0, 0, 0, 0);
+          for (int s = 0; s < kSlots; ++s) *reinterpret_cast<uint4*>(mine + s * kSlot + t * kTensor + i * kVec) = make_uint4(0, 0, 0, 0);
+        }
+  }
+  // `off`: bytes from the tensors' start to this thread's first vector of the row
+  __device__ __forceinline__ void load(const uint16_t* const (&src)[kTensors], int64_t off, bool on) {
+    if (on) {
+#pragma unroll
+      for (int t = 0; t < kTensors; ++t)
+        if (src[t]) {
+          const uint8_t* from = reinterpret_cast<const uint8_t*>(src[t]) + off;
+          const uint32_t to = smem_u32(mine + write + t * kTensor);
+#pragma unroll
+          for (int i = 0; i < kNV; ++i)
+            if (i < kNV - 1 || last)
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * kVec), "l"(from + i * kVec) : "memory");
         }
     }
-  }
-  __device__ __forceinline__ void load(bool on) {
-#pragma unroll
-    for (int t = 0; t < kTensors; ++t) {
-      if (!src[t]) continue;
-      if (on) {
-#pragma unroll
-        for (int i = 0; i < kNV; ++i)
-          if (i < kNV - 1 || last)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(at(write, t, i))), "l"(src[t] + i * vec) : "memory");
-      }
-      src[t] += row_bytes;
-    }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    write = write + 1 == kSlots ? 0 : write + 1;
+    write = write + kSlot == kSlots * kSlot ? 0u : write + kSlot;
   }
-  // the oldest row that was not read yet
-  __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 2) : "memory"); }
-  __device__ __forceinline__ Pair8 get(int tensor, int i) const { return unpack_pairs(*reinterpret_cast<const uint4*>(at(read, tensor, i))); }
-  __device__ __forceinline__ void next() { read = read + 1 == kSlots ? 0 : read + 1; }
+  __device__ __forceinline__ Pair8 get(int tensor, int i) const {
+    return unpack_pairs(*reinterpret_cast<const uint4*>(mine + read + tensor * kTensor + i * kVec));
+  }
+  __device__ __forceinline__ void next() { read = read + kSlot == kSlots * kSlot ? 0u : read + kSlot; }
 };
 
 // Sums over this thread's columns: of the values, and of the squares of their
@@ -167,8 +163,8 @@ __device__ __forceinline__ float centered_squares(const Pair8 (&t)[kNV], float m
   return total;
 }
 // (mean, 1 / deviation) of a layer norm, (0, 1 / rms) of an RMS norm.
-template <int kNV>
-__device__ __forceinline__ float2 row_stats(const Pair8 (&t)[kNV], bool last, int kind, float eps, float inv_w, BlockSum& sum) {
+template <int kNV, typename Sum>
+__device__ __forceinline__ float2 row_stats(const Pair8 (&t)[kNV], bool last, int kind, float eps, float inv_w, Sum& sum) {
   float mean = 0.f;
   if (kind == kNormLayer) {
     float s[1] = {sum_of<kNV>(t)};
@@ -190,24 +186,25 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_kernel(co
   extern __shared__ __align__(16) uint8_t smem_norm[];
   __shared__ float4 slots[2 * kThreads / 32];
   const int tid = threadIdx.x;
-  const bool last = (tid + (kNV - 1) * static_cast<int>(blockDim.x)) * 8 < a.width;
+  const bool last = (tid + (kNV - 1) * kThreads) * 8 < a.width;
   const bool f32 = a.mod_f32 != 0;
   const int r0 = blockIdx.x * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
   const float inv_w = 1.f / static_cast<float>(a.width);
-  BlockSum sum{slots, static_cast<int>(blockDim.x >> 5)};
+  BlockSum<kThreads / 32> sum{slots};
+  constexpr uint32_t kVec = 16u * kThreads;  // bytes between a thread's vectors
+  const int64_t row_bytes = 2 * static_cast<int64_t>(a.width);
   grid_dependency_wait();
   if (threadIdx.x == 0) grid_launch_dependents();
-  RowsAhead<kNV, 2, kNormFwdSlots> in;
-  in.init(smem_norm, {a.x, a.branch}, a.width, r0, last);
+  const uint16_t* const src[2] = {a.x, a.branch};
+  RowsAhead<kNV, kThreads, 2, kNormFwdSlots> in;
+  in.init(smem_norm, src, last);
+  int64_t off = r0 * row_bytes + 16 * tid;  // of this thread's first vector of the row
 #pragma unroll
-  for (int i = 0; i < kNormFwdSlots - 1; ++i) in.load(r0 + i < r1);
+  for (int i = 0; i < kNormFwdSlots - 1; ++i) in.load(src, off + i * row_bytes, r0 + i < r1);
   Pair8 gate[kNV], scale[kNV], shift[kNV];  // gate (times the branch's weight), weight (1 + scale), shift
   int seg = segment_of(segs, r0) - 1, end = r0;
-  const int64_t off0 = 2 * (static_cast<int64_t>(r0) * a.width + 8 * tid);
-  uint8_t* x_out = a.x_out ? reinterpret_cast<uint8_t*>(a.x_out) + off0 : nullptr;
-  uint8_t* y_out = a.y ? reinterpret_cast<uint8_t*>(a.y) + off0 : nullptr;
 #pragma unroll 1
-  for (int row = r0; row < r1; ++row) {
+  for (int row = r0; row < r1; ++row, off += row_bytes) {
     if (row >= end) {
       do end = segs.cu[++seg + 1];
       while (row >= end);  // (skips requests without rows)
@@ -215,7 +212,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_kernel(co
       for (int i = 0; i < kNV; ++i) {
         gate[i] = scale[i] = shift[i] = pairs_of(fill8(0.f));
         if (i == kNV - 1 && !last) continue;
-        const int col = 8 * (tid + i * blockDim.x);
+        const int col = 8 * (tid + i * kThreads);
         Vec8 g = a.gate ? load_param8(a.gate, seg * a.ld_gate + col, f32) : fill8(1.f);
         const Vec8 pw = a.post_weight ? load_param8(a.post_weight, col, f32) : fill8(1.f);
         const Vec8 w = a.weight ? load_param8(a.weight, col, f32) : fill8(1.f);
@@ -230,7 +227,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_kernel(co
         if (a.shift) shift[i] = pairs_of(load_param8(a.shift, seg * a.ld_shift + col, f32));
       }
     }
-    in.wait();
+    asm volatile("cp.async.wait_group %0;" ::"n"(kNormFwdSlots - 2) : "memory");
     Pair8 t[kNV];
 #pragma unroll
     for (int i = 0; i < kNV; ++i) t[i] = in.get(0, i);
@@ -250,23 +247,21 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_kernel(co
       for (int i = 0; i < kNV; ++i) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) t[i].p[e] = fma_f32x2(gate[i].p[e], h[i].p[e], t[i].p[e]);
-        if (x_out && (i < kNV - 1 || last)) *reinterpret_cast<uint4*>(x_out + i * in.vec) = pack_pairs(t[i]);
+        if (a.x_out && (i < kNV - 1 || last)) *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(a.x_out) + off + i * kVec) = pack_pairs(t[i]);
       }
-      if (x_out) x_out += in.row_bytes;
     }
     in.next();
-    in.load(row + kNormFwdSlots - 1 < r1);
-    if (!y_out) continue;
+    in.load(src, off + (kNormFwdSlots - 1) * row_bytes, row + kNormFwdSlots - 1 < r1);
+    if (!a.y) continue;
     const float2 st = a.norm ? row_stats<kNV>(t, last, a.norm, a.eps, inv_w, sum) : make_float2(0.f, 1.f);
-    const f32x2 r = splat2(st.y), m = splat2(-st.x);
+    const f32x2 r = splat2(st.y), m = splat2(-st.x * st.y);
 #pragma unroll
     for (int i = 0; i < kNV; ++i) {
       Pair8 y;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y.p[e] = fma_f32x2(mul_f32x2(add_f32x2(t[i].p[e], m), r), scale[i].p[e], shift[i].p[e]);
-      if (i < kNV - 1 || last) *reinterpret_cast<uint4*>(y_out + i * in.vec) = pack_pairs(y);
+      for (int e = 0; e < 4; ++e) y.p[e] = fma_f32x2(fma_f32x2(t[i].p[e], r, m), scale[i].p[e], shift[i].p[e]);
+      if (i < kNV - 1 || last) *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(a.y) + off + i * kVec) = pack_pairs(y);
     }
-    y_out += in.row_bytes;
   }
 }
 
@@ -289,20 +284,24 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_backward_
   extern __shared__ __align__(16) uint8_t smem_norm[];
   __shared__ float4 slots[2 * kThreads / 32];
   const int tid = threadIdx.x;
-  const bool last = (tid + (kNV - 1) * static_cast<int>(blockDim.x)) * 8 < a.width;
+  const bool last = (tid + (kNV - 1) * kThreads) * 8 < a.width;
   const bool f32 = a.mod_f32 != 0;
   const int r0 = blockIdx.x * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
   const float inv_w = 1.f / static_cast<float>(a.width);
-  BlockSum sum{slots, static_cast<int>(blockDim.x >> 5)};
+  BlockSum<kThreads / 32> sum{slots};
+  constexpr uint32_t kVec = 16u * kThreads;  // bytes between a thread's vectors
+  const int64_t row_bytes = 2 * static_cast<int64_t>(a.width);
   grid_dependency_wait();
   if (threadIdx.x == 0) grid_launch_dependents();
-  RowsAhead<kNV, 4, kNormBwdSlots> in;
-  in.init(smem_norm, {a.dy ? a.x : nullptr, a.branch, a.dy, a.dx_out}, a.width, r0, last);
+  const uint16_t* const src[4] = {a.dy ? a.x : nullptr, a.branch, a.dy, a.dx_out};
+  RowsAhead<kNV, kThreads, 4, kNormBwdSlots> in;
+  in.init(smem_norm, src, last);
+  int64_t off = r0 * row_bytes + 16 * tid;  // of this thread's first vector of the row
 #pragma unroll
-  for (int i = 0; i < kNormBwdSlots - 1; ++i) in.load(r0 + i < r1);
+  for (int i = 0; i < kNormBwdSlots - 1; ++i) in.load(src, off + i * row_bytes, r0 + i < r1);
   // [scale or gate][vector][half][thread] float4
-  float4* vecs = reinterpret_cast<float4*>(smem_norm + static_cast<uint32_t>(kNormBwdSlots * 4 * kNV) * 16u * blockDim.x) + tid;
-  auto vec = [&](int k, int i, int h) -> float4& { return vecs[((k * kNV + i) * 2 + h) * blockDim.x]; };
+  float4* vecs = reinterpret_cast<float4*>(smem_norm + kNormBwdSlots * in.kSlot) + tid;
+  auto vec = [&](int k, int i, int h) -> float4& { return vecs[((k * kNV + i) * 2 + h) * kThreads]; };
   auto get_vec = [&](int k, int i) -> Pair8 {
     const float4 p = vec(k, i, 0), q = vec(k, i, 1);
     return Pair8{{make_f32x2(p.x, p.y), make_f32x2(p.z, p.w), make_f32x2(q.x, q.y), make_f32x2(q.z, q.w)}};
@@ -311,12 +310,9 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_backward_
 #pragma unroll
   for (int i = 0; i < kNV; ++i) sa[i] = sb[i] = sg[i] = pairs_of(fill8(0.f));
   int seg = segment_of(segs, r0) - 1, end = r0;
-  const int64_t off0 = 2 * (static_cast<int64_t>(r0) * a.width + 8 * tid);
-  uint8_t* dx_out = a.dx ? reinterpret_cast<uint8_t*>(a.dx) + off0 : nullptr;
-  uint8_t* db_out = a.d_branch ? reinterpret_cast<uint8_t*>(a.d_branch) + off0 : nullptr;
   const int kind = a.dy ? a.norm : kNormNone, post = a.branch ? a.post_norm : kNormNone;
 #pragma unroll 1
-  for (int row = r0; row < r1; ++row) {
+  for (int row = r0; row < r1; ++row, off += row_bytes) {
     if (row >= end) {
       do end = segs.cu[++seg + 1];
       while (row >= end);  // (skips requests without rows)
@@ -324,7 +320,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_backward_
       for (int i = 0; i < kNV; ++i) {
         float p[8], q[8];
         const bool on = i < kNV - 1 || last;
-        const int col = 8 * (tid + i * blockDim.x);
+        const int col = 8 * (tid + i * kThreads);
         const Vec8 w = on && a.weight ? load_param8(a.weight, col, f32) : fill8(1.f);
         const Vec8 sc = on && a.scale ? load_param8(a.scale, seg * a.ld_scale + col, f32) : fill8(0.f);
         const Vec8 g = on && a.gate ? load_param8(a.gate, seg * a.ld_gate + col, f32) : fill8(1.f);
@@ -340,7 +336,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_backward_
         vec(1, i, 1) = make_float4(q[4], q[5], q[6], q[7]);
       }
     }
-    in.load(row + kNormBwdSlots - 1 < r1);
+    in.load(src, off + (kNormBwdSlots - 1) * row_bytes, row + kNormBwdSlots - 1 < r1);
     asm volatile("cp.async.wait_group %0;" ::"n"(kNormBwdSlots - 1) : "memory");
     Pair8 x[kNV];
 #pragma unroll
@@ -363,14 +359,14 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_backward_
       if (post) fs.y = rsqrtf(q[1] * inv_w + a.eps);
     }
     f32x2 u0 = splat2(0.f), u1 = splat2(0.f);
-    const f32x2 xm = splat2(-xs.x), xr = splat2(xs.y), fm = splat2(-fs.x), fr = splat2(fs.y);
+    const f32x2 xm = splat2(-xs.x * xs.y), xr = splat2(xs.y), fm = splat2(-fs.x * fs.y), fr = splat2(fs.y);
     if (a.dy) {
 #pragma unroll
       for (int i = 0; i < kNV; ++i) {
         const Pair8 dy = in.get(2, i), w = get_vec(0, i);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          x[i].p[e] = mul_f32x2(add_f32x2(x[i].p[e], xm), xr);
+          x[i].p[e] = fma_f32x2(x[i].p[e], xr, xm);
           sa[i].p[e] = add_f32x2(sa[i].p[e], dy.p[e]);
           sb[i].p[e] = fma_f32x2(dy.p[e], x[i].p[e], sb[i].p[e]);
           const f32x2 u = mul_f32x2(dy.p[e], w.p[e]);
@@ -393,32 +389,28 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_backward_
         for (int e = 0; e < 4; ++e)
           d[i].p[e] = fma_f32x2(xr, fma_f32x2(dy.p[e], w.p[e], fma_f32x2(x[i].p[e], mux, mu)), d[i].p[e]);
       }
-      if (dx_out && (i < kNV - 1 || last)) *reinterpret_cast<uint4*>(dx_out + i * in.vec) = pack_pairs(d[i]);
+      if (a.dx && (i < kNV - 1 || last)) *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(a.dx) + off + i * kVec) = pack_pairs(d[i]);
       if (!a.branch) continue;
       const Pair8 g = get_vec(1, i), f = in.get(1, i);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const f32x2 fhat = mul_f32x2(add_f32x2(f.p[e], fm), fr);
+        const f32x2 fhat = x[i].p[e] = fma_f32x2(f.p[e], fr, fm);  // (in x's place from here on)
         sg[i].p[e] = fma_f32x2(d[i].p[e], fhat, sg[i].p[e]);
         d[i].p[e] = mul_f32x2(d[i].p[e], g.p[e]);
         d0 = add_f32x2(d0, d[i].p[e]);
         d1 = fma_f32x2(d[i].p[e], fhat, d1);
       }
     }
-    if (dx_out) dx_out += in.row_bytes;
-    if (db_out) {
+    if (a.branch && a.d_branch) {
       float d2[2] = {sum2(d0), sum2(d1)};
       if (post) sum(d2);
       const f32x2 md = splat2(post == kNormLayer ? -d2[0] * inv_w : 0.f), mdf = splat2(post ? -d2[1] * inv_w : 0.f);
 #pragma unroll
       for (int i = 0; i < kNV; ++i) {
-        const Pair8 f = in.get(1, i);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          d[i].p[e] = mul_f32x2(fr, add_f32x2(d[i].p[e], fma_f32x2(mul_f32x2(add_f32x2(f.p[e], fm), fr), mdf, md)));
-        if (i < kNV - 1 || last) *reinterpret_cast<uint4*>(db_out + i * in.vec) = pack_pairs(d[i]);
+        for (int e = 0; e < 4; ++e) d[i].p[e] = mul_f32x2(fr, add_f32x2(d[i].p[e], fma_f32x2(x[i].p[e], mdf, md)));
+        if (i < kNV - 1 || last) *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(a.d_branch) + off + i * kVec) = pack_pairs(d[i]);
       }
-      db_out += in.row_bytes;
     }
     in.next();
     if (row + 1 == r1 || row + 1 == end) {
@@ -430,7 +422,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_backward_
             float4 q[2];
             split_f32x2(s.p[0], q[0].x, q[0].y), split_f32x2(s.p[1], q[0].z, q[0].w);
             split_f32x2(s.p[2], q[1].x, q[1].y), split_f32x2(s.p[3], q[1].z, q[1].w);
-            float4* to = reinterpret_cast<float4*>(p + static_cast<int64_t>(k) * a.width + 8 * i * static_cast<int>(blockDim.x));
+            float4* to = reinterpret_cast<float4*>(p + static_cast<int64_t>(k) * a.width + 8 * i * kThreads);
             to[0] = q[0];
             to[1] = q[1];
           }
