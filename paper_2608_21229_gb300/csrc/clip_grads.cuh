@@ -33,15 +33,14 @@ struct ClipPiece {
   bool src32, dst32;
 };
 
-__device__ __forceinline__ ClipPiece clip_piece(const ClipTable& t, int piece) {
-  int lo = 0, hi = t.n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (t.piece0[mid] <= piece)
-      lo = mid;
-    else
-      hi = mid - 1;
-  }
+// The tensor of a piece, from that of a block's piece before it (`lo`, no further than a
+// few tensors away, whichever way the block goes).
+__device__ __forceinline__ int clip_tensor(const ClipTable& t, int piece, int lo) {
+  while (t.piece0[lo + 1] <= piece) ++lo;
+  while (t.piece0[lo] > piece) --lo;
+  return lo;
+}
+__device__ __forceinline__ ClipPiece clip_piece(const ClipTable& t, int piece, int lo) {
   const int64_t at = static_cast<int64_t>(piece - t.piece0[lo]) * kClipPiece;
   ClipPiece p;
   p.src32 = (t.types[lo] & 1) != 0;
@@ -68,8 +67,10 @@ __global__ void __launch_bounds__(kClipThreads) clip_norm_kernel(const __grid_co
   if (threadIdx.x == 0) grid_launch_dependents();
   const int pieces = t.piece0[t.n];
   double total = 0.0;
+  int tensor = 0;
   for (int q = blockIdx.x; q < pieces; q += gridDim.x) {
-    const ClipPiece p = clip_piece(t, q);
+    tensor = clip_tensor(t, q, tensor);
+    const ClipPiece p = clip_piece(t, q, tensor);
     const int size = p.src32 ? 4 : 2, per = 16 / size, head = clip_head(p.src, size, p.n);
     const int nv = (p.n - head) / per;
     const uint4* v = reinterpret_cast<const uint4*>(p.src + head * size);
@@ -125,8 +126,10 @@ __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const __grid_c
   const float coef = ratio < 1.f || isnan(ratio) ? ratio : 1.f;
   if (in_place && coef == 1.f) return;
   const int pieces = t.piece0[t.n];
+  int tensor = max(0, t.n - 1);
   for (int q = pieces - 1 - static_cast<int>(blockIdx.x); q >= 0; q -= static_cast<int>(gridDim.x)) {
-    const ClipPiece p = clip_piece(t, q);
+    tensor = clip_tensor(t, q, tensor);
+    const ClipPiece p = clip_piece(t, q, tensor);
     const int size = p.src32 ? 4 : 2, per = 16 / size, head = clip_head(p.src, size, p.n);
     const int nv = (p.n - head) / per;
     const uint4* v = reinterpret_cast<const uint4*>(p.src + head * size);
