@@ -413,26 +413,23 @@ class RefCache:
         they are None, dk_ref and dv_ref [cached rows, H, D] (``accumulate``: added to what these hold).  ``lse`` is
         the fp32 [live rows, H] that the step wrote."""
         H, D, n = self.seg.num_heads, self.seg.head_dim, self.seg.live_rows
-        ptrs, work = _backward_ptrs(q, k, v, o, lse, d_o, dq, dk, dv, n, H, D, stream)
-        ref = self._ref_ptrs(dk_ref, dv_ref)
+        ptrs, work = _backward_ptrs((q, k, v, o, lse, d_o, dq, dk, dv), n, H, D, stream)
+        ref = (None, None) if dk_ref is None and dv_ref is None else self._ref_ptrs(dk_ref, dv_ref)
         scale = default_scale(D) if scale is None else scale
-        _check(load().step_attention_backward(self.h, layer, *ptrs, *ref, 1 if accumulate else 0, _ptr(work), scale,
+        _check(load().step_attention_backward(self.h, layer, *ptrs, *ref, 1 if accumulate else 0, work.data_ptr(), scale,
                                               _stream(stream)))
 
     def build_backward(self, layer, q, k, v, o, lse, d_o, dq, dk, dv, dk_ref=None, dv_ref=None, scale=None, stream=None):
         """Gradient of ``build``; dk_ref and dv_ref, the cached rows' gradients from ``step_backward``, are added to
         the cached rows' part of dk and dv unless they are None."""
         H, D, n = self.seg.num_heads, self.seg.head_dim, self.seg.static_rows
-        ptrs, work = _backward_ptrs(q, k, v, o, lse, d_o, dq, dk, dv, n, H, D, stream)
-        ref = self._ref_ptrs(dk_ref, dv_ref)
+        ptrs, work = _backward_ptrs((q, k, v, o, lse, d_o, dq, dk, dv), n, H, D, stream)
+        ref = (None, None) if dk_ref is None and dv_ref is None else self._ref_ptrs(dk_ref, dv_ref)
         scale = default_scale(D) if scale is None else scale
-        _check(load().refcache_build_backward(self.h, layer, *ptrs, *ref, _ptr(work), scale, _stream(stream)))
+        _check(load().refcache_build_backward(self.h, layer, *ptrs, *ref, work.data_ptr(), scale, _stream(stream)))
 
     def _ref_ptrs(self, dk_ref, dv_ref):
-        if dk_ref is None and dv_ref is None:
-            return None, None
-        n = sum(s1 - s0 - (0 if self.mask_mode == "beyond_alt" else a)
-                for s0, s1, a in zip(self.seg.cu_static, self.seg.cu_static[1:], self.seg.n_anchor))
+        n = self.seg.static_rows - (0 if self.mask_mode == "beyond_alt" else sum(self.seg.n_anchor))  # cached rows
         return _thd_ptrs((("dk_ref", dk_ref), ("dv_ref", dv_ref)), n, self.seg.num_heads, self.seg.head_dim)
 
 
@@ -454,36 +451,56 @@ def full_attention_noalloc(cu_seqlens, q, k, v, o, lse=None, scale=None, stream=
     _check(load().full_attention_noalloc(len(cu) - 1, H, D, _arr(cu), *ptrs, _ptr(lse), scale, _stream(stream)))
 
 
-def _work(nbytes, like, stream):
-    """A call's workspace from torch's allocator, which hands it on only to work behind this call on its stream."""
+# torch, bfloat16, float32 and int32, once torch is in use (an import statement in a
+# function costs as much as checking a tensor)
+_torch = _bfloat16 = _float32 = _int32 = None
+
+
+def _use_torch():
+    global _torch, _bfloat16, _float32, _int32
     import torch
 
-    work = torch.empty(max(16, nbytes), dtype=torch.uint8, device=like.device)
+    _torch, _bfloat16, _float32, _int32 = torch, torch.bfloat16, torch.float32, torch.int32
+
+
+def _work(nbytes, like, stream):
+    """A call's workspace from torch's allocator, which hands it on only to work behind this call on its stream."""
+    work = _torch.empty(max(16, nbytes), dtype=_torch.uint8, device=like.device)
     if stream is not None:  # allocated for the current stream, used on another
-        s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=like.device)
+        s = stream if hasattr(stream, "cuda_stream") else _torch.cuda.ExternalStream(int(stream), device=like.device)
         work.record_stream(s)
     return work
 
 
-def _backward_ptrs(q, k, v, o, lse, d_o, dq, dk, dv, rows, H, D, stream):
-    import torch
+_BACKWARD = ("q", "k", "v", "o", "lse", "d_o", "dq", "dk", "dv")
 
-    first = _thd_ptrs((("q", q), ("k", k), ("v", v), ("o", o)), rows, H, D)
+
+def _backward_ptrs(tensors, rows, H, D, stream):
+    """The device pointers of a gradient call's tensors, in their order, and its workspace."""
+    if _torch is None:
+        _use_torch()
+    shape, lse = (rows, H, D), tensors[4]
     if lse is None:
         raise ValueError("lse is required")
-    if lse.dtype != torch.float32 or tuple(lse.shape) != (rows, H):
+    if lse.dtype is not _float32 or lse.shape != (rows, H):
         raise ValueError(f"lse: expected float32 [{rows}, {H}], got {lse.dtype} {tuple(lse.shape)}")
-    rest = _thd_ptrs((("d_o", d_o), ("dq", dq), ("dk", dk), ("dv", dv)), rows, H, D)
-    return [*first, _ptr(lse), *rest], _work(load().refcache_backward_bytes(rows, H), q, stream)
+    ptrs = []
+    for t in tensors:
+        if t is not lse and (t is None or t.dtype is not _bfloat16 or t.shape != shape):
+            _check_thd(_BACKWARD[len(ptrs)], t, rows, H, D)
+        if not t.is_cuda or not t.is_contiguous():
+            _ptr(t)
+        ptrs.append(t.data_ptr())
+    return ptrs, _work(load().refcache_backward_bytes(rows, H), lse, stream)
 
 
 def full_attention_backward(cu_seqlens, q, k, v, o, lse, d_o, dq, dk, dv, scale=None, stream=None):
     """Gradient of ``full_attention`` (of either allocation variant)."""
     _, H, D = q.shape
     cu = list(cu_seqlens)
-    ptrs, work = _backward_ptrs(q, k, v, o, lse, d_o, dq, dk, dv, cu[-1], H, D, stream)
+    ptrs, work = _backward_ptrs((q, k, v, o, lse, d_o, dq, dk, dv), cu[-1], H, D, stream)
     scale = default_scale(D) if scale is None else scale
-    _check(load().full_attention_backward(len(cu) - 1, H, D, _arr(cu), *ptrs, _ptr(work), scale, _stream(stream)))
+    _check(load().full_attention_backward(len(cu) - 1, H, D, _arr(cu), *ptrs, work.data_ptr(), scale, _stream(stream)))
 
 
 class Rope:
@@ -496,139 +513,152 @@ class Rope:
         self.c = _Rope()
         _check(load().refcache_rope_init(ctypes.byref(self.c), self.head_dim, len(self.axes), _arr(self.axes), self.theta,
                                          ROPE_PAIRS[pairs]))
+        self._ref = ctypes.byref(self.c)
 
 
 _NOTHING = 16  # the address of a tensor without elements, which torch gives as NULL; nothing is read or written there
 
 
-def _head_rows(name, t, rows, H, D):
-    """(pointer, elements between rows) of [rows, H, D] bf16 whose rows are contiguous."""
-    import torch
+def _rows_apart(names, tensors, shape):
+    """For each tensor its pointer and the elements between its rows: [rows, H, D] bf16 whose rows are contiguous."""
+    n, H, D = shape
+    out = []
+    for name, t in zip(names, tensors):
+        if t is None:
+            out += (None, H * D)
+            continue
+        if t.dtype is not _bfloat16 or t.shape != shape:
+            raise ValueError(f"{name}: expected bf16 {list(shape)}, got {t.dtype} {tuple(t.shape)}")
+        if not t.is_cuda:
+            raise ValueError(f"{name}: tensor must live on the GPU")
+        s = t.stride()
+        if s[2] != 1 or (s[1] != D and H > 1):
+            raise ValueError(f"{name}: the heads of a row must be contiguous, got strides {s}")
+        out += (t.data_ptr() or _NOTHING, s[0] if n > 1 else H * D)
+    return out
 
-    if t is None:
-        return None, H * D
-    if t.dtype is not torch.bfloat16 or t.shape != (rows, H, D):
-        raise ValueError(f"{name}: expected bf16 [{rows}, {H}, {D}], got {t.dtype} {tuple(t.shape)}")
-    if not t.is_cuda:
-        raise ValueError(f"{name}: tensor must live on the GPU")
-    s = t.stride()
-    if s[2] != 1 or (H > 1 and s[1] != D):
-        raise ValueError(f"{name}: the heads of a row must be contiguous, got strides {s}")
-    return t.data_ptr() or _NOTHING, s[0] if rows > 1 else H * D
+
+def _rows_packed(names, tensors, shape):
+    out = []
+    for name, t in zip(names, tensors):
+        if t is None:
+            out.append(None)
+            continue
+        if t.dtype is not _bfloat16 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+            _check_thd(name, t, *shape)
+            _ptr(t)
+        out.append(t.data_ptr() or _NOTHING)
+    return out
 
 
 def _param(name, t, n, f32):
     """The pointer of a contiguous [n] parameter in bf16 or fp32, and whether it is fp32 (``f32``: that of one before)."""
-    import torch
-
     if t is None:
         return None, f32
-    if t.dtype not in (torch.bfloat16, torch.float32) or t.shape != (n,):
+    is32 = t.dtype is _float32
+    if not (is32 or t.dtype is _bfloat16) or t.shape != (n,):
         raise ValueError(f"{name}: expected bf16 or float32 [{n}], got {t.dtype} {tuple(t.shape)}")
-    if f32 is not None and f32 != (t.dtype is torch.float32):
+    if f32 is not None and f32 != is32:
         raise ValueError(f"{name}: the parameters of one call have one type")
-    return _ptr(t), t.dtype is torch.float32
+    return _ptr(t), is32
 
 
-def _rope_rows(rope, positions, like, H, out_rows, wq, wk, rows, eps):
-    import torch
-
-    n = like.shape[0]
-    if positions.dtype is not torch.int32 or positions.shape != (n, len(rope.axes)):
+def _rope_rows(rope, positions, shape, out_rows, wq, wk, rows, eps):
+    n, H, _ = shape
+    if positions.dtype is not _int32 or positions.shape != (n, len(rope.axes)):
         raise ValueError(f"positions: expected int32 [{n}, {len(rope.axes)}], got {positions.dtype} {tuple(positions.shape)}")
-    if rows is not None and (rows.dtype is not torch.int32 or rows.shape != (n,)):
+    if rows is not None and (rows.dtype is not _int32 or rows.shape != (n,)):
         raise ValueError(f"rows: expected int32 [{n}], got {rows.dtype} {tuple(rows.shape)}")
     pq, f32 = _param("weight_q", wq, rope.head_dim, None)
     pk, f32 = _param("weight_k", wk, rope.head_dim, f32)
     return _RopeRows(n, out_rows, H, 1 if f32 else 0, _ptr(positions), _ptr(rows), pq, pk, eps)
 
 
-def _same_rows(named):
-    """The [rows, H, D] of the tensors that are there."""
-    for _, t in named:
-        if t is not None:
-            if t.dim() != 3:
-                raise ValueError(f"expected [rows, heads, dim], got {tuple(t.shape)}")
-            return tuple(t.shape)
-    return None
+def _shape_of(what, a, b, c):
+    """The [rows, H, D] of the first of three tensors that is there."""
+    t = a if a is not None else b if b is not None else c
+    if t is None:
+        raise ValueError(f"{what}: none of the three tensors is there")
+    if t.dim() != 3:
+        raise ValueError(f"{what}: expected [rows, heads, dim], got {tuple(t.shape)}")
+    return t.shape
 
 
 def qkv_rope(rope, positions, q, k, v, q_out, k_out, v_out, weight_q=None, weight_k=None, rows=None, eps=1e-6, stream=None):
     """From a projection's q, k and v ([rows, H, D] bf16, rows may lie apart, as those of a fused projection do) to the
     attention's ([out rows, H, D], packed): RMS norm of each head of q and k (with a weight), rotary positions, row i
     moved to row ``rows[i]``.  q, k or v may be None together with its output."""
-    shape, out = _same_rows((("q", q), ("k", k), ("v", v))), _same_rows((("q_out", q_out), ("k_out", k_out), ("v_out", v_out)))
-    if shape is None or out is None:
-        raise ValueError("qkv_rope needs one of q, k and v with its output")
-    n, H, D = shape
-    r = _rope_rows(rope, positions, next(t for t in (q, k, v) if t is not None), H, out[0], weight_q, weight_k, rows, eps)
-    src = [x for name, t in (("q", q), ("k", k), ("v", v)) for x in _head_rows(name, t, n, H, rope.head_dim)]
-    dst = [None if t is None else _thd_ptrs(((name, t),), out[0], H, rope.head_dim)[0] or _NOTHING
-           for name, t in (("q_out", q_out), ("k_out", k_out), ("v_out", v_out))]
-    _check(load().refcache_qkv_rope(ctypes.byref(rope.c), ctypes.byref(r), *src, *dst, _stream(stream)))
+    if _torch is None:
+        _use_torch()
+    n, H, _ = _shape_of("qkv_rope", q, k, v)
+    out = _shape_of("qkv_rope's outputs", q_out, k_out, v_out)[0]
+    D = rope.head_dim
+    r = _rope_rows(rope, positions, (n, H, D), out, weight_q, weight_k, rows, eps)
+    src = _rows_apart(("q", "k", "v"), (q, k, v), (n, H, D))
+    dst = _rows_packed(("q_out", "k_out", "v_out"), (q_out, k_out, v_out), (out, H, D))
+    _check(load().refcache_qkv_rope(rope._ref, ctypes.byref(r), *src, *dst, _stream(stream)))
 
 
 def qkv_rope_backward(rope, positions, q, k, dq_out, dk_out, dv_out, dq, dk, dv, weight_q=None, weight_k=None, dweight_q=None,
                       dweight_k=None, rows=None, eps=1e-6, stream=None):
     """Gradient of ``qkv_rope``: from those of its outputs to dq, dk and dv (rows may lie apart) and the weights' (fp32
     [D]).  q and k are its inputs, needed where they were normalised."""
-    import torch
-
-    shape = _same_rows((("dq", dq), ("dk", dk), ("dv", dv)))
-    out = _same_rows((("dq_out", dq_out), ("dk_out", dk_out), ("dv_out", dv_out)))
-    if shape is None or out is None:
-        raise ValueError("qkv_rope_backward needs one of dq, dk and dv with the gradient of its output")
-    n, H, D = shape
-    like = next(t for t in (dq, dk, dv) if t is not None)
-    r = _rope_rows(rope, positions, like, H, out[0], weight_q, weight_k, rows, eps)
-    src = [x for name, t in (("q", q), ("k", k)) for x in _head_rows(name, t, n, H, rope.head_dim)]
-    grad = [None if t is None else _thd_ptrs(((name, t),), out[0], H, rope.head_dim)[0] or _NOTHING
-            for name, t in (("dq_out", dq_out), ("dk_out", dk_out), ("dv_out", dv_out))]
-    dst = [x for name, t in (("dq", dq), ("dk", dk), ("dv", dv)) for x in _head_rows(name, t, n, H, rope.head_dim)]
-    for name, t in (("dweight_q", dweight_q), ("dweight_k", dweight_k)):
-        if t is not None and (t.dtype is not torch.float32 or t.shape != (rope.head_dim,)):
-            raise ValueError(f"{name}: expected float32 [{rope.head_dim}], got {t.dtype} {tuple(t.shape)}")
+    if _torch is None:
+        _use_torch()
+    n, H, _ = _shape_of("qkv_rope_backward", dq, dk, dv)
+    out = _shape_of("qkv_rope_backward's inputs", dq_out, dk_out, dv_out)[0]
+    D = rope.head_dim
+    r = _rope_rows(rope, positions, (n, H, D), out, weight_q, weight_k, rows, eps)
+    src = _rows_apart(("q", "k"), (q, k), (n, H, D))
+    grad = _rows_packed(("dq_out", "dk_out", "dv_out"), (dq_out, dk_out, dv_out), (out, H, D))
+    dst = _rows_apart(("dq", "dk", "dv"), (dq, dk, dv), (n, H, D))
     L = load()
-    work = None
+    dw, work = [], None
+    for name, t in (("dweight_q", dweight_q), ("dweight_k", dweight_k)):
+        if t is not None and (t.dtype is not _float32 or t.shape != (D,)):
+            raise ValueError(f"{name}: expected float32 [{D}], got {t.dtype} {tuple(t.shape)}")
+        dw.append(_ptr(t))
     if weight_q is not None or weight_k is not None:
-        work = _work(L.refcache_qkv_rope_backward_bytes(ctypes.byref(rope.c)), like, stream)
-    _check(L.refcache_qkv_rope_backward(ctypes.byref(rope.c), ctypes.byref(r), *src, *grad, *dst, _ptr(dweight_q), _ptr(dweight_k),
-                                        _ptr(work), _stream(stream)))
+        work = _work(L.refcache_qkv_rope_backward_bytes(rope._ref), positions, stream)
+    _check(L.refcache_qkv_rope_backward(rope._ref, ctypes.byref(r), *src, *grad, *dst, *dw, None if work is None else work.data_ptr(),
+                                        _stream(stream)))
 
 
 def _norm_params(cu_rows, width, gate, scale, shift, weight, post_weight, norm, post_norm, eps):
-    import torch
-
     cu = list(cu_rows)
     batch = len(cu) - 1
-    c = _GatedNorm(batch=batch, width=width, cu_rows=_arr(cu), norm=NORMS[norm], post_norm=NORMS[post_norm], eps=eps)
-    f32 = None
+    shape, f32, ptrs, lds = (batch, width), None, [], []
     for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
         if t is None:
+            ptrs.append(None)
+            lds.append(0)
             continue
-        if t.dtype not in (torch.bfloat16, torch.float32) or t.shape != (batch, width):
-            raise ValueError(f"{name}: expected bf16 or float32 [{batch}, {width}], got {t.dtype} {tuple(t.shape)}")
-        if f32 is not None and f32 != (t.dtype is torch.float32):
+        is32 = t.dtype is _float32
+        if not (is32 or t.dtype is _bfloat16) or t.shape != shape:
+            raise ValueError(f"{name}: expected bf16 or float32 {list(shape)}, got {t.dtype} {tuple(t.shape)}")
+        if f32 is not None and f32 != is32:
             raise ValueError(f"{name}: the parameters of one call have one type")
-        if not t.is_cuda or t.stride(1) != 1:
+        s = t.stride()
+        if not t.is_cuda or s[1] != 1:
             raise ValueError(f"{name}: must live on the GPU, its rows contiguous")
-        f32 = t.dtype is torch.float32
-        setattr(c, name, t.data_ptr())
-        setattr(c, "ld_" + name, t.stride(0) if batch > 1 else width)
-    c.weight, f32 = _param("weight", weight, width, f32)
-    c.post_weight, f32 = _param("post_weight", post_weight, width, f32)
-    c.mod_f32 = 1 if f32 else 0
-    return c
+        f32 = is32
+        ptrs.append(t.data_ptr())
+        lds.append(s[0] if batch > 1 else width)
+    w, f32 = _param("weight", weight, width, f32)
+    pw, f32 = _param("post_weight", post_weight, width, f32)
+    return _GatedNorm(batch, width, _arr(cu), NORMS[norm], NORMS[post_norm], 1 if f32 else 0, eps, *ptrs, *lds, w, pw)
 
 
-def _rows_ptr(name, t, rows, width):
-    import torch
-
-    if t is None:
-        return None
-    if t.dtype is not torch.bfloat16 or t.shape != (rows, width):
-        raise ValueError(f"{name}: expected bf16 [{rows}, {width}], got {t.dtype} {tuple(t.shape)}")
-    return _ptr(t)
+def _row_ptrs(names, tensors, shape):
+    out = []
+    for name, t in zip(names, tensors):
+        if t is None:
+            out.append(None)
+            continue
+        if t.dtype is not _bfloat16 or t.shape != shape:
+            raise ValueError(f"{name}: expected bf16 {list(shape)}, got {t.dtype} {tuple(t.shape)}")
+        out.append(_ptr(t))
+    return out
 
 
 def gated_norm(cu_rows, x, y=None, branch=None, x_out=None, gate=None, scale=None, shift=None, weight=None, post_weight=None,
@@ -636,11 +666,12 @@ def gated_norm(cu_rows, x, y=None, branch=None, x_out=None, gate=None, scale=Non
     """x_out = x + gate * h with h = branch, or its ``post_norm`` times post_weight; y = norm(x_out) * weight *
     (1 + scale) + shift.  x, branch, x_out (may be x) and y: [rows, width] bf16, packed; gate, scale and shift: a row for
     each request of ``cu_rows``, rows may lie apart; norms "layer", "rms" or None."""
-    n, width = x.shape
+    if _torch is None:
+        _use_torch()
+    width = x.shape[1]
     c = _norm_params(cu_rows, width, gate, scale, shift, weight, post_weight, norm, post_norm, eps)
-    n = cu_rows[-1]
-    _check(load().refcache_gated_norm(ctypes.byref(c), _rows_ptr("x", x, n, width), _rows_ptr("branch", branch, n, width),
-                                      _rows_ptr("x_out", x_out, n, width), _rows_ptr("y", y, n, width), _stream(stream)))
+    ptrs = _row_ptrs(("x", "branch", "x_out", "y"), (x, branch, x_out, y), (cu_rows[-1], width))
+    _check(load().refcache_gated_norm(ctypes.byref(c), *ptrs, _stream(stream)))
 
 
 def gated_norm_backward(cu_rows, x_out, dy, dx, branch=None, dx_out=None, d_branch=None, gate=None, scale=None, weight=None,
@@ -649,55 +680,58 @@ def gated_norm_backward(cu_rows, x_out, dy, dx, branch=None, dx_out=None, d_bran
     """Gradient of ``gated_norm``: from dy and dx_out, the gradients of its outputs (either may be None), to dx, d_branch,
     the modulation's (fp32 [requests, width]) and the weights' (fp32 [width]), each unless it is None.  ``x_out`` is the
     call's output (its x where there was no branch)."""
-    import torch
-
-    like = next((t for t in (dy, dx_out, x_out) if t is not None), None)
+    if _torch is None:
+        _use_torch()
+    like = dy if dy is not None else dx_out
     if like is None:
         raise ValueError("gated_norm_backward needs dy or dx_out")
-    width, n = like.shape[1], cu_rows[-1]
+    width = like.shape[1]
     c = _norm_params(cu_rows, width, gate, scale, None, weight, post_weight, norm, post_norm, eps)
-    for name, t, shape in (("d_gate", d_gate, (c.batch, width)), ("d_scale", d_scale, (c.batch, width)),
-                           ("d_shift", d_shift, (c.batch, width)), ("d_weight", d_weight, (width,)),
-                           ("d_post_weight", d_post_weight, (width,))):
-        if t is not None and (t.dtype is not torch.float32 or t.shape != shape):
+    ptrs = _row_ptrs(("x_out", "branch", "dy", "dx_out", "dx", "d_branch"), (x_out, branch, dy, dx_out, dx, d_branch), (cu_rows[-1], width))
+    sums = []
+    for name, t in (("d_gate", d_gate), ("d_scale", d_scale), ("d_shift", d_shift), ("d_weight", d_weight), ("d_post_weight", d_post_weight)):
+        shape = (c.batch, width) if len(sums) < 3 else (width,)
+        if t is not None and (t.dtype is not _float32 or t.shape != shape):
             raise ValueError(f"{name}: expected float32 {list(shape)}, got {t.dtype} {tuple(t.shape)}")
-    L = load()
-    work = _work(L.refcache_gated_norm_backward_bytes(ctypes.byref(c)), like, stream)
-    _check(L.refcache_gated_norm_backward(
-        ctypes.byref(c), _rows_ptr("x_out", x_out, n, width), _rows_ptr("branch", branch, n, width), _rows_ptr("dy", dy, n, width),
-        _rows_ptr("dx_out", dx_out, n, width), _rows_ptr("dx", dx, n, width), _rows_ptr("d_branch", d_branch, n, width), _ptr(d_gate),
-        _ptr(d_scale), _ptr(d_shift), _ptr(d_weight), _ptr(d_post_weight), _ptr(work), _stream(stream)))
+        sums.append(_ptr(t))
+    L, ref = load(), ctypes.byref(c)
+    work = _work(L.refcache_gated_norm_backward_bytes(ref), like, stream)
+    _check(L.refcache_gated_norm_backward(ref, *ptrs, *sums, work.data_ptr(), _stream(stream)))
 
 
 def clip_gradients(grads, max_norm, out=None, norm=None, stream=None):
     """Scales gradients (bf16 or float32 tensors of any shapes) so that their global norm is at most ``max_norm``, in
     place or into the tensors ``out``; returns the norm before (float32, on the GPU; ``norm`` if given).  max_norm
     may be infinite: the norm alone."""
-    import torch
-
+    if _torch is None:
+        _use_torch()
     grads = list(grads)
-    outs = grads if out is None else list(out)
-    if len(outs) != len(grads):
-        raise ValueError(f"{len(grads)} gradients and {len(outs)} outputs")
-    bf16, f32 = torch.bfloat16, torch.float32
     n = len(grads)
-    ptrs, outp, counts, types = (ctypes.c_void_p * n)(), (ctypes.c_void_p * n)(), (ctypes.c_int64 * n)(), (ctypes.c_int32 * n)()
-    for i, (g, o) in enumerate(zip(grads, outs)):
-        gt, ot = g.dtype, o.dtype
-        if (gt is not bf16 and gt is not f32) or (ot is not bf16 and ot is not f32):
-            raise ValueError(f"gradient {i}: expected bf16 or float32, got {gt} to {ot}")
-        if not (g.is_cuda and g.is_contiguous() and o.is_cuda and o.is_contiguous()):
-            raise ValueError(f"gradient {i}: tensors must live on the GPU and be contiguous")
-        m = g.numel()
-        if o is not g and o.numel() != m:
-            raise ValueError(f"gradient {i}: {m} elements and an output of {o.numel()}")
-        ptrs[i], outp[i], counts[i], types[i] = g.data_ptr(), o.data_ptr(), m, (gt is f32) + 2 * (ot is f32)
+    outs = None if out is None else list(out)
+    if outs is not None and len(outs) != n:
+        raise ValueError(f"{n} gradients and {len(outs)} outputs")
+    counts = [g.numel() for g in grads]
+    if outs is not None and [o.numel() for o in outs] != counts:
+        i, o = next((i, o) for i, (m, o) in enumerate(zip(counts, outs)) if o.numel() != m)
+        raise ValueError(f"gradient {i}: {counts[i]} elements and an output of {o.numel()}")
+    for tensors in (grads,) if outs is None else (grads, outs):
+        for i, t in enumerate(tensors):
+            if not (t.is_cuda and t.is_contiguous()):
+                raise ValueError(f"gradient {i}: tensors must live on the GPU and be contiguous")
+    kind = {_bfloat16: 0, _float32: 1}
+    try:
+        types = [kind[g.dtype] for g in grads]
+        types = [3 * t for t in types] if outs is None else [t + 2 * kind[o.dtype] for t, o in zip(types, outs)]
+    except KeyError as e:
+        raise ValueError(f"gradients: expected bf16 or float32, got {e.args[0]}") from None
     if norm is None:
-        norm = torch.empty((), dtype=f32, device=grads[0].device if grads else "cuda")
-    elif norm.dtype is not f32 or norm.numel() != 1:
+        norm = _torch.empty((), dtype=_float32, device=grads[0].device if grads else "cuda")
+    elif norm.dtype is not _float32 or norm.numel() != 1:
         raise ValueError(f"norm: expected one float32, got {norm.dtype} {tuple(norm.shape)}")
     L = load()
     work = _work(L.refcache_clip_gradients_bytes(n), norm, stream)
-    _check(L.refcache_clip_gradients(n, ptrs, None if out is None else outp, counts, types, max_norm, _ptr(norm), _ptr(work),
-                                     _stream(stream)))
+    pointers = ctypes.c_void_p * n
+    _check(L.refcache_clip_gradients(n, pointers(*[g.data_ptr() for g in grads]),
+                                     None if outs is None else pointers(*[o.data_ptr() for o in outs]), (ctypes.c_int64 * n)(*counts),
+                                     (ctypes.c_int32 * n)(*types), max_norm, _ptr(norm), work.data_ptr(), _stream(stream)))
     return norm
