@@ -21,7 +21,9 @@
 // The tensor core's order of work is
 //   S_0 dP_0 | dV_0 S_1 | dK_0 dP_1 | dV_1 S_2 | dK_1 dP_2 | ...
 // so that P_i is found from S_i while dK_i-1 and dP_i run, and dS_i from dP_i while
-// dV_i and S_i+1 run: each has 1024 tensor cycles, with one buffer each.
+// dV_i and S_i+1 run: each has 1024 tensor cycles, with one buffer each.  At head dim 64
+// these are 512, less than the way from S to P to the next S takes, and there is room
+// for two S: S_i+2 follows dV_i.
 // Queries kernel: S [0, 128), dP twice [128, 384), dQ [384, 512); P never leaves
 // the registers, S is free as soon as it is read, and the order is
 //   S_i dP_i dQ_i-1 | S_i+1 dP_i+1 dQ_i | ...
@@ -77,6 +79,7 @@ struct Smem {
   static constexpr int kXSlots = kKeys ? 1 : 2, kYSlots = kXSlots;
   static constexpr uint32_t kXSlot = kKeys ? kOwn : 32768;  // (32 rows x 64 columns a warp are staged in it)
   static constexpr uint32_t kXBytes = kKeys ? 2 * kOwn : kOwn;  // one CTA's bytes of a load: with Y in the keys kernel
+  static constexpr int kSBufs = kKeys && D == 64 ? 2 : 1;       // S in tensor memory
   static constexpr int kSlots = D == 64 ? 4 : 2;                // of each ring of a tile
   static constexpr bool kRApart = !kKeys && D == 128;           // R of S and of dP are loads of their own
   static constexpr uint32_t kR1Bytes = kRApart ? kHalf : 2 * kHalf;
@@ -88,8 +91,8 @@ struct Smem {
   // barriers; those of loads first: X, Y, rows of S, rows of dP, columns
   static constexpr int kXFull = 0, kYFull = kXFull + kXSlots, kR1Full = kYFull + kYSlots, kR2Full = kR1Full + kSlots,
                        kCFull = kR2Full + kSlots, kXEmpty = kCFull + kSlots, kYEmpty = kXEmpty + kXSlots, kR1Empty = kYEmpty + kYSlots,
-                       kR2Empty = kR1Empty + kSlots, kCEmpty = kR2Empty + kSlots, kSDone = kCEmpty + kSlots, kPDone = kSDone + 1,
-                       kSUsed = kPDone + 2, kDsFull = kSUsed + 1, kAccFree = kDsFull + 2, kAccDone = kAccFree + 1,
+                       kR2Empty = kR1Empty + kSlots, kCEmpty = kR2Empty + kSlots, kSDone = kCEmpty + kSlots, kPDone = kSDone + kSBufs,
+                       kSUsed = kPDone + 2, kDsFull = kSUsed + kSBufs, kAccFree = kDsFull + 2, kAccDone = kAccFree + 1,
                        kStatFull = kAccDone + 1, kStatEmpty = kStatFull + kStatSlots, kItemFull = kStatEmpty + kStatSlots,
                        kItemEmpty = kItemFull + kItemSlots, kMmaDone = kItemEmpty + kItemSlots, kNumBars = kMmaDone + 1;
   // warps that read each item from the ring: the leader's MMA warp, and the
@@ -372,7 +375,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
     attn_bwd_keys_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant__ BwdKeys keys, const __grid_constant__ BwdArgs args) {
   using namespace bwd;
   using L = Smem<D, true>;
-  constexpr uint32_t kColS = 0, kColP = 128, kColV = 256, kColK = kColV + D;
+  constexpr int kAhead = L::kSBufs;  // tiles that S is ahead of dV
+  constexpr uint32_t kColS = 0, kColP = 128 * kAhead, kColV = kColP + 128, kColK = kColV + D;
   static_assert(kColK + D <= tc::kTmemCols, "tensor-memory layout");
   extern __shared__ uint8_t smem_raw[];
   Cta<L> c;
@@ -446,8 +450,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
       auto rows = [&](int i) { return rd + static_cast<uint64_t>(i % L::kSlots) * (L::kR1Bytes >> 4); };
       auto rows_ready = [&](int i) { return c.wait_all(L::kR1Full + i % L::kSlots, i / L::kSlots, 37); };
       auto issue_s = [&](int i) {
-        mma_rows<D>(tm + kColS, xd, rows(i));
-        tc2_commit_mc(c.bar(L::kSDone), 3);
+        mma_rows<D>(tm + kColS + 128u * (i % kAhead), xd, rows(i));
+        tc2_commit_mc(c.bar(L::kSDone + i % kAhead), 3);
       };
       // (dP's commit also frees the tile's rows and, with the last tile, the item's own)
       auto issue_dp = [&](int i, bool last) {
@@ -472,18 +476,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
           issue_dp(t, nt == 1);
         }
         __syncwarp();
+        if (kAhead == 2 && nt > 1) {
+          if (!rows_ready(t + 1)) goto mma_done;
+          if (elect_one()) {
+            tc_fence_after();
+            issue_s(t + 1);
+          }
+          __syncwarp();
+        }
 #pragma unroll 1
         for (int j = 0; j < nt; ++j, ++t) {
           const bool next = j + 1 < nt;
           const uint64_t cols = cd + static_cast<uint64_t>(t % L::kSlots) * (L::kCBytes >> 4);
           if (!c.wait_all(L::kCFull + t % L::kSlots, t / L::kSlots, 40)) goto mma_done;
           if (j == 0 && n > 0 && !c.wait_all(L::kAccFree, n - 1, 41)) goto mma_done;
-          if (next && !rows_ready(t + 1)) goto mma_done;
-          if (!c.wait_all(L::kSUsed, t, 42)) goto mma_done;  // P is written
+          const bool s_next = j + kAhead < nt;
+          if (s_next && !rows_ready(t + kAhead)) goto mma_done;
+          if (!c.wait_all(L::kSUsed + t % kAhead, t / kAhead, 42)) goto mma_done;  // P is written
           if (elect_one()) {
             tc_fence_after();
-            mma_cols<D>(tm + kColV, tm + kColS, cols, j > 0 ? 1u : 0u);
-            if (next) issue_s(t + 1);
+            mma_cols<D>(tm + kColV, tm + kColS + 128u * (t % kAhead), cols, j > 0 ? 1u : 0u);
+            if (s_next) issue_s(t + kAhead);
           }
           __syncwarp();
           if (!c.wait_all(L::kDsFull, t, 43)) goto mma_done;
@@ -600,7 +613,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
       for (int i = 0; i < D; i += 8)
         *reinterpret_cast<uint4*>(out + i) = r >= m.v[3] ? *reinterpret_cast<const uint4*>(add + from + i) : make_uint4(0, 0, 0, 0);
     };
-    const uint32_t t_s = c.tmem + lanes + kColS + 64u * half;
     int t = 0, n = 0;  // tiles, and items with tiles, so far
 #pragma unroll 1
     for (int k = 0;; ++k) {
@@ -617,8 +629,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
       for (int j = 0; j < m.nt; ++j, ++t) {
         const int s = t % kStatSlots;
         const uint32_t stat = c.base + L::kStat + 1024u * s + 256u * half;
+        const uint32_t t_s = c.tmem + lanes + kColS + 128u * (t % kAhead) + 64u * half;
         float p[64];
-        if (!c.wait_all(L::kStatFull + s, t / kStatSlots, 44) || !c.wait_all(L::kSDone, t, 45)) goto scores_done;
+        if (!c.wait_all(L::kStatFull + s, t / kStatSlots, 44) || !c.wait_all(L::kSDone + t % kAhead, t / kAhead, 45)) goto scores_done;
         tc_fence_after();
         load64(t_s, p);
 #pragma unroll
@@ -637,7 +650,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
           }
           tmem_st16(t_s + 16u * h, pk);
         }
-        arrive(L::kSUsed);
+        arrive(L::kSUsed + t % kAhead);
         if (!c.wait_all(L::kPDone, t, 46)) goto scores_done;
         tc_fence_after();
         {
