@@ -92,7 +92,7 @@ struct Smem {
   static constexpr int kXFull = 0, kYFull = kXFull + kXSlots, kR1Full = kYFull + kYSlots, kR2Full = kR1Full + kSlots,
                        kCFull = kR2Full + kSlots, kXEmpty = kCFull + kSlots, kYEmpty = kXEmpty + kXSlots, kR1Empty = kYEmpty + kYSlots,
                        kR2Empty = kR1Empty + kSlots, kCEmpty = kR2Empty + kSlots, kSDone = kCEmpty + kSlots, kPDone = kSDone + kSBufs,
-                       kSUsed = kPDone + 2, kDsFull = kSUsed + kSBufs, kAccFree = kDsFull + 2, kAccDone = kAccFree + 1,
+                       kSHalf = kPDone + 2, kSUsed = kSHalf + 1, kDsFull = kSUsed + kSBufs, kAccFree = kDsFull + 2, kAccDone = kAccFree + 1,
                        kStatFull = kAccDone + 1, kStatEmpty = kStatFull + kStatSlots, kItemFull = kStatEmpty + kStatSlots,
                        kItemEmpty = kItemFull + kItemSlots, kMmaDone = kItemEmpty + kItemSlots, kNumBars = kMmaDone + 1;
   // warps that read each item from the ring: the leader's MMA warp, and the
@@ -120,14 +120,15 @@ __device__ __forceinline__ void mma_rows(uint32_t d_tmem, uint64_t a, uint64_t b
                kk > 0 ? 1u : 0u);
 }
 // Weights (128 of them a row, bf16 in tensor memory, the second 64 at +64 columns)
-// by a tile's columns.
-template <int D>
+// by a tile's columns.  Part 0, 1: the first or second 32 of each 64 weights; -1: all.
+template <int D, int kPart>
 __device__ __forceinline__ void mma_cols(uint32_t d_tmem, uint32_t w_tmem, uint64_t b, uint32_t accumulate) {
   constexpr uint32_t kIdesc = idesc_bf16_f32(256, D, true);
 #pragma unroll
   for (int kk = 0; kk < kTile / 16; ++kk)
-    tc2_mma_ts(d_tmem, w_tmem + static_cast<uint32_t>((kk >> 2) * 64 + (kk & 3) * 8), b + ((16u * D * kk) >> 4), kIdesc,
-               kk > 0 ? 1u : accumulate);
+    if (kPart < 0 || ((kk >> 1) & 1) == kPart)
+      tc2_mma_ts(d_tmem, w_tmem + static_cast<uint32_t>((kk >> 2) * 64 + (kk & 3) * 8), b + ((16u * D * kk) >> 4), kIdesc,
+                 kk > 0 ? 1u : accumulate);
 }
 template <int D>
 __device__ __forceinline__ uint64_t cols_desc(uint32_t addr) {
@@ -191,6 +192,7 @@ struct Cta {
     return tc::wait_one(bar(i), static_cast<uint32_t>(n) & 1u, ctl, where);
   }
   __device__ __forceinline__ bool wait_all(int i, int n, int where) const { return __all_sync(0xffffffffu, wait(i, n, where)); }
+  __device__ __forceinline__ bool done(int i, int n) const { return mbar_test_wait(bar(i), static_cast<uint32_t>(n) & 1u); }
   // Items reach the warps through a ring in the shared memory of both CTAs, decoded.
   // The leader's item warp (one lane): waits until item k may be chosen, and passes it
   // on; its head is -1 when none is left.
@@ -260,7 +262,7 @@ __device__ __forceinline__ bool enter(Cta<L>& c, uint8_t* smem, const BwdArgs& a
   uint32_t* holder = reinterpret_cast<uint32_t*>(c.ptr + L::kTmemHolder);
   if (threadIdx.x == 0) {
     for (int i = 0; i < L::kNumBars; ++i) {
-      const bool scores = i >= L::kSUsed && i <= L::kAccFree;  // the score warps of both CTAs
+      const bool scores = i >= L::kSHalf && i <= L::kAccFree;  // the score warps of both CTAs
       const bool local = (i >= L::kStatEmpty && i < L::kItemFull) || (L::kXSlots == 2 && i >= L::kXEmpty && i < L::kYEmpty);  // of this CTA
       const bool items = i >= L::kItemEmpty && i < L::kMmaDone;
       mbar_init(c.bar(i), scores ? 2 * kScoreWarps : local ? kScoreWarps : items ? L::kItemTakers : 1);
@@ -492,17 +494,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
           if (j == 0 && n > 0 && !c.wait_all(L::kAccFree, n - 1, 41)) goto mma_done;
           const bool s_next = j + kAhead < nt;
           if (s_next && !rows_ready(t + kAhead)) goto mma_done;
+          const uint32_t t_p = tm + kColS + 128u * (t % kAhead), acc = j > 0 ? 1u : 0u;
+          if (kAhead == 1) {  // the first half of P
+            if (!c.wait_all(L::kSHalf, t, 49)) goto mma_done;
+            if (elect_one()) {
+              tc_fence_after();
+              mma_cols<D, 0>(tm + kColV, t_p, cols, acc);
+            }
+            __syncwarp();
+          }
           if (!c.wait_all(L::kSUsed + t % kAhead, t / kAhead, 42)) goto mma_done;  // P is written
           if (elect_one()) {
             tc_fence_after();
-            mma_cols<D>(tm + kColV, tm + kColS + 128u * (t % kAhead), cols, j > 0 ? 1u : 0u);
+            mma_cols<D, kAhead == 1 ? 1 : -1>(tm + kColV, t_p, cols, acc);
             if (s_next) issue_s(t + kAhead);
           }
           __syncwarp();
           if (!c.wait_all(L::kDsFull, t, 43)) goto mma_done;
           if (elect_one()) {
             tc_fence_after();
-            mma_cols<D>(tm + kColK, tm + kColP, cols + (L::kHalf >> 4), j > 0 ? 1u : 0u);
+            mma_cols<D, -1>(tm + kColK, tm + kColP, cols + (L::kHalf >> 4), j > 0 ? 1u : 0u);
             tc2_commit_mc(c.bar(L::kCEmpty + t % L::kSlots), 3);
             if (next)
               issue_dp(t + 1, j + 2 == nt);
@@ -625,55 +636,74 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
         if (c.lane == 0) c.release(k);
         continue;
       }
+      bool ready = false;  // this tile's S and statistics were seen at the end of the tile before
 #pragma unroll 1
       for (int j = 0; j < m.nt; ++j, ++t) {
         const int s = t % kStatSlots;
         const uint32_t stat = c.base + L::kStat + 1024u * s + 256u * half;
         const uint32_t t_s = c.tmem + lanes + kColS + 128u * (t % kAhead) + 64u * half;
         float p[64];
-        if (!c.wait_all(L::kStatFull + s, t / kStatSlots, 44) || !c.wait_all(L::kSDone + t % kAhead, t / kAhead, 45)) goto scores_done;
+        if (!ready && (!c.wait_all(L::kStatFull + s, t / kStatSlots, 44) || !c.wait_all(L::kSDone + t % kAhead, t / kAhead, 45))) goto scores_done;
         tc_fence_after();
-        load64(t_s, p);
+        {
+          uint32_t r[2][32];
+          tmem_ld32(t_s, r[0]);
+          tmem_wait_ld(r[0]);
+          tmem_ld32(t_s + 32, r[1]);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t pk[16];
+          for (int h = 0; h < 2; ++h) {
+            if (h == 1) tmem_wait_ld(r[1]);
+            uint32_t pk[16];
 #pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            const float4 nl = ld_shared_f4(stat + 128u * h + 16u * q);
-            float* x = p + 32 * h + 4 * q;
-            float e0, e1, e2, e3;
-            split_f32x2(fma_f32x2(make_f32x2(x[0], x[1]), sl2, make_f32x2(nl.x, nl.y)), e0, e1);
-            split_f32x2(fma_f32x2(make_f32x2(x[2], x[3]), sl2, make_f32x2(nl.z, nl.w)), e2, e3);
-            x[0] = ex2_approx(e0), x[1] = ex2_approx(e1), x[2] = ex2_approx(e2), x[3] = ex2_approx(e3);
-            pk[2 * q] = pack_bf16x2(x[0], x[1]);
-            pk[2 * q + 1] = pack_bf16x2(x[2], x[3]);
+            for (int q = 0; q < 8; ++q) {
+              const float4 nl = ld_shared_f4(stat + 128u * h + 16u * q);
+              const uint32_t* x = r[h] + 4 * q;
+              float* y = p + 32 * h + 4 * q;
+              float e0, e1, e2, e3;
+              split_f32x2(fma_f32x2(make_f32x2(__uint_as_float(x[0]), __uint_as_float(x[1])), sl2, make_f32x2(nl.x, nl.y)), e0, e1);
+              split_f32x2(fma_f32x2(make_f32x2(__uint_as_float(x[2]), __uint_as_float(x[3])), sl2, make_f32x2(nl.z, nl.w)), e2, e3);
+              y[0] = ex2_approx(e0), y[1] = ex2_approx(e1), y[2] = ex2_approx(e2), y[3] = ex2_approx(e3);
+              pk[2 * q] = pack_bf16x2(y[0], y[1]);
+              pk[2 * q + 1] = pack_bf16x2(y[2], y[3]);
+            }
+            // (over the first 32 columns read, which both halves fit in)
+            tmem_st16(t_s + 16u * h, pk);
+            if (kAhead == 1 && h == 0) arrive(L::kSHalf);
           }
-          tmem_st16(t_s + 16u * h, pk);
         }
         arrive(L::kSUsed + t % kAhead);
         if (!c.wait_all(L::kPDone, t, 46)) goto scores_done;
         tc_fence_after();
         {
-          float d[64];
-          load64(t_p, d);
+          uint32_t r[2][32];
+          tmem_ld32(t_p, r[0]);
+          tmem_wait_ld(r[0]);
+          tmem_ld32(t_p + 32, r[1]);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
+            if (h == 1) tmem_wait_ld(r[1]);
             uint32_t pk[16];
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
               const float4 ndl = ld_shared_f4(stat + 512u + 128u * h + 16u * q);
-              const int i = 32 * h + 4 * q;
+              const uint32_t* d = r[h] + 4 * q;
+              const float* y = p + 32 * h + 4 * q;
               float e0, e1, e2, e3;
-              split_f32x2(mul_f32x2(make_f32x2(p[i], p[i + 1]), add_f32x2(make_f32x2(d[i], d[i + 1]), make_f32x2(ndl.x, ndl.y))), e0, e1);
-              split_f32x2(mul_f32x2(make_f32x2(p[i + 2], p[i + 3]), add_f32x2(make_f32x2(d[i + 2], d[i + 3]), make_f32x2(ndl.z, ndl.w))), e2,
-                          e3);
+              split_f32x2(mul_f32x2(make_f32x2(y[0], y[1]),
+                                    add_f32x2(make_f32x2(__uint_as_float(d[0]), __uint_as_float(d[1])), make_f32x2(ndl.x, ndl.y))), e0, e1);
+              split_f32x2(mul_f32x2(make_f32x2(y[2], y[3]),
+                                    add_f32x2(make_f32x2(__uint_as_float(d[2]), __uint_as_float(d[3])), make_f32x2(ndl.z, ndl.w))), e2, e3);
               pk[2 * q] = pack_bf16x2(e0, e1);
               pk[2 * q + 1] = pack_bf16x2(e2, e3);
             }
             tmem_st16(t_p + 16u * h, pk);
           }
         }
+        // a look at the next tile, whose latency passes beside the stores
+        const int u = t + 1;
+        const bool next = j + 1 < m.nt && c.done(L::kStatFull + u % kStatSlots, u / kStatSlots) && c.done(L::kSDone + u % kAhead, u / kAhead);
         arrive(L::kDsFull);
+        ready = __all_sync(0xffffffffu, next);
         if (c.lane == 0) mbar_arrive(c.bar(L::kStatEmpty + s));
       }
       if (!write_out(m, n)) goto scores_done;
@@ -849,7 +879,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
           if (!c.wait_all(L::kDsFull + u, i >> 1, 63)) goto mma_done;
           if (elect_one()) {
             tc_fence_after();
-            mma_cols<D>(tm + kColQ, tm + kColP + 128u * u, cd + static_cast<uint64_t>(r) * (L::kCBytes >> 4), pj > 0 ? 1u : 0u);
+            mma_cols<D, -1>(tm + kColQ, tm + kColP + 128u * u, cd + static_cast<uint64_t>(r) * (L::kCBytes >> 4), pj > 0 ? 1u : 0u);
             tc2_commit_mc(c.bar(L::kCEmpty + r), 3);
             if (pj + 1 == pnt) tc2_commit_mc(c.bar(L::kAccDone), 3);
           }
