@@ -446,7 +446,7 @@ REFCACHE_API int refcache_qkv_rope_backward(const refcache_rope_t* rope, const r
  *   x_out = x + gate * h                            (no branch: x)
  *   y = norm(x_out) * weight * (1 + scale) + shift  (before x_out is rounded)
  * gate, scale and shift are rows of the request (ld elements between requests'
- * rows, a multiple of 8); gate NULL is 1, scale and shift NULL are 0, weights NULL
+ * rows, a multiple of 8; 0: one row for all requests); gate NULL is 1, scale and shift NULL are 0, weights NULL
  * are 1.  Layer norm: (x - mean) / sqrt(var + eps); RMS norm: x / sqrt(mean(x^2) +
  * eps).  Statistics and arithmetic in fp32.
  */

@@ -117,7 +117,7 @@ int check_norm(const refcache_gated_norm_t* p) {
   for (int i = 0; i < 5; ++i) {
     int rc = check_optional(tensors[i], names[i]);
     if (rc) return rc;
-    if (i < 3 && tensors[i] && (rc = check_ld(lds[i], p->width, names[i])) != 0) return rc;
+    if (i < 3 && tensors[i] && lds[i] != 0 && (rc = check_ld(lds[i], p->width, names[i])) != 0) return rc;  // (0: one row for all)
   }
   if (p->post_weight && p->post_norm == REFCACHE_NORM_NONE)
     return fail(REFCACHE_ERR_INVALID_ARG, "post_weight without post_norm");

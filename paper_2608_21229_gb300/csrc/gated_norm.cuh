@@ -360,35 +360,29 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_backward_
     }
     f32x2 u0 = splat2(0.f), u1 = splat2(0.f);
     const f32x2 xm = splat2(-xs.x * xs.y), xr = splat2(xs.y), fm = splat2(-fs.x * fs.y), fr = splat2(fs.y);
-    if (a.dy) {
+    Pair8 d[kNV];  // u, then d, then dh times post_weight
 #pragma unroll
-      for (int i = 0; i < kNV; ++i) {
-        const Pair8 dy = in.get(2, i), w = get_vec(0, i);
+    for (int i = 0; i < kNV; ++i) {
+      const Pair8 dy = in.get(2, i), w = get_vec(0, i);  // (zeros without dy)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[i].p[e] = fma_f32x2(x[i].p[e], xr, xm);
-          sa[i].p[e] = add_f32x2(sa[i].p[e], dy.p[e]);
-          sb[i].p[e] = fma_f32x2(dy.p[e], x[i].p[e], sb[i].p[e]);
-          const f32x2 u = mul_f32x2(dy.p[e], w.p[e]);
-          u0 = add_f32x2(u0, u);
-          u1 = fma_f32x2(u, x[i].p[e], u1);
-        }
+      for (int e = 0; e < 4; ++e) {
+        x[i].p[e] = fma_f32x2(x[i].p[e], xr, xm);
+        sa[i].p[e] = add_f32x2(sa[i].p[e], dy.p[e]);
+        sb[i].p[e] = fma_f32x2(dy.p[e], x[i].p[e], sb[i].p[e]);
+        d[i].p[e] = mul_f32x2(dy.p[e], w.p[e]);
+        u0 = add_f32x2(u0, d[i].p[e]);
+        u1 = fma_f32x2(d[i].p[e], x[i].p[e], u1);
       }
     }
     float u2[2] = {sum2(u0), sum2(u1)};
     if (kind) sum(u2);
     const f32x2 mu = splat2(kind == kNormLayer ? -u2[0] * inv_w : 0.f), mux = splat2(kind ? -u2[1] * inv_w : 0.f);
     f32x2 d0 = splat2(0.f), d1 = splat2(0.f);
-    Pair8 d[kNV];  // dh times post_weight, in the end
 #pragma unroll
     for (int i = 0; i < kNV; ++i) {
-      d[i] = in.get(3, i);
-      if (a.dy) {
-        const Pair8 dy = in.get(2, i), w = get_vec(0, i);
+      const Pair8 dxo = in.get(3, i);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          d[i].p[e] = fma_f32x2(xr, fma_f32x2(dy.p[e], w.p[e], fma_f32x2(x[i].p[e], mux, mu)), d[i].p[e]);
-      }
+      for (int e = 0; e < 4; ++e) d[i].p[e] = fma_f32x2(xr, add_f32x2(d[i].p[e], fma_f32x2(x[i].p[e], mux, mu)), dxo.p[e]);
       if (a.dx && (i < kNV - 1 || last)) *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(a.dx) + off + i * kVec) = pack_pairs(d[i]);
       if (!a.branch) continue;
       const Pair8 g = get_vec(1, i), f = in.get(1, i);

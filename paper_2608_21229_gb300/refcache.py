@@ -665,7 +665,7 @@ def gated_norm(cu_rows, x, y=None, branch=None, x_out=None, gate=None, scale=Non
                norm="layer", post_norm=None, eps=1e-6, stream=None):
     """x_out = x + gate * h with h = branch, or its ``post_norm`` times post_weight; y = norm(x_out) * weight *
     (1 + scale) + shift.  x, branch, x_out (may be x) and y: [rows, width] bf16, packed; gate, scale and shift: a row for
-    each request of ``cu_rows``, rows may lie apart; norms "layer", "rms" or None."""
+    each request of ``cu_rows``, rows may lie apart or be one expanded row; norms "layer", "rms" or None."""
     if _torch is None:
         _use_torch()
     width = x.shape[1]

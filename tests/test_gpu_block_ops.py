@@ -266,6 +266,47 @@ def test_gated_norm_backward_of_parts():
     check("d_gate", dg, torch.stack([prod[:30].sum(0), prod[30:].sum(0)]), 30 * 30, rounding=0)
 
 
+def test_one_modulation_for_all_requests():
+    """An expanded row of scale and shift is read as the same rows apart."""
+    c = NormCase([5, 0, 7], 512, "rms", None, BF16, False)
+    one = {k: t[:1] for k, t in c.mods.items()}
+    want, got = torch.empty_like(c.x), torch.empty_like(c.x)
+    rcb.gated_norm(c.cu, c.x, want, branch=c.branch, norm="rms", **{k: t.repeat(3, 1) for k, t in one.items()})
+    rcb.gated_norm(c.cu, c.x, got, branch=c.branch, norm="rms", **{k: t.expand(3, -1) for k, t in one.items()})
+    assert torch.equal(want, got)
+
+
+def test_calls_replay_from_a_cuda_graph():
+    r = RopeCase(70, 3, 128, (16, 56, 56), "halves", BF16, out_rows=80)
+    n = NormCase([30, 12], 4096, "layer", "rms", BF16, True)  # (rows ahead of more shared memory than a launch has by default)
+    g = tensors([300, 5000], (BF16,), 1.0)
+    out = [torch.zeros(80, 3, 128, dtype=BF16, device="cuda") for _ in range(3)]
+    dqkv, dw = torch.zeros_like(r.qkv), [torch.zeros(128, device="cuda") for _ in range(2)]
+    y, dx, dg, clipped = torch.zeros_like(n.x), torch.zeros_like(n.x), torch.zeros(2, 4096, device="cuda"), [torch.zeros_like(t) for t in g]
+    norm = torch.zeros((), device="cuda")
+
+    def calls():
+        q, k, v = r.qkv.unbind(1)
+        rcb.qkv_rope(r.rope, r.pos, q, k, v, *out, *r.w, rows=r.rows)
+        rcb.qkv_rope_backward(r.rope, r.pos, q, k, *r.grads, *dqkv.unbind(1), *r.w, *dw, rows=r.rows)
+        rcb.gated_norm(n.cu, n.x, y, branch=n.branch, **n.mods, **n.w, **n.kw)
+        rcb.gated_norm_backward(n.cu, n.x, n.dy, dx, branch=n.branch, gate=n.mods["gate"], d_gate=dg, **n.w, **n.kw)
+        rcb.clip_gradients(g, 0.5, out=clipped, norm=norm)
+
+    results = [*out, dqkv, *dw, y, dx, dg, *clipped, norm]
+    calls()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in results]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for t in results:
+        t.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(results, want))
+
+
 def test_norm_of_a_large_mean():
     """Mean 1000, deviation 4 (the spacing of bf16 there): squares would cancel, deviations do not."""
     g = gen_of(2)
