@@ -157,6 +157,25 @@ struct RowsOut {
   __device__ __forceinline__ void put(int chunk, uint4 v) const {
     st_shared_v4(stage + 128u * lane + (static_cast<uint32_t>(chunk ^ (lane & 7)) << 4), v);
   }
+  __device__ __forceinline__ uint4 get(int chunk) const {
+    return ld_shared_v4(stage + 128u * lane + (static_cast<uint32_t>(chunk ^ (lane & 7)) << 4));
+  }
+  // rows [from, rows) of the warp come from src + row * stride, zeros elsewhere
+  __device__ __forceinline__ void fetch(const __nv_bfloat16* src, int64_t stride, int from, int rows) const {
+    const int r0 = lane >> 3, ch = lane & 7;
+    uint4 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = 4 * i + r0;
+      v[i] = r >= from && r < rows ? *reinterpret_cast<const uint4*>(src + r * stride + 8 * ch) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = 4 * i + r0;
+      st_shared_v4(stage + 128u * r + (static_cast<uint32_t>(ch ^ (r & 7)) << 4), v[i]);
+    }
+    __syncwarp();
+  }
   // rows [0, rows) of the warp go to dst + row * stride
   __device__ __forceinline__ void flush(__nv_bfloat16* dst, int64_t stride, int rows) const {
     __syncwarp();
@@ -578,17 +597,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
     };
     // dV (warps 0-3) and dK (warps 4-7) of this warp's 32 keys for the n-th item with tiles
     auto write_out = [&](const Item& m, int n) -> bool {
+      const float scale = half ? args.scale : 1.f;
+      const int64_t at = (static_cast<int64_t>(m.row0) + row) * args.row_stride + m.head * D;
+      __nv_bfloat16* out = (half ? (m.v[2] ? args.dkb : args.dka) : (m.v[2] ? args.dvb : args.dva)) + at;
+      const int first = m.v[3] - row, rows = m.rows - row;  // of the warp's rows: from `first` on something is added
+      const bool adds = first < min(32, rows);
+      const __nv_bfloat16* add =
+          (half ? args.add_k : args.add_v) + (static_cast<int64_t>(m.v[4]) + row) * args.row_stride + m.head * D;
+      const RowsOut stage{c.base + L::kStage + 4096u * c.warp, c.lane};
+      // (in whole lines through the stage, before the wait: from the registers, 16 bytes of
+      // each of 32 rows at a time, it took 4000 cycles of an item)
+      if (adds) stage.fetch(add, args.row_stride, first, rows);
       if (!c.wait_all(L::kAccDone, n, 47)) return false;
       tc_fence_after();
-      const float scale = half ? args.scale : 1.f;
-      __nv_bfloat16* out = half ? (m.v[2] ? args.dkb : args.dka) : (m.v[2] ? args.dvb : args.dva);
-      out += (static_cast<int64_t>(m.row0) + row) * args.row_stride + m.head * D;
-      const bool adds = row + c.lane >= m.v[3] && row + c.lane < m.rows;
-      const __nv_bfloat16* from =
-          adds ? (half ? args.add_k : args.add_v) + (static_cast<int64_t>(m.v[4]) + row + c.lane) * args.row_stride + m.head * D : nullptr;
-      const RowsOut rows{c.base + L::kStage + 4096u * c.warp, c.lane};
 #pragma unroll
       for (int cc = 0; cc < D / 64; ++cc) {
+        if (cc > 0 && adds) stage.fetch(add + 64 * cc, args.row_stride, first, rows);
         float v[64];
         load64(c.tmem + lanes + (half ? kColK : kColV) + 64 * cc, v);
         if (cc + 1 == D / 64) {  // all of it is read
@@ -601,14 +625,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
           Vec8 x;
 #pragma unroll
           for (int e = 0; e < 8; ++e) x.v[e] = v[8 * q + e] * scale;
-          if (adds) {
-            const Vec8 y = unpack8(*reinterpret_cast<const uint4*>(from + 64 * cc + 8 * q));
+          if (adds) {  // (zeros where nothing is added)
+            const Vec8 y = unpack8(stage.get(q));
 #pragma unroll
             for (int e = 0; e < 8; ++e) x.v[e] += y.v[e];
           }
-          rows.put(q, pack8(x));
+          stage.put(q, pack8(x));
         }
-        rows.flush(out + 64 * cc, args.row_stride, m.rows - row);
+        stage.flush(out + 64 * cc, args.row_stride, rows);
       }
       return true;
     };
@@ -706,9 +730,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
         ready = __all_sync(0xffffffffu, next);
         if (c.lane == 0) mbar_arrive(c.bar(L::kStatEmpty + s));
       }
+      __syncwarp();
+      if (c.lane == 0) c.release(k);  // (before the stores: a release behind them waits until they are performed, 2000 cycles)
       if (!write_out(m, n)) goto scores_done;
       ++n;
-      if (c.lane == 0) c.release(k);
     }
   scores_done:;
   }
@@ -907,6 +932,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
     // dQ of item k: columns [D / 2 half, D / 2 (half + 1)) of this warp's 32 rows
     auto write_out = [&](int k) -> bool {
       const Item m = c.read(k);
+      __syncwarp();
+      if (c.lane == 0) c.release(k);  // (before the stores, for which a release behind them would wait)
       if (!c.wait_all(L::kAccDone, k, 67)) return false;
       tc_fence_after();
       uint32_t v[D / 2];
@@ -948,10 +975,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
       }
       fence_proxy_async_smem();  // the buffer is free for the loads of the item after the next
       __syncwarp();
-      if (c.lane == 0) {
-        mbar_arrive(c.bar(L::kXEmpty + (k & 1)));
-        c.release(k);
-      }
+      if (c.lane == 0) mbar_arrive(c.bar(L::kXEmpty + (k & 1)));
       return true;
     };
     int t = 0, k = 0;
