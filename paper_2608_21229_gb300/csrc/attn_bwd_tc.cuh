@@ -30,7 +30,7 @@
 //
 // Warps: 0-7 scores (warp w: lanes 32 (w % 4).., columns 64 (w / 4)..; P and dS are
 // written over the columns that the same warp has read), 8 TMA producer, 9 MMAs
-// (leader), 10 statistics of the query tiles (keys kernel), 11 items (leader).
+// (leader), 10 statistics of the query tiles (keys kernel), 11 items.
 //
 // The queries kernel is launched first and the keys kernel as its programmatic
 // dependent: the keys kernel's CTAs take SMs as the queries kernel's leave, which they
@@ -94,10 +94,11 @@ struct Smem {
                        kR2Empty = kR1Empty + kSlots, kCEmpty = kR2Empty + kSlots, kSDone = kCEmpty + kSlots, kPDone = kSDone + kSBufs,
                        kSHalf = kPDone + 2, kSUsed = kSHalf + 1, kDsFull = kSUsed + kSBufs, kAccFree = kDsFull + 2, kAccDone = kAccFree + 1,
                        kStatFull = kAccDone + 1, kStatEmpty = kStatFull + kStatSlots, kItemFull = kStatEmpty + kStatSlots,
-                       kItemEmpty = kItemFull + kItemSlots, kMmaDone = kItemEmpty + kItemSlots, kNumBars = kMmaDone + 1;
-  // warps that read each item from the ring: the leader's MMA warp, and the
-  // producer, score (and statistics) warps of both CTAs
-  static constexpr int kItemTakers = 1 + 2 * (1 + kScoreWarps + (kKeys ? 1 : 0));
+                       kItemEmpty = kItemFull + kItemSlots, kItemIn = kItemEmpty + kItemSlots, kItemPeer = kItemIn + kItemSlots,
+                       kMmaDone = kItemPeer + kItemSlots, kNumBars = kMmaDone + 1;
+  // warps that read each item from a CTA's ring: its producer, score (and statistics)
+  // warps, and the leader's MMA warp
+  static constexpr int kItemTakers = 1 + kScoreWarps + (kKeys ? 1 : 0);
   static constexpr uint32_t kTmemHolder = kBars + 8 * kNumBars;
   static constexpr uint32_t kAbort = kTmemHolder + 4, kPeerAbort = kAbort + 4;
   static constexpr uint32_t kLoadRec = kPeerAbort + 4;  // each CTA's loads: X, Y, rows of S, rows of dP, columns
@@ -212,39 +213,53 @@ struct Cta {
   }
   __device__ __forceinline__ bool wait_all(int i, int n, int where) const { return __all_sync(0xffffffffu, wait(i, n, where)); }
   __device__ __forceinline__ bool done(int i, int n) const { return mbar_test_wait(bar(i), static_cast<uint32_t>(n) & 1u); }
-  // Items reach the warps through a ring in the shared memory of both CTAs, decoded.
-  // The leader's item warp (one lane): waits until item k may be chosen, and passes it
-  // on; its head is -1 when none is left.
+  // Items reach the warps through a ring in the shared memory of both CTAs, decoded:
+  // the leader's item warp (one lane) writes item k to both, the follower's tells its CTA
+  // that it has come, and the leader when its CTA is done with it.  All other warps meet
+  // at barriers of their own CTA: an arrival with release at cluster scope waits for the
+  // stores of the warp to be performed, which after an item's output took 2000 cycles.
+  // Whether item k may be chosen yet:
   __device__ __forceinline__ bool may_choose(int k) const {
-    const int s = k % kItemSlots;
-    return k < kItemSlots || (wait(L::kItemEmpty + s, k / kItemSlots - 1, 81) &&
-                              mbar_try_wait_acquire_cluster(bar(L::kItemEmpty + s), static_cast<uint32_t>(k / kItemSlots - 1) & 1u));
+    const int s = k % kItemSlots, n = k / kItemSlots - 1;
+    return k < kItemSlots || (wait(L::kItemEmpty + s, n, 81) && wait(L::kItemPeer + s, n, 83) &&
+                              mbar_try_wait_acquire_cluster(bar(L::kItemPeer + s), static_cast<uint32_t>(n) & 1u));
   }
+  __device__ __forceinline__ uint32_t slot_of(int k) const { return base + L::kItemRing + 48u * static_cast<uint32_t>(k % kItemSlots); }
   __device__ __forceinline__ void publish(int k, const Item& item) const {
     const int s = k % kItemSlots;
-    const uint32_t at = base + L::kItemRing + 48u * static_cast<uint32_t>(s);
+    const uint32_t at = slot_of(k), to = mapa_shared(at, 1);
     const uint4 x = make_uint4(item.head, item.row0, item.rows, item.nt), y = make_uint4(item.v[0], item.v[1], item.v[2], item.v[3]);
     const uint4 z = make_uint4(item.v[4], 0, 0, 0);
     st_shared_v4(at, x);
     st_shared_v4(at + 16, y);
     st_shared_v4(at + 32, z);
     mbar_arrive(bar(L::kItemFull + s));
-    const uint32_t to = mapa_shared(at, 1);
     st_cluster_v4(to, x);
     st_cluster_v4(to + 16, y);
     st_cluster_v4(to + 32, z);
-    mbar_arrive_release_cluster(mapa_shared(bar(L::kItemFull + s), 1));
+    mbar_arrive_release_cluster(mapa_shared(bar(L::kItemIn + s), 1));
   }
-  // The other roles wait for it (a whole warp, or one lane alone), read it and, when
-  // they are done with it, release it (one lane).
+  __device__ __forceinline__ void relay() const {  // the follower's item warp (one lane)
+    for (int k = 0;; ++k) {
+      const int s = k % kItemSlots, n = k / kItemSlots;
+      if (!wait(L::kItemIn + s, n, 82) || !mbar_try_wait_acquire_cluster(bar(L::kItemIn + s), static_cast<uint32_t>(n) & 1u)) return;
+      const int head = static_cast<int>(ld_shared_v4(slot_of(k)).x);
+      mbar_arrive(bar(L::kItemFull + s));
+      if (head < 0) return;
+      if (k == 0) continue;
+      // (the item before: a warp may be done with it only when it has seen this one)
+      const int before = (k - 1) % kItemSlots;
+      if (!wait(L::kItemEmpty + before, (k - 1) / kItemSlots, 84)) return;
+      mbar_arrive_release_cluster(lbar(L::kItemPeer + before));
+    }
+  }
+  // The other warps wait for item k (all lanes, or one alone), read it, and release it (one lane).
   __device__ __forceinline__ bool await(int k, bool whole_warp) const {
-    const int s = k % kItemSlots;
-    const bool ok = wait(L::kItemFull + s, k / kItemSlots, 82) &&
-                    (leader || mbar_try_wait_acquire_cluster(bar(L::kItemFull + s), static_cast<uint32_t>(k / kItemSlots) & 1u));
+    const bool ok = wait(L::kItemFull + k % kItemSlots, k / kItemSlots, 85);
     return whole_warp ? __all_sync(0xffffffffu, ok) : ok;
   }
   __device__ __forceinline__ Item read(int k) const {
-    const uint32_t at = base + L::kItemRing + 48u * static_cast<uint32_t>(k % kItemSlots);
+    const uint32_t at = slot_of(k);
     const uint4 a = ld_shared_v4(at), b = ld_shared_v4(at + 16), d = ld_shared_v4(at + 32);
     Item t;
     t.head = static_cast<int>(a.x), t.row0 = static_cast<int>(a.y), t.rows = static_cast<int>(a.z), t.nt = static_cast<int>(a.w);
@@ -252,7 +267,7 @@ struct Cta {
     t.v[4] = static_cast<int>(d.x);
     return t;
   }
-  __device__ __forceinline__ void release(int k) const { mbar_arrive_release_cluster(lbar(L::kItemEmpty + k % kItemSlots)); }
+  __device__ __forceinline__ void release(int k) const { mbar_arrive(bar(L::kItemEmpty + k % kItemSlots)); }
 };
 // The item that the leader chooses as its k-th: its cluster's index first, then the
 // next of the list (a counter that the pass over the outputs has set to zero), or
@@ -283,8 +298,8 @@ __device__ __forceinline__ bool enter(Cta<L>& c, uint8_t* smem, const BwdArgs& a
     for (int i = 0; i < L::kNumBars; ++i) {
       const bool scores = i >= L::kSHalf && i <= L::kAccFree;  // the score warps of both CTAs
       const bool local = (i >= L::kStatEmpty && i < L::kItemFull) || (L::kXSlots == 2 && i >= L::kXEmpty && i < L::kYEmpty);  // of this CTA
-      const bool items = i >= L::kItemEmpty && i < L::kMmaDone;
-      mbar_init(c.bar(i), scores ? 2 * kScoreWarps : local ? kScoreWarps : items ? L::kItemTakers : 1);
+      const bool items = i >= L::kItemEmpty && i < L::kItemIn;
+      mbar_init(c.bar(i), scores ? 2 * kScoreWarps : local ? kScoreWarps : items ? L::kItemTakers + (c.leader ? 1 : 0) : 1);
     }
     *abort_flag = 0;
     fence_barrier_init();
@@ -459,6 +474,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
         c.publish(k, t);
         if (t.head < 0) break;
       }
+    } else if (c.lane == 0) {
+      c.relay();
     }
     __syncwarp();
   } else if (c.warp == kMmaWarp) {
@@ -731,7 +748,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
         if (c.lane == 0) mbar_arrive(c.bar(L::kStatEmpty + s));
       }
       __syncwarp();
-      if (c.lane == 0) c.release(k);  // (before the stores: a release behind them waits until they are performed, 2000 cycles)
+      if (c.lane == 0) c.release(k);
       if (!write_out(m, n)) goto scores_done;
       ++n;
     }
@@ -841,6 +858,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
         c.publish(k, t);
         if (t.head < 0) break;
       }
+    } else if (c.lane == 0) {
+      c.relay();
     }
     __syncwarp();
   } else if (c.warp == kMmaWarp) {
@@ -933,7 +952,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
     auto write_out = [&](int k) -> bool {
       const Item m = c.read(k);
       __syncwarp();
-      if (c.lane == 0) c.release(k);  // (before the stores, for which a release behind them would wait)
+      if (c.lane == 0) c.release(k);
       if (!c.wait_all(L::kAccDone, k, 67)) return false;
       tc_fence_after();
       uint32_t v[D / 2];
