@@ -334,9 +334,11 @@ REFCACHE_API int full_attention_noalloc(int batch, int num_heads, int head_dim, 
  *   - work: refcache_backward_bytes(rows, H) bytes of device memory, 16-byte
  *     aligned, overwritten; free again when the call's work on the stream is done.
  *   - Every q, k, v, o, d_o row must hold finite values, as in the forward calls.
- *   - They launch kernels only (two chains of three at most for every 32
- *     requests), so they can be captured in a CUDA graph, after a first call on
- *     the device outside the capture.
+ *   - They launch kernels only (one over the outputs, then two for every 32
+ *     requests) and allocate nothing, so they can be captured in a CUDA graph,
+ *     after a first call on the device outside the capture.  Calls share no
+ *     state but what the caller passes: they may overlap on several streams,
+ *     each with its own work and outputs.
  *   - Outputs must not overlap inputs.
  */
 REFCACHE_API size_t refcache_backward_bytes(int64_t rows, int num_heads);
@@ -446,8 +448,8 @@ REFCACHE_API int refcache_qkv_rope_backward(const refcache_rope_t* rope, const r
  *   x_out = x + gate * h                            (no branch: x)
  *   y = norm(x_out) * weight * (1 + scale) + shift  (before x_out is rounded)
  * gate, scale and shift are rows of the request (ld elements between requests'
- * rows, a multiple of 8; 0: one row for all requests); gate NULL is 1, scale and shift NULL are 0, weights NULL
- * are 1.  Layer norm: (x - mean) / sqrt(var + eps); RMS norm: x / sqrt(mean(x^2) +
+ * rows, a multiple of 8; 0: one row for all requests); gate NULL is 1, scale and
+ * shift NULL are 0, weights NULL are 1.  Layer norm: (x - mean) / sqrt(var + eps); RMS norm: x / sqrt(mean(x^2) +
  * eps).  Statistics and arithmetic in fp32.
  */
 #define REFCACHE_NORM_NONE 0

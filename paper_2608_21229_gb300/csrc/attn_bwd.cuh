@@ -90,7 +90,9 @@ __device__ __forceinline__ BwdItem bwd_item(const List& l, int it, int num_heads
 }
 
 // stats[head][row] = (lse log2 e, delta).  A block takes 256 / (D / 8) rows of four
-// heads; bound by reading dO and O once.
+// heads; bound by reading dO and O once (the statistics lie by head, as the kernels read
+// them, so four heads a block: 128 bytes of lse and of statistics a line).  1280 rows of 24
+// heads of 128 take 6.0 us (15.9 MB), 9431 rows of 16 heads of 64 11 us (39 MB, 3.6 TB/s).
 constexpr int kBwdPrepHeads = 4;
 template <int D>
 __global__ void __launch_bounds__(256) attn_bwd_prep_kernel(const __nv_bfloat16* __restrict__ o, const __nv_bfloat16* __restrict__ d_o,
@@ -132,6 +134,10 @@ __global__ void __launch_bounds__(256) attn_bwd_prep_kernel(const __nv_bfloat16*
 }
 
 // ---------------------------------------------------------------- mma.sync
+// The plain form of the two kernels, kept beside the tcgen05 ones as attn_mma_kernel is
+// beside the forward's: a second implementation that the tests compare.  Bound by the
+// mma.sync pipe and its operands' way through registers: 4608 queries and 25088 keys of 24
+// heads of 128 take 15.2 ms (234 TFLOP/s of the five products, 2.8 ms on tcgen05).
 namespace mm {
 constexpr int kBwdRows = 64;  // rows of a CTA (keys or queries), 16 per warp
 constexpr int kBwdStep = 32;  // rows of the other side per step

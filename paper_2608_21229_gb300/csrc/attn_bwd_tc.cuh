@@ -11,10 +11,10 @@
 // The B operand of a pair's MMA is split along N between its CTAs, so a tile is
 // held twice: rows [64 r, 64 r + 64) of it in CTA r for the products over the
 // head dim, columns [D/2 r, D/2 (r + 1)) of all 128 rows for the products
-// over the rows.  Per tile of 128 x 128 (512 tensor cycles a product at D = 128)
-// the tensor core then reads 192 KB (keys kernel) of shared memory in 2048
-// cycles, and 64 KB arrive: below the 128 bytes a cycle that an SM's shared memory
-// gives, which one CTA alone (M = 128) would need in full.
+// over the rows.  Per tile of 128 queries and 256 keys (512 tensor cycles a
+// product at D = 128) each CTA's tensor core then reads 128 KB of its shared memory in the
+// keys kernel's 2048 cycles, and 64 KB arrive: three quarters of the 128 bytes a cycle that
+// the memory gives.  One CTA alone (M = 128) would need 320 KB in that time.
 //
 // Tensor memory (512 columns), keys kernel: S^T [0, 128), dP^T [128, 256), dV
 // [256, 384), dK [384, 512); P^T and dS^T as bf16 over the scores they come from.
@@ -27,6 +27,7 @@
 // Queries kernel: S [0, 128), dP twice [128, 384), dQ [384, 512); P never leaves
 // the registers, S is free as soon as it is read, and the order is
 //   S_i dP_i dQ_i-1 | S_i+1 dP_i+1 dQ_i | ...
+// across items: an item's first S and dP are issued inside the item before it.
 //
 // Warps: 0-7 scores (warp w: lanes 32 (w % 4).., columns 64 (w / 4)..; P and dS are
 // written over the columns that the same warp has read), 8 TMA producer, 9 MMAs
@@ -37,6 +38,19 @@
 // need not wait for (its CTAs have all passed their own wait for the pass over the
 // outputs by then), only before their own end.  Items are handed out to whichever
 // pair is free.
+//
+// What bounds them: at D = 128 the tensor pipe (with many tiles an item, under the power
+// cap), at D = 64 the score warps.  Measured, each alone on the GPU:
+//                                    keys kernel              queries kernel
+//   cycles per tile, D = 128         2250 (MMAs: 2048)        1690 (1536)
+//   cycles per tile, D = 64          1710 (1024)              1510 (768)
+//   and between items                5700 (its output)        2500
+//   24 heads of 128, 1280 queries    78 us, 1340 TFLOP/s      57 us, 1380 TFLOP/s
+//     and 3328 keys                  of its four products     of its three
+//   4608 queries, 25088 keys         1403 us, 2025            1067 us, 2000
+//   16 heads of 64, three requests   280 us, 1290             240 us, 1130
+//     of 9431 rows together
+// One after the other with the pass over the outputs, call after call: 128, 2830 and 532 us.
 //
 // All waits are bounded as in attn_tc2_kernel, and the teardown is that kernel's:
 // loads complete on the leader's barriers, which it arms for both CTAs' bytes.
@@ -109,9 +123,8 @@ struct Smem {
   static_assert(kUsed <= kMaxDynamic, "shared-memory layout too large");
 };
 
-// The MMAs of one product.  Offsets are in 16-byte units of a descriptor.
-// Rows by rows (over the head dim): A is this CTA's 128 rows, B 64 rows, both in
-// boxes of 64 columns.
+// The MMAs of one product; a descriptor counts in units of 16 bytes.  Products over the
+// head dim: A is this CTA's 128 rows, B 64 rows of the tile, both in boxes of 64 columns.
 template <int D>
 __device__ __forceinline__ void mma_rows(uint32_t d_tmem, uint64_t a, uint64_t b) {
   constexpr uint32_t kIdesc = idesc_bf16_f32(256, kTile, false);
@@ -120,8 +133,8 @@ __device__ __forceinline__ void mma_rows(uint32_t d_tmem, uint64_t a, uint64_t b
     tc2_mma_ss(d_tmem, a + (((kk >> 2) * 16384u + (kk & 3) * 32u) >> 4), b + (((kk >> 2) * 8192u + (kk & 3) * 32u) >> 4), kIdesc,
                kk > 0 ? 1u : 0u);
 }
-// Weights (128 of them a row, bf16 in tensor memory, the second 64 at +64 columns)
-// by a tile's columns.  Part 0, 1: the first or second 32 of each 64 weights; -1: all.
+// Products over a tile's rows: A is P or dS (128 weights a row, bf16 in tensor memory, the
+// second 64 at +64 columns), B the tile's columns.  Part 0, 1: the first or second 32 of each 64 weights; -1: all.
 template <int D, int kPart>
 __device__ __forceinline__ void mma_cols(uint32_t d_tmem, uint32_t w_tmem, uint64_t b, uint32_t accumulate) {
   constexpr uint32_t kIdesc = idesc_bf16_f32(256, D, true);

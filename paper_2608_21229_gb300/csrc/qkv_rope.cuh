@@ -14,7 +14,8 @@
 // position and frequency is off by 2^-24 of the whole angle).  sincospif then
 // needs no range reduction of its own.
 //
-// All of it is bound by memory: every head row is read once and written once.
+// All of it is bound by memory: every head row is read once and written once.  Forward,
+// 20608 rows of q, k and v of 24 heads of 128: 122.5 us call after call, 6.2 TB/s.
 // A row of one head is 16 bytes for each of D / 8 lanes, so that a warp holds
 // 32 / (D / 8) heads of one token at a time, the mean takes log2(D / 8)
 // shuffles, and the angles of a token (4 or 8 for each lane) are found once for
@@ -151,7 +152,10 @@ __global__ void __launch_bounds__(kRopeThreads) qkv_rope_kernel(const __grid_con
 }
 
 // The gradient: a warp walks over tokens row, row + stride, ... so that the sums
-// of dw stay in registers; the block's sum goes to dw_part.
+// of dw stay in registers; the block's sum goes to dw_part.  Bound by the latency of its
+// loads, two warps a scheduler: 4608 rows of 24 heads of 128 take 42.6 us, 5.3 TB/s, and
+// the sums below 4.  (128 registers a thread; at 80, for three blocks an SM, they spill:
+// 67 us.  Loads through a ring in shared memory: 45 us.)
 template <int D, bool kHalves>
 __global__ void __launch_bounds__(kRopeThreads, 2) qkv_rope_backward_kernel(const __grid_constant__ RopeTable table,
                                                                          const __grid_constant__ RopeArgs a) {
