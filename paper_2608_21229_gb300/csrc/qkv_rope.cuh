@@ -175,7 +175,14 @@ __global__ void __launch_bounds__(kRopeThreads, 2) qkv_rope_backward_kernel(cons
   for (int64_t row = static_cast<int64_t>(blockIdx.x) * kRopeTokens + warp; row < a.rows;
        row += static_cast<int64_t>(gridDim.x) * kRopeTokens) {
     const int64_t to = a.row_map ? a.row_map[row] : row;
-    const bool kept = to >= 0 && to < a.out_rows;  // a row that was not kept has no gradient
+    if (to < 0 || to >= a.out_rows) {  // a row that was not kept has no gradient, whatever it holds
+#pragma unroll
+      for (int t = 0; t < 3; ++t)
+        if (a.grad[t])
+          for (int h = h0 + sub; h < h1; h += kPer)
+            *reinterpret_cast<uint4*>(a.dst[t] + row * a.ld_dst[t] + h * D + 8 * l) = make_uint4(0, 0, 0, 0);
+      continue;
+    }
     Turn<D, kHalves> turn;
     if (a.grad[0] || a.grad[1]) turn.set(table, a.positions + row * table.num_axes, l);
 #pragma unroll
@@ -183,7 +190,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) qkv_rope_backward_kernel(cons
       if (!a.grad[t]) continue;
       const bool normed = t < 2 && a.weight[t];
       const uint16_t* src = normed ? a.src[t] + row * a.ld[t] + 8 * l : nullptr;
-      const uint16_t* grad = a.grad[t] + (kept ? to : 0) * static_cast<int64_t>(a.num_heads) * D + 8 * l;
+      const uint16_t* grad = a.grad[t] + to * a.num_heads * D + 8 * l;
       uint16_t* dst = a.dst[t] + row * a.ld_dst[t] + 8 * l;
 #pragma unroll 1
       for (int h = h0; h < h1; h += kUnroll * kPer) {
@@ -191,7 +198,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) qkv_rope_backward_kernel(cons
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
           const int hh = h + u * kPer + sub;
-          graw[u] = kept && hh < h1 ? ld_stream(grad + hh * D) : make_uint4(0, 0, 0, 0);
+          graw[u] = hh < h1 ? ld_stream(grad + hh * D) : make_uint4(0, 0, 0, 0);
           xraw[u] = normed && hh < h1 ? ld_stream(src + hh * D) : make_uint4(0, 0, 0, 0);
         }
 #pragma unroll

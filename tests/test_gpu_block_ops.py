@@ -120,6 +120,23 @@ def test_qkv_rope_backward(case):
     assert torch.equal(dqkv[:, 2].double(), g[2])
 
 
+def test_rows_that_go_nowhere_may_hold_anything():
+    """Padding: infinities and NaN in rows that the forward call drops reach neither their own gradient nor the weights'."""
+    c = RopeCase(70, 3, 64, (8, 28, 28), "halves", BF16, 90, seed=3)
+    lost = ~c.kept
+    assert 0 < lost.sum() < 70
+    dqkv, dw = [], []
+    for fill in (1.0, math.nan, math.inf):
+        x = c.qkv.clone()
+        x[lost] = fill
+        dqkv.append(torch.full_like(x, 7.0))
+        dw.append([torch.empty(64, device="cuda") for _ in range(2)])
+        rcb.qkv_rope_backward(c.rope, c.pos, x[:, 0], x[:, 1], *c.grads, *dqkv[-1].unbind(1), *c.w, *dw[-1], rows=c.rows)
+    assert (dqkv[0][lost] == 0).all() and torch.isfinite(dw[0][0]).all()
+    for i in (1, 2):
+        assert torch.equal(dqkv[i], dqkv[0]) and all(torch.equal(a, b) for a, b in zip(dw[i], dw[0]))
+
+
 def test_rope_angles_at_large_positions():
     """Position 2^24 at frequency 1: an fp32 product of the two would be right here, and off by a radian at the next pair."""
     c = RopeCase(50, 1, 64, (64,), "halves", None, span=2 ** 24)
