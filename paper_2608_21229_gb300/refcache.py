@@ -463,13 +463,20 @@ def _use_torch():
     _torch, _bfloat16, _float32, _int32 = torch, torch.bfloat16, torch.float32, torch.int32
 
 
+def _empty(shape, dtype, device, stream):
+    """Memory for a call on ``stream`` from torch's allocator, of that stream's own blocks: what was freed on the current
+    stream may still be in use there, and what this call leaves goes on only to work behind it."""
+    if stream is None:
+        return _torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, _torch.cuda.Stream):
+        stream = _torch.cuda.ExternalStream(_stream(stream), device=device)
+    with _torch.cuda.stream(stream):
+        return _torch.empty(shape, dtype=dtype, device=device)
+
+
 def _work(nbytes, like, stream):
-    """A call's workspace from torch's allocator, which hands it on only to work behind this call on its stream."""
-    work = _torch.empty(max(16, nbytes), dtype=_torch.uint8, device=like.device)
-    if stream is not None:  # allocated for the current stream, used on another
-        s = stream if hasattr(stream, "cuda_stream") else _torch.cuda.ExternalStream(int(stream), device=like.device)
-        work.record_stream(s)
-    return work
+    """A call's workspace."""
+    return _empty(max(16, nbytes), _torch.uint8, like.device, stream)
 
 
 _BACKWARD = ("q", "k", "v", "o", "lse", "d_o", "dq", "dk", "dv")
@@ -725,7 +732,7 @@ def clip_gradients(grads, max_norm, out=None, norm=None, stream=None):
     except KeyError as e:
         raise ValueError(f"gradients: expected bf16 or float32, got {e.args[0]}") from None
     if norm is None:
-        norm = _torch.empty((), dtype=_float32, device=grads[0].device if grads else "cuda")
+        norm = _empty((), _float32, grads[0].device if grads else _torch.device("cuda", _torch.cuda.current_device()), stream)
     elif norm.dtype is not _float32 or norm.numel() != 1:
         raise ValueError(f"norm: expected one float32, got {norm.dtype} {tuple(norm.shape)}")
     L = load()

@@ -400,6 +400,31 @@ def test_other_stream():
     assert torch.equal(want, got) and torch.equal(a, b)
 
 
+@pytest.mark.parametrize("handle", [False, True])
+def test_memory_for_another_stream_is_that_streams(handle):
+    """A block that the current stream has just freed may still be in use there: a call on another stream must not get it."""
+    side = torch.cuda.Stream()
+    g = torch.ones(1000, device="cuda")
+    rcb.clip_gradients([g], math.inf)
+    torch.cuda.synchronize()
+    on = side.cuda_stream if handle else side
+    for nbytes in (512, 3 << 20):
+        x = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+        freed = x.data_ptr()
+        del x
+        assert rcb._work(nbytes, g, on).data_ptr() != freed
+        x = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+        assert x.data_ptr() == freed  # (it was there to be had)
+        del x
+    x = torch.empty((), device="cuda")
+    freed = x.data_ptr()
+    del x
+    norm = rcb.clip_gradients([g], math.inf, stream=on)
+    assert norm.data_ptr() != freed
+    side.synchronize()
+    assert abs(norm.item() - 1000 ** 0.5) < 1e-4
+
+
 def test_refusals_of_tensors():
     c = RopeCase(6, 2, 64, (8, 28, 28), "halves", BF16)
     q, k, v = c.qkv.unbind(1)
