@@ -417,8 +417,8 @@ typedef struct {
 /*
  * q, k, v: rows of num_heads x head_dim bf16, contiguous within a row, ld elements
  * between rows (a multiple of 8: a fused projection's [rows, 3, H, d] may be passed
- * as three tensors).  Outputs: [out_rows, H, d] bf16, packed, as the attention calls
- * take them; k_out and v_out may be a cache's slots (refcache_kv_ptr), before
+ * as three tensors).  Outputs must not overlap inputs; they are [out_rows, H, d]
+ * bf16, packed, as the attention calls take them; k_out and v_out may be a cache's slots (refcache_kv_ptr), before
  * refcache_build_in_slot.  v is moved only.  Each of the three may be NULL together
  * with its output.  Output rows that no row goes to are left as they are.
  */
@@ -449,7 +449,8 @@ REFCACHE_API int refcache_qkv_rope_backward(const refcache_rope_t* rope, const r
  *   y = norm(x_out) * weight * (1 + scale) + shift  (before x_out is rounded)
  * gate, scale and shift are rows of the request (ld elements between requests'
  * rows, a multiple of 8; 0: one row for all requests); gate NULL is 1, scale and
- * shift NULL are 0, weights NULL are 1.  Layer norm: (x - mean) / sqrt(var + eps); RMS norm: x / sqrt(mean(x^2) +
+ * shift NULL are 0, weights NULL are 1.
+ * Layer norm: (x - mean) / sqrt(var + eps); RMS norm: x / sqrt(mean(x^2) +
  * eps).  Statistics and arithmetic in fp32.
  */
 #define REFCACHE_NORM_NONE 0
@@ -467,7 +468,10 @@ typedef struct {
   const void *weight, *post_weight; /* device, [width] */
 } refcache_gated_norm_t;
 
-/* x, branch (may be NULL): [rows, width] bf16.  x_out (may be NULL, or x itself) and y (may be NULL) are written. */
+/*
+ * x, branch (may be NULL): [rows, width] bf16.  x_out (may be NULL, or x itself) and
+ * y (may be NULL) are written; they overlap nothing else.
+ */
 REFCACHE_API int refcache_gated_norm(const refcache_gated_norm_t* p, const void* x, const void* branch, void* x_out,
                                      void* y, void* stream);
 

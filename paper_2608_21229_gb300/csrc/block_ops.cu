@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <type_traits>
 
 #include "refcache.h"
@@ -36,6 +37,12 @@ int check_tensor(const void* p, const char* name) {
   return REFCACHE_OK;
 }
 int check_optional(const void* p, const char* name) { return p ? check_tensor(p, name) : REFCACHE_OK; }
+// fp32 results, each of which may be absent
+int check_floats(std::initializer_list<const float*> tensors, const char* name) {
+  for (const float* p : tensors)
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return fail(REFCACHE_ERR_INVALID_ARG, "%s: a float32 result is not 4-byte aligned", name);
+  return REFCACHE_OK;
+}
 
 // ---------------------------------------------------------------- rotary positions
 int check_rope(const refcache_rope_t* r, const refcache_rope_rows_t* w) {
@@ -306,6 +313,7 @@ int refcache_qkv_rope_backward(const refcache_rope_t* r, const refcache_rope_row
     a.ld_dst[i] = ld_dst[i];
   }
   const bool weights = a.weight[0] || a.weight[1];
+  if ((rc = check_floats({dweight_q, dweight_k}, "qkv_rope_backward")) != 0) return rc;
   if (weights && (rc = check_tensor(work, "work")) != 0) return rc;
   a.dw_part = static_cast<float*>(work);
   int sms = 0;
@@ -386,6 +394,7 @@ int refcache_gated_norm_backward(const refcache_gated_norm_t* p, const void* x_o
   if (!dy && !dx_out) return fail(REFCACHE_ERR_INVALID_ARG, "neither dy nor dx_out");
   if ((d_weight && !p->weight) || (d_post_weight && !p->post_weight))
     return fail(REFCACHE_ERR_INVALID_ARG, "the gradient of a weight that is not there");
+  if ((rc = check_floats({d_gate, d_scale, d_shift, d_weight, d_post_weight}, "gated_norm_backward")) != 0) return rc;
   int sms = 0;
   if ((rc = device_sms(&sms)) != 0) return rc;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -449,7 +458,7 @@ int refcache_clip_gradients(int n, const void* const* grads, void* const* out, c
   if (n < 0 || (n > 0 && (!grads || !counts || !types))) return fail(REFCACHE_ERR_INVALID_ARG, "clip_gradients: NULL list or n < 0");
   if (!(max_norm >= 0.f)) return fail(REFCACHE_ERR_INVALID_ARG, "max_norm must be >= 0");  // (+inf: the norm alone)
   int rc = check_tensor(work, "work");
-  if (rc) return rc;
+  if (rc || (rc = check_floats({norm}, "clip_gradients")) != 0) return rc;
   for (int i = 0; i < n; ++i) {
     if (counts[i] < 0) return fail(REFCACHE_ERR_INVALID_ARG, "counts[%d] is negative", i);
     if (types[i] & ~3) return fail(REFCACHE_ERR_INVALID_ARG, "types[%d] = %d is none of REFCACHE_CLIP_*", i, types[i]);
@@ -493,7 +502,7 @@ int refcache_clip_gradients(int n, const void* const* grads, void* const* out, c
     if (e != cudaSuccess) return cuda_fail(e, "clip_norm_kernel launch");
     parts += grid;
   }
-  const bool scale = !(max_norm > 3.0e38f) || out != nullptr;  // an infinite bound in place leaves the tensors as they are
+  const bool scale = !std::isinf(max_norm) || out != nullptr;  // an infinite bound in place leaves the tensors as they are
   for (int b = 0; b == 0 || (b < n && scale); b += rc::kClipMaxTensors) {
     rc::ClipTable t = table(b);
     if (!scale) t.n = 0, t.piece0[0] = 0;

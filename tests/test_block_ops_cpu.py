@@ -103,6 +103,19 @@ def test_gated_norm_tensor_refusals(lib):
         assert go(p, **{**base, **kw}) == rcb.ERR_INVALID_ARG, kw
 
 
+def test_float_results_are_aligned(lib):
+    """A float32 result at an odd address is refused, not written."""
+    rope, w = rcb.Rope(64, (64,)), rope_rows(weight_q=P)
+    assert lib.refcache_qkv_rope_backward(ctypes.byref(rope.c), ctypes.byref(w), P, 128, None, 0, P, None, None, P, 128, None, 0, None, 0,
+                                          P + 2, None, P, None) == rcb.ERR_INVALID_ARG
+    c = norm_params(weight=P, post_weight=P, post_norm=2)
+    for i in range(5):
+        sums = [P + 1 if j == i else P for j in range(5)]
+        assert lib.refcache_gated_norm_backward(ctypes.byref(c), P, P, P, P, P, P, *sums, P, None) == rcb.ERR_INVALID_ARG, i
+    ok = ((ctypes.c_void_p * 1)(P), None, (ctypes.c_int64 * 1)(4), (ctypes.c_int32 * 1)(0))
+    assert lib.refcache_clip_gradients(1, *ok, 1.0, P + 2, P, None) == rcb.ERR_INVALID_ARG
+
+
 def test_clip_refusals(lib):
     vp, i64, i32 = ctypes.c_void_p * 1, ctypes.c_int64 * 1, ctypes.c_int32 * 1
     f = lib.refcache_clip_gradients

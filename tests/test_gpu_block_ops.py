@@ -387,6 +387,12 @@ def test_clip_of_special_values():
     assert rcb.clip_gradients([], 1.0).item() == 0.0
 
 
+def test_largest_finite_bound_is_a_bound():
+    g = torch.tensor([math.inf, 2.0], device="cuda")
+    assert rcb.clip_gradients([g], 3.3e38).item() == math.inf
+    assert g[0].isnan() and g[1] == 0
+
+
 def test_other_stream():
     c = NormCase([30, 12], 512, "layer", "rms", BF16, True)
     side = torch.cuda.Stream()
