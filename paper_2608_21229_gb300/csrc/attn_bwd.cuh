@@ -95,9 +95,8 @@ __device__ __forceinline__ BwdItem bwd_item(const List& l, int it, int num_heads
 // heads of 128 take 6.0 us (15.9 MB), 9431 rows of 16 heads of 64 11 us (39 MB, 3.6 TB/s).
 constexpr int kBwdPrepHeads = 4;
 template <int D>
-__global__ void __launch_bounds__(256) attn_bwd_prep_kernel(const __nv_bfloat16* __restrict__ o, const __nv_bfloat16* __restrict__ d_o,
-                                                            const float* __restrict__ lse, float2* __restrict__ stats, int64_t rows,
-                                                            int num_heads) {
+__global__ void __launch_bounds__(256) attn_bwd_prep_kernel(const __nv_bfloat16* o, const __nv_bfloat16* d_o, const float* lse,
+                                                            float2* stats, int64_t rows, int num_heads) {
   constexpr int kLanes = D / 8, kRows = 256 / kLanes;
   grid_dependency_wait();
   if (threadIdx.x == 0) grid_launch_dependents();

@@ -79,14 +79,14 @@ __global__ void __launch_bounds__(kClipThreads) clip_norm_kernel(const __grid_co
     if (p.src32) {
 #pragma unroll 8
       for (int i = threadIdx.x; i < nv; i += kClipThreads) {
-        const uint4 r = __ldg(v + i);
+        const uint4 r = v[i];
         const float a = __uint_as_float(r.x), b = __uint_as_float(r.y), c = __uint_as_float(r.z), d = __uint_as_float(r.w);
         s = fmaf(a, a, s), s = fmaf(b, b, s), s = fmaf(c, c, s), s = fmaf(d, d, s);
       }
     } else {
 #pragma unroll 8
       for (int i = threadIdx.x; i < nv; i += kClipThreads) {
-        const Vec8 r = unpack8(__ldg(v + i));
+        const Vec8 r = unpack8(v[i]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) s = fmaf(r.v[e], r.v[e], s);
       }

@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) qkv_rope_backward_kernel(cons
 // dw = the sum of the blocks' parts, kRopeSumCols columns of one weight a block: 1024 /
 // kRopeSumCols groups take every n-th part and are joined in a fixed order.
 constexpr int kRopeSumCols = 8;
-__global__ void __launch_bounds__(1024) rope_weight_grad_kernel(const float* __restrict__ part, int n_parts, int D, float* dwq,
+__global__ void __launch_bounds__(1024) rope_weight_grad_kernel(const float* part, int n_parts, int D, float* dwq,
                                                                 float* dwk) {
   __shared__ float sums[32][kRopeSumCols];
   grid_dependency_wait();

@@ -31,14 +31,16 @@ __device__ __forceinline__ Vec8 fill8(float x) {
   for (int i = 0; i < 8; ++i) o.v[i] = x;
   return o;
 }
-// Elements [i, i + 8) of a parameter row held in bf16 or fp32.
+// Elements [i, i + 8) of a parameter row held in bf16 or fp32.  Plain loads here and in the
+// kernels: one through the read-only path might be moved above the wait for the kernel
+// before, which may have written what is read.
 __device__ __forceinline__ Vec8 load_param8(const void* p, int64_t i, bool f32) {
   if (f32) {
     const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
-    const float4 a = __ldg(q), b = __ldg(q + 1);
+    const float4 a = q[0], b = q[1];
     return Vec8{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
   }
-  return unpack8(__ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i)));
+  return unpack8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i));
 }
 // Loads and stores of data that is used once.
 __device__ __forceinline__ uint4 ld_stream(const void* p) { return __ldcs(static_cast<const uint4*>(p)); }
