@@ -183,6 +183,16 @@ int norm_blocks(int rows, int sms, const NormShape& n) {
   const int per_sm = std::max(1, std::min({512 / n.threads, (227 << 10) / (n.smem + 2048), 16}));
   return std::min(rows, per_sm * sms);
 }
+// Rows of a forward block.  SMs run at different speeds, so more blocks than are resident at
+// once end sooner, as long as a block has enough rows to be worth its start (16, or 32 where
+// one block has an SM to itself): as many whole rounds of resident blocks as leave that.
+// One round against these, no post norm and with one: 8704 rows of 4096 53.6 and 49.0 us
+// (two rounds), 9216 rows 56.3 and 50.5, 52.2 and 53.5; 40000 rows of 2048 123 and 104, 164
+// and 120 (eight); 20000 rows of 2048 with ten rows a block 53 and 65, with these 55 and 63.
+int norm_rows_per_block(int rows, int sms, const NormShape& n) {
+  const int64_t resident = norm_blocks(rows, sms, n), least = (n.threads < 512 ? 16 : 32) * resident;
+  return ceil_div(rows, resident * std::max<int64_t>(1, (rows + least / 2) / least));
+}
 // f(kNV, kThreads) of the shape, as constants.
 template <typename F>
 cudaError_t with_norm_shape(const NormShape& n, const F& f) {
@@ -362,7 +372,7 @@ int refcache_gated_norm(const refcache_gated_norm_t* p, const void* x, const voi
     a.branch = branch ? static_cast<const uint16_t*>(branch) + off : nullptr;
     a.x_out = x_out ? static_cast<uint16_t*>(x_out) + off : nullptr;
     a.y = y ? static_cast<uint16_t*>(y) + off : nullptr;
-    a.rows_per_block = ceil_div(a.rows, norm_blocks(a.rows, sms, shape));
+    a.rows_per_block = norm_rows_per_block(a.rows, sms, shape);
     const int blocks = ceil_div(a.rows, a.rows_per_block);
     const cudaError_t e = with_norm_shape(shape, [&](auto nv, auto threads) {
       return launch_norm(rc::gated_norm_kernel<decltype(nv)::value, decltype(threads)::value>, shape, blocks, s, segs, a);

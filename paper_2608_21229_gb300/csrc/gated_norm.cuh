@@ -16,8 +16,8 @@
 // weights) is made into a few vectors at the request's first row.  The rows ahead are on
 // their way into shared memory meanwhile (cp.async; every thread copies and reads its own
 // columns, so that no barrier is needed for them).  8704 rows of 4096 columns, layer norm:
-// 46 us alone on the GPU, 6.2 TB/s, 53 call after call; 67.6 when a row was loaded into
-// registers as its turn came, since a block waits for memory once a row then.
+// 49 us call after call, 5.8 TB/s; 67.6 when a row was loaded into registers as its turn
+// came, since a block waits for memory once a row then.
 //
 // The mean is found before the squares, from values in registers: two exchanges of the
 // block's warps for a layer norm, and no cancellation where the mean is large.
