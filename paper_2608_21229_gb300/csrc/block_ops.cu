@@ -27,7 +27,7 @@ namespace {
 constexpr int64_t kMaxRows = (1ll << 31) - 1 - 512;
 constexpr int kRopeMaxParts = 1024;   // blocks of the rotary gradient's launch
 constexpr int kNormMaxBlocks = 1280;  // blocks of a gated norm's gradient launch
-constexpr int kClipMaxBlocks = 1024;  // blocks of a clipping launch
+constexpr int kClipMaxBlocks = 2560;  // blocks of a norm launch of clip_gradients
 
 int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
 
@@ -460,7 +460,8 @@ int refcache_gated_norm_backward(const refcache_gated_norm_t* p, const void* x_o
 
 size_t refcache_clip_gradients_bytes(int n) {
   if (n < 0) return 0;
-  return static_cast<size_t>(std::max(1, ceil_div(n, rc::kClipMaxTensors))) * kClipMaxBlocks * sizeof(double);
+  // the blocks' sums of every table, and a counter each
+  return static_cast<size_t>(std::max(1, ceil_div(n, rc::kClipMaxTensors))) * (kClipMaxBlocks * sizeof(double) + 16);
 }
 
 int refcache_clip_gradients(int n, const void* const* grads, void* const* out, const int64_t* counts, const int32_t* types,
@@ -500,15 +501,20 @@ int refcache_clip_gradients(int n, const void* const* grads, void* const* out, c
     return t;
   };
   double* part = static_cast<double*>(work);
+  int* taken = reinterpret_cast<int*>(part + static_cast<int64_t>(std::max(1, ceil_div(n, rc::kClipMaxTensors))) * kClipMaxBlocks);
   int parts = 0;
-  const int most = std::min(4 * sms, kClipMaxBlocks);
+  const int resident = std::min(4 * sms, kClipMaxBlocks);
   for (int b = 0; b < n; b += rc::kClipMaxTensors) {
     const rc::ClipTable t = table(b);
     const int pieces = t.piece0[t.n];
     if (pieces == (1ll << 31) - 1) return fail(REFCACHE_ERR_INVALID_ARG, "clip_gradients: too many elements");
     if (pieces == 0) continue;
-    const int grid = std::min(pieces, most);
-    const cudaError_t e = launch_dependent(rc::clip_norm_kernel, dim3(static_cast<unsigned>(grid)), dim3(rc::kClipThreads), 0, s, t, part + parts);
+    // (Pieces are dealt out in a fixed order, for the sums' sake; up to four rounds of blocks
+    // even out the SMs' speeds: 906 M elements 811 us with one, 794 with four.)
+    const int rounds = std::max(1, std::min(pieces / (8 * resident), kClipMaxBlocks / resident));
+    const int grid = std::min(pieces, std::min(4, rounds) * resident);
+    const cudaError_t e =
+        launch_dependent(rc::clip_norm_kernel, dim3(static_cast<unsigned>(grid)), dim3(rc::kClipThreads), 0, s, t, part + parts, taken + 4 * (b / rc::kClipMaxTensors));
     if (e != cudaSuccess) return cuda_fail(e, "clip_norm_kernel launch");
     parts += grid;
   }
@@ -516,9 +522,9 @@ int refcache_clip_gradients(int n, const void* const* grads, void* const* out, c
   for (int b = 0; b == 0 || (b < n && scale); b += rc::kClipMaxTensors) {
     rc::ClipTable t = table(b);
     if (!scale) t.n = 0, t.piece0[0] = 0;
-    const int grid = std::max(1, std::min(t.piece0[t.n], most));
+    const int grid = std::max(1, std::min(t.piece0[t.n], resident));
     const cudaError_t e = launch_dependent(rc::clip_scale_kernel, dim3(static_cast<unsigned>(grid)), dim3(rc::kClipThreads), 0, s, t,
-                                           static_cast<const double*>(part), parts, max_norm, b == 0 ? norm : nullptr, out == nullptr ? 1 : 0);
+                                           static_cast<const double*>(part), parts, taken + 4 * (b / rc::kClipMaxTensors), max_norm, b == 0 ? norm : nullptr, out == nullptr ? 1 : 0);
     if (e != cudaSuccess) return cuda_fail(e, "clip_scale_kernel launch");
   }
   return REFCACHE_OK;

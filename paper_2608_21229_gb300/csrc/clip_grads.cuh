@@ -5,8 +5,9 @@
 //
 // Bound by memory: the tensors are read for the norm, read again to be scaled,
 // and written.  The second pass takes the pieces in the opposite order, so that
-// what the first read last is still in the L2 (129 MB).  907 M bf16 elements: norm 299 us,
-// 6.1 TB/s, scaling 567 us, 6.4 TB/s.  Sums are fp32 within a
+// what the first read last is still in the L2 (129 MB).  906 M bf16 elements in place: 778
+// us, 7.0 TB/s of the two reads and the write (836 with as many pieces for every block).
+// Sums are fp32 within a
 // thread's piece, fp64 from there on, and in a fixed order: the same tensors give
 // the same bits.
 #pragma once
@@ -62,10 +63,11 @@ __device__ __forceinline__ int clip_head(const uint8_t* p, int size, int n) {
   return min(n, static_cast<int>((16u - (reinterpret_cast<uintptr_t>(p) & 15u)) & 15u) / size);
 }
 
-__global__ void __launch_bounds__(kClipThreads) clip_norm_kernel(const __grid_constant__ ClipTable t, double* part) {
+__global__ void __launch_bounds__(kClipThreads) clip_norm_kernel(const __grid_constant__ ClipTable t, double* part, int* taken) {
   __shared__ double sums[kClipThreads / 32];
   grid_dependency_wait();
   if (threadIdx.x == 0) grid_launch_dependents();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *taken = 0;
   const int pieces = t.piece0[t.n];
   double total = 0.0;
   int tensor = 0;
@@ -107,10 +109,14 @@ __global__ void __launch_bounds__(kClipThreads) clip_norm_kernel(const __grid_co
   }
 }
 
-// The scaled tensors of one launch; every block adds up all parts by itself.
-__global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const __grid_constant__ ClipTable t, const double* part, int n_parts,
-                                                                  float max_norm, float* norm, int in_place) {
+// The scaled tensors of one launch; every block adds up all parts by itself.  `taken`
+// counts the pieces taken beyond the blocks' first: SMs run at different speeds.  (Many
+// rounds of blocks would even that out too, but each adds the parts up again: with nothing
+// to scale, 400 M fp32 elements took 260 us instead of 224.)
+__global__ void __launch_bounds__(kClipThreads, 4) clip_scale_kernel(const __grid_constant__ ClipTable t, const double* part, int n_parts,
+                                                                  int* taken, float max_norm, float* norm, int in_place) {
   __shared__ double sums[kClipThreads / 32];
+  __shared__ int next[2];
   grid_dependency_wait();
   if (threadIdx.x == 0) grid_launch_dependents();
   double total = 0.0;
@@ -128,7 +134,9 @@ __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const __grid_c
   if (in_place && coef == 1.f) return;
   const int pieces = t.piece0[t.n];
   int tensor = max(0, t.n - 1);
-  for (int q = pieces - 1 - static_cast<int>(blockIdx.x); q >= 0; q -= static_cast<int>(gridDim.x)) {
+  int q = pieces - 1 - static_cast<int>(blockIdx.x);
+  for (int k = 0; q >= 0; ++k) {
+    if (threadIdx.x == 0) next[k & 1] = pieces - 1 - static_cast<int>(gridDim.x) - atomicAdd(taken, 1);
     tensor = clip_tensor(t, q, tensor);
     const ClipPiece p = clip_piece(t, q, tensor);
     const int size = p.src32 ? 4 : 2, per = 16 / size, head = clip_head(p.src, size, p.n);
@@ -186,6 +194,8 @@ __global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const __grid_c
       const int at = i < head ? i : i + nv * per;
       put(p.dst, at, clip_load(p.src, at, p.src32) * coef);
     }
+    __syncthreads();
+    q = next[k & 1];
   }
 }
 
