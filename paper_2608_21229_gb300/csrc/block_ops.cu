@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdint>
 #include <initializer_list>
 #include <type_traits>
 
@@ -103,6 +104,23 @@ int rope_slices(const refcache_rope_t* r, const refcache_rope_rows_t* w, int sms
   int slices = static_cast<int>(std::min<int64_t>(most, std::max<int64_t>(1, want)));
   *step = ceil_div(ceil_div(w->num_heads, slices), per) * per;
   return ceil_div(w->num_heads, *step);
+}
+
+// The gradient's blocks of each slice.  Every block stays for the whole launch, so the slices
+// are as many as let the warp with the most rows have the fewest heads in all; a row's angles
+// cost as much as three.  24 heads of 128, one slice and as chosen: 2500 rows 37.5 and 32.0
+// us (three), 20608 rows 177 and 204 with three.
+int rope_backward_blocks(const refcache_rope_t* r, const refcache_rope_rows_t* w, int resident, int unroll, int* slices, int* step) {
+  const int per = 32 / (r->head_dim / 8), most = std::min(64, ceil_div(w->num_heads, unroll * per));
+  int64_t best = INT64_MAX;
+  int blocks = 1;
+  for (int want = 1; want <= most; ++want) {
+    const int heads = ceil_div(ceil_div(w->num_heads, want), per) * per, n = ceil_div(w->num_heads, heads);
+    const int b = std::min(ceil_div(w->rows, rc::kRopeTokens), std::max(1, resident / n));
+    const int64_t cost = ceil_div(w->rows, static_cast<int64_t>(b) * rc::kRopeTokens) * (heads + 3ll);
+    if (cost < best) best = cost, blocks = b, *slices = n, *step = heads;
+  }
+  return blocks;
 }
 
 // ---------------------------------------------------------------- gated norm
@@ -332,8 +350,8 @@ int refcache_qkv_rope_backward(const refcache_rope_t* r, const refcache_rope_row
   cudaError_t e = cudaSuccess;
   int parts = 0;
   if (w->rows > 0 && (dq_out || dk_out || dv_out)) {
-    const int slices = rope_slices(r, w, sms, 4, &a.head_step);
-    const int blocks = std::max(1, std::min({ceil_div(w->rows, rc::kRopeTokens), 2 * sms, kRopeMaxParts / slices}));
+    int slices = 1;
+    const int blocks = rope_backward_blocks(r, w, std::min(2 * sms, kRopeMaxParts), 4, &slices, &a.head_step);
     parts = blocks * slices;
     const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(slices), 1);
     auto go = [&](auto kernel) { return launch_dependent(kernel, grid, dim3(rc::kRopeThreads), 0, s, t, a); };

@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kRopeThreads) qkv_rope_kernel(const __grid_con
 
 // The gradient: a warp walks over tokens row, row + stride, ... so that the sums
 // of dw stay in registers; the block's sum goes to dw_part.  Bound by the latency of its
-// loads, two warps a scheduler: 4608 rows of 24 heads of 128 take 42.6 us, 5.3 TB/s, and
+// loads, two blocks an SM: 4608 rows of 24 heads of 128 take 42.6 us, 5.3 TB/s, and
 // the sums below 4.  (128 registers a thread; at 80, for three blocks an SM, they spill:
 // 67 us.  Loads through a ring in shared memory: 45 us.)
 template <int D, bool kHalves>
