@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+from array import array
 from typing import Optional, Sequence
 
 from . import build as _build
@@ -737,8 +738,9 @@ def clip_gradients(grads, max_norm, out=None, norm=None, stream=None):
         raise ValueError(f"norm: expected one float32, got {norm.dtype} {tuple(norm.shape)}")
     L = load()
     work = _work(L.refcache_clip_gradients_bytes(n), norm, stream)
-    pointers = ctypes.c_void_p * n
-    _check(L.refcache_clip_gradients(n, pointers(*[g.data_ptr() for g in grads]),
-                                     None if outs is None else pointers(*[o.data_ptr() for o in outs]), (ctypes.c_int64 * n)(*counts),
-                                     (ctypes.c_int32 * n)(*types), max_norm, _ptr(norm), work.data_ptr(), _stream(stream)))
+    # (arrays of the array module: ctypes' took half of the time that a tensor costs)
+    lists = [array("Q", [g.data_ptr() for g in grads]), None if outs is None else array("Q", [o.data_ptr() for o in outs]),
+             array("q", counts), array("i", types)]
+    _check(L.refcache_clip_gradients(n, *[None if a is None else a.buffer_info()[0] for a in lists], max_norm, _ptr(norm),
+                                     work.data_ptr(), _stream(stream)))
     return norm
