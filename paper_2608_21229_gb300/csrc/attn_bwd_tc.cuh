@@ -40,7 +40,8 @@
 // pair is free.
 //
 // What bounds them: at D = 128 the tensor pipe (with many tiles an item, under the power
-// cap), at D = 64 the score warps.  Measured, each alone on the GPU:
+// cap), at D = 64 the score warps and as long a chain from one S to the next (arrivals,
+// MMAs, commits).  Measured, each alone on the GPU:
 //                                    keys kernel              queries kernel
 //   cycles per tile, D = 128         2250 (MMAs: 2048)        1690 (1536)
 //   cycles per tile, D = 64          1710 (1024)              1510 (768)
