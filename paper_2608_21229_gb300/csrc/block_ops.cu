@@ -470,7 +470,12 @@ int refcache_gated_norm_backward(const refcache_gated_norm_t* p, const void* x_o
     g.rows_per_block = a.rows_per_block;
     g.mod_f32 = a.mod_f32;
     g.add = b > 0;
-    e = launch_dependent(rc::norm_param_grad_kernel, dim3(static_cast<unsigned>(ceil_div(p->width, 64)), 3), dim3(32 * rc::kSumWarps), 0, s, segs, g);
+    // (by slots a request.  Call with the many and the few form: 5888 rows of 4096 in 8 requests, 37 slots each, 71 and 67
+    // us, 300 of 256, 37 each, 4.7 and 11; 4608 of 8192 in 8, 19 each, 117 and 98; 5888 of 4096 in 64, 5 each, 153 and 66)
+    const bool few = ceil_div(a.rows, a.rows_per_block) < 32 * n, weights = d_weight || d_post_weight;
+    const dim3 grid(static_cast<unsigned>(ceil_div(p->width, few ? rc::kSumFewCols : rc::kSumCols)), 3,
+                    weights ? 1u : static_cast<unsigned>(few ? ceil_div(n, rc::kSumWarps) : n));
+    e = launch_dependent(few ? rc::norm_param_grad_few_kernel : rc::norm_param_grad_kernel, grid, dim3(rc::kSumThreads), 0, s, segs, g);
     if (e != cudaSuccess) return cuda_fail(e, "norm_param_grad_kernel launch");
   }
   return REFCACHE_OK;

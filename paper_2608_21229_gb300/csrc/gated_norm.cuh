@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_kernel(co
 // request) has.  The request's two vectors lie in shared memory beside the rows ahead,
 // for the registers' sake; two blocks of 256 threads then share an SM.  Bound by the
 // latency of a row's four exchanges and by issue (46 % of the slots): 5888 rows of 4096
-// columns in two requests, both norms: 60 us, 4.8 TB/s.  (A vector a thread and 512 threads
+// columns in two requests, both norms: 58 us, 5.0 TB/s, and the sums 6.  (A vector a thread and 512 threads
 // at 64 registers spill: 183 us.)
 template <int kNV, int kThreads>
 __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_backward_kernel(const __grid_constant__ NormSegs segs,
@@ -446,66 +446,112 @@ __device__ __forceinline__ float load_param(const void* p, int64_t i, bool f32) 
   return f32 ? static_cast<const float*>(p)[i] : __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(p)[i]) << 16);
 }
 
-// The parameters' gradients from the blocks' sums: blockIdx.y = which sum (A, B,
-// G); a lane has two columns, a warp takes every kSumWarps-th slot of a request, and the
-// warps' sums are joined in their order.  Reads `part` once: 14.7 MB, 5 us behind the
-// kernel that has just written it.
-constexpr int kSumWarps = 16;
-__global__ void __launch_bounds__(32 * kSumWarps) norm_param_grad_kernel(const __grid_constant__ NormSegs segs,
-                                                                         const __grid_constant__ NormSumArgs a) {
-  __shared__ float2 sums[kSumWarps][32];
+// The result of one request and column: sum k (A, B, G) is v.  Returns what it adds to the
+// weight's gradient.
+__device__ __forceinline__ float norm_param_grad(const NormSumArgs& a, int k, int s, int col, float v) {
+  const int64_t at = static_cast<int64_t>(s) * a.width + col;
+  const bool f32 = a.mod_f32 != 0;
+  if (k == 0) {
+    if (a.d_shift) a.d_shift[at] = v;
+    return 0.f;
+  }
+  if (k == 1) {
+    if (a.d_scale) a.d_scale[at] = a.weight ? v * load_param(a.weight, col, f32) : v;
+    return (a.scale ? 1.f + load_param(a.scale, s * a.ld_scale + col, f32) : 1.f) * v;
+  }
+  if (a.d_gate) a.d_gate[at] = a.post_weight ? v * load_param(a.post_weight, col, f32) : v;
+  return (a.gate ? load_param(a.gate, s * a.ld_gate + col, f32) : 1.f) * v;
+}
+__device__ __forceinline__ void norm_weight_grad(const NormSumArgs& a, int k, int col, float total) {
+  float* w = k == 1 ? a.d_weight : k == 2 ? a.d_post_weight : nullptr;
+  if (w) w[col] = a.add ? w[col] + total : total;
+}
+
+// The parameters' gradients from the blocks' sums, which are read once; blockIdx.y = which
+// sum.  One request, or some, for each blockIdx.z, or all of them one after the other where a
+// weight's gradient needs their sum (gridDim.z = 1).  Two forms, for many and for few slots a
+// request; all orders are fixed.
+//
+// Many: kSumCols columns a block, four for each of kSumCols / 4 threads that take every
+// kSumGroups-th slot, so that most of its loads are under way at once; a warp's groups are
+// joined by shuffles and the warps in their order.  295 slots of 4096 columns (14.7 MB) add
+// 6 us to the call that wrote them.
+constexpr int kSumThreads = 512, kSumWarps = kSumThreads / 32, kSumCols = 32, kSumGroups = kSumThreads / (kSumCols / 4);
+__global__ void __launch_bounds__(kSumThreads) norm_param_grad_kernel(const __grid_constant__ NormSegs segs,
+                                                                      const __grid_constant__ NormSumArgs a) {
+  __shared__ float4 sums[kSumWarps][kSumCols / 4];
   grid_dependency_wait();
   if (threadIdx.x == 0) grid_launch_dependents();
-  const int lane = threadIdx.x & 31, g = threadIdx.x >> 5, k = blockIdx.y, col = 64 * blockIdx.x + 2 * lane;
-  const bool on = col < a.width;
-  const bool f32 = a.mod_f32 != 0;
-  float2 total = make_float2(0.f, 0.f);
-  for (int s = 0; s < segs.n; ++s) {
-    float2 sum = make_float2(0.f, 0.f);
-    if (on && segs.cu[s + 1] > segs.cu[s]) {
+  const int tid = threadIdx.x, k = blockIdx.y, g = tid / (kSumCols / 4), first = kSumCols * blockIdx.x;
+  const int col = first + 4 * (tid % (kSumCols / 4)), mine = first + tid;  // of the loads; of the results (the first warp)
+  const bool all = gridDim.z == 1;
+  const int s1 = all ? segs.n : static_cast<int>(blockIdx.z) + 1;
+  float total = 0.f;
+  for (int s = all ? 0 : blockIdx.z; s < s1; ++s) {
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (col < a.width && segs.cu[s + 1] > segs.cu[s]) {
       const int b0 = segs.cu[s] / a.rows_per_block, b1 = (segs.cu[s + 1] - 1) / a.rows_per_block;
       const float* p = a.part + (static_cast<int64_t>(s) * 3 + k) * a.width + col;
-      int b = b0 + g;
-      for (; b + 3 * kSumWarps <= b1; b += 4 * kSumWarps) {
-        float2 v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float2*>(p + static_cast<int64_t>(b + i * kSumWarps) * 3 * a.width);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum.x += v[i].x, sum.y += v[i].y;
-      }
-      for (; b <= b1; b += kSumWarps) {
-        const float2 v = *reinterpret_cast<const float2*>(p + static_cast<int64_t>(b) * 3 * a.width);
-        sum.x += v.x, sum.y += v.y;
+#pragma unroll 4
+      for (int b = b0 + g; b <= b1; b += kSumGroups) {
+        const float4 v = *reinterpret_cast<const float4*>(p + static_cast<int64_t>(b) * 3 * a.width);
+        sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
       }
     }
-    sums[g][lane] = sum;
-    __syncthreads();
-    if (g == 0 && on) {
-      for (int i = 1; i < kSumWarps; ++i) sum.x += sums[i][lane].x, sum.y += sums[i][lane].y;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int c = col + h;
-        const float v = h ? sum.y : sum.x;
-        float& t = h ? total.y : total.x;
-        const int64_t at = static_cast<int64_t>(s) * a.width + c;
-        if (k == 0) {
-          if (a.d_shift) a.d_shift[at] = v;
-        } else if (k == 1) {
-          if (a.d_scale) a.d_scale[at] = a.weight ? v * load_param(a.weight, c, f32) : v;
-          t += (a.scale ? 1.f + load_param(a.scale, s * a.ld_scale + c, f32) : 1.f) * v;
-        } else {
-          if (a.d_gate) a.d_gate[at] = a.post_weight ? v * load_param(a.post_weight, c, f32) : v;
-          t += (a.gate ? load_param(a.gate, s * a.ld_gate + c, f32) : 1.f) * v;
-        }
-      }
+    for (int o = kSumCols / 4; o < 32; o <<= 1) {
+      sum.x += __shfl_xor_sync(0xffffffffu, sum.x, o);
+      sum.y += __shfl_xor_sync(0xffffffffu, sum.y, o);
+      sum.z += __shfl_xor_sync(0xffffffffu, sum.z, o);
+      sum.w += __shfl_xor_sync(0xffffffffu, sum.w, o);
+    }
+    if ((tid & 31) < kSumCols / 4) sums[tid >> 5][tid & 31] = sum;
+    __syncthreads();
+    if (tid < kSumCols && mine < a.width) {
+      float v = 0.f;
+#pragma unroll
+      for (int w = 0; w < kSumWarps; ++w) v += reinterpret_cast<const float*>(sums[w])[tid];
+      total += norm_param_grad(a, k, s, mine, v);
     }
     __syncthreads();
   }
-  float* w = k == 1 ? a.d_weight : k == 2 ? a.d_post_weight : nullptr;
-  if (g == 0 && on && w) {
-    w[col] = a.add ? w[col] + total.x : total.x;
-    w[col + 1] = a.add ? w[col + 1] + total.y : total.y;
+  if (tid < kSumCols && mine < a.width) norm_weight_grad(a, k, mine, total);
+}
+
+// Few: 128 columns a block, four a lane, and a request for each warp.
+constexpr int kSumFewCols = 128;
+__global__ void __launch_bounds__(kSumThreads) norm_param_grad_few_kernel(const __grid_constant__ NormSegs segs,
+                                                                          const __grid_constant__ NormSumArgs a) {
+  __shared__ float4 sums[kSumWarps][32];
+  grid_dependency_wait();
+  if (threadIdx.x == 0) grid_launch_dependents();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = blockIdx.y, col = kSumFewCols * blockIdx.x + 4 * lane;
+  const bool on = col < a.width;
+  float4 total = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s = kSumWarps * blockIdx.z + warp; on && s < segs.n; s += kSumWarps * gridDim.z) {
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (segs.cu[s + 1] > segs.cu[s]) {
+      const int b0 = segs.cu[s] / a.rows_per_block, b1 = (segs.cu[s + 1] - 1) / a.rows_per_block;
+      const float* p = a.part + (static_cast<int64_t>(s) * 3 + k) * a.width + col;
+#pragma unroll 4
+      for (int b = b0; b <= b1; ++b) {
+        const float4 v = *reinterpret_cast<const float4*>(p + static_cast<int64_t>(b) * 3 * a.width);
+        sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+      }
+    }
+    total.x += norm_param_grad(a, k, s, col, sum.x);
+    total.y += norm_param_grad(a, k, s, col + 1, sum.y);
+    total.z += norm_param_grad(a, k, s, col + 2, sum.z);
+    total.w += norm_param_grad(a, k, s, col + 3, sum.w);
   }
+  sums[warp][lane] = total;
+  __syncthreads();
+  const int mine = kSumFewCols * blockIdx.x + threadIdx.x;
+  if (gridDim.z > 1 || threadIdx.x >= kSumFewCols || mine >= a.width) return;
+  float v = 0.f;
+#pragma unroll
+  for (int w = 0; w < kSumWarps; ++w) v += reinterpret_cast<const float*>(sums[w])[threadIdx.x];
+  norm_weight_grad(a, k, mine, v);
 }
 
 }  // namespace rc

@@ -264,6 +264,18 @@ def test_gated_norm_backward(case):
     assert all(torch.equal(a, b) for a, b in zip(got.values(), again.values()))
 
 
+@pytest.mark.parametrize("case", [
+    ([70, 0, 95], 200, "rms", None, BF16, False),  # many blocks a request, each request by itself
+    ([3] * 40, 136, "layer", "rms", torch.float32, False),  # few
+    ([9] * 40, 136, "layer", None, torch.float32, True),  # few, added up over the requests
+    ([1500, 1, 900], 2056, "rms", "rms", BF16, True),  # blocks that take several rows and go on to the next request
+    ([1100, 1300], 1032, "layer", "layer", BF16, False),
+], **IDS)
+def test_gated_norm_backward_sums(case):
+    """The forms in which the parameters' gradients are added up."""
+    test_gated_norm_backward(case)
+
+
 def test_gated_norm_backward_of_parts():
     """Only the norm (no branch), and only the residual (no y)."""
     c = NormCase([30, 12], 512, "layer", None, BF16, False)
