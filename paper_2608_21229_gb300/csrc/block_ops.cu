@@ -97,10 +97,11 @@ void rope_tables(const refcache_rope_t* r, const refcache_rope_rows_t* w, rc::Ro
 }
 
 // Slices of the heads: few tokens leave SMs without a warp, so a token's heads are
-// divided among up to as many warps as have a full set of loads each.
+// divided among up to as many warps as have a full set of loads each, as long as there are
+// fewer than 56 an SM (32 are resident; 24 heads of 128, 2500 rows: one slice 22.5 us, three 18.3).
 int rope_slices(const refcache_rope_t* r, const refcache_rope_rows_t* w, int sms, int unroll, int* step) {
   const int per = 32 / (r->head_dim / 8), most = std::min(64, ceil_div(w->num_heads, unroll * per));
-  const int64_t want = 32ll * sms / w->rows;
+  const int64_t want = 56ll * sms / w->rows;
   int slices = static_cast<int>(std::min<int64_t>(most, std::max<int64_t>(1, want)));
   *step = ceil_div(ceil_div(w->num_heads, slices), per) * per;
   return ceil_div(w->num_heads, *step);
@@ -108,7 +109,7 @@ int rope_slices(const refcache_rope_t* r, const refcache_rope_rows_t* w, int sms
 
 // The gradient's blocks of each slice.  Every block stays for the whole launch, so the slices
 // are as many as let the warp with the most rows have the fewest heads in all; a row's angles
-// cost as much as three.  24 heads of 128, one slice and as chosen: 2500 rows 37.5 and 32.0
+// count as three.  24 heads of 128, one slice and as chosen: 2500 rows 37.5 and 32.0
 // us (three), 20608 rows 177 and 204 with three.
 int rope_backward_blocks(const refcache_rope_t* r, const refcache_rope_rows_t* w, int resident, int unroll, int* slices, int* step) {
   const int per = 32 / (r->head_dim / 8), most = std::min(64, ceil_div(w->num_heads, unroll * per));

@@ -15,7 +15,7 @@
 // needs no range reduction of its own.
 //
 // All of it is bound by memory: every head row is read once and written once.  Forward,
-// 20608 rows of q, k and v of 24 heads of 128: 122.5 us call after call, 6.2 TB/s.
+// 20608 rows of q, k and v of 24 heads of 128: 120.5 us call after call, 6.3 TB/s.
 // A row of one head is 16 bytes for each of D / 8 lanes, so that a warp holds
 // 32 / (D / 8) heads of one token at a time, the mean takes log2(D / 8)
 // shuffles, and the angles of a token (4 or 8 for each lane) are found once for
@@ -52,21 +52,57 @@ struct RopeArgs {
   float eps;
 };
 
+// The table in shared memory: lanes read different entries of it, which a kernel parameter
+// gives one after the other.  (Both kernels fill it before they wait for the one before.
+// Without it, and with all eight angles of a lane found by the lane itself, 4608 rows of 24
+// heads of 128 took 38 us with pairs in halves, now 29.)
+struct RopeShared {
+  float4 hi[kRopeMaxPairs / 4], lo[kRopeMaxPairs / 4];
+  uint32_t axes[kRopeMaxPairs / 4];  // of four pairs, a byte each
+  __device__ __forceinline__ void fill(const RopeTable& t) {
+    const int i = threadIdx.x;
+    if (i < kRopeMaxPairs) {
+      reinterpret_cast<float*>(hi)[i] = t.turn_hi[i];
+      reinterpret_cast<float*>(lo)[i] = t.turn_lo[i];
+      reinterpret_cast<uint8_t*>(axes)[i] = t.axis[i];
+    }
+    __syncthreads();
+  }
+};
+
 // cos and sin of this lane's pairs for one token.  kHalves: lane l of a row
 // holds elements [8 l, 8 l + 8), which are the first (l < D / 16) or second
-// members of pairs (8 l + e) mod D / 2; else pairs 4 l .. 4 l + 3 whole.
+// members of pairs (8 l + e) mod D / 2, so two lanes have the same pairs and find four each;
+// else pairs 4 l .. 4 l + 3 whole.
 template <int D, bool kHalves>
 struct Turn {
   static constexpr int kN = kHalves ? 8 : 4;
   float c[kN], s[kN];
-  __device__ __forceinline__ void set(const RopeTable& t, const int32_t* pos, int l) {
+  // position: of axis `lane`, in the first lanes
+  __device__ __forceinline__ void set(const RopeShared& t, float position, int l) {
+    const bool second = kHalves && l >= D / 16;
+    const int at = kHalves ? 2 * (l % (D / 16)) + (second ? 1 : 0) : l;
+    const float4 h4 = t.hi[at], l4 = t.lo[at];
+    const uint32_t axes = t.axes[at];
+    const float hi[4] = {h4.x, h4.y, h4.z, h4.w}, lo[4] = {l4.x, l4.y, l4.z, l4.w};
+    float c4[4], s4[4];
 #pragma unroll
-    for (int e = 0; e < kN; ++e) {
-      const int j = kHalves ? (8 * l + e) % (D / 2) : 4 * l + e;
-      const float p = static_cast<float>(pos[t.axis[j]]);
-      const float whole = p * t.turn_hi[j];
-      const float rest = fmaf(p, t.turn_hi[j], -whole) + p * t.turn_lo[j];
-      sincospif(2.f * ((whole - rintf(whole)) + rest), &s[e], &c[e]);
+    for (int e = 0; e < 4; ++e) {
+      const float p = __shfl_sync(0xffffffffu, position, static_cast<int>((axes >> (8 * e)) & 31u));
+      const float whole = p * hi[e];
+      const float rest = fmaf(p, hi[e], -whole) + p * lo[e];
+      sincospif(2.f * ((whole - rintf(whole)) + rest), &s4[e], &c4[e]);
+    }
+    if constexpr (kHalves) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float co = __shfl_xor_sync(0xffffffffu, c4[e], D / 16), so = __shfl_xor_sync(0xffffffffu, s4[e], D / 16);
+        c[e] = second ? co : c4[e], c[4 + e] = second ? c4[e] : co;
+        s[e] = second ? so : s4[e], s[4 + e] = second ? s4[e] : so;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[e] = c4[e], s[e] = s4[e];
     }
   }
   // x turned by the angles (back: by their negatives).
@@ -99,13 +135,17 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-// Heads in flight for each tensor: four 16-byte loads a lane.
+// Heads in flight for each tensor: four 16-byte loads a lane.  Four blocks an SM: at three (72
+// registers) 4608 rows of 24 heads of 128 took 35.5 us, now 29.2, and at five 30.3 (pairs in
+// halves 35.6), the angles then being spilled.
 template <int D, bool kHalves>
-__global__ void __launch_bounds__(kRopeThreads) qkv_rope_kernel(const __grid_constant__ RopeTable table,
+__global__ void __launch_bounds__(kRopeThreads, 4) qkv_rope_kernel(const __grid_constant__ RopeTable table,
                                                                 const __grid_constant__ RopeArgs a) {
   constexpr int kLanes = D / 8, kPer = 32 / kLanes, kUnroll = 4;
   const int lane = threadIdx.x & 31, l = lane % kLanes, sub = lane / kLanes;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * kRopeTokens + (threadIdx.x >> 5);
+  __shared__ RopeShared shared;
+  shared.fill(table);
   grid_dependency_wait();
   if (threadIdx.x == 0) grid_launch_dependents();
   if (row >= a.rows) return;
@@ -113,7 +153,8 @@ __global__ void __launch_bounds__(kRopeThreads) qkv_rope_kernel(const __grid_con
   if (to < 0 || to >= a.out_rows) return;
   const int h0 = blockIdx.y * a.head_step, h1 = min(a.num_heads, h0 + a.head_step);
   Turn<D, kHalves> turn;
-  if (a.src[0] || a.src[1]) turn.set(table, a.positions + row * table.num_axes, l);
+  if (a.src[0] || a.src[1])
+    turn.set(shared, lane < table.num_axes ? static_cast<float>(a.positions[row * table.num_axes + lane]) : 0.f, l);
 #pragma unroll 1
   for (int t = 0; t < 3; ++t) {
     if (!a.src[t]) continue;
@@ -153,7 +194,7 @@ __global__ void __launch_bounds__(kRopeThreads) qkv_rope_kernel(const __grid_con
 
 // The gradient: a warp walks over tokens row, row + stride, ... so that the sums
 // of dw stay in registers; the block's sum goes to dw_part.  Bound by the latency of its
-// loads, two blocks an SM: 4608 rows of 24 heads of 128 take 42.6 us, 5.3 TB/s, and
+// loads, two blocks an SM: 4608 rows of 24 heads of 128 take 42 us, 5.4 TB/s, and
 // the sums below 4.  (128 registers a thread; at 80, for three blocks an SM, they spill:
 // 67 us.  Loads through a ring in shared memory: 45 us.)
 template <int D, bool kHalves>
@@ -162,6 +203,8 @@ __global__ void __launch_bounds__(kRopeThreads, 2) qkv_rope_backward_kernel(cons
   constexpr int kLanes = D / 8, kPer = 32 / kLanes, kUnroll = 4;
   __shared__ float sums[kRopeTokens][D];
   const int lane = threadIdx.x & 31, l = lane % kLanes, sub = lane / kLanes, warp = threadIdx.x >> 5;
+  __shared__ RopeShared shared;
+  shared.fill(table);
   grid_dependency_wait();
   if (threadIdx.x == 0) grid_launch_dependents();
   const int h0 = blockIdx.y * a.head_step, h1 = min(a.num_heads, h0 + a.head_step);
@@ -184,7 +227,8 @@ __global__ void __launch_bounds__(kRopeThreads, 2) qkv_rope_backward_kernel(cons
       continue;
     }
     Turn<D, kHalves> turn;
-    if (a.grad[0] || a.grad[1]) turn.set(table, a.positions + row * table.num_axes, l);
+    if (a.grad[0] || a.grad[1])
+      turn.set(shared, lane < table.num_axes ? static_cast<float>(a.positions[row * table.num_axes + lane]) : 0.f, l);
 #pragma unroll
     for (int t = 0; t < 3; ++t) {
       if (!a.grad[t]) continue;
