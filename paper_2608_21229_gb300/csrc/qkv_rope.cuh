@@ -136,8 +136,8 @@ __device__ __forceinline__ float row_sum(float x) {
 }
 
 // Heads in flight for each tensor: four 16-byte loads a lane.  Four blocks an SM: at three (72
-// registers) 4608 rows of 24 heads of 128 took 35.5 us, now 29.2, and at five 30.3 (pairs in
-// halves 35.6), the angles then being spilled.
+// registers) 4608 rows of 24 heads of 128 take 35.5 us, at four 29.2, at five (51 registers)
+// 30.3, and 35.6 with pairs in halves.
 template <int D, bool kHalves>
 __global__ void __launch_bounds__(kRopeThreads, 4) qkv_rope_kernel(const __grid_constant__ RopeTable table,
                                                                 const __grid_constant__ RopeArgs a) {

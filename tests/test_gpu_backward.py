@@ -281,6 +281,20 @@ def test_many_requests():
         ref.check(n, t)
 
 
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_no_live_rows_at_all(kernel):
+    """Cached rows that no query sees: zeros, or what was there."""
+    rcb.set_kernel(kernel)
+    c = Case(2, 128, [(7, 0, 0, 300), (0, 0, 0, 1)])
+    o, lse = torch.empty(0, 2, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(0, 2, device="cuda")
+    g = c.step_backward(o, lse)
+    assert (g["dk_ref"] == 0).all() and (g["dv_ref"] == 0).all()
+    held = [rnd(torch.Generator(device="cuda"), *c.ref_shape) for _ in range(2)]
+    into = [t.clone() for t in held]
+    c.step_backward(o, lse, into=into, accumulate=True)
+    assert all(torch.equal(a, b) for a, b in zip(into, held))
+
+
 def test_large_scores_and_zero_gradients():
     """Scores of hundreds (P is one-hot, its other weights underflow), and a do of zeros."""
     c = Case(2, 128, [(4, 8, 150, 200)], gain=40.0)
