@@ -63,9 +63,19 @@ struct BwdArgs {
   int* status;
   int *work_keys, *work_queries;  // tcgen05 kernels: counters of items, zero at launch (null: fixed order)
   int32_t behind_queries;         // keys kernel: launched right behind the queries kernel
+  uint64_t* passed;               // tcgen05 kernels: see kBwdPassed
+  uint64_t ticket;
 };
-// The workspace of a call: the statistics, then a pair of counters for each list of requests.
-constexpr int kBwdCounters = 256;
+// The workspace of a call: the statistics, then words that the pass over the outputs sets to
+// zero: a pair of counters for each list of requests, and in the last two the ticket with
+// which the queries kernel says that it has passed its wait for that pass.  The keys kernel
+// starts while the queries kernel runs, and griddepcontrol.wait would hold it until that has
+// ended; a ticket read with acquire orders it behind the release in the queries kernel, and
+// so behind all that this one's wait has made visible.  The ticket is the call's own (a random
+// sequence of 64 bits) and the keys kernel sets the word back to zero at its end, so that a
+// replayed graph never finds that of the replay before.  No ticket there: the keys kernel
+// waits in the ordinary way.
+constexpr int kBwdCounters = 256, kBwdPassed = kBwdCounters - 2;
 
 // Item `it` of a list: runs in the list's order (longest first), within a run
 // head by head, so that the CTAs that work at the same time share few heads' rows

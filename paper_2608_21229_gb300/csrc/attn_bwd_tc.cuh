@@ -35,9 +35,10 @@
 //
 // The queries kernel is launched first and the keys kernel as its programmatic
 // dependent: the keys kernel's CTAs take SMs as the queries kernel's leave, which they
-// need not wait for (its CTAs have all passed their own wait for the pass over the
-// outputs by then), only before their own end.  Items are handed out to whichever
-// pair is free.
+// need not wait for, only before their own end.  What both read (inputs, statistics,
+// counters) was there when the queries kernel passed its wait, which it says with a
+// ticket that the keys kernel's CTAs acquire (kBwdPassed).  Items are handed out to
+// whichever pair is free.
 //
 // What bounds them: at D = 128 the tensor pipe (with many tiles an item, under the power
 // cap), at D = 64 the score warps and as long a chain from one S to the next (arrivals,
@@ -290,10 +291,11 @@ __device__ __forceinline__ int64_t choose_item(int* work, int k, int cluster, in
   return k == 0 ? cluster : work ? static_cast<int64_t>(n_clusters) + atomicAdd(work, 1) : cluster + static_cast<int64_t>(k) * n_clusters;
 }
 
-// Returns false where the block has to leave (both CTAs of the pair alike).  late:
-// the wait for the kernel before this one is at the end (BwdArgs::behind_queries).
+// Returns false where the block has to leave (both CTAs of the pair alike).  says: this is
+// the queries kernel, which leaves its ticket behind its wait; late: the keys kernel behind
+// it (BwdArgs::behind_queries), whose wait is at its end when it finds the ticket.
 template <typename L>
-__device__ __forceinline__ bool enter(Cta<L>& c, uint8_t* smem, const BwdArgs& a, const BwdMaps& maps, bool late) {
+__device__ __forceinline__ bool enter(Cta<L>& c, uint8_t* smem, const BwdArgs& a, const BwdMaps& maps, bool says, bool late) {
   const uint32_t raw = smem_u32(smem);
   c.base = (raw + 1023u) & ~1023u;
   c.ptr = smem + (c.base - raw);
@@ -332,12 +334,18 @@ __device__ __forceinline__ bool enter(Cta<L>& c, uint8_t* smem, const BwdArgs& a
     tmem_relinquish_pair();
   }
   tc_fence_before();
-  __syncthreads();
+  const bool passed = __syncthreads_or(late && threadIdx.x == 0 && ld_acquire_gpu(a.passed) == a.ticket) != 0;
   cluster_sync();
   tc_fence_after();
   c.ctl = Ctl{abort_flag, a.timeout_ns, a.status};
-  if (!late) grid_dependency_wait();
-  if (threadIdx.x == 0) grid_launch_dependents();
+  if (passed)
+    fence_proxy_async_global();
+  else
+    grid_dependency_wait();
+  if (threadIdx.x == 0) {
+    if (says && blockIdx.x == 0) st_release_gpu(a.passed, a.ticket);
+    grid_launch_dependents();
+  }
   c.tmem = __shfl_sync(0xffffffffu, *holder, 0);
   return true;
 }
@@ -430,7 +438,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
   static_assert(kColK + D <= tc::kTmemCols, "tensor-memory layout");
   extern __shared__ uint8_t smem_raw[];
   Cta<L> c;
-  if (!enter(c, smem_raw, args, maps, args.behind_queries != 0)) return;
+  if (!enter(c, smem_raw, args, maps, false, args.behind_queries != 0)) return;
   const int cluster = static_cast<int>(blockIdx.x >> 1), n_clusters = static_cast<int>(gridDim.x >> 1);
   const int n_items = keys.n_tiles * args.num_heads;
   Loads loads;
@@ -769,7 +777,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
   scores_done:;
   }
   leave(c, loads);
-  if (args.behind_queries) grid_dependency_wait();  // the work after this kernel sees both
+  if (args.behind_queries) {
+    grid_dependency_wait();  // the work after this kernel sees both
+    // (a CTA that starts later and finds no ticket waits for nothing any more)
+    if (blockIdx.x == 0 && threadIdx.x == 0) *args.passed = 0;
+  }
 }
 
 template <int D>
@@ -781,7 +793,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
   constexpr uint32_t kColS = 0, kColP = 128, kColQ = 384;
   extern __shared__ uint8_t smem_raw[];
   Cta<L> c;
-  if (!enter(c, smem_raw, args, maps, false)) return;
+  if (!enter(c, smem_raw, args, maps, true, false)) return;
   const int cluster = static_cast<int>(blockIdx.x >> 1), n_clusters = static_cast<int>(gridDim.x >> 1);
   const int n_items = queries.n_tiles * args.num_heads;
   Loads loads;

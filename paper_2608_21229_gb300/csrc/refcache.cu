@@ -10,6 +10,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <chrono>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -894,6 +895,17 @@ int enter_device(refcache* h, DeviceInfo** info) {
 // ---------------------------------------------------------------- gradients
 constexpr int kBwdRequests = rc::kBwdMaxSegs / 2;  // requests of one launch (two runs of rows each)
 
+// A value for rc::kBwdPassed that no other call has: the splitmix64 generator (Steele, Lea, Flood 2014), started at the clock,
+// since a workspace may hold anything.
+uint64_t next_ticket() {
+  static const uint64_t start = static_cast<uint64_t>(std::chrono::steady_clock::now().time_since_epoch().count());
+  static std::atomic<uint64_t> calls{0};
+  uint64_t z = start + 0x9E3779B97F4A7C15ull * (calls.fetch_add(1) + 1);
+  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+  return (z ^ (z >> 31)) | 1;  // (never the zero of a word that was set back)
+}
+
 // What a request's rows see, for the two kernels of attn_bwd.cuh.
 struct BwdRequest {
   rc::BwdQuerySeg q[2];
@@ -995,6 +1007,8 @@ int run_backward(int batch, int H, int D, rc::BwdArgs a, const float* lse, const
     if (e != cudaSuccess) return cuda_fail(e, "attn_bwd_prep_kernel launch");
   }
   int* counters = reinterpret_cast<int*>(static_cast<float2*>(work) + a.rows * H);
+  a.passed = reinterpret_cast<uint64_t*>(counters + rc::kBwdPassed);
+  a.ticket = next_ticket();
   const bool mma = g_kernel.load() == REFCACHE_KERNEL_MMA_SYNC;
   const int tile = mma ? rc::mm::kBwdRows : rc::bwd::kBlock;
   rc::BwdMaps for_keys{}, for_queries{};
@@ -1028,7 +1042,7 @@ int run_backward(int batch, int H, int D, rc::BwdArgs a, const float* lse, const
       keys.n_tiles += (keys.seg[i].k_rows + tile - 1) / tile;
     }
     const int list = b0 / kBwdRequests;
-    if (a.rows > 0 && 2 * list + 1 < rc::kBwdCounters) {
+    if (a.rows > 0 && 2 * list + 1 < rc::kBwdPassed) {
       a.work_keys = counters + 2 * list;
       a.work_queries = counters + 2 * list + 1;
     } else {
