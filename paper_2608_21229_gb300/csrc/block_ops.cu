@@ -376,7 +376,7 @@ int refcache_gated_norm(const refcache_gated_norm_t* p, const void* x, const voi
   if (rows > 0 && ((rc = check_tensor(x, "x")) != 0 || (rc = check_optional(branch, "branch")) != 0 ||
                    (rc = check_optional(x_out, "x_out")) != 0 || (rc = check_optional(y, "y")) != 0))
     return rc;
-  if (x_out && !branch) return fail(REFCACHE_ERR_INVALID_ARG, "x_out without a branch");
+  if (rows > 0 && x_out && !branch) return fail(REFCACHE_ERR_INVALID_ARG, "x_out without a branch");
   int sms = 0;
   if ((rc = device_sms(&sms)) != 0) return rc;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -418,9 +418,10 @@ int refcache_gated_norm_backward(const refcache_gated_norm_t* p, const void* x_o
                    (rc = check_optional(dx, "dx")) != 0 || (rc = check_optional(d_branch, "d_branch")) != 0 ||
                    (rc = check_tensor(work, "work")) != 0))
     return rc;
-  if (!branch && (d_branch || d_gate || d_post_weight))
+  // (a tensor without rows may well be NULL)
+  if (rows > 0 && !branch && (d_branch || d_gate || d_post_weight))
     return fail(REFCACHE_ERR_INVALID_ARG, "gradients of the branch, its gate or its norm without a branch");
-  if (!dy && !dx_out) return fail(REFCACHE_ERR_INVALID_ARG, "neither dy nor dx_out");
+  if (rows > 0 && !dy && !dx_out) return fail(REFCACHE_ERR_INVALID_ARG, "neither dy nor dx_out");
   if ((d_weight && !p->weight) || (d_post_weight && !p->post_weight))
     return fail(REFCACHE_ERR_INVALID_ARG, "the gradient of a weight that is not there");
   if ((rc = check_floats({d_gate, d_scale, d_shift, d_weight, d_post_weight}, "gated_norm_backward")) != 0) return rc;
