@@ -498,8 +498,9 @@ REFCACHE_API int refcache_gated_norm_backward(const refcache_gated_norm_t* p, co
  * (norm + 1e-6)).  The lists are HOST arrays: device pointers, element counts, and
  * types[i] = REFCACHE_CLIP_* flags.  Tensors need the alignment of their elements
  * only.  out NULL: in place (nothing is written where the factor is 1).  norm: device
- * fp32, may be NULL.  max_norm may be +inf (the norm alone).  A norm that is NaN
- * makes the outputs NaN; an infinite one makes finite elements 0.  (Squares are summed
+ * fp32, may be NULL.  max_norm may be +inf: the norm alone, with out = grads whatever it
+ * is.  Under a finite bound a norm that is NaN makes the outputs NaN, and an infinite
+ * one makes finite elements 0.  (Squares are summed
  * in fp32 per thread and in fp64 from there on: the norm is infinite where a
  * thread's squares overflow fp32.)  work: refcache_clip_gradients_bytes(n) bytes of
  * device memory, 16-byte aligned.

@@ -1,7 +1,8 @@
 // clip_grads.cuh -- the global norm of many gradient tensors, and the tensors
 // scaled so that it is at most max_norm:
 //
-//   norm = sqrt(sum of squares over all tensors),  out = g * min(1, max_norm / (norm + 1e-6))
+//   norm = sqrt(sum of squares over all tensors),  out = g * min(1, max_norm / (norm + 1e-6)),
+//   out = g for an infinite max_norm
 //
 // Bound by memory: the tensors are read for the norm, read again to be scaled,
 // and written.  The second pass takes the pieces in the opposite order, so that
@@ -129,7 +130,8 @@ __global__ void __launch_bounds__(kClipThreads, 4) clip_scale_kernel(const __gri
   const float nrm = static_cast<float>(sqrt(total));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = nrm;
   const float ratio = max_norm / (nrm + 1e-6f);
-  const float coef = ratio < 1.f || isnan(ratio) ? ratio : 1.f;
+  // (an infinite bound bounds nothing, whatever the norm)
+  const float coef = !isinf(max_norm) && (ratio < 1.f || isnan(ratio)) ? ratio : 1.f;
   if (in_place && coef == 1.f) return;
   const int pieces = t.piece0[t.n];
   int tensor = max(0, t.n - 1);

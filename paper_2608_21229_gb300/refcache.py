@@ -710,7 +710,7 @@ def gated_norm_backward(cu_rows, x_out, dy, dx, branch=None, dx_out=None, d_bran
 def clip_gradients(grads, max_norm, out=None, norm=None, stream=None):
     """Scales gradients (bf16 or float32 tensors of any shapes) so that their global norm is at most ``max_norm``, in
     place or into the tensors ``out``; returns the norm before (float32, on the GPU; ``norm`` if given).  max_norm
-    may be infinite: the norm alone."""
+    may be infinite: the norm alone, the gradients as they are."""
     if _torch is None:
         _use_torch()
     grads = list(grads)
