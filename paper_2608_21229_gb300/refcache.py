@@ -1,7 +1,8 @@
 """Thin ctypes binding of librefcache.so (include/refcache.h).
 
 Argument marshalling only: torch tensors are passed as raw device pointers,
-the current torch stream as the CUDA stream.  Every attention step runs in the
+the current torch stream as the CUDA stream.  A call's tensors are on one device,
+the cache's or else the current one.  Every attention step runs in the
 library's CUDA kernels; when the library is missing this module raises, it
 never falls back to another implementation.
 """
@@ -162,11 +163,35 @@ def _arr(vals: Optional[Sequence[int]]):
     return (ctypes.c_int32 * len(vals))(*[int(v) for v in vals])
 
 
-def _ptr(t) -> Optional[int]:
+def _device() -> int:
+    """The current device, on which calls without a cache launch (-2, no tensor's, where there is none)."""
+    global _get_device
+    if _get_device is None:
+        import torch
+
+        _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    try:
+        return _get_device()
+    except (AssertionError, RuntimeError):
+        return -2
+
+
+_get_device = None  # () -> the current device, once torch is in use
+
+
+def _elsewhere(t, device, name=None):
+    """The error of a tensor that is not on the device that the call runs on, whose kernels could not, or not in order, read it."""
+    what = "" if name is None else name + ": "
+    if not t.is_cuda:
+        return ValueError(what + "tensor must live on the GPU")
+    return ValueError(f"{what}tensor is on cuda:{t.get_device()}, the call runs on cuda:{device}")
+
+
+def _ptr(t, device, name=None) -> Optional[int]:
     if t is None:
         return None
-    if not t.is_cuda:
-        raise ValueError("tensor must live on the GPU")
+    if t.get_device() != device:
+        raise _elsewhere(t, device, name)
     if not t.is_contiguous():
         raise ValueError("tensor must be contiguous")
     return t.data_ptr()
@@ -200,8 +225,8 @@ def _check_thd(name, t, rows, H, D):
 _bf16 = None  # torch.bfloat16, once torch is in use
 
 
-def _thd_ptrs(named, rows, H, D):
-    """The device pointers of THD tensors, which _check_thd and _ptr check in
+def _thd_ptrs(named, rows, H, D, device):
+    """The device pointers of THD tensors on `device`, which _check_thd and _ptr check in
     this order.  The first line is what a good call runs: the separate checks
     took a third of the 11 us that the host spends on a small step."""
     global _bf16
@@ -211,13 +236,13 @@ def _thd_ptrs(named, rows, H, D):
         _bf16 = torch.bfloat16
     shape = (rows, H, D)
     for _, t in named:
-        if t is None or t.dtype is not _bf16 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        if t is None or t.dtype is not _bf16 or t.shape != shape or t.get_device() != device or not t.is_contiguous():
             break
     else:
         return [t.data_ptr() for _, t in named]
     for name, t in named:
         _check_thd(name, t, rows, H, D)
-    return [_ptr(t) for _, t in named]
+    return [_ptr(t, device, name) for name, t in named]
 
 
 def set_kernel(name: str) -> str:
@@ -380,9 +405,10 @@ class RefCache:
 
     def build(self, layer, q, k, v, o, lse=None, scale=None, stream=None):
         H, D, n = self.seg.num_heads, self.seg.head_dim, self.seg.static_rows
-        ptrs = _thd_ptrs((("q", q), ("k", k), ("v", v), ("o", o)), n, H, D)
+        device = self.mem.get_device()
+        ptrs = _thd_ptrs((("q", q), ("k", k), ("v", v), ("o", o)), n, H, D, device)
         scale = default_scale(D) if scale is None else scale
-        _check(load().refcache_build(self.h, layer, *ptrs, _ptr(lse), scale, _stream(stream)))
+        _check(load().refcache_build(self.h, layer, *ptrs, _ptr(lse, device, "lse"), scale, _stream(stream)))
 
     def build_in_slot(self, layer, q, k_anchor, v_anchor, o, lse=None, scale=None, stream=None):
         """The prefill of a layer whose cached rows' K/V the caller already
@@ -399,14 +425,16 @@ class RefCache:
         else:
             k_anchor = v_anchor = None
         scale = default_scale(D) if scale is None else scale
-        _check(load().refcache_build_in_slot(self.h, layer, _ptr(q), _ptr(k_anchor), _ptr(v_anchor), _ptr(o),
-                                             _ptr(lse), scale, _stream(stream)))
+        device = self.mem.get_device()
+        _check(load().refcache_build_in_slot(self.h, layer, *(_ptr(t, device) for t in (q, k_anchor, v_anchor, o, lse)), scale,
+                                             _stream(stream)))
 
     def step(self, layer, q, k, v, o, lse=None, scale=None, stream=None):
         H, D, n = self.seg.num_heads, self.seg.head_dim, self.seg.live_rows
-        ptrs = _thd_ptrs((("q", q), ("k", k), ("v", v), ("o", o)), n, H, D)
+        device = self.mem.get_device()
+        ptrs = _thd_ptrs((("q", q), ("k", k), ("v", v), ("o", o)), n, H, D, device)
         scale = default_scale(D) if scale is None else scale
-        _check(load().step_attention(self.h, layer, *ptrs, _ptr(lse), scale, _stream(stream)))
+        _check(load().step_attention(self.h, layer, *ptrs, _ptr(lse, device, "lse"), scale, _stream(stream)))
 
     def step_backward(self, layer, q, k, v, o, lse, d_o, dq, dk, dv, dk_ref=None, dv_ref=None, accumulate=False, scale=None,
                       stream=None):
@@ -414,7 +442,7 @@ class RefCache:
         they are None, dk_ref and dv_ref [cached rows, H, D] (``accumulate``: added to what these hold).  ``lse`` is
         the fp32 [live rows, H] that the step wrote."""
         H, D, n = self.seg.num_heads, self.seg.head_dim, self.seg.live_rows
-        ptrs, work = _backward_ptrs((q, k, v, o, lse, d_o, dq, dk, dv), n, H, D, stream)
+        ptrs, work = _backward_ptrs((q, k, v, o, lse, d_o, dq, dk, dv), n, H, D, self.mem.get_device(), stream)
         ref = (None, None) if dk_ref is None and dv_ref is None else self._ref_ptrs(dk_ref, dv_ref)
         scale = default_scale(D) if scale is None else scale
         _check(load().step_attention_backward(self.h, layer, *ptrs, *ref, 1 if accumulate else 0, work.data_ptr(), scale,
@@ -424,22 +452,23 @@ class RefCache:
         """Gradient of ``build``; dk_ref and dv_ref, the cached rows' gradients from ``step_backward``, are added to
         the cached rows' part of dk and dv unless they are None."""
         H, D, n = self.seg.num_heads, self.seg.head_dim, self.seg.static_rows
-        ptrs, work = _backward_ptrs((q, k, v, o, lse, d_o, dq, dk, dv), n, H, D, stream)
+        ptrs, work = _backward_ptrs((q, k, v, o, lse, d_o, dq, dk, dv), n, H, D, self.mem.get_device(), stream)
         ref = (None, None) if dk_ref is None and dv_ref is None else self._ref_ptrs(dk_ref, dv_ref)
         scale = default_scale(D) if scale is None else scale
         _check(load().refcache_build_backward(self.h, layer, *ptrs, *ref, work.data_ptr(), scale, _stream(stream)))
 
     def _ref_ptrs(self, dk_ref, dv_ref):
         n = self.seg.static_rows - (0 if self.mask_mode == "beyond_alt" else sum(self.seg.n_anchor))  # cached rows
-        return _thd_ptrs((("dk_ref", dk_ref), ("dv_ref", dv_ref)), n, self.seg.num_heads, self.seg.head_dim)
+        return _thd_ptrs((("dk_ref", dk_ref), ("dv_ref", dv_ref)), n, self.seg.num_heads, self.seg.head_dim, self.mem.get_device())
 
 
 def full_attention(cu_seqlens, q, k, v, o, lse=None, scale=None, stream=None):
     rows, H, D = q.shape
     cu = list(cu_seqlens)
-    ptrs = _thd_ptrs((("q", q), ("k", k), ("v", v), ("o", o)), cu[-1], H, D)
+    device = _device()
+    ptrs = _thd_ptrs((("q", q), ("k", k), ("v", v), ("o", o)), cu[-1], H, D, device)
     scale = default_scale(D) if scale is None else scale
-    _check(load().full_attention(len(cu) - 1, H, D, _arr(cu), *ptrs, _ptr(lse), scale, _stream(stream)))
+    _check(load().full_attention(len(cu) - 1, H, D, _arr(cu), *ptrs, _ptr(lse, device, "lse"), scale, _stream(stream)))
 
 
 def full_attention_noalloc(cu_seqlens, q, k, v, o, lse=None, scale=None, stream=None):
@@ -447,9 +476,10 @@ def full_attention_noalloc(cu_seqlens, q, k, v, o, lse=None, scale=None, stream=
     memory: the call allocates no device memory (see include/refcache.h)."""
     rows, H, D = q.shape
     cu = list(cu_seqlens)
-    ptrs = _thd_ptrs((("q", q), ("k", k), ("v", v), ("o", o)), cu[-1], H, D)
+    device = _device()
+    ptrs = _thd_ptrs((("q", q), ("k", k), ("v", v), ("o", o)), cu[-1], H, D, device)
     scale = default_scale(D) if scale is None else scale
-    _check(load().full_attention_noalloc(len(cu) - 1, H, D, _arr(cu), *ptrs, _ptr(lse), scale, _stream(stream)))
+    _check(load().full_attention_noalloc(len(cu) - 1, H, D, _arr(cu), *ptrs, _ptr(lse, device, "lse"), scale, _stream(stream)))
 
 
 # torch, bfloat16, float32 and int32, once torch is in use (an import statement in a
@@ -483,7 +513,7 @@ def _work(nbytes, like, stream):
 _BACKWARD = ("q", "k", "v", "o", "lse", "d_o", "dq", "dk", "dv")
 
 
-def _backward_ptrs(tensors, rows, H, D, stream):
+def _backward_ptrs(tensors, rows, H, D, device, stream):
     """The device pointers of a gradient call's tensors, in their order, and its workspace."""
     if _torch is None:
         _use_torch()
@@ -496,8 +526,8 @@ def _backward_ptrs(tensors, rows, H, D, stream):
     for t in tensors:
         if t is not lse and (t is None or t.dtype is not _bfloat16 or t.shape != shape):
             _check_thd(_BACKWARD[len(ptrs)], t, rows, H, D)
-        if not t.is_cuda or not t.is_contiguous():
-            _ptr(t)
+        if t.get_device() != device or not t.is_contiguous():
+            _ptr(t, device, _BACKWARD[len(ptrs)])
         ptrs.append(t.data_ptr())
     return ptrs, _work(load().refcache_backward_bytes(rows, H), lse, stream)
 
@@ -506,7 +536,7 @@ def full_attention_backward(cu_seqlens, q, k, v, o, lse, d_o, dq, dk, dv, scale=
     """Gradient of ``full_attention`` (of either allocation variant)."""
     _, H, D = q.shape
     cu = list(cu_seqlens)
-    ptrs, work = _backward_ptrs((q, k, v, o, lse, d_o, dq, dk, dv), cu[-1], H, D, stream)
+    ptrs, work = _backward_ptrs((q, k, v, o, lse, d_o, dq, dk, dv), cu[-1], H, D, _device(), stream)
     scale = default_scale(D) if scale is None else scale
     _check(load().full_attention_backward(len(cu) - 1, H, D, _arr(cu), *ptrs, work.data_ptr(), scale, _stream(stream)))
 
@@ -527,7 +557,7 @@ class Rope:
 _NOTHING = 16  # the address of a tensor without elements, which torch gives as NULL; nothing is read or written there
 
 
-def _rows_apart(names, tensors, shape):
+def _rows_apart(names, tensors, shape, device):
     """For each tensor its pointer and the elements between its rows: [rows, H, D] bf16 whose rows are contiguous."""
     n, H, D = shape
     out = []
@@ -537,8 +567,8 @@ def _rows_apart(names, tensors, shape):
             continue
         if t.dtype is not _bfloat16 or t.shape != shape:
             raise ValueError(f"{name}: expected bf16 {list(shape)}, got {t.dtype} {tuple(t.shape)}")
-        if not t.is_cuda:
-            raise ValueError(f"{name}: tensor must live on the GPU")
+        if t.get_device() != device:
+            raise _elsewhere(t, device, name)
         s = t.stride()
         if s[2] != 1 or (s[1] != D and H > 1):
             raise ValueError(f"{name}: the heads of a row must be contiguous, got strides {s}")
@@ -546,20 +576,20 @@ def _rows_apart(names, tensors, shape):
     return out
 
 
-def _rows_packed(names, tensors, shape):
+def _rows_packed(names, tensors, shape, device):
     out = []
     for name, t in zip(names, tensors):
         if t is None:
             out.append(None)
             continue
-        if t.dtype is not _bfloat16 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        if t.dtype is not _bfloat16 or t.shape != shape or t.get_device() != device or not t.is_contiguous():
             _check_thd(name, t, *shape)
-            _ptr(t)
+            _ptr(t, device, name)
         out.append(t.data_ptr() or _NOTHING)
     return out
 
 
-def _param(name, t, n, f32):
+def _param(name, t, n, f32, device):
     """The pointer of a contiguous [n] parameter in bf16 or fp32, and whether it is fp32 (``f32``: that of one before)."""
     if t is None:
         return None, f32
@@ -568,18 +598,18 @@ def _param(name, t, n, f32):
         raise ValueError(f"{name}: expected bf16 or float32 [{n}], got {t.dtype} {tuple(t.shape)}")
     if f32 is not None and f32 != is32:
         raise ValueError(f"{name}: the parameters of one call have one type")
-    return _ptr(t), is32
+    return _ptr(t, device, name), is32
 
 
-def _rope_rows(rope, positions, shape, out_rows, wq, wk, rows, eps):
+def _rope_rows(rope, positions, shape, out_rows, wq, wk, rows, eps, device):
     n, H, _ = shape
     if positions.dtype is not _int32 or positions.shape != (n, len(rope.axes)):
         raise ValueError(f"positions: expected int32 [{n}, {len(rope.axes)}], got {positions.dtype} {tuple(positions.shape)}")
     if rows is not None and (rows.dtype is not _int32 or rows.shape != (n,)):
         raise ValueError(f"rows: expected int32 [{n}], got {rows.dtype} {tuple(rows.shape)}")
-    pq, f32 = _param("weight_q", wq, rope.head_dim, None)
-    pk, f32 = _param("weight_k", wk, rope.head_dim, f32)
-    return _RopeRows(n, out_rows, H, 1 if f32 else 0, _ptr(positions), _ptr(rows), pq, pk, eps)
+    pq, f32 = _param("weight_q", wq, rope.head_dim, None, device)
+    pk, f32 = _param("weight_k", wk, rope.head_dim, f32, device)
+    return _RopeRows(n, out_rows, H, 1 if f32 else 0, _ptr(positions, device, "positions"), _ptr(rows, device, "rows"), pq, pk, eps)
 
 
 def _shape_of(what, a, b, c):
@@ -600,10 +630,10 @@ def qkv_rope(rope, positions, q, k, v, q_out, k_out, v_out, weight_q=None, weigh
         _use_torch()
     n, H, _ = _shape_of("qkv_rope", q, k, v)
     out = _shape_of("qkv_rope's outputs", q_out, k_out, v_out)[0]
-    D = rope.head_dim
-    r = _rope_rows(rope, positions, (n, H, D), out, weight_q, weight_k, rows, eps)
-    src = _rows_apart(("q", "k", "v"), (q, k, v), (n, H, D))
-    dst = _rows_packed(("q_out", "k_out", "v_out"), (q_out, k_out, v_out), (out, H, D))
+    D, device = rope.head_dim, _device()
+    r = _rope_rows(rope, positions, (n, H, D), out, weight_q, weight_k, rows, eps, device)
+    src = _rows_apart(("q", "k", "v"), (q, k, v), (n, H, D), device)
+    dst = _rows_packed(("q_out", "k_out", "v_out"), (q_out, k_out, v_out), (out, H, D), device)
     _check(load().refcache_qkv_rope(rope._ref, ctypes.byref(r), *src, *dst, _stream(stream)))
 
 
@@ -615,24 +645,24 @@ def qkv_rope_backward(rope, positions, q, k, dq_out, dk_out, dv_out, dq, dk, dv,
         _use_torch()
     n, H, _ = _shape_of("qkv_rope_backward", dq, dk, dv)
     out = _shape_of("qkv_rope_backward's inputs", dq_out, dk_out, dv_out)[0]
-    D = rope.head_dim
-    r = _rope_rows(rope, positions, (n, H, D), out, weight_q, weight_k, rows, eps)
-    src = _rows_apart(("q", "k"), (q, k), (n, H, D))
-    grad = _rows_packed(("dq_out", "dk_out", "dv_out"), (dq_out, dk_out, dv_out), (out, H, D))
-    dst = _rows_apart(("dq", "dk", "dv"), (dq, dk, dv), (n, H, D))
+    D, device = rope.head_dim, _device()
+    r = _rope_rows(rope, positions, (n, H, D), out, weight_q, weight_k, rows, eps, device)
+    src = _rows_apart(("q", "k"), (q, k), (n, H, D), device)
+    grad = _rows_packed(("dq_out", "dk_out", "dv_out"), (dq_out, dk_out, dv_out), (out, H, D), device)
+    dst = _rows_apart(("dq", "dk", "dv"), (dq, dk, dv), (n, H, D), device)
     L = load()
     dw, work = [], None
     for name, t in (("dweight_q", dweight_q), ("dweight_k", dweight_k)):
         if t is not None and (t.dtype is not _float32 or t.shape != (D,)):
             raise ValueError(f"{name}: expected float32 [{D}], got {t.dtype} {tuple(t.shape)}")
-        dw.append(_ptr(t))
+        dw.append(_ptr(t, device, name))
     if weight_q is not None or weight_k is not None:
         work = _work(L.refcache_qkv_rope_backward_bytes(rope._ref), positions, stream)
     _check(L.refcache_qkv_rope_backward(rope._ref, ctypes.byref(r), *src, *grad, *dst, *dw, None if work is None else work.data_ptr(),
                                         _stream(stream)))
 
 
-def _norm_params(cu_rows, width, gate, scale, shift, weight, post_weight, norm, post_norm, eps):
+def _norm_params(cu_rows, width, gate, scale, shift, weight, post_weight, norm, post_norm, eps, device):
     cu = list(cu_rows)
     batch = len(cu) - 1
     shape, f32, ptrs, lds = (batch, width), None, [], []
@@ -646,18 +676,20 @@ def _norm_params(cu_rows, width, gate, scale, shift, weight, post_weight, norm, 
             raise ValueError(f"{name}: expected bf16 or float32 {list(shape)}, got {t.dtype} {tuple(t.shape)}")
         if f32 is not None and f32 != is32:
             raise ValueError(f"{name}: the parameters of one call have one type")
+        if t.get_device() != device:
+            raise _elsewhere(t, device, name)
         s = t.stride()
-        if not t.is_cuda or s[1] != 1:
-            raise ValueError(f"{name}: must live on the GPU, its rows contiguous")
+        if s[1] != 1:
+            raise ValueError(f"{name}: its rows must be contiguous")
         f32 = is32
         ptrs.append(t.data_ptr())
         lds.append(s[0] if batch > 1 else width)
-    w, f32 = _param("weight", weight, width, f32)
-    pw, f32 = _param("post_weight", post_weight, width, f32)
+    w, f32 = _param("weight", weight, width, f32, device)
+    pw, f32 = _param("post_weight", post_weight, width, f32, device)
     return _GatedNorm(batch, width, _arr(cu), NORMS[norm], NORMS[post_norm], 1 if f32 else 0, eps, *ptrs, *lds, w, pw)
 
 
-def _row_ptrs(names, tensors, shape):
+def _row_ptrs(names, tensors, shape, device):
     out = []
     for name, t in zip(names, tensors):
         if t is None:
@@ -665,7 +697,7 @@ def _row_ptrs(names, tensors, shape):
             continue
         if t.dtype is not _bfloat16 or t.shape != shape:
             raise ValueError(f"{name}: expected bf16 {list(shape)}, got {t.dtype} {tuple(t.shape)}")
-        out.append(_ptr(t))
+        out.append(_ptr(t, device, name))
     return out
 
 
@@ -676,9 +708,9 @@ def gated_norm(cu_rows, x, y=None, branch=None, x_out=None, gate=None, scale=Non
     each request of ``cu_rows``, rows may lie apart or be one expanded row; norms "layer", "rms" or None."""
     if _torch is None:
         _use_torch()
-    width = x.shape[1]
-    c = _norm_params(cu_rows, width, gate, scale, shift, weight, post_weight, norm, post_norm, eps)
-    ptrs = _row_ptrs(("x", "branch", "x_out", "y"), (x, branch, x_out, y), (cu_rows[-1], width))
+    width, device = x.shape[1], _device()
+    c = _norm_params(cu_rows, width, gate, scale, shift, weight, post_weight, norm, post_norm, eps, device)
+    ptrs = _row_ptrs(("x", "branch", "x_out", "y"), (x, branch, x_out, y), (cu_rows[-1], width), device)
     _check(load().refcache_gated_norm(ctypes.byref(c), *ptrs, _stream(stream)))
 
 
@@ -693,15 +725,15 @@ def gated_norm_backward(cu_rows, x_out, dy, dx, branch=None, dx_out=None, d_bran
     like = dy if dy is not None else dx_out
     if like is None:
         raise ValueError("gated_norm_backward needs dy or dx_out")
-    width = like.shape[1]
-    c = _norm_params(cu_rows, width, gate, scale, None, weight, post_weight, norm, post_norm, eps)
-    ptrs = _row_ptrs(("x_out", "branch", "dy", "dx_out", "dx", "d_branch"), (x_out, branch, dy, dx_out, dx, d_branch), (cu_rows[-1], width))
+    width, device = like.shape[1], _device()
+    c = _norm_params(cu_rows, width, gate, scale, None, weight, post_weight, norm, post_norm, eps, device)
+    ptrs = _row_ptrs(("x_out", "branch", "dy", "dx_out", "dx", "d_branch"), (x_out, branch, dy, dx_out, dx, d_branch), (cu_rows[-1], width), device)
     sums = []
     for name, t in (("d_gate", d_gate), ("d_scale", d_scale), ("d_shift", d_shift), ("d_weight", d_weight), ("d_post_weight", d_post_weight)):
         shape = (c.batch, width) if len(sums) < 3 else (width,)
         if t is not None and (t.dtype is not _float32 or t.shape != shape):
             raise ValueError(f"{name}: expected float32 {list(shape)}, got {t.dtype} {tuple(t.shape)}")
-        sums.append(_ptr(t))
+        sums.append(_ptr(t, device, name))
     L, ref = load(), ctypes.byref(c)
     work = _work(L.refcache_gated_norm_backward_bytes(ref), like, stream)
     _check(L.refcache_gated_norm_backward(ref, *ptrs, *sums, work.data_ptr(), _stream(stream)))
@@ -722,10 +754,13 @@ def clip_gradients(grads, max_norm, out=None, norm=None, stream=None):
     if outs is not None and [o.numel() for o in outs] != counts:
         i, o = next((i, o) for i, (m, o) in enumerate(zip(counts, outs)) if o.numel() != m)
         raise ValueError(f"gradient {i}: {counts[i]} elements and an output of {o.numel()}")
+    device = _device()
     for tensors in (grads,) if outs is None else (grads, outs):
         for i, t in enumerate(tensors):
-            if not (t.is_cuda and t.is_contiguous()):
-                raise ValueError(f"gradient {i}: tensors must live on the GPU and be contiguous")
+            if t.get_device() != device:
+                raise _elsewhere(t, device, f"gradient {i}")
+            if not t.is_contiguous():
+                raise ValueError(f"gradient {i}: tensors must be contiguous")
     kind = {_bfloat16: 0, _float32: 1}
     try:
         types = [kind[g.dtype] for g in grads]
@@ -733,14 +768,15 @@ def clip_gradients(grads, max_norm, out=None, norm=None, stream=None):
     except KeyError as e:
         raise ValueError(f"gradients: expected bf16 or float32, got {e.args[0]}") from None
     if norm is None:
-        norm = _empty((), _float32, grads[0].device if grads else _torch.device("cuda", _torch.cuda.current_device()), stream)
+        norm = _empty((), _float32, _torch.device("cuda", device), stream)
     elif norm.dtype is not _float32 or norm.numel() != 1:
         raise ValueError(f"norm: expected one float32, got {norm.dtype} {tuple(norm.shape)}")
+    norm_ptr = _ptr(norm, device, "norm")
     L = load()
     work = _work(L.refcache_clip_gradients_bytes(n), norm, stream)
     # (arrays of the array module: ctypes' took half of the time that a tensor costs)
     lists = [array("Q", [g.data_ptr() for g in grads]), None if outs is None else array("Q", [o.data_ptr() for o in outs]),
              array("q", counts), array("i", types)]
-    _check(L.refcache_clip_gradients(n, *[None if a is None else a.buffer_info()[0] for a in lists], max_norm, _ptr(norm),
+    _check(L.refcache_clip_gradients(n, *[None if a is None else a.buffer_info()[0] for a in lists], max_norm, norm_ptr,
                                      work.data_ptr(), _stream(stream)))
     return norm
