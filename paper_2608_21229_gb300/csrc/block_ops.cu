@@ -506,6 +506,13 @@ int refcache_clip_gradients(int n, const void* const* grads, void* const* out, c
       return fail(REFCACHE_ERR_INVALID_ARG, "tensor %d is not aligned to its elements", i);
     if (!out && gs != os) return fail(REFCACHE_ERR_INVALID_ARG, "types[%d]: a tensor in place keeps its type", i);
   }
+  // (of every launch, before the first)
+  auto pieces_of = [](int64_t count) { return count / rc::kClipPiece + (count % rc::kClipPiece != 0); };
+  for (int b = 0; b < n; b += rc::kClipMaxTensors) {
+    int64_t pieces = 0;  // (512 times 2^63 / 2^14 at most)
+    for (int i = b; i < std::min(n, b + rc::kClipMaxTensors); ++i) pieces += pieces_of(counts[i]);
+    if (pieces >= (1ll << 31) - 1) return fail(REFCACHE_ERR_INVALID_ARG, "clip_gradients: too many elements");
+  }
   int sms = 0;
   if ((rc = device_sms(&sms)) != 0) return rc;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -520,7 +527,7 @@ int refcache_clip_gradients(int n, const void* const* grads, void* const* out, c
       t.count[k] = counts[i];
       t.types[k] = static_cast<uint8_t>(types[i]);
       t.piece0[k] = static_cast<int32_t>(pieces);
-      pieces = std::min<int64_t>(pieces + (counts[i] + rc::kClipPiece - 1) / rc::kClipPiece, (1ll << 31) - 1);
+      pieces += pieces_of(counts[i]);
     }
     t.piece0[t.n] = static_cast<int32_t>(pieces);
     return t;
@@ -532,7 +539,6 @@ int refcache_clip_gradients(int n, const void* const* grads, void* const* out, c
   for (int b = 0; b < n; b += rc::kClipMaxTensors) {
     const rc::ClipTable t = table(b);
     const int pieces = t.piece0[t.n];
-    if (pieces == (1ll << 31) - 1) return fail(REFCACHE_ERR_INVALID_ARG, "clip_gradients: too many elements");
     if (pieces == 0) continue;
     // (Pieces are dealt out in a fixed order, for the sums' sake; up to four rounds of blocks
     // even out the SMs' speeds: 906 M elements 811 us with one, 794 with four.)
