@@ -480,8 +480,8 @@ REFCACHE_API int refcache_gated_norm(const refcache_gated_norm_t* p, const void*
  * branch), needed with dy; dy, dx_out: gradients of y and x_out, either may be
  * NULL for zero, not both.  Written, each unless NULL: dx, d_branch [rows, width] bf16;
  * d_gate, d_scale, d_shift fp32 [batch, width]; d_weight, d_post_weight fp32 [width].
- * Without rows (cu_rows[batch] = 0) any tensor of rows may be NULL, and the parameters'
- * gradients are zeros.
+ * A request without rows has gradients of zero and adds nothing to the weights', whatever
+ * its gate and scale hold; without any rows all tensors of rows may be NULL.
  * The statistics are found again from x_out and branch.  Column sums are fp32, in a
  * fixed order for a given device.  work: refcache_gated_norm_backward_bytes(p)
  * bytes of device memory, 16-byte aligned.

@@ -447,10 +447,15 @@ __device__ __forceinline__ float load_param(const void* p, int64_t i, bool f32) 
 }
 
 // The result of one request and column: sum k (A, B, G) is v.  Returns what it adds to the
-// weight's gradient.
-__device__ __forceinline__ float norm_param_grad(const NormSumArgs& a, int k, int s, int col, float v) {
+// weight's gradient: nothing for a request without rows, whatever its gate and scale hold.
+__device__ __forceinline__ float norm_param_grad(const NormSumArgs& a, int k, int s, int col, bool rows, float v) {
   const int64_t at = static_cast<int64_t>(s) * a.width + col;
   const bool f32 = a.mod_f32 != 0;
+  if (!rows) {
+    float* to = k == 0 ? a.d_shift : k == 1 ? a.d_scale : a.d_gate;
+    if (to) to[at] = 0.f;
+    return 0.f;
+  }
   if (k == 0) {
     if (a.d_shift) a.d_shift[at] = v;
     return 0.f;
@@ -511,7 +516,7 @@ __global__ void __launch_bounds__(kSumThreads) norm_param_grad_kernel(const __gr
       float v = 0.f;
 #pragma unroll
       for (int w = 0; w < kSumWarps; ++w) v += reinterpret_cast<const float*>(sums[w])[tid];
-      total += norm_param_grad(a, k, s, mine, v);
+      total += norm_param_grad(a, k, s, mine, segs.cu[s + 1] > segs.cu[s], v);
     }
     __syncthreads();
   }
@@ -530,7 +535,8 @@ __global__ void __launch_bounds__(kSumThreads) norm_param_grad_few_kernel(const 
   float4 total = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int s = kSumWarps * blockIdx.z + warp; on && s < segs.n; s += kSumWarps * gridDim.z) {
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (segs.cu[s + 1] > segs.cu[s]) {
+    const bool rows = segs.cu[s + 1] > segs.cu[s];
+    if (rows) {
       const int b0 = segs.cu[s] / a.rows_per_block, b1 = (segs.cu[s + 1] - 1) / a.rows_per_block;
       const float* p = a.part + (static_cast<int64_t>(s) * 3 + k) * a.width + col;
 #pragma unroll 4
@@ -539,10 +545,10 @@ __global__ void __launch_bounds__(kSumThreads) norm_param_grad_few_kernel(const 
         sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
       }
     }
-    total.x += norm_param_grad(a, k, s, col, sum.x);
-    total.y += norm_param_grad(a, k, s, col + 1, sum.y);
-    total.z += norm_param_grad(a, k, s, col + 2, sum.z);
-    total.w += norm_param_grad(a, k, s, col + 3, sum.w);
+    total.x += norm_param_grad(a, k, s, col, rows, sum.x);
+    total.y += norm_param_grad(a, k, s, col + 1, rows, sum.y);
+    total.z += norm_param_grad(a, k, s, col + 2, rows, sum.z);
+    total.w += norm_param_grad(a, k, s, col + 3, rows, sum.w);
   }
   sums[warp][lane] = total;
   __syncthreads();
