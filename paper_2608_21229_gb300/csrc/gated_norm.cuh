@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_kernel(co
   const int tid = threadIdx.x;
   const bool last = (tid + (kNV - 1) * kThreads) * 8 < a.width;
   const bool f32 = a.mod_f32 != 0;
-  const int r0 = blockIdx.x * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
+  const int r0 = blockIdx.x * a.rows_per_block, r1 = r0 + min(a.rows - r0, a.rows_per_block);  // (the sum of the two may pass 2^31)
   const float inv_w = 1.f / static_cast<float>(a.width);
   BlockSum<kThreads / 32> sum{slots};
   constexpr uint32_t kVec = 16u * kThreads;  // bytes between a thread's vectors
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) gated_norm_backward_
   const int tid = threadIdx.x;
   const bool last = (tid + (kNV - 1) * kThreads) * 8 < a.width;
   const bool f32 = a.mod_f32 != 0;
-  const int r0 = blockIdx.x * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
+  const int r0 = blockIdx.x * a.rows_per_block, r1 = r0 + min(a.rows - r0, a.rows_per_block);  // (the sum of the two may pass 2^31)
   const float inv_w = 1.f / static_cast<float>(a.width);
   BlockSum<kThreads / 32> sum{slots};
   constexpr uint32_t kVec = 16u * kThreads;  // bytes between a thread's vectors
