@@ -544,7 +544,11 @@ REFCACHE_API int refcache_set_kernel(int kernel);
  * non-zero, the next launch's TMA producer skips its first K-tile load, so
  * the consumers' bounded waits run out and the kernel reports
  * REFCACHE_ERR_TIMEOUT through refcache_status() instead of hanging.  The
- * switch clears itself after one launch.  Only the tcgen05 kernel has it.
+ * switch clears itself after one call.  Only the tcgen05 kernels have it.
+ *
+ * In a gradient call, bits 0-7 are the load before which a producer stops (1: it
+ * loads nothing), of the queries kernel, or of the keys kernel with bit 8, in the
+ * first CTA of each pair, or in the second with bit 9.
  */
 REFCACHE_API void refcache_debug_skip_first_load(int on);
 

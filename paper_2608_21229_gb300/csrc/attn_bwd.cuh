@@ -63,6 +63,7 @@ struct BwdArgs {
   int* status;
   int *work_keys, *work_queries;  // tcgen05 kernels: counters of items, zero at launch (null: fixed order)
   int32_t behind_queries;         // keys kernel: launched right behind the queries kernel
+  int32_t dbg_stop;               // tcgen05 kernels: refcache_debug_skip_first_load's argument
   uint64_t* passed;               // tcgen05 kernels: see kBwdPassed
   uint64_t ticket;
 };

@@ -367,6 +367,10 @@ __device__ __forceinline__ void load_half(uint32_t dst, const CUtensorMap* m, ui
 // Loads that a CTA's producer has issued, by ring: X, Y, rows of S, rows of dP, columns.
 struct Loads {
   int n[5] = {0, 0, 0, 0, 0};
+  int left;  // until the producer stops: all of them, but for fault injection
+  __device__ __forceinline__ Loads(int stop, bool keys, uint32_t rank) {
+    left = stop != 0 && ((stop >> 8) & 1) == (keys ? 1 : 0) && static_cast<uint32_t>((stop >> 9) & 1) == rank ? (stop & 255) - 1 : 0x7fffffff;
+  }
 };
 
 // Teardown, after the roles (`loads` of the producer's lane 0).  As in
@@ -421,9 +425,11 @@ __device__ __forceinline__ void leave(const Cta<L>& c, const Loads& loads) {
 template <typename L>
 __device__ __forceinline__ int begin_load(const Cta<L>& c, Loads& loads, int ring, int slots, int full, int empty, uint32_t bytes, int where) {
   const int n = loads.n[ring], slot = n % slots;
+  if (loads.left == 0) return -1;
   if (n >= slots && !c.wait(empty + slot, n / slots - 1, where)) return -1;
   if (c.leader) mbar_arrive_expect_tx(c.bar(full + slot), 2 * bytes);
   ++loads.n[ring];
+  --loads.left;
   return slot;
 }
 }  // namespace bwd
@@ -441,7 +447,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
   if (!enter(c, smem_raw, args, maps, false, args.behind_queries != 0)) return;
   const int cluster = static_cast<int>(blockIdx.x >> 1), n_clusters = static_cast<int>(gridDim.x >> 1);
   const int n_items = keys.n_tiles * args.num_heads;
-  Loads loads;
+  Loads loads(args.dbg_stop, true, c.rank);
   if (c.warp == kProducerWarp) {
     if (c.lane == 0) {
       int s = 0;
@@ -796,7 +802,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
   if (!enter(c, smem_raw, args, maps, true, false)) return;
   const int cluster = static_cast<int>(blockIdx.x >> 1), n_clusters = static_cast<int>(gridDim.x >> 1);
   const int n_items = queries.n_tiles * args.num_heads;
-  Loads loads;
+  Loads loads(args.dbg_stop, false, c.rank);
   if (c.warp == kProducerWarp) {
     if (c.lane == 0) {
       Item t{}, next{};

@@ -1010,6 +1010,7 @@ int run_backward(int batch, int H, int D, rc::BwdArgs a, const float* lse, const
   a.passed = reinterpret_cast<uint64_t*>(counters + rc::kBwdPassed);
   a.ticket = next_ticket();
   const bool mma = g_kernel.load() == REFCACHE_KERNEL_MMA_SYNC;
+  a.dbg_stop = mma ? 0 : g_dbg_skip.exchange(0);
   const int tile = mma ? rc::mm::kBwdRows : rc::bwd::kBlock;
   rc::BwdMaps for_keys{}, for_queries{};
   if (!mma && a.rows > 0) {
@@ -1623,7 +1624,7 @@ int refcache_set_kernel(int kernel) {
   return g_kernel.exchange(kernel);
 }
 
-void refcache_debug_skip_first_load(int on) { g_dbg_skip.store(on ? 1 : 0); }
+void refcache_debug_skip_first_load(int on) { g_dbg_skip.store(on); }
 
 int refcache_ex2_rate(double* per_clk_per_sm, void* stream) {
   if (!per_clk_per_sm) return fail(REFCACHE_ERR_INVALID_ARG, "per_clk_per_sm is NULL");

@@ -255,8 +255,8 @@ def set_wait_timeout_ns(ns: int) -> int:
     return int(load().refcache_set_wait_timeout_ns(int(ns)))
 
 
-def debug_skip_first_load(on: bool = True) -> None:
-    load().refcache_debug_skip_first_load(1 if on else 0)
+def debug_skip_first_load(on: int = 1) -> None:
+    load().refcache_debug_skip_first_load(int(on))
 
 
 def status(stream=None) -> int:
