@@ -30,7 +30,6 @@ constexpr int kBwdMaxSegs = 64;
 struct BwdQuerySeg {
   int32_t q_row0, q_rows, a_row0, a_len, b_row0, b_len;
   int32_t tile0;  // first query tile of the launch
-  int32_t pad;
 };
 // A run of key rows (of the call's keys, or of the cache) that all of query rows
 // [q_row0, q_row0 + q_rows) see.  Row k_row0 + i with i >= add_from has the

@@ -104,12 +104,14 @@ struct Smem {
                             kC = kR2 + (kRApart ? kSlots * kHalf : 0), kStage = kC + kSlots * kCBytes,
                             kStat = kStage + (kKeys ? kScoreWarps * 4096 : 0);
   static constexpr uint32_t kBars = kStat + (kKeys ? kStatSlots * 1024 : 0);
-  // barriers; those of loads first: X, Y, rows of S, rows of dP, columns
-  static constexpr int kXFull = 0, kYFull = kXFull + kXSlots, kR1Full = kYFull + kYSlots, kR2Full = kR1Full + kSlots,
-                       kCFull = kR2Full + kSlots, kXEmpty = kCFull + kSlots, kYEmpty = kXEmpty + kXSlots, kR1Empty = kYEmpty + kYSlots,
-                       kR2Empty = kR1Empty + kSlots, kCEmpty = kR2Empty + kSlots, kSDone = kCEmpty + kSlots, kPDone = kSDone + kSBufs,
-                       kSHalf = kPDone + 2, kSUsed = kSHalf + 1, kDsFull = kSUsed + kSBufs, kAccFree = kDsFull + 2, kAccDone = kAccFree + 1,
-                       kStatFull = kAccDone + 1, kStatEmpty = kStatFull + kStatSlots, kItemFull = kStatEmpty + kStatSlots,
+  // barriers; those of loads first: X, Y, rows of S, rows of dP, columns (Y and rows of dP: where they are loads of their own)
+  static constexpr int kYLoads = kKeys ? 0 : kYSlots, kR2Loads = kRApart ? kSlots : 0;
+  static constexpr int kPBufs = kKeys ? 1 : 2, kHalves = kKeys && kSBufs == 1 ? 1 : 0, kStats = kKeys ? kStatSlots : 0;
+  static constexpr int kXFull = 0, kYFull = kXFull + kXSlots, kR1Full = kYFull + kYLoads, kR2Full = kR1Full + kSlots,
+                       kCFull = kR2Full + kR2Loads, kXEmpty = kCFull + kSlots, kYEmpty = kXEmpty + kXSlots, kR1Empty = kYEmpty + kYLoads,
+                       kR2Empty = kR1Empty + kSlots, kCEmpty = kR2Empty + kR2Loads, kSDone = kCEmpty + kSlots, kPDone = kSDone + kSBufs,
+                       kSHalf = kPDone + kPBufs, kSUsed = kSHalf + kHalves, kDsFull = kSUsed + kSBufs, kAccFree = kDsFull + kPBufs,
+                       kAccDone = kAccFree + 1, kStatFull = kAccDone + 1, kStatEmpty = kStatFull + kStats, kItemFull = kStatEmpty + kStats,
                        kItemEmpty = kItemFull + kItemSlots, kItemIn = kItemEmpty + kItemSlots, kItemPeer = kItemIn + kItemSlots,
                        kMmaDone = kItemPeer + kItemSlots, kNumBars = kMmaDone + 1;
   // warps that read each item from a CTA's ring: its producer, score (and statistics)
@@ -151,7 +153,7 @@ __device__ __forceinline__ uint64_t cols_desc(uint32_t addr) {
   return D == 64 ? sdesc_sw64(addr, 128 * D, 512) : sdesc_sw128(addr, 128 * D, 1024);
 }
 
-// 64 columns of this thread's lane, and their bf16 pairs back over the first 32.
+// 64 columns of this thread's lane.
 __device__ __forceinline__ void load64(uint32_t t, float (&s)[64]) {
   uint32_t r0[32], r1[32];
   tmem_ld32(t, r0);
@@ -412,9 +414,9 @@ __device__ __forceinline__ void leave(const Cta<L>& c, const Loads& loads) {
       }
     };
     settle(L::kXFull, 0, L::kXSlots, L::kXBytes);
-    settle(L::kYFull, 1, L::kYSlots, L::kOwn);
+    settle(L::kYFull, 1, L::kYLoads, L::kOwn);
     settle(L::kR1Full, 2, L::kSlots, L::kR1Bytes);
-    settle(L::kR2Full, 3, L::kSlots, L::kHalf);
+    settle(L::kR2Full, 3, L::kR2Loads, L::kHalf);
     settle(L::kCFull, 4, L::kSlots, L::kCBytes);
   }
   cluster_sync();

@@ -912,7 +912,7 @@ struct BwdRequest {
   rc::BwdKeySeg k[2];
   int nq = 0, nk = 0;
   void queries(int row0, int n, int a0, int na, int b0, int nb) {
-    if (n > 0) q[nq++] = rc::BwdQuerySeg{row0, n, a0, na, b0, nb, 0, 0};
+    if (n > 0) q[nq++] = rc::BwdQuerySeg{row0, n, a0, na, b0, nb, 0};
   }
   void keys(int row0, int n, int q0, int n_q, bool in_b, int add_from, int add_row0) {
     if (n > 0) k[nk++] = rc::BwdKeySeg{row0, n, q0, n_q, in_b ? 1 : 0, add_from, add_row0, 0};

@@ -42,7 +42,7 @@ __device__ __forceinline__ Vec8 load_param8(const void* p, int64_t i, bool f32) 
   }
   return unpack8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i));
 }
-// Loads and stores of data that is used once.
+// A load of data that is used once.
 __device__ __forceinline__ uint4 ld_stream(const void* p) { return __ldcs(static_cast<const uint4*>(p)); }
 
 // The same as four pairs, for the two-lane fp32 operations.
@@ -77,12 +77,6 @@ __device__ __forceinline__ float sum2(f32x2 a) {
   float lo, hi;
   split_f32x2(a, lo, hi);
   return lo + hi;
-}
-
-__device__ __forceinline__ float warp_sum(float x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  return x;
 }
 
 }  // namespace rc
