@@ -348,8 +348,10 @@ REFCACHE_API size_t refcache_backward_bytes(int64_t rows, int num_heads);
  * gradients of the live rows' own keys; dk_ref, dv_ref [cached rows, H, d] bf16
  * (the slots' row order, refcache_kv_ptr) those of the cached rows, or both NULL
  * when the cache takes no gradient (their work is then left out).  With
- * accumulate != 0 the call adds to what dk_ref and dv_ref hold (several denoising
- * steps of one rollout share a cache; the sum is rounded to bf16 at each call).
+ * accumulate != 0 the call adds to what dk_ref and dv_ref hold: several denoising
+ * steps of one rollout share a cache.  In bf16 that sum is rounded at each call, n
+ * times for n steps, and loses what is below 2^-9 of it; step_attention_backward_ref_f32
+ * holds it in fp32.
  * A bf16 cache; REFCACHE_ERR_UNSUPPORTED for an E4M3 cache, whose quantisation has
  * no gradient, REFCACHE_ERR_NOT_BUILT for a layer that was never built.
  */
@@ -357,6 +359,13 @@ REFCACHE_API int step_attention_backward(refcache_t* cache, int layer, const voi
                                          const void* v_live, const void* o_live, const float* lse_live,
                                          const void* do_live, void* dq_live, void* dk_live, void* dv_live, void* dk_ref,
                                          void* dv_ref, int accumulate, void* work, float softmax_scale, void* stream);
+
+/* The same with dk_ref and dv_ref in fp32. */
+REFCACHE_API int step_attention_backward_ref_f32(refcache_t* cache, int layer, const void* q_live, const void* k_live,
+                                                 const void* v_live, const void* o_live, const float* lse_live,
+                                                 const void* do_live, void* dq_live, void* dk_live, void* dv_live,
+                                                 float* dk_ref, float* dv_ref, int accumulate, void* work,
+                                                 float softmax_scale, void* stream);
 
 /*
  * Gradient of refcache_build: rows = cu_static[batch], under the cache's mask
@@ -370,6 +379,13 @@ REFCACHE_API int refcache_build_backward(refcache_t* cache, int layer, const voi
                                          const void* do_static, void* dq_static, void* dk_static, void* dv_static,
                                          const void* dk_ref, const void* dv_ref, void* work, float softmax_scale,
                                          void* stream);
+
+/* The same with dk_ref and dv_ref in fp32. */
+REFCACHE_API int refcache_build_backward_ref_f32(refcache_t* cache, int layer, const void* q_static, const void* k_static,
+                                                 const void* v_static, const void* o_static, const float* lse_static,
+                                                 const void* do_static, void* dq_static, void* dk_static, void* dv_static,
+                                                 const float* dk_ref, const float* dv_ref, void* work,
+                                                 float softmax_scale, void* stream);
 
 /* Gradient of full_attention (and full_attention_noalloc); capturable, allocates nothing. */
 REFCACHE_API int full_attention_backward(int batch, int num_heads, int head_dim, const int32_t* cu_seqlens,

@@ -14,8 +14,20 @@
 // memory would take 5), and in return no sum crosses CTAs: no atomics, no fp32
 // image of dQ in memory, and the same inputs give the same bits, as the forward
 // calls promise.
+//
+// Scores, dP, P and dS are fp32 and so are all sums.  P and dS are rounded to bf16 where
+// they become operands: a 16-bit MMA takes both of its operands in one type, and the
+// other one here (dO, Q or K) is bf16; in TF32 three of the seven products would run at half
+// the rate on operands of twice the size.  The gradients are then 0.0024 to 0.0026 from
+// those in 64 bits (relative 2-norm), where their own rounding to bf16 alone makes 0.0017 to 0.0019.
+//
+// The cached rows' gradients (kRef32) may also be fp32: what steps add to from call to call
+// then is not rounded to bf16 each time.  1280 queries, 3328 keys, 24 heads of 128: 120.6
+// us written in bf16 and 128.6 added, 127.5 and 142.4 in fp32.
 #pragma once
 #include <cuda_bf16.h>
+
+#include <type_traits>
 
 #include "attn_mma.cuh"
 #include "common.cuh"
@@ -50,8 +62,9 @@ struct BwdKeys {
 
 struct BwdArgs {
   const __nv_bfloat16 *q, *ka, *va, *kb, *vb, *d_o;
-  __nv_bfloat16 *dq, *dka, *dva, *dkb, *dvb;
-  const __nv_bfloat16 *add_k, *add_v;  // see BwdKeySeg
+  __nv_bfloat16 *dq, *dka, *dva;
+  void *dkb, *dvb;            // gradients of the cached rows, bf16 or (kRef32 kernels) fp32
+  const void *add_k, *add_v;  // see BwdKeySeg; of the same type
   const float2* stats;                 // [heads][rows]: (lse log2 e, delta) of each query row
   int64_t row_stride;                  // elements between rows (= H * D)
   int64_t rows;                        // query rows
@@ -195,7 +208,8 @@ __device__ __forceinline__ void add_weighted(float (&acc)[D / 8][4], const float
 }  // namespace mm
 
 // dK and dV of 64 keys (16 per warp): S^T = K Q^T and dP^T = V dO^T, 32 queries at a time.
-template <int D>
+// kRef32: the cached rows' gradients are fp32, here and in what is added.
+template <int D, bool kRef32>
 __global__ void __launch_bounds__(128) attn_bwd_mma_keys_kernel(const __grid_constant__ BwdKeys keys, const BwdArgs a) {
   using namespace mm;
   extern __shared__ __align__(128) uint8_t smem_mm[];
@@ -271,16 +285,28 @@ __global__ void __launch_bounds__(128) attn_bwd_mma_keys_kernel(const __grid_con
     const int64_t at = (sg.k_row0 + r) * ld + head * D;
     const bool add = r >= sg.add_from;
     const int64_t from = (static_cast<int64_t>(sg.add_row0) + r) * ld + head * D;
-    uint32_t* ok = reinterpret_cast<uint32_t*>((sg.in_b ? a.dkb : a.dka) + at);
-    uint32_t* ov = reinterpret_cast<uint32_t*>((sg.in_b ? a.dvb : a.dva) + at);
+    using Ref = std::conditional_t<kRef32, float, __nv_bfloat16>;
+    uint32_t* ok = reinterpret_cast<uint32_t*>((sg.in_b ? static_cast<__nv_bfloat16*>(a.dkb) : a.dka) + at);
+    uint32_t* ov = reinterpret_cast<uint32_t*>((sg.in_b ? static_cast<__nv_bfloat16*>(a.dvb) : a.dva) + at);
+    const Ref *add_k = static_cast<const Ref*>(a.add_k) + from, *add_v = static_cast<const Ref*>(a.add_v) + from;
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) {
       const int c = 4 * i + q4;
       float k0 = dk[i][2 * h] * a.scale, k1 = dk[i][2 * h + 1] * a.scale, v0 = dv[i][2 * h], v1 = dv[i][2 * h + 1];
       if (add) {
-        const uint32_t xk = reinterpret_cast<const uint32_t*>(a.add_k + from)[c], xv = reinterpret_cast<const uint32_t*>(a.add_v + from)[c];
-        k0 += __uint_as_float(xk << 16), k1 += __uint_as_float(xk & 0xFFFF0000u);
-        v0 += __uint_as_float(xv << 16), v1 += __uint_as_float(xv & 0xFFFF0000u);
+        if constexpr (kRef32) {
+          const float2 xk = reinterpret_cast<const float2*>(add_k)[c], xv = reinterpret_cast<const float2*>(add_v)[c];
+          k0 += xk.x, k1 += xk.y, v0 += xv.x, v1 += xv.y;
+        } else {
+          const uint32_t xk = reinterpret_cast<const uint32_t*>(add_k)[c], xv = reinterpret_cast<const uint32_t*>(add_v)[c];
+          k0 += __uint_as_float(xk << 16), k1 += __uint_as_float(xk & 0xFFFF0000u);
+          v0 += __uint_as_float(xv << 16), v1 += __uint_as_float(xv & 0xFFFF0000u);
+        }
+      }
+      if (kRef32 && sg.in_b) {
+        reinterpret_cast<float2*>(static_cast<float*>(a.dkb) + at)[c] = make_float2(k0, k1);
+        reinterpret_cast<float2*>(static_cast<float*>(a.dvb) + at)[c] = make_float2(v0, v1);
+        continue;
       }
       ok[c] = pack2(k0, k1);
       ov[c] = pack2(v0, v1);

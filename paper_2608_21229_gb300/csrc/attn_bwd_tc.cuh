@@ -167,8 +167,8 @@ __device__ __forceinline__ void load64(uint32_t t, float (&s)[64]) {
   }
 }
 
-// One warp's 32 rows x 64 columns (chunks [chunk0, chunk0 + 8) of 16 bytes of each
-// row) through shared memory, so that whole 128-byte lines are written.
+// One warp's 32 rows x 64 columns of bf16, or 32 of fp32 (eight chunks of 16 bytes of each
+// row), through shared memory, so that whole 128-byte lines are written.
 struct RowsOut {
   uint32_t stage;  // this warp's 4 KB
   int lane;
@@ -179,13 +179,14 @@ struct RowsOut {
     return ld_shared_v4(stage + 128u * lane + (static_cast<uint32_t>(chunk ^ (lane & 7)) << 4));
   }
   // rows [from, rows) of the warp come from src + row * stride, zeros elsewhere
-  __device__ __forceinline__ void fetch(const __nv_bfloat16* src, int64_t stride, int from, int rows) const {
+  template <typename T>
+  __device__ __forceinline__ void fetch(const T* src, int64_t stride, int from, int rows) const {
     const int r0 = lane >> 3, ch = lane & 7;
     uint4 v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int r = 4 * i + r0;
-      v[i] = r >= from && r < rows ? *reinterpret_cast<const uint4*>(src + r * stride + 8 * ch) : make_uint4(0, 0, 0, 0);
+      v[i] = r >= from && r < rows ? *reinterpret_cast<const uint4*>(src + r * stride + 16 / sizeof(T) * ch) : make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -195,14 +196,15 @@ struct RowsOut {
     __syncwarp();
   }
   // rows [0, rows) of the warp go to dst + row * stride
-  __device__ __forceinline__ void flush(__nv_bfloat16* dst, int64_t stride, int rows) const {
+  template <typename T>
+  __device__ __forceinline__ void flush(T* dst, int64_t stride, int rows) const {
     __syncwarp();
     const int r0 = lane >> 3, ch = lane & 7;
 #pragma unroll 4
     for (int i = 0; i < 8; ++i) {
       const int r = 4 * i + r0;
       const uint4 v = ld_shared_v4(stage + 128u * r + (static_cast<uint32_t>(ch ^ (r & 7)) << 4));
-      if (r < rows) *reinterpret_cast<uint4*>(dst + r * stride + 8 * ch) = v;
+      if (r < rows) *reinterpret_cast<uint4*>(dst + r * stride + 16 / sizeof(T) * ch) = v;
     }
     __syncwarp();
   }
@@ -436,7 +438,8 @@ __device__ __forceinline__ int begin_load(const Cta<L>& c, Loads& loads, int rin
 }
 }  // namespace bwd
 
-template <int D>
+// kRef32: the cached rows' gradients are fp32, here and in what is added (BwdArgs).
+template <int D, bool kRef32>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
     attn_bwd_keys_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant__ BwdKeys keys, const __grid_constant__ BwdArgs args) {
   using namespace bwd;
@@ -646,11 +649,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
     auto write_out = [&](const Item& m, int n) -> bool {
       const float scale = half ? args.scale : 1.f;
       const int64_t at = (static_cast<int64_t>(m.row0) + row) * args.row_stride + m.head * D;
-      __nv_bfloat16* out = (half ? (m.v[2] ? args.dkb : args.dka) : (m.v[2] ? args.dvb : args.dva)) + at;
+      using Ref = std::conditional_t<kRef32, float, __nv_bfloat16>;
+      void* const ref = half ? args.dkb : args.dvb;
+      __nv_bfloat16* const out = (m.v[2] ? static_cast<__nv_bfloat16*>(ref) : half ? args.dka : args.dva) + at;
       const int first = m.v[3] - row, rows = m.rows - row;  // of the warp's rows: from `first` on something is added
       const bool adds = first < min(32, rows);
-      const __nv_bfloat16* add =
-          (half ? args.add_k : args.add_v) + (static_cast<int64_t>(m.v[4]) + row) * args.row_stride + m.head * D;
+      const Ref* add = static_cast<const Ref*>(half ? args.add_k : args.add_v) + (static_cast<int64_t>(m.v[4]) + row) * args.row_stride + m.head * D;
       const RowsOut stage{c.base + L::kStage + 4096u * c.warp, c.lane};
       // (in whole lines through the stage, before the wait: from the registers, 16 bytes of
       // each of 32 rows at a time, it took 4000 cycles of an item)
@@ -667,12 +671,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
           __syncwarp();
           if (c.lane == 0) mbar_arrive_cluster(l_bars + 8u * L::kAccFree);
         }
+        if constexpr (kRef32) {  // 32 columns at a time
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            if (s > 0 && adds) {
+              __syncwarp();
+              stage.fetch(add + 64 * cc + 32, args.row_stride, first, rows);
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              const uint4 y = adds ? stage.get(q) : make_uint4(0, 0, 0, 0);  // (zeros where nothing is added)
+              float* x = v + 32 * s + 4 * q;
+              const uint32_t add4[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e)  // (the product rounded by itself, as below: the same sums as with bf16)
+                x[e] = __fadd_rn(__fmul_rn(x[e], scale), __uint_as_float(add4[e]));
+            }
+          }
+          __syncwarp();
+          if (m.v[2]) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+#pragma unroll
+              for (int q = 0; q < 8; ++q) {
+                const float* x = v + 32 * s + 4 * q;
+                stage.put(q, make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])));
+              }
+              stage.flush(static_cast<float*>(ref) + at + 64 * cc + 32 * s, args.row_stride, rows);
+            }
+            continue;
+          }
+        }
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
           Vec8 x;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x.v[e] = v[8 * q + e] * scale;
-          if (adds) {  // (zeros where nothing is added)
+          for (int e = 0; e < 8; ++e) x.v[e] = kRef32 ? v[8 * q + e] : v[8 * q + e] * scale;
+          if (!kRef32 && adds) {
             const Vec8 y = unpack8(stage.get(q));
 #pragma unroll
             for (int e = 0; e < 8; ++e) x.v[e] += y.v[e];
@@ -689,11 +724,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
       if (r >= m.rows) return;
       const int64_t at = (static_cast<int64_t>(m.row0) + r) * args.row_stride + m.head * D;
       const int64_t from = (static_cast<int64_t>(m.v[4]) + r) * args.row_stride + m.head * D;
-      __nv_bfloat16* out = (half ? (m.v[2] ? args.dkb : args.dka) : (m.v[2] ? args.dvb : args.dva)) + at;
-      const __nv_bfloat16* add = half ? args.add_k : args.add_v;
+      auto write = [&](auto* out, const auto* add) {
+        constexpr int kPer = 16 / sizeof(*out);
 #pragma unroll 1
-      for (int i = 0; i < D; i += 8)
-        *reinterpret_cast<uint4*>(out + i) = r >= m.v[3] ? *reinterpret_cast<const uint4*>(add + from + i) : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < D; i += kPer)
+          *reinterpret_cast<uint4*>(out + i) = r >= m.v[3] ? *reinterpret_cast<const uint4*>(add + i) : make_uint4(0, 0, 0, 0);
+      };
+      // (the call's own keys, which the call's own queries see, are never of such an item)
+      using Ref = std::conditional_t<kRef32, float, __nv_bfloat16>;
+      write(static_cast<Ref*>(half ? args.dkb : args.dvb) + at, static_cast<const Ref*>(half ? args.add_k : args.add_v) + from);
     };
     int t = 0, n = 0;  // tiles, and items with tiles, so far
 #pragma unroll 1

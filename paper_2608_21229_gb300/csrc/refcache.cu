@@ -79,8 +79,8 @@ struct DeviceInfo {
   bool ok = false;
   int num_sms = 0;
   bool attr_set[9] = {false, false, false, false, false, false, false, false, false};
-  bool bwd_attr_set[2] = {false, false};
-  int bwd_clusters[4] = {0, 0, 0, 0};  // CTA pairs of each tcgen05 gradient kernel that fit at once (0: not asked yet)
+  bool bwd_attr_set[4] = {false, false, false, false};
+  int bwd_clusters[6] = {0, 0, 0, 0, 0, 0};  // CTA pairs of each tcgen05 gradient kernel that fit at once (0: not asked yet)
   int max_clusters[5] = {0, 0, 0, 0, 0};  // CTA pairs of each attn_tc2_kernel variant that fit at once
 };
 DeviceInfo g_dev[kMaxDevices];
@@ -920,17 +920,18 @@ struct BwdRequest {
 };
 constexpr int kNoAdd = 0x7fffffff;
 
-template <int D>
+template <int D, bool kRef32>
 int launch_bwd_mma(const rc::BwdKeys& keys, const rc::BwdQueries& queries, const rc::BwdArgs& a, DeviceInfo* info, cudaStream_t s) {
   constexpr int smem = rc::mm::bwd_smem<D>();
-  const int key = D == 64 ? 0 : 1;
+  const int key = (D == 64 ? 0 : 1) + (kRef32 ? 2 : 0);
   if (!info->bwd_attr_set[key]) {
-    cudaError_t e = cudaFuncSetAttribute(rc::attn_bwd_mma_keys_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    cudaError_t e = cudaFuncSetAttribute(rc::attn_bwd_mma_keys_kernel<D, kRef32>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(rc::attn_bwd_mma_queries_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(attn_bwd_mma)");
     info->bwd_attr_set[key] = true;
   }
-  if (keys.n_tiles > 0) rc::attn_bwd_mma_keys_kernel<D><<<static_cast<unsigned>(keys.n_tiles) * a.num_heads, 128, smem, s>>>(keys, a);
+  if (keys.n_tiles > 0)
+    rc::attn_bwd_mma_keys_kernel<D, kRef32><<<static_cast<unsigned>(keys.n_tiles) * a.num_heads, 128, smem, s>>>(keys, a);
   if (queries.n_tiles > 0)
     rc::attn_bwd_mma_queries_kernel<D><<<static_cast<unsigned>(queries.n_tiles) * a.num_heads, 128, smem, s>>>(queries, a);
   const cudaError_t e = cudaGetLastError();
@@ -976,18 +977,21 @@ int launch_bwd_tc(Kernel kernel, uint32_t smem, int which, const rc::BwdMaps& ma
   return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "attn_bwd kernel launch");
 }
 
-template <int D>
+template <int D, bool kRef32>
 int launch_bwd(const rc::BwdKeys& keys, const rc::BwdQueries& queries, const rc::BwdMaps& for_keys, const rc::BwdMaps& for_queries,
                rc::BwdArgs a, DeviceInfo* info, cudaStream_t s) {
   a.behind_queries = queries.n_tiles > 0;
   const int v = D == 64 ? 0 : 2;
   const int rc = launch_bwd_tc(rc::attn_bwd_queries_kernel<D>, rc::bwd::Smem<D, false>::kDynamic, v + 1, for_queries, queries, a, info, s);
-  return rc ? rc : launch_bwd_tc(rc::attn_bwd_keys_kernel<D>, rc::bwd::Smem<D, true>::kDynamic, v, for_keys, keys, a, info, s);
+  return rc ? rc
+            : launch_bwd_tc(rc::attn_bwd_keys_kernel<D, kRef32>, rc::bwd::Smem<D, true>::kDynamic, kRef32 ? 4 + v / 2 : v, for_keys, keys, a,
+                            info, s);
 }
 
-// The gradients of `batch` requests, request(b, &out) naming what request b's rows see.
+// The gradients of `batch` requests, request(b, &out) naming what request b's rows see.  ref_f32: BwdArgs' gradients of
+// cached rows are fp32.
 template <typename Request>
-int run_backward(int batch, int H, int D, rc::BwdArgs a, const float* lse, const void* o, void* work, float scale, int* status,
+int run_backward(int batch, int H, int D, bool ref_f32, rc::BwdArgs a, const float* lse, const void* o, void* work, float scale, int* status,
                  DeviceInfo* info, cudaStream_t s, const Request& request) {
   a.row_stride = static_cast<int64_t>(H) * D;
   a.num_heads = H;
@@ -1049,9 +1053,15 @@ int run_backward(int batch, int H, int D, rc::BwdArgs a, const float* lse, const
     } else {
       a.work_keys = a.work_queries = nullptr;
     }
-    const int rc = mma ? (D == 64 ? launch_bwd_mma<64>(keys, queries, a, info, s) : launch_bwd_mma<128>(keys, queries, a, info, s))
-                   : D == 64 ? launch_bwd<64>(keys, queries, for_keys, for_queries, a, info, s)
-                             : launch_bwd<128>(keys, queries, for_keys, for_queries, a, info, s);
+    auto go = [&](auto dim, auto f32) {
+      constexpr int kD = decltype(dim)::value;
+      constexpr bool kRef32 = decltype(f32)::value;
+      return mma ? launch_bwd_mma<kD, kRef32>(keys, queries, a, info, s)
+                 : launch_bwd<kD, kRef32>(keys, queries, for_keys, for_queries, a, info, s);
+    };
+    using std::integral_constant;
+    const int rc = D == 64 ? (ref_f32 ? go(integral_constant<int, 64>{}, std::true_type{}) : go(integral_constant<int, 64>{}, std::false_type{}))
+                           : (ref_f32 ? go(integral_constant<int, 128>{}, std::true_type{}) : go(integral_constant<int, 128>{}, std::false_type{}));
     if (rc) return rc;
   }
   return REFCACHE_OK;
@@ -1064,6 +1074,90 @@ int check_backward(std::initializer_list<const void*> tensors, const float* lse,
   if (!work || !aligned16(work)) return fail(REFCACHE_ERR_INVALID_ARG, "%s: work is NULL or not 16-byte aligned", what);
   if ((rows + 63) / 64 > (1ll << 30) / H) return fail(REFCACHE_ERR_INVALID_ARG, "%s: too many work items", what);
   return REFCACHE_OK;
+}
+
+// The two calls of a cache; ref_f32: dk_ref and dv_ref are fp32.
+int step_backward(bool ref_f32, refcache_t* h, int layer, const void* q_live, const void* k_live, const void* v_live, const void* o_live,
+                  const float* lse_live, const void* do_live, void* dq_live, void* dk_live, void* dv_live, void* dk_ref, void* dv_ref,
+                  int accumulate, void* work, float softmax_scale, void* stream) {
+  int rc = check_handle_layer(h, layer);
+  if (rc) return rc;
+  if (h->f8) return fail(REFCACHE_ERR_UNSUPPORTED, "step_attention_backward needs a bf16 cache");
+  if (!h->built[layer]) return fail(REFCACHE_ERR_NOT_BUILT, "layer %d has not been built", layer);
+  if ((rc = check_scale(softmax_scale)) != 0) return rc;
+  if ((rc = check_backward({q_live, k_live, v_live, o_live, do_live, dq_live, dk_live, dv_live}, lse_live, work, h->live_rows, h->H,
+                           "step_attention_backward")) != 0)
+    return rc;
+  if ((dk_ref == nullptr) != (dv_ref == nullptr)) return fail(REFCACHE_ERR_INVALID_ARG, "dk_ref without dv_ref, or the reverse");
+  if (dk_ref && (rc = check_ptrs({dk_ref, dv_ref}, h->cache_rows, "step_attention_backward")) != 0) return rc;
+  DeviceInfo* info = nullptr;
+  if ((rc = enter_device(h, &info)) != 0) return rc;
+  void *kslot = nullptr, *vslot = nullptr;
+  refcache_kv_ptr(h, layer, &kslot, &vslot, nullptr);
+  rc::BwdArgs a{};
+  a.q = static_cast<const __nv_bfloat16*>(q_live);
+  a.ka = static_cast<const __nv_bfloat16*>(k_live);
+  a.va = static_cast<const __nv_bfloat16*>(v_live);
+  a.kb = static_cast<const __nv_bfloat16*>(kslot);
+  a.vb = static_cast<const __nv_bfloat16*>(vslot);
+  a.d_o = static_cast<const __nv_bfloat16*>(do_live);
+  a.dq = static_cast<__nv_bfloat16*>(dq_live);
+  a.dka = static_cast<__nv_bfloat16*>(dk_live);
+  a.dva = static_cast<__nv_bfloat16*>(dv_live);
+  a.add_k = a.dkb = dk_ref;
+  a.add_v = a.dvb = dv_ref;
+  a.rows = h->live_rows;
+  a.a_rows = h->live_rows;
+  a.b_rows = h->cache_rows;
+  return run_backward(h->batch, h->H, h->D, ref_f32, a, lse_live, o_live, work, softmax_scale, h->d_status, info,
+                      static_cast<cudaStream_t>(stream), [&](int b, BwdRequest* r) {
+                        const int l0 = h->cu_live[b], nl = h->cu_live[b + 1] - l0;
+                        const int c0 = static_cast<int>(h->cache_off[b]), nc = static_cast<int>(h->cache_off[b + 1]) - c0;
+                        r->queries(l0, nl, l0, nl, c0, nc);
+                        r->keys(l0, nl, l0, nl, false, kNoAdd, 0);
+                        if (dk_ref) r->keys(c0, nc, l0, nl, true, accumulate ? 0 : kNoAdd, c0);
+                      });
+}
+
+int build_backward(bool ref_f32, refcache_t* h, int layer, const void* q_static, const void* k_static, const void* v_static,
+                   const void* o_static, const float* lse_static, const void* do_static, void* dq_static, void* dk_static, void* dv_static,
+                   const void* dk_ref, const void* dv_ref, void* work, float softmax_scale, void* stream) {
+  int rc = check_handle_layer(h, layer);
+  if (rc) return rc;
+  if ((rc = check_scale(softmax_scale)) != 0) return rc;
+  if ((rc = check_backward({q_static, k_static, v_static, o_static, do_static, dq_static, dk_static, dv_static}, lse_static, work,
+                           h->static_rows, h->H, "refcache_build_backward")) != 0)
+    return rc;
+  if ((dk_ref == nullptr) != (dv_ref == nullptr)) return fail(REFCACHE_ERR_INVALID_ARG, "dk_ref without dv_ref, or the reverse");
+  if (dk_ref && (rc = check_ptrs({dk_ref, dv_ref}, h->cache_rows, "refcache_build_backward")) != 0) return rc;
+  DeviceInfo* info = nullptr;
+  if ((rc = enter_device(h, &info)) != 0) return rc;
+  rc::BwdArgs a{};
+  a.q = static_cast<const __nv_bfloat16*>(q_static);
+  a.ka = static_cast<const __nv_bfloat16*>(k_static);
+  a.va = static_cast<const __nv_bfloat16*>(v_static);
+  a.d_o = static_cast<const __nv_bfloat16*>(do_static);
+  a.dq = static_cast<__nv_bfloat16*>(dq_static);
+  a.dka = static_cast<__nv_bfloat16*>(dk_static);
+  a.dva = static_cast<__nv_bfloat16*>(dv_static);
+  a.add_k = dk_ref;
+  a.add_v = dv_ref;
+  a.rows = h->static_rows;
+  a.a_rows = h->static_rows;
+  return run_backward(h->batch, h->H, h->D, ref_f32, a, lse_static, o_static, work, softmax_scale, h->d_status, info,
+                      static_cast<cudaStream_t>(stream), [&](int b, BwdRequest* r) {
+                        const int s0 = h->cu_static[b], ns = h->cu_static[b + 1] - s0, na = h->n_anchor[b];
+                        const int c0 = static_cast<int>(h->cache_off[b]);
+                        if (h->mode == REFCACHE_MASK_BEYOND_ALT) {  // ST sees ST, R sees [ST; R]; all of it is cached
+                          r->queries(s0, na, s0, na, 0, 0);
+                          r->queries(s0 + na, ns - na, s0, ns, 0, 0);
+                          r->keys(s0, na, s0, ns, false, dk_ref ? 0 : kNoAdd, c0);
+                          r->keys(s0 + na, ns - na, s0 + na, ns - na, false, dk_ref ? 0 : kNoAdd, c0 + na);
+                        } else {
+                          r->queries(s0, ns, s0, ns, 0, 0);
+                          r->keys(s0, ns, s0, ns, false, dk_ref ? na : kNoAdd, c0 - na);
+                        }
+                      });
 }
 
 }  // namespace
@@ -1472,84 +1566,31 @@ size_t refcache_backward_bytes(int64_t rows, int num_heads) {
 int step_attention_backward(refcache_t* h, int layer, const void* q_live, const void* k_live, const void* v_live, const void* o_live,
                             const float* lse_live, const void* do_live, void* dq_live, void* dk_live, void* dv_live, void* dk_ref,
                             void* dv_ref, int accumulate, void* work, float softmax_scale, void* stream) {
-  int rc = check_handle_layer(h, layer);
-  if (rc) return rc;
-  if (h->f8) return fail(REFCACHE_ERR_UNSUPPORTED, "step_attention_backward needs a bf16 cache");
-  if (!h->built[layer]) return fail(REFCACHE_ERR_NOT_BUILT, "layer %d has not been built", layer);
-  if ((rc = check_scale(softmax_scale)) != 0) return rc;
-  if ((rc = check_backward({q_live, k_live, v_live, o_live, do_live, dq_live, dk_live, dv_live}, lse_live, work, h->live_rows, h->H,
-                           "step_attention_backward")) != 0)
-    return rc;
-  if ((dk_ref == nullptr) != (dv_ref == nullptr)) return fail(REFCACHE_ERR_INVALID_ARG, "dk_ref without dv_ref, or the reverse");
-  if (dk_ref && (rc = check_ptrs({dk_ref, dv_ref}, h->cache_rows, "step_attention_backward")) != 0) return rc;
-  DeviceInfo* info = nullptr;
-  if ((rc = enter_device(h, &info)) != 0) return rc;
-  void *kslot = nullptr, *vslot = nullptr;
-  refcache_kv_ptr(h, layer, &kslot, &vslot, nullptr);
-  rc::BwdArgs a{};
-  a.q = static_cast<const __nv_bfloat16*>(q_live);
-  a.ka = static_cast<const __nv_bfloat16*>(k_live);
-  a.va = static_cast<const __nv_bfloat16*>(v_live);
-  a.kb = static_cast<const __nv_bfloat16*>(kslot);
-  a.vb = static_cast<const __nv_bfloat16*>(vslot);
-  a.d_o = static_cast<const __nv_bfloat16*>(do_live);
-  a.dq = static_cast<__nv_bfloat16*>(dq_live);
-  a.dka = static_cast<__nv_bfloat16*>(dk_live);
-  a.dva = static_cast<__nv_bfloat16*>(dv_live);
-  a.add_k = a.dkb = static_cast<__nv_bfloat16*>(dk_ref);
-  a.add_v = a.dvb = static_cast<__nv_bfloat16*>(dv_ref);
-  a.rows = h->live_rows;
-  a.a_rows = h->live_rows;
-  a.b_rows = h->cache_rows;
-  return run_backward(h->batch, h->H, h->D, a, lse_live, o_live, work, softmax_scale, h->d_status, info,
-                      static_cast<cudaStream_t>(stream), [&](int b, BwdRequest* r) {
-                        const int l0 = h->cu_live[b], nl = h->cu_live[b + 1] - l0;
-                        const int c0 = static_cast<int>(h->cache_off[b]), nc = static_cast<int>(h->cache_off[b + 1]) - c0;
-                        r->queries(l0, nl, l0, nl, c0, nc);
-                        r->keys(l0, nl, l0, nl, false, kNoAdd, 0);
-                        if (dk_ref) r->keys(c0, nc, l0, nl, true, accumulate ? 0 : kNoAdd, c0);
-                      });
+  return step_backward(false, h, layer, q_live, k_live, v_live, o_live, lse_live, do_live, dq_live, dk_live, dv_live, dk_ref, dv_ref,
+                       accumulate, work, softmax_scale, stream);
+}
+
+int step_attention_backward_ref_f32(refcache_t* h, int layer, const void* q_live, const void* k_live, const void* v_live,
+                                    const void* o_live, const float* lse_live, const void* do_live, void* dq_live, void* dk_live,
+                                    void* dv_live, float* dk_ref, float* dv_ref, int accumulate, void* work, float softmax_scale,
+                                    void* stream) {
+  return step_backward(true, h, layer, q_live, k_live, v_live, o_live, lse_live, do_live, dq_live, dk_live, dv_live, dk_ref, dv_ref,
+                       accumulate, work, softmax_scale, stream);
 }
 
 int refcache_build_backward(refcache_t* h, int layer, const void* q_static, const void* k_static, const void* v_static,
                             const void* o_static, const float* lse_static, const void* do_static, void* dq_static, void* dk_static,
                             void* dv_static, const void* dk_ref, const void* dv_ref, void* work, float softmax_scale, void* stream) {
-  int rc = check_handle_layer(h, layer);
-  if (rc) return rc;
-  if ((rc = check_scale(softmax_scale)) != 0) return rc;
-  if ((rc = check_backward({q_static, k_static, v_static, o_static, do_static, dq_static, dk_static, dv_static}, lse_static, work,
-                           h->static_rows, h->H, "refcache_build_backward")) != 0)
-    return rc;
-  if ((dk_ref == nullptr) != (dv_ref == nullptr)) return fail(REFCACHE_ERR_INVALID_ARG, "dk_ref without dv_ref, or the reverse");
-  if (dk_ref && (rc = check_ptrs({dk_ref, dv_ref}, h->cache_rows, "refcache_build_backward")) != 0) return rc;
-  DeviceInfo* info = nullptr;
-  if ((rc = enter_device(h, &info)) != 0) return rc;
-  rc::BwdArgs a{};
-  a.q = static_cast<const __nv_bfloat16*>(q_static);
-  a.ka = static_cast<const __nv_bfloat16*>(k_static);
-  a.va = static_cast<const __nv_bfloat16*>(v_static);
-  a.d_o = static_cast<const __nv_bfloat16*>(do_static);
-  a.dq = static_cast<__nv_bfloat16*>(dq_static);
-  a.dka = static_cast<__nv_bfloat16*>(dk_static);
-  a.dva = static_cast<__nv_bfloat16*>(dv_static);
-  a.add_k = static_cast<const __nv_bfloat16*>(dk_ref);
-  a.add_v = static_cast<const __nv_bfloat16*>(dv_ref);
-  a.rows = h->static_rows;
-  a.a_rows = h->static_rows;
-  return run_backward(h->batch, h->H, h->D, a, lse_static, o_static, work, softmax_scale, h->d_status, info,
-                      static_cast<cudaStream_t>(stream), [&](int b, BwdRequest* r) {
-                        const int s0 = h->cu_static[b], ns = h->cu_static[b + 1] - s0, na = h->n_anchor[b];
-                        const int c0 = static_cast<int>(h->cache_off[b]);
-                        if (h->mode == REFCACHE_MASK_BEYOND_ALT) {  // ST sees ST, R sees [ST; R]; all of it is cached
-                          r->queries(s0, na, s0, na, 0, 0);
-                          r->queries(s0 + na, ns - na, s0, ns, 0, 0);
-                          r->keys(s0, na, s0, ns, false, dk_ref ? 0 : kNoAdd, c0);
-                          r->keys(s0 + na, ns - na, s0 + na, ns - na, false, dk_ref ? 0 : kNoAdd, c0 + na);
-                        } else {
-                          r->queries(s0, ns, s0, ns, 0, 0);
-                          r->keys(s0, ns, s0, ns, false, dk_ref ? na : kNoAdd, c0 - na);
-                        }
-                      });
+  return build_backward(false, h, layer, q_static, k_static, v_static, o_static, lse_static, do_static, dq_static, dk_static, dv_static,
+                        dk_ref, dv_ref, work, softmax_scale, stream);
+}
+
+int refcache_build_backward_ref_f32(refcache_t* h, int layer, const void* q_static, const void* k_static, const void* v_static,
+                                    const void* o_static, const float* lse_static, const void* do_static, void* dq_static,
+                                    void* dk_static, void* dv_static, const float* dk_ref, const float* dv_ref, void* work,
+                                    float softmax_scale, void* stream) {
+  return build_backward(true, h, layer, q_static, k_static, v_static, o_static, lse_static, do_static, dq_static, dk_static, dv_static,
+                        dk_ref, dv_ref, work, softmax_scale, stream);
 }
 
 int full_attention_backward(int batch, int num_heads, int head_dim, const int32_t* cu_seqlens, const void* q, const void* k,
@@ -1573,7 +1614,7 @@ int full_attention_backward(int batch, int num_heads, int head_dim, const int32_
   a.dva = static_cast<__nv_bfloat16*>(dv);
   a.rows = rows;
   a.a_rows = rows;
-  return run_backward(batch, num_heads, head_dim, a, lse, o, work, softmax_scale, nullptr, info, static_cast<cudaStream_t>(stream),
+  return run_backward(batch, num_heads, head_dim, false, a, lse, o, work, softmax_scale, nullptr, info, static_cast<cudaStream_t>(stream),
                       [&](int b, BwdRequest* r) {
                         const int s0 = cu_seqlens[b], n = cu_seqlens[b + 1] - s0;
                         r->queries(s0, n, s0, n, 0, 0);

@@ -37,6 +37,7 @@ EXPORTED = (
     "full_attention_noalloc", "refcache_call_launches", "refcache_fp8_ptr", "refcache_build_in_slot",
     "refcache_cache_status", "refcache_ex2_rate",
     "refcache_backward_bytes", "step_attention_backward", "refcache_build_backward", "full_attention_backward",
+    "step_attention_backward_ref_f32", "refcache_build_backward_ref_f32",
     "refcache_rope_init", "refcache_qkv_rope", "refcache_qkv_rope_backward_bytes", "refcache_qkv_rope_backward",
     "refcache_gated_norm", "refcache_gated_norm_backward_bytes", "refcache_gated_norm_backward",
     "refcache_clip_gradients_bytes", "refcache_clip_gradients",
@@ -116,6 +117,8 @@ def load(path: Optional[str] = None):
     L.refcache_backward_bytes.restype = ctypes.c_size_t
     L.step_attention_backward.argtypes = [vp, i32] + [vp] * 11 + [i32, vp, f32, vp]
     L.refcache_build_backward.argtypes = [vp, i32] + [vp] * 12 + [f32, vp]
+    L.step_attention_backward_ref_f32.argtypes = L.step_attention_backward.argtypes
+    L.refcache_build_backward_ref_f32.argtypes = L.refcache_build_backward.argtypes
     L.full_attention_backward.argtypes = [i32, i32, i32, ctypes.POINTER(ctypes.c_int32)] + [vp] * 10 + [f32, vp]
     ropep, rowsp, normp = ctypes.POINTER(_Rope), ctypes.POINTER(_RopeRows), ctypes.POINTER(_GatedNorm)
     L.refcache_rope_init.argtypes = [ropep, i32, i32, ctypes.POINTER(ctypes.c_int32), ctypes.c_double, i32]
@@ -439,27 +442,40 @@ class RefCache:
     def step_backward(self, layer, q, k, v, o, lse, d_o, dq, dk, dv, dk_ref=None, dv_ref=None, accumulate=False, scale=None,
                       stream=None):
         """Gradient of ``step``: from ``d_o``, the gradient of its ``o``, to dq, dk, dv [live rows, H, D] and, unless
-        they are None, dk_ref and dv_ref [cached rows, H, D] (``accumulate``: added to what these hold).  ``lse`` is
-        the fp32 [live rows, H] that the step wrote."""
+        they are None, dk_ref and dv_ref [cached rows, H, D], bf16 or float32 (``accumulate``: added to what these hold; a
+        sum over many steps wants float32).  ``lse`` is the fp32 [live rows, H] that the step wrote."""
         H, D, n = self.seg.num_heads, self.seg.head_dim, self.seg.live_rows
         ptrs, work = _backward_ptrs((q, k, v, o, lse, d_o, dq, dk, dv), n, H, D, self.mem.get_device(), stream)
-        ref = (None, None) if dk_ref is None and dv_ref is None else self._ref_ptrs(dk_ref, dv_ref)
+        f32, *ref = self._ref_ptrs(dk_ref, dv_ref)
         scale = default_scale(D) if scale is None else scale
-        _check(load().step_attention_backward(self.h, layer, *ptrs, *ref, 1 if accumulate else 0, work.data_ptr(), scale,
-                                              _stream(stream)))
+        L = load()
+        call = L.step_attention_backward_ref_f32 if f32 else L.step_attention_backward
+        _check(call(self.h, layer, *ptrs, *ref, 1 if accumulate else 0, work.data_ptr(), scale, _stream(stream)))
 
     def build_backward(self, layer, q, k, v, o, lse, d_o, dq, dk, dv, dk_ref=None, dv_ref=None, scale=None, stream=None):
         """Gradient of ``build``; dk_ref and dv_ref, the cached rows' gradients from ``step_backward``, are added to
         the cached rows' part of dk and dv unless they are None."""
         H, D, n = self.seg.num_heads, self.seg.head_dim, self.seg.static_rows
         ptrs, work = _backward_ptrs((q, k, v, o, lse, d_o, dq, dk, dv), n, H, D, self.mem.get_device(), stream)
-        ref = (None, None) if dk_ref is None and dv_ref is None else self._ref_ptrs(dk_ref, dv_ref)
+        f32, *ref = self._ref_ptrs(dk_ref, dv_ref)
         scale = default_scale(D) if scale is None else scale
-        _check(load().refcache_build_backward(self.h, layer, *ptrs, *ref, work.data_ptr(), scale, _stream(stream)))
+        L = load()
+        call = L.refcache_build_backward_ref_f32 if f32 else L.refcache_build_backward
+        _check(call(self.h, layer, *ptrs, *ref, work.data_ptr(), scale, _stream(stream)))
 
     def _ref_ptrs(self, dk_ref, dv_ref):
+        """Whether the cached rows' gradients are float32, and their pointers."""
+        if dk_ref is None and dv_ref is None:
+            return False, None, None
         n = self.seg.static_rows - (0 if self.mask_mode == "beyond_alt" else sum(self.seg.n_anchor))  # cached rows
-        return _thd_ptrs((("dk_ref", dk_ref), ("dv_ref", dv_ref)), n, self.seg.num_heads, self.seg.head_dim, self.mem.get_device())
+        shape, device = (n, self.seg.num_heads, self.seg.head_dim), self.mem.get_device()
+        if dk_ref is None or dk_ref.dtype is not _float32:
+            return False, *_thd_ptrs((("dk_ref", dk_ref), ("dv_ref", dv_ref)), *shape, device)
+        for name, t in (("dk_ref", dk_ref), ("dv_ref", dv_ref)):
+            if t is None or t.dtype is not _float32 or t.shape != shape:
+                got = None if t is None else f"{t.dtype} {tuple(t.shape)}"
+                raise ValueError(f"{name}: expected float32 {list(shape)} beside the other, got {got}")
+        return True, _ptr(dk_ref, device, "dk_ref"), _ptr(dv_ref, device, "dv_ref")
 
 
 def full_attention(cu_seqlens, q, k, v, o, lse=None, scale=None, stream=None):
