@@ -518,7 +518,7 @@ REFCACHE_API int refcache_gated_norm_backward(const refcache_gated_norm_t* p, co
  * is.  Under a finite bound a norm that is NaN makes the outputs NaN, and an infinite
  * one makes finite elements 0.  (Squares are summed
  * in fp32 per thread and in fp64 from there on: the norm is infinite where a
- * thread's squares overflow fp32.)  work: refcache_clip_gradients_bytes(n) bytes of
+ * thread's squares overflow fp32, and squares below its range count as 0.)  work: refcache_clip_gradients_bytes(n) bytes of
  * device memory, 16-byte aligned.
  */
 #define REFCACHE_CLIP_GRAD_F32 1 /* gradient fp32 (else bf16) */

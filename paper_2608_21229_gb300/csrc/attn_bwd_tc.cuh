@@ -42,17 +42,20 @@
 //
 // What bounds them: at D = 128 the tensor pipe (with many tiles an item, under the power
 // cap), at D = 64 the score warps and as long a chain from one S to the next (arrivals,
-// MMAs, commits).  Measured, each alone on the GPU:
+// MMAs, commits).  Measured, each alone on the GPU and after a pause, at a clock that the
+// power cap does not hold for long:
 //                                    keys kernel              queries kernel
 //   cycles per tile, D = 128         2250 (MMAs: 2048)        1690 (1536)
 //   cycles per tile, D = 64          1710 (1024)              1510 (768)
 //   and between items                5700 (its output)        2500
-//   24 heads of 128, 1280 queries    78 us, 1340 TFLOP/s      57 us, 1380 TFLOP/s
+//   24 heads of 128, 1280 queries    78 us, 1345 TFLOP/s      58 us, 1355 TFLOP/s
 //     and 3328 keys                  of its four products     of its three
 //   4608 queries, 25088 keys         1403 us, 2025            1067 us, 2000
 //   16 heads of 64, three requests   280 us, 1290             240 us, 1130
 //     of 9431 rows together
-// One after the other with the pass over the outputs, call after call: 128, 2830 and 532 us.
+// One after the other with the pass over the outputs, call after call: 128, 2820 and 531 us, at
+// 1910, 1575 and 1995 MHz (sampled).  Of the 4.44 M cycles that 2820 us are, the seven
+// products' MMAs take 3.99 M.
 //
 // All waits are bounded as in attn_tc2_kernel, and the teardown is that kernel's:
 // loads complete on the leader's barriers, which it arms for both CTAs' bytes.
