@@ -830,7 +830,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(bwd::kThreads, 1)
   if (args.behind_queries) {
     grid_dependency_wait();  // the work after this kernel sees both
     // (a CTA that starts later and finds no ticket waits for nothing any more)
-    if (blockIdx.x == 0 && threadIdx.x == 0) *args.passed = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) st_release_gpu(args.passed, 0);
   }
 }
 

@@ -31,7 +31,7 @@ def test_a_cta_starts_behind_a_wait_or_an_acquired_ticket():
     # the queries kernel says it, the keys kernel behind it looks for it, waits at its end and sets the word back
     assert "enter(c, smem_raw, args, maps, true, false)" in code and "enter(c, smem_raw, args, maps, false, args.behind_queries != 0)" in code
     keys = re.sub(r"\s+", " ", code[code.index("attn_bwd_keys_kernel("):code.index("attn_bwd_queries_kernel(")])
-    assert "if (args.behind_queries) { grid_dependency_wait(); if (blockIdx.x == 0 && threadIdx.x == 0) *args.passed = 0; }" in keys
+    assert "if (args.behind_queries) { grid_dependency_wait(); if (blockIdx.x == 0 && threadIdx.x == 0) st_release_gpu(args.passed, 0); }" in keys
 
 
 def _call(work, n, H, D, t, out, lse):
