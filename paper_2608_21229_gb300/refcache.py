@@ -196,7 +196,7 @@ def _ptr(t, device, name=None) -> Optional[int]:
     if t.get_device() != device:
         raise _elsewhere(t, device, name)
     if not t.is_contiguous():
-        raise ValueError("tensor must be contiguous")
+        raise ValueError(("" if name is None else name + ": ") + "tensor must be contiguous")
     return t.data_ptr()
 
 
@@ -445,32 +445,36 @@ class RefCache:
         they are None, dk_ref and dv_ref [cached rows, H, D], bf16 or float32 (``accumulate``: added to what these hold; a
         sum over many steps wants float32).  ``lse`` is the fp32 [live rows, H] that the step wrote."""
         H, D, n = self.seg.num_heads, self.seg.head_dim, self.seg.live_rows
-        ptrs, work = _backward_ptrs((q, k, v, o, lse, d_o, dq, dk, dv), n, H, D, self.mem.get_device(), stream)
-        f32, *ref = self._ref_ptrs(dk_ref, dv_ref)
+        device = self.mem.get_device()
+        ptrs, work = _backward_ptrs((q, k, v, o, lse, d_o, dq, dk, dv), n, H, D, device, stream)
+        f32, dk_ref, dv_ref = self._ref_ptrs(dk_ref, dv_ref, device)
         scale = default_scale(D) if scale is None else scale
         L = load()
         call = L.step_attention_backward_ref_f32 if f32 else L.step_attention_backward
-        _check(call(self.h, layer, *ptrs, *ref, 1 if accumulate else 0, work.data_ptr(), scale, _stream(stream)))
+        _check(call(self.h, layer, *ptrs, dk_ref, dv_ref, 1 if accumulate else 0, work.data_ptr(), scale, _stream(stream)))
 
     def build_backward(self, layer, q, k, v, o, lse, d_o, dq, dk, dv, dk_ref=None, dv_ref=None, scale=None, stream=None):
         """Gradient of ``build``; dk_ref and dv_ref, the cached rows' gradients from ``step_backward``, are added to
         the cached rows' part of dk and dv unless they are None."""
         H, D, n = self.seg.num_heads, self.seg.head_dim, self.seg.static_rows
-        ptrs, work = _backward_ptrs((q, k, v, o, lse, d_o, dq, dk, dv), n, H, D, self.mem.get_device(), stream)
-        f32, *ref = self._ref_ptrs(dk_ref, dv_ref)
+        device = self.mem.get_device()
+        ptrs, work = _backward_ptrs((q, k, v, o, lse, d_o, dq, dk, dv), n, H, D, device, stream)
+        f32, dk_ref, dv_ref = self._ref_ptrs(dk_ref, dv_ref, device)
         scale = default_scale(D) if scale is None else scale
         L = load()
         call = L.refcache_build_backward_ref_f32 if f32 else L.refcache_build_backward
-        _check(call(self.h, layer, *ptrs, *ref, work.data_ptr(), scale, _stream(stream)))
+        _check(call(self.h, layer, *ptrs, dk_ref, dv_ref, work.data_ptr(), scale, _stream(stream)))
 
-    def _ref_ptrs(self, dk_ref, dv_ref):
+    def _ref_ptrs(self, dk_ref, dv_ref, device):
         """Whether the cached rows' gradients are float32, and their pointers."""
         if dk_ref is None and dv_ref is None:
             return False, None, None
         n = self.seg.static_rows - (0 if self.mask_mode == "beyond_alt" else sum(self.seg.n_anchor))  # cached rows
-        shape, device = (n, self.seg.num_heads, self.seg.head_dim), self.mem.get_device()
+        H, D = self.seg.num_heads, self.seg.head_dim
         if dk_ref is None or dk_ref.dtype is not _float32:
-            return False, *_thd_ptrs((("dk_ref", dk_ref), ("dv_ref", dv_ref)), *shape, device)
+            k, v = _thd_ptrs((("dk_ref", dk_ref), ("dv_ref", dv_ref)), n, H, D, device)
+            return False, k, v
+        shape = (n, H, D)
         for name, t in (("dk_ref", dk_ref), ("dv_ref", dv_ref)):
             if t is None or t.dtype is not _float32 or t.shape != shape:
                 got = None if t is None else f"{t.dtype} {tuple(t.shape)}"
@@ -773,10 +777,8 @@ def clip_gradients(grads, max_norm, out=None, norm=None, stream=None):
     device = _device()
     for tensors in (grads,) if outs is None else (grads, outs):
         for i, t in enumerate(tensors):
-            if t.get_device() != device:
-                raise _elsewhere(t, device, f"gradient {i}")
-            if not t.is_contiguous():
-                raise ValueError(f"gradient {i}: tensors must be contiguous")
+            if t.get_device() != device or not t.is_contiguous():
+                _ptr(t, device, f"gradient {i}")
     kind = {_bfloat16: 0, _float32: 1}
     try:
         types = [kind[g.dtype] for g in grads]
@@ -784,7 +786,7 @@ def clip_gradients(grads, max_norm, out=None, norm=None, stream=None):
     except KeyError as e:
         raise ValueError(f"gradients: expected bf16 or float32, got {e.args[0]}") from None
     if norm is None:
-        norm = _empty((), _float32, _torch.device("cuda", device), stream)
+        norm = _empty((), _float32, grads[0].device if grads else _torch.device("cuda", device), stream)
     elif norm.dtype is not _float32 or norm.numel() != 1:
         raise ValueError(f"norm: expected one float32, got {norm.dtype} {tuple(norm.shape)}")
     norm_ptr = _ptr(norm, device, "norm")
