@@ -527,6 +527,90 @@ REFCACHE_API size_t refcache_clip_gradients_bytes(int n);
 REFCACHE_API int refcache_clip_gradients(int n, const void* const* grads, void* const* out, const int64_t* counts,
                                          const int32_t* types, float max_norm, float* norm, void* work, void* stream);
 
+/* ---- linear layers in 8 bits ----------------------------------------------
+ *
+ * The 8-bit form of rows (bf16 activations or gradients) is OCP E4M3 codes and, for
+ * each block of 128 columns of a row, a power of two as scale, kept as UE8M0: byte b
+ * is 2^(b - 127), the smallest with amax / 2^(b - 127) <= 448 (127 for a block of
+ * zeros, at least 1); code = E4M3(x / 2^(b - 127)), round to nearest even.  A block
+ * that holds a NaN or an infinity has b = 255 and NaN codes: all of it is NaN.  A
+ * weight has one scale for each 128 x 128.  Where a row's last block is short it is
+ * over the columns that are there.
+ *
+ * Rows in this form are what the products below take, and serve as the checkpoint of
+ * the activations until the backward pass, which reads them as they are.
+ *   - Widths are multiples of 16 up to 2^20, rows up to 2^31 - 513.
+ *   - Codes are packed [rows, width], 16-byte aligned; scales are rows of
+ *     REFCACHE_F8_PITCH(width) bytes, 16-byte aligned, of which the first
+ *     ceil(width / 128) are used and written.
+ *   - Products are summed in fp32; results are rounded once.
+ *   - bf16 tensors of rows may have ld elements between rows (a multiple of 8).
+ *   - Outputs must not overlap inputs or each other (but for dw over add).
+ *   - The calls launch kernels only and allocate nothing: they can be captured in a
+ *     CUDA graph, after a first call on the device outside the capture, and may overlap
+ *     on several streams.  Sums have a fixed order for a given device: the same inputs
+ *     give the same bits.
+ */
+#define REFCACHE_F8_PITCH(width) (((width) + 511) / 512 * 4)
+typedef struct {
+  int64_t rows;
+  int32_t width;
+  void* codes;  /* [rows, width] */
+  void* scales; /* [rows, REFCACHE_F8_PITCH(width)] */
+} refcache_f8_rows_t;
+typedef struct {
+  int32_t out_width, in_width; /* w is [out_width, in_width] */
+  void *codes, *scales;        /* [out, in]; [ceil(out / 128), REFCACHE_F8_PITCH(in)] */
+  void *codes_t, *scales_t;    /* transposed: [in, out]; [ceil(in / 128), REFCACHE_F8_PITCH(out)] (same values) */
+} refcache_f8_weight_t;
+
+/* x: [out->rows, out->width] bf16, ld elements between rows. */
+REFCACHE_API int refcache_f8_quantize(const void* x, int64_t ld, const refcache_f8_rows_t* out, void* stream);
+
+/* w: [out_width, in_width], packed, fp32 (w_f32 != 0) or bf16.  codes_t and scales_t may both be NULL. */
+REFCACHE_API int refcache_f8_quantize_weight(const void* w, int w_f32, const refcache_f8_weight_t* out, void* stream);
+
+/*
+ * y = x w^T + bias [rows, out_width] (reads codes and scales), or with transposed != 0
+ * y = x w [rows, in_width] (codes_t, scales_t): a layer's output, and its input's
+ * gradient from the 8-bit form of its output's.  y bf16; bias: one value for each
+ * column of y, fp32 (bias_f32 != 0) or bf16, or NULL.
+ */
+REFCACHE_API int refcache_f8_linear(const refcache_f8_rows_t* x, const refcache_f8_weight_t* w, int transposed, const void* bias,
+                                    int bias_f32, void* y, int64_t ld_y, void* stream);
+
+/*
+ * An MLP's first layer: u = x w^T + bias, a = the 8-bit form of gelu(u), u8 (may be
+ * NULL) that of u, the checkpoint for the gradient.  u is not rounded before it goes into
+ * either.  form: the normal distribution's function, or its tanh approximation.
+ */
+#define REFCACHE_GELU_ERF 0
+#define REFCACHE_GELU_TANH 1
+REFCACHE_API int refcache_f8_linear_gelu(const refcache_f8_rows_t* x, const refcache_f8_weight_t* w, const void* bias, int bias_f32,
+                                         int form, const refcache_f8_rows_t* a, const refcache_f8_rows_t* u8, void* stream);
+
+/*
+ * Its gradient together with that of the layer behind it: from the 8-bit form of dy, the
+ * gradient of that layer's output, and its weight w (reads codes_t, scales_t),
+ * du = (dy w) gelu'(u) with u as u8 holds it.  du [rows, in_width of w] bf16 and du8, the 8-bit
+ * form of du before its rounding, are written; either may be NULL, not both.
+ */
+REFCACHE_API int refcache_f8_linear_gelu_backward(const refcache_f8_rows_t* dy, const refcache_f8_weight_t* w, int form,
+                                                  const refcache_f8_rows_t* u8, void* du, int64_t ld_du,
+                                                  const refcache_f8_rows_t* du8, void* stream);
+
+/*
+ * The weight's gradient: dw = add + dy^T x [out_width, width of x], fp32 (dw_f32 != 0) or
+ * bf16, packed; add like dw, dw itself or NULL; d_bias = sums of dy over the rows, fp32
+ * [out_width], or NULL.  dy [rows of x, out_width] bf16.  x's values are taken as they
+ * are (exact in bf16 from 2^-126 on): the product is bf16 with fp32 sums.  Without rows dw is add, or zero.
+ * work: refcache_f8_weight_grad_bytes bytes of device memory, 16-byte aligned (may be NULL
+ * where these are 0).
+ */
+REFCACHE_API size_t refcache_f8_weight_grad_bytes(int64_t rows, int out_width, int in_width);
+REFCACHE_API int refcache_f8_weight_grad(const void* dy, int64_t ld_dy, const refcache_f8_rows_t* x, int out_width, const void* add,
+                                         void* dw, int dw_f32, float* d_bias, void* work, void* stream);
+
 /*
  * Synchronise `stream`, then read and clear the current device's error word
  * written by kernels whose bounded waits ran out.  Returns REFCACHE_OK,

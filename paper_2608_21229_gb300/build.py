@@ -1,7 +1,8 @@
 """Build the CUDA library (librefcache.so) for sm_103a with nvcc, in-tree.
 
-The library is two translation units, compiled in parallel (csrc/refcache.cu
-with the attention kernels, csrc/block_ops.cu with those of the block around it),
+The library is three translation units, compiled in parallel (csrc/refcache.cu
+with the attention kernels, csrc/block_ops.cu with those of the block around it,
+csrc/f8_ops.cu with the linear layers in 8 bits),
 compiled with ``-gencode arch=compute_103a,code=sm_103a`` and linked
 against the shared CUDA runtime, so that it shares the runtime (and the
 streams) of the host process.
@@ -19,7 +20,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(BUILD_DIR, "librefcache.so")
-UNITS = ("refcache.cu", "block_ops.cu")
+UNITS = ("refcache.cu", "block_ops.cu", "f8_ops.cu")
 ARCH_FLAGS = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

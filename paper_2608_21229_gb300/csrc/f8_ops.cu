@@ -1,0 +1,184 @@
+// f8_ops.cu -- the entry points of include/refcache.h for linear layers in 8 bits:
+// rows and weights into their 8-bit form (f8_rows.cuh), products on it (f8_simple.cuh).
+// Argument checks and launches; no call allocates memory.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "refcache.h"
+#include "f8_rows.cuh"
+#include "f8_simple.cuh"
+#include "host_common.h"
+
+using rc_host::aligned16;
+using rc_host::cuda_fail;
+using rc_host::device_sms;
+using rc_host::fail;
+using rc_host::launch_dependent;
+
+namespace {
+
+constexpr int64_t kMaxRows = (1ll << 31) - 1 - 512;
+constexpr int kMaxWidth = 1 << 20;
+
+unsigned ceil_div(int64_t a, int64_t b) { return static_cast<unsigned>((a + b - 1) / b); }
+
+int check_tensor(const void* p, const char* name) {
+  if (!p) return fail(REFCACHE_ERR_INVALID_ARG, "%s is NULL", name);
+  if (!aligned16(p)) return fail(REFCACHE_ERR_INVALID_ARG, "%s: tensor pointer not 16-byte aligned", name);
+  return REFCACHE_OK;
+}
+int check_width(int64_t width, const char* name) {
+  if (width < 16 || width > kMaxWidth || width % 16)
+    return fail(REFCACHE_ERR_INVALID_ARG, "%s: widths are multiples of 16 from 16 to %d (got %lld)", name, kMaxWidth, static_cast<long long>(width));
+  return REFCACHE_OK;
+}
+int check_ld(int64_t ld, int64_t width, const char* name) {
+  if (ld < width || ld % 8 || ld > (1ll << 32))
+    return fail(REFCACHE_ERR_INVALID_ARG, "%s: %lld elements between rows of %lld (a multiple of 8, at least the width)", name,
+                static_cast<long long>(ld), static_cast<long long>(width));
+  return REFCACHE_OK;
+}
+// Rows in 8-bit form (of `width`, unless it is 0).
+int check_rows(const refcache_f8_rows_t* r, int64_t rows, int width, const char* name) {
+  if (!r) return fail(REFCACHE_ERR_INVALID_ARG, "%s is NULL", name);
+  int rc = check_width(r->width, name);
+  if (rc) return rc;
+  if (r->rows < 0 || r->rows > kMaxRows) return fail(REFCACHE_ERR_INVALID_ARG, "%s: %lld rows", name, static_cast<long long>(r->rows));
+  if (width && r->width != width) return fail(REFCACHE_ERR_INVALID_ARG, "%s: width %d, expected %d", name, r->width, width);
+  if (rows >= 0 && r->rows != rows)
+    return fail(REFCACHE_ERR_INVALID_ARG, "%s: %lld rows, expected %lld", name, static_cast<long long>(r->rows), static_cast<long long>(rows));
+  if (r->rows > 0 && ((rc = check_tensor(r->codes, name)) != 0 || (rc = check_tensor(r->scales, name)) != 0)) return rc;
+  return REFCACHE_OK;
+}
+int check_weight(const refcache_f8_weight_t* w, bool plain, bool transposed) {
+  if (!w) return fail(REFCACHE_ERR_INVALID_ARG, "weight is NULL");
+  int rc;
+  if ((rc = check_width(w->out_width, "weight")) != 0 || (rc = check_width(w->in_width, "weight")) != 0) return rc;
+  if (plain && ((rc = check_tensor(w->codes, "weight codes")) != 0 || (rc = check_tensor(w->scales, "weight scales")) != 0)) return rc;
+  if (transposed && ((rc = check_tensor(w->codes_t, "weight codes_t")) != 0 || (rc = check_tensor(w->scales_t, "weight scales_t")) != 0)) return rc;
+  return REFCACHE_OK;
+}
+int check_bias(const void* bias, int f32) {
+  if (bias && (reinterpret_cast<uintptr_t>(bias) & (f32 ? 3u : 1u))) return fail(REFCACHE_ERR_INVALID_ARG, "bias is not aligned");
+  return REFCACHE_OK;
+}
+
+rc::f8::Rows rows_of(const refcache_f8_rows_t* r) {
+  if (!r) return {};
+  return {static_cast<uint8_t*>(r->codes), static_cast<uint8_t*>(r->scales), r->rows, r->width, REFCACHE_F8_PITCH(r->width)};
+}
+rc::f8::Rows rows_of(const refcache_f8_weight_t* w, bool transposed) {
+  if (transposed)
+    return {static_cast<uint8_t*>(w->codes_t), static_cast<uint8_t*>(w->scales_t), w->in_width, w->out_width, REFCACHE_F8_PITCH(w->out_width)};
+  return {static_cast<uint8_t*>(w->codes), static_cast<uint8_t*>(w->scales), w->out_width, w->in_width, REFCACHE_F8_PITCH(w->in_width)};
+}
+
+template <int kEpi>
+int launch_linear(const rc::f8::Rows& x, const rc::f8::Rows& w, const rc::f8::Out& o, void* stream) {
+  if (o.rows == 0) return REFCACHE_OK;
+  int sms = 0;
+  const int rc = device_sms(&sms);
+  if (rc) return rc;
+  const cudaError_t e = launch_dependent(rc::f8::f8_linear_simple_kernel<kEpi>, dim3(ceil_div(o.width, 128), ceil_div(o.rows, 32)), dim3(256), 0,
+                                         static_cast<cudaStream_t>(stream), x, w, o);
+  return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "f8_linear launch");
+}
+
+}  // namespace
+
+extern "C" {
+
+int refcache_f8_quantize(const void* x, int64_t ld, const refcache_f8_rows_t* out, void* stream) {
+  int rc = check_rows(out, -1, 0, "out");
+  if (rc || (rc = check_ld(ld, out->width, "x")) != 0) return rc;
+  if (out->rows == 0) return REFCACHE_OK;
+  if ((rc = check_tensor(x, "x")) != 0) return rc;
+  int sms = 0;
+  if ((rc = device_sms(&sms)) != 0) return rc;
+  const int64_t warps = out->rows * ((out->width + 255) / 256);
+  const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(ceil_div(warps, rc::f8::kRowsThreads / 32), 8ll * sms));
+  const cudaError_t e = launch_dependent(rc::f8::f8_quantize_kernel, dim3(blocks), dim3(rc::f8::kRowsThreads), 0, static_cast<cudaStream_t>(stream),
+                                         static_cast<const uint16_t*>(x), ld, rows_of(out));
+  return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "f8_quantize launch");
+}
+
+int refcache_f8_quantize_weight(const void* w, int w_f32, const refcache_f8_weight_t* out, void* stream) {
+  const bool both = out && (out->codes_t || out->scales_t);
+  int rc = check_weight(out, true, both);
+  if (rc || (rc = check_tensor(w, "w")) != 0) return rc;
+  int sms = 0;
+  if ((rc = device_sms(&sms)) != 0) return rc;
+  const rc::f8::Rows t = both ? rows_of(out, true) : rc::f8::Rows{};
+  const dim3 grid(ceil_div(out->in_width, 128), ceil_div(out->out_width, 128));
+  auto go = [&](auto kernel) { return launch_dependent(kernel, grid, dim3(256), 0, static_cast<cudaStream_t>(stream), w, rows_of(out, false), t); };
+  const cudaError_t e = w_f32 ? go(rc::f8::f8_quantize_weight_kernel<true>) : go(rc::f8::f8_quantize_weight_kernel<false>);
+  return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "f8_quantize_weight launch");
+}
+
+int refcache_f8_linear(const refcache_f8_rows_t* x, const refcache_f8_weight_t* w, int transposed, const void* bias, int bias_f32, void* y,
+                       int64_t ld_y, void* stream) {
+  const bool t = transposed != 0;
+  int rc = check_weight(w, !t, t);
+  if (rc) return rc;
+  const int in = t ? w->out_width : w->in_width, out = t ? w->in_width : w->out_width;
+  if ((rc = check_rows(x, -1, in, "x")) != 0 || (rc = check_bias(bias, bias_f32)) != 0 || (rc = check_ld(ld_y, out, "y")) != 0) return rc;
+  if (x->rows > 0 && (rc = check_tensor(y, "y")) != 0) return rc;
+  rc::f8::Out o{};
+  o.bias = bias, o.bias_f32 = bias_f32, o.width = out, o.rows = x->rows;
+  o.y = static_cast<uint16_t*>(y), o.ld = ld_y;
+  return launch_linear<rc::f8::kStore>(rows_of(x), rows_of(w, t), o, stream);
+}
+
+int refcache_f8_linear_gelu(const refcache_f8_rows_t* x, const refcache_f8_weight_t* w, const void* bias, int bias_f32, int form,
+                            const refcache_f8_rows_t* a, const refcache_f8_rows_t* u8, void* stream) {
+  int rc = check_weight(w, true, false);
+  if (rc || (rc = check_rows(x, -1, w->in_width, "x")) != 0 || (rc = check_rows(a, x->rows, w->out_width, "a")) != 0 ||
+      (u8 && (rc = check_rows(u8, x->rows, w->out_width, "u8")) != 0) || (rc = check_bias(bias, bias_f32)) != 0)
+    return rc;
+  if (form != REFCACHE_GELU_ERF && form != REFCACHE_GELU_TANH) return fail(REFCACHE_ERR_INVALID_ARG, "unknown form %d of the GELU", form);
+  rc::f8::Out o{};
+  o.bias = bias, o.bias_f32 = bias_f32, o.width = w->out_width, o.rows = x->rows;
+  o.a = rows_of(a), o.u = rows_of(u8);
+  return form == REFCACHE_GELU_ERF ? launch_linear<rc::f8::kGelu>(rows_of(x), rows_of(w, false), o, stream)
+                                   : launch_linear<rc::f8::kGelu + 1>(rows_of(x), rows_of(w, false), o, stream);
+}
+
+int refcache_f8_linear_gelu_backward(const refcache_f8_rows_t* dy, const refcache_f8_weight_t* w, int form, const refcache_f8_rows_t* u8,
+                                     void* du, int64_t ld_du, const refcache_f8_rows_t* du8, void* stream) {
+  int rc = check_weight(w, false, true);
+  if (rc || (rc = check_rows(dy, -1, w->out_width, "dy")) != 0 || (rc = check_rows(u8, dy->rows, w->in_width, "u8")) != 0 ||
+      (du8 && (rc = check_rows(du8, dy->rows, w->in_width, "du8")) != 0))
+    return rc;
+  if (form != REFCACHE_GELU_ERF && form != REFCACHE_GELU_TANH) return fail(REFCACHE_ERR_INVALID_ARG, "unknown form %d of the GELU", form);
+  if (!du && !du8) return fail(REFCACHE_ERR_INVALID_ARG, "neither du nor du8 is given");
+  if (du && ((rc = check_tensor(du, "du")) != 0 || (rc = check_ld(ld_du, w->in_width, "du")) != 0)) return rc;
+  rc::f8::Out o{};
+  o.width = w->in_width, o.rows = dy->rows;
+  o.y = static_cast<uint16_t*>(du), o.ld = ld_du;
+  o.a = rows_of(du8), o.u = rows_of(u8);
+  return form == REFCACHE_GELU_ERF ? launch_linear<rc::f8::kGeluGrad>(rows_of(dy), rows_of(w, true), o, stream)
+                                   : launch_linear<rc::f8::kGeluGrad + 1>(rows_of(dy), rows_of(w, true), o, stream);
+}
+
+size_t refcache_f8_weight_grad_bytes(int64_t, int, int) { return 0; }
+
+int refcache_f8_weight_grad(const void* dy, int64_t ld_dy, const refcache_f8_rows_t* x, int out_width, const void* add, void* dw, int dw_f32,
+                            float* d_bias, void* work, void* stream) {
+  int rc = check_rows(x, -1, 0, "x");
+  if (rc || (rc = check_width(out_width, "dy")) != 0 || (rc = check_ld(ld_dy, out_width, "dy")) != 0 || (rc = check_tensor(dw, "dw")) != 0 ||
+      (add && (rc = check_tensor(add, "add")) != 0) || (x->rows > 0 && (rc = check_tensor(dy, "dy")) != 0))
+    return rc;
+  if (reinterpret_cast<uintptr_t>(d_bias) & 3u) return fail(REFCACHE_ERR_INVALID_ARG, "d_bias is not 4-byte aligned");
+  if (refcache_f8_weight_grad_bytes(x->rows, out_width, x->width) && (rc = check_tensor(work, "work")) != 0) return rc;
+  int sms = 0;
+  if ((rc = device_sms(&sms)) != 0) return rc;
+  const rc::f8::WgradArgs a{static_cast<const uint16_t*>(dy), ld_dy, rows_of(x), out_width, add, dw, dw_f32, d_bias};
+  const cudaError_t e = launch_dependent(rc::f8::f8_wgrad_simple_kernel, dim3(ceil_div(x->width, 128), ceil_div(out_width, 32)), dim3(256), 0,
+                                         static_cast<cudaStream_t>(stream), a);
+  return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "f8_weight_grad launch");
+}
+
+}  // extern "C"

@@ -27,6 +27,7 @@ ERR_TIMEOUT = -6
 MASK_MODES = {"beyond": 0, "beyond_alt": 1, "isolated": 2}
 KERNELS = {"tcgen05": 0, "mma_sync": 1, "tcgen05_k128": 2}
 NORMS = {None: 0, "layer": 1, "rms": 2}
+GELU_FORMS = {"erf": 0, "tanh": 1}
 ROPE_PAIRS = {"halves": 0, "interleaved": 1}
 CACHE_DTYPES = {"bf16": 0, "fp8": 0x100}  # REFCACHE_CACHE_FP8: E4M3 codes with per-tile scales
 
@@ -41,6 +42,8 @@ EXPORTED = (
     "refcache_rope_init", "refcache_qkv_rope", "refcache_qkv_rope_backward_bytes", "refcache_qkv_rope_backward",
     "refcache_gated_norm", "refcache_gated_norm_backward_bytes", "refcache_gated_norm_backward",
     "refcache_clip_gradients_bytes", "refcache_clip_gradients",
+    "refcache_f8_quantize", "refcache_f8_quantize_weight", "refcache_f8_linear", "refcache_f8_linear_gelu",
+    "refcache_f8_linear_gelu_backward", "refcache_f8_weight_grad_bytes", "refcache_f8_weight_grad",
 )
 NOALLOC_MAX_TASKS = 16384
 
@@ -76,6 +79,15 @@ class _GatedNorm(ctypes.Structure):
                 ("gate", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("shift", ctypes.c_void_p),
                 ("ld_gate", ctypes.c_int64), ("ld_scale", ctypes.c_int64), ("ld_shift", ctypes.c_int64),
                 ("weight", ctypes.c_void_p), ("post_weight", ctypes.c_void_p)]
+
+
+class _F8Rows(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int32), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class _F8Weight(ctypes.Structure):
+    _fields_ = [("out_width", ctypes.c_int32), ("in_width", ctypes.c_int32), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("codes_t", ctypes.c_void_p), ("scales_t", ctypes.c_void_p)]
 
 
 _lib = None
@@ -133,6 +145,15 @@ def load(path: Optional[str] = None):
     L.refcache_clip_gradients_bytes.argtypes = [i32]
     L.refcache_clip_gradients_bytes.restype = ctypes.c_size_t
     L.refcache_clip_gradients.argtypes = [i32, vp, vp, vp, vp, f32, vp, vp, vp]
+    f8p, f8wp = ctypes.POINTER(_F8Rows), ctypes.POINTER(_F8Weight)
+    L.refcache_f8_quantize.argtypes = [vp, i64, f8p, vp]
+    L.refcache_f8_quantize_weight.argtypes = [vp, i32, f8wp, vp]
+    L.refcache_f8_linear.argtypes = [f8p, f8wp, i32, vp, i32, vp, i64, vp]
+    L.refcache_f8_linear_gelu.argtypes = [f8p, f8wp, vp, i32, i32, f8p, f8p, vp]
+    L.refcache_f8_linear_gelu_backward.argtypes = [f8p, f8wp, i32, f8p, vp, i64, f8p, vp]
+    L.refcache_f8_weight_grad_bytes.argtypes = [i64, i32, i32]
+    L.refcache_f8_weight_grad_bytes.restype = ctypes.c_size_t
+    L.refcache_f8_weight_grad.argtypes = [vp, i64, f8p, i32, vp, vp, i32, vp, vp, vp]
     L.refcache_status.argtypes = [vp]
     L.refcache_cache_status.argtypes = [vp, vp]
     L.refcache_set_wait_timeout_ns.argtypes = [ctypes.c_uint64]
@@ -798,3 +819,173 @@ def clip_gradients(grads, max_norm, out=None, norm=None, stream=None):
     _check(L.refcache_clip_gradients(n, *[None if a is None else a.buffer_info()[0] for a in lists], max_norm, norm_ptr,
                                      work.data_ptr(), _stream(stream)))
     return norm
+
+
+# ---------------------------------------------------------------- linear layers in 8 bits
+def _f8_scales(rows, blocks, device):
+    """Memory for rows of scales, and its used part as torch's UE8M0."""
+    mem = _torch.empty((rows, (blocks + 3) // 4 * 4), dtype=_torch.uint8, device=device)
+    return mem, mem[:, :blocks].view(_torch.float8_e8m0fnu)
+
+
+class F8Rows:
+    """Rows in 8-bit form (refcache_f8_rows_t): ``codes`` [rows, width] float8_e4m3fn, and ``scales`` [rows, blocks of
+    128 columns] float8_e8m0fnu.  A value is its code times its block's scale."""
+
+    def __init__(self, rows, width, device=None):
+        if _torch is None:
+            _use_torch()
+        device = _torch.device("cuda", _device()) if device is None else _torch.device(device)
+        self.rows, self.width = int(rows), int(width)
+        self.codes = _torch.empty((self.rows, self.width), dtype=_torch.float8_e4m3fn, device=device)
+        self._mem, self.scales = _f8_scales(self.rows, (self.width + 127) // 128, device)
+        self.device = self.codes.get_device()
+        self.c = _F8Rows(self.rows, self.width, self.codes.data_ptr(), self._mem.data_ptr())
+        self._ref = ctypes.byref(self.c)
+
+
+class F8Weight:
+    """A weight [out, in] in 8-bit form, as it lies (``codes``, ``scales``) and transposed (``codes_t``, ``scales_t``), one scale
+    for each 128 x 128 (refcache_f8_weight_t)."""
+
+    def __init__(self, out_width, in_width, device=None):
+        if _torch is None:
+            _use_torch()
+        device = _torch.device("cuda", _device()) if device is None else _torch.device(device)
+        self.out_width, self.in_width = n, k = int(out_width), int(in_width)
+        self.codes, self.codes_t = (_torch.empty(s, dtype=_torch.float8_e4m3fn, device=device) for s in ((n, k), (k, n)))
+        nb, kb = (n + 127) // 128, (k + 127) // 128
+        self._mem, self.scales = _f8_scales(nb, kb, device)
+        self._mem_t, self.scales_t = _f8_scales(kb, nb, device)
+        self.device = self.codes.get_device()
+        self.c = _F8Weight(n, k, *(t.data_ptr() for t in (self.codes, self._mem, self.codes_t, self._mem_t)))
+        self._ref = ctypes.byref(self.c)
+
+
+def _f8_refs(device, kind, **forms):
+    """References to 8-bit forms (None where there is none) on the call's device."""
+    out = []
+    for name, f in forms.items():
+        if f is None:
+            out.append(None)
+            continue
+        if not isinstance(f, kind):
+            raise ValueError(f"{name}: expected {kind.__name__}, got {type(f).__name__}")
+        if f.device != device:
+            raise _elsewhere(f.codes, device, name)
+        out.append(f._ref)
+    return out
+
+
+def _f8_tensor(name, t, rows, width, device):
+    """The pointer of a bf16 [rows, width] tensor whose rows may lie apart, and the elements between them."""
+    if t.dtype is not _bfloat16 or t.shape != (rows, width):
+        raise ValueError(f"{name}: expected bf16 [{rows}, {width}], got {t.dtype} {tuple(t.shape)}")
+    if t.get_device() != device:
+        raise _elsewhere(t, device, name)
+    s = t.stride()
+    if s[1] != 1 and width > 1:
+        raise ValueError(f"{name}: its rows must be contiguous, got strides {s}")
+    return t.data_ptr() or _NOTHING, s[0] if rows > 1 else width
+
+
+def f8_quantize(x, out=None, stream=None):
+    """The 8-bit form of ``x`` [rows, width] bf16 (rows may lie apart): an F8Rows, ``out`` if given."""
+    if _torch is None:
+        _use_torch()
+    device = _device()
+    if x.dim() != 2:
+        raise ValueError(f"x: expected [rows, width], got {tuple(x.shape)}")
+    ptr, ld = _f8_tensor("x", x, *x.shape, device)
+    if out is None:
+        out = F8Rows(*x.shape)
+    ref, = _f8_refs(device, F8Rows, out=out)
+    if (out.rows, out.width) != x.shape:
+        raise ValueError(f"out: expected {tuple(x.shape)}, got {(out.rows, out.width)}")
+    _check(load().refcache_f8_quantize(ptr, ld, ref, _stream(stream)))
+    return out
+
+
+def f8_quantize_weight(w, out=None, stream=None):
+    """The 8-bit form of a weight [out, in], bf16 or float32: an F8Weight, ``out`` if given."""
+    if _torch is None:
+        _use_torch()
+    device = _device()
+    f32 = w.dtype is _float32
+    if w.dim() != 2 or not (f32 or w.dtype is _bfloat16):
+        raise ValueError(f"w: expected bf16 or float32 [out, in], got {w.dtype} {tuple(w.shape)}")
+    ptr = _ptr(w, device, "w")
+    if out is None:
+        out = F8Weight(*w.shape)
+    ref, = _f8_refs(device, F8Weight, out=out)
+    if (out.out_width, out.in_width) != w.shape:
+        raise ValueError(f"out: expected {tuple(w.shape)}, got {(out.out_width, out.in_width)}")
+    _check(load().refcache_f8_quantize_weight(ptr, 1 if f32 else 0, ref, _stream(stream)))
+    return out
+
+
+def f8_linear(x, weight, y, bias=None, transposed=False, stream=None):
+    """y = x w^T + bias from the 8-bit forms of x [rows, in] and w [out, in]; with ``transposed`` y = x w from x [rows, out]
+    (the input's gradient, from the output's).  y bf16, its rows may lie apart; bias bf16 or float32."""
+    if _torch is None:
+        _use_torch()
+    device = _device()
+    rx, = _f8_refs(device, F8Rows, x=x)
+    rw, = _f8_refs(device, F8Weight, weight=weight)
+    width = weight.in_width if transposed else weight.out_width
+    pb, f32 = _param("bias", bias, width, None, device)
+    py, ld = _f8_tensor("y", y, x.rows, width, device)
+    _check(load().refcache_f8_linear(rx, rw, 1 if transposed else 0, pb, 1 if f32 else 0, py, ld, _stream(stream)))
+
+
+def _gelu_form(form):
+    if form not in GELU_FORMS:
+        raise ValueError(f"form: expected one of {sorted(GELU_FORMS)}, got {form!r}")
+    return GELU_FORMS[form]
+
+
+def f8_linear_gelu(x, weight, a, u8=None, bias=None, form="erf", stream=None):
+    """u = x w^T + bias; ``a`` gets the 8-bit form of gelu(u) and ``u8`` (the checkpoint, may be None) that of u."""
+    if _torch is None:
+        _use_torch()
+    device = _device()
+    rx, ra, ru = _f8_refs(device, F8Rows, x=x, a=a, u8=u8)
+    rw, = _f8_refs(device, F8Weight, weight=weight)
+    pb, f32 = _param("bias", bias, weight.out_width, None, device)
+    _check(load().refcache_f8_linear_gelu(rx, rw, pb, 1 if f32 else 0, _gelu_form(form), ra, ru, _stream(stream)))
+
+
+def f8_linear_gelu_backward(dy, weight, u8, du=None, du8=None, form="erf", stream=None):
+    """du = (dy w) gelu'(u) from the 8-bit forms of dy, the gradient of the output of the layer behind the GELU, that layer's
+    weight and the checkpoint of u: bf16 ``du`` (rows may lie apart) and its 8-bit form ``du8``, either of them None."""
+    if _torch is None:
+        _use_torch()
+    device = _device()
+    rdy, ru, rdu = _f8_refs(device, F8Rows, dy=dy, u8=u8, du8=du8)
+    rw, = _f8_refs(device, F8Weight, weight=weight)
+    pd, ld = (None, 0) if du is None else _f8_tensor("du", du, dy.rows, weight.in_width, device)
+    _check(load().refcache_f8_linear_gelu_backward(rdy, rw, _gelu_form(form), ru, pd, ld, rdu, _stream(stream)))
+
+
+def f8_weight_grad(dy, x, dw, add=None, d_bias=None, stream=None):
+    """dw = add + dy^T x from bf16 dy [rows, out] (rows may lie apart) and the 8-bit form of x [rows, in]: dw [out, in]
+    float32 or bf16, ``add`` like it (or it itself, or None); d_bias float32 [out] = the sums of dy, unless it is None."""
+    if _torch is None:
+        _use_torch()
+    device = _device()
+    rx, = _f8_refs(device, F8Rows, x=x)
+    if dw.dim() != 2:
+        raise ValueError(f"dw: expected [out, in], got {tuple(dw.shape)}")
+    n, f32 = dw.shape[0], dw.dtype is _float32
+    if not (f32 or dw.dtype is _bfloat16) or dw.shape[1] != x.width:
+        raise ValueError(f"dw: expected bf16 or float32 [out, {x.width}], got {dw.dtype} {tuple(dw.shape)}")
+    if add is not None and (add.dtype is not dw.dtype or add.shape != dw.shape):
+        raise ValueError(f"add: expected {dw.dtype} {tuple(dw.shape)}, got {add.dtype} {tuple(add.shape)}")
+    if d_bias is not None and (d_bias.dtype is not _float32 or d_bias.shape != (n,)):
+        raise ValueError(f"d_bias: expected float32 [{n}], got {d_bias.dtype} {tuple(d_bias.shape)}")
+    pdy, ld = _f8_tensor("dy", dy, x.rows, n, device)
+    L = load()
+    nbytes = L.refcache_f8_weight_grad_bytes(x.rows, n, x.width)
+    work = _work(nbytes, dw, stream) if nbytes else None
+    _check(L.refcache_f8_weight_grad(pdy, ld, rx, n, _ptr(add, device, "add"), _ptr(dw, device, "dw"), 1 if f32 else 0,
+                                     _ptr(d_bias, device, "d_bias"), None if work is None else work.data_ptr(), _stream(stream)))
