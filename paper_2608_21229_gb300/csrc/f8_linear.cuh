@@ -1,0 +1,288 @@
+// f8_linear.cuh -- y = x w^T on 8-bit rows and weights (f8_common.cuh): block-scaled
+// tcgen05 MMAs over CTA pairs, 256 rows x up to 256 columns a tile.
+//
+// CTA r of a pair holds rows [128 r, 128 r + 128) of x's tile and half of w's; a
+// stage is 128 columns of both (32 KB), four MMAs of K = 32.  The scales are applied
+// by the tensor core: a warp of each CTA collects the words of 512 columns (four blocks'
+// bytes a row) and lays them out for tcgen05.cp, which the MMA thread issues before
+// the first MMA that needs them; sums stay in tensor memory from the first column to the
+// last.
+//
+// Tensor memory: two halves of 128 columns of sums, then the scales' slots.  A tile wider
+// than 128 takes both halves, a narrower one every second; a half is free as soon as its
+// four warps have its 128 columns in registers, a row's block of 128 to a thread, which
+// then finds the block's scale, the GELU or its gradient without another thread's help
+// while the MMAs of the next tile run.
+#pragma once
+#include "f8_pair.cuh"
+
+namespace rc {
+namespace f8 {
+
+struct LinearArgs {
+  Out o;
+  const uint8_t *x_scales, *w_scales;
+  int32_t x_pitch, w_pitch, w_rows;  // w_rows: rows of w's scales
+  int32_t k;                         // columns of x
+  int32_t bn;                        // columns of a tile: a multiple of 32 up to 256
+  Tiles tiles;
+  Guard guard;
+};
+
+struct LinearSmem {
+  static constexpr int kSlots = 6, kScaleSlots = 4;
+  static constexpr uint32_t kA = 16384, kSlot = 2 * kA, kScaleSlot = 512 * 3;
+  static constexpr uint32_t kScales = kSlots * kSlot, kBars = kScales + kScaleSlots * kScaleSlot;
+  static constexpr int kFull = 0, kEmpty = kFull + kSlots, kScFull = kEmpty + kSlots, kScEmpty = kScFull + kScaleSlots,
+                       kAccFull = kScEmpty + kScaleSlots, kAccEmpty = kAccFull + 2, kDone = kAccEmpty + 2, kNumBars = kDone + 1;
+  static constexpr uint32_t kAux = kBars + 8 * kNumBars, kUsed = kAux + 20, kDynamic = kUsed + 1024;
+  static constexpr int kEpiWarps = 8, kProducer = 8, kMma = 9, kScaler = 10, kThreads = 32 * 11;
+  static constexpr uint32_t kTmemScales = 256;
+  static_assert(kDynamic <= kMaxDynamic, "shared-memory layout too large");
+  __device__ static constexpr uint32_t arrivals(int i) {
+    return i >= kScFull && i < kScEmpty ? 2 : i >= kAccEmpty && i < kDone ? 8 : 1;
+  }
+};
+
+// 128 columns of this thread's lane; those from `cols` on are not there.
+__device__ __forceinline__ void load_sums(uint32_t t, int cols, float (&v)[128]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (32 * i >= cols) break;
+    uint32_t r[32];
+    tmem_ld32(t + 32 * i, r);
+    tmem_wait_ld(r);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[32 * i + j] = __uint_as_float(r[j]);
+  }
+}
+
+// One row's block of 128 columns in a thread, `cols` of them there (a multiple of 16).
+__device__ __forceinline__ void quantize_row(const Rows& r, int64_t row, int col0, int cols, const float (&v)[128]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 128; ++i) m = (i & ~15) < cols ? max(m, abs_bits(v[i])) : m;
+  const uint32_t b = scale_byte(m);
+  const float s = to_codes(b);
+  uint8_t* to = r.codes + row * r.width + col0;
+#pragma unroll
+  for (int i = 0; i < 128; i += 16)
+    if (i < cols)
+      *reinterpret_cast<uint4*>(to + i) =
+          make_uint4(pack_e4m3x4(v[i] * s, v[i + 1] * s, v[i + 2] * s, v[i + 3] * s), pack_e4m3x4(v[i + 4] * s, v[i + 5] * s, v[i + 6] * s, v[i + 7] * s),
+                     pack_e4m3x4(v[i + 8] * s, v[i + 9] * s, v[i + 10] * s, v[i + 11] * s),
+                     pack_e4m3x4(v[i + 12] * s, v[i + 13] * s, v[i + 14] * s, v[i + 15] * s));
+  r.scales[row * r.pitch + col0 / kBlock] = static_cast<uint8_t>(b);
+}
+__device__ __forceinline__ void store_row(uint16_t* y, int cols, const float (&v)[128]) {
+#pragma unroll
+  for (int i = 0; i < 128; i += 8)
+    if ((i & ~15) < cols)
+      *reinterpret_cast<uint4*>(y + i) = make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]), pack_bf16x2(v[i + 4], v[i + 5]),
+                                                    pack_bf16x2(v[i + 6], v[i + 7]));
+}
+template <int kEpi>
+__device__ __forceinline__ void finish_block(const Out& o, int64_t row, int col0, int cols, float (&v)[128], const uint4 (&u)[8]) {
+  if (o.bias) {
+#pragma unroll
+    for (int i = 0; i < 128; i += 8)
+      if ((i & ~15) < cols) {
+        if (reinterpret_cast<uintptr_t>(o.bias) % 16) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[i + j] += bias_at(o, col0 + i + j);
+        } else {
+          const Vec8 b = load_param8(o.bias, col0 + i, o.bias_f32 != 0);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[i + j] += b.v[j];
+        }
+      }
+  }
+  if (kEpi == kStore) store_row(o.y + row * o.ld + col0, cols, v);
+  if ((kEpi & ~1) == kGelu) {
+    if (o.u.codes) quantize_row(o.u, row, col0, cols, v);
+#pragma unroll
+    for (int i = 0; i < 128; ++i) v[i] = gelu<kEpi & 1>(v[i]);
+    quantize_row(o.a, row, col0, cols, v);
+  }
+  if ((kEpi & ~1) == kGeluGrad) {
+    const float s = from_codes(o.u.scales[row * o.u.pitch + col0 / kBlock]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float4 x = unpack_e4m3x4(w[j]);
+        float* p = v + 16 * i + 4 * j;
+        p[0] *= gelu_grad<kEpi & 1>(x.x * s), p[1] *= gelu_grad<kEpi & 1>(x.y * s);
+        p[2] *= gelu_grad<kEpi & 1>(x.z * s), p[3] *= gelu_grad<kEpi & 1>(x.w * s);
+      }
+    }
+    if (o.y) store_row(o.y + row * o.ld + col0, cols, v);
+    if (o.a.codes) quantize_row(o.a, row, col0, cols, v);
+  }
+}
+
+template <int kEpi>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads, 1)
+    f8_linear_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ LinearArgs a) {
+  using L = LinearSmem;
+  extern __shared__ uint8_t smem_raw[];
+  Cta<L> c;
+  if (!c.enter(smem_raw, a.guard)) return;
+  const int cluster = static_cast<int>(blockIdx.x >> 1), n_clusters = static_cast<int>(gridDim.x >> 1);
+  const int n_tiles = a.tiles.m * a.tiles.n, blocks = (a.k + kBlock - 1) / kBlock;
+  const bool wide = a.bn > 128;  // a tile takes both halves
+  const uint32_t cta_bytes = L::kA + static_cast<uint32_t>(a.bn) * 64u;
+  int loads = 0;
+  if (c.warp == L::kProducer) {
+    if (c.lane == 0) {
+      const int most = loads_before_stop(a.guard.stop, c.rank);
+      bool ok = true;
+#pragma unroll 1
+      for (int t = cluster; ok && t < n_tiles; t += n_clusters) {
+        int i, j;
+        a.tiles.at(t, &i, &j);
+        const int y = i * 256 + 128 * static_cast<int>(c.rank), z = j * a.bn + a.bn / 2 * static_cast<int>(c.rank);
+#pragma unroll 1
+        for (int kb = 0; kb < blocks; ++kb) {
+          const int s = loads % L::kSlots, n = loads / L::kSlots;
+          if (loads == most || (n > 0 && !c.wait(L::kEmpty + s, n - 1, 101))) {
+            ok = false;
+            break;
+          }
+          const uint32_t at = c.base + static_cast<uint32_t>(s) * L::kSlot, full = c.lbar(L::kFull + s);
+          if (c.leader) mbar_arrive_expect_tx(c.bar(L::kFull + s), 2 * cta_bytes);
+          tma_load_2d_pair(at, &x_map, full, kb * kBlock, y);
+          tma_load_2d_pair(at + L::kA, &w_map, full, kb * kBlock, z);
+          ++loads;
+        }
+      }
+    }
+    __syncwarp();
+  } else if (c.warp == L::kScaler) {
+    int n = 0;
+    bool ok = true;
+    const int groups = (blocks + 3) / 4;
+#pragma unroll 1
+    for (int t = cluster; ok && t < n_tiles; t += n_clusters) {
+      int i, j;
+      a.tiles.at(t, &i, &j);
+      const int64_t row0 = static_cast<int64_t>(i) * 256 + 128 * c.rank + c.lane;
+      const int wr0 = j * a.bn;
+#pragma unroll 1
+      for (int g = 0; g < groups; ++g, ++n) {
+        const int s = n % L::kScaleSlots;
+        uint32_t w[12];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int64_t row = row0 + 32 * q;
+          w[q] = row < a.o.rows ? *reinterpret_cast<const uint32_t*>(a.x_scales + row * a.x_pitch + 4 * g) : 0x7F7F7F7Fu;
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const int row = (wr0 + 32 * q) / kBlock;
+          w[4 + q] = 32 * q < a.bn && row < a.w_rows ? *reinterpret_cast<const uint32_t*>(a.w_scales + static_cast<int64_t>(row) * a.w_pitch + 4 * g) : 0x7F7F7F7Fu;
+        }
+        if (n >= L::kScaleSlots && !c.wait_all(L::kScEmpty + s, n / L::kScaleSlots - 1, 102)) {
+          ok = false;
+          break;
+        }
+        const uint32_t at = c.base + L::kScales + static_cast<uint32_t>(s) * L::kScaleSlot + 16u * c.lane;
+        st_shared_v4(at, make_uint4(w[0], w[1], w[2], w[3]));
+        st_shared_v4(at + 512, make_uint4(w[4], w[5], w[6], w[7]));
+        st_shared_v4(at + 1024, make_uint4(w[8], w[9], w[10], w[11]));
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (c.lane == 0) mbar_arrive_release_cluster(c.lbar(L::kScFull + s));
+        __syncwarp();
+      }
+    }
+  } else if (c.warp == L::kMma) {
+    if (c.leader) {
+      const uint64_t ad = sdesc_sw128(c.base, 16, 1024), bd = sdesc_sw128(c.base + L::kA, 16, 1024);
+      const uint64_t sd = scales_desc(c.base + L::kScales);
+      const uint32_t idesc = idesc_mx(256, a.bn);
+      bool issued = false, ok = true;
+      int load = 0, group = 0, used = 0;
+#pragma unroll 1
+      for (int t = cluster; ok && t < n_tiles; t += n_clusters, ++used) {
+        const uint32_t d = c.tmem + (wide ? 0u : 128u * (used & 1));
+        // the half's (both halves') earlier sums are in registers
+        const int before = wide ? used : used >> 1;
+        if (before > 0 && !(wide ? c.wait_all(L::kAccEmpty, before - 1, 103) && c.wait_all(L::kAccEmpty + 1, before - 1, 103)
+                                 : c.wait_all(L::kAccEmpty + (used & 1), before - 1, 103)))
+          break;
+#pragma unroll 1
+        for (int kb = 0; kb < blocks; ++kb, ++load) {
+          const int s = load % L::kSlots, sc = group % L::kScaleSlots;
+          const uint32_t sfa = c.tmem + L::kTmemScales + 16u * sc, sfb = sfa + 4;
+          if ((kb & 3) == 0) {
+            ok = c.wait_all(L::kScFull + sc, group / L::kScaleSlots, 104) &&
+                 __all_sync(0xffffffffu, mbar_try_wait_acquire_cluster(c.bar(L::kScFull + sc), static_cast<uint32_t>(group / L::kScaleSlots) & 1u));
+            if (!ok) break;
+          }
+          ok = c.wait_all(L::kFull + s, load / L::kSlots, 105);
+          if (!ok) break;
+          issued = true;
+          const int steps = min(4, (a.k - kb * kBlock + 31) / 32);
+          const bool last = kb + 1 == blocks;
+          if (elect_one()) {
+            tc_fence_after();
+            if ((kb & 3) == 0) {
+              const uint64_t at = sd + static_cast<uint64_t>(sc) * (L::kScaleSlot >> 4);
+              copy_scales_pair(sfa, at);
+              copy_scales_pair(sfb, at + (512 >> 4));
+              copy_scales_pair(sfb + 4, at + (1024 >> 4));
+            }
+            const uint64_t off = static_cast<uint64_t>(s) * (L::kSlot >> 4);
+            const uint32_t id = idesc_byte(idesc, kb & 3);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              if (q < steps) mx_mma_pair(d, ad + off + 2 * q, bd + off + 2 * q, id, sfa, sfb, kb > 0 || q > 0 ? 1u : 0u);
+            tc2_commit_mc(c.bar(L::kEmpty + s), 3);
+            if ((kb & 3) == 3 || last) tc2_commit_mc(c.bar(L::kScEmpty + sc), 3);
+            if (last) {
+              if (wide || !(used & 1)) tc2_commit_mc(c.bar(L::kAccFull), 3);
+              if (wide || (used & 1)) tc2_commit_mc(c.bar(L::kAccFull + 1), 3);
+            }
+          }
+          __syncwarp();
+          if ((kb & 3) == 3 || last) ++group;
+        }
+      }
+      c.finish_mmas(issued);
+    }
+  } else {
+    const int half = c.warp >> 2, quarter = c.warp & 3;
+    int used = 0;
+#pragma unroll 1
+    for (int t = cluster; t < n_tiles; t += n_clusters, ++used) {
+      if (!wide && (used & 1) != half) continue;
+      int i, j;
+      a.tiles.at(t, &i, &j);
+      const int64_t row = static_cast<int64_t>(i) * 256 + 128 * c.rank + 32 * quarter + c.lane;
+      const int col0 = j * a.bn + (wide ? 128 * half : 0);
+      const int in_tile = wide ? min(128, a.bn - 128 * half) : a.bn, cols = min(in_tile, a.o.width - col0);
+      const bool in = row < a.o.rows && cols > 0;
+      uint4 u[8] = {};
+      if ((kEpi & ~1) == kGeluGrad && in) {
+        const uint8_t* from = a.o.u.codes + row * a.o.u.width + col0;
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          if (16 * q < cols) u[q] = *reinterpret_cast<const uint4*>(from + 16 * q);
+      }
+      if (!c.wait_all(L::kAccFull + half, wide ? used : used >> 1, 106)) break;
+      tc_fence_after();
+      float v[128];
+      load_sums(c.tmem + 128u * half + (static_cast<uint32_t>(quarter) << 21), in_tile, v);
+      tc_fence_before();
+      __syncwarp();
+      if (c.lane == 0) mbar_arrive_cluster(c.lbar(L::kAccEmpty + half));
+      if (in) finish_block<kEpi>(a.o, row, col0, cols, v, u);
+    }
+  }
+  c.leave(loads, cta_bytes);
+}
+
+}  // namespace f8
+}  // namespace rc

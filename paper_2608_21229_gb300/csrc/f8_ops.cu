@@ -1,13 +1,15 @@
 // f8_ops.cu -- the entry points of include/refcache.h for linear layers in 8 bits:
-// rows and weights into their 8-bit form (f8_rows.cuh), products on it (f8_simple.cuh).
+// rows and weights into their 8-bit form (f8_rows.cuh), products on it (f8_linear.cuh).
 // Argument checks and launches; no call allocates memory.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstdint>
 
 #include "refcache.h"
+#include "f8_linear.cuh"
 #include "f8_rows.cuh"
 #include "f8_simple.cuh"
 #include "host_common.h"
@@ -76,15 +78,69 @@ rc::f8::Rows rows_of(const refcache_f8_weight_t* w, bool transposed) {
   return {static_cast<uint8_t*>(w->codes), static_cast<uint8_t*>(w->scales), w->out_width, w->in_width, REFCACHE_F8_PITCH(w->in_width)};
 }
 
+// CTA pairs of a kernel that run at once on the current device; sets its attributes on first use.
+template <typename Kernel>
+int pairs_of(Kernel kernel, std::atomic<int>& kept, int threads, uint32_t smem, int sms, int* pairs) {
+  int n = kept.load();
+  if (n == 0) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(f8)");
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(2 * static_cast<unsigned>(sms / 2));
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+    if (e != cudaSuccess || n < 1) n = sms / 2;
+    kept.store(n);
+  }
+  *pairs = n;
+  return REFCACHE_OK;
+}
+
+// Columns of a tile, a multiple of `step`: the fewest cycles by rounds of tiles over the pairs.  A
+// block of 128 columns of x takes a pair 2 bn cycles of MMAs, or (256 + bn) to bring its 16 KB + 64 bn
+// bytes into each CTA's shared memory and read them out at 128 bytes a cycle.
+int tile_columns(int64_t rows, int width, int blocks, int pairs, int step) {
+  int best = step;
+  int64_t least = -1;
+  for (int bn = step; bn <= 256; bn += step) {
+    const int64_t tiles = static_cast<int64_t>(ceil_div(rows, 256)) * ceil_div(width, bn);
+    const int64_t cost = ((tiles + pairs - 1) / pairs) * (static_cast<int64_t>(blocks) * (256 + bn) + 700);
+    if (least < 0 || cost <= least) least = cost, best = bn;
+  }
+  return best;
+}
+
 template <int kEpi>
 int launch_linear(const rc::f8::Rows& x, const rc::f8::Rows& w, const rc::f8::Out& o, void* stream) {
+  using L = rc::f8::LinearSmem;
   if (o.rows == 0) return REFCACHE_OK;
-  int sms = 0;
-  const int rc = device_sms(&sms);
-  if (rc) return rc;
-  const cudaError_t e = launch_dependent(rc::f8::f8_linear_simple_kernel<kEpi>, dim3(ceil_div(o.width, 128), ceil_div(o.rows, 32)), dim3(256), 0,
-                                         static_cast<cudaStream_t>(stream), x, w, o);
-  return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "f8_linear launch");
+  static std::atomic<int> kept[rc_host::kMaxDevices];
+  int sms = 0, dev = 0, pairs = 0;
+  rc::f8::LinearArgs a{};
+  int rc = device_sms(&sms);
+  if (rc || (rc = rc_host::device_status_word(&dev, &a.guard.status)) != 0 ||
+      (rc = pairs_of(rc::f8::f8_linear_kernel<kEpi>, kept[dev], L::kThreads, L::kDynamic, sms, &pairs)) != 0)
+    return rc;
+  const int blocks = static_cast<int>(ceil_div(x.width, 128));
+  a.o = o;
+  a.x_scales = x.scales, a.x_pitch = x.pitch, a.w_scales = w.scales, a.w_pitch = w.pitch;
+  a.w_rows = static_cast<int>(ceil_div(w.rows, 128));
+  a.k = x.width;
+  a.bn = tile_columns(o.rows, o.width, blocks, pairs, kEpi == rc::f8::kStore ? 32 : 128);
+  const int64_t tiles_m = ceil_div(o.rows, 256), tiles_n = ceil_div(o.width, a.bn);
+  if (tiles_m * tiles_n > (1ll << 30)) return fail(REFCACHE_ERR_INVALID_ARG, "too many rows for a width of %d", o.width);
+  a.tiles = {static_cast<int32_t>(tiles_m), static_cast<int32_t>(tiles_n)};
+  a.guard.timeout_ns = rc_host::wait_timeout_ns();
+  CUtensorMap xm, wm;
+  if ((rc = rc_host::encode_map(&xm, x.codes, 1, x.width, x.rows, x.width, 128)) != 0 ||
+      (rc = rc_host::encode_map(&wm, w.codes, 1, w.width, w.rows, w.width, static_cast<uint32_t>(a.bn / 2))) != 0)
+    return rc;
+  a.guard.stop = rc_host::take_debug_stop();
+  const unsigned clusters = static_cast<unsigned>(std::min<int64_t>(tiles_m * tiles_n, pairs));
+  const cudaError_t e = launch_dependent(rc::f8::f8_linear_kernel<kEpi>, dim3(2 * clusters), dim3(L::kThreads), L::kDynamic,
+                                         static_cast<cudaStream_t>(stream), xm, wm, a);
+  return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "f8_linear_kernel launch");
 }
 
 }  // namespace

@@ -1,4 +1,4 @@
-// f8_simple.cuh -- the products on 8-bit rows and weights, in fp32 FMAs: tiles of 32 x
+// f8_simple.cuh -- the weight gradient on 8-bit rows, in fp32 FMAs: tiles of 32 x
 // 128 outputs, one warp to four rows, four columns a lane.
 #pragma once
 #include "f8_common.cuh"
@@ -46,16 +46,6 @@ __device__ __forceinline__ void simple_product(int64_t rows, int cols, int64_t l
     if (r0 + 4 * warp + i < rows) finish(r0 + 4 * warp + i, c0, lane, acc[i]);
 }
 
-// w: the orientation whose rows are the outputs' columns.
-template <int kEpi>
-__global__ void __launch_bounds__(256) f8_linear_simple_kernel(const Rows x, const Rows w, const Out o) {
-  grid_dependency_wait();
-  grid_launch_dependents();
-  simple_product(
-      o.rows, o.width, x.width, [&](int64_t r, int64_t l) { return value_of(x, r, r, static_cast<int>(l)); },
-      [&](int c, int64_t l) { return value_of(w, c, c / kBlock, static_cast<int>(l)); },
-      [&](int64_t r, int c, int lane, float4 v) { finish_row<kEpi>(o, r, c, lane, v); });
-}
 
 struct WgradArgs {
   const uint16_t* dy;  // [rows, n], ld elements between rows

@@ -1,6 +1,7 @@
 // host_common.h -- what the library's translation units share on the host: the
 // error message of the calling thread and the check of the current device.
 #pragma once
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -15,6 +16,17 @@ int cuda_fail(cudaError_t e, const char* what);
 
 // The current device's number of SMs; REFCACHE_ERR_UNSUPPORTED unless it is an sm_103 device.
 int device_sms(int* sms);
+
+// The current device and its error word (refcache_status), whose address is looked up once.
+int device_status_word(int* dev, int** word);
+
+// The limit of every wait in a kernel, and the fault injection of the next launch (cleared).
+uint64_t wait_timeout_ns();
+int take_debug_stop();
+
+// A 2-D tensor map with the 128-byte swizzle: `outer` rows of `inner` elements (1 byte, or 2:
+// bf16), `pitch` bytes apart; boxes of 128 bytes x box_outer rows.
+int encode_map(CUtensorMap* m, const void* base, int elem_bytes, int64_t inner, int64_t outer, int64_t pitch, uint32_t box_outer);
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
