@@ -543,6 +543,11 @@ REFCACHE_API int refcache_clip_gradients(int n, const void* const* grads, void* 
  *   - Codes are packed [rows, width], 16-byte aligned; scales are rows of
  *     REFCACHE_F8_PITCH(width) bytes, 16-byte aligned, of which the first
  *     ceil(width / 128) are used and written.
+ *   - tiles, REFCACHE_F8_TILES(rows, width) bytes, 16-byte aligned, hold the same scales once
+ *     more, as the tensor cores take them: the four bytes of 512 columns of row r are the word at
+ *     512 (g ceil(rows / 128) + r / 128) + 16 (r % 32) + 4 (r / 32 % 4) for the g-th 512
+ *     columns (a weight's rows of one block alike).  What belongs to no row or block is not
+ *     written, and may hold anything.
  *   - Products are summed in fp32; results are rounded once.
  *   - bf16 tensors of rows may have ld elements between rows (a multiple of 8).
  *   - Outputs must not overlap inputs or each other (but for dw over add).
@@ -552,27 +557,31 @@ REFCACHE_API int refcache_clip_gradients(int n, const void* const* grads, void* 
  *     give the same bits.
  */
 #define REFCACHE_F8_PITCH(width) (((width) + 511) / 512 * 4)
+#define REFCACHE_F8_TILES(rows, width) (((width) + 511) / 512 * (((int64_t)(rows) + 127) / 128) * 512)
 typedef struct {
   int64_t rows;
   int32_t width;
   void* codes;  /* [rows, width] */
   void* scales; /* [rows, REFCACHE_F8_PITCH(width)] */
+  void* tiles;  /* REFCACHE_F8_TILES(rows, width) bytes */
 } refcache_f8_rows_t;
 typedef struct {
   int32_t out_width, in_width; /* w is [out_width, in_width] */
   void *codes, *scales;        /* [out, in]; [ceil(out / 128), REFCACHE_F8_PITCH(in)] */
+  void* tiles;                 /* REFCACHE_F8_TILES(out, in) */
   void *codes_t, *scales_t;    /* transposed: [in, out]; [ceil(in / 128), REFCACHE_F8_PITCH(out)] (same values) */
+  void* tiles_t;               /* REFCACHE_F8_TILES(in, out) */
 } refcache_f8_weight_t;
 
 /* x: [out->rows, out->width] bf16, ld elements between rows. */
 REFCACHE_API int refcache_f8_quantize(const void* x, int64_t ld, const refcache_f8_rows_t* out, void* stream);
 
-/* w: [out_width, in_width], packed, fp32 (w_f32 != 0) or bf16.  codes_t and scales_t may both be NULL. */
+/* w: [out_width, in_width], packed, fp32 (w_f32 != 0) or bf16.  codes_t, scales_t and tiles_t may all be NULL. */
 REFCACHE_API int refcache_f8_quantize_weight(const void* w, int w_f32, const refcache_f8_weight_t* out, void* stream);
 
 /*
- * y = x w^T + bias [rows, out_width] (reads codes and scales), or with transposed != 0
- * y = x w [rows, in_width] (codes_t, scales_t): a layer's output, and its input's
+ * y = x w^T + bias [rows, out_width] (reads codes and tiles), or with transposed != 0
+ * y = x w [rows, in_width] (codes_t, tiles_t): a layer's output, and its input's
  * gradient from the 8-bit form of its output's.  y bf16; bias: one value for each
  * column of y, fp32 (bias_f32 != 0) or bf16, or NULL.
  */
@@ -591,7 +600,7 @@ REFCACHE_API int refcache_f8_linear_gelu(const refcache_f8_rows_t* x, const refc
 
 /*
  * Its gradient together with that of the layer behind it: from the 8-bit form of dy, the
- * gradient of that layer's output, and its weight w (reads codes_t, scales_t),
+ * gradient of that layer's output, and its weight w (reads codes_t, tiles_t),
  * du = (dy w) gelu'(u) with u as u8 holds it.  du [rows, in_width of w] bf16 and du8, the 8-bit
  * form of du before its rounding, are written; either may be NULL, not both.
  */

@@ -22,9 +22,23 @@ constexpr int kBlock = 128;  // columns of a scale
 struct Rows {  // refcache_f8_rows_t, or one orientation of a weight
   uint8_t* codes;
   uint8_t* scales;
+  uint8_t* tiles;
   int64_t rows;
   int32_t width, pitch;  // bytes between rows of scales
+  int32_t chunks;        // of 128 rows
 };
+// The scales are kept twice, by rows for those who read the values (weight gradients,
+// the GELU's gradient, a caller) and in the order that tcgen05.cp takes, 512 bytes
+// for 128 rows and 512 columns, which TMA brings in as they are.  Laid out by a warp
+// of the product's kernel instead, the words of 512 columns took 3200 cycles, longer than
+// their MMAs (2048).  The byte of a row's block in that order:
+__device__ __forceinline__ uint8_t* tile_byte(const Rows& r, int64_t row, int block) {
+  return r.tiles + (static_cast<int64_t>(block >> 2) * r.chunks + (row >> 7)) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3);
+}
+__device__ __forceinline__ void put_scale(const Rows& r, int64_t row, int block, uint32_t b) {
+  r.scales[row * r.pitch + block] = static_cast<uint8_t>(b);
+  *tile_byte(r, row, block) = static_cast<uint8_t>(b);
+}
 
 // The largest magnitude of a block is found as the largest of the bits without their
 // sign: above every finite value's lie infinity's, above these a NaN's.
@@ -99,7 +113,7 @@ __device__ __forceinline__ void quantize_warp(const Rows& r, int64_t row, int co
   const uint32_t b = scale_byte(m);
   const float s = to_codes(b);
   if (in) *reinterpret_cast<uint32_t*>(r.codes + row * r.width + col) = pack_e4m3x4(v.x * s, v.y * s, v.z * s, v.w * s);
-  if (lane == 0) r.scales[row * r.pitch + col / kBlock] = static_cast<uint8_t>(b);
+  if (lane == 0) put_scale(r, row, col / kBlock, b);
 }
 template <int kEpi>
 __device__ __forceinline__ void finish_row(const Out& o, int64_t row, int col0, int lane, float4 v) {

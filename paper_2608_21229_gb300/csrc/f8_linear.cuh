@@ -3,10 +3,9 @@
 //
 // CTA r of a pair holds rows [128 r, 128 r + 128) of x's tile and half of w's; a
 // stage is 128 columns of both (32 KB), four MMAs of K = 32.  The scales are applied
-// by the tensor core: a warp of each CTA collects the words of 512 columns (four blocks'
-// bytes a row) and lays them out for tcgen05.cp, which the MMA thread issues before
-// the first MMA that needs them; sums stay in tensor memory from the first column to the
-// last.
+// by the tensor core: those of 512 columns come as a load of their own (a word with
+// the bytes of four blocks for each row) and go into tensor memory by tcgen05.cp, issued before the
+// first MMA that needs them.  Sums stay in tensor memory from the first column to the last.
 //
 // Tensor memory: two halves of 128 columns of sums, then the scales' slots.  A tile wider
 // than 128 takes both halves, a narrower one every second; a half is free as soon as its
@@ -21,27 +20,29 @@ namespace f8 {
 
 struct LinearArgs {
   Out o;
-  const uint8_t *x_scales, *w_scales;
-  int32_t x_pitch, w_pitch, w_rows;  // w_rows: rows of w's scales
-  int32_t k;                         // columns of x
-  int32_t bn;                        // columns of a tile: a multiple of 32 up to 256
+  int32_t x_chunks, w_chunks;  // 128 rows each
+  int32_t k;                   // columns of x
+  int32_t bn;                  // columns of a tile: 64, 128, 192 or 256
   Tiles tiles;
   Guard guard;
 };
 
+struct LinearMaps {
+  CUtensorMap x, w;                // 128 rows, half a tile's columns; 128 codes
+  CUtensorMap x_tiles, w_tiles;    // 512 bytes
+};
+
 struct LinearSmem {
-  static constexpr int kSlots = 6, kScaleSlots = 4;
-  static constexpr uint32_t kA = 16384, kSlot = 2 * kA, kScaleSlot = 512 * 3;
-  static constexpr uint32_t kScales = kSlots * kSlot, kBars = kScales + kScaleSlots * kScaleSlot;
-  static constexpr int kFull = 0, kEmpty = kFull + kSlots, kScFull = kEmpty + kSlots, kScEmpty = kScFull + kScaleSlots,
-                       kAccFull = kScEmpty + kScaleSlots, kAccEmpty = kAccFull + 2, kDone = kAccEmpty + 2, kNumBars = kDone + 1;
-  static constexpr uint32_t kAux = kBars + 8 * kNumBars, kUsed = kAux + 20, kDynamic = kUsed + 1024;
-  static constexpr int kEpiWarps = 8, kProducer = 8, kMma = 9, kScaler = 10, kThreads = 32 * 11;
-  static constexpr uint32_t kTmemScales = 256;
+  static constexpr int kSlots = 6, kSlots2 = 4;  // stages, scales
+  static constexpr uint32_t kA = 16384, kSlot = 2 * kA, kScaleSlot = 3 * 512;
+  static constexpr uint32_t kScales = kSlots * kSlot, kBars = kScales + kSlots2 * kScaleSlot;
+  static constexpr int kFull = 0, kEmpty = kFull + kSlots, kFull2 = kEmpty + kSlots, kEmpty2 = kFull2 + kSlots2, kAccFull = kEmpty2 + kSlots2,
+                       kAccEmpty = kAccFull + 2, kDone = kAccEmpty + 2, kNumBars = kDone + 1;
+  static constexpr uint32_t kAux = kBars + 8 * kNumBars, kUsed = kAux + 28, kDynamic = kUsed + 1024;
+  static constexpr int kProducer = 8, kMma = 9, kThreads = 32 * 10;  // warps 0-7: sums
+  static constexpr uint32_t kTmemScales = 256;                       // 16 columns a slot: four of x's words, eight of w's
   static_assert(kDynamic <= kMaxDynamic, "shared-memory layout too large");
-  __device__ static constexpr uint32_t arrivals(int i) {
-    return i >= kScFull && i < kScEmpty ? 2 : i >= kAccEmpty && i < kDone ? 8 : 1;
-  }
+  __device__ static constexpr uint32_t arrivals(int i) { return i >= kAccEmpty && i < kDone ? 8 : 1; }  // four warps of each CTA
 };
 
 // 128 columns of this thread's lane; those from `cols` on are not there.
@@ -72,7 +73,7 @@ __device__ __forceinline__ void quantize_row(const Rows& r, int64_t row, int col
           make_uint4(pack_e4m3x4(v[i] * s, v[i + 1] * s, v[i + 2] * s, v[i + 3] * s), pack_e4m3x4(v[i + 4] * s, v[i + 5] * s, v[i + 6] * s, v[i + 7] * s),
                      pack_e4m3x4(v[i + 8] * s, v[i + 9] * s, v[i + 10] * s, v[i + 11] * s),
                      pack_e4m3x4(v[i + 12] * s, v[i + 13] * s, v[i + 14] * s, v[i + 15] * s));
-  r.scales[row * r.pitch + col0 / kBlock] = static_cast<uint8_t>(b);
+  put_scale(r, row, col0 / kBlock, b);
 }
 __device__ __forceinline__ void store_row(uint16_t* y, int cols, const float (&v)[128]) {
 #pragma unroll
@@ -124,7 +125,7 @@ __device__ __forceinline__ void finish_block(const Out& o, int64_t row, int col0
 
 template <int kEpi>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads, 1)
-    f8_linear_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ LinearArgs a) {
+    f8_linear_kernel(const __grid_constant__ LinearMaps maps, const __grid_constant__ LinearArgs a) {
   using L = LinearSmem;
   extern __shared__ uint8_t smem_raw[];
   Cta<L> c;
@@ -133,7 +134,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
   const int n_tiles = a.tiles.m * a.tiles.n, blocks = (a.k + kBlock - 1) / kBlock;
   const bool wide = a.bn > 128;  // a tile takes both halves
   const uint32_t cta_bytes = L::kA + static_cast<uint32_t>(a.bn) * 64u;
-  int loads = 0;
+  const uint32_t scale_bytes = 512u * (1 + (a.bn + 127) / 128);
+  int loads = 0, loads2 = 0;
   if (c.warp == L::kProducer) {
     if (c.lane == 0) {
       const int most = loads_before_stop(a.guard.stop, c.rank);
@@ -144,59 +146,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
         a.tiles.at(t, &i, &j);
         const int y = i * 256 + 128 * static_cast<int>(c.rank), z = j * a.bn + a.bn / 2 * static_cast<int>(c.rank);
 #pragma unroll 1
-        for (int kb = 0; kb < blocks; ++kb) {
-          const int s = loads % L::kSlots, n = loads / L::kSlots;
-          if (loads == most || (n > 0 && !c.wait(L::kEmpty + s, n - 1, 101))) {
-            ok = false;
-            break;
+        for (int kb = 0; ok && kb < blocks; ++kb) {
+          if ((kb & 3) == 0) {
+            const int s = loads2 % L::kSlots2, n = loads2 / L::kSlots2;
+            ok = n == 0 || c.wait(L::kEmpty2 + s, n - 1, 102);
+            if (!ok) break;
+            const uint32_t at = c.base + L::kScales + static_cast<uint32_t>(s) * L::kScaleSlot, full = c.lbar(L::kFull2 + s);
+            const int g = kb >> 2, chunk = j * a.bn / kBlock;
+            if (c.leader) mbar_arrive_expect_tx(c.bar(L::kFull2 + s), 2 * scale_bytes);
+            tma_load_2d_pair(at, &maps.x_tiles, full, 0, g * a.x_chunks + y / 128);
+            tma_load_2d_pair(at + 512, &maps.w_tiles, full, 0, g * a.w_chunks + chunk);
+            if (wide) tma_load_2d_pair(at + 1024, &maps.w_tiles, full, 0, g * a.w_chunks + chunk + 1);
+            ++loads2;
           }
+          const int s = loads % L::kSlots, n = loads / L::kSlots;
+          ok = loads != most && (n == 0 || c.wait(L::kEmpty + s, n - 1, 101));
+          if (!ok) break;
           const uint32_t at = c.base + static_cast<uint32_t>(s) * L::kSlot, full = c.lbar(L::kFull + s);
           if (c.leader) mbar_arrive_expect_tx(c.bar(L::kFull + s), 2 * cta_bytes);
-          tma_load_2d_pair(at, &x_map, full, kb * kBlock, y);
-          tma_load_2d_pair(at + L::kA, &w_map, full, kb * kBlock, z);
+          tma_load_2d_pair(at, &maps.x, full, kb * kBlock, y);
+          tma_load_2d_pair(at + L::kA, &maps.w, full, kb * kBlock, z);
           ++loads;
         }
       }
     }
     __syncwarp();
-  } else if (c.warp == L::kScaler) {
-    int n = 0;
-    bool ok = true;
-    const int groups = (blocks + 3) / 4;
-#pragma unroll 1
-    for (int t = cluster; ok && t < n_tiles; t += n_clusters) {
-      int i, j;
-      a.tiles.at(t, &i, &j);
-      const int64_t row0 = static_cast<int64_t>(i) * 256 + 128 * c.rank + c.lane;
-      const int wr0 = j * a.bn;
-#pragma unroll 1
-      for (int g = 0; g < groups; ++g, ++n) {
-        const int s = n % L::kScaleSlots;
-        uint32_t w[12];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int64_t row = row0 + 32 * q;
-          w[q] = row < a.o.rows ? *reinterpret_cast<const uint32_t*>(a.x_scales + row * a.x_pitch + 4 * g) : 0x7F7F7F7Fu;
-        }
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          const int row = (wr0 + 32 * q) / kBlock;
-          w[4 + q] = 32 * q < a.bn && row < a.w_rows ? *reinterpret_cast<const uint32_t*>(a.w_scales + static_cast<int64_t>(row) * a.w_pitch + 4 * g) : 0x7F7F7F7Fu;
-        }
-        if (n >= L::kScaleSlots && !c.wait_all(L::kScEmpty + s, n / L::kScaleSlots - 1, 102)) {
-          ok = false;
-          break;
-        }
-        const uint32_t at = c.base + L::kScales + static_cast<uint32_t>(s) * L::kScaleSlot + 16u * c.lane;
-        st_shared_v4(at, make_uint4(w[0], w[1], w[2], w[3]));
-        st_shared_v4(at + 512, make_uint4(w[4], w[5], w[6], w[7]));
-        st_shared_v4(at + 1024, make_uint4(w[8], w[9], w[10], w[11]));
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (c.lane == 0) mbar_arrive_release_cluster(c.lbar(L::kScFull + s));
-        __syncwarp();
-      }
-    }
   } else if (c.warp == L::kMma) {
     if (c.leader) {
       const uint64_t ad = sdesc_sw128(c.base, 16, 1024), bd = sdesc_sw128(c.base + L::kA, 16, 1024);
@@ -207,6 +181,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
 #pragma unroll 1
       for (int t = cluster; ok && t < n_tiles; t += n_clusters, ++used) {
         const uint32_t d = c.tmem + (wide ? 0u : 128u * (used & 1));
+        int ti, tj;
+        a.tiles.at(t, &ti, &tj);
+        const uint32_t shift = static_cast<uint32_t>(tj * a.bn % kBlock) / 32u;  // the tile may begin in the middle of a chunk
         // the half's (both halves') earlier sums are in registers
         const int before = wide ? used : used >> 1;
         if (before > 0 && !(wide ? c.wait_all(L::kAccEmpty, before - 1, 103) && c.wait_all(L::kAccEmpty + 1, before - 1, 103)
@@ -214,11 +191,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
           break;
 #pragma unroll 1
         for (int kb = 0; kb < blocks; ++kb, ++load) {
-          const int s = load % L::kSlots, sc = group % L::kScaleSlots;
+          const int s = load % L::kSlots, sc = group % L::kSlots2;
           const uint32_t sfa = c.tmem + L::kTmemScales + 16u * sc, sfb = sfa + 4;
           if ((kb & 3) == 0) {
-            ok = c.wait_all(L::kScFull + sc, group / L::kScaleSlots, 104) &&
-                 __all_sync(0xffffffffu, mbar_try_wait_acquire_cluster(c.bar(L::kScFull + sc), static_cast<uint32_t>(group / L::kScaleSlots) & 1u));
+            ok = c.wait_all(L::kFull2 + sc, group / L::kSlots2, 104);
             if (!ok) break;
           }
           ok = c.wait_all(L::kFull + s, load / L::kSlots, 105);
@@ -232,15 +208,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
               const uint64_t at = sd + static_cast<uint64_t>(sc) * (L::kScaleSlot >> 4);
               copy_scales_pair(sfa, at);
               copy_scales_pair(sfb, at + (512 >> 4));
-              copy_scales_pair(sfb + 4, at + (1024 >> 4));
+              if (wide) copy_scales_pair(sfb + 4, at + (1024 >> 4));
             }
             const uint64_t off = static_cast<uint64_t>(s) * (L::kSlot >> 4);
             const uint32_t id = idesc_byte(idesc, kb & 3);
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-              if (q < steps) mx_mma_pair(d, ad + off + 2 * q, bd + off + 2 * q, id, sfa, sfb, kb > 0 || q > 0 ? 1u : 0u);
+              if (q < steps) mx_mma_pair(d, ad + off + 2 * q, bd + off + 2 * q, id, sfa, sfb + shift, kb > 0 || q > 0 ? 1u : 0u);
             tc2_commit_mc(c.bar(L::kEmpty + s), 3);
-            if ((kb & 3) == 3 || last) tc2_commit_mc(c.bar(L::kScEmpty + sc), 3);
+            if ((kb & 3) == 3 || last) tc2_commit_mc(c.bar(L::kEmpty2 + sc), 3);
             if (last) {
               if (wide || !(used & 1)) tc2_commit_mc(c.bar(L::kAccFull), 3);
               if (wide || (used & 1)) tc2_commit_mc(c.bar(L::kAccFull + 1), 3);
@@ -281,7 +257,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
       if (in) finish_block<kEpi>(a.o, row, col0, cols, v, u);
     }
   }
-  c.leave(loads, cta_bytes);
+  c.leave(loads, cta_bytes, loads2, scale_bytes);
 }
 
 }  // namespace f8

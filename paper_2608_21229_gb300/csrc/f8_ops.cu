@@ -52,15 +52,21 @@ int check_rows(const refcache_f8_rows_t* r, int64_t rows, int width, const char*
   if (width && r->width != width) return fail(REFCACHE_ERR_INVALID_ARG, "%s: width %d, expected %d", name, r->width, width);
   if (rows >= 0 && r->rows != rows)
     return fail(REFCACHE_ERR_INVALID_ARG, "%s: %lld rows, expected %lld", name, static_cast<long long>(r->rows), static_cast<long long>(rows));
-  if (r->rows > 0 && ((rc = check_tensor(r->codes, name)) != 0 || (rc = check_tensor(r->scales, name)) != 0)) return rc;
+  if (r->rows > 0 && ((rc = check_tensor(r->codes, name)) != 0 || (rc = check_tensor(r->scales, name)) != 0 ||
+                      (rc = check_tensor(r->tiles, name)) != 0))
+    return rc;
   return REFCACHE_OK;
 }
 int check_weight(const refcache_f8_weight_t* w, bool plain, bool transposed) {
   if (!w) return fail(REFCACHE_ERR_INVALID_ARG, "weight is NULL");
   int rc;
   if ((rc = check_width(w->out_width, "weight")) != 0 || (rc = check_width(w->in_width, "weight")) != 0) return rc;
-  if (plain && ((rc = check_tensor(w->codes, "weight codes")) != 0 || (rc = check_tensor(w->scales, "weight scales")) != 0)) return rc;
-  if (transposed && ((rc = check_tensor(w->codes_t, "weight codes_t")) != 0 || (rc = check_tensor(w->scales_t, "weight scales_t")) != 0)) return rc;
+  if (plain && ((rc = check_tensor(w->codes, "weight codes")) != 0 || (rc = check_tensor(w->scales, "weight scales")) != 0 ||
+                (rc = check_tensor(w->tiles, "weight tiles")) != 0))
+    return rc;
+  if (transposed && ((rc = check_tensor(w->codes_t, "weight codes_t")) != 0 || (rc = check_tensor(w->scales_t, "weight scales_t")) != 0 ||
+                     (rc = check_tensor(w->tiles_t, "weight tiles_t")) != 0))
+    return rc;
   return REFCACHE_OK;
 }
 int check_bias(const void* bias, int f32) {
@@ -68,14 +74,14 @@ int check_bias(const void* bias, int f32) {
   return REFCACHE_OK;
 }
 
-rc::f8::Rows rows_of(const refcache_f8_rows_t* r) {
-  if (!r) return {};
-  return {static_cast<uint8_t*>(r->codes), static_cast<uint8_t*>(r->scales), r->rows, r->width, REFCACHE_F8_PITCH(r->width)};
+rc::f8::Rows rows_of(void* codes, void* scales, void* tiles, int64_t rows, int width) {
+  return {static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales), static_cast<uint8_t*>(tiles), rows, width, REFCACHE_F8_PITCH(width),
+          static_cast<int32_t>(ceil_div(rows, 128))};
 }
+rc::f8::Rows rows_of(const refcache_f8_rows_t* r) { return r ? rows_of(r->codes, r->scales, r->tiles, r->rows, r->width) : rc::f8::Rows{}; }
 rc::f8::Rows rows_of(const refcache_f8_weight_t* w, bool transposed) {
-  if (transposed)
-    return {static_cast<uint8_t*>(w->codes_t), static_cast<uint8_t*>(w->scales_t), w->in_width, w->out_width, REFCACHE_F8_PITCH(w->out_width)};
-  return {static_cast<uint8_t*>(w->codes), static_cast<uint8_t*>(w->scales), w->out_width, w->in_width, REFCACHE_F8_PITCH(w->in_width)};
+  return transposed ? rows_of(w->codes_t, w->scales_t, w->tiles_t, w->in_width, w->out_width)
+                    : rows_of(w->codes, w->scales, w->tiles, w->out_width, w->in_width);
 }
 
 // CTA pairs of a kernel that run at once on the current device; sets its attributes on first use.
@@ -111,6 +117,10 @@ int tile_columns(int64_t rows, int width, int blocks, int pairs, int step) {
   return best;
 }
 
+int tiles_map(CUtensorMap* m, const rc::f8::Rows& r) {
+  return rc_host::encode_lines(m, r.tiles, static_cast<int64_t>(r.pitch / 4) * r.chunks);
+}
+
 template <int kEpi>
 int launch_linear(const rc::f8::Rows& x, const rc::f8::Rows& w, const rc::f8::Out& o, void* stream) {
   using L = rc::f8::LinearSmem;
@@ -124,22 +134,22 @@ int launch_linear(const rc::f8::Rows& x, const rc::f8::Rows& w, const rc::f8::Ou
     return rc;
   const int blocks = static_cast<int>(ceil_div(x.width, 128));
   a.o = o;
-  a.x_scales = x.scales, a.x_pitch = x.pitch, a.w_scales = w.scales, a.w_pitch = w.pitch;
-  a.w_rows = static_cast<int>(ceil_div(w.rows, 128));
+  a.x_chunks = x.chunks, a.w_chunks = w.chunks;
   a.k = x.width;
-  a.bn = tile_columns(o.rows, o.width, blocks, pairs, kEpi == rc::f8::kStore ? 32 : 128);
+  a.bn = tile_columns(o.rows, o.width, blocks, pairs, kEpi == rc::f8::kStore ? 64 : 128);
   const int64_t tiles_m = ceil_div(o.rows, 256), tiles_n = ceil_div(o.width, a.bn);
   if (tiles_m * tiles_n > (1ll << 30)) return fail(REFCACHE_ERR_INVALID_ARG, "too many rows for a width of %d", o.width);
   a.tiles = {static_cast<int32_t>(tiles_m), static_cast<int32_t>(tiles_n)};
   a.guard.timeout_ns = rc_host::wait_timeout_ns();
-  CUtensorMap xm, wm;
-  if ((rc = rc_host::encode_map(&xm, x.codes, 1, x.width, x.rows, x.width, 128)) != 0 ||
-      (rc = rc_host::encode_map(&wm, w.codes, 1, w.width, w.rows, w.width, static_cast<uint32_t>(a.bn / 2))) != 0)
+  rc::f8::LinearMaps maps;
+  if ((rc = rc_host::encode_map(&maps.x, x.codes, x.width, x.rows, x.width, 128)) != 0 ||
+      (rc = rc_host::encode_map(&maps.w, w.codes, w.width, w.rows, w.width, static_cast<uint32_t>(a.bn / 2))) != 0 ||
+      (rc = tiles_map(&maps.x_tiles, x)) != 0 || (rc = tiles_map(&maps.w_tiles, w)) != 0)
     return rc;
   a.guard.stop = rc_host::take_debug_stop();
   const unsigned clusters = static_cast<unsigned>(std::min<int64_t>(tiles_m * tiles_n, pairs));
   const cudaError_t e = launch_dependent(rc::f8::f8_linear_kernel<kEpi>, dim3(2 * clusters), dim3(L::kThreads), L::kDynamic,
-                                         static_cast<cudaStream_t>(stream), xm, wm, a);
+                                         static_cast<cudaStream_t>(stream), maps, a);
   return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "f8_linear_kernel launch");
 }
 
@@ -162,7 +172,7 @@ int refcache_f8_quantize(const void* x, int64_t ld, const refcache_f8_rows_t* ou
 }
 
 int refcache_f8_quantize_weight(const void* w, int w_f32, const refcache_f8_weight_t* out, void* stream) {
-  const bool both = out && (out->codes_t || out->scales_t);
+  const bool both = out && (out->codes_t || out->scales_t || out->tiles_t);
   int rc = check_weight(out, true, both);
   if (rc || (rc = check_tensor(w, "w")) != 0) return rc;
   int sms = 0;

@@ -67,8 +67,8 @@ __device__ __forceinline__ void mx_mma_pair(uint32_t d, uint64_t a, uint64_t b, 
       "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(acc)
       : "memory");
 }
-// 128 rows' scale words from shared memory (row r at 16 (r % 32) + 4 (r / 32)) into four
-// columns of tensor memory (row r in lane r % 32 of each 32, column r / 32).
+// 128 rows' scale words (Rows::tiles) from shared memory into four columns of tensor memory:
+// row r into lane r % 32 of each 32 lanes, column r / 32.
 __device__ __forceinline__ uint64_t scales_desc(uint32_t addr) {  // no swizzle, 8 rows of 16 bytes each 128 bytes
   return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(128 >> 4) << 32) | (1ull << 46);
 }
@@ -78,8 +78,8 @@ __device__ __forceinline__ void copy_scales_pair(uint32_t tmem, uint64_t desc) {
 
 // ---------------------------------------------------------------- a CTA of a pair
 // L: kNumBars, kBars, kAux (abort flag, tensor memory's address, the other CTA's abort
-// flag, both CTAs' loads), kUsed, kDynamic, arrivals(barrier), kFull, kSlots, kDone, and
-// the warps kProducer and kMma.
+// flag, both CTAs' loads of each ring), kUsed, kDynamic, arrivals(barrier), kDone, the warps
+// kProducer and kMma, and two rings of loads: their first barriers kFull and kFull2, kSlots and kSlots2.
 template <typename L>
 struct Cta {
   uint32_t base, rank;
@@ -143,12 +143,15 @@ struct Cta {
     __syncwarp();
   }
 
-  // `loads`: issued by this CTA's producer (its lane 0).  When neither CTA gave up, every load
-  // was waited for by the MMAs that read it; else the leader, on whose barriers both CTAs'
-  // loads complete, arms or counts what one half lacks of the other and waits for the
-  // last phase of each.
-  __device__ __forceinline__ void leave(int loads, uint32_t cta_bytes) const {
-    if (warp == L::kProducer && lane == 0) st_cluster_u32(mapa_shared(base + L::kAux + 12 + 4 * rank, 0), static_cast<uint32_t>(loads));
+  // Loads that this CTA's producer issued (its lane 0) and a load's bytes of one CTA, by ring.  When
+  // neither CTA gave up, every load was waited for by the MMAs that read it; else the leader, on
+  // whose barriers both CTAs' loads complete, arms or counts what one half lacks of the
+  // other and waits for the last phase of each.
+  __device__ __forceinline__ void leave(int loads, uint32_t bytes, int loads2, uint32_t bytes2) const {
+    if (warp == L::kProducer && lane == 0) {
+      st_cluster_u32(mapa_shared(base + L::kAux + 12 + 8 * rank, 0), static_cast<uint32_t>(loads));
+      st_cluster_u32(mapa_shared(base + L::kAux + 16 + 8 * rank, 0), static_cast<uint32_t>(loads2));
+    }
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0) st_cluster_u32(mapa_shared(base + L::kAux + 8, rank ^ 1u), static_cast<uint32_t>(*ctl.abort_flag));
@@ -160,19 +163,23 @@ struct Cta {
     const volatile int* aux = reinterpret_cast<const volatile int*>(ptr + L::kAux);
     if (aux[0] == 0 && aux[2] == 0) return;
     if (leader && warp == L::kProducer && lane == 0) {
+      auto settle = [&](int full, int slots, int mine, int theirs, uint32_t cta_bytes) {
 #pragma unroll 1
-      for (int slot = 0; slot < L::kSlots; ++slot) {
-        auto count = [&](int total) { return (total - slot + L::kSlots - 1) / L::kSlots; };
-        int m = count(aux[3]);
-        const int theirs = count(aux[4]);
-        if (theirs == m + 1) {
-          mbar_arrive_expect_tx(bar(L::kFull + slot), cta_bytes);
-          m = theirs;
-        } else if (m == theirs + 1) {
-          mbar_complete_tx(bar(L::kFull + slot), cta_bytes);
+        for (int slot = 0; slot < slots; ++slot) {
+          auto count = [&](int total) { return (total - slot + slots - 1) / slots; };
+          int m = count(mine);
+          const int t = count(theirs);
+          if (t == m + 1) {
+            mbar_arrive_expect_tx(bar(full + slot), cta_bytes);
+            m = t;
+          } else if (m == t + 1) {
+            mbar_complete_tx(bar(full + slot), cta_bytes);
+          }
+          if (m > 0) drain(bar(full + slot), static_cast<uint32_t>(m - 1) & 1u, ctl.timeout_ns);
         }
-        if (m > 0) drain(bar(L::kFull + slot), static_cast<uint32_t>(m - 1) & 1u, ctl.timeout_ns);
-      }
+      };
+      settle(L::kFull, L::kSlots, aux[3], aux[5], bytes);
+      settle(L::kFull2, L::kSlots2, aux[4], aux[6], bytes2);
     }
     cluster_sync();
   }

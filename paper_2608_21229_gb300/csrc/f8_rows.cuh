@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(kRowsThreads) f8_quantize_kernel(const uint16_
     if (!in) continue;
     *reinterpret_cast<uint2*>(out.codes + row * out.width + col) =
         make_uint2(pack_e4m3x4(v.v[0] * s, v.v[1] * s, v.v[2] * s, v.v[3] * s), pack_e4m3x4(v.v[4] * s, v.v[5] * s, v.v[6] * s, v.v[7] * s));
-    if ((lane & 15) == 0) out.scales[row * out.pitch + col / kBlock] = static_cast<uint8_t>(b);
+    if ((lane & 15) == 0) put_scale(out, row, col / kBlock, b);
   }
 }
 
@@ -101,6 +101,10 @@ __global__ void __launch_bounds__(256) f8_quantize_weight_kernel(const void* w, 
   if (threadIdx.x == 0) {
     out.scales[static_cast<int64_t>(blockIdx.y) * out.pitch + blockIdx.x] = static_cast<uint8_t>(b);
     if (out_t.codes) out_t.scales[static_cast<int64_t>(blockIdx.x) * out_t.pitch + blockIdx.y] = static_cast<uint8_t>(b);
+  }
+  if (threadIdx.x < 128) {  // (tiles have room for whole blocks of rows)
+    *tile_byte(out, static_cast<int64_t>(r0) + threadIdx.x, blockIdx.x) = static_cast<uint8_t>(b);
+    if (out_t.codes) *tile_byte(out_t, static_cast<int64_t>(c0) + threadIdx.x, blockIdx.y) = static_cast<uint8_t>(b);
   }
 }
 

@@ -24,9 +24,10 @@ int device_status_word(int* dev, int** word);
 uint64_t wait_timeout_ns();
 int take_debug_stop();
 
-// A 2-D tensor map with the 128-byte swizzle: `outer` rows of `inner` elements (1 byte, or 2:
-// bf16), `pitch` bytes apart; boxes of 128 bytes x box_outer rows.
-int encode_map(CUtensorMap* m, const void* base, int elem_bytes, int64_t inner, int64_t outer, int64_t pitch, uint32_t box_outer);
+// 2-D tensor maps.  `outer` rows of `inner` bytes, `pitch` bytes apart: boxes of 128 bytes x box_outer
+// rows with the 128-byte swizzle; `lines` lines of 512 bytes, one line a box.
+int encode_map(CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t pitch, uint32_t box_outer);
+int encode_lines(CUtensorMap* m, const void* base, int64_t lines);
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

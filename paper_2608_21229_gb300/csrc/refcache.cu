@@ -201,18 +201,26 @@ int device_status_word(int* dev, int** word) {
 uint64_t wait_timeout_ns() { return g_timeout_ns.load(); }
 int take_debug_stop() { return g_dbg_skip.exchange(0); }
 
-int encode_map(CUtensorMap* m, const void* base, int elem_bytes, int64_t inner, int64_t outer, int64_t pitch, uint32_t box_outer) {
+static int encode_2d(CUtensorMap* m, CUtensorMapDataType type, const void* base, int64_t inner, int64_t outer, int64_t pitch, uint32_t box_inner,
+                     uint32_t box_outer, CUtensorMapSwizzle swizzle) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return fail(REFCACHE_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable");
   const cuuint64_t dims[2] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(std::max<int64_t>(outer, 1))};
   const cuuint64_t strides[1] = {static_cast<cuuint64_t>(pitch)};
-  const cuuint32_t box[2] = {128u / static_cast<cuuint32_t>(elem_bytes), box_outer};
+  const cuuint32_t box[2] = {box_inner, box_outer};
   const cuuint32_t estr[2] = {1, 1};
-  const CUresult r = fn(m, elem_bytes == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims,
-                        strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const CUresult r = fn(m, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(REFCACHE_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
   return REFCACHE_OK;
+}
+
+int encode_map(CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t pitch, uint32_t box_outer) {
+  return encode_2d(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, inner, outer, pitch, 128, box_outer, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+int encode_lines(CUtensorMap* m, const void* base, int64_t lines) {
+  return encode_2d(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, base, 128, lines, 512, 128, 1, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 }  // namespace rc_host

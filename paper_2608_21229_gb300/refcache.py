@@ -82,12 +82,13 @@ class _GatedNorm(ctypes.Structure):
 
 
 class _F8Rows(ctypes.Structure):
-    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int32), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int32), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("tiles", ctypes.c_void_p)]
 
 
 class _F8Weight(ctypes.Structure):
     _fields_ = [("out_width", ctypes.c_int32), ("in_width", ctypes.c_int32), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
-                ("codes_t", ctypes.c_void_p), ("scales_t", ctypes.c_void_p)]
+                ("tiles", ctypes.c_void_p), ("codes_t", ctypes.c_void_p), ("scales_t", ctypes.c_void_p), ("tiles_t", ctypes.c_void_p)]
 
 
 _lib = None
@@ -822,10 +823,12 @@ def clip_gradients(grads, max_norm, out=None, norm=None, stream=None):
 
 
 # ---------------------------------------------------------------- linear layers in 8 bits
-def _f8_scales(rows, blocks, device):
-    """Memory for rows of scales, and its used part as torch's UE8M0."""
-    mem = _torch.empty((rows, (blocks + 3) // 4 * 4), dtype=_torch.uint8, device=device)
-    return mem, mem[:, :blocks].view(_torch.float8_e8m0fnu)
+def _f8_scales(rows, height, width, device):
+    """Memory for the scales of ``height`` rows (``rows`` of scales), their used part as torch's UE8M0, and memory for
+    them as the tensor cores take them."""
+    groups, blocks = (width + 511) // 512, (width + 127) // 128
+    mem = _torch.empty((rows, 4 * groups), dtype=_torch.uint8, device=device)
+    return mem, mem[:, :blocks].view(_torch.float8_e8m0fnu), _torch.empty((groups, (height + 127) // 128, 512), dtype=_torch.uint8, device=device)
 
 
 class F8Rows:
@@ -838,9 +841,9 @@ class F8Rows:
         device = _torch.device("cuda", _device()) if device is None else _torch.device(device)
         self.rows, self.width = int(rows), int(width)
         self.codes = _torch.empty((self.rows, self.width), dtype=_torch.float8_e4m3fn, device=device)
-        self._mem, self.scales = _f8_scales(self.rows, (self.width + 127) // 128, device)
+        self._mem, self.scales, self._tiles = _f8_scales(self.rows, self.rows, self.width, device)
         self.device = self.codes.get_device()
-        self.c = _F8Rows(self.rows, self.width, self.codes.data_ptr(), self._mem.data_ptr())
+        self.c = _F8Rows(self.rows, self.width, *(t.data_ptr() for t in (self.codes, self._mem, self._tiles)))
         self._ref = ctypes.byref(self.c)
 
 
@@ -855,10 +858,10 @@ class F8Weight:
         self.out_width, self.in_width = n, k = int(out_width), int(in_width)
         self.codes, self.codes_t = (_torch.empty(s, dtype=_torch.float8_e4m3fn, device=device) for s in ((n, k), (k, n)))
         nb, kb = (n + 127) // 128, (k + 127) // 128
-        self._mem, self.scales = _f8_scales(nb, kb, device)
-        self._mem_t, self.scales_t = _f8_scales(kb, nb, device)
+        self._mem, self.scales, self._tiles = _f8_scales(nb, n, k, device)
+        self._mem_t, self.scales_t, self._tiles_t = _f8_scales(kb, k, n, device)
         self.device = self.codes.get_device()
-        self.c = _F8Weight(n, k, *(t.data_ptr() for t in (self.codes, self._mem, self.codes_t, self._mem_t)))
+        self.c = _F8Weight(n, k, *(t.data_ptr() for t in (self.codes, self._mem, self._tiles, self.codes_t, self._mem_t, self._tiles_t)))
         self._ref = ctypes.byref(self.c)
 
 

@@ -15,16 +15,16 @@ def lib():
     return rcb.load()
 
 
-def rows(n=4, width=64, codes=P, scales=P):
-    return ctypes.byref(rcb._F8Rows(n, width, codes, scales))
+def rows(n=4, width=64, codes=P, scales=P, tiles=P):
+    return ctypes.byref(rcb._F8Rows(n, width, codes, scales, tiles))
 
 
-def weight(out=32, inn=64, codes=P, scales=P, codes_t=P, scales_t=P):
-    return ctypes.byref(rcb._F8Weight(out, inn, codes, scales, codes_t, scales_t))
+def weight(out=32, inn=64, codes=P, scales=P, tiles=P, codes_t=P, scales_t=P, tiles_t=P):
+    return ctypes.byref(rcb._F8Weight(out, inn, codes, scales, tiles, codes_t, scales_t, tiles_t))
 
 
 BAD_ROWS = [dict(n=-1), dict(n=(1 << 31) - 1), dict(width=0), dict(width=24), dict(width=(1 << 20) + 16), dict(codes=None), dict(scales=None),
-            dict(codes=P + 8), dict(scales=P + 4)]
+            dict(codes=P + 8), dict(scales=P + 4), dict(tiles=None), dict(tiles=P + 8)]
 BAD_WEIGHT = [dict(out=0), dict(out=40), dict(inn=-16), dict(inn=(1 << 20) + 16)]
 INVALID = rcb.ERR_INVALID_ARG
 
@@ -56,11 +56,11 @@ def test_weight_refusals(lib, kw):
 
 
 def test_missing_orientation_refusals(lib):
-    for kw in (dict(codes=None), dict(scales=None), dict(codes=P + 8), dict(scales=P + 8)):
+    for kw in (dict(codes=None), dict(scales=None), dict(tiles=None), dict(codes=P + 8), dict(scales=P + 8), dict(tiles=P + 8)):
         assert lib.refcache_f8_linear(rows(), weight(**kw), 0, None, 0, P, 64, None) == INVALID
         assert lib.refcache_f8_linear_gelu(rows(), weight(**kw), None, 0, 0, rows(width=32), None, None) == INVALID
         assert lib.refcache_f8_quantize_weight(P, 0, weight(**kw), None) == INVALID
-    for kw in (dict(codes_t=None), dict(scales_t=None), dict(codes_t=P + 8), dict(scales_t=P + 8)):
+    for kw in (dict(codes_t=None), dict(scales_t=None), dict(tiles_t=None), dict(codes_t=P + 8), dict(scales_t=P + 8), dict(tiles_t=P + 8)):
         assert lib.refcache_f8_linear(rows(width=32), weight(**kw), 1, None, 0, P, 64, None) == INVALID
         assert lib.refcache_f8_linear_gelu_backward(rows(width=32), weight(**kw), 0, rows(), P, 64, None, None) == INVALID
         assert lib.refcache_f8_quantize_weight(P, 0, weight(**kw), None) == INVALID
@@ -97,7 +97,7 @@ def test_tensor_refusals(lib):
 
 def test_calls_without_rows_need_no_tensors(lib):
     """Nothing to do: accepted before a device is asked for."""
-    empty = lambda w: rows(0, w, None, None)  # noqa: E731
+    empty = lambda w: rows(0, w, None, None, None)  # noqa: E731
     assert lib.refcache_f8_quantize(None, 64, empty(64), None) == rcb.OK
     assert lib.refcache_f8_linear(empty(64), weight(), 0, None, 0, None, 32, None) == rcb.OK
     assert lib.refcache_f8_linear_gelu(empty(64), weight(), None, 0, 0, empty(32), empty(32), None) == rcb.OK

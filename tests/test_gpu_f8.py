@@ -72,6 +72,16 @@ def near_form(f, want, delta):
     assert (off <= tol * (1 + 1e-12)).all(), float((off - tol).max())
 
 
+def check_tiles(f):
+    """The tensor cores' copies of the scales, as the header says where each lies."""
+    for tiles, scales, height, tall in ((f._tiles, f.scales, f.codes.shape[0], 128 if hasattr(f, "codes_t") else 1),) + (
+            ((f._tiles_t, f.scales_t, f.codes_t.shape[0], 128),) if hasattr(f, "codes_t") else ()):
+        b = scales.view(torch.uint8)
+        r, j = torch.arange(height, device="cuda")[:, None], torch.arange(b.shape[1], device="cuda")[None]
+        at = 512 * ((j // 4) * -(-height // 128) + r // 128) + 16 * (r % 32) + 4 * (r // 32 % 4) + j % 4
+        assert torch.equal(tiles.flatten()[at], b.repeat_interleave(tall, 0)[:height])
+
+
 # ---------------------------------------------------------------- the 8-bit form
 @pytest.mark.parametrize("r, c", [(1, 16), (1, 4096), (3, 128), (5, 144), (33, 272), (257, 1808), (2, 8208), (1000, 256)])
 def test_rows_bit_for_bit(r, c):
@@ -86,6 +96,7 @@ def test_rows_bit_for_bit(r, c):
         codes, b = ref.form(x)
         assert torch.equal(f.scales.view(torch.uint8).long(), b)
         assert torch.equal(f.codes.double(), codes)
+        check_tiles(f)
 
 
 def test_rows_at_the_borders_of_scales_and_codes():
@@ -134,12 +145,13 @@ def test_weight_bit_for_bit(n, k, dtype):
     codes, b = ref.form(w, 128)
     assert torch.equal(f.scales.view(torch.uint8).long(), b) and torch.equal(f.scales_t.view(torch.uint8).long(), b.t())
     assert torch.equal(f.codes.double(), codes) and torch.equal(f.codes_t.double(), codes.t())
+    check_tiles(f)
 
 
 def test_one_orientation_alone():
     w = randn(gen(9), 144, 272)
     f, both = rc.F8Weight(144, 272), rc.f8_quantize_weight(w)
-    f.c.codes_t = f.c.scales_t = None
+    f.c.codes_t = f.c.scales_t = f.c.tiles_t = None
     f.codes_t.view(torch.uint8).fill_(3)
     rc.f8_quantize_weight(w, f)
     assert torch.equal(f.codes.view(torch.uint8), both.codes.view(torch.uint8)) and (f.codes_t.view(torch.uint8) == 3).all()
@@ -195,6 +207,8 @@ def test_linear_gelu(r, n, k, form):
     near_form(u8, u, delta)
     # the derivative is at most 1.13; exp, divide and erfc are off by some units of fp32
     near_form(a, ref.gelu(u, form), 1.13 * delta + 2.0 ** -19 * ref.gelu(u, form).abs() + 2.0 ** -126)
+    check_tiles(u8)
+    check_tiles(a)
     only = rc.F8Rows(r, n)
     rc.f8_linear_gelu(x, w, only, bias=bias, form=form)
     assert torch.equal(only.codes.view(torch.uint8), a.codes.view(torch.uint8))
@@ -222,6 +236,7 @@ def test_linear_gelu_backward(r, n, k, form):
     off = (du.double() - want).abs()
     assert (off <= delta * (1 + 2.0 ** -8) + 2.0 ** -8 * want.abs() + 2.0 ** -133).all()
     near_form(du8, want, delta + 2.0 ** -140)
+    check_tiles(du8)
     alone, alone8 = torch.empty(r, k, dtype=BF16, device="cuda"), rc.F8Rows(r, k)
     rc.f8_linear_gelu_backward(dy, w, u8, alone, None, form=form)
     rc.f8_linear_gelu_backward(dy, w, u8, None, alone8, form=form)
