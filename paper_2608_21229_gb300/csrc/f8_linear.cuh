@@ -34,6 +34,7 @@ struct LinearMaps {
 
 struct LinearSmem {
   static constexpr int kSlots = 6, kSlots2 = 4;  // stages, scales
+  static constexpr bool kOwn2 = false;
   static constexpr uint32_t kA = 16384, kSlot = 2 * kA, kScaleSlot = 3 * 512;
   static constexpr uint32_t kScales = kSlots * kSlot, kBars = kScales + kSlots2 * kScaleSlot;
   static constexpr int kFull = 0, kEmpty = kFull + kSlots, kFull2 = kEmpty + kSlots, kEmpty2 = kFull2 + kSlots2, kAccFull = kEmpty2 + kSlots2,

@@ -1,5 +1,5 @@
 // f8_ops.cu -- the entry points of include/refcache.h for linear layers in 8 bits:
-// rows and weights into their 8-bit form (f8_rows.cuh), products on it (f8_linear.cuh).
+// rows and weights into their 8-bit form (f8_rows.cuh), products on it (f8_linear.cuh, f8_wgrad.cuh).
 // Argument checks and launches; no call allocates memory.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -11,7 +11,7 @@
 #include "refcache.h"
 #include "f8_linear.cuh"
 #include "f8_rows.cuh"
-#include "f8_simple.cuh"
+#include "f8_wgrad.cuh"
 #include "host_common.h"
 
 using rc_host::aligned16;
@@ -153,6 +153,38 @@ int launch_linear(const rc::f8::Rows& x, const rc::f8::Rows& w, const rc::f8::Ou
   return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "f8_linear_kernel launch");
 }
 
+// How a weight gradient is taken apart.
+struct WgradPlan {
+  int bn, stages, splits, per_split;
+  int64_t tiles_m, tiles_n;
+};
+// The plan is for the 76 CTA pairs of a GB300, whatever the device has to spare, so that a workspace's size
+// does not depend on it.  Cycles by rounds of items over the pairs: a stage of 64 rows takes 2 bn of
+// MMAs, or what its conversion lets through (400); parts have to be written and read again, at about 3.5
+// KB a cycle, by a second kernel (5000).
+WgradPlan plan_wgrad(int64_t rows, int n, int k) {
+  constexpr int kPairs = 76;
+  WgradPlan best{};
+  int64_t least = -1;
+  for (int bn = k > 128 ? 256 : 128; bn >= 128; bn -= 128) {
+    WgradPlan p{};
+    p.bn = bn;
+    p.stages = static_cast<int>((rows + 63) / 64);
+    p.tiles_m = ceil_div(n, 256), p.tiles_n = ceil_div(k, bn);
+    const int64_t tiles = p.tiles_m * p.tiles_n;
+    for (int s = 1; s <= 32; ++s) {
+      if (s > 1 && (s > p.stages || s * tiles > kPairs)) break;
+      p.per_split = static_cast<int>(ceil_div(p.stages, s));
+      p.splits = p.per_split ? static_cast<int>(ceil_div(p.stages, p.per_split)) : 1;
+      const int64_t rounds = (p.splits * tiles + kPairs - 1) / kPairs;
+      const int64_t cost = rounds * (static_cast<int64_t>(p.per_split) * std::max(2 * bn, 400) + 1500) +
+                           (p.splits > 1 ? 5000 + (p.splits + 1ll) * n * k * 4 / 3500 : 0);
+      if (least < 0 || cost < least) least = cost, best = p;
+    }
+  }
+  return best;
+}
+
 }  // namespace
 
 extern "C" {
@@ -229,22 +261,62 @@ int refcache_f8_linear_gelu_backward(const refcache_f8_rows_t* dy, const refcach
                                    : launch_linear<rc::f8::kGeluGrad + 1>(rows_of(dy), rows_of(w, true), o, stream);
 }
 
-size_t refcache_f8_weight_grad_bytes(int64_t, int, int) { return 0; }
+size_t refcache_f8_weight_grad_bytes(int64_t rows, int out_width, int in_width) {
+  if (rows <= 0 || rows > kMaxRows || check_width(out_width, "dw") != 0 || check_width(in_width, "dw") != 0) return 0;
+  const WgradPlan p = plan_wgrad(rows, out_width, in_width);
+  return p.splits > 1 ? static_cast<size_t>(p.splits) * out_width * in_width * sizeof(float) : 0;
+}
 
 int refcache_f8_weight_grad(const void* dy, int64_t ld_dy, const refcache_f8_rows_t* x, int out_width, const void* add, void* dw, int dw_f32,
                             float* d_bias, void* work, void* stream) {
+  using L = rc::f8::WgradSmem;
   int rc = check_rows(x, -1, 0, "x");
   if (rc || (rc = check_width(out_width, "dy")) != 0 || (rc = check_ld(ld_dy, out_width, "dy")) != 0 || (rc = check_tensor(dw, "dw")) != 0 ||
       (add && (rc = check_tensor(add, "add")) != 0) || (x->rows > 0 && (rc = check_tensor(dy, "dy")) != 0))
     return rc;
   if (reinterpret_cast<uintptr_t>(d_bias) & 3u) return fail(REFCACHE_ERR_INVALID_ARG, "d_bias is not 4-byte aligned");
-  if (refcache_f8_weight_grad_bytes(x->rows, out_width, x->width) && (rc = check_tensor(work, "work")) != 0) return rc;
-  int sms = 0;
-  if ((rc = device_sms(&sms)) != 0) return rc;
-  const rc::f8::WgradArgs a{static_cast<const uint16_t*>(dy), ld_dy, rows_of(x), out_width, add, dw, dw_f32, d_bias};
-  const cudaError_t e = launch_dependent(rc::f8::f8_wgrad_simple_kernel, dim3(ceil_div(x->width, 128), ceil_div(out_width, 32)), dim3(256), 0,
-                                         static_cast<cudaStream_t>(stream), a);
-  return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "f8_weight_grad launch");
+  const int n = out_width, k = x->width;
+  const WgradPlan p = plan_wgrad(x->rows, n, k);
+  if (p.splits > 1 && (rc = check_tensor(work, "work")) != 0) return rc;
+  if (p.tiles_m * p.tiles_n > (1ll << 30)) return fail(REFCACHE_ERR_INVALID_ARG, "a gradient of %d x %d is too large", n, k);
+  static std::atomic<int> kept[rc_host::kMaxDevices];
+  rc::f8::WgradArgs a{};
+  int sms = 0, dev = 0, pairs = 0;
+  if ((rc = device_sms(&sms)) != 0 || (rc = rc_host::device_status_word(&dev, &a.guard.status)) != 0 ||
+      (rc = pairs_of(rc::f8::f8_wgrad_kernel, kept[dev], L::kThreads, L::kDynamic, sms, &pairs)) != 0)
+    return rc;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaSuccess;
+  if (x->rows > 0) {
+    const rc::f8::Rows r = rows_of(x);
+    a.add = add, a.dw = p.splits > 1 ? work : dw, a.f32 = p.splits > 1 || dw_f32;
+    a.n = n, a.k = k, a.bn = p.bn;
+    a.rows = r.rows, a.chunks = r.chunks;
+    a.stages = p.stages, a.splits = p.splits, a.per_split = p.per_split;
+    a.tiles = {static_cast<int32_t>(p.tiles_m), static_cast<int32_t>(p.tiles_n)};
+    a.guard.timeout_ns = rc_host::wait_timeout_ns();
+    rc::f8::WgradMaps maps;
+    if ((rc = rc_host::encode_map(&maps.dy, dy, 2 * static_cast<int64_t>(n), r.rows, 2 * ld_dy, 64)) != 0 ||
+        (rc = rc_host::encode_plain(&maps.codes, r.codes, k, r.rows, k, static_cast<uint32_t>(p.bn / 2), 64)) != 0 || (rc = tiles_map(&maps.tiles, r)) != 0)
+      return rc;
+    a.guard.stop = rc_host::take_debug_stop();
+    const unsigned clusters = static_cast<unsigned>(std::min<int64_t>(p.tiles_m * p.tiles_n * p.splits, pairs));
+    e = launch_dependent(rc::f8::f8_wgrad_kernel, dim3(2 * clusters), dim3(L::kThreads), L::kDynamic, s, maps, a);
+    if (e != cudaSuccess) return cuda_fail(e, "f8_wgrad_kernel launch");
+  }
+  if (x->rows == 0 || p.splits > 1) {
+    const int64_t count = static_cast<int64_t>(n) * k;
+    const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(ceil_div(count, 2048), 8ll * sms));
+    e = launch_dependent(rc::f8::f8_wgrad_sum_kernel, dim3(blocks), dim3(256), 0, s, static_cast<const float*>(work), x->rows == 0 ? 0 : p.splits,
+                         count, add, dw, dw_f32);
+    if (e != cudaSuccess) return cuda_fail(e, "f8_wgrad_sum_kernel launch");
+  }
+  if (d_bias) {
+    e = launch_dependent(rc::f8::f8_bias_grad_kernel, dim3(ceil_div(n, 64), rc::f8::kBiasSplit), dim3(256), 0, s, static_cast<const uint16_t*>(dy), ld_dy,
+                         x->rows, n, d_bias);
+    if (e != cudaSuccess) return cuda_fail(e, "f8_bias_grad_kernel launch");
+  }
+  return REFCACHE_OK;
 }
 
 }  // extern "C"

@@ -79,7 +79,8 @@ __device__ __forceinline__ void copy_scales_pair(uint32_t tmem, uint64_t desc) {
 // ---------------------------------------------------------------- a CTA of a pair
 // L: kNumBars, kBars, kAux (abort flag, tensor memory's address, the other CTA's abort
 // flag, both CTAs' loads of each ring), kUsed, kDynamic, arrivals(barrier), kDone, the warps
-// kProducer and kMma, and two rings of loads: their first barriers kFull and kFull2, kSlots and kSlots2.
+// kProducer and kMma, and two rings of loads: their first barriers kFull and kFull2, kSlots and kSlots2;
+// kOwn2: loads of the second complete on the CTA's own barriers.
 template <typename L>
 struct Cta {
   uint32_t base, rank;
@@ -144,9 +145,9 @@ struct Cta {
   }
 
   // Loads that this CTA's producer issued (its lane 0) and a load's bytes of one CTA, by ring.  When
-  // neither CTA gave up, every load was waited for by the MMAs that read it; else the leader, on
+  // neither CTA gave up, every load was waited for by what read it; else the leader, on
   // whose barriers both CTAs' loads complete, arms or counts what one half lacks of the
-  // other and waits for the last phase of each.
+  // other and waits for the last phase of each (a CTA's own ring needs the wait alone).
   __device__ __forceinline__ void leave(int loads, uint32_t bytes, int loads2, uint32_t bytes2) const {
     if (warp == L::kProducer && lane == 0) {
       st_cluster_u32(mapa_shared(base + L::kAux + 12 + 8 * rank, 0), static_cast<uint32_t>(loads));
@@ -162,7 +163,7 @@ struct Cta {
     }
     const volatile int* aux = reinterpret_cast<const volatile int*>(ptr + L::kAux);
     if (aux[0] == 0 && aux[2] == 0) return;
-    if (leader && warp == L::kProducer && lane == 0) {
+    if (warp == L::kProducer && lane == 0) {
       auto settle = [&](int full, int slots, int mine, int theirs, uint32_t cta_bytes) {
 #pragma unroll 1
         for (int slot = 0; slot < slots; ++slot) {
@@ -178,8 +179,11 @@ struct Cta {
           if (m > 0) drain(bar(full + slot), static_cast<uint32_t>(m - 1) & 1u, ctl.timeout_ns);
         }
       };
-      settle(L::kFull, L::kSlots, aux[3], aux[5], bytes);
-      settle(L::kFull2, L::kSlots2, aux[4], aux[6], bytes2);
+      if (leader) settle(L::kFull, L::kSlots, aux[3], aux[5], bytes);
+      if (L::kOwn2)
+        settle(L::kFull2, L::kSlots2, loads2, loads2, bytes2);
+      else if (leader)
+        settle(L::kFull2, L::kSlots2, aux[4], aux[6], bytes2);
     }
     cluster_sync();
   }
