@@ -40,24 +40,11 @@ struct LinearSmem {
   static constexpr int kFull = 0, kEmpty = kFull + kSlots, kFull2 = kEmpty + kSlots, kEmpty2 = kFull2 + kSlots2, kAccFull = kEmpty2 + kSlots2,
                        kAccEmpty = kAccFull + 2, kDone = kAccEmpty + 2, kNumBars = kDone + 1;
   static constexpr uint32_t kAux = kBars + 8 * kNumBars, kUsed = kAux + 28, kDynamic = kUsed + 1024;
-  static constexpr int kProducer = 8, kMma = 9, kThreads = 32 * 10;  // warps 0-7: sums
+  static constexpr int kProducer = 8, kProducer2 = kProducer, kMma = 9, kThreads = 32 * 10;  // warps 0-7: sums
   static constexpr uint32_t kTmemScales = 256;                       // 16 columns a slot: four of x's words, eight of w's
   static_assert(kDynamic <= kMaxDynamic, "shared-memory layout too large");
   __device__ static constexpr uint32_t arrivals(int i) { return i >= kAccEmpty && i < kDone ? 8 : 1; }  // four warps of each CTA
 };
-
-// 128 columns of this thread's lane; those from `cols` on are not there.
-__device__ __forceinline__ void load_sums(uint32_t t, int cols, float (&v)[128]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (32 * i >= cols) break;
-    uint32_t r[32];
-    tmem_ld32(t + 32 * i, r);
-    tmem_wait_ld(r);
-#pragma unroll
-    for (int j = 0; j < 32; ++j) v[32 * i + j] = __uint_as_float(r[j]);
-  }
-}
 
 // One row's block of 128 columns in a thread, `cols` of them there (a multiple of 16).
 __device__ __forceinline__ void quantize_row(const Rows& r, int64_t row, int col0, int cols, const float (&v)[128]) {

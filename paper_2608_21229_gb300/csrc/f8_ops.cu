@@ -160,24 +160,24 @@ struct WgradPlan {
 };
 // The plan is for the 76 CTA pairs of a GB300, whatever the device has to spare, so that a workspace's size
 // does not depend on it.  Cycles by rounds of items over the pairs: a stage of 64 rows takes 2 bn of
-// MMAs, or what its conversion lets through (400); parts have to be written and read again, at about 3.5
-// KB a cycle, by a second kernel (5000).
+// MMAs, or what its conversion lets through (400), and a tile's sums about 10 bn to write; parts have to be
+// written and read again, at about 3.5 KB a cycle, by a second kernel (5000).
 WgradPlan plan_wgrad(int64_t rows, int n, int k) {
   constexpr int kPairs = 76;
   WgradPlan best{};
   int64_t least = -1;
-  for (int bn = k > 128 ? 256 : 128; bn >= 128; bn -= 128) {
+  for (int bn = n > 128 ? 256 : 128; bn >= 128; bn -= 128) {
     WgradPlan p{};
     p.bn = bn;
     p.stages = static_cast<int>((rows + 63) / 64);
-    p.tiles_m = ceil_div(n, 256), p.tiles_n = ceil_div(k, bn);
+    p.tiles_m = ceil_div(n, bn), p.tiles_n = ceil_div(k, 256);
     const int64_t tiles = p.tiles_m * p.tiles_n;
     for (int s = 1; s <= 32; ++s) {
       if (s > 1 && (s > p.stages || s * tiles > kPairs)) break;
       p.per_split = static_cast<int>(ceil_div(p.stages, s));
       p.splits = p.per_split ? static_cast<int>(ceil_div(p.stages, p.per_split)) : 1;
       const int64_t rounds = (p.splits * tiles + kPairs - 1) / kPairs;
-      const int64_t cost = rounds * (static_cast<int64_t>(p.per_split) * std::max(2 * bn, 400) + 1500) +
+      const int64_t cost = rounds * (static_cast<int64_t>(p.per_split) * std::max(2 * bn, 400) + 10 * bn) +
                            (p.splits > 1 ? 5000 + (p.splits + 1ll) * n * k * 4 / 3500 : 0);
       if (least < 0 || cost < least) least = cost, best = p;
     }
@@ -297,7 +297,7 @@ int refcache_f8_weight_grad(const void* dy, int64_t ld_dy, const refcache_f8_row
     a.guard.timeout_ns = rc_host::wait_timeout_ns();
     rc::f8::WgradMaps maps;
     if ((rc = rc_host::encode_map(&maps.dy, dy, 2 * static_cast<int64_t>(n), r.rows, 2 * ld_dy, 64)) != 0 ||
-        (rc = rc_host::encode_plain(&maps.codes, r.codes, k, r.rows, k, static_cast<uint32_t>(p.bn / 2), 64)) != 0 || (rc = tiles_map(&maps.tiles, r)) != 0)
+        (rc = rc_host::encode_map(&maps.codes, r.codes, k, r.rows, k, 64)) != 0 || (rc = tiles_map(&maps.tiles, r)) != 0)
       return rc;
     a.guard.stop = rc_host::take_debug_stop();
     const unsigned clusters = static_cast<unsigned>(std::min<int64_t>(p.tiles_m * p.tiles_n * p.splits, pairs));

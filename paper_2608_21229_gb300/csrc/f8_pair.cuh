@@ -76,10 +76,23 @@ __device__ __forceinline__ void copy_scales_pair(uint32_t tmem, uint64_t desc) {
   asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
 
+// 128 columns of this thread's lane; those from `cols` on are not there.
+__device__ __forceinline__ void load_sums(uint32_t t, int cols, float (&v)[128]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (32 * i >= cols) break;
+    uint32_t r[32];
+    tmem_ld32(t + 32 * i, r);
+    tmem_wait_ld(r);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[32 * i + j] = __uint_as_float(r[j]);
+  }
+}
+
 // ---------------------------------------------------------------- a CTA of a pair
 // L: kNumBars, kBars, kAux (abort flag, tensor memory's address, the other CTA's abort
-// flag, both CTAs' loads of each ring), kUsed, kDynamic, arrivals(barrier), kDone, the warps
-// kProducer and kMma, and two rings of loads: their first barriers kFull and kFull2, kSlots and kSlots2;
+// flag, both CTAs' loads of the first ring and of the second), kUsed, kDynamic, arrivals(barrier), kDone, the warps
+// kProducer, kProducer2 and kMma, and two rings of loads: their first barriers kFull and kFull2, kSlots and kSlots2;
 // kOwn2: loads of the second complete on the CTA's own barriers.
 template <typename L>
 struct Cta {
@@ -144,14 +157,15 @@ struct Cta {
     __syncwarp();
   }
 
-  // Loads that this CTA's producer issued (its lane 0) and a load's bytes of one CTA, by ring.  When
+  // Loads that this CTA's producers issued (lane 0 of each) and a load's bytes of one CTA, by ring.  When
   // neither CTA gave up, every load was waited for by what read it; else the leader, on
   // whose barriers both CTAs' loads complete, arms or counts what one half lacks of the
   // other and waits for the last phase of each (a CTA's own ring needs the wait alone).
   __device__ __forceinline__ void leave(int loads, uint32_t bytes, int loads2, uint32_t bytes2) const {
-    if (warp == L::kProducer && lane == 0) {
-      st_cluster_u32(mapa_shared(base + L::kAux + 12 + 8 * rank, 0), static_cast<uint32_t>(loads));
-      st_cluster_u32(mapa_shared(base + L::kAux + 16 + 8 * rank, 0), static_cast<uint32_t>(loads2));
+    if (warp == L::kProducer && lane == 0) st_cluster_u32(mapa_shared(base + L::kAux + 12 + 4 * rank, 0), static_cast<uint32_t>(loads));
+    if (warp == L::kProducer2 && lane == 0) {
+      // (a ring of each CTA's own is settled there)
+      st_cluster_u32(mapa_shared(base + L::kAux + 20 + 4 * rank, L::kOwn2 ? rank : 0), static_cast<uint32_t>(loads2));
     }
     tc_fence_before();
     __syncthreads();
@@ -179,11 +193,11 @@ struct Cta {
           if (m > 0) drain(bar(full + slot), static_cast<uint32_t>(m - 1) & 1u, ctl.timeout_ns);
         }
       };
-      if (leader) settle(L::kFull, L::kSlots, aux[3], aux[5], bytes);
+      if (leader) settle(L::kFull, L::kSlots, aux[3], aux[4], bytes);
       if (L::kOwn2)
-        settle(L::kFull2, L::kSlots2, loads2, loads2, bytes2);
+        settle(L::kFull2, L::kSlots2, aux[5 + rank], aux[5 + rank], bytes2);
       else if (leader)
-        settle(L::kFull2, L::kSlots2, aux[4], aux[6], bytes2);
+        settle(L::kFull2, L::kSlots2, aux[5], aux[6], bytes2);
     }
     cluster_sync();
   }

@@ -1,23 +1,27 @@
 // f8_wgrad.cuh -- a weight's gradient, dw = add + dy^T x, from bf16 dy [rows, n] and x [rows, k]
-// in its 8-bit form: bf16 tcgen05 MMAs over CTA pairs, 256 x 256 (or 128) of dw a tile.
+// in its 8-bit form: bf16 tcgen05 MMAs over CTA pairs, 256 columns of x times 256 (or 128) of
+// dy a tile.
 //
 // The sum runs over the rows, along which x has a scale each, so the tensor core cannot
 // apply them.  A code times its power of two is exact in bf16: eight warps of each CTA turn 64
-// rows of codes into bf16 in the shared memory that the MMAs read, and the product is that of
-// dy and of the values that x stands for.  Both operands lie with the rows of dw and its
-// columns contiguous (MN-major), as they come.
+// rows of codes into bf16 in tensor memory, where the MMAs take x from as their first
+// operand, and the product is that of dy and of the values that x stands for.
 //
-// CTA r of a pair holds columns [128 r, 128 r + 128) of dy's tile and half of x's.  A stage
-// is 64 rows: 16 KB of dy by TMA, 8 KB of codes (and 512 bytes of scales) by TMA into a
-// ring of their own, 16 KB of bf16, in which the MMAs take 512 cycles.  The converted
-// operand of the second CTA is read by MMAs that the first one issues: its warps arrive
-// at a barrier of their own CTA, and a warp passes that on with release at cluster scope
-// to one of the first CTA that acquires it and opens the MMA warp's barrier; either takes
-// longer than a stage has (about 1000 cycles), so two warps of each CTA take turns.
+// CTA r of a pair holds columns [128 r, 128 r + 128) of x's tile, one block of scales, and half
+// of dy's.  A stage is 64 rows: 16 KB of dy, as it lies (MN-major), 8 KB of codes and their
+// 512 bytes of scales, which a warp spreads to one bf16 a row.  ldmatrix on bytes with
+// transposition gives a thread four rows of one column, whose eight bytes of bf16 are what
+// tcgen05.st.16x256b takes from that thread; 64 rows of 16 columns are one such store.
+// (Converted in shared memory instead, the second CTA's half had to be released to the first
+// one, which issues the MMAs, at cluster scope: 1320 cycles an arrival, and 1180 a stage;
+// arrivals that order tensor memory need no such release.)
 //
-// Sums: two buffers of 256 columns of tensor memory; four warps write one out while the
-// other is added to.  Where the tiles are few the rows are split and the parts added by
-// another kernel in a fixed order.
+// Tensor memory: 384 columns of sums and four stages of x.  Lane = column of x, so that each store
+// of a lane joins those of its warp in one line of dw.  All tiles end at about the same time, and
+// what they write waits for the memory, so a tile's sums must not: tiles take columns
+// [0, 256) and [128, 384) in turn, eight warps take the 128 columns that both share into
+// registers as soon as a tile ends, and the other 128 while the next tile's MMAs run.  Where the
+// tiles are few the rows are split and the parts added by another kernel in a fixed order.
 #pragma once
 #include "f8_pair.cuh"
 
@@ -28,51 +32,67 @@ struct WgradArgs {
   const void* add;   // [n, k] like dw, or null
   void* dw;          // [n, k]; the parts, fp32, where there are several
   int32_t f32;       // dw (and add) fp32, else bf16
-  int32_t n, k, bn;  // bn: columns of a tile, 128 or 256
+  int32_t n, k, bn;  // bn: columns of dy in a tile, 128 or 256
   int64_t rows;
   int32_t chunks;  // of 128 rows
   int32_t stages;  // of 64 rows
   int32_t splits, per_split;  // parts, and stages of each
-  Tiles tiles;
+  Tiles tiles;                // m: of n; n: of k
   Guard guard;
 };
 struct WgradMaps {
-  CUtensorMap dy, codes, tiles;  // 64 rows x 64 columns (128 bytes); 64 rows x half a tile's columns; 512 bytes
+  CUtensorMap dy, codes, tiles;  // 64 rows x 64 columns (128 bytes); 64 rows x 128 columns; 512 bytes
 };
 
 struct WgradSmem {
-  static constexpr int kSlots = 4, kSlots2 = 6, kSlotsB = 6;  // dy, codes, converted
+  static constexpr int kSlots = 8, kSlots2 = 8, kSlotsA = 4;  // dy, codes, converted (in tensor memory)
   static constexpr bool kOwn2 = true;  // codes complete on barriers of the CTA that loads them
-  static constexpr int kAhead = 3;                            // stages that codes are loaded ahead of dy
-  static constexpr uint32_t kA = 16384, kCodes = 8192, kC = kCodes + 512, kB = 16384;
-  static constexpr uint32_t kOffA = 0, kOffB = kSlots * kA, kOffC = kOffB + kSlotsB * kB, kBars = kOffC + kSlots2 * kC;
-  // kFull2 and kEmpty2 are of each CTA's own codes; kBDone: converted, in this CTA; kBPeer: in the other one; kBFull: in both
-  static constexpr int kFull = 0, kEmpty = kFull + kSlots, kFull2 = kEmpty + kSlots, kEmpty2 = kFull2 + kSlots2, kBDone = kEmpty2 + kSlots2,
-                       kBPeer = kBDone + kSlotsB, kBFull = kBPeer + kSlotsB, kBEmpty = kBFull + kSlotsB, kAccFull = kBEmpty + kSlotsB,
-                       kAccEmpty = kAccFull + 2, kDone = kAccEmpty + 2, kNumBars = kDone + 1;
+  static constexpr uint32_t kB = 16384, kCodes = 8192;
+  static constexpr uint32_t kOffB = 0, kOffC = kOffB + kSlots * kB, kOffT = kOffC + kSlots2 * kCodes, kOffS = kOffT + kSlots2 * 512,
+                            kBars = kOffS + kSlots2 * 128;
+  // kFull2, kEmpty2, kScale (a stage's scales are spread) are of each CTA alone; kAccEmpty: the shared sums, the others by turns
+  static constexpr int kFull = 0, kEmpty = kFull + kSlots, kFull2 = kEmpty + kSlots, kScale = kFull2 + kSlots2, kEmpty2 = kScale + kSlots2,
+                       kAFull = kEmpty2 + kSlots2, kAEmpty = kAFull + kSlotsA, kAccFull = kAEmpty + kSlotsA, kAccEmpty = kAccFull + 1,
+                       kDone = kAccEmpty + 3, kNumBars = kDone + 1;
   static constexpr uint32_t kAux = kBars + 8 * kNumBars, kUsed = kAux + 28, kDynamic = kUsed + 1024;
-  // warps 0-3: sums, 4-11: codes into bf16
-  static constexpr int kConvert = 4, kConvertWarps = 8, kProducer = 12, kMma = 13, kRelay = 14, kThreads = 32 * 16;
+  // warps 0-7: sums; 8-15: codes into bf16, two groups that take turns
+  static constexpr int kConvert = 8, kProducer = 16, kMma = 17, kSpread = 18, kProducer2 = 19, kThreads = 32 * 20;
+  static constexpr uint32_t kTmemA = 384;
   static_assert(kDynamic <= kMaxDynamic, "shared-memory layout too large");
   __device__ static constexpr uint32_t arrivals(int i) {
-    return (i >= kEmpty2 && i < kBPeer) || (i >= kAccEmpty && i < kDone) ? 8 : 1;  // kEmpty2, kBDone: the converting warps; kAccEmpty: four warps of each CTA
+    // kEmpty2: the four warps of a group; kAFull: of each CTA; kAccEmpty: eight of each
+    return i >= kEmpty2 && i < kAFull ? 4 : i >= kAFull && i < kAEmpty ? 8 : i >= kAccEmpty && i < kDone ? 16 : 1;
   }
 };
 
-// Four codes times s (a power of two in both halves, or NaN) as four bf16.  A code's bits
-// shifted to bf16's places are its value times 2^-120, E4M3's subnormals being bf16's.
-__device__ __forceinline__ uint2 codes_to_bf16(uint32_t c, uint32_t s) {
-  auto two = [&](uint32_t h) {  // codes in the upper bytes
-    const uint32_t v = ((h >> 4) & 0x07F007F0u) | (h & 0x80008000u);
+// Four codes of four rows as bf16, times the rows' scales.  A code's bits shifted to
+// bf16's places are its value times 2^-120, E4M3's subnormals being bf16's.
+__device__ __forceinline__ void codes_to_bf16(uint32_t c, uint2 scales, uint32_t* to) {
+  auto two = [](uint32_t h, uint32_t s) {  // codes in the upper bytes
+    const uint32_t v = ((h >> 4) & 0x07F007F0u) | (h & 0x80008000u), up = 0x7B807B80u;  // 2^120
     __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162*>(&v);
-    const uint32_t up = 0x7B807B80u;  // 2^120
     x = __hmul2(__hmul2(x, *reinterpret_cast<const __nv_bfloat162*>(&up)), *reinterpret_cast<const __nv_bfloat162*>(&s));
     return *reinterpret_cast<const uint32_t*>(&x);
   };
-  return make_uint2(two(__byte_perm(c, 0, 0x1404)), two(__byte_perm(c, 0, 0x3424)));
+  to[0] = two(__byte_perm(c, 0, 0x1404), scales.x);
+  to[1] = two(__byte_perm(c, 0, 0x3424), scales.y);
 }
-
-__host__ __device__ constexpr uint32_t idesc_wgrad(int n) { return idesc_bf16_f32(256, n, true) | (1u << 15); }
+// Two 16 x 16 tiles of bytes, transposed: r[0], r[1] are rows 4 (lane % 4) .. + 3 of columns
+// lane / 4 and lane / 4 + 8 of the first, r[2], r[3] of the second.  Lane l gives row l % 16 of tile l / 16.
+__device__ __forceinline__ void ldmatrix_bytes(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+// 16 lanes of 32 columns: of each eight columns, a thread has two of lane (lane / 4) and two of that + 8.
+__device__ __forceinline__ void tmem_st_16x256(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), "r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]),
+      "r"(r[14]), "r"(r[15])
+      : "memory");
+}
 
 // The items of a launch: part by part, each over all tiles.
 struct WgradItem {
@@ -88,6 +108,32 @@ __device__ __forceinline__ WgradItem wgrad_item(const WgradArgs& a, int item) {
   return t;
 }
 
+// One lane's column of x, 64 rows of dw (the first `rows` of them there), each a line's part with the
+// other lanes'.  What is added comes first, then the sums, then all is stored.
+// (The pointers go from row to row: with the rows' addresses kept for the whole tile the registers spill.)
+template <typename T>
+__device__ __forceinline__ void next_row(T& p, int64_t stride) {
+  p += stride;
+  asm volatile("" : "+l"(p));
+}
+template <typename T>
+__device__ __forceinline__ void load_rows(float (&v)[64], const T* from, int64_t stride, int rows) {
+#pragma unroll
+  for (int e = 0; e < 64; ++e) {
+    v[e] = 0.f;
+    if (e < rows) v[e] = sizeof(T) == 4 ? __uint_as_float(static_cast<uint32_t>(*from)) : __uint_as_float(static_cast<uint32_t>(*from) << 16);
+    next_row(from, stride);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_rows(const float (&v)[64], T* to, int64_t stride, int rows) {
+#pragma unroll
+  for (int e = 0; e < 64; ++e) {
+    if (e < rows) *to = sizeof(T) == 4 ? static_cast<T>(__float_as_uint(v[e])) : static_cast<T>(pack_bf16x2(v[e], 0.f));
+    next_row(to, stride);
+  }
+}
+
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WgradSmem::kThreads, 1)
     f8_wgrad_kernel(const __grid_constant__ WgradMaps maps, const __grid_constant__ WgradArgs a) {
   using L = WgradSmem;
@@ -95,208 +141,208 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WgradSmem::kThreads,
   Cta<L> c;
   if (!c.enter(smem_raw, a.guard)) return;
   const int cluster = static_cast<int>(blockIdx.x >> 1), n_clusters = static_cast<int>(gridDim.x >> 1);
-  const int n_items = a.tiles.m * a.tiles.n * a.splits, half = a.bn / 2;  // half: columns of x in a CTA
-  const uint32_t code_bytes = static_cast<uint32_t>(half) * 64u, c_bytes = code_bytes + 512u;
+  const int n_items = a.tiles.m * a.tiles.n * a.splits;
+  const uint32_t b_bytes = static_cast<uint32_t>(a.bn) * 64u, c_bytes = L::kCodes + 512u;
   int loads = 0, loads2 = 0;
-  if (c.warp == L::kProducer) {
-    if (c.lane == 0) {
-      const int most = loads_before_stop(a.guard.stop, c.rank);
-      // codes go kAhead stages ahead of dy: they are needed earlier by their conversion
-      int item2 = cluster, at2 = -1;
-      WgradItem t2{};
-      auto next_codes = [&]() -> bool {  // false: gave up
-        if (at2 < 0) {
-          if (item2 >= n_items) return true;
-          t2 = wgrad_item(a, item2);
-          at2 = t2.first;
-        }
-        const int s = loads2 % L::kSlots2, n = loads2 / L::kSlots2;
-        if (n > 0 && !c.wait(L::kEmpty2 + s, n - 1, 112)) return false;
-        const uint32_t to = c.base + L::kOffC + static_cast<uint32_t>(s) * L::kC, full = c.bar(L::kFull2 + s);
-        const int col = t2.j * a.bn + half * static_cast<int>(c.rank);
-        mbar_arrive_expect_tx(full, c_bytes);
-        tma_load_2d_pair(to, &maps.codes, mapa_shared(full, c.rank), col, at2 * 64);
-        tma_load_2d_pair(to + L::kCodes, &maps.tiles, mapa_shared(full, c.rank), 0, (col / (4 * kBlock)) * a.chunks + at2 / 2);
-        ++loads2;
-        if (++at2 == t2.last) at2 = -1, item2 += n_clusters;
-        return true;
-      };
-      bool ok = true;
-      for (int i = 0; ok && i < L::kAhead; ++i) ok = next_codes();
+  if (c.warp < L::kConvert) {
+    const int group = c.warp >> 2, quarter = c.warp & 3;
+    int used = 0;
+    bool ok = true;
 #pragma unroll 1
-      for (int item = cluster; ok && item < n_items; item += n_clusters) {
-        const WgradItem t = wgrad_item(a, item);
-        const int col = t.i * 256 + 128 * static_cast<int>(c.rank);
-#pragma unroll 1
-        for (int st = t.first; st < t.last; ++st) {
-          ok = next_codes();
-          const int s = loads % L::kSlots, n = loads / L::kSlots;
-          ok = ok && loads != most && (n == 0 || c.wait(L::kEmpty + s, n - 1, 111));
-          if (!ok) break;
-          const uint32_t to = c.base + L::kOffA + static_cast<uint32_t>(s) * L::kA, full = c.lbar(L::kFull + s);
-          if (c.leader) mbar_arrive_expect_tx(c.bar(L::kFull + s), 2 * L::kA);
-          tma_load_2d_pair(to, &maps.dy, full, 2 * col, st * 64);  // (a map of bytes)
-          tma_load_2d_pair(to + 8192, &maps.dy, full, 2 * col + 128, st * 64);
-          ++loads;
-        }
-      }
-    }
-    __syncwarp();
-  } else if (c.warp == L::kMma) {
-    if (c.leader) {
-      // (64 columns of 64 rows are 8 KB; 8 rows 1 KB)
-      const uint64_t ad = sdesc_sw128(c.base + L::kOffA, 8192, 1024), bd = sdesc_sw128(c.base + L::kOffB, 8192, 1024);
-      const uint32_t idesc = idesc_wgrad(a.bn);
-      bool issued = false, ok = true;
-      int load = 0, used = 0;
-#pragma unroll 1
-      for (int item = cluster; ok && item < n_items; item += n_clusters, ++used) {
-        const WgradItem t = wgrad_item(a, item);
-        const uint32_t d = c.tmem + 256u * (used & 1);
-        if (used >= 2 && !c.wait_all(L::kAccEmpty + (used & 1), (used >> 1) - 1, 113)) break;
-#pragma unroll 1
-        for (int st = t.first; st < t.last; ++st, ++load) {
-          const int s = load % L::kSlots, b = load % L::kSlotsB;
-          ok = c.wait_all(L::kFull + s, load / L::kSlots, 114) && c.wait_all(L::kBFull + b, load / L::kSlotsB, 115);
-          if (!ok) break;
-          issued = true;
-          if (elect_one()) {
-            tc_fence_after();
-            const uint64_t at = ad + static_cast<uint64_t>(s) * (L::kA >> 4), bt = bd + static_cast<uint64_t>(b) * (L::kB >> 4);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) tc2_mma_ss(d, at + 128 * q, bt + 128 * q, idesc, st > t.first || q > 0 ? 1u : 0u);
-            tc2_commit_mc(c.bar(L::kEmpty + s), 3);
-            tc2_commit_mc(c.bar(L::kBEmpty + b), 3);
-            if (st + 1 == t.last) tc2_commit_mc(c.bar(L::kAccFull + (used & 1)), 3);
-          }
-          __syncwarp();
-        }
-      }
-      c.finish_mmas(issued);
-    }
-  } else if (c.warp >= L::kRelay) {
-    int total = 0;
-    for (int item = cluster; item < n_items; item += n_clusters) {
+    for (int item = cluster; ok && item < n_items; item += n_clusters, ++used) {
       const WgradItem t = wgrad_item(a, item);
-      total += t.last - t.first;
-    }
+      const int col = t.j * 256 + 128 * static_cast<int>(c.rank) + 32 * quarter + c.lane;
+      const bool add = a.add != nullptr && a.splits == 1;
+      const int turn = used & 1;
 #pragma unroll 1
-    for (int n = c.warp - L::kRelay; n < total; n += 2) {
-      const int b = n % L::kSlotsB, k = n / L::kSlotsB;
-      if (!c.wait_all(L::kBDone + b, k, 116)) break;
-      if (c.leader) {
-        if (!c.wait_all(L::kBPeer + b, k, 117) || !__all_sync(0xffffffffu, mbar_try_wait_acquire_cluster(c.bar(L::kBPeer + b), static_cast<uint32_t>(k) & 1u))) break;
-        if (c.lane == 0) mbar_arrive(c.bar(L::kBFull + b));
-      } else {
-        if (c.lane == 0) mbar_arrive_release_cluster(c.lbar(L::kBPeer + b));
+      for (int i = 0; i < 2; ++i) {
+        const int h = turn ? i : 1 - i;  // the half in the shared columns first
+        const int row0 = t.i * a.bn + 128 * h + 64 * group, rows = col < a.k && 128 * h < a.bn ? a.n - row0 : 0;
+        const int64_t at = (static_cast<int64_t>(t.part) * a.n + row0) * a.k + col;
+        float v[64];
+        if (!add) {
+#pragma unroll
+          for (int e = 0; e < 64; ++e) v[e] = 0.f;
+        } else if (a.f32) {
+          load_rows(v, static_cast<const uint32_t*>(a.add) + at, a.k, rows);
+        } else {
+          load_rows(v, static_cast<const uint16_t*>(a.add) + at, a.k, rows);
+        }
+        if (i == 0) ok = c.wait_all(L::kAccFull, used, 120);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t from = c.tmem + 128u * (turn + h) + 64u * group + (static_cast<uint32_t>(quarter) << 21);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t r[16];
+          tmem_ld16(from + 16 * q, r);
+          tmem_wait_ld(r);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[16 * q + e] += __uint_as_float(r[e]);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (c.lane == 0) mbar_arrive_cluster(c.lbar(L::kAccEmpty + (i == 0 ? 0 : 1 + turn)));
+        if (a.f32)
+          store_rows(v, static_cast<uint32_t*>(a.dw) + at, a.k, rows);
+        else
+          store_rows(v, static_cast<uint16_t*>(a.dw) + at, a.k, rows);
       }
-      __syncwarp();
     }
-  } else if (c.warp >= L::kConvert) {
-    // A warp takes four rows at a time, 16 codes a lane (fewer lanes where the tile is narrow).
-    const int w = c.warp - L::kConvert, unit = c.lane & 7, sub = c.lane >> 3;
-    const bool in = 16 * unit < half;
+  } else if (c.warp < L::kProducer) {
+    const int group = (c.warp - L::kConvert) >> 2, quarter = c.warp & 3;
+    const uint32_t lanes = static_cast<uint32_t>(quarter) << 21;
     int n = 0;
     bool ok = true;
 #pragma unroll 1
     for (int item = cluster; ok && item < n_items; item += n_clusters) {
       const WgradItem t = wgrad_item(a, item);
-      const int block = (t.j * a.bn + half * static_cast<int>(c.rank)) / kBlock;
 #pragma unroll 1
       for (int st = t.first; st < t.last; ++st, ++n) {
-        const int s = n % L::kSlots2, b = n % L::kSlotsB;
-        ok = c.wait_all(L::kFull2 + s, n / L::kSlots2, 118) && (n < L::kSlotsB || c.wait_all(L::kBEmpty + b, n / L::kSlotsB - 1, 119));
+        if ((n & 1) != group) continue;
+        const int s = n % L::kSlots2, x = n % L::kSlotsA;
+        // (the spread scales are there after the codes)
+        ok = c.wait_all(L::kScale + s, n / L::kSlots2, 117) && c.wait_all(L::kFull2 + s, n / L::kSlots2, 118) &&
+             (n < L::kSlotsA || c.wait_all(L::kAEmpty + x, n / L::kSlotsA - 1, 119));
         if (!ok) break;
-        const uint8_t* codes = c.ptr + L::kOffC + s * L::kC;
-        const uint32_t to = c.base + L::kOffB + static_cast<uint32_t>(b) * L::kB;
+        tc_fence_after();
+        const uint32_t codes = c.base + L::kOffC + static_cast<uint32_t>(s) * L::kCodes;
+        const uint8_t* scales = c.ptr + L::kOffS + s * 128 + 8 * (c.lane & 3);
+        uint2 f[4];
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          const int r = 32 * p + 4 * w + sub;
-          const int rt = (st & 1) * 64 + r;  // of the scales' 128 rows
-          const uint32_t e = codes[L::kCodes + 16 * (rt & 31) + 4 * (rt >> 5) + (block & 3)];
-          // rows past the end hold zeros and anything as scale
-          const uint32_t sc = static_cast<int64_t>(st) * 64 + r >= a.rows ? 0u : e == 255u ? 0x7FC0u : e << 7;
-          if (in) {
-            const uint4 v = *reinterpret_cast<const uint4*>(codes + r * half + 16 * unit);
-            const uint2 x0 = codes_to_bf16(v.x, sc * 0x10001u), x1 = codes_to_bf16(v.y, sc * 0x10001u);
-            const uint2 x2 = codes_to_bf16(v.z, sc * 0x10001u), x3 = codes_to_bf16(v.w, sc * 0x10001u);
-            const uint4 lo = make_uint4(x0.x, x0.y, x1.x, x1.y), hi = make_uint4(x2.x, x2.y, x3.x, x3.y);
-            // 64 columns (128 bytes) a row and half of the tile, 16-byte pieces swizzled; the lanes of the
-            // second 64 write their odd piece first, so that eight lanes fill all banks
-            const uint32_t row = to + (unit >> 2) * 8192u + 128u * r, odd = unit >> 2, piece = 2 * (unit & 3);
-            st_shared_v4(row + (((piece + odd) ^ (r & 7)) << 4), odd ? hi : lo);
-            st_shared_v4(row + (((piece + 1 - odd) ^ (r & 7)) << 4), odd ? lo : hi);
+        for (int g = 0; g < 4; ++g) f[g] = *reinterpret_cast<const uint2*>(scales + 32 * g);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t out[16];
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            const int r = 32 * p + c.lane;  // this lane's row of codes, 128 bytes swizzled
+            uint32_t v[4];
+            ldmatrix_bytes(codes + 128u * r + (((2u * quarter + h) ^ (r & 7)) << 4), v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) codes_to_bf16(v[e], f[2 * p + (e >> 1)], out + 8 * p + 2 * e);
           }
+          tmem_st_16x256(c.tmem + L::kTmemA + 32u * x + lanes + (static_cast<uint32_t>(h) << 20), out);
         }
-        fence_proxy_async_smem();
+        tmem_wait_st();
+        tc_fence_before();
         __syncwarp();
         if (c.lane == 0) {
           mbar_arrive(c.bar(L::kEmpty2 + s));
-          mbar_arrive(c.bar(L::kBDone + b));
+          mbar_arrive_cluster(c.lbar(L::kAFull + x));
         }
         __syncwarp();
       }
     }
   } else {
-    const int quarter = c.warp;
-    int used = 0;
+    if (c.warp == L::kProducer) {
+      if (c.lane == 0) {
+        const int most = loads_before_stop(a.guard.stop, c.rank);
+        bool ok = true;
 #pragma unroll 1
-    for (int item = cluster; item < n_items; item += n_clusters, ++used) {
-      const WgradItem t = wgrad_item(a, item);
-      const int row = t.i * 256 + 128 * static_cast<int>(c.rank) + 32 * quarter + c.lane, col0 = t.j * a.bn;
-      const int cols = row < a.n ? min(a.bn, a.k - col0) : 0;
-      const int64_t at = (static_cast<int64_t>(t.part) * a.n + row) * a.k + col0;
-      const bool add = a.add != nullptr && a.splits == 1;
-      if (!c.wait_all(L::kAccFull + (used & 1), used >> 1, 120)) break;
-      tc_fence_after();
-      const uint32_t from = c.tmem + 256u * (used & 1) + (static_cast<uint32_t>(quarter) << 21);
+        for (int item = cluster; ok && item < n_items; item += n_clusters) {
+          const WgradItem t = wgrad_item(a, item);
+          const int col = t.i * a.bn + a.bn / 2 * static_cast<int>(c.rank);
 #pragma unroll 1
-      for (int x = 0; x < a.bn; x += 32) {
-        uint32_t r[32];
-        tmem_ld32(from + x, r);
-        tmem_wait_ld(r);
-        if (x + 32 == a.bn) {
-          tc_fence_before();
-          __syncwarp();
-          if (c.lane == 0) mbar_arrive_cluster(c.lbar(L::kAccEmpty + (used & 1)));
-        }
-#pragma unroll
-        for (int h = 0; h < 32; h += 16) {
-          if (x + h >= cols) continue;
-          if (a.f32) {
-            float4* y = reinterpret_cast<float4*>(static_cast<float*>(a.dw) + at + x + h);
-            const float4* z = reinterpret_cast<const float4*>(static_cast<const float*>(a.add) + at + x + h);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              float4 v = make_float4(__uint_as_float(r[h + 4 * q]), __uint_as_float(r[h + 4 * q + 1]), __uint_as_float(r[h + 4 * q + 2]),
-                                     __uint_as_float(r[h + 4 * q + 3]));
-              if (add) {
-                const float4 o = z[q];
-                v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
-              }
-              y[q] = v;
-            }
-          } else {
-            uint4* y = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.dw) + at + x + h);
-            const uint4* z = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.add) + at + x + h);
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              Vec8 v;
-#pragma unroll
-              for (int e = 0; e < 8; ++e) v.v[e] = __uint_as_float(r[h + 8 * q + e]);
-              if (add) {
-                const Vec8 o = unpack8(z[q]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v.v[e] += o.v[e];
-              }
-              y[q] = pack8(v);
-            }
+          for (int st = t.first; st < t.last; ++st) {
+            const int s = loads % L::kSlots, n = loads / L::kSlots;
+            ok = loads != most && (n == 0 || c.wait(L::kEmpty + s, n - 1, 111));
+            if (!ok) break;
+            const uint32_t to = c.base + L::kOffB + static_cast<uint32_t>(s) * L::kB, full = c.lbar(L::kFull + s);
+            if (c.leader) mbar_arrive_expect_tx(c.bar(L::kFull + s), 2 * b_bytes);
+            tma_load_2d_pair(to, &maps.dy, full, 2 * col, st * 64);  // (a map of bytes)
+            if (a.bn > 128) tma_load_2d_pair(to + 8192, &maps.dy, full, 2 * col + 128, st * 64);
+            ++loads;
           }
+        }
+      }
+      __syncwarp();
+    } else if (c.warp == L::kProducer2) {
+      if (c.lane == 0) {
+        bool ok = true;
+#pragma unroll 1
+        for (int item = cluster; ok && item < n_items; item += n_clusters) {
+          const WgradItem t = wgrad_item(a, item);
+          const int col = t.j * 256 + 128 * static_cast<int>(c.rank), line0 = (col / (4 * kBlock)) * a.chunks;
+#pragma unroll 1
+          for (int st = t.first; st < t.last; ++st) {
+            const int s = loads2 % L::kSlots2, n = loads2 / L::kSlots2;
+            ok = n == 0 || c.wait(L::kEmpty2 + s, n - 1, 112);
+            if (!ok) break;
+            const uint32_t bar = c.bar(L::kFull2 + s), full = mapa_shared(bar, c.rank);
+            mbar_arrive_expect_tx(bar, c_bytes);
+            tma_load_2d_pair(c.base + L::kOffC + static_cast<uint32_t>(s) * L::kCodes, &maps.codes, full, col, st * 64);
+            tma_load_2d_pair(c.base + L::kOffT + static_cast<uint32_t>(s) * 512u, &maps.tiles, full, 0, line0 + st / 2);
+            ++loads2;
+          }
+        }
+      }
+      __syncwarp();
+    } else if (c.warp == L::kMma) {
+      if (c.leader) {
+        const uint64_t bd = sdesc_sw128(c.base + L::kOffB, 8192, 1024);  // (64 columns of 64 rows are 8 KB; 8 rows 1 KB)
+        const uint32_t idesc = idesc_bf16_f32(256, a.bn, true);
+        bool issued = false, ok = true;
+        int load = 0, used = 0;
+#pragma unroll 1
+        for (int item = cluster; ok && item < n_items; item += n_clusters, ++used) {
+          const WgradItem t = wgrad_item(a, item);
+          const uint32_t d = c.tmem + 128u * (used & 1);
+#pragma unroll 1
+          for (int st = t.first; st < t.last; ++st, ++load) {
+            const int s = load % L::kSlots, x = load % L::kSlotsA;
+            ok = c.wait_all(L::kFull + s, load / L::kSlots, 114) && c.wait_all(L::kAFull + x, load / L::kSlotsA, 115);
+            if (ok && st == t.first)
+              ok = (used < 1 || c.wait_all(L::kAccEmpty, used - 1, 113)) && (used < 2 || c.wait_all(L::kAccEmpty + 1 + (used & 1), (used >> 1) - 1, 113));
+            if (!ok) break;
+            issued = true;
+            if (elect_one()) {
+              tc_fence_after();
+              const uint64_t bt = bd + static_cast<uint64_t>(s) * (L::kB >> 4);
+              const uint32_t at = c.tmem + L::kTmemA + 32u * x;
+#pragma unroll
+              for (int q = 0; q < 4; ++q) tc2_mma_ts(d, at + 8u * q, bt + 128 * q, idesc, st > t.first || q > 0 ? 1u : 0u);
+              tc2_commit_mc(c.bar(L::kEmpty + s), 3);
+              tc2_commit_mc(c.bar(L::kAEmpty + x), 3);
+              if (st + 1 == t.last) tc2_commit_mc(c.bar(L::kAccFull), 3);
+            }
+            __syncwarp();
+          }
+        }
+        c.finish_mmas(issued);
+      }
+    } else if (c.warp == L::kSpread) {
+      // A stage's scales, one bf16 for each of its 64 rows (two a lane).  Rows past the end hold zeros as codes and
+      // anything as scale: theirs is 0.
+      int n = 0;
+      bool ok = true;
+#pragma unroll 1
+      for (int item = cluster; ok && item < n_items; item += n_clusters) {
+        const WgradItem t = wgrad_item(a, item);
+        const int block = t.j * 2 + static_cast<int>(c.rank);
+#pragma unroll 1
+        for (int st = t.first; st < t.last; ++st, ++n) {
+          const int s = n % L::kSlots2;
+          ok = c.wait_all(L::kFull2 + s, n / L::kSlots2, 116);
+          if (!ok) break;
+          const uint8_t* tile = c.ptr + L::kOffT + s * 512;
+          uint32_t two = 0;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int r = 2 * c.lane + i, rt = (st & 1) * 64 + r;
+            const uint32_t e = tile[16 * (rt & 31) + 4 * (rt >> 5) + (block & 3)];
+            const uint32_t v = static_cast<int64_t>(st) * 64 + r >= a.rows ? 0u : e == 255u ? 0x7FC0u : e << 7;
+            two |= v << (16 * i);
+          }
+          *reinterpret_cast<uint32_t*>(c.ptr + L::kOffS + s * 128 + 4 * c.lane) = two;
+          __syncwarp();
+          if (c.lane == 0) mbar_arrive(c.bar(L::kScale + s));
+          __syncwarp();
         }
       }
     }
   }
-  c.leave(loads, L::kA, loads2, c_bytes);
+  c.leave(loads, b_bytes, loads2, c_bytes);
 }
 
 // dw = add + the parts, one after the other.

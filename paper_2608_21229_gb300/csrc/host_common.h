@@ -25,9 +25,8 @@ uint64_t wait_timeout_ns();
 int take_debug_stop();
 
 // 2-D tensor maps.  `outer` rows of `inner` bytes, `pitch` bytes apart: boxes of 128 bytes x box_outer
-// rows with the 128-byte swizzle, or of box_inner bytes without one; `lines` lines of 512 bytes, one line a box.
+// rows with the 128-byte swizzle; `lines` lines of 512 bytes, one line a box.
 int encode_map(CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t pitch, uint32_t box_outer);
-int encode_plain(CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t pitch, uint32_t box_inner, uint32_t box_outer);
 int encode_lines(CUtensorMap* m, const void* base, int64_t lines);
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

@@ -219,10 +219,6 @@ int encode_map(CUtensorMap* m, const void* base, int64_t inner, int64_t outer, i
   return encode_2d(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, inner, outer, pitch, 128, box_outer, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-int encode_plain(CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t pitch, uint32_t box_inner, uint32_t box_outer) {
-  return encode_2d(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, inner, outer, pitch, box_inner, box_outer, CU_TENSOR_MAP_SWIZZLE_NONE);
-}
-
 int encode_lines(CUtensorMap* m, const void* base, int64_t lines) {
   return encode_2d(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, base, 128, lines, 512, 128, 1, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
