@@ -155,33 +155,39 @@ int launch_linear(const rc::f8::Rows& x, const rc::f8::Rows& w, const rc::f8::Ou
 
 // How a weight gradient is taken apart.
 struct WgradPlan {
+  int panel;  // columns of x whose values are in the workspace at a time
   int bn, stages, splits, per_split;
-  int64_t tiles_m, tiles_n;
+  size_t values_bytes, parts_bytes;
 };
+constexpr int64_t kPanelBytes = 256ll << 20;  // of a panel, unless 256 columns are more
+
 // The plan is for the 76 CTA pairs of a GB300, whatever the device has to spare, so that a workspace's size
 // does not depend on it.  Cycles by rounds of items over the pairs: a stage of 64 rows takes 2 bn of
-// MMAs, or what its conversion lets through (400), and a tile's sums about 10 bn to write; parts have to be
-// written and read again, at about 3.5 KB a cycle, by a second kernel (5000).
+// MMAs or 256 + bn to move its operands, a tile about 1000 at its ends; parts have to be written and
+// read again, at about 3.5 KB a cycle, by another kernel (5000).
 WgradPlan plan_wgrad(int64_t rows, int n, int k) {
   constexpr int kPairs = 76;
   WgradPlan best{};
+  const int64_t fit = std::max<int64_t>(kPanelBytes / (2 * std::max<int64_t>(rows, 1)) / 256 * 256, 256);
+  const int panel = static_cast<int>(std::min<int64_t>(fit, k));
   int64_t least = -1;
   for (int bn = n > 128 ? 256 : 128; bn >= 128; bn -= 128) {
     WgradPlan p{};
-    p.bn = bn;
+    p.panel = panel, p.bn = bn;
     p.stages = static_cast<int>((rows + 63) / 64);
-    p.tiles_m = ceil_div(n, bn), p.tiles_n = ceil_div(k, 256);
-    const int64_t tiles = p.tiles_m * p.tiles_n;
+    const int64_t tiles = static_cast<int64_t>(ceil_div(n, bn)) * ceil_div(panel, 256);
     for (int s = 1; s <= 32; ++s) {
-      if (s > 1 && (s > p.stages || s * tiles > kPairs)) break;
+      if (s > 1 && (panel < k || s > p.stages || s * tiles > kPairs)) break;
       p.per_split = static_cast<int>(ceil_div(p.stages, s));
       p.splits = p.per_split ? static_cast<int>(ceil_div(p.stages, p.per_split)) : 1;
       const int64_t rounds = (p.splits * tiles + kPairs - 1) / kPairs;
-      const int64_t cost = rounds * (static_cast<int64_t>(p.per_split) * std::max(2 * bn, 400) + 10 * bn) +
+      const int64_t cost = rounds * (static_cast<int64_t>(p.per_split) * std::max(2 * bn, 256 + bn) + 1000) +
                            (p.splits > 1 ? 5000 + (p.splits + 1ll) * n * k * 4 / 3500 : 0);
       if (least < 0 || cost < least) least = cost, best = p;
     }
   }
+  best.values_bytes = (static_cast<size_t>(rows) * panel * 2 + 255) / 256 * 256;
+  best.parts_bytes = best.splits > 1 ? static_cast<size_t>(best.splits) * n * k * sizeof(float) : 0;
   return best;
 }
 
@@ -264,7 +270,7 @@ int refcache_f8_linear_gelu_backward(const refcache_f8_rows_t* dy, const refcach
 size_t refcache_f8_weight_grad_bytes(int64_t rows, int out_width, int in_width) {
   if (rows <= 0 || rows > kMaxRows || check_width(out_width, "dw") != 0 || check_width(in_width, "dw") != 0) return 0;
   const WgradPlan p = plan_wgrad(rows, out_width, in_width);
-  return p.splits > 1 ? static_cast<size_t>(p.splits) * out_width * in_width * sizeof(float) : 0;
+  return p.values_bytes + p.parts_bytes;
 }
 
 int refcache_f8_weight_grad(const void* dy, int64_t ld_dy, const refcache_f8_rows_t* x, int out_width, const void* add, void* dw, int dw_f32,
@@ -277,8 +283,7 @@ int refcache_f8_weight_grad(const void* dy, int64_t ld_dy, const refcache_f8_row
   if (reinterpret_cast<uintptr_t>(d_bias) & 3u) return fail(REFCACHE_ERR_INVALID_ARG, "d_bias is not 4-byte aligned");
   const int n = out_width, k = x->width;
   const WgradPlan p = plan_wgrad(x->rows, n, k);
-  if (p.splits > 1 && (rc = check_tensor(work, "work")) != 0) return rc;
-  if (p.tiles_m * p.tiles_n > (1ll << 30)) return fail(REFCACHE_ERR_INVALID_ARG, "a gradient of %d x %d is too large", n, k);
+  if (x->rows > 0 && (rc = check_tensor(work, "work")) != 0) return rc;
   static std::atomic<int> kept[rc_host::kMaxDevices];
   rc::f8::WgradArgs a{};
   int sms = 0, dev = 0, pairs = 0;
@@ -287,27 +292,35 @@ int refcache_f8_weight_grad(const void* dy, int64_t ld_dy, const refcache_f8_row
     return rc;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
-  if (x->rows > 0) {
+  float* parts = reinterpret_cast<float*>(static_cast<uint8_t*>(work) + p.values_bytes);
+  a.guard.stop = rc_host::take_debug_stop();
+  a.guard.timeout_ns = rc_host::wait_timeout_ns();
+  for (int col0 = 0; x->rows > 0 && col0 < k; col0 += p.panel) {
     const rc::f8::Rows r = rows_of(x);
-    a.add = add, a.dw = p.splits > 1 ? work : dw, a.f32 = p.splits > 1 || dw_f32;
-    a.n = n, a.k = k, a.bn = p.bn;
-    a.rows = r.rows, a.chunks = r.chunks;
+    const int cols = std::min(p.panel, k - col0);
+    const int64_t size = dw_f32 ? 4 : 2;
+    a.add = add ? static_cast<const uint8_t*>(add) + col0 * size : nullptr;
+    a.dw = p.splits > 1 ? static_cast<void*>(parts) : static_cast<uint8_t*>(dw) + col0 * size;
+    a.ld = k, a.f32 = p.splits > 1 || dw_f32;
+    a.n = n, a.k = cols, a.bn = p.bn;
     a.stages = p.stages, a.splits = p.splits, a.per_split = p.per_split;
-    a.tiles = {static_cast<int32_t>(p.tiles_m), static_cast<int32_t>(p.tiles_n)};
-    a.guard.timeout_ns = rc_host::wait_timeout_ns();
+    a.tiles = {static_cast<int32_t>(ceil_div(n, p.bn)), static_cast<int32_t>(ceil_div(cols, 256))};
     rc::f8::WgradMaps maps;
     if ((rc = rc_host::encode_map(&maps.dy, dy, 2 * static_cast<int64_t>(n), r.rows, 2 * ld_dy, 64)) != 0 ||
-        (rc = rc_host::encode_map(&maps.codes, r.codes, k, r.rows, k, 64)) != 0 || (rc = tiles_map(&maps.tiles, r)) != 0)
+        (rc = rc_host::encode_map(&maps.x, work, 2 * static_cast<int64_t>(cols), r.rows, 2 * static_cast<int64_t>(cols), 64)) != 0)
       return rc;
-    a.guard.stop = rc_host::take_debug_stop();
-    const unsigned clusters = static_cast<unsigned>(std::min<int64_t>(p.tiles_m * p.tiles_n * p.splits, pairs));
+    const int64_t strips = r.rows * (cols / 16);
+    e = launch_dependent(rc::f8::f8_values_kernel, dim3(static_cast<unsigned>(std::min<int64_t>((strips + 255) / 256, 16ll * sms))),
+                         dim3(rc::f8::kRowsThreads), 0, s, r, col0, cols, static_cast<uint16_t*>(work));
+    if (e != cudaSuccess) return cuda_fail(e, "f8_values_kernel launch");
+    const unsigned clusters = static_cast<unsigned>(std::min<int64_t>(static_cast<int64_t>(a.tiles.m) * a.tiles.n * p.splits, pairs));
     e = launch_dependent(rc::f8::f8_wgrad_kernel, dim3(2 * clusters), dim3(L::kThreads), L::kDynamic, s, maps, a);
     if (e != cudaSuccess) return cuda_fail(e, "f8_wgrad_kernel launch");
   }
   if (x->rows == 0 || p.splits > 1) {
     const int64_t count = static_cast<int64_t>(n) * k;
-    const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(ceil_div(count, 2048), 8ll * sms));
-    e = launch_dependent(rc::f8::f8_wgrad_sum_kernel, dim3(blocks), dim3(256), 0, s, static_cast<const float*>(work), x->rows == 0 ? 0 : p.splits,
+    const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((count + 2047) / 2048, 8ll * sms));
+    e = launch_dependent(rc::f8::f8_wgrad_sum_kernel, dim3(blocks), dim3(256), 0, s, static_cast<const float*>(parts), x->rows == 0 ? 0 : p.splits,
                          count, add, dw, dw_f32);
     if (e != cudaSuccess) return cuda_fail(e, "f8_wgrad_sum_kernel launch");
   }

@@ -265,6 +265,19 @@ def test_weight_grad(r, n, k, dtype):
         assert torch.equal(add, dw)
 
 
+def test_weight_grad_of_large_and_small_scales():
+    """Rows whose scales lie anywhere between 2^-100 and 2^100, beside ordinary ones and alone."""
+    g = gen(31)
+    for spread in ((-100, 100), (8, 100), (-100, -60), (7, 9)):
+        e = torch.randint(spread[0], spread[1], (200, 1), generator=g, device="cuda").float()
+        x = rc.f8_quantize((torch.randn(200, 272, generator=g, device="cuda") * torch.exp2(e)).to(BF16))
+        dy = (torch.randn(200, 144, generator=g, device="cuda") * torch.exp2(-e)).to(BF16)
+        dw = torch.empty(144, 272, device="cuda")
+        rc.f8_weight_grad(dy, x, dw)
+        v = ref.meant(x)
+        check(dw, dy.double().t() @ v, dy.double().abs().t() @ v.abs(), 201, 2.0 ** -24)
+
+
 def test_weight_grad_by_differences():
     """L(w) = sum of dy times (x w^T), in 64 bits, has dw as its slope (it is linear in w: any step will do)."""
     g = gen(77)
