@@ -66,25 +66,68 @@ __device__ __forceinline__ float4 unpack_e4m3x4(uint32_t c) {
 
 // ---------------------------------------------------------------- GELU
 enum Gelu { kErf = 0, kTanh = 1 };
-constexpr float kTanhA = 0.7978845608028654f, kTanhB = 0.044715f;  // sqrt(2 / pi)
 
-// With phi the normal distribution function (or its tanh form, 1 / (1 + exp(-2 z)),
-// z = sqrt(2 / pi) (u + 0.044715 u^3)): gelu(u) = u phi, and its derivative.  (Both forms
-// keep their relative precision far below zero, where 1 + erf and 1 + tanh cancel: a
-// block of nothing but such values has a scale of its own.)
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ f32x2 rcp2(f32x2 x) {
+  float a, b;
+  split_f32x2(x, a, b);
+  return make_f32x2(rcp_approx(a), rcp_approx(b));
+}
+__device__ __forceinline__ f32x2 exp2_2(f32x2 x) {
+  float a, b;
+  split_f32x2(x, a, b);
+  return make_f32x2(ex2_approx(a), ex2_approx(b));
+}
+__device__ __forceinline__ f32x2 abs2(f32x2 x) { return f32x2{x.v & 0x7FFFFFFF7FFFFFFFull}; }
+
+// The normal distribution's tail Q(x), x >= 0: t exp(-x^2 / 2 + P(t)) with t = 1 / (1 + c x),
+// P by a weighted least-squares fit of log2 Q + x^2 / 2 log2 e - log2 t over Chebyshev
+// nodes of t up to x = 14.5 (relative error 2.9e-7, and 2^-23 x^2 by the exponent's
+// rounding).  1 - erf and 1 - tanh lose their relative precision far below zero, where a
+// block of nothing but such values has a scale of its own.
+__device__ __forceinline__ f32x2 normal_tail(f32x2 x) {
+  const f32x2 t = rcp2(fma_f32x2(x, splat2(0.22f), splat2(1.0f)));
+  f32x2 p = fma_f32x2(splat2(0.6040645241737366f), t, splat2(-2.3301138877868652f));
+  p = fma_f32x2(p, t, splat2(3.142305374145508f));
+  p = fma_f32x2(p, t, splat2(-2.0992467403411865f));
+  p = fma_f32x2(p, t, splat2(1.3140716552734375f));
+  p = fma_f32x2(p, t, splat2(0.4040454626083374f));
+  p = fma_f32x2(p, t, splat2(1.4770495891571045f));
+  p = fma_f32x2(p, t, splat2(-3.5121757984161377f));
+  return mul_f32x2(t, exp2_2(fma_f32x2(mul_f32x2(x, x), splat2(-0.72134752f), p)));  // (log2 e / 2)
+}
+// 1 / (1 + exp(-2 z)), z = sqrt(2 / pi) (u + 0.044715 u^3): the same distribution's tanh form.
+constexpr float kTanhA = 1.5957691216057308f, kTanhB = kTanhA * 0.044715f, kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ f32x2 logistic(f32x2 u, f32x2 uu) {
+  const f32x2 z = mul_f32x2(u, fma_f32x2(uu, splat2(-kTanhB * kLog2e), splat2(-kTanhA * kLog2e)));
+  return rcp2(add_f32x2(exp2_2(z), splat2(1.0f)));
+}
+// gelu(u) = u phi(u)
 template <int kForm>
-__device__ __forceinline__ float gelu(float u) {
-  if (kForm == kErf) return 0.5f * u * erfcf(u * -0.7071067811865476f);
-  const float z2 = u * (2.0f * kTanhA + 2.0f * kTanhA * kTanhB * u * u);
-  return __fdividef(u, 1.0f + __expf(-z2));
+__device__ __forceinline__ f32x2 gelu(f32x2 u) {
+  if (kForm == kTanh) return mul_f32x2(u, logistic(u, mul_f32x2(u, u)));
+  // u phi(u) = max(u, 0) - |u| Q(|u|)
+  float a, b;
+  split_f32x2(u, a, b);
+  const f32x2 x = abs2(u), minus = f32x2{x.v | 0x8000000080000000ull};
+  return fma_f32x2(minus, normal_tail(x), make_f32x2(fmaxf(a, 0.f), fmaxf(b, 0.f)));
 }
 template <int kForm>
-__device__ __forceinline__ float gelu_grad(float u) {
-  if (kForm == kErf)
-    return 0.5f * erfcf(u * -0.7071067811865476f) + u * __expf(-0.5f * u * u) * 0.3989422804014327f;
-  const float z2 = u * (2.0f * kTanhA + 2.0f * kTanhA * kTanhB * u * u);
-  const float p = __fdividef(1.0f, 1.0f + __expf(-z2));
-  return p + u * p * (1.0f - p) * (2.0f * kTanhA + 6.0f * kTanhA * kTanhB * u * u);
+__device__ __forceinline__ f32x2 gelu_grad(f32x2 u) {
+  const f32x2 uu = mul_f32x2(u, u);
+  if (kForm == kTanh) {
+    const f32x2 p = logistic(u, uu), q = fma_f32x2(p, f32x2{p.v ^ 0x8000000080000000ull}, p);  // p (1 - p)
+    return fma_f32x2(mul_f32x2(u, q), fma_f32x2(uu, splat2(3.0f * kTanhB), splat2(kTanhA)), p);
+  }
+  // phi(u) is Q(|u|) where u's sign is set (-0 too), else 1 - Q(|u|); and u times the density
+  float a, b;
+  split_f32x2(u, a, b);
+  const f32x2 phi = add_f32x2(f32x2{normal_tail(abs2(u)).v ^ (~u.v & 0x8000000080000000ull)}, make_f32x2(__float_as_int(a) < 0 ? 0.f : 1.f, __float_as_int(b) < 0 ? 0.f : 1.f));
+  return fma_f32x2(u, mul_f32x2(exp2_2(mul_f32x2(uu, splat2(-0.72134752f))), splat2(0.3989422804f)), phi);
 }
 
 // ---------------------------------------------------------------- what becomes of a product
@@ -126,15 +169,16 @@ __device__ __forceinline__ void finish_row(const Out& o, int64_t row, int col0, 
   }
   if ((kEpi & ~1) == kGelu) {
     if (o.u.codes) quantize_warp(o.u, row, col, in, v, lane);
-    v = make_float4(gelu<kEpi & 1>(v.x), gelu<kEpi & 1>(v.y), gelu<kEpi & 1>(v.z), gelu<kEpi & 1>(v.w));
+    split_f32x2(gelu<kEpi & 1>(make_f32x2(v.x, v.y)), v.x, v.y);
+    split_f32x2(gelu<kEpi & 1>(make_f32x2(v.z, v.w)), v.z, v.w);
     quantize_warp(o.a, row, col, in, v, lane);
     return;
   }
   if (in) {
     const float4 u = unpack_e4m3x4(*reinterpret_cast<const uint32_t*>(o.u.codes + row * o.u.width + col));
     const float s = from_codes(o.u.scales[row * o.u.pitch + col / kBlock]);
-    v.x *= gelu_grad<kEpi & 1>(u.x * s), v.y *= gelu_grad<kEpi & 1>(u.y * s);
-    v.z *= gelu_grad<kEpi & 1>(u.z * s), v.w *= gelu_grad<kEpi & 1>(u.w * s);
+    split_f32x2(mul_f32x2(make_f32x2(v.x, v.y), gelu_grad<kEpi & 1>(make_f32x2(u.x * s, u.y * s))), v.x, v.y);
+    split_f32x2(mul_f32x2(make_f32x2(v.z, v.w), gelu_grad<kEpi & 1>(make_f32x2(u.z * s, u.w * s))), v.z, v.w);
     if (o.y) *reinterpret_cast<uint2*>(o.y + row * o.ld + col) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
   }
   if (o.a.codes) quantize_warp(o.a, row, col, in, v, lane);

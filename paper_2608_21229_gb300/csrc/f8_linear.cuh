@@ -36,78 +36,96 @@ struct LinearSmem {
   static constexpr int kSlots = 6, kSlots2 = 4;  // stages, scales
   static constexpr bool kOwn2 = false;
   static constexpr uint32_t kA = 16384, kSlot = 2 * kA, kScaleSlot = 3 * 512;
-  static constexpr uint32_t kScales = kSlots * kSlot, kBars = kScales + kSlots2 * kScaleSlot;
+  static constexpr uint32_t kScales = kSlots * kSlot, kBias = kScales + kSlots2 * kScaleSlot, kBars = kBias + 8 * 512;
   static constexpr int kFull = 0, kEmpty = kFull + kSlots, kFull2 = kEmpty + kSlots, kEmpty2 = kFull2 + kSlots2, kAccFull = kEmpty2 + kSlots2,
                        kAccEmpty = kAccFull + 2, kDone = kAccEmpty + 2, kNumBars = kDone + 1;
   static constexpr uint32_t kAux = kBars + 8 * kNumBars, kUsed = kAux + 28, kDynamic = kUsed + 1024;
-  static constexpr int kProducer = 8, kProducer2 = kProducer, kMma = 9, kThreads = 32 * 10;  // warps 0-7: sums
+  static constexpr int kProducer = 8, kProducer2 = kProducer, kMma = 9, kThreads = 32 * 12;  // warps 0-7: sums; 10, 11: none
+  static constexpr int kSumRegs = 208, kOtherRegs = 80;  // of 168 at launch
+  static_assert(256 * kSumRegs + 128 * kOtherRegs <= kThreads * 168, "more registers than the block has");
   static constexpr uint32_t kTmemScales = 256;                       // 16 columns a slot: four of x's words, eight of w's
   static_assert(kDynamic <= kMaxDynamic, "shared-memory layout too large");
   __device__ static constexpr uint32_t arrivals(int i) { return i >= kAccEmpty && i < kDone ? 8 : 1; }  // four warps of each CTA
 };
 
-// One row's block of 128 columns in a thread, `cols` of them there (a multiple of 16).
-__device__ __forceinline__ void quantize_row(const Rows& r, int64_t row, int col0, int cols, const float (&v)[128]) {
-  uint32_t m = 0;
+// One row's block of 128 columns, in a thread as 64 pairs.  Of a block that the width cuts, the columns
+// behind its end (where `cols`, a multiple of 16, are there) are zero, as their weights are.
+__device__ __forceinline__ void load_block(uint32_t t, int cols, f32x2 (&v)[64]) {
 #pragma unroll
-  for (int i = 0; i < 128; ++i) m = (i & ~15) < cols ? max(m, abs_bits(v[i])) : m;
-  const uint32_t b = scale_byte(m);
-  const float s = to_codes(b);
+  for (int i = 0; i < 4; ++i) {
+    if (32 * i >= cols) break;
+    uint32_t r[32];
+    tmem_ld32(t + 32 * i, r);
+    tmem_wait_ld(r);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[16 * i + j] = make_f32x2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+  }
+}
+__device__ __forceinline__ void quantize_block(const Rows& r, int64_t row, int col0, int cols, const f32x2 (&v)[64]) {
+  float m[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 64; ++i) {
+    float a, b;
+    split_f32x2(v[i], a, b);
+    m[i & 1] = fmax3_abs_nan(a, b, m[i & 1]);
+  }
+  const uint32_t b = scale_byte(abs_bits(fmax3_abs_nan(m[0], m[1], 0.f)));
+  const f32x2 s = splat2(to_codes(b));
   uint8_t* to = r.codes + row * r.width + col0;
+  auto four = [&](int i) {
+    float x, y, z, w;
+    split_f32x2(mul_f32x2(v[i], s), x, y);
+    split_f32x2(mul_f32x2(v[i + 1], s), z, w);
+    return pack_e4m3x4(x, y, z, w);
+  };
 #pragma unroll
-  for (int i = 0; i < 128; i += 16)
-    if (i < cols)
-      *reinterpret_cast<uint4*>(to + i) =
-          make_uint4(pack_e4m3x4(v[i] * s, v[i + 1] * s, v[i + 2] * s, v[i + 3] * s), pack_e4m3x4(v[i + 4] * s, v[i + 5] * s, v[i + 6] * s, v[i + 7] * s),
-                     pack_e4m3x4(v[i + 8] * s, v[i + 9] * s, v[i + 10] * s, v[i + 11] * s),
-                     pack_e4m3x4(v[i + 12] * s, v[i + 13] * s, v[i + 14] * s, v[i + 15] * s));
+  for (int i = 0; i < 64; i += 8)
+    if (2 * i < cols) *reinterpret_cast<uint4*>(to + 2 * i) = make_uint4(four(i), four(i + 2), four(i + 4), four(i + 6));
   put_scale(r, row, col0 / kBlock, b);
 }
-__device__ __forceinline__ void store_row(uint16_t* y, int cols, const float (&v)[128]) {
+__device__ __forceinline__ void store_block(uint16_t* y, int cols, const f32x2 (&v)[64]) {
+  auto two = [&](int i) {
+    float a, b;
+    split_f32x2(v[i], a, b);
+    return pack_bf16x2(a, b);
+  };
 #pragma unroll
-  for (int i = 0; i < 128; i += 8)
-    if ((i & ~15) < cols)
-      *reinterpret_cast<uint4*>(y + i) = make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]), pack_bf16x2(v[i + 4], v[i + 5]),
-                                                    pack_bf16x2(v[i + 6], v[i + 7]));
+  for (int i = 0; i < 64; i += 4)
+    if (2 * (i & ~7) < cols) *reinterpret_cast<uint4*>(y + 2 * i) = make_uint4(two(i), two(i + 1), two(i + 2), two(i + 3));
 }
+// bias: shared memory, 128 floats; u: the codes of the GELU's argument.
 template <int kEpi>
-__device__ __forceinline__ void finish_block(const Out& o, int64_t row, int col0, int cols, float (&v)[128], const uint4 (&u)[8]) {
-  if (o.bias) {
+__device__ __forceinline__ void finish_block(const Out& o, int64_t row, int col0, int cols, f32x2 (&v)[64], uint32_t bias, const uint4 (&u)[8], float u_scale) {
+  if (kEpi < kGeluGrad && o.bias) {
 #pragma unroll
-    for (int i = 0; i < 128; i += 8)
-      if ((i & ~15) < cols) {
-        if (reinterpret_cast<uintptr_t>(o.bias) % 16) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[i + j] += bias_at(o, col0 + i + j);
-        } else {
-          const Vec8 b = load_param8(o.bias, col0 + i, o.bias_f32 != 0);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[i + j] += b.v[j];
-        }
-      }
+    for (int i = 0; i < 32; ++i) {
+      const float4 b = ld_shared_f4(bias + 16u * i);
+      v[2 * i] = add_f32x2(v[2 * i], make_f32x2(b.x, b.y));
+      v[2 * i + 1] = add_f32x2(v[2 * i + 1], make_f32x2(b.z, b.w));
+    }
   }
-  if (kEpi == kStore) store_row(o.y + row * o.ld + col0, cols, v);
+  if (kEpi == kStore) store_block(o.y + row * o.ld + col0, cols, v);
   if ((kEpi & ~1) == kGelu) {
-    if (o.u.codes) quantize_row(o.u, row, col0, cols, v);
+    if (o.u.codes) quantize_block(o.u, row, col0, cols, v);
 #pragma unroll
-    for (int i = 0; i < 128; ++i) v[i] = gelu<kEpi & 1>(v[i]);
-    quantize_row(o.a, row, col0, cols, v);
+    for (int i = 0; i < 64; ++i) v[i] = gelu<kEpi & 1>(v[i]);
+    quantize_block(o.a, row, col0, cols, v);
   }
   if ((kEpi & ~1) == kGeluGrad) {
-    const float s = from_codes(o.u.scales[row * o.u.pitch + col0 / kBlock]);
+    const f32x2 s = splat2(u_scale);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint32_t w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float4 x = unpack_e4m3x4(w[j]);
-        float* p = v + 16 * i + 4 * j;
-        p[0] *= gelu_grad<kEpi & 1>(x.x * s), p[1] *= gelu_grad<kEpi & 1>(x.y * s);
-        p[2] *= gelu_grad<kEpi & 1>(x.z * s), p[3] *= gelu_grad<kEpi & 1>(x.w * s);
+        f32x2* p = v + 8 * i + 2 * j;
+        p[0] = mul_f32x2(p[0], gelu_grad<kEpi & 1>(mul_f32x2(make_f32x2(x.x, x.y), s)));
+        p[1] = mul_f32x2(p[1], gelu_grad<kEpi & 1>(mul_f32x2(make_f32x2(x.z, x.w), s)));
       }
     }
-    if (o.y) store_row(o.y + row * o.ld + col0, cols, v);
-    if (o.a.codes) quantize_row(o.a, row, col0, cols, v);
+    if (o.y) store_block(o.y + row * o.ld + col0, cols, v);
+    if (o.a.codes) quantize_block(o.a, row, col0, cols, v);
   }
 }
 
@@ -124,100 +142,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
   const uint32_t cta_bytes = L::kA + static_cast<uint32_t>(a.bn) * 64u;
   const uint32_t scale_bytes = 512u * (1 + (a.bn + 127) / 128);
   int loads = 0, loads2 = 0;
-  if (c.warp == L::kProducer) {
-    if (c.lane == 0) {
-      const int most = loads_before_stop(a.guard.stop, c.rank);
-      bool ok = true;
-#pragma unroll 1
-      for (int t = cluster; ok && t < n_tiles; t += n_clusters) {
-        int i, j;
-        a.tiles.at(t, &i, &j);
-        const int y = i * 256 + 128 * static_cast<int>(c.rank), z = j * a.bn + a.bn / 2 * static_cast<int>(c.rank);
-#pragma unroll 1
-        for (int kb = 0; ok && kb < blocks; ++kb) {
-          if ((kb & 3) == 0) {
-            const int s = loads2 % L::kSlots2, n = loads2 / L::kSlots2;
-            ok = n == 0 || c.wait(L::kEmpty2 + s, n - 1, 102);
-            if (!ok) break;
-            const uint32_t at = c.base + L::kScales + static_cast<uint32_t>(s) * L::kScaleSlot, full = c.lbar(L::kFull2 + s);
-            const int g = kb >> 2, chunk = j * a.bn / kBlock;
-            if (c.leader) mbar_arrive_expect_tx(c.bar(L::kFull2 + s), 2 * scale_bytes);
-            tma_load_2d_pair(at, &maps.x_tiles, full, 0, g * a.x_chunks + y / 128);
-            tma_load_2d_pair(at + 512, &maps.w_tiles, full, 0, g * a.w_chunks + chunk);
-            if (wide) tma_load_2d_pair(at + 1024, &maps.w_tiles, full, 0, g * a.w_chunks + chunk + 1);
-            ++loads2;
-          }
-          const int s = loads % L::kSlots, n = loads / L::kSlots;
-          ok = loads != most && (n == 0 || c.wait(L::kEmpty + s, n - 1, 101));
-          if (!ok) break;
-          const uint32_t at = c.base + static_cast<uint32_t>(s) * L::kSlot, full = c.lbar(L::kFull + s);
-          if (c.leader) mbar_arrive_expect_tx(c.bar(L::kFull + s), 2 * cta_bytes);
-          tma_load_2d_pair(at, &maps.x, full, kb * kBlock, y);
-          tma_load_2d_pair(at + L::kA, &maps.w, full, kb * kBlock, z);
-          ++loads;
-        }
-      }
-    }
-    __syncwarp();
-  } else if (c.warp == L::kMma) {
-    if (c.leader) {
-      const uint64_t ad = sdesc_sw128(c.base, 16, 1024), bd = sdesc_sw128(c.base + L::kA, 16, 1024);
-      const uint64_t sd = scales_desc(c.base + L::kScales);
-      const uint32_t idesc = idesc_mx(256, a.bn);
-      bool issued = false, ok = true;
-      int load = 0, group = 0, used = 0;
-#pragma unroll 1
-      for (int t = cluster; ok && t < n_tiles; t += n_clusters, ++used) {
-        const uint32_t d = c.tmem + (wide ? 0u : 128u * (used & 1));
-        int ti, tj;
-        a.tiles.at(t, &ti, &tj);
-        const uint32_t shift = static_cast<uint32_t>(tj * a.bn % kBlock) / 32u;  // the tile may begin in the middle of a chunk
-        // the half's (both halves') earlier sums are in registers
-        const int before = wide ? used : used >> 1;
-        if (before > 0 && !(wide ? c.wait_all(L::kAccEmpty, before - 1, 103) && c.wait_all(L::kAccEmpty + 1, before - 1, 103)
-                                 : c.wait_all(L::kAccEmpty + (used & 1), before - 1, 103)))
-          break;
-#pragma unroll 1
-        for (int kb = 0; kb < blocks; ++kb, ++load) {
-          const int s = load % L::kSlots, sc = group % L::kSlots2;
-          const uint32_t sfa = c.tmem + L::kTmemScales + 16u * sc, sfb = sfa + 4;
-          if ((kb & 3) == 0) {
-            ok = c.wait_all(L::kFull2 + sc, group / L::kSlots2, 104);
-            if (!ok) break;
-          }
-          ok = c.wait_all(L::kFull + s, load / L::kSlots, 105);
-          if (!ok) break;
-          issued = true;
-          const int steps = min(4, (a.k - kb * kBlock + 31) / 32);
-          const bool last = kb + 1 == blocks;
-          if (elect_one()) {
-            tc_fence_after();
-            if ((kb & 3) == 0) {
-              const uint64_t at = sd + static_cast<uint64_t>(sc) * (L::kScaleSlot >> 4);
-              copy_scales_pair(sfa, at);
-              copy_scales_pair(sfb, at + (512 >> 4));
-              if (wide) copy_scales_pair(sfb + 4, at + (1024 >> 4));
-            }
-            const uint64_t off = static_cast<uint64_t>(s) * (L::kSlot >> 4);
-            const uint32_t id = idesc_byte(idesc, kb & 3);
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-              if (q < steps) mx_mma_pair(d, ad + off + 2 * q, bd + off + 2 * q, id, sfa, sfb + shift, kb > 0 || q > 0 ? 1u : 0u);
-            tc2_commit_mc(c.bar(L::kEmpty + s), 3);
-            if ((kb & 3) == 3 || last) tc2_commit_mc(c.bar(L::kEmpty2 + sc), 3);
-            if (last) {
-              if (wide || !(used & 1)) tc2_commit_mc(c.bar(L::kAccFull), 3);
-              if (wide || (used & 1)) tc2_commit_mc(c.bar(L::kAccFull + 1), 3);
-            }
-          }
-          __syncwarp();
-          if ((kb & 3) == 3 || last) ++group;
-        }
-      }
-      c.finish_mmas(issued);
-    }
-  } else {
+  if (c.warp < L::kProducer) {
+    more_registers<L::kSumRegs>();
     const int half = c.warp >> 2, quarter = c.warp & 3;
+    const uint32_t bias = c.base + L::kBias + 512u * c.warp;
     int used = 0;
 #pragma unroll 1
     for (int t = cluster; t < n_tiles; t += n_clusters, ++used) {
@@ -229,20 +157,125 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
       const int in_tile = wide ? min(128, a.bn - 128 * half) : a.bn, cols = min(in_tile, a.o.width - col0);
       const bool in = row < a.o.rows && cols > 0;
       uint4 u[8] = {};
+      float u_scale = 0.f;
       if ((kEpi & ~1) == kGeluGrad && in) {
         const uint8_t* from = a.o.u.codes + row * a.o.u.width + col0;
 #pragma unroll
         for (int q = 0; q < 8; ++q)
           if (16 * q < cols) u[q] = *reinterpret_cast<const uint4*>(from + 16 * q);
+        u_scale = from_codes(a.o.u.scales[row * a.o.u.pitch + col0 / kBlock]);
+      }
+      if (kEpi < kGeluGrad && a.o.bias) {  // four columns a lane
+        float b[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) b[q] = 4 * c.lane + q < cols ? bias_at(a.o, col0 + 4 * c.lane + q) : 0.f;
+        __syncwarp();  // (the tile before has read its own)
+        st_shared_v4(bias + 16u * c.lane, make_uint4(__float_as_uint(b[0]), __float_as_uint(b[1]), __float_as_uint(b[2]), __float_as_uint(b[3])));
+        __syncwarp();
       }
       if (!c.wait_all(L::kAccFull + half, wide ? used : used >> 1, 106)) break;
       tc_fence_after();
-      float v[128];
-      load_sums(c.tmem + 128u * half + (static_cast<uint32_t>(quarter) << 21), in_tile, v);
+      f32x2 v[64];
+      load_block(c.tmem + 128u * half + (static_cast<uint32_t>(quarter) << 21), in_tile, v);
       tc_fence_before();
       __syncwarp();
       if (c.lane == 0) mbar_arrive_cluster(c.lbar(L::kAccEmpty + half));
-      if (in) finish_block<kEpi>(a.o, row, col0, cols, v, u);
+      if (in) finish_block<kEpi>(a.o, row, col0, cols, v, bias, u, u_scale);
+    }
+  } else {
+    fewer_registers<L::kOtherRegs>();
+    if (c.warp == L::kProducer) {
+      if (c.lane == 0) {
+        const int most = loads_before_stop(a.guard.stop, c.rank);
+        bool ok = true;
+#pragma unroll 1
+        for (int t = cluster; ok && t < n_tiles; t += n_clusters) {
+          int i, j;
+          a.tiles.at(t, &i, &j);
+          const int y = i * 256 + 128 * static_cast<int>(c.rank), z = j * a.bn + a.bn / 2 * static_cast<int>(c.rank);
+#pragma unroll 1
+          for (int kb = 0; ok && kb < blocks; ++kb) {
+            if ((kb & 3) == 0) {
+              const int s = loads2 % L::kSlots2, n = loads2 / L::kSlots2;
+              ok = n == 0 || c.wait(L::kEmpty2 + s, n - 1, 102);
+              if (!ok) break;
+              const uint32_t at = c.base + L::kScales + static_cast<uint32_t>(s) * L::kScaleSlot, full = c.lbar(L::kFull2 + s);
+              const int g = kb >> 2, chunk = j * a.bn / kBlock;
+              if (c.leader) mbar_arrive_expect_tx(c.bar(L::kFull2 + s), 2 * scale_bytes);
+              tma_load_2d_pair(at, &maps.x_tiles, full, 0, g * a.x_chunks + y / 128);
+              tma_load_2d_pair(at + 512, &maps.w_tiles, full, 0, g * a.w_chunks + chunk);
+              if (wide) tma_load_2d_pair(at + 1024, &maps.w_tiles, full, 0, g * a.w_chunks + chunk + 1);
+              ++loads2;
+            }
+            const int s = loads % L::kSlots, n = loads / L::kSlots;
+            ok = loads != most && (n == 0 || c.wait(L::kEmpty + s, n - 1, 101));
+            if (!ok) break;
+            const uint32_t at = c.base + static_cast<uint32_t>(s) * L::kSlot, full = c.lbar(L::kFull + s);
+            if (c.leader) mbar_arrive_expect_tx(c.bar(L::kFull + s), 2 * cta_bytes);
+            tma_load_2d_pair(at, &maps.x, full, kb * kBlock, y);
+            tma_load_2d_pair(at + L::kA, &maps.w, full, kb * kBlock, z);
+            ++loads;
+          }
+        }
+      }
+      __syncwarp();
+    } else if (c.warp == L::kMma) {
+      if (c.leader) {
+        const uint64_t ad = sdesc_sw128(c.base, 16, 1024), bd = sdesc_sw128(c.base + L::kA, 16, 1024);
+        const uint64_t sd = scales_desc(c.base + L::kScales);
+        const uint32_t idesc = idesc_mx(256, a.bn);
+        bool issued = false, ok = true;
+        int load = 0, group = 0, used = 0;
+#pragma unroll 1
+        for (int t = cluster; ok && t < n_tiles; t += n_clusters, ++used) {
+          const uint32_t d = c.tmem + (wide ? 0u : 128u * (used & 1));
+          int ti, tj;
+          a.tiles.at(t, &ti, &tj);
+          const uint32_t shift = static_cast<uint32_t>(tj * a.bn % kBlock) / 32u;  // the tile may begin in the middle of a chunk
+          // the half's (both halves') earlier sums are in registers
+          const int before = wide ? used : used >> 1;
+          if (before > 0 && !(wide ? c.wait_all(L::kAccEmpty, before - 1, 103) && c.wait_all(L::kAccEmpty + 1, before - 1, 103)
+                                   : c.wait_all(L::kAccEmpty + (used & 1), before - 1, 103)))
+            break;
+#pragma unroll 1
+          for (int kb = 0; kb < blocks; ++kb, ++load) {
+            const int s = load % L::kSlots, sc = group % L::kSlots2;
+            const uint32_t sfa = c.tmem + L::kTmemScales + 16u * sc, sfb = sfa + 4;
+            if ((kb & 3) == 0) {
+              ok = c.wait_all(L::kFull2 + sc, group / L::kSlots2, 104);
+              if (!ok) break;
+            }
+            ok = c.wait_all(L::kFull + s, load / L::kSlots, 105);
+            if (!ok) break;
+            issued = true;
+            const int steps = min(4, (a.k - kb * kBlock + 31) / 32);
+            const bool last = kb + 1 == blocks;
+            if (elect_one()) {
+              tc_fence_after();
+              if ((kb & 3) == 0) {
+                const uint64_t at = sd + static_cast<uint64_t>(sc) * (L::kScaleSlot >> 4);
+                copy_scales_pair(sfa, at);
+                copy_scales_pair(sfb, at + (512 >> 4));
+                if (wide) copy_scales_pair(sfb + 4, at + (1024 >> 4));
+              }
+              const uint64_t off = static_cast<uint64_t>(s) * (L::kSlot >> 4);
+              const uint32_t id = idesc_byte(idesc, kb & 3);
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                if (q < steps) mx_mma_pair(d, ad + off + 2 * q, bd + off + 2 * q, id, sfa, sfb + shift, kb > 0 || q > 0 ? 1u : 0u);
+              tc2_commit_mc(c.bar(L::kEmpty + s), 3);
+              if ((kb & 3) == 3 || last) tc2_commit_mc(c.bar(L::kEmpty2 + sc), 3);
+              if (last) {
+                if (wide || !(used & 1)) tc2_commit_mc(c.bar(L::kAccFull), 3);
+                if (wide || (used & 1)) tc2_commit_mc(c.bar(L::kAccFull + 1), 3);
+              }
+            }
+            __syncwarp();
+            if ((kb & 3) == 3 || last) ++group;
+          }
+        }
+        c.finish_mmas(issued);
+      }
     }
   }
   c.leave(loads, cta_bytes, loads2, scale_bytes);

@@ -29,8 +29,8 @@ struct Ctl {
   uint64_t timeout_ns;
 };
 
-// (out of line: the polling loops would be most of the kernels' code)
-__device__ __noinline__ bool wait_more(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, uint64_t timeout_ns, int where) {
+// (not a function of its own: ptxas allots no registers beside a call where warpgroups change theirs)
+__device__ __forceinline__ bool wait_more(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, uint64_t timeout_ns, int where) {
   const uint64_t t0 = globaltimer_ns();
   for (;;) {
 #pragma unroll 1
@@ -76,17 +76,15 @@ __device__ __forceinline__ void copy_scales_pair(uint32_t tmem, uint64_t desc) {
   asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
 
-// 128 columns of this thread's lane; those from `cols` on are not there.
-__device__ __forceinline__ void load_sums(uint32_t t, int cols, float (&v)[128]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (32 * i >= cols) break;
-    uint32_t r[32];
-    tmem_ld32(t + 32 * i, r);
-    tmem_wait_ld(r);
-#pragma unroll
-    for (int j = 0; j < 32; ++j) v[32 * i + j] = __uint_as_float(r[j]);
-  }
+// Registers of a warpgroup, all four warps alike: fewer than at launch, or more, of what others gave
+// up.  On a path of its own for each: after a join the compiler would count with the fewest.
+template <int kRegs>
+__device__ __forceinline__ void fewer_registers() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs));
+}
+template <int kRegs>
+__device__ __forceinline__ void more_registers() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs));
 }
 
 // ---------------------------------------------------------------- a CTA of a pair

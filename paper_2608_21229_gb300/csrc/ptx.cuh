@@ -393,6 +393,12 @@ __device__ __forceinline__ float fmax3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
+// max(|a|, |b|, c); NaN where one of them is.
+__device__ __forceinline__ float fmax3_abs_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)), "f"(c));
+  return r;
+}
 
 // Two fp32 lanes in one 64-bit register; each lane of the f32x2 operations
 // below is rounded exactly as the scalar fp32 operation would be.
