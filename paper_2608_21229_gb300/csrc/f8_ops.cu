@@ -1,5 +1,5 @@
 // f8_ops.cu -- the entry points of include/refcache.h for linear layers in 8 bits:
-// rows and weights into their 8-bit form (f8_rows.cuh), products on it (f8_linear.cuh, f8_wgrad.cuh).
+// rows and weights into their 8-bit form (f8_rows.cuh), products on it (f8_linear.cuh, f8_few.cuh, f8_wgrad.cuh).
 // Argument checks and launches; no call allocates memory.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -9,6 +9,7 @@
 #include <cstdint>
 
 #include "refcache.h"
+#include "f8_few.cuh"
 #include "f8_linear.cuh"
 #include "f8_rows.cuh"
 #include "f8_wgrad.cuh"
@@ -103,22 +104,90 @@ int pairs_of(Kernel kernel, std::atomic<int>& kept, int threads, uint32_t smem, 
   return REFCACHE_OK;
 }
 
-// Columns of a tile, a multiple of `step`: the fewest cycles by rounds of tiles over the pairs.  A
-// block of 128 columns of x takes a pair 2 bn cycles of MMAs, or (256 + bn) to bring its 16 KB + 64 bn
-// bytes into each CTA's shared memory and read them out at 128 bytes a cycle.
-int tile_columns(int64_t rows, int width, int blocks, int pairs, int step) {
-  int best = step;
+// How a product is taken apart: tiles of 256 rows over CTA pairs, `bn` columns each, or (few) the
+// weight streamed by clusters of `splits` CTAs.
+struct LinearPlan {
+  bool few;
+  int bn, splits, per;
+};
+
+// By estimated cycles, whose constants are fitted to calls one behind the other (microseconds, on weights from memory):
+//   rows x out x in       pairs   few, splits 1 / 2 / 3 / 4 / 8
+//   2 x 24576 x 4096      35.9    21.0 / 25.4 / 23.7 / 26.2 / 38.8
+//   2 x 4096 x 4096       14.4    16.3 /  9.9 /  8.4 /  7.0 /  6.4
+//   64 x 4096 x 16384     37.7    60.1 / 33.6 / 25.7 / 21.1 / 18.1
+//   200 x 2048 x 8192     20.7    35.8 / 22.3 / 19.1 / 16.0 / 14.9
+//   300 x 4096 x 4096     13.2    22.2 / 18.7 / 16.6 / 22.3 / 31.0
+// Pairs: rounds of tiles; a block of 128 columns of x takes a pair 2 bn cycles of MMAs, or (256 + bn) to bring
+// its 16 KB + 64 bn bytes into each CTA's shared memory and read them out at 128 bytes a cycle; a weight of which
+// every tile is read once comes at 1800 bytes a cycle.  Few: the weight at 3300 bytes a cycle, all that the CTAs load at
+// 5500, and a CTA's own loads at 24.
+LinearPlan plan_linear(int64_t rows, int width, int k, int pairs, int sms, int step) {
+  const int64_t blocks = ceil_div(k, 128);
+  LinearPlan best{};
   int64_t least = -1;
   for (int bn = step; bn <= 256; bn += step) {
     const int64_t tiles = static_cast<int64_t>(ceil_div(rows, 256)) * ceil_div(width, bn);
-    const int64_t cost = ((tiles + pairs - 1) / pairs) * (static_cast<int64_t>(blocks) * (256 + bn) + 700);
-    if (least < 0 || cost <= least) least = cost, best = bn;
+    const int64_t cost = 8000 + std::max(((tiles + pairs - 1) / pairs) * (blocks * (256 + bn) + 700), static_cast<int64_t>(width) * k / 1800);
+    if (least < 0 || cost <= least) least = cost, best = {false, bn, 1, 0};
+  }
+  if (rows > 128 * 65535ll || ceil_div(width, 128) > 65535) return best;
+  const int64_t wide = ceil_div(width, 128), tiles = wide * ceil_div(rows, 128);
+  const int64_t bytes = rc::f8::FewSmem::slot_bytes(rc::f8::FewSmem::rows_of_tile(rows));
+  for (int s = 1; s <= 8; ++s) {
+    const int64_t per = (blocks + 4 * s - 1) / (4 * s) * 4;
+    if ((blocks + per - 1) / per != s) continue;
+    const int64_t waves = (tiles * s + 2 * sms - 1) / (2 * sms);
+    const int64_t cost = 6000 + 1700 * waves + std::max({wide * blocks * rc::f8::FewSmem::kA / 3300, tiles * blocks * bytes / 5500, waves * per * bytes / 24});
+    if (cost <= least) least = cost, best = {true, 128, s, static_cast<int>(per)};
   }
   return best;
 }
 
 int tiles_map(CUtensorMap* m, const rc::f8::Rows& r) {
   return rc_host::encode_lines(m, r.tiles, static_cast<int64_t>(r.pitch / 4) * r.chunks);
+}
+
+template <int kEpi>
+int launch_few(const LinearPlan& p, const rc::f8::Rows& x, const rc::f8::Rows& w, const rc::f8::Out& o, int* status, int dev, void* stream) {
+  using L = rc::f8::FewSmem;
+  static std::atomic<bool> set[rc_host::kMaxDevices];
+  if (!set[dev].load()) {
+    const cudaError_t e = cudaFuncSetAttribute(rc::f8::f8_few_kernel<kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynamic);
+    if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(f8_few_kernel)");
+    set[dev].store(true);
+  }
+  rc::f8::FewArgs a{};
+  a.o = o;
+  a.x_chunks = x.chunks, a.w_chunks = w.chunks;
+  a.k = x.width, a.per = p.per;
+  const int n = L::rows_of_tile(o.rows);
+  a.n = n, a.slots = std::min<int>(L::kMaxSlots, L::kStages / L::slot_bytes(n));
+  a.guard.status = status;
+  a.guard.timeout_ns = rc_host::wait_timeout_ns();
+  rc::f8::LinearMaps maps;
+  int rc;
+  if ((rc = rc_host::encode_map(&maps.x, x.codes, x.width, x.rows, x.width, static_cast<uint32_t>(n))) != 0 ||
+      (rc = rc_host::encode_map(&maps.w, w.codes, w.width, w.rows, w.width, 128)) != 0 ||
+      (rc = tiles_map(&maps.x_tiles, x)) != 0 || (rc = tiles_map(&maps.w_tiles, w)) != 0)
+    return rc;
+  a.guard.stop = rc_host::take_debug_stop();
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(p.splits), ceil_div(o.width, 128), ceil_div(o.rows, 128));
+  cfg.blockDim = dim3(L::kThreads);
+  cfg.dynamicSmemBytes = L::kDynamic;
+  cfg.stream = static_cast<cudaStream_t>(stream);
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(p.splits);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  cudaError_t e = cudaLaunchKernelEx(&cfg, rc::f8::f8_few_kernel<kEpi>, maps, a);
+  if (e == cudaSuccess) e = cudaGetLastError();
+  return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "f8_few_kernel launch");
 }
 
 template <int kEpi>
@@ -132,11 +201,12 @@ int launch_linear(const rc::f8::Rows& x, const rc::f8::Rows& w, const rc::f8::Ou
   if (rc || (rc = rc_host::device_status_word(&dev, &a.guard.status)) != 0 ||
       (rc = pairs_of(rc::f8::f8_linear_kernel<kEpi>, kept[dev], L::kThreads, L::kDynamic, sms, &pairs)) != 0)
     return rc;
-  const int blocks = static_cast<int>(ceil_div(x.width, 128));
+  const LinearPlan p = plan_linear(o.rows, o.width, x.width, pairs, sms, kEpi == rc::f8::kStore ? 64 : 128);
+  if (p.few) return launch_few<kEpi>(p, x, w, o, a.guard.status, dev, stream);
   a.o = o;
   a.x_chunks = x.chunks, a.w_chunks = w.chunks;
   a.k = x.width;
-  a.bn = tile_columns(o.rows, o.width, blocks, pairs, kEpi == rc::f8::kStore ? 64 : 128);
+  a.bn = p.bn;
   const int64_t tiles_m = ceil_div(o.rows, 256), tiles_n = ceil_div(o.width, a.bn);
   if (tiles_m * tiles_n > (1ll << 30)) return fail(REFCACHE_ERR_INVALID_ARG, "too many rows for a width of %d", o.width);
   a.tiles = {static_cast<int32_t>(tiles_m), static_cast<int32_t>(tiles_n)};
