@@ -12,9 +12,11 @@
 // CTA r of a pair holds columns [128 r, 128 r + 128) of x's tile and half of dy's; both
 // lie as they come, columns contiguous (MN-major).  A stage is 64 rows, 32 KB, 512 cycles of
 // MMAs.  Sums: two buffers of 256 columns of tensor memory, lane = column of x, so that each
-// store of a lane joins those of its warp in one line of dw; eight warps write a tile while
-// the MMAs of the next one run.  Where the tiles are few the rows are split and the parts added
-// by another kernel in a fixed order.
+// store of a lane joins those of its warp in one line of dw.  The tensor core cuts off
+// what does not fit when it adds, so that an error grows with the rows (1.7e-6 of dw's norm at
+// 4608); each 1024 rows' sums are therefore added up, rounded to nearest, in the registers of
+// eight warps (4e-7), which write a tile while the MMAs of the next one run.  Where the tiles
+// are few the rows are split and the parts added by another kernel in a fixed order.
 #pragma once
 #include "f8_pair.cuh"
 
@@ -38,6 +40,7 @@ struct WgradMaps {
 
 struct WgradSmem {
   static constexpr int kSlots = 6, kSlots2 = 0;
+  static constexpr int kChunk = 16;  // stages whose sums are taken out together
   static constexpr bool kOwn2 = false;
   static constexpr uint32_t kOperand = 16384, kSlot = 2 * kOperand, kBars = kSlots * kSlot;
   static constexpr int kFull = 0, kFull2 = 0, kEmpty = kFull + kSlots, kAccFull = kEmpty + kSlots, kAccEmpty = kAccFull + 2, kDone = kAccEmpty + 2,
@@ -62,7 +65,7 @@ __device__ __forceinline__ WgradItem wgrad_item(const WgradArgs& a, int item) {
   return t;
 }
 
-// One lane's column of x, 64 rows of dw (the first `rows` of them there), each a line's part with the
+// One lane's column of x, up to 128 rows of dw (the first `rows` of them there), each a line's part with the
 // other lanes'.  What is added comes first, then the sums, then all is stored.
 // (The pointers go from row to row: with the rows' addresses kept for the whole tile the registers spill.)
 template <typename T>
@@ -71,18 +74,18 @@ __device__ __forceinline__ void next_row(T& p, int64_t stride) {
   asm volatile("" : "+l"(p));
 }
 template <typename T>
-__device__ __forceinline__ void load_rows(float (&v)[64], const T* from, int64_t stride, int rows) {
+__device__ __forceinline__ void load_rows(float (&v)[128], const T* from, int64_t stride, int rows) {
 #pragma unroll
-  for (int e = 0; e < 64; ++e) {
+  for (int e = 0; e < 128; ++e) {
     v[e] = 0.f;
     if (e < rows) v[e] = sizeof(T) == 4 ? __uint_as_float(static_cast<uint32_t>(*from)) : __uint_as_float(static_cast<uint32_t>(*from) << 16);
     next_row(from, stride);
   }
 }
 template <typename T>
-__device__ __forceinline__ void store_rows(const float (&v)[64], T* to, int64_t stride, int rows) {
+__device__ __forceinline__ void store_rows(const float (&v)[128], T* to, int64_t stride, int rows) {
 #pragma unroll
-  for (int e = 0; e < 64; ++e) {
+  for (int e = 0; e < 128; ++e) {
     if (e < rows) *to = sizeof(T) == 4 ? static_cast<T>(__float_as_uint(v[e])) : static_cast<T>(pack_bf16x2(v[e], 0.f));
     next_row(to, stride);
   }
@@ -129,76 +132,77 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WgradSmem::kThreads,
       const uint64_t ad = sdesc_sw128(c.base, 8192, 1024), bd = sdesc_sw128(c.base + L::kOperand, 8192, 1024);
       const uint32_t idesc = idesc_bf16_f32(256, a.bn, true) | (1u << 15);  // A MN-major too
       bool issued = false, ok = true;
-      int load = 0, used = 0;
+      int load = 0, used = 0;  // stages, chunks
 #pragma unroll 1
-      for (int item = cluster; ok && item < n_items; item += n_clusters, ++used) {
+      for (int item = cluster; ok && item < n_items; item += n_clusters) {
         const WgradItem t = wgrad_item(a, item);
-        const uint32_t d = c.tmem + 256u * (used & 1);
-        if (used >= 2 && !c.wait_all(L::kAccEmpty + (used & 1), (used >> 1) - 1, 113)) break;
 #pragma unroll 1
-        for (int st = t.first; st < t.last; ++st, ++load) {
+        for (int st = t.first, in_chunk = 0; st < t.last; ++st, ++load) {
           const int s = load % L::kSlots;
-          ok = c.wait_all(L::kFull + s, load / L::kSlots, 114);
+          ok = (in_chunk > 0 || used < 2 || c.wait_all(L::kAccEmpty + (used & 1), (used >> 1) - 1, 113)) && c.wait_all(L::kFull + s, load / L::kSlots, 114);
           if (!ok) break;
           issued = true;
+          const bool end = in_chunk + 1 == L::kChunk || st + 1 == t.last;
           if (elect_one()) {
             tc_fence_after();
+            const uint32_t d = c.tmem + 256u * (used & 1);
             const uint64_t off = static_cast<uint64_t>(s) * (L::kSlot >> 4);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) tc2_mma_ss(d, ad + off + 128 * q, bd + off + 128 * q, idesc, st > t.first || q > 0 ? 1u : 0u);
+            for (int q = 0; q < 4; ++q) tc2_mma_ss(d, ad + off + 128 * q, bd + off + 128 * q, idesc, in_chunk > 0 || q > 0 ? 1u : 0u);
             tc2_commit_mc(c.bar(L::kEmpty + s), 3);
-            if (st + 1 == t.last) tc2_commit_mc(c.bar(L::kAccFull + (used & 1)), 3);
+            if (end) tc2_commit_mc(c.bar(L::kAccFull + (used & 1)), 3);
           }
           __syncwarp();
+          in_chunk = end ? 0 : in_chunk + 1;
+          used += end ? 1 : 0;
         }
       }
       c.finish_mmas(issued);
     }
   } else {
-    const int group = c.warp >> 2, quarter = c.warp & 3;
+    // A warp has half of dw's rows, 128 (or 64) of them, of 32 columns of x.
+    const int group = c.warp >> 2, quarter = c.warp & 3, half = a.bn / 2;
     int used = 0;
     bool ok = true;
 #pragma unroll 1
-    for (int item = cluster; ok && item < n_items; item += n_clusters, ++used) {
+    for (int item = cluster; ok && item < n_items; item += n_clusters) {
       const WgradItem t = wgrad_item(a, item);
       const int col = t.j * 256 + 128 * static_cast<int>(c.rank) + 32 * quarter + c.lane;
-      const bool add = a.add != nullptr && a.splits == 1;
-      const int half = a.bn / 2;  // rows of dw of this warp
-#pragma unroll 1
-      for (int i = 0; i < half; i += 64) {
-        const int row0 = t.i * a.bn + half * group + i, rows = col < a.k ? a.n - row0 : 0;
-        const int64_t at = (a.splits == 1 ? row0 * a.ld : (static_cast<int64_t>(t.part) * a.n + row0) * a.k) + col, ld = a.splits == 1 ? a.ld : a.k;
-        float v[64];
-        if (!add) {
+      const int row0 = t.i * a.bn + half * group, rows = col < a.k ? min(half, a.n - row0) : 0;
+      const int64_t ld = a.splits == 1 ? a.ld : a.k, at = (static_cast<int64_t>(t.part) * (a.splits == 1 ? 0 : a.n) + row0) * ld + col;
+      float v[128];  // (what is to be added first: it is on its way while the MMAs run)
+      if (a.add == nullptr || a.splits > 1) {
 #pragma unroll
-          for (int e = 0; e < 64; ++e) v[e] = 0.f;
-        } else if (a.f32) {
-          load_rows(v, static_cast<const uint32_t*>(a.add) + at, ld, rows);
-        } else {
-          load_rows(v, static_cast<const uint16_t*>(a.add) + at, ld, rows);
-        }
-        if (i == 0) ok = c.wait_all(L::kAccFull + (used & 1), used >> 1, 120);
+        for (int e = 0; e < 128; ++e) v[e] = 0.f;
+      } else if (a.f32) {
+        load_rows(v, static_cast<const uint32_t*>(a.add) + at, ld, rows);
+      } else {
+        load_rows(v, static_cast<const uint16_t*>(a.add) + at, ld, rows);
+      }
+#pragma unroll 1
+      for (int st = t.first; ok && st < t.last; st += L::kChunk, ++used) {
+        ok = c.wait_all(L::kAccFull + (used & 1), used >> 1, 120);
         if (!ok) break;
         tc_fence_after();
-        const uint32_t from = c.tmem + 256u * (used & 1) + static_cast<uint32_t>(half * group + i) + (static_cast<uint32_t>(quarter) << 21);
+        const uint32_t from = c.tmem + 256u * (used & 1) + static_cast<uint32_t>(half * group) + (static_cast<uint32_t>(quarter) << 21);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < 8; ++q) {
+          if (16 * q >= half) break;
           uint32_t r[16];
           tmem_ld16(from + 16 * q, r);
           tmem_wait_ld(r);
 #pragma unroll
           for (int e = 0; e < 16; ++e) v[16 * q + e] += __uint_as_float(r[e]);
         }
-        if (i + 64 == half) {
-          tc_fence_before();
-          __syncwarp();
-          if (c.lane == 0) mbar_arrive_cluster(c.lbar(L::kAccEmpty + (used & 1)));
-        }
-        if (a.f32)
-          store_rows(v, static_cast<uint32_t*>(a.dw) + at, ld, rows);
-        else
-          store_rows(v, static_cast<uint16_t*>(a.dw) + at, ld, rows);
+        tc_fence_before();
+        __syncwarp();
+        if (c.lane == 0) mbar_arrive_cluster(c.lbar(L::kAccEmpty + (used & 1)));
       }
+      if (!ok) break;
+      if (a.f32)
+        store_rows(v, static_cast<uint32_t*>(a.dw) + at, ld, rows);
+      else
+        store_rows(v, static_cast<uint16_t*>(a.dw) + at, ld, rows);
     }
   }
   c.leave(loads, cta_bytes, 0, 0);
