@@ -7,29 +7,50 @@ namespace f8 {
 
 constexpr int kRowsThreads = 256;
 
-// bf16 rows.  A warp takes 256 columns of a row at a time: eight a lane, a block to
-// each half of its lanes.
+// bf16 rows.  A warp takes 1024 columns of a row at a time, four strips of 256: eight
+// columns a lane, a block to each half of its lanes.  Bound by memory: four loads a lane are on
+// their way together, and a group's four scales are stored as one word.
+constexpr int kRowsColumns = 1024;
 __global__ void __launch_bounds__(kRowsThreads) f8_quantize_kernel(const uint16_t* x, int64_t ld, const Rows out) {
   grid_dependency_wait();
   grid_launch_dependents();
-  const int lane = threadIdx.x & 31, strips = (out.width + 255) / 256;
-  const int64_t n = out.rows * strips, step = static_cast<int64_t>(gridDim.x) * (kRowsThreads / 32);
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * (kRowsThreads / 32) + (threadIdx.x >> 5); i < n; i += step) {
-    const int64_t row = i / strips;
-    const int col = static_cast<int>(i - row * strips) * 256 + 8 * lane;
-    const bool in = col < out.width;
-    const Vec8 v = in ? unpack8(ld_stream(x + row * ld + col)) : fill8(0.f);
-    uint32_t m = 0;
+  const int lane = threadIdx.x & 31, parts = (out.width + kRowsColumns - 1) / kRowsColumns;
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * (kRowsThreads / 32) + (threadIdx.x >> 5), step = static_cast<int64_t>(gridDim.x) * (kRowsThreads / 32);
+  const int64_t step_rows = step / parts;
+  const int step_parts = static_cast<int>(step - step_rows * parts);
+  int64_t row = first / parts;
+  int part = static_cast<int>(first - row * parts);
+  for (; row < out.rows; row += step_rows, part += step_parts) {
+    if (part >= parts) part -= parts, ++row;
+    if (row >= out.rows) break;
+    const int col0 = part * kRowsColumns + 8 * lane;
+    const uint16_t* from = x + row * ld + col0;
+    uint4 raw[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v.v[j]));
+    for (int q = 0; q < 4; ++q) raw[q] = col0 + 256 * q < out.width ? ld_stream(from + 256 * q) : make_uint4(0, 0, 0, 0);
+    uint32_t b[4];
 #pragma unroll
-    for (int d = 1; d < 16; d *= 2) m = max(m, __shfl_xor_sync(0xffffffffu, m, d));
-    const uint32_t b = scale_byte(m);
-    const float s = to_codes(b);
-    if (!in) continue;
-    *reinterpret_cast<uint2*>(out.codes + row * out.width + col) =
-        make_uint2(pack_e4m3x4(v.v[0] * s, v.v[1] * s, v.v[2] * s, v.v[3] * s), pack_e4m3x4(v.v[4] * s, v.v[5] * s, v.v[6] * s, v.v[7] * s));
-    if ((lane & 15) == 0) put_scale(out, row, col / kBlock, b);
+    for (int q = 0; q < 4; ++q) {
+      const Vec8 v = unpack8(raw[q]);
+      uint32_t m = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v.v[j]));
+#pragma unroll
+      for (int d = 1; d < 16; d *= 2) m = max(m, __shfl_xor_sync(0xffffffffu, m, d));
+      b[q] = scale_byte(m);
+      const float s = to_codes(b[q]);
+      if (col0 + 256 * q < out.width)
+        *reinterpret_cast<uint2*>(out.codes + row * out.width + col0 + 256 * q) = make_uint2(
+            pack_e4m3x4(v.v[0] * s, v.v[1] * s, v.v[2] * s, v.v[3] * s), pack_e4m3x4(v.v[4] * s, v.v[5] * s, v.v[6] * s, v.v[7] * s));
+    }
+    // lane 0 has the first block of each strip, lane 16 the second; lane 0 stores the first two strips' word, lane 16 the others'
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, lane < 16 ? b[2] | b[3] << 16 : b[0] | b[1] << 16, 16);
+    const uint32_t word = lane < 16 ? b[0] | b[1] << 16 | other << 8 : other | b[2] << 8 | b[3] << 24;
+    const int group = 2 * part + (lane >> 4);
+    if ((lane & 15) == 0 && 4 * group < out.pitch) {
+      *reinterpret_cast<uint32_t*>(out.scales + row * out.pitch + 4 * group) = word;
+      *reinterpret_cast<uint32_t*>(tile_byte(out, row, 4 * group)) = word;
+    }
   }
 }
 
