@@ -272,10 +272,13 @@ int refcache_f8_quantize(const void* x, int64_t ld, const refcache_f8_rows_t* ou
   if ((rc = check_tensor(x, "x")) != 0) return rc;
   int sms = 0;
   if ((rc = device_sms(&sms)) != 0) return rc;
-  const int64_t warps = out->rows * ceil_div(out->width, rc::f8::kRowsColumns);
-  const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((warps + rc::f8::kRowsThreads / 32 - 1) / (rc::f8::kRowsThreads / 32), 8ll * sms));
-  const cudaError_t e = launch_dependent(rc::f8::f8_quantize_kernel, dim3(blocks), dim3(rc::f8::kRowsThreads), 0, static_cast<cudaStream_t>(stream),
-                                         static_cast<const uint16_t*>(x), ld, rows_of(out));
+  const int strips = out->width > 512 ? 4 : out->width > 256 ? 2 : 1;
+  const int64_t warps = (out->rows + 4 / strips - 1) / (4 / strips) * ceil_div(out->width, 256 * strips);
+  const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((warps + rc::f8::kRowsThreads / 32 - 1) / (rc::f8::kRowsThreads / 32), 32ll * sms));
+  auto go = [&](auto kernel) {
+    return launch_dependent(kernel, dim3(blocks), dim3(rc::f8::kRowsThreads), 0, static_cast<cudaStream_t>(stream), static_cast<const uint16_t*>(x), ld, rows_of(out));
+  };
+  const cudaError_t e = strips == 4 ? go(rc::f8::f8_quantize_kernel<4>) : strips == 2 ? go(rc::f8::f8_quantize_kernel<2>) : go(rc::f8::f8_quantize_kernel<1>);
   return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "f8_quantize launch");
 }
 

@@ -83,7 +83,8 @@ def check_tiles(f):
 
 
 # ---------------------------------------------------------------- the 8-bit form
-@pytest.mark.parametrize("r, c", [(1, 16), (1, 4096), (3, 128), (5, 144), (33, 272), (257, 1808), (2, 8208), (1000, 256)])
+@pytest.mark.parametrize("r, c", [(1, 16), (1, 4096), (3, 128), (5, 144), (33, 272), (257, 1808), (2, 8208), (1000, 256),
+                                  (40000, 16), (30001, 272), (10000, 1040), (5, 512), (6, 528)])
 def test_rows_bit_for_bit(r, c):
     g = gen(r * 10007 + c)
     x = uneven(g, r, c)
