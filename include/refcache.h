@@ -657,7 +657,8 @@ REFCACHE_API int refcache_set_kernel(int kernel);
  *
  * In a gradient call, bits 0-7 are the load before which a producer stops (1: it
  * loads nothing), of the queries kernel, or of the keys kernel with bit 8, in the
- * first CTA of each pair, or in the second with bit 9.
+ * first CTA of each pair, or in the second with bit 9.  In an 8-bit product, bits 0-7
+ * and 9 likewise (products of few rows, whose CTAs are no pairs: in each cluster's CTAs of even or odd number).
  */
 REFCACHE_API void refcache_debug_skip_first_load(int on);
 

@@ -823,25 +823,30 @@ def clip_gradients(grads, max_norm, out=None, norm=None, stream=None):
 
 
 # ---------------------------------------------------------------- linear layers in 8 bits
-def _f8_scales(rows, height, width, device):
+def _f8_scales(rows, height, width, device, stream):
     """Memory for the scales of ``height`` rows (``rows`` of scales), their used part as torch's UE8M0, and memory for
     them as the tensor cores take them."""
     groups, blocks = (width + 511) // 512, (width + 127) // 128
-    mem = _torch.empty((rows, 4 * groups), dtype=_torch.uint8, device=device)
-    return mem, mem[:, :blocks].view(_torch.float8_e8m0fnu), _torch.empty((groups, (height + 127) // 128, 512), dtype=_torch.uint8, device=device)
+    mem = _empty((rows, 4 * groups), _torch.uint8, device, stream)
+    return mem, mem[:, :blocks].view(_torch.float8_e8m0fnu), _empty((groups, (height + 127) // 128, 512), _torch.uint8, device, stream)
+
+
+def _f8_device(device):
+    if _torch is None:
+        _use_torch()
+    return _torch.device("cuda", _device()) if device is None else _torch.device(device)
 
 
 class F8Rows:
     """Rows in 8-bit form (refcache_f8_rows_t): ``codes`` [rows, width] float8_e4m3fn, and ``scales`` [rows, blocks of
-    128 columns] float8_e8m0fnu.  A value is its code times its block's scale."""
+    128 columns] float8_e8m0fnu.  A value is its code times its block's scale.  Written by the library's calls; ``stream``:
+    the one on which the first of them runs."""
 
-    def __init__(self, rows, width, device=None):
-        if _torch is None:
-            _use_torch()
-        device = _torch.device("cuda", _device()) if device is None else _torch.device(device)
+    def __init__(self, rows, width, device=None, stream=None):
+        device = _f8_device(device)
         self.rows, self.width = int(rows), int(width)
-        self.codes = _torch.empty((self.rows, self.width), dtype=_torch.float8_e4m3fn, device=device)
-        self._mem, self.scales, self._tiles = _f8_scales(self.rows, self.rows, self.width, device)
+        self.codes = _empty((self.rows, self.width), _torch.float8_e4m3fn, device, stream)
+        self._mem, self.scales, self._tiles = _f8_scales(self.rows, self.rows, self.width, device, stream)
         self.device = self.codes.get_device()
         self.c = _F8Rows(self.rows, self.width, *(t.data_ptr() for t in (self.codes, self._mem, self._tiles)))
         self._ref = ctypes.byref(self.c)
@@ -851,33 +856,25 @@ class F8Weight:
     """A weight [out, in] in 8-bit form, as it lies (``codes``, ``scales``) and transposed (``codes_t``, ``scales_t``), one scale
     for each 128 x 128 (refcache_f8_weight_t)."""
 
-    def __init__(self, out_width, in_width, device=None):
-        if _torch is None:
-            _use_torch()
-        device = _torch.device("cuda", _device()) if device is None else _torch.device(device)
+    def __init__(self, out_width, in_width, device=None, stream=None):
+        device = _f8_device(device)
         self.out_width, self.in_width = n, k = int(out_width), int(in_width)
-        self.codes, self.codes_t = (_torch.empty(s, dtype=_torch.float8_e4m3fn, device=device) for s in ((n, k), (k, n)))
+        self.codes, self.codes_t = (_empty(s, _torch.float8_e4m3fn, device, stream) for s in ((n, k), (k, n)))
         nb, kb = (n + 127) // 128, (k + 127) // 128
-        self._mem, self.scales, self._tiles = _f8_scales(nb, n, k, device)
-        self._mem_t, self.scales_t, self._tiles_t = _f8_scales(kb, k, n, device)
+        self._mem, self.scales, self._tiles = _f8_scales(nb, n, k, device, stream)
+        self._mem_t, self.scales_t, self._tiles_t = _f8_scales(kb, k, n, device, stream)
         self.device = self.codes.get_device()
         self.c = _F8Weight(n, k, *(t.data_ptr() for t in (self.codes, self._mem, self._tiles, self.codes_t, self._mem_t, self._tiles_t)))
         self._ref = ctypes.byref(self.c)
 
 
-def _f8_refs(device, kind, **forms):
-    """References to 8-bit forms (None where there is none) on the call's device."""
-    out = []
-    for name, f in forms.items():
-        if f is None:
-            out.append(None)
-            continue
-        if not isinstance(f, kind):
-            raise ValueError(f"{name}: expected {kind.__name__}, got {type(f).__name__}")
-        if f.device != device:
-            raise _elsewhere(f.codes, device, name)
-        out.append(f._ref)
-    return out
+def _f8_ref(name, f, kind, device):
+    """The reference to an 8-bit form on the call's device."""
+    if type(f) is not kind and not isinstance(f, kind):
+        raise ValueError(f"{name}: expected {kind.__name__}, got {type(f).__name__}")
+    if f.device != device:
+        raise _elsewhere(f.codes, device, name)
+    return f._ref
 
 
 def _f8_tensor(name, t, rows, width, device):
@@ -901,8 +898,8 @@ def f8_quantize(x, out=None, stream=None):
         raise ValueError(f"x: expected [rows, width], got {tuple(x.shape)}")
     ptr, ld = _f8_tensor("x", x, *x.shape, device)
     if out is None:
-        out = F8Rows(*x.shape)
-    ref, = _f8_refs(device, F8Rows, out=out)
+        out = F8Rows(*x.shape, stream=stream)
+    ref = _f8_ref("out", out, F8Rows, device)
     if (out.rows, out.width) != x.shape:
         raise ValueError(f"out: expected {tuple(x.shape)}, got {(out.rows, out.width)}")
     _check(load().refcache_f8_quantize(ptr, ld, ref, _stream(stream)))
@@ -919,8 +916,8 @@ def f8_quantize_weight(w, out=None, stream=None):
         raise ValueError(f"w: expected bf16 or float32 [out, in], got {w.dtype} {tuple(w.shape)}")
     ptr = _ptr(w, device, "w")
     if out is None:
-        out = F8Weight(*w.shape)
-    ref, = _f8_refs(device, F8Weight, out=out)
+        out = F8Weight(*w.shape, stream=stream)
+    ref = _f8_ref("out", out, F8Weight, device)
     if (out.out_width, out.in_width) != w.shape:
         raise ValueError(f"out: expected {tuple(w.shape)}, got {(out.out_width, out.in_width)}")
     _check(load().refcache_f8_quantize_weight(ptr, 1 if f32 else 0, ref, _stream(stream)))
@@ -933,10 +930,9 @@ def f8_linear(x, weight, y, bias=None, transposed=False, stream=None):
     if _torch is None:
         _use_torch()
     device = _device()
-    rx, = _f8_refs(device, F8Rows, x=x)
-    rw, = _f8_refs(device, F8Weight, weight=weight)
+    rx, rw = _f8_ref("x", x, F8Rows, device), _f8_ref("weight", weight, F8Weight, device)
     width = weight.in_width if transposed else weight.out_width
-    pb, f32 = _param("bias", bias, width, None, device)
+    pb, f32 = (None, False) if bias is None else _param("bias", bias, width, None, device)
     py, ld = _f8_tensor("y", y, x.rows, width, device)
     _check(load().refcache_f8_linear(rx, rw, 1 if transposed else 0, pb, 1 if f32 else 0, py, ld, _stream(stream)))
 
@@ -952,8 +948,8 @@ def f8_linear_gelu(x, weight, a, u8=None, bias=None, form="erf", stream=None):
     if _torch is None:
         _use_torch()
     device = _device()
-    rx, ra, ru = _f8_refs(device, F8Rows, x=x, a=a, u8=u8)
-    rw, = _f8_refs(device, F8Weight, weight=weight)
+    rx, ra, rw = _f8_ref("x", x, F8Rows, device), _f8_ref("a", a, F8Rows, device), _f8_ref("weight", weight, F8Weight, device)
+    ru = None if u8 is None else _f8_ref("u8", u8, F8Rows, device)
     pb, f32 = _param("bias", bias, weight.out_width, None, device)
     _check(load().refcache_f8_linear_gelu(rx, rw, pb, 1 if f32 else 0, _gelu_form(form), ra, ru, _stream(stream)))
 
@@ -964,8 +960,8 @@ def f8_linear_gelu_backward(dy, weight, u8, du=None, du8=None, form="erf", strea
     if _torch is None:
         _use_torch()
     device = _device()
-    rdy, ru, rdu = _f8_refs(device, F8Rows, dy=dy, u8=u8, du8=du8)
-    rw, = _f8_refs(device, F8Weight, weight=weight)
+    rdy, ru, rw = _f8_ref("dy", dy, F8Rows, device), _f8_ref("u8", u8, F8Rows, device), _f8_ref("weight", weight, F8Weight, device)
+    rdu = None if du8 is None else _f8_ref("du8", du8, F8Rows, device)
     pd, ld = (None, 0) if du is None else _f8_tensor("du", du, dy.rows, weight.in_width, device)
     _check(load().refcache_f8_linear_gelu_backward(rdy, rw, _gelu_form(form), ru, pd, ld, rdu, _stream(stream)))
 
@@ -976,19 +972,19 @@ def f8_weight_grad(dy, x, dw, add=None, d_bias=None, stream=None):
     if _torch is None:
         _use_torch()
     device = _device()
-    rx, = _f8_refs(device, F8Rows, x=x)
-    if dw.dim() != 2:
-        raise ValueError(f"dw: expected [out, in], got {tuple(dw.shape)}")
-    n, f32 = dw.shape[0], dw.dtype is _float32
-    if not (f32 or dw.dtype is _bfloat16) or dw.shape[1] != x.width:
-        raise ValueError(f"dw: expected bf16 or float32 [out, {x.width}], got {dw.dtype} {tuple(dw.shape)}")
-    if add is not None and (add.dtype is not dw.dtype or add.shape != dw.shape):
-        raise ValueError(f"add: expected {dw.dtype} {tuple(dw.shape)}, got {add.dtype} {tuple(add.shape)}")
+    rx = _f8_ref("x", x, F8Rows, device)
+    shape, dtype, k = dw.shape, dw.dtype, x.width
+    f32 = dtype is _float32
+    if len(shape) != 2 or shape[1] != k or not (f32 or dtype is _bfloat16):
+        raise ValueError(f"dw: expected bf16 or float32 [out, {k}], got {dtype} {tuple(shape)}")
+    n = shape[0]
+    if add is not None and (add.dtype is not dtype or add.shape != shape):
+        raise ValueError(f"add: expected {dtype} {tuple(shape)}, got {add.dtype} {tuple(add.shape)}")
     if d_bias is not None and (d_bias.dtype is not _float32 or d_bias.shape != (n,)):
         raise ValueError(f"d_bias: expected float32 [{n}], got {d_bias.dtype} {tuple(d_bias.shape)}")
     pdy, ld = _f8_tensor("dy", dy, x.rows, n, device)
     L = load()
-    nbytes = L.refcache_f8_weight_grad_bytes(x.rows, n, x.width)
+    nbytes = L.refcache_f8_weight_grad_bytes(x.rows, n, k)
     work = _work(nbytes, dw, stream) if nbytes else None
     _check(L.refcache_f8_weight_grad(pdy, ld, rx, n, _ptr(add, device, "add"), _ptr(dw, device, "dw"), 1 if f32 else 0,
                                      _ptr(d_bias, device, "d_bias"), None if work is None else work.data_ptr(), _stream(stream)))

@@ -164,7 +164,10 @@ def test_one_orientation_alone():
 SHAPES = [  # rows, n, k
     (1, 16, 16), (1, 4096, 1024), (2, 128, 4096), (3, 2576, 528), (7, 48, 2064), (16, 512, 512), (17, 400, 144), (31, 1040, 272),
     (64, 256, 8208), (65, 272, 1040), (100, 768, 256), (129, 128, 128), (255, 272, 640), (256, 256, 512), (257, 528, 528), (320, 768, 256),
-    (333, 272, 208), (513, 1296, 784), (777, 2064, 400), (1024, 1024, 1024), (2100, 3600, 656)]
+    (333, 272, 208), (513, 1296, 784), (777, 2064, 400), (1024, 1024, 1024), (2100, 3600, 656),
+    (200, 2064, 8208),  # few rows in two tiles, columns split
+    (1777, 8240, 784),  # tiles of 192 columns
+    (1500, 4112, 2064)]  # several rounds of tiles, and of 1024 rows
 
 
 @pytest.mark.parametrize("r, n, k", SHAPES)
@@ -422,6 +425,35 @@ def test_two_streams_at_once():
     for i in range(2):
         for g in got[i]:
             assert all(torch.equal(g[n], want[i][n]) for n in g)
+
+
+def test_results_made_on_another_stream():
+    """A call with a stream allocates what it returns for that stream."""
+    x = randn(gen(8), 300, 272)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    want, w = rc.f8_quantize(x), randn(gen(9), 144, 272)
+    want_w = rc.f8_quantize_weight(w)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        torch.empty(300 * 272, dtype=torch.uint8, device="cuda").fill_(7)  # freed, and perhaps still being written
+        f, fw = rc.f8_quantize(x, stream=s), rc.f8_quantize_weight(w, stream=s)
+        s.synchronize()
+        assert torch.equal(f.codes.view(torch.uint8), want.codes.view(torch.uint8)) and torch.equal(f._mem[:, :3], want._mem[:, :3])
+        assert torch.equal(fw.codes_t.view(torch.uint8), want_w.codes_t.view(torch.uint8))
+
+
+def test_weight_grad_in_panels():
+    """x's values are taken in panels of columns where all of them would need too much memory: 36000 rows of 4096 in two.  Few
+    columns of dy, and every 50th column of dw against 64 bits."""
+    g = gen(41)
+    dy, x = randn(g, 36000, 48), rc.f8_quantize(uneven(g, 36000, 4096))
+    dw, add = torch.empty(48, 4096, device="cuda"), randn(g, 48, 4096, dtype=F32)
+    assert rc.load().refcache_f8_weight_grad_bytes(36000, 48, 4096) < 36000 * 4096 * 2
+    rc.f8_weight_grad(dy, x, dw, add=add)
+    v = x.codes[:, ::50].double() * torch.exp2(x.scales.view(torch.uint8).double() - 127).repeat_interleave(128, 1)[:, ::50]
+    check(dw[:, ::50], dy.double().t() @ v + add[:, ::50].double(), dy.double().abs().t() @ v.abs() + add[:, ::50].double().abs(), 36001, 2.0 ** -24)
+    assert rc.status() == rc.OK
 
 
 def test_binding_refusals():
