@@ -84,22 +84,23 @@ __device__ __forceinline__ f32x2 exp2_2(f32x2 x) {
 }
 __device__ __forceinline__ f32x2 abs2(f32x2 x) { return f32x2{x.v & 0x7FFFFFFF7FFFFFFFull}; }
 
-// The normal distribution's tail Q(x), x >= 0: t exp(-x^2 / 2 + P(t)) with t = 1 / (1 + c x),
-// P by a weighted least-squares fit of log2 Q + x^2 / 2 log2 e - log2 t over Chebyshev
-// nodes of t up to x = 14.5 (relative error 2.9e-7, and 2^-23 x^2 by the exponent's
-// rounding).  1 - erf and 1 - tanh lose their relative precision far below zero, where a
-// block of nothing but such values has a scale of its own.
-__device__ __forceinline__ f32x2 normal_tail(f32x2 x) {
-  const f32x2 t = rcp2(fma_f32x2(x, splat2(0.22f), splat2(1.0f)));
-  f32x2 p = fma_f32x2(splat2(0.6040645241737366f), t, splat2(-2.3301138877868652f));
-  p = fma_f32x2(p, t, splat2(3.142305374145508f));
-  p = fma_f32x2(p, t, splat2(-2.0992467403411865f));
-  p = fma_f32x2(p, t, splat2(1.3140716552734375f));
-  p = fma_f32x2(p, t, splat2(0.4040454626083374f));
-  p = fma_f32x2(p, t, splat2(1.4770495891571045f));
-  p = fma_f32x2(p, t, splat2(-3.5121757984161377f));
-  return mul_f32x2(t, exp2_2(fma_f32x2(mul_f32x2(x, x), splat2(-0.72134752f), p)));  // (log2 e / 2)
+// The normal distribution's tail Q(x), x >= 0, from e = exp(-x^2 / 2): e t R(t) with t =
+// 1 / (1 + 0.3 x).  R by a weighted least-squares fit of Q(x) exp(x^2 / 2) / t over Chebyshev nodes of t up
+// to x = 13.5 (relative error 1.3e-7, to which the exponent's rounding adds 2^-23 x^2).  1 - erf and
+// 1 - tanh lose their relative precision far below zero, where a block of nothing but such
+// values has a scale of its own.
+__device__ __forceinline__ f32x2 normal_tail(f32x2 x, f32x2 e) {
+  const f32x2 t = rcp2(fma_f32x2(x, splat2(0.3f), splat2(1.0f)));
+  f32x2 p = fma_f32x2(splat2(0.03593191131949425f), t, splat2(-0.15827666223049164f));
+  p = fma_f32x2(p, t, splat2(0.2082076519727707f));
+  p = fma_f32x2(p, t, splat2(-0.05539471283555031f));
+  p = fma_f32x2(p, t, splat2(0.1294696182012558f));
+  p = fma_f32x2(p, t, splat2(0.09963738173246384f));
+  p = fma_f32x2(p, t, splat2(0.12079837173223495f));
+  p = fma_f32x2(p, t, splat2(0.11962638795375824f));
+  return mul_f32x2(mul_f32x2(t, e), p);
 }
+__device__ __forceinline__ f32x2 bell(f32x2 uu) { return exp2_2(mul_f32x2(uu, splat2(-0.72134752f))); }  // exp(-u^2 / 2)
 // 1 / (1 + exp(-2 z)), z = sqrt(2 / pi) (u + 0.044715 u^3): the same distribution's tanh form.
 constexpr float kTanhA = 1.5957691216057308f, kTanhB = kTanhA * 0.044715f, kLog2e = 1.4426950408889634f;
 __device__ __forceinline__ f32x2 logistic(f32x2 u, f32x2 uu) {
@@ -114,7 +115,7 @@ __device__ __forceinline__ f32x2 gelu(f32x2 u) {
   float a, b;
   split_f32x2(u, a, b);
   const f32x2 x = abs2(u), minus = f32x2{x.v | 0x8000000080000000ull};
-  return fma_f32x2(minus, normal_tail(x), make_f32x2(fmaxf(a, 0.f), fmaxf(b, 0.f)));
+  return fma_f32x2(minus, normal_tail(x, bell(mul_f32x2(u, u))), make_f32x2(fmaxf(a, 0.f), fmaxf(b, 0.f)));
 }
 template <int kForm>
 __device__ __forceinline__ f32x2 gelu_grad(f32x2 u) {
@@ -126,8 +127,10 @@ __device__ __forceinline__ f32x2 gelu_grad(f32x2 u) {
   // phi(u) is Q(|u|) where u's sign is set (-0 too), else 1 - Q(|u|); and u times the density
   float a, b;
   split_f32x2(u, a, b);
-  const f32x2 phi = add_f32x2(f32x2{normal_tail(abs2(u)).v ^ (~u.v & 0x8000000080000000ull)}, make_f32x2(__float_as_int(a) < 0 ? 0.f : 1.f, __float_as_int(b) < 0 ? 0.f : 1.f));
-  return fma_f32x2(u, mul_f32x2(exp2_2(mul_f32x2(uu, splat2(-0.72134752f))), splat2(0.3989422804f)), phi);
+  const f32x2 e = bell(uu);
+  const f32x2 phi = add_f32x2(f32x2{normal_tail(abs2(u), e).v ^ (~u.v & 0x8000000080000000ull)},
+                              make_f32x2(__float_as_int(a) < 0 ? 0.f : 1.f, __float_as_int(b) < 0 ? 0.f : 1.f));
+  return fma_f32x2(mul_f32x2(u, splat2(0.3989422804f)), e, phi);
 }
 
 // ---------------------------------------------------------------- what becomes of a product

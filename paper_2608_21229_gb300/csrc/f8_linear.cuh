@@ -61,16 +61,26 @@ __device__ __forceinline__ void load_block(uint32_t t, int cols, f32x2 (&v)[64])
     for (int j = 0; j < 16; ++j) v[16 * i + j] = make_f32x2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
   }
 }
-// 32 bytes of a thread's row, the second 16 of them where `both`.  Each lane has a row of its own, and half a
-// sector (32 bytes) at a time is twice the requests to the L2: as one store where rows begin on 32 bytes.
-__device__ __forceinline__ void store32(void* to, uint4 a, uint4 b, bool both, bool aligned) {
-  if (aligned && both) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y),
-                 "r"(b.z), "r"(b.w)
-                 : "memory");
+// The first n of 8 pieces of 16 bytes of a thread's row.  Each lane has a row of its own, and half a sector (32
+// bytes) at a time is twice the requests to the L2: so two pieces at a time where they begin on 32 bytes.
+__device__ __forceinline__ void store_pieces(void* to, const uint4 (&c)[8], int n) {
+  uint4* y = static_cast<uint4*>(to);
+  auto two = [&](int i) {
+    if (i + 1 < n)
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(y + i), "r"(c[i].x), "r"(c[i].y), "r"(c[i].z), "r"(c[i].w),
+                   "r"(c[i + 1].x), "r"(c[i + 1].y), "r"(c[i + 1].z), "r"(c[i + 1].w)
+                   : "memory");
+    else if (i < n)
+      y[i] = c[i];
+  };
+  if ((reinterpret_cast<uintptr_t>(to) & 31u) == 0) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) two(i);
   } else {
-    static_cast<uint4*>(to)[0] = a;
-    if (both) static_cast<uint4*>(to)[1] = b;
+    if (n > 0) y[0] = c[0];
+#pragma unroll
+    for (int i = 1; i < 7; i += 2) two(i);
+    if (n >= 8) y[7] = c[7];
   }
 }
 __device__ __forceinline__ void quantize_block(const Rows& r, int64_t row, int col0, int cols, const f32x2 (&v)[64]) {
@@ -83,30 +93,31 @@ __device__ __forceinline__ void quantize_block(const Rows& r, int64_t row, int c
   }
   const uint32_t b = scale_byte(abs_bits(fmax3_abs_nan(m[0], m[1], 0.f)));
   const f32x2 s = splat2(to_codes(b));
-  uint8_t* to = r.codes + row * r.width + col0;
-  const bool aligned = ((reinterpret_cast<uintptr_t>(r.codes) | static_cast<uintptr_t>(r.width)) & 31u) == 0;
   auto four = [&](int i) {
     float x, y, z, w;
     split_f32x2(mul_f32x2(v[i], s), x, y);
     split_f32x2(mul_f32x2(v[i + 1], s), z, w);
     return pack_e4m3x4(x, y, z, w);
   };
+  uint4 c[8];
 #pragma unroll
-  for (int i = 0; i < 64; i += 16)
-    if (2 * i < cols)
-      store32(to + 2 * i, make_uint4(four(i), four(i + 2), four(i + 4), four(i + 6)), make_uint4(four(i + 8), four(i + 10), four(i + 12), four(i + 14)),
-              2 * i + 16 < cols, aligned);
+  for (int i = 0; i < 8; ++i) c[i] = make_uint4(four(8 * i), four(8 * i + 2), four(8 * i + 4), four(8 * i + 6));
+  store_pieces(r.codes + row * r.width + col0, c, cols / 16);
   put_scale(r, row, col0 / kBlock, b);
 }
-__device__ __forceinline__ void store_block(uint16_t* y, int cols, bool aligned, const f32x2 (&v)[64]) {
+__device__ __forceinline__ void store_block(uint16_t* y, int cols, const f32x2 (&v)[64]) {
   auto two = [&](int i) {
     float a, b;
     split_f32x2(v[i], a, b);
     return pack_bf16x2(a, b);
   };
 #pragma unroll
-  for (int i = 0; i < 64; i += 8)
-    if (2 * i < cols) store32(y + 2 * i, make_uint4(two(i), two(i + 1), two(i + 2), two(i + 3)), make_uint4(two(i + 4), two(i + 5), two(i + 6), two(i + 7)), true, aligned);
+  for (int h = 0; h < 2; ++h) {
+    uint4 c[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = make_uint4(two(32 * h + 4 * i), two(32 * h + 4 * i + 1), two(32 * h + 4 * i + 2), two(32 * h + 4 * i + 3));
+    store_pieces(y + 64 * h, c, cols / 8 - 8 * h);
+  }
 }
 // bias: shared memory, 128 floats; u: the codes of the GELU's argument.
 template <int kEpi>
@@ -119,8 +130,7 @@ __device__ __forceinline__ void finish_block(const Out& o, int64_t row, int col0
       v[2 * i + 1] = add_f32x2(v[2 * i + 1], make_f32x2(b.z, b.w));
     }
   }
-  const bool aligned = ((reinterpret_cast<uintptr_t>(o.y) | static_cast<uintptr_t>(2 * o.ld)) & 31u) == 0;
-  if (kEpi == kStore) store_block(o.y + row * o.ld + col0, cols, aligned, v);
+  if (kEpi == kStore) store_block(o.y + row * o.ld + col0, cols, v);
   if ((kEpi & ~1) == kGelu) {
     if (o.u.codes) quantize_block(o.u, row, col0, cols, v);
 #pragma unroll
@@ -140,7 +150,7 @@ __device__ __forceinline__ void finish_block(const Out& o, int64_t row, int col0
         p[1] = mul_f32x2(p[1], gelu_grad<kEpi & 1>(mul_f32x2(make_f32x2(x.z, x.w), s)));
       }
     }
-    if (o.y) store_block(o.y + row * o.ld + col0, cols, aligned, v);
+    if (o.y) store_block(o.y + row * o.ld + col0, cols, v);
     if (o.a.codes) quantize_block(o.a, row, col0, cols, v);
   }
 }

@@ -210,7 +210,7 @@ def test_linear_gelu(r, n, k, form):
     delta = sums(k + 1) * mag
     near_form(u8, u, delta)
     # the derivative is at most 1.13.  The tail of the normal distribution and the logistic function are off by some units of
-    # fp32 (a fit within 2.9e-7, 2^-22 for each of exp2 and the reciprocal: below 2^-19 together) and by what the rounding of their
+    # fp32 (a fit within 1.3e-7, 2^-22 for each of exp2 and the reciprocal, ten roundings: below 2^-19 together) and by what the rounding of their
     # exponents, u^2 / 2 log2 e or (1.6 |u| + 0.072 |u|^3) log2 e, does: three times 2^-24 of them times ln 2
     g = ref.gelu(u, form).abs()
     near_form(a, ref.gelu(u, form), 1.13 * delta + g * (2.0 ** -19 + 2.0 ** -22 * (u.abs() + u * u + u.abs() ** 3 / 8)) + 2.0 ** -126)
