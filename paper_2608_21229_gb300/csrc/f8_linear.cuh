@@ -34,13 +34,12 @@ struct LinearMaps {
 
 struct LinearSmem {
   static constexpr int kSlots = 6, kSlots2 = 4;  // stages, scales
-  static constexpr bool kOwn2 = false;
   static constexpr uint32_t kA = 16384, kSlot = 2 * kA, kScaleSlot = 3 * 512;
   static constexpr uint32_t kScales = kSlots * kSlot, kBias = kScales + kSlots2 * kScaleSlot, kBars = kBias + 8 * 512;
   static constexpr int kFull = 0, kEmpty = kFull + kSlots, kFull2 = kEmpty + kSlots, kEmpty2 = kFull2 + kSlots2, kAccFull = kEmpty2 + kSlots2,
                        kAccEmpty = kAccFull + 2, kDone = kAccEmpty + 2, kNumBars = kDone + 1;
-  static constexpr uint32_t kAux = kBars + 8 * kNumBars, kUsed = kAux + 28, kDynamic = kUsed + 1024;
-  static constexpr int kProducer = 8, kProducer2 = kProducer, kMma = 9, kThreads = 32 * 12;  // warps 0-7: sums; 10, 11: none
+  static constexpr uint32_t kAux = kBars + 8 * kNumBars, kUsed = kAux + kAuxBytes, kDynamic = kUsed + 1024;
+  static constexpr int kProducer = 8, kMma = 9, kProducer2 = 10, kThreads = 32 * 12;  // warps 0-7: sums; 8: loads of x; 10: of w
   static constexpr int kSumRegs = 208, kOtherRegs = 80;  // of 168 at launch
   static_assert(256 * kSumRegs + 128 * kOtherRegs <= kThreads * 168, "more registers than the block has");
   static constexpr uint32_t kTmemScales = 256;                       // 16 columns a slot: four of x's words, eight of w's
@@ -165,8 +164,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
   const int cluster = static_cast<int>(blockIdx.x >> 1), n_clusters = static_cast<int>(gridDim.x >> 1);
   const int n_tiles = a.tiles.m * a.tiles.n, blocks = (a.k + kBlock - 1) / kBlock;
   const bool wide = a.bn > 128;  // a tile takes both halves
-  const uint32_t cta_bytes = L::kA + static_cast<uint32_t>(a.bn) * 64u;
-  const uint32_t scale_bytes = 512u * (1 + (a.bn + 127) / 128);
+  // of one CTA's load: x, w
+  const uint2 bytes = make_uint2(L::kA, static_cast<uint32_t>(a.bn) * 64u), scale_bytes = make_uint2(512u, 512u * ((a.bn + 127) / 128));
   int loads = 0, loads2 = 0;
   if (c.warp < L::kProducer) {
     more_registers<L::kSumRegs>();
@@ -210,36 +209,40 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
     }
   } else {
     fewer_registers<L::kOtherRegs>();
-    if (c.warp == L::kProducer) {
+    if (c.warp == L::kProducer || c.warp == L::kProducer2) {
       if (c.lane == 0) {
-        const int most = loads_before_stop(a.guard.stop, c.rank);
+        const bool of_x = c.warp == L::kProducer, arms = of_x && c.leader;
+        const int most = of_x ? loads_before_stop(a.guard.stop, c.rank) : 0x7FFFFFFF;
+        const CUtensorMap* map = of_x ? &maps.x : &maps.w;
+        const uint32_t to = c.base + (of_x ? 0u : L::kA);
         bool ok = true;
 #pragma unroll 1
         for (int t = cluster; ok && t < n_tiles; t += n_clusters) {
           int i, j;
           a.tiles.at(t, &i, &j);
-          const int y = i * 256 + 128 * static_cast<int>(c.rank), z = j * a.bn + a.bn / 2 * static_cast<int>(c.rank);
+          const int y = of_x ? i * 256 + 128 * static_cast<int>(c.rank) : j * a.bn + a.bn / 2 * static_cast<int>(c.rank);
 #pragma unroll 1
           for (int kb = 0; ok && kb < blocks; ++kb) {
             if ((kb & 3) == 0) {
-              const int s = loads2 % L::kSlots2, n = loads2 / L::kSlots2;
+              const int s = loads2 % L::kSlots2, n = loads2 / L::kSlots2, g = kb >> 2;
               ok = n == 0 || c.wait(L::kEmpty2 + s, n - 1, 102);
               if (!ok) break;
               const uint32_t at = c.base + L::kScales + static_cast<uint32_t>(s) * L::kScaleSlot, full = c.lbar(L::kFull2 + s);
-              const int g = kb >> 2, chunk = j * a.bn / kBlock;
-              if (c.leader) mbar_arrive_expect_tx(c.bar(L::kFull2 + s), 2 * scale_bytes);
-              tma_load_2d_pair(at, &maps.x_tiles, full, 0, g * a.x_chunks + y / 128);
-              tma_load_2d_pair(at + 512, &maps.w_tiles, full, 0, g * a.w_chunks + chunk);
-              if (wide) tma_load_2d_pair(at + 1024, &maps.w_tiles, full, 0, g * a.w_chunks + chunk + 1);
+              if (arms) mbar_arrive_expect_tx(c.bar(L::kFull2 + s), 2 * (scale_bytes.x + scale_bytes.y));
+              if (of_x) {
+                tma_load_2d_pair(at, &maps.x_tiles, full, 0, g * a.x_chunks + y / 128);
+              } else {
+                const int line = g * a.w_chunks + j * a.bn / kBlock;
+                tma_load_2d_pair(at + 512, &maps.w_tiles, full, 0, line);
+                if (wide) tma_load_2d_pair(at + 1024, &maps.w_tiles, full, 0, line + 1);
+              }
               ++loads2;
             }
             const int s = loads % L::kSlots, n = loads / L::kSlots;
             ok = loads != most && (n == 0 || c.wait(L::kEmpty + s, n - 1, 101));
             if (!ok) break;
-            const uint32_t at = c.base + static_cast<uint32_t>(s) * L::kSlot, full = c.lbar(L::kFull + s);
-            if (c.leader) mbar_arrive_expect_tx(c.bar(L::kFull + s), 2 * cta_bytes);
-            tma_load_2d_pair(at, &maps.x, full, kb * kBlock, y);
-            tma_load_2d_pair(at + L::kA, &maps.w, full, kb * kBlock, z);
+            if (arms) mbar_arrive_expect_tx(c.bar(L::kFull + s), 2 * (bytes.x + bytes.y));
+            tma_load_2d_pair(to + static_cast<uint32_t>(s) * L::kSlot, map, c.lbar(L::kFull + s), kb * kBlock, y);
             ++loads;
           }
         }
@@ -304,7 +307,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
       }
     }
   }
-  c.leave(loads, cta_bytes, loads2, scale_bytes);
+  c.leave(loads, loads2, bytes, scale_bytes);
 }
 
 }  // namespace f8

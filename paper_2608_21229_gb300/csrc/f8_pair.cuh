@@ -89,9 +89,12 @@ __device__ __forceinline__ void more_registers() {
 
 // ---------------------------------------------------------------- a CTA of a pair
 // L: kNumBars, kBars, kAux (abort flag, tensor memory's address, the other CTA's abort
-// flag, both CTAs' loads of the first ring and of the second), kUsed, kDynamic, arrivals(barrier), kDone, the warps
-// kProducer, kProducer2 and kMma, and two rings of loads: their first barriers kFull and kFull2, kSlots and kSlots2;
-// kOwn2: loads of the second complete on the CTA's own barriers.
+// flag, the loads of both CTAs' producers), kUsed, kDynamic, arrivals(barrier), kDone, the warps
+// kProducer, kProducer2 and kMma, and two rings of loads: their first barriers kFull and kFull2, kSlots
+// and kSlots2.  Both producers of both CTAs load into each slot of a ring (getting one load out takes a
+// thread 150 cycles, so that one producer alone was busy for 390 of the 512 cycles that a stage's MMAs
+// run); the first CTA's first one arms the barrier, on which all of them complete.
+constexpr uint32_t kAuxBytes = 12 + 4 * 8;
 template <typename L>
 struct Cta {
   uint32_t base, rank;
@@ -155,15 +158,14 @@ struct Cta {
     __syncwarp();
   }
 
-  // Loads that this CTA's producers issued (lane 0 of each) and a load's bytes of one CTA, by ring.  When
-  // neither CTA gave up, every load was waited for by what read it; else the leader, on
-  // whose barriers both CTAs' loads complete, arms or counts what one half lacks of the
-  // other and waits for the last phase of each (a CTA's own ring needs the wait alone).
-  __device__ __forceinline__ void leave(int loads, uint32_t bytes, int loads2, uint32_t bytes2) const {
-    if (warp == L::kProducer && lane == 0) st_cluster_u32(mapa_shared(base + L::kAux + 12 + 4 * rank, 0), static_cast<uint32_t>(loads));
-    if (warp == L::kProducer2 && lane == 0) {
-      // (a ring of each CTA's own is settled there)
-      st_cluster_u32(mapa_shared(base + L::kAux + 20 + 4 * rank, L::kOwn2 ? rank : 0), static_cast<uint32_t>(loads2));
+  // Loads into each ring that a producer issued (lane 0 of both), and the bytes of a load of the first producer and
+  // of the second, by ring.  When neither CTA gave up, every load was waited for by the MMAs that read it; else
+  // the leader arms or counts what some of the four lack of the others and waits for the last phase of each slot.
+  __device__ __forceinline__ void leave(int loads, int loads2, uint2 bytes, uint2 bytes2) const {
+    if ((warp == L::kProducer || warp == L::kProducer2) && lane == 0) {
+      const uint32_t at = mapa_shared(base + L::kAux + 12 + 16 * rank + (warp == L::kProducer ? 0 : 8), 0);
+      st_cluster_u32(at, static_cast<uint32_t>(loads));
+      st_cluster_u32(at + 4, static_cast<uint32_t>(loads2));
     }
     tc_fence_before();
     __syncthreads();
@@ -175,27 +177,28 @@ struct Cta {
     }
     const volatile int* aux = reinterpret_cast<const volatile int*>(ptr + L::kAux);
     if (aux[0] == 0 && aux[2] == 0) return;
-    if (warp == L::kProducer && lane == 0) {
-      auto settle = [&](int full, int slots, int mine, int theirs, uint32_t cta_bytes) {
+    if (leader && warp == L::kProducer && lane == 0) {
+      auto settle = [&](int full, int slots, int ring, uint2 b) {
 #pragma unroll 1
         for (int slot = 0; slot < slots; ++slot) {
-          auto count = [&](int total) { return (total - slot + slots - 1) / slots; };
-          int m = count(mine);
-          const int t = count(theirs);
-          if (t == m + 1) {
-            mbar_arrive_expect_tx(bar(full + slot), cta_bytes);
-            m = t;
-          } else if (m == t + 1) {
-            mbar_complete_tx(bar(full + slot), cta_bytes);
+          int most = 0, n[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {  // the arming one first
+            n[i] = (aux[3 + 2 * i + ring] - slot + slots - 1) / slots;
+            most = max(most, n[i]);
           }
-          if (m > 0) drain(bar(full + slot), static_cast<uint32_t>(m - 1) & 1u, ctl.timeout_ns);
+          uint32_t there = 0, lacking = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) (n[i] == most ? there : lacking) += i & 1 ? b.y : b.x;
+          if (n[0] < most)
+            mbar_arrive_expect_tx(bar(full + slot), there);
+          else if (lacking)
+            mbar_complete_tx(bar(full + slot), lacking);
+          if (most > 0) drain(bar(full + slot), static_cast<uint32_t>(most - 1) & 1u, ctl.timeout_ns);
         }
       };
-      if (leader) settle(L::kFull, L::kSlots, aux[3], aux[4], bytes);
-      if (L::kOwn2)
-        settle(L::kFull2, L::kSlots2, aux[5 + rank], aux[5 + rank], bytes2);
-      else if (leader)
-        settle(L::kFull2, L::kSlots2, aux[5], aux[6], bytes2);
+      settle(L::kFull, L::kSlots, 0, bytes);
+      settle(L::kFull2, L::kSlots2, 1, bytes2);
     }
     cluster_sync();
   }

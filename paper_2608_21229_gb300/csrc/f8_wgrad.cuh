@@ -41,12 +41,11 @@ struct WgradMaps {
 struct WgradSmem {
   static constexpr int kSlots = 6, kSlots2 = 0;
   static constexpr int kChunk = 16;  // stages whose sums are taken out together
-  static constexpr bool kOwn2 = false;
   static constexpr uint32_t kOperand = 16384, kSlot = 2 * kOperand, kBars = kSlots * kSlot;
   static constexpr int kFull = 0, kFull2 = 0, kEmpty = kFull + kSlots, kAccFull = kEmpty + kSlots, kAccEmpty = kAccFull + 2, kDone = kAccEmpty + 2,
                        kNumBars = kDone + 1;
-  static constexpr uint32_t kAux = kBars + 8 * kNumBars, kUsed = kAux + 28, kDynamic = kUsed + 1024;
-  static constexpr int kProducer = 8, kProducer2 = kProducer, kMma = 9, kThreads = 32 * 10;  // warps 0-7: sums
+  static constexpr uint32_t kAux = kBars + 8 * kNumBars, kUsed = kAux + kAuxBytes, kDynamic = kUsed + 1024;
+  static constexpr int kProducer = 8, kMma = 9, kProducer2 = 10, kThreads = 32 * 11;  // warps 0-7: sums; 8: loads of x; 10: of dy
   static_assert(kDynamic <= kMaxDynamic, "shared-memory layout too large");
   __device__ static constexpr uint32_t arrivals(int i) { return i >= kAccEmpty && i < kDone ? 16 : 1; }  // eight warps of each CTA
 };
@@ -99,28 +98,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WgradSmem::kThreads,
   if (!c.enter(smem_raw, a.guard)) return;
   const int cluster = static_cast<int>(blockIdx.x >> 1), n_clusters = static_cast<int>(gridDim.x >> 1);
   const int n_items = a.tiles.m * a.tiles.n * a.splits;
-  const uint32_t cta_bytes = L::kOperand + static_cast<uint32_t>(a.bn) * 64u;
+  const uint2 bytes = make_uint2(L::kOperand, static_cast<uint32_t>(a.bn) * 64u);  // of one CTA's load: x, dy
   int loads = 0;
-  if (c.warp == L::kProducer) {
+  if (c.warp == L::kProducer || c.warp == L::kProducer2) {
     if (c.lane == 0) {
-      const int most = loads_before_stop(a.guard.stop, c.rank);
+      const bool of_x = c.warp == L::kProducer, arms = of_x && c.leader, two = of_x || a.bn > 128;  // 64 columns a load
+      const int most = of_x ? loads_before_stop(a.guard.stop, c.rank) : 0x7FFFFFFF;
+      const CUtensorMap* map = of_x ? &maps.x : &maps.dy;
+      const uint32_t to = c.base + (of_x ? 0u : L::kOperand);
       bool ok = true;
 #pragma unroll 1
       for (int item = cluster; ok && item < n_items; item += n_clusters) {
         const WgradItem t = wgrad_item(a, item);
         // (the maps count bytes)
-        const int x0 = 2 * (t.j * 256 + 128 * static_cast<int>(c.rank)), y0 = 2 * (t.i * a.bn + a.bn / 2 * static_cast<int>(c.rank));
+        const int x = 2 * (of_x ? t.j * 256 + 128 * static_cast<int>(c.rank) : t.i * a.bn + a.bn / 2 * static_cast<int>(c.rank));
 #pragma unroll 1
         for (int st = t.first; st < t.last; ++st) {
           const int s = loads % L::kSlots, n = loads / L::kSlots;
           ok = loads != most && (n == 0 || c.wait(L::kEmpty + s, n - 1, 111));
           if (!ok) break;
-          const uint32_t to = c.base + static_cast<uint32_t>(s) * L::kSlot, full = c.lbar(L::kFull + s);
-          if (c.leader) mbar_arrive_expect_tx(c.bar(L::kFull + s), 2 * cta_bytes);
-          tma_load_2d_pair(to, &maps.x, full, x0, st * 64);
-          tma_load_2d_pair(to + 8192, &maps.x, full, x0 + 128, st * 64);
-          tma_load_2d_pair(to + L::kOperand, &maps.dy, full, y0, st * 64);
-          if (a.bn > 128) tma_load_2d_pair(to + L::kOperand + 8192, &maps.dy, full, y0 + 128, st * 64);
+          const uint32_t at = to + static_cast<uint32_t>(s) * L::kSlot, full = c.lbar(L::kFull + s);
+          if (arms) mbar_arrive_expect_tx(c.bar(L::kFull + s), 2 * (bytes.x + bytes.y));
+          tma_load_2d_pair(at, map, full, x, st * 64);
+          if (two) tma_load_2d_pair(at + 8192, map, full, x + 128, st * 64);
           ++loads;
         }
       }
@@ -205,7 +205,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WgradSmem::kThreads,
         store_rows(v, static_cast<uint16_t*>(a.dw) + at, ld, rows);
     }
   }
-  c.leave(loads, cta_bytes, 0, 0);
+  c.leave(loads, 0, bytes, make_uint2(0, 0));
 }
 
 // dw = add + the parts, one after the other.
