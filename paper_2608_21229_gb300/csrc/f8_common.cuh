@@ -119,8 +119,12 @@ __device__ __forceinline__ f32x2 gelu(f32x2 u) {
 }
 template <int kForm>
 __device__ __forceinline__ f32x2 gelu_grad(f32x2 u) {
-  const f32x2 uu = mul_f32x2(u, u);
+  f32x2 uu = mul_f32x2(u, u);
   if (kForm == kTanh) {
+    // (bounded: q is zero long before, and zero times infinity would be a NaN)
+    float a, b;
+    split_f32x2(uu, a, b);
+    uu = make_f32x2(fminf(a, 1e4f), fminf(b, 1e4f));
     const f32x2 p = logistic(u, uu), q = fma_f32x2(p, f32x2{p.v ^ 0x8000000080000000ull}, p);  // p (1 - p)
     return fma_f32x2(mul_f32x2(u, q), fma_f32x2(uu, splat2(3.0f * kTanhB), splat2(kTanhA)), p);
   }

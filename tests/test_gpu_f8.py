@@ -324,6 +324,18 @@ def test_gelu_gradient_at_zeros_of_both_signs(form):
     assert (du == 8.0).all()
 
 
+@pytest.mark.parametrize("form", ["erf", "tanh"])
+def test_gelu_gradient_far_from_zero(form):
+    """The gradient is 1 above and 0 below, to the largest values that the 8-bit form holds, whose squares are infinite."""
+    u = torch.empty(6, 128, dtype=BF16, device="cuda")
+    for i, size in enumerate((16.0, 2.0 ** 20, 2.0 ** 63, 2.0 ** 64, 2.0 ** 100, 448 * 2.0 ** 118)):
+        u[i, ::2], u[i, 1::2] = size, -size
+    dy, w = rc.f8_quantize(torch.ones(6, 16, dtype=BF16, device="cuda")), rc.f8_quantize_weight(torch.ones(16, 128, dtype=BF16, device="cuda"))
+    du = torch.empty(6, 128, dtype=BF16, device="cuda")
+    rc.f8_linear_gelu_backward(dy, w, rc.f8_quantize(u), du, form=form)
+    assert (du[:, ::2] == 16.0).all() and (du[:, 1::2].abs() <= 1e-20).all()
+
+
 # ---------------------------------------------------------------- no rows, streams, graphs
 def test_without_rows():
     x, w = rc.F8Rows(0, 64), rc.f8_quantize_weight(randn(gen(1), 32, 64))
