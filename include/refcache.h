@@ -542,15 +542,16 @@ REFCACHE_API int refcache_clip_gradients(int n, const void* const* grads, void* 
  *   - Widths are multiples of 16 up to 2^20, rows up to 2^31 - 513.
  *   - Codes are packed [rows, width], 16-byte aligned; scales are rows of
  *     REFCACHE_F8_PITCH(width) bytes, 16-byte aligned, of which the first
- *     ceil(width / 128) are used and written.
+ *     ceil(width / 128) count.
  *   - tiles, REFCACHE_F8_TILES(rows, width) bytes, 16-byte aligned, hold the same scales once
  *     more, as the tensor cores take them: the four bytes of 512 columns of row r are the word at
  *     512 (g ceil(rows / 128) + r / 128) + 16 (r % 32) + 4 (r / 32 % 4) for the g-th 512
- *     columns (a weight's rows of one block alike).  What belongs to no row or block is not
- *     written, and may hold anything.
+ *     columns.  A weight's block has its byte for all of its 128 rows, those behind the weight's
+ *     last one too.  What else belongs to no row or block may hold anything, before and after a call.
  *   - Products are summed in fp32; results are rounded once.
  *   - bf16 tensors of rows may have ld elements between rows (a multiple of 8).
- *   - Outputs must not overlap inputs or each other (but for dw over add).
+ *   - Outputs, and weight_grad's work, that overlap inputs or each other are refused (but for dw over add; of
+ *     rows that lie apart only the first one is looked at).
  *   - The calls launch kernels only and allocate nothing: they can be captured in a
  *     CUDA graph, after a first call on the device outside the capture, and may overlap
  *     on several streams.  Sums have a fixed order for a given device: the same inputs

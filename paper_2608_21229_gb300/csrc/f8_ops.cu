@@ -85,6 +85,39 @@ rc::f8::Rows rows_of(const refcache_f8_weight_t* w, bool transposed) {
                     : rows_of(w->codes, w->scales, w->tiles, w->out_width, w->in_width);
 }
 
+// Memory that a call reads or writes: outputs lie apart from inputs and from each other.
+struct Spans {
+  struct {
+    uintptr_t first, last;
+  } of[9];
+  int n = 0;
+  Spans& add(const void* p, int64_t bytes) {
+    if (p && bytes > 0) of[n++] = {reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes};
+    return *this;
+  }
+  Spans& add(const rc::f8::Rows& r) { return add(r.codes, r.rows * r.width).add(r.scales, r.rows * r.pitch).add(r.tiles, r.pitch / 4 * 512ll * r.chunks); }
+  Spans& add(const refcache_f8_rows_t* r) { return add(rows_of(r)); }
+  // (a weight has a row of scales for each 128)
+  Spans& add(const refcache_f8_weight_t* w, bool transposed) {
+    rc::f8::Rows r = rows_of(w, transposed);
+    add(r.codes, r.rows * r.width).add(r.tiles, r.pitch / 4 * 512ll * r.chunks);
+    return add(r.scales, static_cast<int64_t>(r.chunks) * r.pitch);
+  }
+  // Of rows that lie apart the first one alone: between them there may be anything.
+  Spans& add_bf16(const void* p, int64_t rows, int64_t width, int64_t ld) { return add(p, rows > 0 ? 2 * width * (ld == width ? rows : 1) : 0); }
+};
+int check_apart(const Spans& out, const Spans& in) {
+  for (int i = 0; i < out.n; ++i) {
+    auto meets = [&](const Spans& o, int n) {
+      for (int j = 0; j < n; ++j)
+        if (out.of[i].first < o.of[j].last && o.of[j].first < out.of[i].last) return true;
+      return false;
+    };
+    if (meets(out, i) || meets(in, in.n)) return fail(REFCACHE_ERR_INVALID_ARG, "an output overlaps an input or another output");
+  }
+  return REFCACHE_OK;
+}
+
 // CTA pairs of a kernel that run at once on the current device; sets its attributes on first use.
 template <typename Kernel>
 int pairs_of(Kernel kernel, std::atomic<int>& kept, int threads, uint32_t smem, int sms, int* pairs) {
@@ -269,7 +302,7 @@ int refcache_f8_quantize(const void* x, int64_t ld, const refcache_f8_rows_t* ou
   int rc = check_rows(out, -1, 0, "out");
   if (rc || (rc = check_ld(ld, out->width, "x")) != 0) return rc;
   if (out->rows == 0) return REFCACHE_OK;
-  if ((rc = check_tensor(x, "x")) != 0) return rc;
+  if ((rc = check_tensor(x, "x")) != 0 || (rc = check_apart(Spans().add(out), Spans().add_bf16(x, out->rows, out->width, ld))) != 0) return rc;
   int sms = 0;
   if ((rc = device_sms(&sms)) != 0) return rc;
   const int strips = out->width > 512 ? 4 : out->width > 256 ? 2 : 1;
@@ -286,6 +319,10 @@ int refcache_f8_quantize_weight(const void* w, int w_f32, const refcache_f8_weig
   const bool both = out && (out->codes_t || out->scales_t || out->tiles_t);
   int rc = check_weight(out, true, both);
   if (rc || (rc = check_tensor(w, "w")) != 0) return rc;
+  Spans outs;
+  outs.add(out, false);
+  if (both) outs.add(out, true);
+  if ((rc = check_apart(outs, Spans().add(w, static_cast<int64_t>(out->out_width) * out->in_width * (w_f32 ? 4 : 2)))) != 0) return rc;
   int sms = 0;
   if ((rc = device_sms(&sms)) != 0) return rc;
   const rc::f8::Rows t = both ? rows_of(out, true) : rc::f8::Rows{};
@@ -303,6 +340,7 @@ int refcache_f8_linear(const refcache_f8_rows_t* x, const refcache_f8_weight_t* 
   const int in = t ? w->out_width : w->in_width, out = t ? w->in_width : w->out_width;
   if ((rc = check_rows(x, -1, in, "x")) != 0 || (rc = check_bias(bias, bias_f32)) != 0 || (rc = check_ld(ld_y, out, "y")) != 0) return rc;
   if (x->rows > 0 && (rc = check_tensor(y, "y")) != 0) return rc;
+  if ((rc = check_apart(Spans().add_bf16(y, x->rows, out, ld_y), Spans().add(x).add(w, t).add(bias, static_cast<int64_t>(out) * (bias_f32 ? 4 : 2)))) != 0) return rc;
   rc::f8::Out o{};
   o.bias = bias, o.bias_f32 = bias_f32, o.width = out, o.rows = x->rows;
   o.y = static_cast<uint16_t*>(y), o.ld = ld_y;
@@ -316,6 +354,7 @@ int refcache_f8_linear_gelu(const refcache_f8_rows_t* x, const refcache_f8_weigh
       (u8 && (rc = check_rows(u8, x->rows, w->out_width, "u8")) != 0) || (rc = check_bias(bias, bias_f32)) != 0)
     return rc;
   if (form != REFCACHE_GELU_ERF && form != REFCACHE_GELU_TANH) return fail(REFCACHE_ERR_INVALID_ARG, "unknown form %d of the GELU", form);
+  if ((rc = check_apart(Spans().add(a).add(u8), Spans().add(x).add(w, false).add(bias, static_cast<int64_t>(w->out_width) * (bias_f32 ? 4 : 2)))) != 0) return rc;
   rc::f8::Out o{};
   o.bias = bias, o.bias_f32 = bias_f32, o.width = w->out_width, o.rows = x->rows;
   o.a = rows_of(a), o.u = rows_of(u8);
@@ -332,6 +371,7 @@ int refcache_f8_linear_gelu_backward(const refcache_f8_rows_t* dy, const refcach
   if (form != REFCACHE_GELU_ERF && form != REFCACHE_GELU_TANH) return fail(REFCACHE_ERR_INVALID_ARG, "unknown form %d of the GELU", form);
   if (!du && !du8) return fail(REFCACHE_ERR_INVALID_ARG, "neither du nor du8 is given");
   if (du && ((rc = check_tensor(du, "du")) != 0 || (rc = check_ld(ld_du, w->in_width, "du")) != 0)) return rc;
+  if ((rc = check_apart(Spans().add_bf16(du, dy->rows, w->in_width, ld_du).add(du8), Spans().add(dy).add(u8).add(w, true))) != 0) return rc;
   rc::f8::Out o{};
   o.width = w->in_width, o.rows = dy->rows;
   o.y = static_cast<uint16_t*>(du), o.ld = ld_du;
@@ -357,6 +397,12 @@ int refcache_f8_weight_grad(const void* dy, int64_t ld_dy, const refcache_f8_row
   const int n = out_width, k = x->width;
   const WgradPlan p = plan_wgrad(x->rows, n, k);
   if (x->rows > 0 && (rc = check_tensor(work, "work")) != 0) return rc;
+  const int64_t dw_bytes = static_cast<int64_t>(n) * k * (dw_f32 ? 4 : 2);
+  Spans outs, ins;
+  outs.add(dw, dw_bytes).add(d_bias, 4ll * n).add(work, x->rows > 0 ? static_cast<int64_t>(p.values_bytes + p.parts_bytes) : 0);
+  ins.add_bf16(dy, x->rows, n, ld_dy).add(x);
+  if (add != dw) ins.add(add, dw_bytes);
+  if ((rc = check_apart(outs, ins)) != 0) return rc;
   static std::atomic<int> kept[rc_host::kMaxDevices];
   rc::f8::WgradArgs a{};
   int sms = 0, dev = 0, pairs = 0;

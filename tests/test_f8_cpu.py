@@ -95,6 +95,48 @@ def test_tensor_refusals(lib):
     assert lib.refcache_f8_quantize_weight(P + 8, 1, weight(), None) == INVALID
 
 
+def at(i):
+    """Addresses that are never read, 16 MB apart."""
+    return 0x1000000 * i
+
+
+def test_overlaps_are_refused(lib):
+    """An output on an input or on another output, wholly or in part, before a device is touched."""
+    q, qw, lin, gelu = lib.refcache_f8_quantize, lib.refcache_f8_quantize_weight, lib.refcache_f8_linear, lib.refcache_f8_linear_gelu
+    back, wg = lib.refcache_f8_linear_gelu_backward, lib.refcache_f8_weight_grad
+
+    def form(i, n=4, width=64, **kw):
+        return rows(n, width, **{**dict(codes=at(i), scales=at(i + 1), tiles=at(i + 2)), **kw})
+
+    def w(i, **kw):
+        return weight(64, 64, **{**dict(codes=at(i), scales=at(i + 1), tiles=at(i + 2), codes_t=at(i + 3), scales_t=at(i + 4), tiles_t=at(i + 5)), **kw})
+
+    def refused(status):
+        assert status == INVALID and "overlap" in rcb.last_error()
+
+    refused(q(at(1), 64, form(1), None))
+    refused(q(at(1) + 240, 64, form(2, codes=at(1)), None))  # codes of 256 bytes
+    refused(q(at(1), 64, form(2, tiles=at(1) + 256), None))
+    refused(q(at(9), 64, form(2, scales=at(2) + 240), None))  # scales in the codes
+    refused(qw(at(1), 1, w(1), None))
+    refused(qw(at(9), 0, w(1, codes_t=at(1) + 4080), None))
+    refused(lin(form(1), w(10), 0, None, 0, at(1), 64, None))
+    refused(lin(form(1), w(10), 0, None, 0, at(12), 64, None))
+    refused(lin(form(1), w(10), 1, None, 0, at(13), 64, None))
+    refused(lin(form(1), w(10), 0, at(20), 0, at(20) + 112, 64, None))
+    refused(gelu(form(1), w(10), None, 0, 0, form(1), None, None))
+    refused(gelu(form(1), w(10), None, 0, 0, form(4), form(4), None))
+    refused(gelu(form(1), w(10), None, 0, 0, form(4), form(6), None))  # a's tiles are u's codes
+    refused(back(form(1), w(10), 0, form(4), at(20), 64, form(4), None))
+    refused(back(form(1), w(10), 0, form(4), at(20), 64, form(1), None))
+    refused(back(form(1), w(10), 0, form(4), at(4), 64, None, None))
+    refused(back(form(1), w(10), 0, form(4), at(20), 64, form(20), None))
+    args = dict(dy=at(1), ld=64, x=form(2), n=64, add=None, dw=at(5), f32=1, db=at(6), work=at(7), s=None)
+    for kw in (dict(dw=at(1)), dict(dw=at(2)), dict(db=at(1) + 508), dict(db=at(5) + 16128), dict(work=at(2)), dict(work=at(5)), dict(add=at(5) + 16),
+               dict(add=at(7))):
+        refused(wg(*{**args, **kw}.values()))
+
+
 def test_calls_without_rows_need_no_tensors(lib):
     """Nothing to do: accepted before a device is asked for."""
     empty = lambda w: rows(0, w, None, None, None)  # noqa: E731
