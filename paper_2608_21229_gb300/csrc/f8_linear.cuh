@@ -24,11 +24,12 @@ struct LinearArgs {
   int32_t k;                   // columns of x
   int32_t bn;                  // columns of a tile: 64, 128, 192 or 256
   Tiles tiles;
+  int32_t n_whole, tail, n_items;  // tiles taken whole; the others in pieces of 64 or 128 columns, of 256; whole tiles and pieces
   Guard guard;
 };
 
 struct LinearMaps {
-  CUtensorMap x, w;                // 128 rows, half a tile's columns; 128 codes
+  CUtensorMap x, w, w_tail;        // 128 rows, half a tile's (a piece's) columns; 128 codes
   CUtensorMap x_tiles, w_tiles;    // 512 bytes
 };
 
@@ -46,6 +47,27 @@ struct LinearSmem {
   static_assert(kDynamic <= kMaxDynamic, "shared-memory layout too large");
   __device__ static constexpr uint32_t arrivals(int i) { return i >= kAccEmpty && i < kDone ? 8 : 1; }  // four warps of each CTA
 };
+
+// A tile, or a piece of one: where whole tiles fill the pairs some times over and leave a few, these are taken
+// in pieces, one for each pair, as its last.  (A piece of 64 columns takes 320 cycles for each 128 columns of x, a
+// tile 512: plan_linear.  240 tiles, 1280 x 4096 times 4096 x 12288: 45.8 -> 42.9 us; 184 tiles in pieces of 128, 1800 x 2048
+// times 2048 x 5872: 28.4 -> 25.4.)
+struct LinearItem {
+  int i, col0, bn;
+};
+__device__ __forceinline__ LinearItem linear_item(const LinearArgs& a, int t) {
+  LinearItem r;
+  int j;
+  if (t < a.n_whole) {
+    a.tiles.at(t, &r.i, &j);
+    r.col0 = j * a.bn, r.bn = a.bn;
+  } else {
+    const int pieces = a.bn / a.tail, p = t - a.n_whole;
+    a.tiles.at(a.n_whole + p / pieces, &r.i, &j);
+    r.col0 = j * a.bn + p % pieces * a.tail, r.bn = a.tail;
+  }
+  return r;
+}
 
 // One row's block of 128 columns, in a thread as 64 pairs.  Of a block that the width cuts, the columns
 // behind its end (where `cols`, a multiple of 16, are there) are zero, as their weights are.
@@ -162,10 +184,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
   Cta<L> c;
   if (!c.enter(smem_raw, a.guard)) return;
   const int cluster = static_cast<int>(blockIdx.x >> 1), n_clusters = static_cast<int>(gridDim.x >> 1);
-  const int n_tiles = a.tiles.m * a.tiles.n, blocks = (a.k + kBlock - 1) / kBlock;
-  const bool wide = a.bn > 128;  // a tile takes both halves
-  // of one CTA's load: x, w
-  const uint2 bytes = make_uint2(L::kA, static_cast<uint32_t>(a.bn) * 64u), scale_bytes = make_uint2(512u, 512u * ((a.bn + 127) / 128));
+  const int n_items = a.n_items, blocks = (a.k + kBlock - 1) / kBlock;
+  const bool wide = a.bn > 128;  // a whole tile takes both halves, and a piece the first
+  auto bytes = [](int bn) { return make_uint2(L::kA, static_cast<uint32_t>(bn) * 64u); };  // of one CTA's load: x, w
+  auto scale_bytes = [](int bn) { return make_uint2(512u, 512u * ((bn + 127) / 128)); };
   int loads = 0, loads2 = 0;
   if (c.warp < L::kProducer) {
     more_registers<L::kSumRegs>();
@@ -173,13 +195,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
     const uint32_t bias = c.base + L::kBias + 512u * c.warp;
     int used = 0;
 #pragma unroll 1
-    for (int t = cluster; t < n_tiles; t += n_clusters, ++used) {
-      if (!wide && (used & 1) != half) continue;
-      int i, j;
-      a.tiles.at(t, &i, &j);
-      const int64_t row = static_cast<int64_t>(i) * 256 + 128 * c.rank + 32 * quarter + c.lane;
-      const int col0 = j * a.bn + (wide ? 128 * half : 0);
-      const int in_tile = wide ? min(128, a.bn - 128 * half) : a.bn, cols = min(in_tile, a.o.width - col0);
+    for (int t = cluster; t < n_items; t += n_clusters, ++used) {
+      const LinearItem item = linear_item(a, t);
+      const int in_tile = min(128, item.bn - (wide ? 128 * half : 0));
+      if (wide ? in_tile <= 0 : (used & 1) != half) continue;
+      const int64_t row = static_cast<int64_t>(item.i) * 256 + 128 * c.rank + 32 * quarter + c.lane;
+      const int col0 = item.col0 + (wide ? 128 * half : 0);
+      const int cols = min(in_tile, a.o.width - col0);
       const bool in = row < a.o.rows && cols > 0;
       uint4 u[8] = {};
       float u_scale = 0.f;
@@ -213,14 +235,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
       if (c.lane == 0) {
         const bool of_x = c.warp == L::kProducer, arms = of_x && c.leader;
         const int most = of_x ? loads_before_stop(a.guard.stop, c.rank) : 0x7FFFFFFF;
-        const CUtensorMap* map = of_x ? &maps.x : &maps.w;
         const uint32_t to = c.base + (of_x ? 0u : L::kA);
         bool ok = true;
 #pragma unroll 1
-        for (int t = cluster; ok && t < n_tiles; t += n_clusters) {
-          int i, j;
-          a.tiles.at(t, &i, &j);
-          const int y = of_x ? i * 256 + 128 * static_cast<int>(c.rank) : j * a.bn + a.bn / 2 * static_cast<int>(c.rank);
+        for (int t = cluster; ok && t < n_items; t += n_clusters) {
+          const LinearItem item = linear_item(a, t);
+          const CUtensorMap* map = of_x ? &maps.x : t < a.n_whole ? &maps.w : &maps.w_tail;
+          const int y = of_x ? item.i * 256 + 128 * static_cast<int>(c.rank) : item.col0 + item.bn / 2 * static_cast<int>(c.rank);
+          const uint2 b = bytes(item.bn), b2 = scale_bytes(item.bn);
 #pragma unroll 1
           for (int kb = 0; ok && kb < blocks; ++kb) {
             if ((kb & 3) == 0) {
@@ -228,20 +250,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
               ok = n == 0 || c.wait(L::kEmpty2 + s, n - 1, 102);
               if (!ok) break;
               const uint32_t at = c.base + L::kScales + static_cast<uint32_t>(s) * L::kScaleSlot, full = c.lbar(L::kFull2 + s);
-              if (arms) mbar_arrive_expect_tx(c.bar(L::kFull2 + s), 2 * (scale_bytes.x + scale_bytes.y));
+              if (arms) mbar_arrive_expect_tx(c.bar(L::kFull2 + s), 2 * (b2.x + b2.y));
               if (of_x) {
                 tma_load_2d_pair(at, &maps.x_tiles, full, 0, g * a.x_chunks + y / 128);
               } else {
-                const int line = g * a.w_chunks + j * a.bn / kBlock;
+                const int line = g * a.w_chunks + item.col0 / kBlock;
                 tma_load_2d_pair(at + 512, &maps.w_tiles, full, 0, line);
-                if (wide) tma_load_2d_pair(at + 1024, &maps.w_tiles, full, 0, line + 1);
+                if (item.bn > 128) tma_load_2d_pair(at + 1024, &maps.w_tiles, full, 0, line + 1);
               }
               ++loads2;
             }
             const int s = loads % L::kSlots, n = loads / L::kSlots;
             ok = loads != most && (n == 0 || c.wait(L::kEmpty + s, n - 1, 101));
             if (!ok) break;
-            if (arms) mbar_arrive_expect_tx(c.bar(L::kFull + s), 2 * (bytes.x + bytes.y));
+            if (arms) mbar_arrive_expect_tx(c.bar(L::kFull + s), 2 * (b.x + b.y));
             tma_load_2d_pair(to + static_cast<uint32_t>(s) * L::kSlot, map, c.lbar(L::kFull + s), kb * kBlock, y);
             ++loads;
           }
@@ -252,20 +274,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
       if (c.leader) {
         const uint64_t ad = sdesc_sw128(c.base, 16, 1024), bd = sdesc_sw128(c.base + L::kA, 16, 1024);
         const uint64_t sd = scales_desc(c.base + L::kScales);
-        const uint32_t idesc = idesc_mx(256, a.bn);
         bool issued = false, ok = true;
         int load = 0, group = 0, used = 0;
 #pragma unroll 1
-        for (int t = cluster; ok && t < n_tiles; t += n_clusters, ++used) {
-          const uint32_t d = c.tmem + (wide ? 0u : 128u * (used & 1));
-          int ti, tj;
-          a.tiles.at(t, &ti, &tj);
-          const uint32_t shift = static_cast<uint32_t>(tj * a.bn % kBlock) / 32u;  // the tile may begin in the middle of a chunk
+        for (int t = cluster; ok && t < n_items; t += n_clusters, ++used) {
+          const LinearItem item = linear_item(a, t);
+          const bool both = item.bn > 128;
+          const int first = wide ? 0 : used & 1;  // half
+          const uint32_t d = c.tmem + 128u * first, idesc = idesc_mx(256, item.bn);
+          const uint32_t shift = static_cast<uint32_t>(item.col0 % kBlock) / 32u;  // it may begin in the middle of a chunk
           // the half's (both halves') earlier sums are in registers
           const int before = wide ? used : used >> 1;
-          if (before > 0 && !(wide ? c.wait_all(L::kAccEmpty, before - 1, 103) && c.wait_all(L::kAccEmpty + 1, before - 1, 103)
-                                   : c.wait_all(L::kAccEmpty + (used & 1), before - 1, 103)))
-            break;
+          if (before > 0 && !(c.wait_all(L::kAccEmpty + first, before - 1, 103) && (!both || c.wait_all(L::kAccEmpty + 1, before - 1, 103)))) break;
 #pragma unroll 1
           for (int kb = 0; kb < blocks; ++kb, ++load) {
             const int s = load % L::kSlots, sc = group % L::kSlots2;
@@ -285,7 +305,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
                 const uint64_t at = sd + static_cast<uint64_t>(sc) * (L::kScaleSlot >> 4);
                 copy_scales_pair(sfa, at);
                 copy_scales_pair(sfb, at + (512 >> 4));
-                if (wide) copy_scales_pair(sfb + 4, at + (1024 >> 4));
+                if (both) copy_scales_pair(sfb + 4, at + (1024 >> 4));
               }
               const uint64_t off = static_cast<uint64_t>(s) * (L::kSlot >> 4);
               const uint32_t id = idesc_byte(idesc, kb & 3);
@@ -295,8 +315,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
               tc2_commit_mc(c.bar(L::kEmpty + s), 3);
               if ((kb & 3) == 3 || last) tc2_commit_mc(c.bar(L::kEmpty2 + sc), 3);
               if (last) {
-                if (wide || !(used & 1)) tc2_commit_mc(c.bar(L::kAccFull), 3);
-                if (wide || (used & 1)) tc2_commit_mc(c.bar(L::kAccFull + 1), 3);
+                tc2_commit_mc(c.bar(L::kAccFull + first), 3);
+                if (both) tc2_commit_mc(c.bar(L::kAccFull + 1), 3);
               }
             }
             __syncwarp();
@@ -307,7 +327,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
       }
     }
   }
-  c.leave(loads, loads2, bytes, scale_bytes);
+  const int whole = cluster < a.n_whole ? (a.n_whole - cluster + n_clusters - 1) / n_clusters : 0;  // tiles of this pair
+  c.leave(Loads{loads, bytes(a.bn), bytes(a.tail), whole * blocks}, Loads{loads2, scale_bytes(a.bn), scale_bytes(a.tail), whole * ((blocks + 3) / 4)});
 }
 
 }  // namespace f8

@@ -138,10 +138,13 @@ int pairs_of(Kernel kernel, std::atomic<int>& kept, int threads, uint32_t smem, 
 }
 
 // How a product is taken apart: tiles of 256 rows over CTA pairs, `bn` columns each, or (few) the
-// weight streamed by clusters of `splits` CTAs.
+// weight streamed by clusters of `splits` CTAs.  Of tiles of 256 columns, those behind the last full round over
+// the pairs may be taken in pieces of `tail` columns (64 or 128), if that makes no second round.
 struct LinearPlan {
   bool few;
-  int bn, splits, per;
+  int bn, tail;
+  int64_t whole, items;  // tiles that are not in pieces; these and the pieces
+  int splits, per;
 };
 
 // By estimated cycles, whose constants are fitted to calls one behind the other (microseconds, on weights from memory):
@@ -160,9 +163,14 @@ LinearPlan plan_linear(int64_t rows, int width, int k, int pairs, int sms, int s
   LinearPlan best{};
   int64_t least = -1;
   for (int bn = step; bn <= 256; bn += step) {
-    const int64_t tiles = static_cast<int64_t>(ceil_div(rows, 256)) * ceil_div(width, bn);
-    const int64_t cost = 8000 + std::max(((tiles + pairs - 1) / pairs) * (blocks * (256 + bn) + 700), static_cast<int64_t>(width) * k / 1800);
-    if (least < 0 || cost <= least) least = cost, best = {false, bn, 1, 0};
+    const int64_t tiles = static_cast<int64_t>(ceil_div(rows, 256)) * ceil_div(width, bn), over = tiles % pairs;
+    for (int tail = bn == 256 && tiles > pairs ? step : bn; tail <= bn; tail *= 2) {
+      if (tail < bn && (over == 0 || over * (bn / tail) > pairs)) continue;
+      const int64_t rounds = tiles / pairs * (blocks * (256 + bn) + 700) + (over ? blocks * (256 + tail) + 700 : 0);
+      const int64_t cost = 8000 + std::max(rounds, static_cast<int64_t>(width) * k / 1800);
+      if (least < 0 || cost < least || (cost == least && tail == bn))
+        least = cost, best = {false, bn, tail, tail < bn ? tiles - over : tiles, tail < bn ? tiles - over + over * (bn / tail) : tiles, 1, 0};
+    }
   }
   if (rows > 128 * 65535ll || ceil_div(width, 128) > 65535) return best;
   const int64_t wide = ceil_div(width, 128), tiles = wide * ceil_div(rows, 128);
@@ -172,7 +180,7 @@ LinearPlan plan_linear(int64_t rows, int width, int k, int pairs, int sms, int s
     if ((blocks + per - 1) / per != s) continue;
     const int64_t waves = (tiles * s + 2 * sms - 1) / (2 * sms);
     const int64_t cost = 6000 + 1700 * waves + std::max({wide * blocks * rc::f8::FewSmem::kA / 3300, tiles * blocks * bytes / 5500, waves * per * bytes / 24});
-    if (cost <= least) least = cost, best = {true, 128, s, static_cast<int>(per)};
+    if (cost <= least) least = cost, best = {true, 128, 128, 0, 0, s, static_cast<int>(per)};
   }
   return best;
 }
@@ -241,16 +249,19 @@ int launch_linear(const rc::f8::Rows& x, const rc::f8::Rows& w, const rc::f8::Ou
   a.k = x.width;
   a.bn = p.bn;
   const int64_t tiles_m = ceil_div(o.rows, 256), tiles_n = ceil_div(o.width, a.bn);
+  a.tail = p.tail;
   if (tiles_m * tiles_n > (1ll << 30)) return fail(REFCACHE_ERR_INVALID_ARG, "too many rows for a width of %d", o.width);
   a.tiles = {static_cast<int32_t>(tiles_m), static_cast<int32_t>(tiles_n)};
+  a.n_whole = static_cast<int32_t>(p.whole), a.n_items = static_cast<int32_t>(p.items);
   a.guard.timeout_ns = rc_host::wait_timeout_ns();
   rc::f8::LinearMaps maps;
   if ((rc = rc_host::encode_map(&maps.x, x.codes, x.width, x.rows, x.width, 128)) != 0 ||
       (rc = rc_host::encode_map(&maps.w, w.codes, w.width, w.rows, w.width, static_cast<uint32_t>(a.bn / 2))) != 0 ||
+      (rc = rc_host::encode_map(&maps.w_tail, w.codes, w.width, w.rows, w.width, static_cast<uint32_t>(a.tail / 2))) != 0 ||
       (rc = tiles_map(&maps.x_tiles, x)) != 0 || (rc = tiles_map(&maps.w_tiles, w)) != 0)
     return rc;
   a.guard.stop = rc_host::take_debug_stop();
-  const unsigned clusters = static_cast<unsigned>(std::min<int64_t>(tiles_m * tiles_n, pairs));
+  const unsigned clusters = static_cast<unsigned>(std::min<int64_t>(p.items, pairs));
   const cudaError_t e = launch_dependent(rc::f8::f8_linear_kernel<kEpi>, dim3(2 * clusters), dim3(L::kThreads), L::kDynamic,
                                          static_cast<cudaStream_t>(stream), maps, a);
   return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "f8_linear_kernel launch");

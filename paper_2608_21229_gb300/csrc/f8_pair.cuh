@@ -95,6 +95,11 @@ __device__ __forceinline__ void more_registers() {
 // thread 150 cycles, so that one producer alone was busy for 390 of the 512 cycles that a stage's MMAs
 // run); the first CTA's first one arms the barrier, on which all of them complete.
 constexpr uint32_t kAuxBytes = 12 + 4 * 8;
+struct Loads {
+  int n;                     // issued
+  uint2 bytes, bytes_last;   // of one, by the first producer and by the second; of the last tile's loads
+  int before_last;           // loads before these
+};
 template <typename L>
 struct Cta {
   uint32_t base, rank;
@@ -158,14 +163,13 @@ struct Cta {
     __syncwarp();
   }
 
-  // Loads into each ring that a producer issued (lane 0 of both), and the bytes of a load of the first producer and
-  // of the second, by ring.  When neither CTA gave up, every load was waited for by the MMAs that read it; else
+  // Of each ring, what a producer (lane 0 of both) loaded.  When neither CTA gave up, every load was waited for by the MMAs that read it; else
   // the leader arms or counts what some of the four lack of the others and waits for the last phase of each slot.
-  __device__ __forceinline__ void leave(int loads, int loads2, uint2 bytes, uint2 bytes2) const {
+  __device__ __forceinline__ void leave(const Loads& loads, const Loads& loads2) const {
     if ((warp == L::kProducer || warp == L::kProducer2) && lane == 0) {
       const uint32_t at = mapa_shared(base + L::kAux + 12 + 16 * rank + (warp == L::kProducer ? 0 : 8), 0);
-      st_cluster_u32(at, static_cast<uint32_t>(loads));
-      st_cluster_u32(at + 4, static_cast<uint32_t>(loads2));
+      st_cluster_u32(at, static_cast<uint32_t>(loads.n));
+      st_cluster_u32(at + 4, static_cast<uint32_t>(loads2.n));
     }
     tc_fence_before();
     __syncthreads();
@@ -178,7 +182,7 @@ struct Cta {
     const volatile int* aux = reinterpret_cast<const volatile int*>(ptr + L::kAux);
     if (aux[0] == 0 && aux[2] == 0) return;
     if (leader && warp == L::kProducer && lane == 0) {
-      auto settle = [&](int full, int slots, int ring, uint2 b) {
+      auto settle = [&](int full, int slots, int ring, const Loads& of) {
 #pragma unroll 1
         for (int slot = 0; slot < slots; ++slot) {
           int most = 0, n[4];
@@ -187,6 +191,7 @@ struct Cta {
             n[i] = (aux[3 + 2 * i + ring] - slot + slots - 1) / slots;
             most = max(most, n[i]);
           }
+          const uint2 b = slot + (most - 1) * slots < of.before_last ? of.bytes : of.bytes_last;
           uint32_t there = 0, lacking = 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i) (n[i] == most ? there : lacking) += i & 1 ? b.y : b.x;
@@ -197,8 +202,8 @@ struct Cta {
           if (most > 0) drain(bar(full + slot), static_cast<uint32_t>(most - 1) & 1u, ctl.timeout_ns);
         }
       };
-      settle(L::kFull, L::kSlots, 0, bytes);
-      settle(L::kFull2, L::kSlots2, 1, bytes2);
+      settle(L::kFull, L::kSlots, 0, loads);
+      settle(L::kFull2, L::kSlots2, 1, loads2);
     }
     cluster_sync();
   }

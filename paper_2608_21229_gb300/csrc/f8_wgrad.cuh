@@ -205,7 +205,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WgradSmem::kThreads,
         store_rows(v, static_cast<uint16_t*>(a.dw) + at, ld, rows);
     }
   }
-  c.leave(loads, 0, bytes, make_uint2(0, 0));
+  c.leave(Loads{loads, bytes, bytes, 0}, Loads{});
 }
 
 // dw = add + the parts, one after the other.

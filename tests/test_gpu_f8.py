@@ -336,6 +336,18 @@ def test_gelu_gradient_far_from_zero(form):
     assert (du[:, ::2] == 16.0).all() and (du[:, 1::2].abs() <= 1e-20).all()
 
 
+# On 76 CTA pairs: 80, 95, 102 and 184 tiles of 256 columns, of which the last 4 and 19 may go in four pieces each, the last 26 and 32 in two.
+PIECES = [(1025, 4096, 1040), (1025, 4848, 528), (1300, 4112, 272), (1801, 5872, 272)]
+
+
+@pytest.mark.parametrize("r, n, k", PIECES)
+def test_tiles_in_pieces(r, n, k):
+    test_linear(r, n, k, False)
+    test_linear(r, k, n, True)
+    test_linear_gelu(r, n, k, "erf")
+    test_linear_gelu_backward(r, k, n, "tanh")
+
+
 # ---------------------------------------------------------------- no rows, streams, graphs
 def test_without_rows():
     x, w = rc.F8Rows(0, 64), rc.f8_quantize_weight(randn(gen(1), 32, 64))

@@ -51,6 +51,18 @@ def gelu():
     return call
 
 
+def pieces():
+    """80 tiles of nine loads each, so that on 76 pairs the last four are shared out in pieces of nine loads."""
+    x, w = rc.f8_quantize(rnd(0, 1025, 1040).to(BF16)), rc.f8_quantize_weight(rnd(1, 4096, 1040))
+
+    def call():
+        y = torch.empty(1025, 4096, dtype=BF16, device="cuda")
+        rc.f8_linear(x, w, y)
+        return y
+
+    return call
+
+
 def weight_grad():
     x, dy = rc.f8_quantize(rnd(0, 1300, 2064).to(BF16)), rnd(1, 1300, 4112).to(BF16)
 
@@ -64,12 +76,19 @@ def weight_grad():
 
 @pytest.mark.parametrize("make", [linear, few, gelu, weight_grad], ids=lambda f: f.__name__)
 def test_wait_timeouts_are_reported_and_the_context_survives(make):
-    call = make()
+    check_timeouts(make(), (1, 2, 3, 5, 6, 7, 8))
+
+
+def test_wait_timeouts_in_pieces_of_tiles():
+    check_timeouts(pieces(), (9, 10, 11, 12, 13, 14, 16, 18))
+
+
+def check_timeouts(call, loads):
     want = call()
     torch.cuda.synchronize()
     assert rc.status() == rc.OK
     for second in (0, SECOND):
-        for load in (1, 2, 3, 5, 6, 7, 8):
+        for load in loads:
             old = rc.set_wait_timeout_ns(20_000_000)  # 20 ms
             try:
                 rc.debug_skip_first_load(load | second)
