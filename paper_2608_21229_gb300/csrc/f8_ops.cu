@@ -425,8 +425,18 @@ int refcache_f8_weight_grad(const void* dy, int64_t ld_dy, const refcache_f8_row
   float* parts = reinterpret_cast<float*>(static_cast<uint8_t*>(work) + p.values_bytes);
   a.guard.stop = rc_host::take_debug_stop();
   a.guard.timeout_ns = rc_host::wait_timeout_ns();
+  const rc::f8::Rows r = rows_of(x);
+  auto inputs = [&](int col0, int cols) {
+    constexpr int kThreads = rc::f8::kInputThreads, kBlocks = rc::f8::kInputBlocks;
+    const int64_t strips = r.rows * (cols / 16);
+    const unsigned bias = d_bias && col0 == 0 ? ceil_div(n, 64) : 0;
+    const unsigned values = ceil_div(std::min<int64_t>(ceil_div(strips, kThreads), 16ll * sms), kBlocks);
+    e = launch_dependent(rc::f8::f8_wgrad_inputs_kernel, dim3(kBlocks * (bias + values)), dim3(kThreads), 0, s, r, col0, cols,
+                         static_cast<uint16_t*>(work), static_cast<const uint16_t*>(dy), ld_dy, n, d_bias, static_cast<int>(bias));
+    return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "f8_wgrad_inputs_kernel launch");
+  };
+  if (x->rows == 0 && d_bias && (rc = inputs(0, 0)) != 0) return rc;
   for (int col0 = 0; x->rows > 0 && col0 < k; col0 += p.panel) {
-    const rc::f8::Rows r = rows_of(x);
     const int cols = std::min(p.panel, k - col0);
     const int64_t size = dw_f32 ? 4 : 2;
     a.add = add ? static_cast<const uint8_t*>(add) + col0 * size : nullptr;
@@ -439,10 +449,7 @@ int refcache_f8_weight_grad(const void* dy, int64_t ld_dy, const refcache_f8_row
     if ((rc = rc_host::encode_map(&maps.dy, dy, 2 * static_cast<int64_t>(n), r.rows, 2 * ld_dy, 64)) != 0 ||
         (rc = rc_host::encode_map(&maps.x, work, 2 * static_cast<int64_t>(cols), r.rows, 2 * static_cast<int64_t>(cols), 64)) != 0)
       return rc;
-    const int64_t strips = r.rows * (cols / 16);
-    e = launch_dependent(rc::f8::f8_values_kernel, dim3(static_cast<unsigned>(std::min<int64_t>((strips + 255) / 256, 16ll * sms))),
-                         dim3(rc::f8::kRowsThreads), 0, s, r, col0, cols, static_cast<uint16_t*>(work));
-    if (e != cudaSuccess) return cuda_fail(e, "f8_values_kernel launch");
+    if ((rc = inputs(col0, cols)) != 0) return rc;
     const unsigned clusters = static_cast<unsigned>(std::min<int64_t>(static_cast<int64_t>(a.tiles.m) * a.tiles.n * p.splits, pairs));
     e = launch_dependent(rc::f8::f8_wgrad_kernel, dim3(2 * clusters), dim3(L::kThreads), L::kDynamic, s, maps, a);
     if (e != cudaSuccess) return cuda_fail(e, "f8_wgrad_kernel launch");
@@ -453,11 +460,6 @@ int refcache_f8_weight_grad(const void* dy, int64_t ld_dy, const refcache_f8_row
     e = launch_dependent(rc::f8::f8_wgrad_sum_kernel, dim3(blocks), dim3(256), 0, s, static_cast<const float*>(parts), x->rows == 0 ? 0 : p.splits,
                          count, add, dw, dw_f32);
     if (e != cudaSuccess) return cuda_fail(e, "f8_wgrad_sum_kernel launch");
-  }
-  if (d_bias) {
-    e = launch_dependent(rc::f8::f8_bias_grad_kernel, dim3(ceil_div(n, 64), rc::f8::kBiasSplit), dim3(256), 0, s, static_cast<const uint16_t*>(dy), ld_dy,
-                         x->rows, n, d_bias);
-    if (e != cudaSuccess) return cuda_fail(e, "f8_bias_grad_kernel launch");
   }
   return REFCACHE_OK;
 }

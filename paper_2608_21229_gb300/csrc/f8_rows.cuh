@@ -71,30 +71,6 @@ __global__ void __launch_bounds__(kRowsThreads, 6) f8_quantize_kernel(const uint
   }
 }
 
-// Columns [col0, col0 + cols) of rows in 8-bit form as bf16 [rows, cols], exactly: 16 columns a thread.
-__global__ void __launch_bounds__(kRowsThreads) f8_values_kernel(const Rows r, int col0, int cols, uint16_t* to) {
-  grid_dependency_wait();
-  grid_launch_dependents();
-  const int strips = cols / 16;
-  const int64_t n = r.rows * strips, step = static_cast<int64_t>(gridDim.x) * kRowsThreads;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kRowsThreads + threadIdx.x; i < n; i += step) {
-    const int64_t row = i / strips;
-    const int col = static_cast<int>(i - row * strips) * 16;
-    const uint4 c = *reinterpret_cast<const uint4*>(r.codes + row * r.width + col0 + col);
-    const float s = from_codes(r.scales[row * r.pitch + (col0 + col) / kBlock]);
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-    uint32_t out[8];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float4 v = unpack_e4m3x4(w[j]);
-      out[2 * j] = pack_bf16x2(v.x * s, v.y * s), out[2 * j + 1] = pack_bf16x2(v.z * s, v.w * s);
-    }
-    uint4* y = reinterpret_cast<uint4*>(to + row * cols + col);
-    y[0] = make_uint4(out[0], out[1], out[2], out[3]);
-    y[1] = make_uint4(out[4], out[5], out[6], out[7]);
-  }
-}
-
 // A weight [n, k] and its transposed codes: a block of 256 threads takes 128 x 128.
 // Warp w holds rows 16 w .. 16 w + 15, four columns a lane, so that a thread has 16
 // bytes of four rows of the transposed tile, which go through shared memory into

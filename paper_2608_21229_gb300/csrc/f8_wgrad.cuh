@@ -19,6 +19,7 @@
 // are few the rows are split and the parts added by another kernel in a fixed order.
 #pragma once
 #include "f8_pair.cuh"
+#include "vec8.cuh"
 
 namespace rc {
 namespace f8 {
@@ -62,6 +63,78 @@ __device__ __forceinline__ WgradItem wgrad_item(const WgradArgs& a, int item) {
   t.first = t.part * a.per_split;
   t.last = min(a.stages, t.first + a.per_split);
   return t;
+}
+
+// What comes before the product: x's values and d_bias, by blocks of one kernel.  Bound by memory, and in small calls
+// by the launches (two kernels: 333 rows, x of 272 and dy of 1040 columns, 17.3 us a call from the host, one 14.0; 4608 rows, x of 4096 and
+// dy of 16384: 406 and 399).
+constexpr int kInputBlocks = 8;  // of a cluster
+constexpr int kInputThreads = 256;
+
+// Columns [col0, col0 + cols) of rows in 8-bit form as bf16 [rows, cols], exactly: 16 columns a thread.
+__device__ __forceinline__ void write_values(const Rows& r, int col0, int cols, uint16_t* to, int block, int blocks) {
+  const int strips = cols / 16;
+  const int64_t n = r.rows * strips, step = static_cast<int64_t>(blocks) * kInputThreads;
+  for (int64_t i = static_cast<int64_t>(block) * kInputThreads + threadIdx.x; i < n; i += step) {
+    const int64_t row = i / strips;
+    const int col = static_cast<int>(i - row * strips) * 16;
+    const uint4 c = *reinterpret_cast<const uint4*>(r.codes + row * r.width + col0 + col);
+    const float s = from_codes(r.scales[row * r.pitch + (col0 + col) / kBlock]);
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+    uint32_t out[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 v = unpack_e4m3x4(w[j]);
+      out[2 * j] = pack_bf16x2(v.x * s, v.y * s), out[2 * j + 1] = pack_bf16x2(v.z * s, v.w * s);
+    }
+    uint4* y = reinterpret_cast<uint4*>(to + row * cols + col);
+    y[0] = make_uint4(out[0], out[1], out[2], out[3]);
+    y[1] = make_uint4(out[4], out[5], out[6], out[7]);
+  }
+}
+
+// d_bias: the sums of dy over the rows.  A cluster of kInputBlocks blocks has 64 columns, eight a thread; each
+// block takes every kInputBlocks-th 32 rows, and the first one adds up what the others found, in their order.
+__device__ __forceinline__ void write_bias_grad(const uint16_t* dy, int64_t ld, int64_t rows, int n, float* out, int col0) {
+  __shared__ __align__(16) float part[32][64];
+  __shared__ __align__(16) float all[kInputBlocks][64];
+  cluster_sync();  // (the others' shared memory is there)
+  const int lane = threadIdx.x & 7, sub = threadIdx.x >> 3;
+  const int col = col0 + 8 * lane, rank = static_cast<int>(cluster_ctarank());
+  Vec8 v = fill8(0.f);
+  if (col < n) {
+#pragma unroll 4
+    for (int64_t r = 32 * rank + sub; r < rows; r += 32 * kInputBlocks) {
+      const Vec8 x = unpack8(*reinterpret_cast<const uint4*>(dy + r * ld + col));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v.v[e] += x.v[e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) part[sub][8 * lane + e] = v.v[e];
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    float s = 0.f;
+    for (int i = 0; i < 32; ++i) s += part[i][threadIdx.x];
+    st_cluster_u32(mapa_shared(smem_u32(&all[rank][threadIdx.x]), 0), __float_as_uint(s));
+  }
+  cluster_sync();
+  if (rank == 0 && threadIdx.x < 64 && col0 + static_cast<int>(threadIdx.x) < n) {
+    float s = 0.f;
+    for (int i = 0; i < kInputBlocks; ++i) s += all[i][threadIdx.x];
+    out[col0 + threadIdx.x] = s;
+  }
+}
+// The first `bias_clusters` clusters have d_bias.
+__global__ void __cluster_dims__(kInputBlocks, 1, 1) __launch_bounds__(kInputThreads)
+    f8_wgrad_inputs_kernel(const Rows r, int col0, int cols, uint16_t* values, const uint16_t* dy, int64_t ld, int n, float* d_bias, int bias_clusters) {
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int block = static_cast<int>(blockIdx.x) - bias_clusters * kInputBlocks;
+  if (block < 0)
+    write_bias_grad(dy, ld, r.rows, n, d_bias, static_cast<int>(blockIdx.x / kInputBlocks) * 64);
+  else
+    write_values(r, col0, cols, values, block, static_cast<int>(gridDim.x) - bias_clusters * kInputBlocks);
 }
 
 // One lane's column of x, up to 128 rows of dw (the first `rows` of them there), each a line's part with the
@@ -232,42 +305,6 @@ __global__ void __launch_bounds__(256) f8_wgrad_sum_kernel(const float* parts, i
     } else {
       *reinterpret_cast<uint4*>(static_cast<uint16_t*>(dw) + i) = pack8(v);
     }
-  }
-}
-
-// d_bias: the sums of dy over the rows.  A cluster of kBiasSplit blocks has 64 columns, eight a thread;
-// each block takes every kBiasSplit-th 32 rows, and the first one adds up what the others found, in their order.
-constexpr int kBiasSplit = 8;
-__global__ void __cluster_dims__(1, kBiasSplit, 1) __launch_bounds__(256) f8_bias_grad_kernel(const uint16_t* dy, int64_t ld, int64_t rows, int n, float* out) {
-  __shared__ __align__(16) float part[32][64];
-  __shared__ __align__(16) float all[kBiasSplit][64];
-  cluster_sync();  // (the others' shared memory is there)
-  grid_dependency_wait();
-  grid_launch_dependents();
-  const int lane = threadIdx.x & 7, sub = threadIdx.x >> 3;
-  const int col = blockIdx.x * 64 + 8 * lane, rank = static_cast<int>(cluster_ctarank());
-  Vec8 v = fill8(0.f);
-  if (col < n) {
-#pragma unroll 4
-    for (int64_t r = 32 * rank + sub; r < rows; r += 32 * kBiasSplit) {
-      const Vec8 x = unpack8(*reinterpret_cast<const uint4*>(dy + r * ld + col));
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v.v[e] += x.v[e];
-    }
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) part[sub][8 * lane + e] = v.v[e];
-  __syncthreads();
-  if (threadIdx.x < 64) {
-    float s = 0.f;
-    for (int i = 0; i < 32; ++i) s += part[i][threadIdx.x];
-    st_cluster_u32(mapa_shared(smem_u32(&all[rank][threadIdx.x]), 0), __float_as_uint(s));
-  }
-  cluster_sync();
-  if (rank == 0 && threadIdx.x < 64 && blockIdx.x * 64 + threadIdx.x < n) {
-    float s = 0.f;
-    for (int i = 0; i < kBiasSplit; ++i) s += all[i][threadIdx.x];
-    out[blockIdx.x * 64 + threadIdx.x] = s;
   }
 }
 
