@@ -24,7 +24,9 @@
  * around the attention: the three calls' gradients (*_backward), the way from a
  * projection's rows to the attention's q, k and v (refcache_qkv_rope), the gated
  * residual with the norm behind it (refcache_gated_norm), both with their
- * gradients, and the clipping of gradients (refcache_clip_gradients).
+ * gradients, the clipping of gradients (refcache_clip_gradients), and the linear
+ * layers of the block in 8 bits, whose inputs stay as they are for the backward
+ * pass (refcache_f8_*).
  *
  * Conventions shared by every entry point
  *   - Tensors are THD: [tokens, num_heads, head_dim] bf16, head_dim

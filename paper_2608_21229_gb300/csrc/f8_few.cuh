@@ -2,7 +2,8 @@
 // weight is streamed once, 128 of its rows (columns of y) as the first operand of
 // block-scaled MMAs (M = 128), up to 128 rows of x as the second (N = rows, a multiple of 16).
 //
-// What bounds it is the weight's bytes.  Two CTAs an SM, each with up to 100 KB of loads in
+// What bounds it is the weight's bytes: 2 rows, 24576 x 4096: 21.5 us a call, 4.7 TB/s (0.69 of the measured copy; a launch and its
+// first loads are 6 of it).  Two CTAs an SM, each with up to 100 KB of loads in
 // flight, cover the memory's latency; where 128-row tiles alone would leave SMs idle, a
 // cluster of up to eight CTAs splits x's columns, and each of them adds up every so-manieth
 // row of y from the others' shared memory, in their order, with a warp to a row: one block of 128

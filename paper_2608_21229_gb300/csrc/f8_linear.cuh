@@ -7,6 +7,14 @@
 // the bytes of four blocks for each row) and go into tensor memory by tcgen05.cp, issued before the
 // first MMA that needs them.  Sums stay in tensor memory from the first column to the last.
 //
+// What bounds it: the MMAs, 512 cycles for each 128 columns of x and 256 x 256 of y, of which a stage takes 570 to 600, and in long
+// calls the power cap (1.4 to 1.6 GHz); in short ones the last round of tiles.  With half of each
+// stage's MMAs left out a stage still took 584, with half of its loads 581, with both 501: loads and MMAs share the
+// shared memory's 128 bytes a cycle (32 KB written and read in 512).  1280 x 12288 x 4096: 42.9 us, 3.0 PFLOP/s (0.79 of twice the
+// measured bf16 rate); 20608 x 4096 x 12288: 638 us, 3.25 PFLOP/s (0.86).  The GELU (1792 x 8192 x 2048: 30 us) is bound by its sums' warps: 13800
+// cycles a tile for two 8-bit forms and the GELU of 256 x 256, where the MMAs of 2048 columns take 9100: two warps a sub-partition, whose
+// registers leave the latencies of one pair of columns to few others (pairs two, four or eight at a time, step by step, took as long).
+//
 // Tensor memory: two halves of 128 columns of sums, then the scales' slots.  A tile wider
 // than 128 takes both halves, a narrower one every second; a half is free as soon as its
 // four warps have its 128 columns in registers, a row's block of 128 to a thread, which
