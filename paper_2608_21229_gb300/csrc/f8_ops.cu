@@ -445,12 +445,15 @@ int refcache_f8_weight_grad(const void* dy, int64_t ld_dy, const refcache_f8_row
     a.n = n, a.k = cols, a.bn = p.bn;
     a.stages = p.stages, a.splits = p.splits, a.per_split = p.per_split;
     a.tiles = {static_cast<int32_t>(ceil_div(n, p.bn)), static_cast<int32_t>(ceil_div(cols, 256))};
+    const int tiles = a.tiles.m * a.tiles.n * p.splits, over = tiles % pairs;
+    const bool halves = p.splits == 1 && p.bn == 256 && tiles > pairs && 2 * over <= pairs;
+    a.n_whole = halves ? tiles - over : tiles, a.n_items = halves ? tiles + over : tiles;
     rc::f8::WgradMaps maps;
     if ((rc = rc_host::encode_map(&maps.dy, dy, 2 * static_cast<int64_t>(n), r.rows, 2 * ld_dy, 64)) != 0 ||
         (rc = rc_host::encode_map(&maps.x, work, 2 * static_cast<int64_t>(cols), r.rows, 2 * static_cast<int64_t>(cols), 64)) != 0)
       return rc;
     if ((rc = inputs(col0, cols)) != 0) return rc;
-    const unsigned clusters = static_cast<unsigned>(std::min<int64_t>(static_cast<int64_t>(a.tiles.m) * a.tiles.n * p.splits, pairs));
+    const unsigned clusters = static_cast<unsigned>(std::min(a.n_items, pairs));
     e = launch_dependent(rc::f8::f8_wgrad_kernel, dim3(2 * clusters), dim3(L::kThreads), L::kDynamic, s, maps, a);
     if (e != cudaSuccess) return cuda_fail(e, "f8_wgrad_kernel launch");
   }

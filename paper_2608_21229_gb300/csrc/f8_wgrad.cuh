@@ -36,6 +36,7 @@ struct WgradArgs {
   int32_t stages;       // of 64 rows
   int32_t splits, per_split;  // parts, and stages of each
   Tiles tiles;                // m: of n; n: of k
+  int32_t n_whole, n_items;   // tiles taken whole (of all parts); these and the halves, of 128 columns of dy, of the others
   Guard guard;
 };
 struct WgradMaps {
@@ -54,15 +55,21 @@ struct WgradSmem {
   __device__ static constexpr uint32_t arrivals(int i) { return i >= kAccEmpty && i < kDone ? 16 : 1; }  // eight warps of each CTA
 };
 
-// The items of a launch: part by part, each over all tiles.
+// The items of a launch: part by part, each over all tiles; without parts, the tiles behind the last full round over the
+// pairs in halves where these are no more than the pairs (a stage of one takes 384 cycles, of a tile 512: 1500 rows,
+// 4112 x 2064, 153 tiles: 33.6 -> 32.4 us; 4608 rows, 16384 x 4096, 1024 tiles: 362 -> 356).
 struct WgradItem {
-  int i, j, part, first, last;  // stages [first, last)
+  int row0, bn, j, part, first, last;  // rows of dw, columns in 256s, stages [first, last)
 };
 __device__ __forceinline__ WgradItem wgrad_item(const WgradArgs& a, int item) {
-  const int n_tiles = a.tiles.m * a.tiles.n;
+  const int n_tiles = a.tiles.m * a.tiles.n, half = item - a.n_whole;
+  const int tile = half < 0 ? item : a.n_whole + (half >> 1);
   WgradItem t;
-  t.part = item / n_tiles;
-  a.tiles.at(item - t.part * n_tiles, &t.i, &t.j);
+  int i;
+  t.part = tile / n_tiles;
+  a.tiles.at(tile - t.part * n_tiles, &i, &t.j);
+  t.bn = half < 0 ? a.bn : 128;
+  t.row0 = i * a.bn + (half < 0 ? 0 : 128 * (half & 1));
   t.first = t.part * a.per_split;
   t.last = min(a.stages, t.first + a.per_split);
   return t;
@@ -173,12 +180,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WgradSmem::kThreads,
   Cta<L> c;
   if (!c.enter(smem_raw, a.guard)) return;
   const int cluster = static_cast<int>(blockIdx.x >> 1), n_clusters = static_cast<int>(gridDim.x >> 1);
-  const int n_items = a.tiles.m * a.tiles.n * a.splits;
-  const uint2 bytes = make_uint2(L::kOperand, static_cast<uint32_t>(a.bn) * 64u);  // of one CTA's load: x, dy
+  const int n_items = a.n_items;
+  auto bytes = [](int bn) { return make_uint2(L::kOperand, static_cast<uint32_t>(bn) * 64u); };  // of one CTA's load: x, dy
   int loads = 0;
   if (c.warp == L::kProducer || c.warp == L::kProducer2) {
     if (c.lane == 0) {
-      const bool of_x = c.warp == L::kProducer, arms = of_x && c.leader, two = of_x || a.bn > 128;  // 64 columns a load
+      const bool of_x = c.warp == L::kProducer, arms = of_x && c.leader;
       const int most = of_x ? loads_before_stop(a.guard.stop, c.rank) : 0x7FFFFFFF;
       const CUtensorMap* map = of_x ? &maps.x : &maps.dy;
       const uint32_t to = c.base + (of_x ? 0u : L::kOperand);
@@ -187,14 +194,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WgradSmem::kThreads,
       for (int item = cluster; ok && item < n_items; item += n_clusters) {
         const WgradItem t = wgrad_item(a, item);
         // (the maps count bytes)
-        const int x = 2 * (of_x ? t.j * 256 + 128 * static_cast<int>(c.rank) : t.i * a.bn + a.bn / 2 * static_cast<int>(c.rank));
+        const int x = 2 * (of_x ? t.j * 256 + 128 * static_cast<int>(c.rank) : t.row0 + t.bn / 2 * static_cast<int>(c.rank));
+        const bool two = of_x || t.bn > 128;  // 64 columns a load
+        const uint2 b = bytes(t.bn);
 #pragma unroll 1
         for (int st = t.first; st < t.last; ++st) {
           const int s = loads % L::kSlots, n = loads / L::kSlots;
           ok = loads != most && (n == 0 || c.wait(L::kEmpty + s, n - 1, 111));
           if (!ok) break;
           const uint32_t at = to + static_cast<uint32_t>(s) * L::kSlot, full = c.lbar(L::kFull + s);
-          if (arms) mbar_arrive_expect_tx(c.bar(L::kFull + s), 2 * (bytes.x + bytes.y));
+          if (arms) mbar_arrive_expect_tx(c.bar(L::kFull + s), 2 * (b.x + b.y));
           tma_load_2d_pair(at, map, full, x, st * 64);
           if (two) tma_load_2d_pair(at + 8192, map, full, x + 128, st * 64);
           ++loads;
@@ -206,12 +215,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WgradSmem::kThreads,
     if (c.leader) {
       // (64 columns of 64 rows are 8 KB; 8 rows 1 KB)
       const uint64_t ad = sdesc_sw128(c.base, 8192, 1024), bd = sdesc_sw128(c.base + L::kOperand, 8192, 1024);
-      const uint32_t idesc = idesc_bf16_f32(256, a.bn, true) | (1u << 15);  // A MN-major too
       bool issued = false, ok = true;
       int load = 0, used = 0;  // stages, chunks
 #pragma unroll 1
       for (int item = cluster; ok && item < n_items; item += n_clusters) {
         const WgradItem t = wgrad_item(a, item);
+        const uint32_t idesc = idesc_bf16_f32(256, t.bn, true) | (1u << 15);  // A MN-major too
 #pragma unroll 1
         for (int st = t.first, in_chunk = 0; st < t.last; ++st, ++load) {
           const int s = load % L::kSlots;
@@ -237,14 +246,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WgradSmem::kThreads,
     }
   } else {
     // A warp has half of dw's rows, 128 (or 64) of them, of 32 columns of x.
-    const int group = c.warp >> 2, quarter = c.warp & 3, half = a.bn / 2;
+    const int group = c.warp >> 2, quarter = c.warp & 3;
     int used = 0;
     bool ok = true;
 #pragma unroll 1
     for (int item = cluster; ok && item < n_items; item += n_clusters) {
       const WgradItem t = wgrad_item(a, item);
       const int col = t.j * 256 + 128 * static_cast<int>(c.rank) + 32 * quarter + c.lane;
-      const int row0 = t.i * a.bn + half * group, rows = col < a.k ? min(half, a.n - row0) : 0;
+      const int half = t.bn / 2, row0 = t.row0 + half * group, rows = col < a.k ? min(half, a.n - row0) : 0;
       const int64_t ld = a.splits == 1 ? a.ld : a.k, at = (static_cast<int64_t>(t.part) * (a.splits == 1 ? 0 : a.n) + row0) * ld + col;
       float v[128];  // (what is to be added first: it is on its way while the MMAs run)
       if (a.add == nullptr || a.splits > 1) {
@@ -281,7 +290,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WgradSmem::kThreads,
         store_rows(v, static_cast<uint16_t*>(a.dw) + at, ld, rows);
     }
   }
-  c.leave(Loads{loads, bytes, bytes, 0}, Loads{});
+  const int whole = cluster < a.n_whole ? (a.n_whole - cluster + n_clusters - 1) / n_clusters : 0;  // tiles of this pair
+  c.leave(Loads{loads, bytes(a.bn), bytes(a.n_whole < n_items ? 128 : a.bn), whole * a.stages}, Loads{});
 }
 
 // dw = add + the parts, one after the other.

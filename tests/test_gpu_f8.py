@@ -348,6 +348,13 @@ def test_tiles_in_pieces(r, n, k):
     test_linear_gelu_backward(r, k, n, "tanh")
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("r, n, k", [(700, 4848, 1040), (260, 4112, 1296), (1100, 4848, 1040)])
+def test_weight_grad_tiles_in_halves(r, n, k, dtype):
+    """On 76 CTA pairs: 95 and 102 tiles, of which the last 19 and 26 go in halves; one and two sets of 1024 rows."""
+    test_weight_grad(r, n, k, dtype)
+
+
 # ---------------------------------------------------------------- no rows, streams, graphs
 def test_without_rows():
     x, w = rc.F8Rows(0, 64), rc.f8_quantize_weight(randn(gen(1), 32, 64))

@@ -63,6 +63,18 @@ def pieces():
     return call
 
 
+def halves():
+    """95 tiles of eleven loads each, so that on 76 pairs the last 19 are shared out in halves of eleven loads."""
+    x, dy = rc.f8_quantize(rnd(0, 700, 1040).to(BF16)), rnd(1, 700, 4848).to(BF16)
+
+    def call():
+        dw = torch.empty(4848, 1040, device="cuda")
+        rc.f8_weight_grad(dy, x, dw)
+        return dw
+
+    return call
+
+
 def weight_grad():
     x, dy = rc.f8_quantize(rnd(0, 1300, 2064).to(BF16)), rnd(1, 1300, 4112).to(BF16)
 
@@ -81,6 +93,10 @@ def test_wait_timeouts_are_reported_and_the_context_survives(make):
 
 def test_wait_timeouts_in_pieces_of_tiles():
     check_timeouts(pieces(), (9, 10, 11, 12, 13, 14, 16, 18))
+
+
+def test_wait_timeouts_in_halves_of_tiles():
+    check_timeouts(halves(), (10, 11, 12, 13, 15, 17, 18, 22))
 
 
 def check_timeouts(call, loads):
