@@ -138,7 +138,7 @@ __device__ __forceinline__ f32x2 gelu_grad(f32x2 u) {
 }
 
 // ---------------------------------------------------------------- what becomes of a product
-enum Epilogue { kStore = 0, kGelu = 2, kGeluGrad = 4 };  // + the form of the GELU
+enum Epilogue { kStore = 0, kStoreLines = 1, kGelu = 2, kGeluGrad = 4 };  // + the form of the GELU
 
 struct Out {
   const void* bias;  // [width] or null

@@ -112,6 +112,45 @@ __device__ __forceinline__ void store_pieces(void* to, const uint4 (&c)[8], int 
     if (n >= 8) y[7] = c[7];
   }
 }
+// The first n of 8 pieces of 16 bytes of each of a warp's rows, a row a lane: four lanes exchange theirs first, so that each
+// of them has the same 32 bytes of four rows, and together they store a line of one row at a time.  (Stored from its own lane, 32
+// bytes of 32 rows at a time, a tile's 256 columns in bf16 take 5400 cycles, 12 bytes a cycle, which bounds products of
+// few columns: kLinesMost.  The 8-bit forms of a GELU, 8 % slower this way, go from their own lanes.)  `at`: the first row's place; `rows` of the 32 are there.
+__device__ __forceinline__ void store_lines(uint8_t* at, int64_t pitch, int rows, int n, uint4 (&c)[8]) {
+  const int lane = threadIdx.x & 31, q = lane & 3;
+#pragma unroll
+  for (int d = 1; d < 4; d *= 2) {
+    const bool upper = q & d;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i & d) continue;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {  // of a unit of 32 bytes
+        uint4 &lo = c[2 * i + h], &hi = c[2 * (i | d) + h];
+        auto swap = [&](uint32_t& x, uint32_t& y) {
+          const uint32_t other = __shfl_xor_sync(0xffffffffu, upper ? x : y, d);
+          if (upper) x = other; else y = other;
+        };
+        swap(lo.x, hi.x), swap(lo.y, hi.y), swap(lo.z, hi.z), swap(lo.w, hi.w);
+      }
+    }
+  }
+  uint8_t* to = at + (lane - q) * pitch + 32 * q;
+  const int left = rows - (lane - q), there = n - 2 * q;
+#pragma unroll
+  for (int i = 0; i < 4; ++i, to += pitch) {
+    if (i >= left) break;
+    const uint4 x = c[2 * i], y = c[2 * i + 1];
+    if (there > 1 && (reinterpret_cast<uintptr_t>(to) & 31u) == 0) {
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w), "r"(y.x), "r"(y.y),
+                   "r"(y.z), "r"(y.w)
+                   : "memory");
+    } else {
+      if (there > 0) reinterpret_cast<uint4*>(to)[0] = x;
+      if (there > 1) reinterpret_cast<uint4*>(to)[1] = y;
+    }
+  }
+}
 __device__ __forceinline__ void quantize_block(const Rows& r, int64_t row, int col0, int cols, const f32x2 (&v)[64]) {
   float m[2] = {0.f, 0.f};
 #pragma unroll
@@ -134,18 +173,32 @@ __device__ __forceinline__ void quantize_block(const Rows& r, int64_t row, int c
   store_pieces(r.codes + row * r.width + col0, c, cols / 16);
   put_scale(r, row, col0 / kBlock, b);
 }
-__device__ __forceinline__ void store_block(uint16_t* y, int cols, const f32x2 (&v)[64]) {
+__device__ __forceinline__ void pack_block(int h, const f32x2 (&v)[64], uint4 (&c)[8]) {  // columns 64 h .. 64 h + 63 in bf16
   auto two = [&](int i) {
     float a, b;
     split_f32x2(v[i], a, b);
     return pack_bf16x2(a, b);
   };
 #pragma unroll
+  for (int i = 0; i < 8; ++i) c[i] = make_uint4(two(32 * h + 4 * i), two(32 * h + 4 * i + 1), two(32 * h + 4 * i + 2), two(32 * h + 4 * i + 3));
+}
+__device__ __forceinline__ void store_block(uint16_t* y, int cols, const f32x2 (&v)[64]) {
+#pragma unroll
   for (int h = 0; h < 2; ++h) {
     uint4 c[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = make_uint4(two(32 * h + 4 * i), two(32 * h + 4 * i + 1), two(32 * h + 4 * i + 2), two(32 * h + 4 * i + 3));
+    pack_block(h, v, c);
     store_pieces(y + 64 * h, c, cols / 8 - 8 * h);
+  }
+}
+// The same by a whole warp, in lines (row: this lane's).
+__device__ __forceinline__ void store_block_lines(const Out& o, int64_t row, int col0, int cols, const f32x2 (&v)[64]) {
+  const int64_t row0 = row - static_cast<int>(threadIdx.x & 31);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint4 c[8];
+    pack_block(h, v, c);
+    store_lines(reinterpret_cast<uint8_t*>(o.y + row0 * o.ld + col0 + 64 * h), 2 * o.ld, static_cast<int>(min(static_cast<int64_t>(32), o.rows - row0)),
+                cols / 8 - 8 * h, c);
   }
 }
 // bias: shared memory, 128 floats; u: the codes of the GELU's argument.
@@ -160,6 +213,7 @@ __device__ __forceinline__ void finish_block(const Out& o, int64_t row, int col0
     }
   }
   if (kEpi == kStore) store_block(o.y + row * o.ld + col0, cols, v);
+  if (kEpi == kStoreLines) store_block_lines(o, row, col0, cols, v);
   if ((kEpi & ~1) == kGelu) {
     if (o.u.codes) quantize_block(o.u, row, col0, cols, v);
 #pragma unroll
@@ -183,6 +237,11 @@ __device__ __forceinline__ void finish_block(const Out& o, int64_t row, int col0
     if (o.a.codes) quantize_block(o.a, row, col0, cols, v);
   }
 }
+
+// Of x: kStoreLines for products of no more columns (20000 rows and 10000 columns of y, from its own lane / in lines: 144 columns 117 / 89 us,
+// 528 162 / 132, 1040 219 / 208; 4000 and 8192: 1024 columns 30.4 / 32.3, 1536 40.4 / 42.4; 1280 and 12288: 4096 columns 42.6 / 43.8).  Not a branch of one
+// kernel: the other side then took 1.5 to 3.5 % more.
+constexpr int kLinesMost = 640;
 
 template <int kEpi>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads, 1)
@@ -235,7 +294,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
       tc_fence_before();
       __syncwarp();
       if (c.lane == 0) mbar_arrive_cluster(c.lbar(L::kAccEmpty + half));
-      if (in) finish_block<kEpi>(a.o, row, col0, cols, v, bias, u, u_scale);
+      // (all lanes of a warp whose first row is there, where they store together)
+      if (kEpi == kStoreLines ? row - c.lane < a.o.rows && cols > 0 : in) finish_block<kEpi>(a.o, row, col0, cols, v, bias, u, u_scale);
     }
   } else {
     fewer_registers<L::kOtherRegs>();

@@ -242,8 +242,8 @@ int launch_linear(const rc::f8::Rows& x, const rc::f8::Rows& w, const rc::f8::Ou
   if (rc || (rc = rc_host::device_status_word(&dev, &a.guard.status)) != 0 ||
       (rc = pairs_of(rc::f8::f8_linear_kernel<kEpi>, kept[dev], L::kThreads, L::kDynamic, sms, &pairs)) != 0)
     return rc;
-  const LinearPlan p = plan_linear(o.rows, o.width, x.width, pairs, sms, kEpi == rc::f8::kStore ? 64 : 128);
-  if (p.few) return launch_few<kEpi>(p, x, w, o, a.guard.status, dev, stream);
+  const LinearPlan p = plan_linear(o.rows, o.width, x.width, pairs, sms, kEpi < rc::f8::kGelu ? 64 : 128);
+  if (p.few) return launch_few<kEpi == rc::f8::kStoreLines ? rc::f8::kStore : kEpi>(p, x, w, o, a.guard.status, dev, stream);
   a.o = o;
   a.x_chunks = x.chunks, a.w_chunks = w.chunks;
   a.k = x.width;
@@ -355,7 +355,8 @@ int refcache_f8_linear(const refcache_f8_rows_t* x, const refcache_f8_weight_t* 
   rc::f8::Out o{};
   o.bias = bias, o.bias_f32 = bias_f32, o.width = out, o.rows = x->rows;
   o.y = static_cast<uint16_t*>(y), o.ld = ld_y;
-  return launch_linear<rc::f8::kStore>(rows_of(x), rows_of(w, t), o, stream);
+  return in <= rc::f8::kLinesMost ? launch_linear<rc::f8::kStoreLines>(rows_of(x), rows_of(w, t), o, stream)
+                                  : launch_linear<rc::f8::kStore>(rows_of(x), rows_of(w, t), o, stream);
 }
 
 int refcache_f8_linear_gelu(const refcache_f8_rows_t* x, const refcache_f8_weight_t* w, const void* bias, int bias_f32, int form,

@@ -348,6 +348,12 @@ def test_tiles_in_pieces(r, n, k):
     test_linear_gelu_backward(r, k, n, "tanh")
 
 
+@pytest.mark.parametrize("r, n, k", [(3001, 8208, 16), (2990, 2576, 640), (2990, 2576, 656), (5000, 4112, 144)])
+def test_many_rows_of_few_columns(r, n, k):
+    test_linear(r, n, k, False)
+    test_linear(r, k, n, True)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
 @pytest.mark.parametrize("r, n, k", [(700, 4848, 1040), (260, 4112, 1296), (1100, 4848, 1040)])
 def test_weight_grad_tiles_in_halves(r, n, k, dtype):
