@@ -165,8 +165,9 @@ __global__ void __launch_bounds__(FewSmem::kThreads, 2)
       if ((after & 3) == 0 || end) ++group;
       kb = after;
     }
-    if (!ok && issued && elect_one()) {  // (else the sums' warps have waited for the last one)
-      commit(bar(L::kAccFull));
+    // (always: the sums' warps may have given up on MMAs that go on)
+    if (issued && elect_one()) {
+      if (!ok) commit(bar(L::kAccFull));
       drain(bar(L::kAccFull), 0u, a.guard.timeout_ns);
     }
     __syncwarp();
