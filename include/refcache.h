@@ -645,7 +645,12 @@ REFCACHE_API int refcache_status(void* stream);
  */
 REFCACHE_API int refcache_cache_status(refcache_t* cache, void* stream);
 
-/* Wait limit of every in-kernel wait, nanoseconds (default 1e9).  Returns the old value. */
+/*
+ * Wait limit of every in-kernel wait, nanoseconds (default 1e9; less than REFCACHE_LEAST_WAIT_NS counts as
+ * that).  Returns the old value.  The same limit holds for the waits of a kernel that gives up for its own loads and MMAs
+ * in flight, which take microseconds: a shorter one would let it leave before they are done.
+ */
+#define REFCACHE_LEAST_WAIT_NS 1000000ull
 REFCACHE_API uint64_t refcache_set_wait_timeout_ns(uint64_t ns);
 
 /* Select the kernel for subsequent calls (REFCACHE_KERNEL_*); returns the old one or < 0. */

@@ -1704,7 +1704,7 @@ int refcache_cache_status(refcache_t* h, void* stream) {
   return REFCACHE_OK;
 }
 
-uint64_t refcache_set_wait_timeout_ns(uint64_t ns) { return g_timeout_ns.exchange(ns ? ns : 1); }
+uint64_t refcache_set_wait_timeout_ns(uint64_t ns) { return g_timeout_ns.exchange(std::max<uint64_t>(ns, REFCACHE_LEAST_WAIT_NS)); }
 
 int refcache_set_kernel(int kernel) {
   if (kernel != REFCACHE_KERNEL_TCGEN05 && kernel != REFCACHE_KERNEL_MMA_SYNC &&
