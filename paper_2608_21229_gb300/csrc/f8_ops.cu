@@ -130,7 +130,8 @@ int pairs_of(Kernel kernel, std::atomic<int>& kept, int threads, uint32_t smem, 
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
-    if (e != cudaSuccess || n < 1) n = sms / 2;
+    if (e != cudaSuccess) return cuda_fail(e, "cudaOccupancyMaxActiveClusters(f8)");
+    if (n < 1) return fail(REFCACHE_ERR_CUDA, "no CTA pair of an 8-bit product fits on the device");
     kept.store(n);
   }
   *pairs = n;

@@ -62,6 +62,7 @@ int fail(int code, const char* fmt, ...) {
 }
 
 int cuda_fail(cudaError_t e, const char* what) {
+  cudaGetLastError();  // (the runtime keeps it, and the next call would report it as its own)
   return fail(REFCACHE_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
