@@ -615,7 +615,8 @@ REFCACHE_API int refcache_f8_linear_gelu_backward(const refcache_f8_rows_t* dy, 
  * The weight's gradient: dw = add + dy^T x [out_width, width of x], fp32 (dw_f32 != 0) or
  * bf16, packed; add like dw, dw itself or NULL; d_bias = sums of dy over the rows, fp32
  * [out_width], or NULL.  dy [rows of x, out_width] bf16.  x's values are taken as they
- * are (exact in bf16 from 2^-126 on): the product is bf16 with fp32 sums.  Without rows dw is add, or zero.
+ * are (exact in bf16 from 2^-126 on; 2^128, to which the largest bf16 values round, as 255 * 2^120): the
+ * product is bf16 with fp32 sums.  Without rows dw is add, or zero.
  * work: refcache_f8_weight_grad_bytes bytes of device memory (x's values in bf16, at most 256 MB of them
  * or 256 columns at a time, and partial sums where dw is small), 16-byte aligned; may be NULL without rows.
  */

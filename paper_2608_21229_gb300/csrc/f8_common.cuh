@@ -4,7 +4,8 @@
 // exact and a code's only error is its rounding: at most 2^-4 of the value, or
 // 2^-10 s below E4M3's normal range.  A power of two costs no accuracy against a
 // scale of amax / 448 (E4M3 is a floating format), lets the tensor core apply it
-// (UE8M0, kind::mxf8f6f4) and makes a decoded value exact in bf16.
+// (UE8M0, kind::mxf8f6f4) and makes a decoded value exact in bf16, but for its ends: below 2^-126 bf16
+// has fewer bits, and the largest code of a block whose amax is 248 x 2^120 or more is 256, which stands for 2^128.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -54,6 +55,10 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
 // 1 / s; NaN for b = 255, which makes every code of the block a NaN.
 __device__ __forceinline__ float to_codes(uint32_t b) { return __uint_as_float(b == 255u ? 0x7FFFFFFFu : (254u - b) << 23); }
 __device__ __forceinline__ float from_codes(uint32_t b) { return __uint_as_float(b == 255u ? 0x7FFFFFFFu : b << 23); }
+
+// The same for a GELU's argument.  2^128 would be an infinity; at half its size a block with such values has the
+// same derivative, 1, 0 or at zero 1/2: its codes that are not zero are 2^110 or more.
+__device__ __forceinline__ float argument_from_codes(uint32_t b) { return from_codes(b == 247u ? 246u : b); }
 
 // Four codes as floats (exact).
 __device__ __forceinline__ float4 unpack_e4m3x4(uint32_t c) {
@@ -183,7 +188,7 @@ __device__ __forceinline__ void finish_row(const Out& o, int64_t row, int col0, 
   }
   if (in) {
     const float4 u = unpack_e4m3x4(*reinterpret_cast<const uint32_t*>(o.u.codes + row * o.u.width + col));
-    const float s = from_codes(o.u.scales[row * o.u.pitch + col / kBlock]);
+    const float s = argument_from_codes(o.u.scales[row * o.u.pitch + col / kBlock]);
     split_f32x2(mul_f32x2(make_f32x2(v.x, v.y), gelu_grad<kEpi & 1>(make_f32x2(u.x * s, u.y * s))), v.x, v.y);
     split_f32x2(mul_f32x2(make_f32x2(v.z, v.w), gelu_grad<kEpi & 1>(make_f32x2(u.z * s, u.w * s))), v.z, v.w);
     if (o.y) *reinterpret_cast<uint2*>(o.y + row * o.ld + col) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));

@@ -277,7 +277,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
 #pragma unroll
         for (int q = 0; q < 8; ++q)
           if (16 * q < cols) u[q] = *reinterpret_cast<const uint4*>(from + 16 * q);
-        u_scale = from_codes(a.o.u.scales[row * a.o.u.pitch + col0 / kBlock]);
+        u_scale = argument_from_codes(a.o.u.scales[row * a.o.u.pitch + col0 / kBlock]);
       }
       if (kEpi < kGeluGrad && a.o.bias) {  // four columns a lane
         float b[4];

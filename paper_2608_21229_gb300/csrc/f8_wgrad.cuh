@@ -3,7 +3,7 @@
 // dy a tile.
 //
 // The sum runs over the rows, along which x has a scale each, so the tensor core cannot
-// apply them.  A code times its power of two is exact in bf16: a first kernel writes x's
+// apply them.  A code times its power of two is exact in bf16 (from 2^-126 on, and 2^128 is taken as the largest value): a first kernel writes x's
 // values, or a panel of their columns, to the workspace, and the product is that of dy and of the
 // values that x stands for.  (Turned into bf16 on the way to the MMAs, a code is converted once for
 // each 256 columns of dy: eight warps took 766 cycles for what 512 cycles of MMAs
@@ -81,7 +81,13 @@ __device__ __forceinline__ WgradItem wgrad_item(const WgradArgs& a, int item) {
 constexpr int kInputBlocks = 8;  // of a cluster
 constexpr int kInputThreads = 256;
 
-// Columns [col0, col0 + cols) of rows in 8-bit form as bf16 [rows, cols], exactly: 16 columns a thread.
+// Two values in bf16; above its largest, that (NaNs as they are).
+__device__ __forceinline__ uint32_t pack_finite_bf16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// Columns [col0, col0 + cols) of rows in 8-bit form as bf16 [rows, cols]: 16 columns a thread.
 __device__ __forceinline__ void write_values(const Rows& r, int col0, int cols, uint16_t* to, int block, int blocks) {
   const int strips = cols / 16;
   const int64_t n = r.rows * strips, step = static_cast<int64_t>(blocks) * kInputThreads;
@@ -95,7 +101,7 @@ __device__ __forceinline__ void write_values(const Rows& r, int col0, int cols, 
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float4 v = unpack_e4m3x4(w[j]);
-      out[2 * j] = pack_bf16x2(v.x * s, v.y * s), out[2 * j + 1] = pack_bf16x2(v.z * s, v.w * s);
+      out[2 * j] = pack_finite_bf16x2(v.x * s, v.y * s), out[2 * j + 1] = pack_finite_bf16x2(v.z * s, v.w * s);
     }
     uint4* y = reinterpret_cast<uint4*>(to + row * cols + col);
     y[0] = make_uint4(out[0], out[1], out[2], out[3]);
