@@ -27,7 +27,7 @@ struct FewSmem {
   static constexpr int kMaxSlots = 6, kScaleSlots = 4;
   static constexpr uint32_t kStages = 104 * 1024, kA = 16384, kScales = kStages, kBars = kScales + kScaleSlots * 1024;
   static constexpr int kFull = 0, kEmpty = kFull + kMaxSlots, kScFull = kEmpty + kMaxSlots, kScEmpty = kScFull + kScaleSlots, kAccFull = kScEmpty + kScaleSlots,
-                       kNumBars = kAccFull + 1;
+                       kAccEmpty = kAccFull + 1, kNumBars = kAccEmpty + 1;
   static constexpr uint32_t kAux = kBars + 8 * kNumBars, kUsed = kAux + 8, kDynamic = kUsed + 1024;
   static constexpr int kProducer = 4, kMma = 5, kThreads = 32 * 6;  // warps 0-3: sums
   static constexpr uint32_t kTmemCols = 256, kTmemScales = 128;      // 8 columns a slot
@@ -61,8 +61,9 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
   return v;
 }
 
-// Grid: (CTAs of a cluster, tiles of 128 columns of y, tiles of 128 rows).
-template <int kEpi>
+// Grid: (CTAs of a cluster, tiles of 128 columns of y, tiles of 128 rows).  kLong: a CTA has more than kSumBlocks blocks of
+// columns, after each of which the sums go into registers (f8_linear.cuh).
+template <int kEpi, bool kLong>
 __global__ void __launch_bounds__(FewSmem::kThreads, 2)
     f8_few_kernel(const __grid_constant__ LinearMaps maps, const __grid_constant__ FewArgs a) {
   using L = FewSmem;
@@ -81,7 +82,7 @@ __global__ void __launch_bounds__(FewSmem::kThreads, 2)
   };
   auto wait_all = [&](int i, int k, int where) { return __all_sync(0xffffffffu, wait(i, k, where)); };
   if (threadIdx.x == 0) {
-    for (int i = 0; i < L::kNumBars; ++i) mbar_init(bar(i), 1);
+    for (int i = 0; i < L::kNumBars; ++i) mbar_init(bar(i), i == L::kAccEmpty ? 4 : 1);
     aux[0] = 0;
     fence_barrier_init();
     fence_proxy_async_smem();
@@ -132,17 +133,18 @@ __global__ void __launch_bounds__(FewSmem::kThreads, 2)
   } else if (warp == L::kMma) {
     const uint64_t sd = scales_desc(base + L::kScales);
     const uint32_t idesc = idesc_mx(128, n);
-    int load = 0, group = 0;
-    bool ok = true, issued = false;
+    int load = 0, group = 0, sums = 0;  // sums: committed
+    bool ok = true, issued = false;     // issued: since the last of these
 #pragma unroll 1
     for (int i = first, kb = begin; i < last; ++i, ++load) {
-      const int s = load % a.slots, sc = group % L::kScaleSlots;
+      const int s = load % a.slots, sc = group % L::kScaleSlots, in_sum = kLong ? load % kSumBlocks : load;
       const uint32_t sfa = tmem + L::kTmemScales + 8u * sc;
-      ok = ((kb & 3) != 0 || wait_all(L::kScFull + sc, group / L::kScaleSlots, 134)) && wait_all(L::kFull + s, load / a.slots, 135);
+      ok = (!kLong || in_sum > 0 || sums == 0 || wait_all(L::kAccEmpty, sums - 1, 133)) &&
+           ((kb & 3) != 0 || wait_all(L::kScFull + sc, group / L::kScaleSlots, 134)) && wait_all(L::kFull + s, load / a.slots, 135);
       if (!ok) break;
       issued = true;
       const int steps = min(4, (a.k - kb * kBlock + 31) / 32);
-      const bool end = i + 1 == last;
+      const bool end = i + 1 == last, out = end || (kLong && in_sum == kSumBlocks - 1);
       const int after = next(kb);
       if (elect_one()) {
         tc_fence_after();
@@ -156,26 +158,55 @@ __global__ void __launch_bounds__(FewSmem::kThreads, 2)
         const uint32_t id = idesc_byte(idesc, kb & 3);
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          if (q < steps) mx_mma(tmem, ad + 2 * q, bd + 2 * q, id, sfa, sfa + 4, i > first || q > 0 ? 1u : 0u);
+          if (q < steps) mx_mma(tmem, ad + 2 * q, bd + 2 * q, id, sfa, sfa + 4, in_sum > 0 || q > 0 ? 1u : 0u);
         commit(bar(L::kEmpty + s));
         if ((after & 3) == 0 || end) commit(bar(L::kScEmpty + sc));
-        if (end) commit(bar(L::kAccFull));
+        if (out) commit(bar(L::kAccFull));
       }
       __syncwarp();
       if ((after & 3) == 0 || end) ++group;
+      if (out) ++sums, issued = false;
       kb = after;
     }
     // (always: the sums' warps may have given up on MMAs that go on)
-    if (issued && elect_one()) {
-      if (!ok) commit(bar(L::kAccFull));
-      drain(bar(L::kAccFull), 0u, a.guard.timeout_ns);
+    if (elect_one()) {
+      if (issued) commit(bar(L::kAccFull));
+      if (issued || sums > 0) drain(bar(L::kAccFull), static_cast<uint32_t>(issued ? sums : sums - 1) & 1u, a.guard.timeout_ns);
     }
     __syncwarp();
   } else {
     // The sums as [row][128 columns of y] into the stages' memory: every load has been read.
-    if (wait_all(L::kAccFull, 0, 136)) {
+    const uint32_t to = base + 4u * (32 * warp + lane);
+    if (kLong) {
+      const int sums = (last - first + kSumBlocks - 1) / kSumBlocks;
+      float v[128];
+#pragma unroll
+      for (int e = 0; e < 128; ++e) v[e] = 0.f;
+      int i = 0;
+#pragma unroll 1
+      for (; i < sums; ++i) {
+        if (!wait_all(L::kAccFull, i, 136)) break;
+        tc_fence_after();
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          if (16 * q >= n) break;
+          uint32_t r[16];
+          tmem_ld16(tmem + 16 * q + (static_cast<uint32_t>(warp) << 21), r);
+          tmem_wait_ld(r);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[16 * q + e] += __uint_as_float(r[e]);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(L::kAccEmpty));
+      }
+      if (i == sums) {
+#pragma unroll
+        for (int e = 0; e < 128; ++e)
+          if (e < n) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + 512u * e), "r"(__float_as_uint(v[e])) : "memory");
+      }
+    } else if (wait_all(L::kAccFull, 0, 136)) {
       tc_fence_after();
-      const uint32_t to = base + 4u * (32 * warp + lane);
 #pragma unroll 1
       for (int r = 0; r < n; r += 16) {
         uint32_t v[16];

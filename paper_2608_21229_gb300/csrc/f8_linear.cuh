@@ -5,7 +5,7 @@
 // stage is 128 columns of both (32 KB), four MMAs of K = 32.  The scales are applied
 // by the tensor core: those of 512 columns come as a load of their own (a word with
 // the bytes of four blocks for each row) and go into tensor memory by tcgen05.cp, issued before the
-// first MMA that needs them.  Sums stay in tensor memory from the first column to the last.
+// first MMA that needs them.  Sums stay in tensor memory from the first column to the last, of 16384 at most (kSumBlocks).
 //
 // What bounds it: the MMAs, 512 cycles for each 128 columns of x and 256 x 256 of y, of which a stage takes 570 to 600, and in long
 // calls the power cap (1.4 to 1.6 GHz); in short ones the last round of tiles.  With half of each
@@ -77,6 +77,14 @@ __device__ __forceinline__ LinearItem linear_item(const LinearArgs& a, int t) {
   return r;
 }
 
+// Blocks of 128 columns of x whose products are added up in tensor memory, where an addition cuts off what does not
+// fit: the error grows with the number of columns (of y's norm, where the products' signs vary / are all alike: 2.2e-7 / 1.4e-6 at 4096
+// columns, 1.2e-6 / 9.8e-6 at 16384, 7.4e-6 / 6.0e-5 at 65536).  Of wider rows (kLong) the sums so far go into registers and are added up
+// there, rounded to nearest, so that it grows no further (65536: 1.2e-6 / 9.8e-6; 4608 x 512 x 65536 takes 123.9 us, 123.1 without; 2 x
+// 24576 x 65536, few rows, 266, 256).  Every 4096 columns instead would cost three waits of some 1300 cycles in the 76000 of a tile of 16384.
+// An instance of its own: with the loop over sets in all of them the registers spill.
+constexpr int kSumBlocks = 128;
+
 // One row's block of 128 columns, in a thread as 64 pairs.  Of a block that the width cuts, the columns
 // behind its end (where `cols`, a multiple of 16, are there) are zero, as their weights are.
 __device__ __forceinline__ void load_block(uint32_t t, int cols, f32x2 (&v)[64]) {
@@ -88,6 +96,17 @@ __device__ __forceinline__ void load_block(uint32_t t, int cols, f32x2 (&v)[64])
     tmem_wait_ld(r);
 #pragma unroll
     for (int j = 0; j < 16; ++j) v[16 * i + j] = make_f32x2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+  }
+}
+__device__ __forceinline__ void add_block(uint32_t t, int cols, f32x2 (&v)[64]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (16 * i >= cols) break;
+    uint32_t r[16];
+    tmem_ld16(t + 16 * i, r);
+    tmem_wait_ld(r);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[8 * i + j] = add_f32x2(v[8 * i + j], make_f32x2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])));
   }
 }
 // The first n of 8 pieces of 16 bytes of a thread's row.  Each lane has a row of its own, and half a sector (32
@@ -243,7 +262,7 @@ __device__ __forceinline__ void finish_block(const Out& o, int64_t row, int col0
 // kernel: the other side then took 1.5 to 3.5 % more.
 constexpr int kLinesMost = 640;
 
-template <int kEpi>
+template <int kEpi, bool kLong>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads, 1)
     f8_linear_kernel(const __grid_constant__ LinearMaps maps, const __grid_constant__ LinearArgs a) {
   using L = LinearSmem;
@@ -251,7 +270,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
   Cta<L> c;
   if (!c.enter(smem_raw, a.guard)) return;
   const int cluster = static_cast<int>(blockIdx.x >> 1), n_clusters = static_cast<int>(gridDim.x >> 1);
-  const int n_items = a.n_items, blocks = (a.k + kBlock - 1) / kBlock;
+  const int n_items = a.n_items, blocks = (a.k + kBlock - 1) / kBlock, sums = kLong ? (blocks + kSumBlocks - 1) / kSumBlocks : 1;
   const bool wide = a.bn > 128;  // a whole tile takes both halves, and a piece the first
   auto bytes = [](int bn) { return make_uint2(L::kA, static_cast<uint32_t>(bn) * 64u); };  // of one CTA's load: x, w
   auto scale_bytes = [](int bn) { return make_uint2(512u, 512u * ((bn + 127) / 128)); };
@@ -287,13 +306,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
         st_shared_v4(bias + 16u * c.lane, make_uint4(__float_as_uint(b[0]), __float_as_uint(b[1]), __float_as_uint(b[2]), __float_as_uint(b[3])));
         __syncwarp();
       }
-      if (!c.wait_all(L::kAccFull + half, wide ? used : used >> 1, 106)) break;
-      tc_fence_after();
+      const int before = (wide ? used : used >> 1) * sums;
+      const uint32_t from = c.tmem + 128u * half + (static_cast<uint32_t>(quarter) << 21);
       f32x2 v[64];
-      load_block(c.tmem + 128u * half + (static_cast<uint32_t>(quarter) << 21), in_tile, v);
-      tc_fence_before();
-      __syncwarp();
-      if (c.lane == 0) mbar_arrive_cluster(c.lbar(L::kAccEmpty + half));
+      int n = 0;
+#pragma unroll 1
+      for (; n < sums; ++n) {
+        if (!c.wait_all(L::kAccFull + half, before + n, 106)) break;
+        tc_fence_after();
+        if (n == 0)
+          load_block(from, in_tile, v);
+        else
+          add_block(from, in_tile, v);
+        tc_fence_before();
+        __syncwarp();
+        if (c.lane == 0) mbar_arrive_cluster(c.lbar(L::kAccEmpty + half));
+      }
+      if (n < sums) break;
       // (all lanes of a warp whose first row is there, where they store together)
       if (kEpi == kStoreLines ? row - c.lane < a.o.rows && cols > 0 : in) finish_block<kEpi>(a.o, row, col0, cols, v, bias, u, u_scale);
     }
@@ -352,10 +381,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
           const uint32_t d = c.tmem + 128u * first, idesc = idesc_mx(256, item.bn);
           const uint32_t shift = static_cast<uint32_t>(item.col0 % kBlock) / 32u;  // it may begin in the middle of a chunk
           // the half's (both halves') earlier sums are in registers
-          const int before = wide ? used : used >> 1;
-          if (before > 0 && !(c.wait_all(L::kAccEmpty + first, before - 1, 103) && (!both || c.wait_all(L::kAccEmpty + 1, before - 1, 103)))) break;
+          int before = (wide ? used : used >> 1) * sums;
 #pragma unroll 1
           for (int kb = 0; kb < blocks; ++kb, ++load) {
+            const int in_sum = kLong ? kb % kSumBlocks : kb;
+            if (in_sum == 0) {
+              ok = before == 0 || (c.wait_all(L::kAccEmpty + first, before - 1, 103) && (!both || c.wait_all(L::kAccEmpty + 1, before - 1, 103)));
+              if (!ok) break;
+              ++before;
+            }
             const int s = load % L::kSlots, sc = group % L::kSlots2;
             const uint32_t sfa = c.tmem + L::kTmemScales + 16u * sc, sfb = sfa + 4;
             if ((kb & 3) == 0) {
@@ -366,7 +400,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
             if (!ok) break;
             issued = true;
             const int steps = min(4, (a.k - kb * kBlock + 31) / 32);
-            const bool last = kb + 1 == blocks;
+            const bool last = kb + 1 == blocks, out = last || (kLong && in_sum == kSumBlocks - 1);
             if (elect_one()) {
               tc_fence_after();
               if ((kb & 3) == 0) {
@@ -379,10 +413,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LinearSmem::kThreads
               const uint32_t id = idesc_byte(idesc, kb & 3);
 #pragma unroll
               for (int q = 0; q < 4; ++q)
-                if (q < steps) mx_mma_pair(d, ad + off + 2 * q, bd + off + 2 * q, id, sfa, sfb + shift, kb > 0 || q > 0 ? 1u : 0u);
+                if (q < steps) mx_mma_pair(d, ad + off + 2 * q, bd + off + 2 * q, id, sfa, sfb + shift, in_sum > 0 || q > 0 ? 1u : 0u);
               tc2_commit_mc(c.bar(L::kEmpty + s), 3);
               if ((kb & 3) == 3 || last) tc2_commit_mc(c.bar(L::kEmpty2 + sc), 3);
-              if (last) {
+              if (out) {
                 tc2_commit_mc(c.bar(L::kAccFull + first), 3);
                 if (both) tc2_commit_mc(c.bar(L::kAccFull + 1), 3);
               }

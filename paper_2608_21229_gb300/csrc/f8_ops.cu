@@ -190,12 +190,12 @@ int tiles_map(CUtensorMap* m, const rc::f8::Rows& r) {
   return rc_host::encode_lines(m, r.tiles, static_cast<int64_t>(r.pitch / 4) * r.chunks);
 }
 
-template <int kEpi>
+template <int kEpi, bool kLong>
 int launch_few(const LinearPlan& p, const rc::f8::Rows& x, const rc::f8::Rows& w, const rc::f8::Out& o, int* status, int dev, void* stream) {
   using L = rc::f8::FewSmem;
   static std::atomic<bool> set[rc_host::kMaxDevices];
   if (!set[dev].load()) {
-    const cudaError_t e = cudaFuncSetAttribute(rc::f8::f8_few_kernel<kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynamic);
+    const cudaError_t e = cudaFuncSetAttribute(rc::f8::f8_few_kernel<kEpi, kLong>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kDynamic);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(f8_few_kernel)");
     set[dev].store(true);
   }
@@ -227,13 +227,13 @@ int launch_few(const LinearPlan& p, const rc::f8::Rows& x, const rc::f8::Rows& w
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  cudaError_t e = cudaLaunchKernelEx(&cfg, rc::f8::f8_few_kernel<kEpi>, maps, a);
+  cudaError_t e = cudaLaunchKernelEx(&cfg, rc::f8::f8_few_kernel<kEpi, kLong>, maps, a);
   if (e == cudaSuccess) e = cudaGetLastError();
   return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "f8_few_kernel launch");
 }
 
-template <int kEpi>
-int launch_linear(const rc::f8::Rows& x, const rc::f8::Rows& w, const rc::f8::Out& o, void* stream) {
+template <int kEpi, bool kLong>
+int launch_linear_of(const rc::f8::Rows& x, const rc::f8::Rows& w, const rc::f8::Out& o, void* stream) {
   using L = rc::f8::LinearSmem;
   if (o.rows == 0) return REFCACHE_OK;
   static std::atomic<int> kept[rc_host::kMaxDevices];
@@ -241,10 +241,12 @@ int launch_linear(const rc::f8::Rows& x, const rc::f8::Rows& w, const rc::f8::Ou
   rc::f8::LinearArgs a{};
   int rc = device_sms(&sms);
   if (rc || (rc = rc_host::device_status_word(&dev, &a.guard.status)) != 0 ||
-      (rc = pairs_of(rc::f8::f8_linear_kernel<kEpi>, kept[dev], L::kThreads, L::kDynamic, sms, &pairs)) != 0)
+      (rc = pairs_of(rc::f8::f8_linear_kernel<kEpi, kLong>, kept[dev], L::kThreads, L::kDynamic, sms, &pairs)) != 0)
     return rc;
   const LinearPlan p = plan_linear(o.rows, o.width, x.width, pairs, sms, kEpi < rc::f8::kGelu ? 64 : 128);
-  if (p.few) return launch_few<kEpi == rc::f8::kStoreLines ? rc::f8::kStore : kEpi>(p, x, w, o, a.guard.status, dev, stream);
+  constexpr int kFew = kEpi == rc::f8::kStoreLines ? rc::f8::kStore : kEpi;
+  if (p.few && kLong && p.per > rc::f8::kSumBlocks) return launch_few<kFew, kLong>(p, x, w, o, a.guard.status, dev, stream);
+  if (p.few) return launch_few<kFew, false>(p, x, w, o, a.guard.status, dev, stream);
   a.o = o;
   a.x_chunks = x.chunks, a.w_chunks = w.chunks;
   a.k = x.width;
@@ -263,9 +265,17 @@ int launch_linear(const rc::f8::Rows& x, const rc::f8::Rows& w, const rc::f8::Ou
     return rc;
   a.guard.stop = rc_host::take_debug_stop();
   const unsigned clusters = static_cast<unsigned>(std::min<int64_t>(p.items, pairs));
-  const cudaError_t e = launch_dependent(rc::f8::f8_linear_kernel<kEpi>, dim3(2 * clusters), dim3(L::kThreads), L::kDynamic,
+  const cudaError_t e = launch_dependent(rc::f8::f8_linear_kernel<kEpi, kLong>, dim3(2 * clusters), dim3(L::kThreads), L::kDynamic,
                                          static_cast<cudaStream_t>(stream), maps, a);
   return e == cudaSuccess ? REFCACHE_OK : cuda_fail(e, "f8_linear_kernel launch");
+}
+
+template <int kEpi>
+int launch_linear(const rc::f8::Rows& x, const rc::f8::Rows& w, const rc::f8::Out& o, void* stream) {
+  static_assert(kEpi != rc::f8::kStoreLines || rc::f8::kLinesMost <= rc::f8::kBlock * rc::f8::kSumBlocks, "lines of long rows");
+  if (kEpi != rc::f8::kStoreLines && x.width > rc::f8::kBlock * rc::f8::kSumBlocks)
+    return launch_linear_of<kEpi == rc::f8::kStoreLines ? rc::f8::kStore : kEpi, true>(x, w, o, stream);
+  return launch_linear_of<kEpi, false>(x, w, o, stream);
 }
 
 // How a weight gradient is taken apart.

@@ -14,7 +14,7 @@ def test_tensor_memory_is_freed_behind_every_mma_that_was_issued():
     itself, whether or not its own waits were fulfilled, before tensor memory is freed."""
     few = _code("f8_few.cuh")
     loop, freed = few.index("mx_mma(tmem"), few.index("tcgen05.dealloc")
-    own = few.index("if (issued && elect_one()) { if (!ok) commit(bar(L::kAccFull)); drain(bar(L::kAccFull)")
+    own = few.index("if (elect_one()) { if (issued) commit(bar(L::kAccFull)); if (issued || sums > 0) drain(bar(L::kAccFull), static_cast<uint32_t>(issued ? sums : sums - 1) & 1u")
     assert loop < own < freed
     pair = _code("f8_pair.cuh")
     finish = pair[pair.index("void finish_mmas("):]
