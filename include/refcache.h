@@ -552,7 +552,7 @@ REFCACHE_API int refcache_clip_gradients(int n, const void* const* grads, void* 
  *     last one too.  What else belongs to no row or block may hold anything, before and after a call.
  *   - Products are summed in fp32 by the tensor cores, whose additions cut off what does not fit: y is off by up to 3e-7 of its norm at
  *     4096 columns of x and 1.5e-6 from 16384 on where the products' signs vary, by 2e-6 and 1.2e-5 (toward zero) where they are all alike, dw
- *     by up to 1e-6 with any number of rows.  Results are rounded once; a code or a scale next to a border may be its neighbour.
+ *     by up to 1e-6 at 20608 rows.  Results are rounded once; a code or a scale next to a border may be its neighbour.
  *   - bf16 tensors of rows may have ld elements between rows (a multiple of 8).
  *   - Outputs, and weight_grad's work, that overlap inputs or each other are refused (but for dw over add; of
  *     rows that lie apart only the first one is looked at).

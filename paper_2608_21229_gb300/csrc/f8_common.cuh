@@ -91,7 +91,7 @@ __device__ __forceinline__ f32x2 abs2(f32x2 x) { return f32x2{x.v & 0x7FFFFFFF7F
 
 // The normal distribution's tail Q(x), x >= 0, from e = exp(-x^2 / 2): e t R(t) with t =
 // 1 / (1 + 0.3 x).  R by a weighted least-squares fit of Q(x) exp(x^2 / 2) / t over Chebyshev nodes of t up
-// to x = 13.5 (relative error 1.3e-7, to which the exponent's rounding adds 2^-23 x^2).  1 - erf and
+// to x = 13.5 (relative error 1.5e-7, 1.8e-7 with 0.3 in fp32; the exponent's rounding adds 2^-23 x^2).  1 - erf and
 // 1 - tanh lose their relative precision far below zero, where a block of nothing but such
 // values has a scale of its own.
 __device__ __forceinline__ f32x2 normal_tail(f32x2 x, f32x2 e) {

@@ -7,11 +7,13 @@
 // the bytes of four blocks for each row) and go into tensor memory by tcgen05.cp, issued before the
 // first MMA that needs them.  Sums stay in tensor memory from the first column to the last, of 16384 at most (kSumBlocks).
 //
-// What bounds it: the MMAs, 512 cycles for each 128 columns of x and 256 x 256 of y, of which a stage takes 570 to 600, and in long
-// calls the power cap (1.4 to 1.6 GHz); in short ones the last round of tiles.  With half of each
-// stage's MMAs left out a stage still took 584, with half of its loads 581, with both 501: loads and MMAs share the
-// shared memory's 128 bytes a cycle (32 KB written and read in 512).  1280 x 12288 x 4096: 42.9 us, 3.0 PFLOP/s (0.79 of twice the
-// measured bf16 rate); 20608 x 4096 x 12288: 638 us, 3.25 PFLOP/s (0.86).  The GELU (1792 x 8192 x 2048: 30 us) is bound by its sums' warps: 13800
+// What bounds it: a stage of 128 columns of x and 256 x 256 of y takes 570 to 600 cycles, of which 512 are MMAs; in long
+// calls the power cap (1.4 to 1.6 GHz); in short ones the last round of tiles.  Two sides of a stage take about as long.  With half
+// of its MMAs left out it still took 584: its loads alone, 32 KB a CTA at 56 bytes a cycle.  With half of its loads 581: the MMAs
+// with the scales' copies and their ring (the weight gradient, which has no scales, came to 529).  With half of both 501, so that each
+// side has a part that does not shrink with its work.  1280 x 12288 x 4096: 42.9 to 48.3 us on different GPUs, 2.7 to 3.0 PFLOP/s (0.71 to 0.79 of
+// twice the measured bf16 rate); 20608 x 4096 x 12288: 638 to 684 us, 3.0 to 3.25 PFLOP/s (0.80 to 0.86); 4608 rows, 4096 -> 16384 with
+// the GELU's two forms: 215 us (tanh), 227 (erf).  The GELU (1792 x 8192 x 2048: 30 us) is bound by its sums' warps: 13800
 // cycles a tile for two 8-bit forms and the GELU of 256 x 256, where the MMAs of 2048 columns take 9100: two warps a sub-partition, whose
 // registers leave the latencies of one pair of columns to few others (pairs two, four or eight at a time, step by step, took as long).
 //

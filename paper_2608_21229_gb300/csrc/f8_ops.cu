@@ -155,8 +155,8 @@ struct LinearPlan {
 //   64 x 4096 x 16384     37.7    60.1 / 33.6 / 25.7 / 21.1 / 18.1
 //   200 x 2048 x 8192     20.7    35.8 / 22.3 / 19.1 / 16.0 / 14.9
 //   300 x 4096 x 4096     13.2    22.2 / 18.7 / 16.6 / 22.3 / 31.0
-// Pairs: rounds of tiles; a block of 128 columns of x takes a pair 2 bn cycles of MMAs, or (256 + bn) to bring
-// its 16 KB + 64 bn bytes into each CTA's shared memory and read them out at 128 bytes a cycle; a weight of which
+// Pairs: rounds of tiles; a block of 128 columns of x takes a pair 2 bn cycles of MMAs, or (256 + bn) for its
+// loads, 16 KB + 64 bn bytes to each CTA (a fit: in long rows a stage takes more of both, f8_linear.cuh); a weight of which
 // every tile is read once comes at 1800 bytes a cycle.  Few: the weight at 3300 bytes a cycle, all that the CTAs load at
 // 5500, and a CTA's own loads at 24.
 LinearPlan plan_linear(int64_t rows, int width, int k, int pairs, int sms, int step) {

@@ -18,8 +18,9 @@
 // eight warps (4e-7), which write a tile while the MMAs of the next one run.  Where the tiles
 // are few the rows are split and the parts added by another kernel in a fixed order.
 //
-// What bounds it: the MMAs, of whose 512 cycles a stage makes 592 (588 with half of the MMAs left out, 529 with half of the
-// loads, 444 with half of both), and the power cap.  4608 rows, 16384 x 4096: 365 us, 1.69 PFLOP/s (0.90 of measured).
+// What bounds it: a stage's loads, 592 cycles for 512 of MMAs (588 with half of the MMAs left out: the loads alone; 529 with half of the
+// loads; 444 with half of both: each side has a part that does not shrink with its work), and the power cap.  4608 rows, 16384 x 4096: 350
+// to 391 us on different GPUs, 1.58 to 1.77 PFLOP/s (0.84 to 0.93 of measured).
 #pragma once
 #include "f8_pair.cuh"
 #include "vec8.cuh"
